@@ -56,6 +56,7 @@ enum {
 #define ORDERMOE_MAX_EXPERTS 64
 #define ORDERMOE_MAX_SERVERS 32
 #define ORDERMOE_MAX_TOPK 8
+#define ORDERMOE_FEW_TOKENS 16 /* tokens of an ordermoe_layer_few call, at most */
 
 /* Message for the last error returned on this host thread. */
 const char* ordermoe_last_error(void);
@@ -331,6 +332,58 @@ int ordermoe_layer_forward_residual(const ordermoe_layer_desc* layer, int T, con
                                     const uint16_t* h, const uint8_t* home, uint8_t* loc,
                                     float* qhat, float eps, uint16_t* h_out, uint16_t* x_out,
                                     float* logits_out, int32_t* counters, ordermoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * One whole MoE layer for a few tokens (a decoding batch of 1 to 16) in one
+ * launch: what ordermoe_layer_forward and ordermoe_layer_forward_residual
+ * compute, for calls whose time is one pass over the chosen experts' weights
+ * and the latency of the launches. Differences: an expert's output is not
+ * rounded to bf16 before the weighted sum,
+ *   y[t] = bf16( sum_j topk_w[t][j] W2_e H_j ),  H_j = bf16( silu(W1_e x) * (W3_e x) ),
+ * (fp32 sums in a fixed order, expert after expert, so the same call gives the
+ * same bits), and the router logits are summed in another order: decisions are
+ * those of ordermoe_route_select from the logits that `out` returns.
+ *   layer      the descriptor of ordermoe_layer_forward; T_max and scratch are not
+ *              read. lookahead_H > 1: ordermoe_route_select_lookahead's launches
+ *              decide first.
+ *   T          0 <= T <= 16 (more: ORDERMOE_ERR_UNSUPPORTED_SHAPE)
+ *   X, home, loc, qhat, y   device pointers, as ordermoe_layer_forward
+ *   x, h, eps, h_out, x_out as ordermoe_layer_forward_residual
+ *   out        host, nullable, and each of its device pointers nullable
+ *   workspace  device scratch of ordermoe_layer_few_workspace_bytes(T, E, d, dff,
+ *              k) bytes (enough for every smaller T), 256-byte aligned, prepared
+ *              once by ordermoe_layer_few_init. Calls that may overlap on the GPU
+ *              need one each; calls in one stream, and graphs replayed one after
+ *              the other, may share one. After ORDERMOE_DEV_WAIT_TIMEOUT prepare
+ *              it again.
+ * Weights that a token does not use do not reach its output, whatever they hold. A token
+ * whose decisions fail (a NaN logit, a bad home or location) is reported as by
+ * ordermoe_route_select; its rows of y, h_out and x_out, loc and qhat are left
+ * unwritten, the other tokens are computed.
+ * The launch is cooperative, one CTA per SM: it starts when that many fit beside what
+ * runs, and can be captured into a graph.
+ * Shapes: d % 256 == 0, dff % 128 == 0, 1 <= k <= min(E, 8), E <= 64. */
+typedef struct {
+  float* logits;          /* [T][E] router logits                              */
+  int32_t* topk_idx;      /* [T][k] and on: as ordermoe_route_select's outputs */
+  float* topk_w;
+  int32_t* chosen_expert;
+  uint8_t* chosen_server;
+  uint8_t* kind;
+  int32_t* counters;      /* [4] += slots of each kind                         */
+} ordermoe_few_out;
+
+size_t ordermoe_layer_few_workspace_bytes(int T, int E, int d, int dff, int k);
+int ordermoe_layer_few_init(void* workspace, size_t workspace_bytes, ordermoe_stream_t stream);
+int ordermoe_layer_few(const ordermoe_layer_desc* layer, int T, const uint16_t* X,
+                       const uint8_t* home, uint8_t* loc, float* qhat, uint16_t* y,
+                       const ordermoe_few_out* out, void* workspace, size_t workspace_bytes,
+                       ordermoe_stream_t stream);
+int ordermoe_layer_few_residual(const ordermoe_layer_desc* layer, int T, const uint16_t* x,
+                                const uint16_t* h, const uint8_t* home, uint8_t* loc, float* qhat,
+                                float eps, uint16_t* h_out, uint16_t* x_out,
+                                const ordermoe_few_out* out, void* workspace,
+                                size_t workspace_bytes, ordermoe_stream_t stream);
 
 /* nbatch independent batches of T tokens through one layer, from and to
  * pinned HOST memory, each batch as ordermoe_layer_forward with host_io = 1

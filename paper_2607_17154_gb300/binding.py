@@ -68,8 +68,14 @@ _SIGNATURES = {
     "ordermoe_rmsnorm": ([_P, _I, _I, _F, _P, _P], _I),
     "ordermoe_combine_residual_norm": ([_P, _P, _P, _P, _I, _I, _I, _F, _P, _P, _P], _I),
     "ordermoe_layer_forward_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P], _I),
+    "ordermoe_layer_few_workspace_bytes": ([_I, _I, _I, _I, _I], _SZ),
+    "ordermoe_layer_few_init": ([_P, _SZ, _P], _I),
+    "ordermoe_layer_few": ([_P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
+    "ordermoe_layer_few_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _SZ, _P], _I),
     "ordermoe_transitions_strided": ([_P, _I64, _I, _I, _I, _I64, _I64, _P, _P, _P], _I),
 }
+
+FEW_TOKENS = 16  # tokens of an ordermoe_layer_few call, at most
 
 # RMSNorm epsilon of the residual map between stacked layers
 NORM_EPS = 1e-6
@@ -81,6 +87,12 @@ class LayerDesc(ctypes.Structure):
                 ("W_r", _P), ("W1", _P), ("W3", _P), ("W2", _P), ("tables", _P),
                 ("tables_bytes", _SZ), ("scratch", _P), ("scratch_bytes", _SZ),
                 ("lookahead_H", _I), ("tables_stride", _SZ), ("P", _P)]
+
+
+class FewOut(ctypes.Structure):
+    """Mirror of ordermoe_few_out."""
+    _fields_ = [(n, _P) for n in ("logits", "topk_idx", "topk_w", "chosen_expert", "chosen_server",
+                                  "kind", "counters")]
 
 
 class OrderMoEError(RuntimeError):
@@ -444,6 +456,79 @@ def ordermoe_layer_forward_residual(desc, T, x, h, home, loc, qhat, eps, h_out, 
                                                _ptr(x_out), _ptr(logits_out), _ptr(counters),
                                                _stream(stream))
     _check("ordermoe_layer_forward_residual", rc)
+
+
+def _here(*tensors):
+    """The tensors' device must be the current one, where the launch goes."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != dev:
+            raise ValueError("tensor on cuda:%d, but the current device is cuda:%d"
+                             % (t.device.index, dev))
+
+
+def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):
+    return int(lib().ordermoe_layer_few_workspace_bytes(T, E, d, dff, k))
+
+
+def ordermoe_layer_few_init(workspace, stream=None):
+    _here(workspace)
+    _check("ordermoe_layer_few_init", lib().ordermoe_layer_few_init(
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def make_few_out(logits=None, topk_idx=None, topk_w=None, chosen_expert=None, chosen_server=None,
+                 kind=None, counters=None):
+    """The decisions that ordermoe_layer_few is to return (device tensors or None)."""
+    _dt(logits, torch.float32, "logits"); _dt(topk_idx, torch.int32, "topk_idx")
+    _dt(topk_w, torch.float32, "topk_w"); _dt(chosen_expert, torch.int32, "chosen_expert")
+    _dt(chosen_server, torch.uint8, "chosen_server"); _dt(kind, torch.uint8, "kind")
+    _dt(counters, torch.int32, "counters")
+    ts = (logits, topk_idx, topk_w, chosen_expert, chosen_server, kind, counters)
+    out = FewOut(*(_ptr(t) for t in ts))
+    out._keep = ts
+    return out
+
+
+def _few_check(desc, T, rows, home, loc, qhat, out, workspace):
+    """Types, sizes and devices of a few-token call: rows [T, d] and on."""
+    for n, t in rows:
+        _dt(t, torch.bfloat16, n)
+        if t.numel() < T * desc.d:
+            raise ValueError("%s has fewer than T rows of d" % n)
+    _dt(home, torch.uint8, "home"); _dt(loc, torch.uint8, "loc"); _dt(qhat, torch.float32, "qhat")
+    for n, t, w in (("home", home, 1), ("loc", loc, 1), ("qhat", qhat, 1)):
+        if t is not None and t.numel() < T * w:
+            raise ValueError("%s has fewer than T entries" % n)
+    if out is not None:
+        for (n, _), t, w in zip(FewOut._fields_, out._keep, (desc.E,) + (desc.k,) * 5 + (0,)):
+            if t is not None and t.numel() < max(T * w, 0 if w else 4):
+                raise ValueError("%s is too small" % n)
+    _here(*(t for _, t in rows), home, loc, qhat, workspace, *(out._keep if out is not None else ()))
+
+
+def ordermoe_layer_few(desc, T, X, home, loc, qhat, y, workspace, out=None, stream=None):
+    """A whole MoE layer for T <= FEW_TOKENS tokens in one launch (out: make_few_out)."""
+    _few_check(desc, T, (("X", X), ("y", y)), home, loc, qhat, out, workspace)
+    rc = lib().ordermoe_layer_few(ctypes.byref(desc), T, _ptr(X), _ptr(home), _ptr(loc), _ptr(qhat),
+                                  _ptr(y), None if out is None else ctypes.byref(out),
+                                  _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                  _stream(stream))
+    _check("ordermoe_layer_few", rc)
+
+
+def ordermoe_layer_few_residual(desc, T, x, h, home, loc, qhat, eps, h_out, x_out, workspace,
+                                out=None, stream=None):
+    """ordermoe_layer_few on the residual map: h_out = h + y, x_out = RMSNorm(h_out)."""
+    _few_check(desc, T, (("x", x), ("h", h), ("h_out", h_out), ("x_out", x_out)), home, loc, qhat, out,
+               workspace)
+    rc = lib().ordermoe_layer_few_residual(ctypes.byref(desc), T, _ptr(x), _ptr(h), _ptr(home),
+                                           _ptr(loc), _ptr(qhat), float(eps), _ptr(h_out),
+                                           _ptr(x_out), None if out is None else ctypes.byref(out),
+                                           _ptr(workspace),
+                                           workspace.numel() * workspace.element_size(),
+                                           _stream(stream))
+    _check("ordermoe_layer_few_residual", rc)
 
 
 def ordermoe_layer_batches_scratch_bytes(T_max, E, d, dff, k):

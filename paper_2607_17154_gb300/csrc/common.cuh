@@ -23,6 +23,10 @@ int num_sms();                                     // SM count of the current de
 // rows, 128-byte swizzle, zero fill out of bounds.
 int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
                    uint32_t box_rows);
+// The same tensor as [cols / 64][rows][64] (cols % 64 == 0): a box of box_kb blocks of 64
+// columns x box_rows rows, block after block.
+int make_tmap_bf16_kb(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
+                      uint32_t box_kb);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

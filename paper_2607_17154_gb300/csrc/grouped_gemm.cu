@@ -809,6 +809,21 @@ int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t c
   return ORDERMOE_OK;
 }
 
+int make_tmap_bf16_kb(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
+                      uint32_t box_kb) {
+  gg::EncodeTiledFn enc = gg::encode_fn();
+  if (!enc) return fail(ORDERMOE_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  cuuint64_t dims[3] = {gg::BK, rows, cols / gg::BK};
+  cuuint64_t strides[2] = {cols * 2, gg::BK * 2};
+  cuuint32_t box[3] = {gg::BK, box_rows, box_kb};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+                   box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(ORDERMOE_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  return ORDERMOE_OK;
+}
+
 template <int MODE, bool PAIR>
 static cudaError_t ffn_attr() {
   return cudaFuncSetAttribute(gg::ffn_gemm_kernel<MODE, PAIR>,

@@ -8,7 +8,8 @@ from . import binding as B
 class MoELayer:
     """Holds a layer's weights, tables and scratch for up to T_max tokens."""
 
-    def __init__(self, W_r, W1, W3, W2, tables, k, T_max, renorm=1, device=None):
+    def __init__(self, W_r, W1, W3, W2, tables, k, T_max, renorm=1, device=None, few=False):
+        """few: also keep the workspace of forward_few (calls of up to B.FEW_TOKENS tokens)."""
         self.device = device or W1.device
         self.W_r, self.W1, self.W3, self.W2 = W_r, W1, W3, W2
         self.E, self.dff, self.d = W1.shape
@@ -31,6 +32,12 @@ class MoELayer:
         self.Y_perm = torch.empty(R, self.d, dtype=torch.bfloat16, device=dev)
         ws = B.ordermoe_dispatch_workspace_bytes(T_max, k, self.E)
         self.ws = torch.empty(ws, dtype=torch.uint8, device=dev)
+        self.few_ws = None
+        if few:
+            self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), self.E, self.d, self.dff, k, dev)
+            self.few_desc = B.make_layer_desc(T_max, W_r, W1, W3, W2, tables, k, self.ws, renorm)
+            self.few_out = B.make_few_out(self.logits, self.topk_idx, self.topk_w, self.chosen,
+                                          self.server, self.kind, self.counters)
 
     def forward(self, X, home, loc, qhat, y, T=None, logits_in=None, stream=None):
         """y[:T] = MoE(X[:T]); loc/qhat are updated in place (Eq. 44)."""
@@ -70,6 +77,34 @@ class MoELayer:
         return h_out, x_out
 
 
+    def forward_few(self, X, home, loc, qhat, y, T=None, stream=None):
+        """forward() of at most B.FEW_TOKENS tokens in one launch: the decisions in the same
+        buffers, the combine's sum without the experts' bf16 rounding."""
+        T = X.shape[0] if T is None else T
+        assert T <= self.T_max and self.few_ws is not None
+        B.ordermoe_layer_few(self.few_desc, T, X, home, loc, qhat, y, self.few_ws, self.few_out,
+                             stream)
+        return y
+
+    def forward_few_residual(self, x, h, home, loc, qhat, h_out, x_out, T=None, eps=B.NORM_EPS,
+                             stream=None):
+        """forward_residual() of at most B.FEW_TOKENS tokens in one launch."""
+        T = x.shape[0] if T is None else T
+        assert T <= self.T_max and self.few_ws is not None
+        B.ordermoe_layer_few_residual(self.few_desc, T, x, h, home, loc, qhat, eps, h_out, x_out,
+                                      self.few_ws, self.few_out, stream)
+        return h_out, x_out
+
+
+def few_workspace(T, E, d, dff, k, device):
+    """The workspace of ordermoe_layer_few calls of up to T tokens, prepared."""
+    ws = torch.empty(B.ordermoe_layer_few_workspace_bytes(T, E, d, dff, k), dtype=torch.uint8,
+                     device=device)
+    with torch.cuda.device(device):
+        B.ordermoe_layer_few_init(ws)
+    return ws
+
+
 def build_tables(sim, group, placement, theta, qbar, sp, device, out=None):
     """Device tables for one layer from host arrays (sim, group, placement) and
     server parameters sp (synth.ServerParams); written into `out` (a uint8
@@ -88,7 +123,7 @@ class LayerStack:
     """L MoE layers run through ordermoe_layer_forward with the token state
     (location, accumulated loss; Eqs. 36 and 44) carried from layer to layer."""
 
-    def __init__(self, layers, tables, k, T_max, device, H=1, stride=0, P=None):
+    def __init__(self, layers, tables, k, T_max, device, H=1, stride=0, P=None, few=False):
         """layers: dicts with W_r, W1, W3, W2 (device bf16). tables: a list of
         per-layer device buffers, or (for look-ahead, H > 1) one device buffer
         holding all layers' tables `stride` bytes apart; P [L-1, E, E] the
@@ -109,12 +144,20 @@ class LayerStack:
                                                 t, k, self.scratch, lookahead_H=Hl,
                                                 tables_stride=stride, P=Pl))
         self.d, self.T_max = d, T_max
+        self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), E, d, dff, k, device) if few else None
+
+    def _few(self, T):
+        return self.few_ws is not None and T <= B.FEW_TOKENS
 
     def step(self, X_layers, home, loc, qhat, y_layers, counters=None, stream=None):
         """Layer l reads X_layers[l] and writes y_layers[l]; loc/qhat carry the
         trajectory (set loc = home, qhat = 0 before the first layer)."""
         T = X_layers[0].shape[0]
+        out = B.make_few_out(counters=counters) if self._few(T) and counters is not None else None
         for desc, X, y in zip(self.descs, X_layers, y_layers):
+            if self._few(T):
+                B.ordermoe_layer_few(desc, T, X, home, loc, qhat, y, self.few_ws, out, stream)
+                continue
             B.ordermoe_layer_forward(desc, T, X, home, loc, qhat, y, counters, 0, stream)
 
     def step_residual(self, hs, xs, home, loc, qhat, counters=None, logits=None,
@@ -127,6 +170,11 @@ class LayerStack:
         T = hs[0].shape[0]
         B.ordermoe_rmsnorm(hs[0], T, self.d, eps, xs[0], stream)
         for l, desc in enumerate(self.descs):
+            if self._few(T):
+                out = B.make_few_out(logits=None if logits is None else logits[l], counters=counters)
+                B.ordermoe_layer_few_residual(desc, T, xs[l], hs[l], home, loc, qhat, eps, hs[l + 1],
+                                              xs[l + 1], self.few_ws, out, stream)
+                continue
             B.ordermoe_layer_forward_residual(desc, T, xs[l], hs[l], home, loc, qhat, eps,
                                               hs[l + 1], xs[l + 1],
                                               None if logits is None else logits[l], counters,
