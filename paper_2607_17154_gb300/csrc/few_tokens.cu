@@ -8,8 +8,8 @@
 // the columns of B; a token's column of an expert it does not use is dropped).
 // What a chain of launches costs beside that pass is their latency and the pauses
 // of HBM between them, so one cooperative kernel of a CTA per SM runs it all:
-//   route    every CTA computes all logits X W_r^T and takes the same decisions
-//            (the router is small, and a grid barrier would take longer);
+//   route    every pair of CTAs computes all logits X W_r^T, half of K each, and both take
+//            the same decisions (the router is small; a grid barrier would take longer);
 //   gate/up  units of 8 MT columns of W1 and W3 of one expert over the whole K = d,
 //            dealt out to the CTAs in turn: gate in rows 0-7 of a 16-row MMA tile
 //            and up in rows 8-15, so that SwiGLU is in one lane's registers;
@@ -24,6 +24,7 @@
 // epilogue warp adds their eight partial accumulators. Between gate/up and down
 // the producer fills the ring with W2 while the other CTAs finish H: the grid
 // barrier there costs HBM no pause.
+#include <cstddef>
 #include <type_traits>
 
 #include "select.cuh"
@@ -52,7 +53,8 @@ struct Cfg {
   static constexpr int STAGE_BYTES = W_BYTES + 4096 * NT;  // and 8 NT tokens x 256
   static constexpr int DOWN_ROWS = 32 * MT;
   // partial accumulators of the MMA warps: two sets of a unit's, or one of a row tile's
-  static constexpr int RED_FLOATS = MMA_WARPS * MT * NT * 128 * 2;
+  // (the router has up to four tiles, once)
+  static constexpr int RED_FLOATS = MMA_WARPS * (MT == 1 ? 4 : 2 * MT) * NT * 128;
   // shared memory beside the ring: alignment, partials, the selection's Q and Cq
   static constexpr int other_bytes(int E) { return 1024 + RED_FLOATS * 4 + ((8 * E * E + 15) & ~15); }
 };
@@ -63,11 +65,12 @@ struct Smem {
   uint64_t red_full[3], red_empty[3];  // a unit's two sets; [2]: a row tile's
   int abort, zero;
   int n_act;                       // chosen experts
-  uint16_t mask[64];               // of the i-th chosen expert: the tokens that use it
-  uint8_t act[64];                 // its index
+  uint8_t act[64];                 // their indices, ascending
+  unsigned int mask[64];           // of an expert: the tokens that use it
   float gate[64][TOKENS];          // and their gate weights
-  float logits[TOKENS][68];        // -inf past E
-  float ex[TOKENS][68];            // exponentials of the softmax
+  float logits[2][TOKENS][68];     // shares of K of either CTA; [0] is -inf past E
+  alignas(16) float ex[TOKENS][68];  // exponentials of the softmax, read 16 bytes at a time
+  float delay[TOKENS][ORDERMOE_MAX_SERVERS];  // A[home][location] of the tokens
   int32_t target[TOKENS * ORDERMOE_MAX_TOPK];
   float weight[TOKENS * ORDERMOE_MAX_TOPK];
   int32_t chosen[TOKENS * ORDERMOE_MAX_TOPK];
@@ -77,6 +80,7 @@ struct Smem {
   int valid[TOKENS];               // decided: its outputs are written
   float sum[THREADS / 32];
 };
+static_assert(offsetof(Smem, ex) % 16 == 0 && alignof(Smem) == 16, "16-byte loads");
 // A ring takes what the layer's tables leave of the 227 KB.
 template <int MT, int NT>
 constexpr int stages(int E) {
@@ -87,7 +91,7 @@ constexpr int stages(int E) {
 static_assert(stages<1, 1>(64) >= 12 && stages<2, 1>(64) >= 6 && stages<2, 2>(64) >= 5, "ring");
 
 struct Maps {
-  CUtensorMap Wr, X, W1, W3, W2, H;
+  CUtensorMap Wr, Xr, X, W1, W3, W2, H;
 };
 
 struct Args {
@@ -186,40 +190,56 @@ __device__ __forceinline__ void mma_stage(float (&acc)[TILES][NT][4], uint32_t w
   }
 }
 
-// Top-k, softmax and Alg. 2 of the four tokens of warp `warp`, eight lanes each, from
-// s.logits; the arithmetic of the router kernels, so the same logits give the
-// same bits. Decisions into s.
-__device__ void decide(Smem& s, SelSmem& sm, const Args& a, const float* s_Q, const float* s_Cq, int warp,
-                       int lane, bool tables_ok) {
-  const int t = warp * 4 + (lane >> 3), sub = lane & 7;
-  const int E = a.E, k = a.k;
-  const bool in = t < a.T;
-  int home = 0, loc = 0;
-  float q = 0.0f;
-  if (in) {
-    home = a.home[t];
-    loc = a.loc != nullptr ? a.loc[t] : home;  // no state given: first layer (Eq. 36)
-    q = a.qhat != nullptr ? a.qhat[t] : 0.0f;
+// A value to the same place in both CTAs of the pair.
+__device__ __forceinline__ void store_both(float* p, uint32_t peer, float v) {
+  *p = v;
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(p), peer)), "f"(v) : "memory");
+}
+
+// A token's state (eight lanes a token) and what the tables say of all tokens, loaded while
+// the router's products run.
+struct State {
+  int home, loc, M;
+  float q, qbar;
+};
+__device__ __forceinline__ State load_state(Smem& s, const Args& a, int t, int sub) {
+  State st{0, 0, 0, 0.0f, 0.0f};
+  st.M = reinterpret_cast<const int32_t*>(a.tab)[2];
+  st.qbar = reinterpret_cast<const float*>(a.tab)[5];
+  if (t < a.T) {
+    st.home = a.home[t];
+    st.loc = a.loc != nullptr ? a.loc[t] : st.home;  // no state given: first layer (Eq. 36)
+    st.q = a.qhat != nullptr ? a.qhat[t] : 0.0f;
+    if (st.M > 0 && st.M <= ORDERMOE_MAX_SERVERS && st.home < st.M && st.loc < st.M) {
+      const float* A = reinterpret_cast<const float*>(a.tab + off_a(a.E)) + (st.home * st.M + st.loc) * st.M;
+      for (int m = sub; m < st.M; m += 8) s.delay[t][m] = A[m];
+    }
   }
-  float v[8];
-  bool nan = false;
+  return st;
+}
+
+// Top-k by (logit desc, index asc) of a token on eight lanes; lane j keeps slot j
+// (my_v, my_e), every lane the slots' experts. Lane `sub` holds the logits sub, sub + 8, ...
+struct Top {
+  float v[8], my_v, max;
+  int my_e, idx[ORDERMOE_MAX_TOPK];
+  bool nan;
+};
+__device__ __forceinline__ void top_k(Top& r, const Smem& s, int t, int sub, int lane, int E, int k) {
+  r.nan = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i] = s.logits[t][sub + 8 * i];
-    nan |= v[i] != v[i];
+    r.v[i] = s.logits[0][t][sub + 8 * i] + s.logits[1][t][sub + 8 * i];
+    r.nan |= r.v[i] != r.v[i];
   }
   const unsigned group = 0xFFu << (lane & 24);  // the token's lanes
-  nan = (__ballot_sync(0xffffffffu, nan) & group) != 0u;
-  bool active = in && !nan;
-  if (in && nan && sub == 0 && blockIdx.x == 0) report(&g_err_route, ORDERMOE_DEV_NAN_LOGIT, t);
-  // top-k by (logit desc, index asc); lane j keeps slot j
-  float my_v = -INFINITY, lmax = -INFINITY;
-  int my_e = 0;
+  r.nan = (__ballot_sync(0xffffffffu, r.nan) & group) != 0u;
+  r.my_v = r.max = -INFINITY;
+  r.my_e = 0;
   uint32_t used = 0;
-  int idx[ORDERMOE_MAX_TOPK];
 #pragma unroll
   for (int j = 0; j < ORDERMOE_MAX_TOPK; ++j) {
-    idx[j] = 0;
+    r.idx[j] = 0;
     if (j >= k) continue;  // the same for every lane
     float bv = -INFINITY;
     int be = 1 << 20, bi = 0;
@@ -227,8 +247,8 @@ __device__ void decide(Smem& s, SelSmem& sm, const Args& a, const float* s_Q, co
     for (int i = 0; i < 8; ++i) {
       const int e = sub + 8 * i;
       // an unused expert, a real one before the padding past E
-      if (!((used >> i) & 1u) && e < E && (be == (1 << 20) || v[i] > bv)) {
-        bv = v[i];
+      if (!((used >> i) & 1u) && e < E && (be == (1 << 20) || r.v[i] > bv)) {
+        bv = r.v[i];
         be = e;
         bi = i;
       }
@@ -244,79 +264,61 @@ __device__ void decide(Smem& s, SelSmem& sm, const Args& a, const float* s_Q, co
       }
     }
     if (own == be && own != (1 << 20)) used |= 1u << bi;
-    idx[j] = active ? be : 0;
-    if (j == 0) lmax = bv;
+    r.idx[j] = be < E ? be : 0;
+    if (j == 0) r.max = bv;
     if (sub == j) {
-      my_v = bv;
-      my_e = be;
+      r.my_v = bv;
+      r.my_e = be;
     }
   }
-  // softmax over all E in fp32, summed in index order; gate weights of the slots
+}
+
+// The gate weights of four tokens (fp32 softmax over all E, summed in index order) and their
+// targets: the arithmetic of the router kernels, so the same logits give the same bits.
+__device__ void weigh(Smem& s, const Args& a, const Top& r, int t, int sub, int lane) {
+  const int E = a.E, k = a.k;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s.ex[t][sub + 8 * i] = expf(v[i] - lmax);
+  for (int i = 0; i < 8; ++i) s.ex[t][sub + 8 * i] = expf(r.v[i] - r.max);
   __syncwarp();
   float denom = 0.0f;
-  for (int e = 0; e < E; ++e) denom += s.ex[t][e];
-  const float wsel = sub < k ? expf(my_v - lmax) / denom : 0.0f;
+#pragma unroll 4
+  for (int c = 0; c < (E + 3) / 4; ++c) {  // past E: exact zeros
+    const float4 x = *reinterpret_cast<const float4*>(&s.ex[t][4 * c]);
+    denom += x.x;
+    denom += x.y;
+    denom += x.z;
+    denom += x.w;
+  }
+  const float wsel = sub < k ? expf(r.my_v - r.max) / denom : 0.0f;
   float ssel = 0.0f;
   for (int j = 0; j < k; ++j) ssel += __shfl_sync(0xffffffffu, wsel, (lane & 24) + j);
   if (sub < k) {
-    s.target[t * k + sub] = active ? my_e : -1;
+    const bool active = t < a.T && !r.nan;
+    s.target[t * k + sub] = active ? r.my_e : -1;
     s.weight[t * k + sub] = active ? (a.renorm ? wsel / ssel : wsel) : 0.0f;
+  }
+}
+
+// Alg. 2 of four tokens, eight lanes each.
+__device__ void decide(Smem& s, SelSmem& sm, const Args& a, const Top& r, const State& st, const float* s_Q,
+                       const float* s_Cq, int t, int sub) {
+  const int k = a.k;
+  const bool active = t < a.T && !r.nan;
+  if (t < a.T && r.nan && sub == 0 && blockIdx.x == 0) report(&g_err_route, ORDERMOE_DEV_NAN_LOGIT, t);
+  if (sub < k) {
     s.chosen[t * k + sub] = -1;
     s.server[t * k + sub] = 0;
     s.kind[t * k + sub] = 0;
   }
-  s.loc[t] = static_cast<uint8_t>(loc);
-  s.qhat[t] = q;
-  __syncwarp();
-  if (tables_ok) {  // the same for the block
-    const int M = reinterpret_cast<const int32_t*>(a.tab)[2];
-    const float qbar = reinterpret_cast<const float*>(a.tab)[5];
-    const float* Aas = reinterpret_cast<const float*>(a.tab + off_a(E)) +
-                       (active && home < M && loc < M ? (home * M + loc) * M : 0);
-    int kind_count[4] = {0, 0, 0, 0};
-    select_slots(t, active, sub, idx, E, k, M, qbar, Aas, sm, s_Q, s_Cq, home, loc, q, s.loc, s.qhat,
-                 s.chosen, s.server, s.kind, kind_count);
-    if (blockIdx.x == 0) flush_kind_counts(sm, kind_count, a.counters);
-  }
-}
-
-// The chosen experts in ascending order with the tokens that use them and their gate
-// weights, by warp 0: two experts a lane. A token counts when all of its slots
-// were decided.
-__device__ void list_experts(Smem& s, const Args& a, int lane) {
-  const int T = a.T, k = a.k, E = a.E;
-  if (lane < T) {
-    bool ok = s.target[lane * k] >= 0;
-    for (int j = 0; j < k; ++j) ok = ok && s.chosen[lane * k + j] >= 0 && s.chosen[lane * k + j] < E;
-    s.valid[lane] = ok;
+  if (sub == 0) {
+    s.loc[t] = static_cast<uint8_t>(st.loc);
+    s.qhat[t] = st.q;
   }
   __syncwarp();
-  int base = 0;
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int e = lane + 32 * r;
-    unsigned int m = 0;
-    for (int t = 0; t < T; ++t)
-      if (s.valid[t])
-        for (int j = 0; j < k; ++j) m |= s.chosen[t * k + j] == e ? 1u << t : 0u;
-    const unsigned int any = __ballot_sync(0xffffffffu, m != 0);
-    if (m != 0) {
-      const int at = base + __popc(any & ((1u << lane) - 1));
-      s.act[at] = static_cast<uint8_t>(e);
-      s.mask[at] = static_cast<uint16_t>(m);
-      for (int t = 0; t < TOKENS; ++t) {
-        float w = 0.0f;
-        if ((m >> t) & 1u)
-          for (int j = 0; j < k; ++j)
-            if (s.chosen[t * k + j] == e) w += s.weight[t * k + j];
-        s.gate[at][t] = w;
-      }
-    }
-    base += __popc(any);
-  }
-  if (lane == 0) s.n_act = base;
+  int kind_count[4] = {0, 0, 0, 0};
+  select_slots(t, active, sub, r.idx, a.E, k, st.M, st.qbar, s.delay[t], sm, s_Q, s_Cq, st.home, st.loc, st.q,
+               s.loc, s.qhat, s.chosen, s.server, s.kind, kind_count);
+  if (blockIdx.x == 0) flush_kind_counts(sm, kind_count, a.counters);
 }
 
 // The ring's position, the same walk in the producer and in the MMA warps. A slot belongs to one
@@ -352,6 +354,31 @@ struct Share {
   }
 };
 
+// A walk over a share: row tile, chosen expert and K stage of the next one.
+struct Walk {
+  int tile, act, k;
+  int left;  // stages: a share is at most 2^31 / G of them
+  __device__ __forceinline__ explicit Walk(const Share& s) : tile(0), act(0), k(0) {
+    left = static_cast<int>(s.end - s.begin);
+    if (left > 0) {
+      tile = static_cast<int>(s.begin / s.per_tile);
+      const int r = static_cast<int>(s.begin - static_cast<long long>(tile) * s.per_tile);
+      act = r / s.per_expert;
+      k = r - act * s.per_expert;
+    }
+  }
+  __device__ __forceinline__ void next(const Share& s, int n_act) {
+    --left;
+    if (++k == s.per_expert) {
+      k = 0;
+      if (++act == n_act) {
+        act = 0;
+        ++tile;
+      }
+    }
+  }
+};
+
 template <int MT, int NT>
 __global__ void __launch_bounds__(THREADS, 1)
     few_tokens_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
@@ -383,8 +410,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     fence_mbar_init();
   }
   if (tid < 4) sm.kind[tid] = 0;
-  for (int i = tid; i < TOKENS * 68; i += THREADS) (&s.logits[0][0])[i] = -INFINITY;
-  __syncthreads();
+  for (int i = tid; i < TOKENS * 68; i += THREADS) {
+    (&s.logits[0][0][0])[i] = -INFINITY;
+    (&s.logits[1][0][0])[i] = 0.0f;
+  }
+  for (int i = tid; i < 64 * TOKENS; i += THREADS) (&s.gate[0][0])[i] = 0.0f;
+  for (int i = tid; i < 64; i += THREADS) s.mask[i] = 0;
+  cluster_sync();  // both CTAs run: the peer's shared memory may be written
 
   Ring ring_at(STAGES);          // producer and MMA warps
   uint32_t units = 0, rows = 0;  // hand-overs to the epilogue warp so far: units, row tiles
@@ -400,12 +432,16 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (!*abort) report(&g_err_route, ORDERMOE_DEV_WAIT_TIMEOUT, where);
     *abort = 1;
   };
-  auto claim = [&](uint32_t bytes) {  // producer: the next slot, its barrier set; false: give up
-    if (!mbar_wait(&s.empty[ring_at.slot], ring_at.phase ^ 1u, a.limit_ns, abort)) {
-      timeout(31);
+  // The producer walks the stages as a converged warp and one elected lane issues: a lane
+  // walking alone took about 550 cycles a stage whatever its bytes (1 token on 8 wide
+  // experts 190 us).
+  const bool issuer = elect_one();
+  auto claim = [&](uint32_t bytes) {  // the next slot, its barrier set; false: give up
+    if (!__all_sync(0xffffffffu, mbar_wait(&s.empty[ring_at.slot], ring_at.phase ^ 1u, a.limit_ns, abort))) {
+      if (issuer) timeout(31);
       return false;
     }
-    mbar_arrive_expect_tx(&s.full[ring_at.slot], bytes);
+    if (issuer) mbar_arrive_expect_tx(&s.full[ring_at.slot], bytes);
     issued_mask |= 1u << ring_at.slot;
     last_phase_bits = (last_phase_bits & ~(1u << ring_at.slot)) | (ring_at.phase << ring_at.slot);
     return true;
@@ -501,52 +537,70 @@ __global__ void __launch_bounds__(THREADS, 1)
     return take(MT2c{}, 0, 2, parity, body);
   };
   // ---------------------------------------------------------------- route
-  if (!a.given) {
-    const int tiles = (a.E + 16 * MT - 1) / (16 * MT);
+  const uint32_t rank = cluster_ctarank();
+  auto route = [&](auto row_tiles, State& st) {
+    // stages of all experts' rows (RT tiles of 16) by KB blocks of K, the first half of them
+    // in rank 0
+    constexpr int RT = decltype(row_tiles)::value, KB = RT == 4 && MT == 1 ? 1 : 2;
+    constexpr uint32_t W = RT * 2048 * KB;
+    const int all = a.d / (64 * KB), half = (all + 1) / 2;
+    const int s0 = rank == 0 ? 0 : half, s1 = rank == 0 ? half : all;
     if (warp == PRODUCER) {
-      if (lane == 0)
-        for (int i = 0; i < tiles && !*abort; ++i)
-          for (int kb = 0; kb < k_up; ++kb) {
-            if (!claim(C::STAGE_BYTES)) break;
-            tma_load_3d(slot_ptr(ring_at.slot), &maps.Wr, &s.full[ring_at.slot], i * 16 * MT, kb * KB_UP);
-            tma_load_3d(slot_ptr(ring_at.slot) + C::W_BYTES, &maps.X, &s.full[ring_at.slot], 0, kb * KB_UP);
-            ring_at.next();
-          }
-    } else if (warp < MMA_WARPS) {
-      tables_ok = load_tables_range(a.tab, a.E, sm, s_Q, s_Cq, tid, 32 * MMA_WARPS);
-      float acc[MT][NT][4] = {};
-      for (int i = 0; i < tiles; ++i) {
-        bool ok = true;
-        for (int kb = 0; kb < k_up && ok; ++kb) {
-          if (ring_at.slot % MMA_WARPS == warp) {
-            ok = arrived();
-            if (!ok) break;
-            const uint32_t w = ring0 + ring_at.slot * C::STAGE_BYTES;
-            mma_stage<MT, NT, KB_UP>(acc, w, 2048 * MT, 1024, 2048, w + C::W_BYTES, lane);
-            release();
-          }
-          ring_at.next();
+      for (int i = s0; i < s1; ++i) {
+        if (!claim(W + KB * 1024 * NT)) break;
+        if (issuer) {
+          uint8_t* p = slot_ptr(ring_at.slot);
+          tma_load_3d(p, &maps.Wr, &s.full[ring_at.slot], 0, i * KB);
+          tma_load_3d(p + C::W_BYTES, &maps.Xr, &s.full[ring_at.slot], 0, i * KB);
         }
-        if (!ok || !put_unit(acc)) break;
+        ring_at.next();
       }
+    } else if (warp < MMA_WARPS) {
+      if (warp < TOKENS / 4) st = load_state(s, a, warp * 4 + (lane >> 3), lane & 7);
+      tables_ok = load_tables_range(a.tab, a.E, sm, s_Q, s_Cq, tid, 32 * MMA_WARPS);
+      float acc[RT][NT][4] = {};
+      bool ok = true;
+      for (int i = s0; i < s1; ++i) {
+        if (ring_at.slot % MMA_WARPS == warp) {
+          if (!(ok = arrived())) break;
+          const uint32_t w = ring0 + ring_at.slot * C::STAGE_BYTES;
+          mma_stage<RT, NT, KB>(acc, w, 2048 * RT, 1024, 2048, w + C::W_BYTES, lane);
+          release();
+        }
+        ring_at.next();
+      }
+      if (ok) put(acc, row_tiles, 0, 0);
+      ++units;
     } else {
-      for (int i = 0; i < tiles; ++i) {
-        const bool ok = take_unit([&](int m, int n, float4 v) {
-          const int e = i * 16 * MT + m * 16 + (lane >> 2), t = n * 8 + (lane & 3) * 2;
-          if (e < a.E) {
-            s.logits[t][e] = v.x;
-            s.logits[t + 1][e] = v.y;
-          }
-          if (e + 8 < a.E) {
-            s.logits[t][e + 8] = v.z;
-            s.logits[t + 1][e + 8] = v.w;
-          }
-        });
-        if (!ok) break;
-      }
+      take(row_tiles, 0, 0, 0, [&](int m, int n, float4 v) {
+        const int e = m * 16 + (lane >> 2), t = n * 8 + (lane & 3) * 2;
+        float* p = &s.logits[rank][t][e];
+        if (e < a.E) {
+          store_both(p, rank ^ 1u, v.x);
+          store_both(p + 68, rank ^ 1u, v.y);
+        }
+        if (e + 8 < a.E) {
+          store_both(p + 8, rank ^ 1u, v.z);
+          store_both(p + 68 + 8, rank ^ 1u, v.w);
+        }
+      });
+      ++units;
     }
-    __syncthreads();
-    if (warp < TOKENS / 4) decide(s, sm, a, s_Q, s_Cq, warp, lane, tables_ok);
+  };
+  if (!a.given) {
+    State st{};
+    if (a.E <= 16) route(std::integral_constant<int, 1>{}, st);
+    else if (a.E <= 32) route(std::integral_constant<int, 2>{}, st);
+    else route(std::integral_constant<int, 4>{}, st);
+    cluster_sync();  // the peer's half of the logits is here
+    if (warp < 2 * (TOKENS / 4)) {  // warps 0-3 decide, 4-7 weigh: four tokens each
+      const int t = (warp % (TOKENS / 4)) * 4 + (lane >> 3), sub = lane & 7;
+      Top r;
+      top_k(r, s, t, sub, lane, a.E, a.k);
+      if (warp >= TOKENS / 4) weigh(s, a, r, t, sub, lane);
+      else if (tables_ok) decide(s, sm, a, r, st, s_Q, s_Cq, t, sub);  // the same for the block
+      else if (sub < a.k) s.chosen[t * a.k + sub] = -1;
+    }
   } else {
     for (int i = tid; i < a.T * a.k; i += THREADS) {
       s.target[i] = a.topk_idx[i];
@@ -555,7 +609,28 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   }
   __syncthreads();
-  if (warp == 0) list_experts(s, a, lane);
+  // The chosen experts in ascending order, the tokens that use them and their gate weights. A
+  // token counts when all of its slots were decided.
+  if (tid < a.T) {
+    bool ok = s.target[tid * a.k] >= 0;
+    for (int j = 0; j < a.k; ++j) ok = ok && s.chosen[tid * a.k + j] >= 0 && s.chosen[tid * a.k + j] < a.E;
+    s.valid[tid] = ok;
+    if (ok)
+      for (int j = 0; j < a.k; ++j) {  // a token's experts are distinct
+        const int e = s.chosen[tid * a.k + j];
+        atomicOr(&s.mask[e], 1u << tid);
+        s.gate[e][tid] += s.weight[tid * a.k + j];
+      }
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const bool lo = s.mask[lane] != 0, hi = s.mask[lane + 32] != 0;
+    const unsigned int l = __ballot_sync(0xffffffffu, lo), h = __ballot_sync(0xffffffffu, hi);
+    const unsigned int before = (1u << lane) - 1;
+    if (lo) s.act[__popc(l & before)] = static_cast<uint8_t>(lane);
+    if (hi) s.act[__popc(l) + __popc(h & before)] = static_cast<uint8_t>(lane + 32);
+    if (lane == 0) s.n_act = __popc(l) + __popc(h);
+  }
   if (cta == 0 && !a.given && !*abort) {  // one CTA writes the decisions
     for (int i = tid; i < a.T * a.k; i += THREADS) {
       const bool ok = s.target[i] >= 0 && s.chosen[i] >= 0;
@@ -568,7 +643,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
     if (a.logits != nullptr)
-      for (int i = tid; i < a.T * a.E; i += THREADS) a.logits[i] = s.logits[i / a.E][i % a.E];
+      for (int i = tid; i < a.T * a.E; i += THREADS) {
+        const int t = i / a.E, e = i - t * a.E;
+        a.logits[i] = s.logits[0][t][e] + s.logits[1][t][e];
+      }
     if (a.counters != nullptr && tid < 4 && sm.kind[tid]) atomicAdd(&a.counters[tid], sm.kind[tid]);
   }
   __syncthreads();
@@ -579,57 +657,51 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int n_units = n_act * per;
   const Share share(a.d, a.dff, C::DOWN_ROWS, n_act, cta, G);
   if (warp == PRODUCER) {
-    if (lane == 0) {
-      bool ok = true;
-      for (int u = cta; u < n_units && ok; u += G) {
-        const int row = s.act[u / per] * a.dff + (u % per) * 8 * MT;
-        for (int kb = 0; kb < k_up; ++kb) {
-          if (!(ok = claim(C::STAGE_BYTES))) break;
+    bool ok = true;
+    for (int u = cta; u < n_units && ok; u += G) {
+      const int row = s.act[u / per] * a.dff + (u % per) * 8 * MT;
+      for (int kb = 0; kb < k_up; ++kb) {
+        if (!(ok = claim(C::STAGE_BYTES))) break;
+        if (issuer) {
           uint8_t* p = slot_ptr(ring_at.slot);
           tma_load_3d(p, &maps.W1, &s.full[ring_at.slot], row, kb * KB_UP);
           tma_load_3d(p + C::W_BYTES / 2, &maps.W3, &s.full[ring_at.slot], row, kb * KB_UP);
           tma_load_3d(p + C::W_BYTES, &maps.X, &s.full[ring_at.slot], 0, kb * KB_UP);
-          ring_at.next();
         }
+        ring_at.next();
       }
-      // down: the weights of a stage as soon as its slot is free, H behind the
-      // barrier that every CTA's gate/up passes
-      auto where = [&](long long i, int& tile, int& act, int& kk) {
-        tile = static_cast<int>(i / share.per_tile);
-        const int r = static_cast<int>(i - static_cast<long long>(tile) * share.per_tile);
-        act = r / share.per_expert;
-        kk = (r - act * share.per_expert) * KB_DOWN;
-      };
-      const uint32_t bytes = C::W_BYTES + 2048 * NT;
-      long long i = share.begin;
-      Ring first = ring_at;
-      int tile, act, kk;
-      for (; ok && i < share.end && i - share.begin < STAGES; ++i) {
-        if (!(ok = claim(bytes))) break;
-        where(i, tile, act, kk);
+    }
+    // down: the weights of a stage as soon as its slot is free, H behind the barrier
+    // that every CTA's gate/up passes
+    const uint32_t bytes = C::W_BYTES + 2048 * NT;
+    Walk w(share), hw(share);
+    Ring first = ring_at;
+    auto load_w = [&]() {
+      if (issuer)
         tma_load_3d(slot_ptr(ring_at.slot), &maps.W2, &s.full[ring_at.slot],
-                    s.act[act] * a.d + tile * C::DOWN_ROWS, kk);
-        ring_at.next();
-      }
-      if (ok && !grid_wait(&a.sync[0], G, a.limit_ns, abort)) {
-        timeout(35);
-        ok = false;
-      }
-      fence_proxy_async();
-      // (also after a failure: the barriers of the stages under way expect these bytes)
-      for (long long j = share.begin; j < i; ++j) {
-        where(j, tile, act, kk);
-        tma_load_3d(slot_ptr(first.slot) + C::W_BYTES, &maps.H, &s.full[first.slot], act * a.T, kk);
-        first.next();
-      }
-      for (; ok && i < share.end; ++i) {
-        if (!(ok = claim(bytes))) break;
-        where(i, tile, act, kk);
-        uint8_t* p = slot_ptr(ring_at.slot);
-        tma_load_3d(p, &maps.W2, &s.full[ring_at.slot], s.act[act] * a.d + tile * C::DOWN_ROWS, kk);
-        tma_load_3d(p + C::W_BYTES, &maps.H, &s.full[ring_at.slot], act * a.T, kk);
-        ring_at.next();
-      }
+                    s.act[w.act] * a.d + w.tile * C::DOWN_ROWS, w.k * KB_DOWN);
+      ring_at.next();
+      w.next(share, n_act);
+    };
+    auto load_h = [&]() {
+      if (issuer)
+        tma_load_3d(slot_ptr(first.slot) + C::W_BYTES, &maps.H, &s.full[first.slot], hw.act * a.T,
+                    hw.k * KB_DOWN);
+      first.next();
+      hw.next(share, n_act);
+    };
+    while (ok && w.left > 0 && hw.left - w.left < STAGES && (ok = claim(bytes))) load_w();
+    if (ok) {
+      const bool up = !issuer || grid_wait(&a.sync[0], G, a.limit_ns, abort);
+      if (!up) timeout(35);
+      ok = __all_sync(0xffffffffu, up);
+    }
+    fence_proxy_async();
+    // (also after a failure: the barriers of the stages under way expect these bytes)
+    while (hw.left > w.left) load_h();
+    while (ok && w.left > 0 && (ok = claim(bytes))) {
+      load_w();
+      load_h();
     }
   } else if (warp < MMA_WARPS) {
     bool ok = true;
@@ -649,27 +721,27 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
     float acc[2 * MT][NT][4] = {}, tot[2 * MT][NT][4] = {};
-    int act = static_cast<int>(share.begin % max(share.per_tile, 1)) / max(share.per_expert, 1);
-    int kk = static_cast<int>(share.begin % max(share.per_expert, 1));
     bool any = false;
-    for (long long i = share.begin; i < share.end && ok; ++i) {
+    for (Walk w(share); w.left > 0 && ok;) {
       if (ring_at.slot % MMA_WARPS == warp) {
         if (!(ok = arrived())) break;
-        const uint32_t w = ring0 + ring_at.slot * C::STAGE_BYTES;
-        mma_stage<2 * MT, NT, KB_DOWN>(acc, w, 4096 * MT, 1024, 2048, w + C::W_BYTES, lane);
+        const uint32_t p = ring0 + ring_at.slot * C::STAGE_BYTES;
+        mma_stage<2 * MT, NT, KB_DOWN>(acc, p, 4096 * MT, 1024, 2048, p + C::W_BYTES, lane);
         release();
         any = true;
       }
       ring_at.next();
-      const bool expert_end = ++kk == share.per_expert;
-      if ((expert_end || i + 1 == share.end) && any) {
+      const int act = w.act, tile = w.tile;
+      w.next(share, n_act);
+      if (any && (w.k == 0 || w.left == 0)) {
         // the expert's sums to the tokens that use it
-        const unsigned int m = s.mask[act];
+        const int e = s.act[act];
+        const unsigned int m = s.mask[e];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int t = n * 8 + (lane & 3) * 2;
           const bool u0 = (m >> t) & 1u, u1 = (m >> (t + 1)) & 1u;
-          const float g0 = s.gate[act][t], g1 = s.gate[act][t + 1];
+          const float g0 = s.gate[e][t], g1 = s.gate[e][t + 1];
 #pragma unroll
           for (int j = 0; j < 2 * MT; ++j) {
             float (&c)[4] = acc[j][n];
@@ -683,11 +755,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         any = false;
       }
-      if (expert_end) {
-        kk = 0;
-        if (++act == n_act) act = 0;
-      }
-      if ((expert_end && act == 0) || i + 1 == share.end) ok = put_tile(tot);
+      if (w.tile != tile || w.left == 0) ok = put_tile(tot);
     }
   } else {
     bool ok = true;
@@ -735,34 +803,67 @@ __global__ void __launch_bounds__(THREADS, 1)
   __syncthreads();
 
   // ---------------------------------------------------------------- finish
-  if (cta < a.T) {
+  // On the residual map a CTA a token (its norm is a sum over the row), otherwise every token's
+  // columns over G / T CTAs.
+  const int parts = a.h != nullptr ? 1 : max(1, G / a.T);
+  if (cta < a.T * parts) {
+    const int tiles = a.d / C::DOWN_ROWS, part = cta / a.T;
+    const int first_tile = tiles * part / parts, last_tile = tiles * (part + 1) / parts;
+    // the first and last owner of every row tile, while the others finish (the ring is free)
+    int16_t* own = reinterpret_cast<int16_t*>(ring);
+    const int cap = STAGES * C::STAGE_BYTES / 4;  // tiles that fit
+    const bool listed = tiles <= cap;
+    auto owners = [&](int tile, int& c0, int& c1) {
+      c0 = share.owner(static_cast<long long>(tile) * share.per_tile);
+      c1 = share.owner(static_cast<long long>(tile + 1) * share.per_tile - 1);
+    };
+    if (listed && share.total > 0)
+      for (int i = first_tile + tid; i < last_tile; i += THREADS) {
+        int c0, c1;
+        owners(i, c0, c1);
+        own[2 * i] = static_cast<int16_t>(c0);
+        own[2 * i + 1] = static_cast<int16_t>(c1);
+      }
     if (tid == 0 && !grid_wait(&a.sync[1], G, a.limit_ns, abort)) timeout(36);
     __syncthreads();
-    for (int t = cta; t < a.T && !*abort; t += G) {
+    for (int t = cta % a.T; t < a.T && !*abort; t += G) {
       if (!s.valid[t]) continue;
       float sq = 0.0f;
-      for (int c = tid * 4; c < a.d; c += THREADS * 4) {
+      const size_t row = static_cast<size_t>(t) * a.d;
+      for (int c = first_tile * C::DOWN_ROWS + tid * 4; c < last_tile * C::DOWN_ROWS; c += THREADS * 4) {
         const int tile = c / C::DOWN_ROWS;
-        const int c0 = share.owner(static_cast<long long>(tile) * share.per_tile);
-        const int c1 = share.owner(static_cast<long long>(tile + 1) * share.per_tile - 1);
+        uint2 hv = make_uint2(0, 0);
+        if (a.h != nullptr) hv = *reinterpret_cast<const uint2*>(a.h + row + c);
+        int c0, c1;
+        if (listed) {
+          c0 = own[2 * tile];
+          c1 = own[2 * tile + 1];
+        } else {
+          owners(tile, c0, c1);
+        }
+        const size_t pitch = static_cast<size_t>(a.T) * C::DOWN_ROWS;
         const float* p = a.part + (static_cast<size_t>(tile + c0) * a.T + t) * C::DOWN_ROWS + c % C::DOWN_ROWS;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int q = c0; q <= c1; ++q, p += static_cast<size_t>(a.T) * C::DOWN_ROWS) {
-          const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
-          v.x += u.x;
-          v.y += u.y;
-          v.z += u.z;
-          v.w += u.w;
+        for (int q = c0; q <= c1; q += 4, p += 4 * pitch) {  // four loads under way
+          float4 u[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (q + j <= c1) u[j] = __ldcg(reinterpret_cast<const float4*>(p + j * pitch));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (q + j <= c1) {
+              v.x += u[j].x;
+              v.y += u[j].y;
+              v.z += u[j].z;
+              v.w += u[j].w;
+            }
         }
-        if (a.h != nullptr) {
-          const uint2 hv = *reinterpret_cast<const uint2*>(a.h + static_cast<size_t>(t) * a.d + c);
-          v.x += bf16_lo(hv.x);
-          v.y += bf16_hi(hv.x);
-          v.z += bf16_lo(hv.y);
-          v.w += bf16_hi(hv.y);
-        }
+        v.x += bf16_lo(hv.x);
+        v.y += bf16_hi(hv.x);
+        v.z += bf16_lo(hv.y);
+        v.w += bf16_hi(hv.y);
         const uint2 o = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-        *reinterpret_cast<uint2*>(a.y + static_cast<size_t>(t) * a.d + c) = o;
+        *reinterpret_cast<uint2*>(a.y + row + c) = o;
         const float f[4] = {bf16_lo(o.x), bf16_hi(o.x), bf16_lo(o.y), bf16_hi(o.y)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) sq = fmaf(f[j], f[j], sq);
@@ -778,8 +879,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int w = 0; w < THREADS / 32; ++w) total += s.sum[w];
       const float r = 1.0f / sqrtf(total / static_cast<float>(a.d) + a.eps);
       for (int c = tid * 4; c < a.d; c += THREADS * 4) {  // each thread's own columns again
-        const uint2 o = *reinterpret_cast<const uint2*>(a.y + static_cast<size_t>(t) * a.d + c);
-        *reinterpret_cast<uint2*>(a.x_out + static_cast<size_t>(t) * a.d + c) =
+        const uint2 o = *reinterpret_cast<const uint2*>(a.y + row + c);
+        *reinterpret_cast<uint2*>(a.x_out + row + c) =
             make_uint2(pack_bf16x2(bf16_lo(o.x) * r, bf16_hi(o.x) * r),
                        pack_bf16x2(bf16_lo(o.y) * r, bf16_hi(o.y) * r));
       }
@@ -791,11 +892,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   }
   __syncthreads();
-  if (s.abort && warp == PRODUCER && lane == 0) {  // every copy that this CTA issued (bounded)
+  if (s.abort && warp == PRODUCER && issuer) {  // every copy that this CTA issued (bounded)
     volatile int* never = &s.zero;
     for (int i = 0; i < STAGES; ++i)
       if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
   }
+  cluster_sync();  // (no access to the peer is under way)
   // the last CTA to leave sets the counters back
   if (tid == 0) {
     __threadfence();
@@ -863,7 +965,9 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   const int R = a.T * a.k, act = R < a.E ? R : a.E;
   fw::Maps m;
   int rc;
-  if ((rc = make_tmap_bf16_kb(&m.Wr, L->W_r, a.E, a.d, 16 * MT, fw::KB_UP))) return rc;
+  const int rt = a.E <= 16 ? 1 : a.E <= 32 ? 2 : 4, kb = rt == 4 && MT == 1 ? 1 : 2;  // as the kernel's route
+  if ((rc = make_tmap_bf16_kb(&m.Wr, L->W_r, a.E, a.d, 16 * rt, kb))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.Xr, X, a.T, a.d, 8 * NT, kb))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.X, X, a.T, a.d, 8 * NT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W1, L->W1, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W3, L->W3, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
@@ -874,16 +978,22 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   int grid = num_sms() < kFewMaxCtas ? num_sms() : kFewMaxCtas;
   const long long units = (long long)act * (a.dff / (8 * MT));
   if (units < grid) grid = static_cast<int>(units);
+  grid = (grid < a.T ? a.T : grid) / 2 * 2;  // pairs
+  if (grid < 2) grid = 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
   cfg.blockDim = dim3(fw::THREADS, 1, 1);
   cfg.dynamicSmemBytes = a.stages * C::STAGE_BYTES + C::other_bytes(a.E);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeCooperative;  // the CTAs wait for one another: all or none run
   attr[0].val.cooperative = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, fw::few_tokens_kernel<MT, NT>, m, a);
   if (e != cudaSuccess) return cuda_fail(e, "few_tokens_kernel");
   OM_LAUNCHED("few_tokens_kernel");
