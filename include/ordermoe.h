@@ -362,7 +362,7 @@ int ordermoe_layer_forward_residual(const ordermoe_layer_desc* layer, int T, con
  * unwritten, the other tokens are computed.
  * The launch is cooperative, one CTA per SM: it starts when that many fit beside what
  * runs, and can be captured into a graph.
- * Shapes: d % 256 == 0, dff % 128 == 0, 1 <= k <= min(E, 8), E <= 64. */
+ * Shapes: d % 256 == 0, d <= 32768, dff % 128 == 0, 1 <= k <= min(E, 8), E <= 64. */
 typedef struct {
   float* logits;          /* [T][E] router logits                              */
   int32_t* topk_idx;      /* [T][k] and on: as ordermoe_route_select's outputs */

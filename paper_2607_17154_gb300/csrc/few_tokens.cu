@@ -19,10 +19,10 @@
 //   finish   one CTA a token adds the partials of every row tile in CTA order and
 //            writes y, or h + y and its norm.
 // Sums are fp32 in a fixed order: the same call gives the same bits.
-// A producer warp streams the weights and the tokens' K blocks through a ring of TMA
+// Two producer warps stream the weights and the tokens' K blocks through a ring of TMA
 // boxes with the 128-byte swizzle; eight MMA warps take its slots in turn; an
 // epilogue warp adds their eight partial accumulators. Between gate/up and down
-// the producer fills the ring with W2 while the other CTAs finish H: the grid
+// the producers fill the ring with W2 while the other CTAs finish H: the grid
 // barrier there costs HBM no pause.
 #include <cstddef>
 #include <type_traits>
@@ -42,9 +42,11 @@ namespace fw {
 
 constexpr int TOKENS = ORDERMOE_FEW_TOKENS;
 constexpr int MMA_WARPS = 8;
-constexpr int PRODUCER = MMA_WARPS;  // the last warp is the epilogue's
-constexpr int THREADS = 32 * (MMA_WARPS + 2);
+constexpr int PRODUCERS = 2;  // the warps behind the MMA warps; the last is the epilogue's
+constexpr int THREADS = 32 * (MMA_WARPS + PRODUCERS + 1);
 constexpr int KB_UP = 4, KB_DOWN = 2;  // 64-element K blocks a stage
+// and in the router, whose stage holds rt tiles of 16 experts (8 MT KB of them, at most 4 blocks)
+__host__ __device__ constexpr int route_kb(int mt, int rt) { return 4 * mt / rt < 4 ? 4 * mt / rt : 4; }
 
 // MT: 16-row MMA tiles of a gate/up unit; NT: 8-token column tiles.
 template <int MT, int NT>
@@ -59,6 +61,7 @@ struct Cfg {
   static constexpr int other_bytes(int E) { return 1024 + RED_FLOATS * 4 + ((8 * E * E + 15) & ~15); }
 };
 constexpr int MAX_STAGES = 16;
+constexpr int MAX_D = 32768;  // a row and its tiles' owners fit in the ring's memory
 
 struct Smem {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];
@@ -75,8 +78,10 @@ struct Smem {
   float weight[TOKENS * ORDERMOE_MAX_TOPK];
   int32_t chosen[TOKENS * ORDERMOE_MAX_TOPK];
   uint8_t server[TOKENS * ORDERMOE_MAX_TOPK], kind[TOKENS * ORDERMOE_MAX_TOPK];
-  uint8_t loc[TOKENS];
-  float qhat[TOKENS];
+  uint8_t loc[TOKENS];             // location and loss, before and then after
+  float qhat[TOKENS], qbar;
+  int nan[TOKENS];                 // a logit is NaN
+  int placed[TOKENS];              // home and location are servers
   int valid[TOKENS];               // decided: its outputs are written
   float sum[THREADS / 32];
 };
@@ -89,6 +94,9 @@ constexpr int stages(int E) {
   return n < MAX_STAGES ? n : MAX_STAGES;
 }
 static_assert(stages<1, 1>(64) >= 12 && stages<2, 1>(64) >= 6 && stages<2, 2>(64) >= 5, "ring");
+static_assert(MAX_D / 32 * 4 + MAX_D * 2 <= 5 * Cfg<2, 2>::STAGE_BYTES && Cfg<1, 1>::STAGE_BYTES * 12 >= 5 * Cfg<2, 2>::STAGE_BYTES &&
+                  Cfg<2, 1>::STAGE_BYTES * 6 >= 5 * Cfg<2, 2>::STAGE_BYTES, "finish");
+static_assert(TOKENS * ORDERMOE_MAX_TOPK * 64 * 12 <= 5 * Cfg<2, 2>::STAGE_BYTES, "candidates");
 
 struct Maps {
   CUtensorMap Wr, Xr, X, W1, W3, W2, H;
@@ -159,23 +167,31 @@ __device__ __forceinline__ bool grid_wait(const unsigned int* count, unsigned in
 
 // acc += the rows of a stage's weights times its token columns, KB blocks of 64.
 // Rows 0-7 of MMA tile i start at w + i * tile_pitch, rows 8-15 hi bytes on; a K
-// block's rows are kb_pitch bytes, its tokens 1024 NT. Rows of 128 bytes,
-// 16-byte chunk c of row r at c ^ (r % 8): the eight rows that an ldmatrix phase
-// reads are in different banks.
+// block's rows are kb_pitch bytes; its T token rows follow the block before's. Rows of
+// 128 bytes, 16-byte chunk c of the row at 128 r at c ^ (r % 8): the eight rows that an
+// ldmatrix phase reads are in different banks. Columns past T read the first
+// token's row and are dropped later. (Boxes of 8 or 16 rows, zero-filled past T, took
+// TMA's time for every row: it copies a row of 128 bytes in about 3 cycles.)
 template <int TILES, int NT, int KB>
 __device__ __forceinline__ void mma_stage(float (&acc)[TILES][NT][4], uint32_t w, uint32_t kb_pitch,
-                                          uint32_t hi, uint32_t tile_pitch, uint32_t x, int lane) {
+                                          uint32_t hi, uint32_t tile_pitch, uint32_t x, int T, int lane) {
   const uint32_t r = lane & 7;
-  const uint32_t wr = w + ((lane >> 3) & 1) * hi + r * 128, xr = x + r * 128;
+  const uint32_t wr = w + ((lane >> 3) & 1) * hi + r * 128;
+  uint32_t xr[NT];  // the lane's token rows
+#pragma unroll
+  for (int n = 0; n < NT; ++n) xr[n] = static_cast<int>(n * 8 + r) < T ? n * 8 + r : 0;
   const uint32_t wc = lane >> 4, xc = lane >> 3;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
+    if (kb > 0)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) xr[n] += T;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {  // 32 elements: two K steps of the MMA
       uint32_t b[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        ldmatrix4(b[n], xr + kb * (1024 * NT) + n * 1024 + (((half * 4 + xc) ^ r) << 4));
+        ldmatrix4(b[n], x + xr[n] * 128 + (((half * 4 + xc) ^ (xr[n] & 7)) << 4));
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
 #pragma unroll
@@ -196,133 +212,192 @@ __device__ __forceinline__ void store_both(float* p, uint32_t peer, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(p), peer)), "f"(v) : "memory");
 }
 
-// A token's state (eight lanes a token) and what the tables say of all tokens, loaded while
-// the router's products run.
-struct State {
-  int home, loc, M;
-  float q, qbar;
-};
-__device__ __forceinline__ State load_state(Smem& s, const Args& a, int t, int sub) {
-  State st{0, 0, 0, 0.0f, 0.0f};
-  st.M = reinterpret_cast<const int32_t*>(a.tab)[2];
-  st.qbar = reinterpret_cast<const float*>(a.tab)[5];
-  if (t < a.T) {
-    st.home = a.home[t];
-    st.loc = a.loc != nullptr ? a.loc[t] : st.home;  // no state given: first layer (Eq. 36)
-    st.q = a.qhat != nullptr ? a.qhat[t] : 0.0f;
-    if (st.M > 0 && st.M <= ORDERMOE_MAX_SERVERS && st.home < st.M && st.loc < st.M) {
-      const float* A = reinterpret_cast<const float*>(a.tab + off_a(a.E)) + (st.home * st.M + st.loc) * st.M;
-      for (int m = sub; m < st.M; m += 8) s.delay[t][m] = A[m];
+// The tokens' states and delay rows into shared memory, a token a warp in turn, while the
+// router's products run.
+__device__ __forceinline__ void load_states(Smem& s, const Args& a, int warp, int lane) {
+  const int M = reinterpret_cast<const int32_t*>(a.tab)[2];
+#pragma unroll 1
+  for (int t = warp; t < a.T; t += MMA_WARPS) {
+    const int home = a.home[t];
+    const int loc = a.loc != nullptr ? a.loc[t] : home;  // no state given: first layer (Eq. 36)
+    const bool ok = M > 0 && M <= ORDERMOE_MAX_SERVERS && home < M && loc < M;
+    if (ok && lane < M)
+      s.delay[t][lane] = reinterpret_cast<const float*>(a.tab + off_a(a.E))[(home * M + loc) * M + lane];
+    if (lane == 0) {
+      s.placed[t] = ok;
+      s.loc[t] = static_cast<uint8_t>(loc);
+      s.qhat[t] = a.qhat != nullptr ? a.qhat[t] : 0.0f;
     }
   }
-  return st;
+  if (warp == 0 && lane == 0) s.qbar = reinterpret_cast<const float*>(a.tab)[5];
 }
 
-// Top-k by (logit desc, index asc) of a token on eight lanes; lane j keeps slot j
-// (my_v, my_e), every lane the slots' experts. Lane `sub` holds the logits sub, sub + 8, ...
-struct Top {
-  float v[8], my_v, max;
-  int my_e, idx[ORDERMOE_MAX_TOPK];
-  bool nan;
-};
-__device__ __forceinline__ void top_k(Top& r, const Smem& s, int t, int sub, int lane, int E, int k) {
-  r.nan = false;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    r.v[i] = s.logits[0][t][sub + 8 * i] + s.logits[1][t][sub + 8 * i];
-    r.nan |= r.v[i] != r.v[i];
-  }
-  const unsigned group = 0xFFu << (lane & 24);  // the token's lanes
-  r.nan = (__ballot_sync(0xffffffffu, r.nan) & group) != 0u;
-  r.my_v = r.max = -INFINITY;
-  r.my_e = 0;
-  uint32_t used = 0;
-#pragma unroll
-  for (int j = 0; j < ORDERMOE_MAX_TOPK; ++j) {
-    r.idx[j] = 0;
-    if (j >= k) continue;  // the same for every lane
-    float bv = -INFINITY;
-    int be = 1 << 20, bi = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = sub + 8 * i;
-      // an unused expert, a real one before the padding past E
-      if (!((used >> i) & 1u) && e < E && (be == (1 << 20) || r.v[i] > bv)) {
-        bv = r.v[i];
-        be = e;
-        bi = i;
-      }
-    }
-    const int own = be;
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) {
-      const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-      const int oe = __shfl_xor_sync(0xffffffffu, be, o);
-      if (oe != (1 << 20) && (be == (1 << 20) || ov > bv || (ov == bv && oe < be))) {
-        bv = ov;
-        be = oe;
-      }
-    }
-    if (own == be && own != (1 << 20)) used |= 1u << bi;
-    r.idx[j] = be < E ? be : 0;
-    if (j == 0) r.max = bv;
-    if (sub == j) {
-      r.my_v = bv;
-      r.my_e = be;
-    }
-  }
+__device__ __forceinline__ void mma_warps_sync() {
+  asm volatile("bar.sync 1, %0;" ::"n"(32 * MMA_WARPS) : "memory");
 }
 
-// The gate weights of four tokens (fp32 softmax over all E, summed in index order) and their
-// targets: the arithmetic of the router kernels, so the same logits give the same bits.
-__device__ void weigh(Smem& s, const Args& a, const Top& r, int t, int sub, int lane) {
-  const int E = a.E, k = a.k;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s.ex[t][sub + 8 * i] = expf(r.v[i] - r.max);
+// The decisions in three steps on the MMA warps: the top-k, a warp a token; the candidates of
+// every slot, whose costs hang on no other slot, eight lanes each; then the slots of a token in
+// rank order on eight lanes, beside the gate weights in the other warps. What bounds it is the
+// latency of dependent instructions at ten warps an SM.
+
+// The k largest logits by (logit desc, index asc), as unsigned keys in their order, -0 as +0; 0 is
+// below every key.
+__device__ __forceinline__ void top_k(Smem& s, const Args& a, int t, int lane) {
+  const float x0 = s.logits[0][t][lane] + s.logits[1][t][lane];
+  const float x1 = s.logits[0][t][lane + 32] + s.logits[1][t][lane + 32];
+  const bool nan = __any_sync(0xffffffffu, x0 != x0 || x1 != x1);
+  auto key = [](float x) {
+    const unsigned int u = __float_as_uint(x + 0.0f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+  };
+  unsigned int k0 = lane < a.E ? key(x0) : 0u, k1 = lane + 32 < a.E ? key(x1) : 0u;
+  unsigned int lo = 0, hi = 0;
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {
+    const unsigned int best = __reduce_max_sync(0xffffffffu, max(k0, k1));
+    lo = __ballot_sync(0xffffffffu, k0 == best);
+    hi = __ballot_sync(0xffffffffu, k1 == best);
+    const int e = lo ? __ffs(lo) - 1 : __ffs(hi) + 31;
+    if (lane == (e & 31)) {
+      if (e < 32) k0 = 0u;
+      else k1 = 0u;
+      s.target[t * a.k + j] = e;
+      s.weight[t * a.k + j] = e < 32 ? x0 : x1;  // the logit, until the weights are taken
+    }
+  }
+  if (lane == 0) s.nan[t] = nan;
+}
+
+// A token's gate weights on eight lanes (sub): fp32 softmax over all E, summed in index order,
+// the arithmetic of the router kernels, so the same logits give the same bits.
+__device__ __forceinline__ void weigh(Smem& s, const Args& a, int t, int sub, int lane) {
+  const int k = a.k;
+  const bool in = t < a.T;  // (the others' rows hold nothing that is read)
+  const float top = s.weight[t * k], mine = sub < k ? s.weight[t * k + sub] : 0.0f;
+  __syncwarp();  // (read before the weights take the logits' place)
+#pragma unroll 1
+  for (int e = sub; e < a.E; e += 8) s.ex[t][e] = expf(s.logits[0][t][e] + s.logits[1][t][e] - top);
+  if (a.E % 4 != 0 && sub == 0)
+    for (int e = a.E; e % 4 != 0; ++e) s.ex[t][e] = 0.0f;
   __syncwarp();
   float denom = 0.0f;
 #pragma unroll 4
-  for (int c = 0; c < (E + 3) / 4; ++c) {  // past E: exact zeros
+  for (int c = 0; c < (a.E + 3) / 4; ++c) {  // past E: exact zeros
     const float4 x = *reinterpret_cast<const float4*>(&s.ex[t][4 * c]);
     denom += x.x;
     denom += x.y;
     denom += x.z;
     denom += x.w;
   }
-  const float wsel = sub < k ? expf(r.my_v - r.max) / denom : 0.0f;
-  float ssel = 0.0f;
-  for (int j = 0; j < k; ++j) ssel += __shfl_sync(0xffffffffu, wsel, (lane & 24) + j);
-  if (sub < k) {
-    const bool active = t < a.T && !r.nan;
-    s.target[t * k + sub] = active ? r.my_e : -1;
-    s.weight[t * k + sub] = active ? (a.renorm ? wsel / ssel : wsel) : 0.0f;
+  const float w = sub < k ? expf(mine - top) / denom : 0.0f;
+  float sum = 0.0f;
+#pragma unroll 1
+  for (int j = 0; j < k; ++j) sum += __shfl_sync(0xffffffffu, w, (lane & 24) + j);
+  if (in && sub < k) s.weight[t * k + sub] = s.nan[t] ? 0.0f : a.renorm ? w / sum : w;
+}
+
+// A candidate of a slot: the fp32 bits of its lowest cost over the servers that host it (none:
+// all ones), then (substitute, away, server, expert) of it, and its loss.
+struct Candidate {
+  unsigned int cost, rest;
+  float loss;
+};
+
+// The candidates of slot i = t k + j on eight lanes: the target, and its substitutes in turn.
+__device__ __forceinline__ void candidates(const Smem& s, const SelSmem& sm, const Args& a, const float* s_Q,
+                                           const float* s_Cq, Candidate* list, int i, int sub) {
+  const int t = i / a.k, target = s.target[i], loc = s.loc[t], nsub = sm.nsub[target];
+#pragma unroll 1
+  for (int c = sub; c <= nsub; c += 8) {
+    const int e = c == 0 ? target : sm.sublist[target * 64 + c - 1];
+    const float loss = c == 0 ? 0.0f : s_Q[target * a.E + e], quality = c == 0 ? 0.0f : s_Cq[target * a.E + e];
+    unsigned int best = ~0u, low = ~0u;
+#pragma unroll 1
+    for (uint32_t pm = sm.pmask[e]; pm; pm &= pm - 1) {
+      const int m = __ffs(pm) - 1;
+      const unsigned int cost = __float_as_uint(__fadd_rn(s.delay[t][m], quality));
+      const unsigned int rest = (c != 0 ? 1u << 31 : 0u) | (m != loc ? 1u << 30 : 0u) |
+                                static_cast<unsigned int>(m) << 8 | static_cast<unsigned int>(e);
+      if (cost < best || (cost == best && rest < low)) {
+        best = cost;
+        low = rest;
+      }
+    }
+    list[c] = Candidate{best, low, loss};
   }
 }
 
-// Alg. 2 of four tokens, eight lanes each.
-__device__ void decide(Smem& s, SelSmem& sm, const Args& a, const Top& r, const State& st, const float* s_Q,
-                       const float* s_Cq, int t, int sub) {
+// Alg. 2 of a token on eight lanes, slots in rank order: the costs, the order and the ties of
+// select_slots. lists: the candidates of its slots.
+__device__ __forceinline__ void decide(Smem& s, SelSmem& sm, const Args& a, const Candidate* lists, int t, int sub,
+                                       int lane) {
   const int k = a.k;
-  const bool active = t < a.T && !r.nan;
-  if (t < a.T && r.nan && sub == 0 && blockIdx.x == 0) report(&g_err_route, ORDERMOE_DEV_NAN_LOGIT, t);
-  if (sub < k) {
-    s.chosen[t * k + sub] = -1;
-    s.server[t * k + sub] = 0;
-    s.kind[t * k + sub] = 0;
+  const bool in = t < a.T;
+  if (!in) t = 0;
+  const bool speaks = in && sub == 0 && blockIdx.x == 0, bad = s.nan[t] || !s.placed[t];
+  if (speaks && bad) report(&g_err_route, s.nan[t] ? ORDERMOE_DEV_NAN_LOGIT : ORDERMOE_DEV_BAD_INDEX, t);
+  const int mine = sub < k ? s.target[t * k + sub] : -1;
+  unsigned long long taken = mine >= 0 ? 1ull << mine : 0ull;
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) taken |= __shfl_xor_sync(0xffffffffu, taken, o);
+  const int loc = s.loc[t];
+  const float qbar = s.qbar;
+  float q = s.qhat[t];
+  int first_server = loc;
+#pragma unroll 1
+  for (int j = 0; j < k; ++j) {
+    const int target = __shfl_sync(0xffffffffu, mine, (lane & 24) + j), nsub = sm.nsub[target];
+    unsigned long long best = ~0ull;
+    float loss = 0.0f;
+#pragma unroll 1
+    for (int c = sub; c <= nsub; c += 8) {
+      const Candidate v = lists[j * 64 + c];
+      const unsigned long long key = static_cast<unsigned long long>(v.cost) << 32 | v.rest;
+      const bool open = c == 0 || (!((taken >> (v.rest & 63u)) & 1ull) && __fadd_rn(q, v.loss) <= qbar);  // Eq. 40
+      if (open && key < best) {
+        best = key;
+        loss = v.loss;
+      }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
+      const float its = __shfl_xor_sync(0xffffffffu, loss, o);
+      if (other < best) {
+        best = other;
+        loss = its;
+      }
+    }
+    const unsigned int rest = static_cast<unsigned int>(best);
+    const bool none = best == ~0ull;
+    const int issub = none ? 0 : rest >> 31;
+    const int kd = none ? 0 : 2 * ((rest >> 30) & 1u) + issub;
+    const int kstar = none ? target : rest & 0xFFu, mstar = none ? loc : (rest >> 8) & 0xFFu;
+    if (issub) {
+      taken |= 1ull << kstar;
+      q = __fadd_rn(q, loss);
+    }
+    if (j == 0) first_server = mstar;
+    if (speaks && !bad) {
+      if (none) report(&g_err_route, ORDERMOE_DEV_NO_CANDIDATE, t);
+      atomicAdd(&sm.kind[kd], 1);
+    }
+    if (in && sub == 0) {
+      s.chosen[t * k + j] = bad ? -1 : kstar;
+      s.server[t * k + j] = static_cast<uint8_t>(mstar);
+      s.kind[t * k + j] = static_cast<uint8_t>(kd);
+    }
   }
-  if (sub == 0) {
-    s.loc[t] = static_cast<uint8_t>(st.loc);
-    s.qhat[t] = st.q;
+  if (in && sub == 0 && !bad) {
+    s.loc[t] = static_cast<uint8_t>(first_server);
+    s.qhat[t] = q;
   }
-  __syncwarp();
-  int kind_count[4] = {0, 0, 0, 0};
-  select_slots(t, active, sub, r.idx, a.E, k, st.M, st.qbar, s.delay[t], sm, s_Q, s_Cq, st.home, st.loc, st.q,
-               s.loc, s.qhat, s.chosen, s.server, s.kind, kind_count);
-  if (blockIdx.x == 0) flush_kind_counts(sm, kind_count, a.counters);
 }
 
-// The ring's position, the same walk in the producer and in the MMA warps. A slot belongs to one
-// MMA warp, which sees its phases in order: a wait by parity tells only a phase from the next.
+// The ring's position, the same walk in the producers and in the MMA warps. A slot belongs to one
+// producer and to one MMA warp, which see its phases in order: a wait by parity tells only a
+// phase from the next, and slots are not consumed in the order in which they are filled.
 struct Ring {
   int slot = 0, stages;
   uint32_t phase = 0;
@@ -336,8 +411,8 @@ struct Ring {
 };
 
 // A CTA's contiguous share of the down stages: row tiles outer, chosen experts, then
-// K stages. The first n CTAs have at least one stage each, stage i belongs to CTA
-// ((i + 1) n - 1) / total.
+// K stages. The first n CTAs have four stages or more each (a few MMA warps work at once and a
+// row tile has fewer partials); stage i belongs to CTA ((i + 1) n - 1) / total.
 struct Share {
   long long total, begin, end;
   int per_tile, per_expert, n;
@@ -345,7 +420,7 @@ struct Share {
     per_expert = dff / (64 * KB_DOWN);
     per_tile = per_expert * n_act;
     total = static_cast<long long>(d / rows) * per_tile;
-    n = total < G ? static_cast<int>(total) : G;
+    n = total < 4ll * G ? static_cast<int>((total + 3) / 4) : G;
     begin = c < n ? total * c / n : total;
     end = c < n ? total * (c + 1) / n : total;
   }
@@ -396,6 +471,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int G = gridDim.x, cta = blockIdx.x;
   volatile int* abort = &s.abort;
 
+  if (warp == MMA_WARPS + PRODUCERS && lane < static_cast<int>(sizeof(Maps) / sizeof(CUtensorMap)))
+    tma_prefetch_map(reinterpret_cast<const CUtensorMap*>(&maps) + lane);
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(&s.full[i], 1);
@@ -435,7 +512,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   // The producer walks the stages as a converged warp and one elected lane issues: a lane
   // walking alone took about 550 cycles a stage whatever its bytes (1 token on 8 wide
   // experts 190 us).
+  // Two of them take the slots in turn: one issued a stage of two or three boxes in about 0.17
+  // us, 8 KB of weights at the rate of HBM.
   const bool issuer = elect_one();
+  const int producer = warp >= MMA_WARPS && warp < MMA_WARPS + PRODUCERS ? warp - MMA_WARPS : -1;
+  auto mine = [&]() { return ring_at.slot % PRODUCERS == producer; };
   auto claim = [&](uint32_t bytes) {  // the next slot, its barrier set; false: give up
     if (!__all_sync(0xffffffffu, mbar_wait(&s.empty[ring_at.slot], ring_at.phase ^ 1u, a.limit_ns, abort))) {
       if (issuer) timeout(31);
@@ -538,17 +619,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   };
   // ---------------------------------------------------------------- route
   const uint32_t rank = cluster_ctarank();
-  auto route = [&](auto row_tiles, State& st) {
-    // stages of all experts' rows (RT tiles of 16) by KB blocks of K, the first half of them
-    // in rank 0
-    constexpr int RT = decltype(row_tiles)::value, KB = RT == 4 && MT == 1 ? 1 : 2;
+  auto route = [&](auto row_tiles) {
+    // stages of all experts' rows (RT tiles of 16) by KB blocks of K, the first half of them in
+    // rank 0
+    constexpr int RT = decltype(row_tiles)::value, KB = route_kb(MT, RT);
     constexpr uint32_t W = RT * 2048 * KB;
     const int all = a.d / (64 * KB), half = (all + 1) / 2;
     const int s0 = rank == 0 ? 0 : half, s1 = rank == 0 ? half : all;
-    if (warp == PRODUCER) {
-      for (int i = s0; i < s1; ++i) {
-        if (!claim(W + KB * 1024 * NT)) break;
-        if (issuer) {
+    if (producer >= 0) {
+      bool ok = true;
+      for (int i = s0; i < s1 && ok; ++i) {
+        if (mine() && (ok = claim(W + a.T * KB * 128)) && issuer) {
           uint8_t* p = slot_ptr(ring_at.slot);
           tma_load_3d(p, &maps.Wr, &s.full[ring_at.slot], 0, i * KB);
           tma_load_3d(p + C::W_BYTES, &maps.Xr, &s.full[ring_at.slot], 0, i * KB);
@@ -556,7 +637,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         ring_at.next();
       }
     } else if (warp < MMA_WARPS) {
-      if (warp < TOKENS / 4) st = load_state(s, a, warp * 4 + (lane >> 3), lane & 7);
+      load_states(s, a, warp, lane);
       tables_ok = load_tables_range(a.tab, a.E, sm, s_Q, s_Cq, tid, 32 * MMA_WARPS);
       float acc[RT][NT][4] = {};
       bool ok = true;
@@ -564,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (ring_at.slot % MMA_WARPS == warp) {
           if (!(ok = arrived())) break;
           const uint32_t w = ring0 + ring_at.slot * C::STAGE_BYTES;
-          mma_stage<RT, NT, KB>(acc, w, 2048 * RT, 1024, 2048, w + C::W_BYTES, lane);
+          mma_stage<RT, NT, KB>(acc, w, 2048 * RT, 1024, 2048, w + C::W_BYTES, a.T, lane);
           release();
         }
         ring_at.next();
@@ -588,18 +669,28 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   };
   if (!a.given) {
-    State st{};
-    if (a.E <= 16) route(std::integral_constant<int, 1>{}, st);
-    else if (a.E <= 32) route(std::integral_constant<int, 2>{}, st);
-    else route(std::integral_constant<int, 4>{}, st);
+    if (a.E <= 16) route(std::integral_constant<int, 1>{});
+    else if (a.E <= 32) route(std::integral_constant<int, 2>{});
+    else route(std::integral_constant<int, 4>{});
     cluster_sync();  // the peer's half of the logits is here
-    if (warp < 2 * (TOKENS / 4)) {  // warps 0-3 decide, 4-7 weigh: four tokens each
-      const int t = (warp % (TOKENS / 4)) * 4 + (lane >> 3), sub = lane & 7;
-      Top r;
-      top_k(r, s, t, sub, lane, a.E, a.k);
-      if (warp >= TOKENS / 4) weigh(s, a, r, t, sub, lane);
-      else if (tables_ok) decide(s, sm, a, r, st, s_Q, s_Cq, t, sub);  // the same for the block
-      else if (sub < a.k) s.chosen[t * a.k + sub] = -1;
+    if (warp < MMA_WARPS) {
+      Candidate* lists = reinterpret_cast<Candidate*>(ring);  // [T * k][64]
+      const int group = warp * 4 + (lane >> 3), sub = lane & 7;
+#pragma unroll 1
+      for (int t = warp; t < a.T; t += MMA_WARPS) top_k(s, a, t, lane);
+      mma_warps_sync();
+      if (tables_ok)  // the same for the block
+#pragma unroll 1
+        for (int i = group; i < a.T * a.k; i += 4 * MMA_WARPS)
+          candidates(s, sm, a, s_Q, s_Cq, lists + i * 64, i, sub);
+      mma_warps_sync();
+      // four warps decide, four weigh: four tokens each
+      static_assert(MMA_WARPS * 2 == TOKENS, "four tokens a warp");
+      const int t = group % TOKENS;
+      if (group >= TOKENS) weigh(s, a, t, sub, lane);
+      else if (tables_ok) decide(s, sm, a, lists + (t < a.T ? t : 0) * a.k * 64, t, sub, lane);
+      else if (t < a.T && sub < a.k) s.chosen[t * a.k + sub] = -1;
+      fence_proxy_async();  // the ring's memory is TMA's again
     }
   } else {
     for (int i = tid; i < a.T * a.k; i += THREADS) {
@@ -612,6 +703,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   // The chosen experts in ascending order, the tokens that use them and their gate weights. A
   // token counts when all of its slots were decided.
   if (tid < a.T) {
+    if (!a.given && s.nan[tid])
+      for (int j = 0; j < a.k; ++j) s.target[tid * a.k + j] = -1;  // no targets
     bool ok = s.target[tid * a.k] >= 0;
     for (int j = 0; j < a.k; ++j) ok = ok && s.chosen[tid * a.k + j] >= 0 && s.chosen[tid * a.k + j] < a.E;
     s.valid[tid] = ok;
@@ -631,24 +724,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (hi) s.act[__popc(l) + __popc(h & before)] = static_cast<uint8_t>(lane + 32);
     if (lane == 0) s.n_act = __popc(l) + __popc(h);
   }
-  if (cta == 0 && !a.given && !*abort) {  // one CTA writes the decisions
-    for (int i = tid; i < a.T * a.k; i += THREADS) {
-      const bool ok = s.target[i] >= 0 && s.chosen[i] >= 0;
-      a.topk_idx[i] = s.target[i];
-      a.topk_w[i] = s.weight[i];
-      if (ok) {
-        a.chosen[i] = s.chosen[i];
-        a.server[i] = s.server[i];
-        a.kind[i] = s.kind[i];
-      }
-    }
-    if (a.logits != nullptr)
-      for (int i = tid; i < a.T * a.E; i += THREADS) {
-        const int t = i / a.E, e = i - t * a.E;
-        a.logits[i] = s.logits[0][t][e] + s.logits[1][t][e];
-      }
-    if (a.counters != nullptr && tid < 4 && sm.kind[tid]) atomicAdd(&a.counters[tid], sm.kind[tid]);
-  }
   __syncthreads();
 
   // -------------------------------------------------------------- gate/up
@@ -656,13 +731,12 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int per = a.dff / (8 * MT);  // units of an expert
   const int n_units = n_act * per;
   const Share share(a.d, a.dff, C::DOWN_ROWS, n_act, cta, G);
-  if (warp == PRODUCER) {
+  if (producer >= 0) {
     bool ok = true;
     for (int u = cta; u < n_units && ok; u += G) {
       const int row = s.act[u / per] * a.dff + (u % per) * 8 * MT;
-      for (int kb = 0; kb < k_up; ++kb) {
-        if (!(ok = claim(C::STAGE_BYTES))) break;
-        if (issuer) {
+      for (int kb = 0; kb < k_up && ok; ++kb) {
+        if (mine() && (ok = claim(C::W_BYTES + a.T * KB_UP * 128)) && issuer) {
           uint8_t* p = slot_ptr(ring_at.slot);
           tma_load_3d(p, &maps.W1, &s.full[ring_at.slot], row, kb * KB_UP);
           tma_load_3d(p + C::W_BYTES / 2, &maps.W3, &s.full[ring_at.slot], row, kb * KB_UP);
@@ -673,24 +747,34 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     // down: the weights of a stage as soon as its slot is free, H behind the barrier
     // that every CTA's gate/up passes
-    const uint32_t bytes = C::W_BYTES + 2048 * NT;
+    const uint32_t bytes = C::W_BYTES + a.T * KB_DOWN * 128;
     Walk w(share), hw(share);
     Ring first = ring_at;
     auto load_w = [&]() {
       if (issuer)
         tma_load_3d(slot_ptr(ring_at.slot), &maps.W2, &s.full[ring_at.slot],
                     s.act[w.act] * a.d + w.tile * C::DOWN_ROWS, w.k * KB_DOWN);
-      ring_at.next();
-      w.next(share, n_act);
     };
     auto load_h = [&]() {
       if (issuer)
         tma_load_3d(slot_ptr(first.slot) + C::W_BYTES, &maps.H, &s.full[first.slot], hw.act * a.T,
                     hw.k * KB_DOWN);
+    };
+    auto next_w = [&]() {
+      ring_at.next();
+      w.next(share, n_act);
+    };
+    auto next_h = [&]() {
       first.next();
       hw.next(share, n_act);
     };
-    while (ok && w.left > 0 && hw.left - w.left < STAGES && (ok = claim(bytes))) load_w();
+    while (ok && w.left > 0 && hw.left - w.left < STAGES) {
+      if (mine()) {
+        if (!(ok = claim(bytes))) break;
+        load_w();
+      }
+      next_w();
+    }
     if (ok) {
       const bool up = !issuer || grid_wait(&a.sync[0], G, a.limit_ns, abort);
       if (!up) timeout(35);
@@ -698,10 +782,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     fence_proxy_async();
     // (also after a failure: the barriers of the stages under way expect these bytes)
-    while (hw.left > w.left) load_h();
-    while (ok && w.left > 0 && (ok = claim(bytes))) {
-      load_w();
-      load_h();
+    while (hw.left > w.left) {
+      if (first.slot % PRODUCERS == producer) load_h();
+      next_h();
+    }
+    while (ok && w.left > 0) {
+      if (mine()) {
+        if (!(ok = claim(bytes))) break;
+        load_w();
+        load_h();
+      }
+      next_w();
+      next_h();
     }
   } else if (warp < MMA_WARPS) {
     bool ok = true;
@@ -712,7 +804,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (ring_at.slot % MMA_WARPS == warp) {
             if (!(ok = arrived())) break;
             const uint32_t w = ring0 + ring_at.slot * C::STAGE_BYTES;
-            mma_stage<MT, NT, KB_UP>(acc, w, 1024 * MT, 4096 * MT, 1024, w + C::W_BYTES, lane);
+            mma_stage<MT, NT, KB_UP>(acc, w, 1024 * MT, 4096 * MT, 1024, w + C::W_BYTES, a.T, lane);
             release();
           }
           ring_at.next();
@@ -726,7 +818,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (ring_at.slot % MMA_WARPS == warp) {
         if (!(ok = arrived())) break;
         const uint32_t p = ring0 + ring_at.slot * C::STAGE_BYTES;
-        mma_stage<2 * MT, NT, KB_DOWN>(acc, p, 4096 * MT, 1024, 2048, p + C::W_BYTES, lane);
+        mma_stage<2 * MT, NT, KB_DOWN>(acc, p, 4096 * MT, 1024, 2048, p + C::W_BYTES, a.T, lane);
         release();
         any = true;
       }
@@ -758,6 +850,22 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (w.tile != tile || w.left == 0) ok = put_tile(tot);
     }
   } else {
+    if (cta == 0 && !a.given && !*abort) {  // one warp of the grid writes the decisions
+      for (int i = lane; i < a.T * a.k; i += 32) {
+        const bool ok = s.target[i] >= 0 && s.chosen[i] >= 0;
+        a.topk_idx[i] = s.target[i];
+        a.topk_w[i] = s.weight[i];
+        if (ok) {
+          a.chosen[i] = s.chosen[i];
+          a.server[i] = s.server[i];
+          a.kind[i] = s.kind[i];
+        }
+      }
+      if (a.logits != nullptr)
+        for (int t = 0; t < a.T; ++t)
+          for (int e = lane; e < a.E; e += 32) a.logits[t * a.E + e] = s.logits[0][t][e] + s.logits[1][t][e];
+      if (a.counters != nullptr && lane < 4 && sm.kind[lane]) atomicAdd(&a.counters[lane], sm.kind[lane]);
+    }
     bool ok = true;
     for (int u = cta; u < n_units && ok; u += G) {
       const int e = u / per, f0 = (u - e * per) * 8 * MT + (lane >> 2);
@@ -811,62 +919,75 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int first_tile = tiles * part / parts, last_tile = tiles * (part + 1) / parts;
     // the first and last owner of every row tile, while the others finish (the ring is free)
     int16_t* own = reinterpret_cast<int16_t*>(ring);
-    const int cap = STAGES * C::STAGE_BYTES / 4;  // tiles that fit
-    const bool listed = tiles <= cap;
-    auto owners = [&](int tile, int& c0, int& c1) {
-      c0 = share.owner(static_cast<long long>(tile) * share.per_tile);
-      c1 = share.owner(static_cast<long long>(tile + 1) * share.per_tile - 1);
-    };
-    if (listed && share.total > 0)
+    uint2* s_row = reinterpret_cast<uint2*>(ring + MAX_D / 32 * 4);  // the token's row of h_out
+    if (share.total > 0)
       for (int i = first_tile + tid; i < last_tile; i += THREADS) {
-        int c0, c1;
-        owners(i, c0, c1);
-        own[2 * i] = static_cast<int16_t>(c0);
-        own[2 * i + 1] = static_cast<int16_t>(c1);
+        own[2 * i] = static_cast<int16_t>(share.owner(static_cast<long long>(i) * share.per_tile));
+        own[2 * i + 1] = static_cast<int16_t>(share.owner(static_cast<long long>(i + 1) * share.per_tile - 1));
       }
     if (tid == 0 && !grid_wait(&a.sync[1], G, a.limit_ns, abort)) timeout(36);
     __syncthreads();
     for (int t = cta % a.T; t < a.T && !*abort; t += G) {
       if (!s.valid[t]) continue;
       float sq = 0.0f;
-      const size_t row = static_cast<size_t>(t) * a.d;
-      for (int c = first_tile * C::DOWN_ROWS + tid * 4; c < last_tile * C::DOWN_ROWS; c += THREADS * 4) {
-        const int tile = c / C::DOWN_ROWS;
-        uint2 hv = make_uint2(0, 0);
-        if (a.h != nullptr) hv = *reinterpret_cast<const uint2*>(a.h + row + c);
-        int c0, c1;
-        if (listed) {
-          c0 = own[2 * tile];
-          c1 = own[2 * tile + 1];
-        } else {
-          owners(tile, c0, c1);
+      const size_t row = static_cast<size_t>(t) * a.d, pitch = static_cast<size_t>(a.T) * C::DOWN_ROWS;
+      const int end = last_tile * C::DOWN_ROWS;
+      // four groups of columns a thread, four partials of each: sixteen loads under way
+#pragma unroll 1
+      for (int c = first_tile * C::DOWN_ROWS + tid * 4; c < end; c += 4 * THREADS * 4) {
+        const float* p[4];
+        int n[4];
+        uint2 hv[4];
+        float4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int cj = c + j * THREADS * 4, tile = cj / C::DOWN_ROWS;
+          int c0 = 0, c1 = -1;
+          if (cj < end) {
+            c0 = own[2 * tile];
+            c1 = own[2 * tile + 1];
+          }
+          n[j] = c1 - c0 + 1;
+          p[j] = a.part + (static_cast<size_t>(tile + c0) * a.T + t) * C::DOWN_ROWS + cj % C::DOWN_ROWS;
+          hv[j] = make_uint2(0, 0);
+          if (a.h != nullptr && cj < end) hv[j] = *reinterpret_cast<const uint2*>(a.h + row + cj);
+          v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
-        const size_t pitch = static_cast<size_t>(a.T) * C::DOWN_ROWS;
-        const float* p = a.part + (static_cast<size_t>(tile + c0) * a.T + t) * C::DOWN_ROWS + c % C::DOWN_ROWS;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int q = c0; q <= c1; q += 4, p += 4 * pitch) {  // four loads under way
-          float4 u[4];
+        const int most = max(max(n[0], n[1]), max(n[2], n[3]));
+#pragma unroll 1
+        for (int q = 0; q < most; q += 4) {
+          float4 u[4][4];
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (q + j <= c1) u[j] = __ldcg(reinterpret_cast<const float4*>(p + j * pitch));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (q + i < n[j]) u[j][i] = __ldcg(reinterpret_cast<const float4*>(p[j] + (q + i) * pitch));
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (q + j <= c1) {
-              v.x += u[j].x;
-              v.y += u[j].y;
-              v.z += u[j].z;
-              v.w += u[j].w;
-            }
-        }
-        v.x += bf16_lo(hv.x);
-        v.y += bf16_hi(hv.x);
-        v.z += bf16_lo(hv.y);
-        v.w += bf16_hi(hv.y);
-        const uint2 o = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-        *reinterpret_cast<uint2*>(a.y + row + c) = o;
-        const float f[4] = {bf16_lo(o.x), bf16_hi(o.x), bf16_lo(o.y), bf16_hi(o.y)};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sq = fmaf(f[j], f[j], sq);
+            for (int i = 0; i < 4; ++i)
+              if (q + i < n[j]) {
+                v[j].x += u[j][i].x;
+                v[j].y += u[j][i].y;
+                v[j].z += u[j][i].z;
+                v[j].w += u[j][i].w;
+              }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int cj = c + j * THREADS * 4;
+          if (cj >= end) continue;
+          v[j].x += bf16_lo(hv[j].x);
+          v[j].y += bf16_hi(hv[j].x);
+          v[j].z += bf16_lo(hv[j].y);
+          v[j].w += bf16_hi(hv[j].y);
+          const uint2 o = make_uint2(pack_bf16x2(v[j].x, v[j].y), pack_bf16x2(v[j].z, v[j].w));
+          *reinterpret_cast<uint2*>(a.y + row + cj) = o;
+          s_row[cj / 4] = o;
+          const float f[4] = {bf16_lo(o.x), bf16_hi(o.x), bf16_lo(o.y), bf16_hi(o.y)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sq = fmaf(f[i], f[i], sq);
+        }
       }
       if (a.h == nullptr) continue;
 #pragma unroll
@@ -879,7 +1000,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int w = 0; w < THREADS / 32; ++w) total += s.sum[w];
       const float r = 1.0f / sqrtf(total / static_cast<float>(a.d) + a.eps);
       for (int c = tid * 4; c < a.d; c += THREADS * 4) {  // each thread's own columns again
-        const uint2 o = *reinterpret_cast<const uint2*>(a.y + row + c);
+        const uint2 o = s_row[c / 4];
         *reinterpret_cast<uint2*>(a.x_out + row + c) =
             make_uint2(pack_bf16x2(bf16_lo(o.x) * r, bf16_hi(o.x) * r),
                        pack_bf16x2(bf16_lo(o.y) * r, bf16_hi(o.y) * r));
@@ -892,7 +1013,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   }
   __syncthreads();
-  if (s.abort && warp == PRODUCER && issuer) {  // every copy that this CTA issued (bounded)
+  if (s.abort && producer >= 0 && issuer) {  // every copy that this CTA issued (bounded)
     volatile int* never = &s.zero;
     for (int i = 0; i < STAGES; ++i)
       if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
@@ -965,14 +1086,14 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   const int R = a.T * a.k, act = R < a.E ? R : a.E;
   fw::Maps m;
   int rc;
-  const int rt = a.E <= 16 ? 1 : a.E <= 32 ? 2 : 4, kb = rt == 4 && MT == 1 ? 1 : 2;  // as the kernel's route
+  const int rt = a.E <= 16 ? 1 : a.E <= 32 ? 2 : 4, kb = fw::route_kb(MT, rt);  // as the kernel's route
   if ((rc = make_tmap_bf16_kb(&m.Wr, L->W_r, a.E, a.d, 16 * rt, kb))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.Xr, X, a.T, a.d, 8 * NT, kb))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.X, X, a.T, a.d, 8 * NT, fw::KB_UP))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.Xr, X, a.T, a.d, a.T, kb))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.X, X, a.T, a.d, a.T, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W1, L->W1, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W3, L->W3, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W2, L->W2, (uint64_t)a.E * a.d, a.dff, C::DOWN_ROWS, fw::KB_DOWN))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.H, a.H, (uint64_t)act * a.T, a.dff, 8 * NT, fw::KB_DOWN))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.H, a.H, (uint64_t)act * a.T, a.dff, a.T, fw::KB_DOWN))) return rc;
   a.stages = fw::stages<MT, NT>(a.E);
   // a CTA per SM, fewer where there are not as many units of gate/up
   int grid = num_sms() < kFewMaxCtas ? num_sms() : kFewMaxCtas;
@@ -1020,6 +1141,7 @@ static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: need 1 <= k <= min(E, 8), E <= 64", who);
   if (L->d <= 0 || L->d % 256 != 0 || L->dff <= 0 || L->dff % 128 != 0)
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: need d %% 256 == 0 and dff %% 128 == 0", who);
+  if (L->d > fw::MAX_D) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: need d <= %d", who, fw::MAX_D);
   if ((long long)L->E * L->dff > INT32_MAX || (long long)L->E * L->d > INT32_MAX)
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: sizes too large", who);
   if (L->lookahead_H > 4) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: look-ahead of at most 4 layers", who);
