@@ -67,10 +67,10 @@ struct Smem {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];
   uint64_t red_full[3], red_empty[3];  // a unit's two sets; [2]: a row tile's
   int abort, zero;
-  int n_act;                       // chosen experts
+  int tables_ok;                   // the header fits the layer
   uint8_t act[64];                 // their indices, ascending
   unsigned int mask[64];           // of an expert: the tokens that use it
-  float gate[64][TOKENS];          // and their gate weights
+  uint8_t slot[64][TOKENS];        // and the slot it is of each
   float logits[2][TOKENS][68];     // shares of K of either CTA; [0] is -inf past E
   alignas(16) float ex[TOKENS][68];  // exponentials of the softmax, read 16 bytes at a time
   float delay[TOKENS][ORDERMOE_MAX_SERVERS];  // A[home][location] of the tokens
@@ -212,25 +212,51 @@ __device__ __forceinline__ void store_both(float* p, uint32_t peer, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(p), peer)), "f"(v) : "memory");
 }
 
-// The tokens' states and delay rows into shared memory, a token a warp in turn, while the
-// router's products run.
-__device__ __forceinline__ void load_states(Smem& s, const Args& a, int warp, int lane) {
-  const int M = reinterpret_cast<const int32_t*>(a.tab)[2];
-#pragma unroll 1
-  for (int t = warp; t < a.T; t += MMA_WARPS) {
-    const int home = a.home[t];
-    const int loc = a.loc != nullptr ? a.loc[t] : home;  // no state given: first layer (Eq. 36)
-    const bool ok = M > 0 && M <= ORDERMOE_MAX_SERVERS && home < M && loc < M;
-    if (ok && lane < M)
-      s.delay[t][lane] = reinterpret_cast<const float*>(a.tab + off_a(a.E))[(home * M + loc) * M + lane];
-    if (lane == 0) {
-      s.placed[t] = ok;
-      s.loc[t] = static_cast<uint8_t>(loc);
-      s.qhat[t] = a.qhat != nullptr ? a.qhat[t] : 0.0f;
-    }
+// The tables' header, the tokens' states and their delay rows into shared memory, by one warp
+// while the router's products run.
+__device__ __forceinline__ void load_states(Smem& s, const Args& a, int lane) {
+  const int32_t* head = reinterpret_cast<const int32_t*>(a.tab);
+  const int Eh = head[1], M = head[2];
+  const float qbar = reinterpret_cast<const float*>(a.tab)[5];
+  int home = 0, loc = 0;
+  float q = 0.0f;
+  if (lane < a.T) {
+    home = a.home[lane];
+    loc = a.loc != nullptr ? a.loc[lane] : home;  // no state given: first layer (Eq. 36)
+    q = a.qhat != nullptr ? a.qhat[lane] : 0.0f;
   }
-  if (warp == 0 && lane == 0) s.qbar = reinterpret_cast<const float*>(a.tab)[5];
+  const bool good = Eh == a.E && M > 0 && M <= ORDERMOE_MAX_SERVERS;
+  if (lane == 0) {
+    if (!good && blockIdx.x == 0) report(&g_err_route, ORDERMOE_DEV_BAD_INDEX, -1);
+    s.tables_ok = good;
+    s.qbar = qbar;
+  }
+  const bool placed = good && lane < a.T && home < M && loc < M;
+  if (lane < TOKENS) {
+    s.placed[lane] = placed;
+    s.loc[lane] = static_cast<uint8_t>(loc);
+    s.qhat[lane] = q;
+  }
+  const int row = placed ? (home * M + loc) * M : 0;
+#pragma unroll 4
+  for (int t = 0; t < a.T; ++t) {
+    const int r = __shfl_sync(0xffffffffu, row, t);
+    if (good && lane < M) s.delay[t][lane] = reinterpret_cast<const float*>(a.tab + off_a(a.E))[r + lane];
+  }
 }
+
+// Qtab and Cq, one after the other in the tables and in shared memory, without a wait
+// (copies_arrived); E odd: 8 bytes at the end.
+__device__ __forceinline__ void copy_tables(const Args& a, float* s_Q, int t0, int nt) {
+  const uint8_t* src = a.tab + kOffQtab;
+  const uint32_t dst = smem_u32(s_Q);
+  const int n = 8 * a.E * a.E;
+  for (int i = t0 * 16; i + 16 <= n; i += nt * 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i), "l"(src + i) : "memory");
+  if (n % 16 != 0 && t0 == 0)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst + n - 8), "l"(src + n - 8) : "memory");
+}
+__device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ void mma_warps_sync() {
   asm volatile("bar.sync 1, %0;" ::"n"(32 * MMA_WARPS) : "memory");
@@ -384,11 +410,16 @@ __device__ __forceinline__ void decide(Smem& s, SelSmem& sm, const Args& a, cons
       atomicAdd(&sm.kind[kd], 1);
     }
     if (in && sub == 0) {
+      if (!bad) {
+        atomicOr(&s.mask[kstar], 1u << t);
+        s.slot[kstar][t] = static_cast<uint8_t>(j);
+      }
       s.chosen[t * k + j] = bad ? -1 : kstar;
       s.server[t * k + j] = static_cast<uint8_t>(mstar);
       s.kind[t * k + j] = static_cast<uint8_t>(kd);
     }
   }
+  if (in && sub == 0) s.valid[t] = !bad;
   if (in && sub == 0 && !bad) {
     s.loc[t] = static_cast<uint8_t>(first_server);
     s.qhat[t] = q;
@@ -491,7 +522,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     (&s.logits[0][0][0])[i] = -INFINITY;
     (&s.logits[1][0][0])[i] = 0.0f;
   }
-  for (int i = tid; i < 64 * TOKENS; i += THREADS) (&s.gate[0][0])[i] = 0.0f;
   for (int i = tid; i < 64; i += THREADS) s.mask[i] = 0;
   cluster_sync();  // both CTAs run: the peer's shared memory may be written
 
@@ -502,7 +532,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint32_t issued_mask = 0, last_phase_bits = 0;  // the producer's, for the drain after an abort
   const uint32_t ring0 = smem_u32(ring);
   const int k_up = a.d / (64 * KB_UP);
-  bool tables_ok = true;
 
   // --- roles' steps
   auto timeout = [&](int where) {
@@ -637,8 +666,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         ring_at.next();
       }
     } else if (warp < MMA_WARPS) {
-      load_states(s, a, warp, lane);
-      tables_ok = load_tables_range(a.tab, a.E, sm, s_Q, s_Cq, tid, 32 * MMA_WARPS);
+      uint32_t pm = 0;
+      unsigned long long sb = 0;
+      if (tid < 64) {
+        pm = reinterpret_cast<const uint32_t*>(a.tab + kOffPmask)[tid];
+        sb = reinterpret_cast<const unsigned long long*>(a.tab + kOffSubst)[tid];
+      }
+      copy_tables(a, s_Q, tid, 32 * MMA_WARPS);
       float acc[RT][NT][4] = {};
       bool ok = true;
       for (int i = s0; i < s1; ++i) {
@@ -652,7 +686,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (ok) put(acc, row_tiles, 0, 0);
       ++units;
+      if (tid < 64) {
+        sm.pmask[tid] = pm;
+        int n = 0;
+#pragma unroll 1
+        for (; sb; sb &= sb - 1) sm.sublist[tid * 64 + n++] = static_cast<uint8_t>(__ffsll(static_cast<long long>(sb)) - 1);
+        sm.nsub[tid] = n;
+      }
+      copies_arrived();
     } else {
+      load_states(s, a, lane);
       take(row_tiles, 0, 0, 0, [&](int m, int n, float4 v) {
         const int e = m * 16 + (lane >> 2), t = n * 8 + (lane & 3) * 2;
         float* p = &s.logits[rank][t][e];
@@ -679,7 +722,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll 1
       for (int t = warp; t < a.T; t += MMA_WARPS) top_k(s, a, t, lane);
       mma_warps_sync();
-      if (tables_ok)  // the same for the block
+      const bool tables_ok = s.tables_ok;
+      if (tables_ok)
 #pragma unroll 1
         for (int i = group; i < a.T * a.k; i += 4 * MMA_WARPS)
           candidates(s, sm, a, s_Q, s_Cq, lists + i * 64, i, sub);
@@ -689,45 +733,37 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int t = group % TOKENS;
       if (group >= TOKENS) weigh(s, a, t, sub, lane);
       else if (tables_ok) decide(s, sm, a, lists + (t < a.T ? t : 0) * a.k * 64, t, sub, lane);
-      else if (t < a.T && sub < a.k) s.chosen[t * a.k + sub] = -1;
+      else if (t < a.T && sub < a.k) s.valid[t] = 0;
       fence_proxy_async();  // the ring's memory is TMA's again
     }
-  } else {
-    for (int i = tid; i < a.T * a.k; i += THREADS) {
-      s.target[i] = a.topk_idx[i];
-      s.weight[i] = a.topk_w[i];
-      s.chosen[i] = a.chosen[i];
+  } else if (tid < a.T) {  // decided by the look-ahead; a NaN token has no targets
+    bool ok = a.topk_idx[tid * a.k] >= 0;
+    for (int j = 0; j < a.k; ++j) {
+      const int e = a.chosen[tid * a.k + j];
+      ok = ok && e >= 0 && e < a.E;
+      s.weight[tid * a.k + j] = a.topk_w[tid * a.k + j];
     }
-  }
-  __syncthreads();
-  // The chosen experts in ascending order, the tokens that use them and their gate weights. A
-  // token counts when all of its slots were decided.
-  if (tid < a.T) {
-    if (!a.given && s.nan[tid])
-      for (int j = 0; j < a.k; ++j) s.target[tid * a.k + j] = -1;  // no targets
-    bool ok = s.target[tid * a.k] >= 0;
-    for (int j = 0; j < a.k; ++j) ok = ok && s.chosen[tid * a.k + j] >= 0 && s.chosen[tid * a.k + j] < a.E;
+    for (int j = 0; j < a.k && ok; ++j) {  // its experts are distinct
+      const int e = a.chosen[tid * a.k + j];
+      atomicOr(&s.mask[e], 1u << tid);
+      s.slot[e][tid] = static_cast<uint8_t>(j);
+    }
     s.valid[tid] = ok;
-    if (ok)
-      for (int j = 0; j < a.k; ++j) {  // a token's experts are distinct
-        const int e = s.chosen[tid * a.k + j];
-        atomicOr(&s.mask[e], 1u << tid);
-        s.gate[e][tid] += s.weight[tid * a.k + j];
-      }
   }
   __syncthreads();
-  if (warp == 0) {
+  // the chosen experts in ascending order, the same in every warp
+  int n_act;
+  {
     const bool lo = s.mask[lane] != 0, hi = s.mask[lane + 32] != 0;
     const unsigned int l = __ballot_sync(0xffffffffu, lo), h = __ballot_sync(0xffffffffu, hi);
     const unsigned int before = (1u << lane) - 1;
     if (lo) s.act[__popc(l & before)] = static_cast<uint8_t>(lane);
     if (hi) s.act[__popc(l) + __popc(h & before)] = static_cast<uint8_t>(lane + 32);
-    if (lane == 0) s.n_act = __popc(l) + __popc(h);
+    n_act = *abort ? 0 : __popc(l) + __popc(h);
+    __syncwarp();
   }
-  __syncthreads();
 
   // -------------------------------------------------------------- gate/up
-  const int n_act = *abort ? 0 : s.n_act;
   const int per = a.dff / (8 * MT);  // units of an expert
   const int n_units = n_act * per;
   const Share share(a.d, a.dff, C::DOWN_ROWS, n_act, cta, G);
@@ -833,7 +869,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int n = 0; n < NT; ++n) {
           const int t = n * 8 + (lane & 3) * 2;
           const bool u0 = (m >> t) & 1u, u1 = (m >> (t + 1)) & 1u;
-          const float g0 = s.gate[e][t], g1 = s.gate[e][t + 1];
+          const float g0 = u0 ? s.weight[t * a.k + s.slot[e][t]] : 0.0f;
+          const float g1 = u1 ? s.weight[(t + 1) * a.k + s.slot[e][t + 1]] : 0.0f;
 #pragma unroll
           for (int j = 0; j < 2 * MT; ++j) {
             float (&c)[4] = acc[j][n];
@@ -852,8 +889,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else {
     if (cta == 0 && !a.given && !*abort) {  // one warp of the grid writes the decisions
       for (int i = lane; i < a.T * a.k; i += 32) {
-        const bool ok = s.target[i] >= 0 && s.chosen[i] >= 0;
-        a.topk_idx[i] = s.target[i];
+        const bool ok = s.valid[i / a.k], nan = s.nan[i / a.k];
+        a.topk_idx[i] = nan ? -1 : s.target[i];
         a.topk_w[i] = s.weight[i];
         if (ok) {
           a.chosen[i] = s.chosen[i];
