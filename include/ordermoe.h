@@ -242,6 +242,35 @@ int ordermoe_expert_down(const uint16_t* H, const int32_t* offsets, int R, const
                          int E, int d, int dff, uint16_t* Y_perm, ordermoe_stream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Matrix product with an epilogue: the dense products around the experts (a
+ * dense feed-forward layer, as every second layer of Switch-Base-8E is; the
+ * projections of an attention half; an output head):
+ *   Y = act(X W^T + bias) + residual,
+ * fp32 accumulation on tcgen05 tensor cores, bias, activation and residual in
+ * fp32, one rounding to Y.
+ *   X [M][K], W [N][K] bf16, rows ldx / ldw elements apart (multiples of 8,
+ *   >= K), both 16-byte aligned
+ *   bias [N] bf16, nullable
+ *   act: ORDERMOE_ACT_*; GELU is v Phi(v), GELU_TANH its tanh form, SILU v sigmoid(v)
+ *   residual [M][N] bf16, rows ldr apart, nullable
+ *   Y [M][N] out, rows ldy apart: bf16, or float when f32 != 0. Y may be the
+ *   residual itself (the same address and stride); it may not overlap anything
+ *   else that is read. What lies between its rows is left as it was.
+ * Any M >= 0 and N, K > 0. Rows of Y and residual that start at a multiple of 8
+ * bytes (16 for float) with strides that are multiples of 4 are moved 4
+ * elements at a time, others one by one. The sums of a call are in a fixed order. */
+enum {
+  ORDERMOE_ACT_NONE = 0,
+  ORDERMOE_ACT_RELU = 1,
+  ORDERMOE_ACT_GELU = 2,
+  ORDERMOE_ACT_GELU_TANH = 3,
+  ORDERMOE_ACT_SILU = 4
+};
+int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw,
+                    const uint16_t* bias, int act, const uint16_t* residual, int64_t ldr, int M,
+                    int N, int K, void* Y, int64_t ldy, int f32, ordermoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * Weighted combine: y[t] = bf16( sum_{j=0..k-1} topk_w[t][j] * Y_perm[row_of[t][j]] )
  * with fp32 accumulation in slot order.
  *   Y_perm [T*k][d] bf16, row_of [T][k] i32, topk_w [T][k] f32, y [T][d] bf16 out.

@@ -68,12 +68,15 @@ _SIGNATURES = {
     "ordermoe_rmsnorm": ([_P, _I, _I, _F, _P, _P], _I),
     "ordermoe_combine_residual_norm": ([_P, _P, _P, _P, _I, _I, _I, _F, _P, _P, _P], _I),
     "ordermoe_layer_forward_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P], _I),
+    "ordermoe_linear": ([_P, _I64, _P, _I64, _P, _I, _P, _I64, _I, _I, _I, _P, _I64, _I, _P], _I),
     "ordermoe_layer_few_workspace_bytes": ([_I, _I, _I, _I, _I], _SZ),
     "ordermoe_layer_few_init": ([_P, _SZ, _P], _I),
     "ordermoe_layer_few": ([_P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
     "ordermoe_layer_few_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _SZ, _P], _I),
     "ordermoe_transitions_strided": ([_P, _I64, _I, _I, _I, _I64, _I64, _P, _P, _P], _I),
 }
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 FEW_TOKENS = 16  # tokens of an ordermoe_layer_few call, at most
 
@@ -465,6 +468,46 @@ def _here(*tensors):
         if t is not None and t.is_cuda and t.device.index != dev:
             raise ValueError("tensor on cuda:%d, but the current device is cuda:%d"
                              % (t.device.index, dev))
+
+
+def _matrix(t, name, dtypes, rows=None, cols=None):
+    """Address and row stride of a device matrix whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise TypeError("%s must be a matrix" % name)
+    if t.dtype not in dtypes:
+        raise TypeError("%s must be %s, got %s" % (name, " or ".join(map(str, dtypes)), t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be on a CUDA device" % name)
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError("%s must be %s x %s, got %s" % (name, rows, cols, tuple(t.shape)))
+    ld = t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8  # (one row: any)
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and ld < t.shape[1]):
+        raise ValueError("the rows of %s must be contiguous and apart" % name)
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def ordermoe_linear(X, W, Y, bias=None, act="none", residual=None, stream=None):
+    """Y = act(X W^T + bias) + residual: X [M, K], W [N, K], residual [M, N] bf16, Y [M, N] bf16
+    or float32, bias [N] bf16; rows may lie in wider buffers (strides are taken from the
+    tensors). act: a name of ACTIVATIONS. Y may be the residual."""
+    if act not in ACTIVATIONS:
+        raise ValueError("unknown activation %r" % (act,))
+    bf16 = (torch.bfloat16,)
+    x, ldx = _matrix(X, "X", bf16)
+    M, K = X.shape
+    w, ldw = _matrix(W, "W", bf16, cols=K)
+    N = W.shape[0]
+    y, ldy = _matrix(Y, "Y", (torch.bfloat16, torch.float32), M, N)
+    r, ldr = _matrix(residual, "residual", bf16, M, N)
+    _dt(bias, torch.bfloat16, "bias")
+    if bias is not None and bias.numel() != N:
+        raise ValueError("bias must have %d entries" % N)
+    _here(X, W, Y, residual, bias)
+    _check("ordermoe_linear", lib().ordermoe_linear(
+        x, ldx, w, ldw, _ptr(bias), ACTIVATIONS[act], r, ldr, M, N, K, y, ldy,
+        int(Y.dtype == torch.float32), _stream(stream)))
 
 
 def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):

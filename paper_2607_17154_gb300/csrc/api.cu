@@ -14,6 +14,7 @@ int read_clear_err_sim(unsigned long long* out);
 int read_clear_err_cost(unsigned long long* out);
 int read_clear_err_simtc(unsigned long long* out);
 int read_clear_err_few(unsigned long long* out);
+int read_clear_err_linear(unsigned long long* out);
 int selftest_wait_timeout(uint64_t limit_ns, cudaStream_t stream);
 
 static thread_local char t_msg[512] = "";
@@ -59,7 +60,7 @@ extern "C" int ordermoe_device_error(int* code, int* detail) {
   OM_TRACE();
   if (!code) return fail(ORDERMOE_ERR_INVALID_ARG, "device_error: null code");
   OM_CUDA(cudaDeviceSynchronize());
-  unsigned long long words[7] = {0, 0, 0, 0, 0, 0, 0};
+  unsigned long long words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   int rc;
   if ((rc = read_clear_err_route(&words[0]))) return rc;
   if ((rc = read_clear_err_dispatch(&words[1]))) return rc;
@@ -68,6 +69,7 @@ extern "C" int ordermoe_device_error(int* code, int* detail) {
   if ((rc = read_clear_err_cost(&words[4]))) return rc;
   if ((rc = read_clear_err_simtc(&words[5]))) return rc;
   if ((rc = read_clear_err_few(&words[6]))) return rc;
+  if ((rc = read_clear_err_linear(&words[7]))) return rc;
   *code = 0;
   if (detail) *detail = 0;
   for (unsigned long long w : words) {

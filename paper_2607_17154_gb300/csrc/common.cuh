@@ -23,6 +23,9 @@ int num_sms();                                     // SM count of the current de
 // rows, 128-byte swizzle, zero fill out of bounds.
 int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
                    uint32_t box_rows);
+// The same with rows ld elements apart (a multiple of 8).
+int make_tmap_bf16_ld(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                      uint32_t box_rows);
 // The same tensor as [cols / 64][rows][64] (cols % 64 == 0): a box of box_kb blocks of 64
 // columns x box_rows rows, block after block.
 int make_tmap_bf16_kb(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,

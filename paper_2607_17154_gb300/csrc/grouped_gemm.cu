@@ -796,10 +796,15 @@ int make_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols) {
 
 int make_tmap_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols,
                    uint32_t box_rows) {
+  return make_tmap_bf16_ld(map, base, rows, cols, cols, box_rows);
+}
+
+int make_tmap_bf16_ld(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                      uint32_t box_rows) {
   gg::EncodeTiledFn enc = gg::encode_fn();
   if (!enc) return fail(ORDERMOE_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
   cuuint64_t dims[2] = {cols, rows};
-  cuuint64_t strides[1] = {cols * 2};
+  cuuint64_t strides[1] = {ld * 2};
   cuuint32_t box[2] = {gg::BK, box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,

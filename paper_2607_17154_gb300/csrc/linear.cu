@@ -1,0 +1,661 @@
+// Matrix product with an epilogue: Y = act(X W^T + bias) + residual, X [M][K] and W [N][K]
+// bf16 with row strides, fp32 sums on tcgen05, one rounding to Y (bf16) or none (f32).
+//
+// The weights are the MMA's M side and the rows of X its N side, as in the expert GEMMs: few
+// rows waste little of the tensor pipe, and the accumulator is transposed (TMEM lane =
+// output column), so a chunk of 32 rows x 128 columns goes through shared memory once and each
+// thread then adds bias, activation and residual to 4 columns of a row and writes them.
+//   linear_split_kernel: one tile of 128 columns x up to 128 rows a cluster of S CTAs, which
+//     share its K and add their accumulators through distributed shared memory, every CTA the
+//     rows of its own share in rank order (the same bits at every call). For few rows, whose
+//     weights are one pass over HBM: all SMs stream them, two CTAs on one.
+//   linear_pair_kernel: persistent CTA pairs, tiles of 256 columns x up to 256 rows with
+//     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
+//     main loop. For batches with a tile for most pairs, bound by the tensor cores.
+// Rows and columns past M, N and K are zero-filled by TMA and not stored. Every wait is bounded; one that
+// runs out reports ORDERMOE_DEV_WAIT_TIMEOUT, and the copies and MMAs under way are drained.
+#include "common.cuh"
+
+namespace om {
+
+static __device__ unsigned long long g_err_linear = 0;
+
+int read_clear_err_linear(unsigned long long* out) {
+  unsigned long long zero = 0;
+  OM_CUDA(cudaMemcpyFromSymbol(out, g_err_linear, sizeof(*out)));
+  OM_CUDA(cudaMemcpyToSymbol(g_err_linear, &zero, sizeof(zero)));
+  return ORDERMOE_OK;
+}
+
+namespace ln {
+
+constexpr int BK = 64;                 // K block: 128 bytes a row
+constexpr int W_BYTES = 128 * BK * 2;  // 128 weight rows of a K block
+
+struct Epilogue {
+  int M, N;
+  const uint16_t* bias;      // nullable
+  const uint16_t* residual;  // nullable; may be Y
+  void* Y;
+  int64_t ldr, ldy;
+  int act, f32;
+  int vec_r, vec_y;          // 4 columns at a time: strides and addresses allow it
+};
+
+// Each activation in fp32 from the product's sum; NaN stays NaN.
+__device__ __forceinline__ float activate(float v, int act) {
+  switch (act) {
+    case ORDERMOE_ACT_RELU: return v < 0.0f ? 0.0f : v;
+    // v Phi(v); erfc keeps the digits of a negative v's tail, which 1 + erf loses
+    case ORDERMOE_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
+    // 0.5 v (1 + tanh u) = v / (1 + e^-2u), u = sqrt(2/pi) (v + 0.044715 v^3)
+    case ORDERMOE_ACT_GELU_TANH:
+      return v / (1.0f + expf(-1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
+    case ORDERMOE_ACT_SILU: return v / (1.0f + expf(-v));
+    default: return v;
+  }
+}
+
+__device__ __forceinline__ void load_bias4(float (&b)[4], const Epilogue& e, int n) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    b[j] = e.bias != nullptr && n + j < e.N ? __uint_as_float(static_cast<uint32_t>(e.bias[n + j]) << 16) : 0.0f;
+}
+
+// Columns n .. n + 3 of row m from their sums v.
+__device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 v, const float (&b)[4]) {
+  float f[4] = {v.x + b[0], v.y + b[1], v.z + b[2], v.w + b[3]};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = activate(f[j], e.act);
+  const bool whole = n + 4 <= e.N;
+  if (e.residual != nullptr) {
+    const uint16_t* r = e.residual + m * e.ldr + n;
+    if (e.vec_r && whole) {
+      const uint2 h = *reinterpret_cast<const uint2*>(r);
+      f[0] += bf16_lo(h.x);
+      f[1] += bf16_hi(h.x);
+      f[2] += bf16_lo(h.y);
+      f[3] += bf16_hi(h.y);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < e.N) f[j] += __uint_as_float(static_cast<uint32_t>(r[j]) << 16);
+    }
+  }
+  if (e.f32) {
+    float* y = static_cast<float*>(e.Y) + m * e.ldy + n;
+    if (e.vec_y && whole) {
+      *reinterpret_cast<float4*>(y) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < e.N) y[j] = f[j];
+    }
+  } else {
+    uint16_t* y = static_cast<uint16_t*>(e.Y) + m * e.ldy + n;
+    const uint2 o = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+    if (e.vec_y && whole) {
+      *reinterpret_cast<uint2*>(y) = o;
+    } else {
+      const uint32_t h[4] = {o.x & 0xFFFFu, o.x >> 16, o.y & 0xFFFFu, o.y >> 16};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < e.N) y[j] = static_cast<uint16_t>(h[j]);
+    }
+  }
+}
+
+// ------------------------------------------------------------ few rows: K over a cluster
+constexpr int S_THREADS = 192;  // TMA warp, MMA warp, four epilogue warps; all of them reduce
+constexpr int S_MAX_STAGES = 12;
+constexpr int S_MAX_SPLIT = 8;
+
+struct SplitSmem {
+  uint64_t full[S_MAX_STAGES], empty[S_MAX_STAGES];
+  uint64_t tfull, drain;
+  uint32_t tmem_base;
+  int abort, zero;
+};
+
+struct SplitArgs {
+  Epilogue e;
+  int rows;      // of a tile: a multiple of 16, at most 128
+  int row_tiles;
+  int kblocks, split, stages, tmem_cols;
+  uint64_t limit_ns;
+};
+
+// Four floats of the same place in a CTA of the cluster.
+__device__ __forceinline__ float4 load_rank(const float* p, uint32_t rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(mapa_shared(smem_u32(p), rank))
+               : "memory");
+  return v;
+}
+
+__global__ void __launch_bounds__(S_THREADS, 2)
+    linear_split_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
+                        const __grid_constant__ SplitArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ SplitSmem s;
+  uint8_t* ring = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  float* sums = reinterpret_cast<float*>(ring);  // [rows][128], when the main loop is done
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_trigger();  // barriers, TMEM and tensor maps while the previous kernel finishes
+  if (warp == 0 && lane == 0) {
+    tma_prefetch_map(&mapW);
+    tma_prefetch_map(&mapX);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < a.stages; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    mbar_init(&s.tfull, 1);
+    mbar_init(&s.drain, 1);
+    s.abort = 0;
+    s.zero = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&s.tmem_base, a.tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();  // every thread: the previous kernel's outputs are visible
+  const uint32_t tmem_base = s.tmem_base;
+  volatile int* abort = &s.abort;
+  const int rank = static_cast<int>(blockIdx.x % a.split), tile = static_cast<int>(blockIdx.x / a.split);
+  const int n0 = tile / a.row_tiles * 128, m0 = tile % a.row_tiles * a.rows;
+  const int kb0 = static_cast<int>(static_cast<long long>(a.kblocks) * rank / a.split);
+  const int kb1 = static_cast<int>(static_cast<long long>(a.kblocks) * (rank + 1) / a.split);
+  const int stage_bytes = W_BYTES + a.rows * BK * 2;
+  uint32_t issued_mask = 0, last_phase_bits = 0;
+  bool mma_issued = false, leader = false;
+
+  if (warp == 0) {
+    const bool issuer = elect_one();
+    int slot = 0;
+    uint32_t phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&s.empty[slot], phase ^ 1u, a.limit_ns, abort))) {
+        if (issuer && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 41);
+        *abort = 1;
+        break;
+      }
+      if (issuer) {
+        uint8_t* p = ring + slot * stage_bytes;
+        mbar_arrive_expect_tx(&s.full[slot], stage_bytes);
+        tma_load_2d(p, &mapW, &s.full[slot], kb * BK, n0);
+        tma_load_2d(p + W_BYTES, &mapX, &s.full[slot], kb * BK, m0);
+      }
+      issued_mask |= 1u << slot;
+      last_phase_bits = (last_phase_bits & ~(1u << slot)) | (phase << slot);
+      if (++slot == a.stages) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    }
+  } else if (warp == 1) {
+    leader = elect_one();
+    const uint64_t desc0 = sdesc_kmajor_sw128(smem_u32(ring));
+    const uint32_t idesc = idesc_bf16_f32(128, a.rows);
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
+        if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 42);
+        *abort = 1;
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const uint64_t dw = desc0 + static_cast<uint64_t>((slot * stage_bytes) >> 4), dx = dw + (W_BYTES >> 4);
+      if (leader) {
+#pragma unroll
+        for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
+          mma_bf16(tmem_base, dw + 2 * kk, dx + 2 * kk, idesc, kb != kb0 || kk != 0 ? 1u : 0u);
+        mma_commit(&s.empty[slot]);
+      }
+      mma_issued = true;
+      if (++slot == a.stages) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    }
+    if (ok && leader) mma_commit(&s.tfull);
+    __syncwarp();
+  } else {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull, 0, a.limit_ns, abort));
+    if (!ok) {
+      if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 43);
+      *abort = 1;
+    } else {
+      tc_fence_after();  // the ring's copies and MMAs are done: its memory takes the sums
+      const int q = warp & 3;
+#pragma unroll 1
+      for (int c = 0; c < a.rows; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (c + i < a.rows) sums[(c + i) * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+      }
+      tc_fence_before();
+    }
+  }
+  __syncthreads();
+  if (s.abort) {
+    volatile int* never = &s.zero;
+    if (warp == 0 && lane == 0)
+      for (int i = 0; i < a.stages; ++i)
+        if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
+    if (leader && mma_issued) {
+      mma_commit(&s.drain);
+      mbar_wait(&s.drain, 0, a.limit_ns, never);
+    }
+    __syncthreads();
+  }
+  cluster_sync();  // every CTA's sums are there
+  {
+    const int r0 = a.rows * rank / a.split, r1 = a.rows * (rank + 1) / a.split;
+    const int n = n0 + lane * 4;
+    float b[4];
+    load_bias4(b, a.e, n);
+#pragma unroll 1
+    for (int r = r0 + warp; r < r1 && m0 + r < a.e.M; r += S_THREADS / 32) {
+      float4 u[S_MAX_SPLIT];
+#pragma unroll
+      for (int j = 0; j < S_MAX_SPLIT; ++j)
+        if (j < a.split) u[j] = load_rank(sums + r * 128 + lane * 4, j);
+      float4 v = u[0];
+#pragma unroll
+      for (int j = 1; j < S_MAX_SPLIT; ++j)
+        if (j < a.split) {
+          v.x += u[j].x;
+          v.y += u[j].y;
+          v.z += u[j].z;
+          v.w += u[j].w;
+        }
+      if (n < a.e.N && !*abort) finish4(a.e, m0 + r, n, v, b);
+    }
+  }
+  cluster_sync();  // no CTA leaves while another reads its sums
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, a.tmem_cols);
+  }
+}
+
+// ---------------------------------------------------------------- CTA pairs
+constexpr int P_STAGES = 6;
+constexpr int P_STAGE_BYTES = 2 * W_BYTES;  // 128 weight rows and up to 128 rows of X a CTA
+constexpr int P_GROUPS = 2;                 // of four epilogue warps, alternate chunks of 32 rows
+constexpr int P_THREADS = 64 + 128 * P_GROUPS;
+constexpr int P_CHUNK_FLOATS = 32 * 128;
+constexpr int P_GROUP_ROWS = 16;            // row tiles that share a pass over the weights
+
+struct PairSmem {
+  uint64_t full[P_STAGES], empty[P_STAGES];
+  uint64_t tfull[2], tempty[2], drain;
+  uint32_t tmem_base;
+  int abort, zero;
+};
+constexpr int P_SMEM =
+    P_STAGES * P_STAGE_BYTES + P_GROUPS * P_CHUNK_FLOATS * 4 + 1024 + static_cast<int>(sizeof(PairSmem));
+static_assert(P_SMEM <= 227 * 1024, "shared memory of the pair kernel");
+
+struct PairArgs {
+  Epilogue e;
+  int rows;  // of a tile: a multiple of 32, at most 256
+  int row_tiles, col_tiles, kblocks;
+  uint64_t limit_ns;
+};
+
+// Tiles in groups of P_GROUP_ROWS row tiles, in a group all row tiles of a column tile one after
+// the other: pairs at work together share their weights and rows in L2.
+__device__ __forceinline__ void pair_tile(int tile, const PairArgs& a, int& m0, int& n0) {
+  const int per = P_GROUP_ROWS * a.col_tiles, g = tile / per, i = tile - g * per;
+  const int in = min(P_GROUP_ROWS, a.row_tiles - g * P_GROUP_ROWS);
+  const int ct = i / in;
+  m0 = (g * P_GROUP_ROWS + i - ct * in) * a.rows;
+  n0 = ct * 256;
+}
+
+// The even CTA's barrier, on which both CTAs' copies and arrivals count.
+__device__ __forceinline__ uint32_t lead_barrier(uint64_t* bar) { return mapa_shared(smem_u32(bar), 0); }
+
+__device__ __forceinline__ void group_sync(int group) {
+  asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+}
+
+__global__ void __launch_bounds__(P_THREADS, 1)
+    linear_pair_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
+                       const __grid_constant__ PairArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  float* chunks = reinterpret_cast<float*>(ring + P_STAGES * P_STAGE_BYTES);
+  PairSmem& s = *reinterpret_cast<PairSmem*>(chunks + P_GROUPS * P_CHUNK_FLOATS);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = static_cast<int>(cluster_ctarank() & 1u);
+  const bool even = rank == 0;
+  pdl_trigger();
+  if (warp == 0 && lane == 0) {
+    tma_prefetch_map(&mapW);
+    tma_prefetch_map(&mapX);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < P_STAGES; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.tfull[i], 1);
+      mbar_init(&s.tempty[i], 2 * 4 * P_GROUPS);  // every epilogue warp of both CTAs
+    }
+    mbar_init(&s.drain, 1);
+    s.abort = 0;
+    s.zero = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&s.tmem_base, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync();  // barriers of both CTAs initialised, TMEM allocated
+  tc_fence_after();
+  pdl_wait();  // every thread: the previous kernel's outputs are visible
+  const uint32_t tmem_base = s.tmem_base;
+  volatile int* abort = &s.abort;
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const int total = a.row_tiles * a.col_tiles;
+  const int half = a.rows / 2;  // rows of X in a CTA's shared memory
+  uint32_t issued_mask = 0, last_phase_bits = 0;
+  bool mma_issued = false, leader = false;
+
+  if (warp == 0) {
+    const bool issuer = elect_one();
+    const uint32_t bytes = 2u * static_cast<uint32_t>(W_BYTES + half * BK * 2);
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int tile = pair; tile < total && ok; tile += pairs) {
+      int m0, n0;
+      pair_tile(tile, a, m0, n0);
+      for (int kb = 0; kb < a.kblocks; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&s.empty[slot], phase ^ 1u, a.limit_ns, abort))) {
+          if (issuer && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 51);
+          *abort = 1;
+          ok = false;
+          break;
+        }
+        if (issuer) {
+          uint8_t* p = ring + slot * P_STAGE_BYTES;
+          if (even) mbar_arrive_expect_tx(&s.full[slot], bytes);
+          const uint32_t full = lead_barrier(&s.full[slot]);
+          tma_load_2d_pair(p, &mapW, full, kb * BK, n0 + rank * 128);
+          tma_load_2d_pair(p + W_BYTES, &mapX, full, kb * BK, m0 + rank * half);
+        }
+        issued_mask |= 1u << slot;
+        last_phase_bits = (last_phase_bits & ~(1u << slot)) | (phase << slot);
+        if (++slot == P_STAGES) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (even) {
+      leader = elect_one();
+      const uint64_t desc0 = sdesc_kmajor_sw128(smem_u32(ring));
+      const uint32_t idesc = idesc_bf16_f32(256, a.rows);
+      int slot = 0, it = 0;
+      uint32_t phase = 0;
+      for (int tile = pair; tile < total; tile += pairs, ++it) {
+        const int b = it & 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(&s.tempty[b], ((it >> 1) & 1) ^ 1u, a.limit_ns, abort))) {
+          if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 52);
+          *abort = 1;
+          break;
+        }
+        tc_fence_after();
+        bool ok = true;
+        for (int kb = 0; kb < a.kblocks; ++kb) {
+          if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
+            if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 53);
+            *abort = 1;
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t dw = desc0 + static_cast<uint64_t>((slot * P_STAGE_BYTES) >> 4), dx = dw + (W_BYTES >> 4);
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
+              mma_bf16_pair(tmem_base + b * 256, dw + 2 * kk, dx + 2 * kk, idesc, (kb | kk) != 0 ? 1u : 0u);
+            mma_commit_pair(&s.empty[slot], 0x3);
+          }
+          mma_issued = true;
+          if (++slot == P_STAGES) {
+            slot = 0;
+            phase ^= 1u;
+          }
+        }
+        if (!ok) break;
+        if (leader) mma_commit_pair(&s.tfull[b], 0x3);
+        __syncwarp();
+      }
+    }
+  } else {
+    const int q = warp & 3, group = (warp - 2) >> 2, et = tid - 64 - 128 * group;
+    float* chunk = chunks + group * P_CHUNK_FLOATS;
+    int it = 0;
+    for (int tile = pair; tile < total; tile += pairs, ++it) {
+      const int b = it & 1;
+      // a wait that fails leaves the group together: the flag is agreed on behind a barrier
+      const bool waited = mbar_wait(&s.tfull[b], (it >> 1) & 1, a.limit_ns, abort);
+      if (!waited && !*abort) {
+        report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 54);
+        *abort = 1;
+      }
+      uint32_t go;
+      asm volatile(
+          "{\n\t.reg .pred p, r;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+          "bar.red.and.pred r, %2, 128, p;\n\tselp.u32 %0, 1, 0, r;\n\t}"
+          : "=r"(go)
+          : "r"(static_cast<uint32_t>(waited)), "r"(1 + group)
+          : "memory");
+      if (!go) break;
+      tc_fence_after();
+      int m0, n0;
+      pair_tile(tile, a, m0, n0);
+      const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * 128 + (et & 31) * 4;
+      float bias[4];
+      load_bias4(bias, a.e, n);
+      const uint32_t tb = tmem_base + b * 256 + (static_cast<uint32_t>(q * 32) << 16);
+#pragma unroll 1
+      for (int c = group * 32; c < rows; c += 32 * P_GROUPS) {
+        uint32_t v[32];
+        tmem_ld32(tb + c, v);  // TMEM column = row c + i of the tile
+        tmem_ld_wait();
+        group_sync(group);     // the chunk before has been read
+#pragma unroll
+        for (int i = 0; i < 32; ++i) chunk[i * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+        group_sync(group);
+        if (n < a.e.N)
+#pragma unroll 2
+          for (int r = et >> 5; r < 32 && c + r < rows; r += 4)
+            finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(lead_barrier(&s.tempty[b]));
+    }
+  }
+
+  __syncthreads();
+  if (s.abort) {
+    volatile int* never = &s.zero;
+    if (warp == 0 && lane == 0 && even)
+      for (int i = 0; i < P_STAGES; ++i)
+        if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
+    if (leader && mma_issued) {
+      mma_commit_pair(&s.drain, 0x1);
+      mbar_wait(&s.drain, 0, a.limit_ns, never);
+    }
+  }
+  tc_fence_before();
+  cluster_sync();  // both CTAs finished: no more arrivals or copies into either
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem_base, 512);
+}
+
+}  // namespace ln
+
+// Tiles of 256 x 256 from which the pair kernel takes a product of more than 128 rows.
+constexpr int kLinearPairTiles = 48;
+
+static cudaError_t linear_attr() {
+  const cudaError_t e = cudaFuncSetAttribute(ln::linear_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             227 * 1024 - static_cast<int>(sizeof(ln::SplitSmem)) - 256);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(ln::linear_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ln::P_SMEM);
+}
+
+static void cluster_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, int size, cudaStream_t stream) {
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // waits in the kernel
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_on(stream) ? 2 : 1;
+}
+
+// CTA pairs that can be resident at once: the persistent grid never exceeds them.
+static int linear_resident_pairs() {
+  static PerDevice cache;
+  return per_device(cache, [] {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cluster_config(cfg, attr, 2, nullptr);
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(2 * (num_sms() / 2), 1, 1);
+    cfg.blockDim = dim3(ln::P_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = ln::P_SMEM;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_kernel, &cfg) != cudaSuccess || n <= 0) {
+      cudaGetLastError();
+      n = num_sms() / 2;
+    }
+    return n < num_sms() / 2 ? n : num_sms() / 2;
+  });
+}
+
+static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, int M, int N, int K,
+                         const ln::Epilogue& e, cudaStream_t stream) {
+  using namespace ln;
+  static PerDevice cache;
+  const cudaError_t ae = static_cast<cudaError_t>(per_device(cache, [] { return static_cast<int>(linear_attr()); }));
+  if (ae != cudaSuccess) return cuda_fail(ae, "cudaFuncSetAttribute(linear)");
+  const int kblocks = (K + BK - 1) / BK;
+  auto div_up = [](long long x, long long y) { return (x + y - 1) / y; };
+  CUtensorMap mW, mX;
+  int rc;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
+  // pairs: even row tiles of at most 256 rows
+  const long long p_tiles = div_up(M, 256) * div_up(N, 256);
+  if (M > 128 && p_tiles >= kLinearPairTiles) {
+    PairArgs a{};
+    a.e = e;
+    a.row_tiles = static_cast<int>(div_up(M, 256));
+    a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 32) * 32);
+    a.row_tiles = static_cast<int>(div_up(M, a.rows));
+    a.col_tiles = static_cast<int>(div_up(N, 256));
+    a.kblocks = kblocks;
+    a.limit_ns = wait_limit_ns();
+    if ((long long)a.row_tiles * a.col_tiles > INT32_MAX / 2)
+      return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+    if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
+    const int most = linear_resident_pairs(), tiles = a.row_tiles * a.col_tiles;
+    cluster_config(cfg, attr, 2, stream);
+    cfg.gridDim = dim3(2 * (tiles < most ? tiles : most), 1, 1);
+    cfg.blockDim = dim3(P_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = P_SMEM;
+    const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_kernel, mW, mX, a);
+    if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_kernel");
+    OM_LAUNCHED("linear_pair_kernel");
+    return ORDERMOE_OK;
+  }
+  SplitArgs a{};
+  a.e = e;
+  a.row_tiles = static_cast<int>(div_up(M, 128));
+  a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 16) * 16);
+  a.row_tiles = static_cast<int>(div_up(M, a.rows));
+  a.kblocks = kblocks;
+  a.limit_ns = wait_limit_ns();
+  const long long tiles = a.row_tiles * div_up(N, 128);
+  if (tiles > INT32_MAX / S_MAX_SPLIT) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+  // K over as many CTAs as two an SM leave room for, four K blocks each at least
+  const int sms = num_sms();
+  a.split = 1;
+  while (a.split * 2 <= S_MAX_SPLIT && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
+  // one CTA an SM takes a ring of most of its shared memory, two half of it each
+  const int stage = W_BYTES + a.rows * BK * 2, most = tiles * a.split <= sms ? 220 * 1024 : 108 * 1024;
+  const int share = (kblocks + a.split - 1) / a.split, need = (a.rows * 512 + stage - 1) / stage;
+  a.stages = most / stage < S_MAX_STAGES ? most / stage : S_MAX_STAGES;
+  if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
+  a.tmem_cols = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+  if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows))) return rc;
+  cluster_config(cfg, attr, a.split, stream);
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split), 1, 1);
+  cfg.blockDim = dim3(S_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = a.stages * stage + 1024;
+  const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_split_kernel, mW, mX, a);
+  if (ce != cudaSuccess) return cuda_fail(ce, "linear_split_kernel");
+  OM_LAUNCHED("linear_split_kernel");
+  return ORDERMOE_OK;
+}
+
+}  // namespace om
+
+using namespace om;
+
+extern "C" int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, const uint16_t* bias,
+                               int act, const uint16_t* residual, int64_t ldr, int M, int N, int K, void* Y,
+                               int64_t ldy, int f32, ordermoe_stream_t stream) {
+  OM_TRACE();
+  if (M < 0 || N <= 0 || K <= 0)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "linear: need M >= 0, N > 0 and K > 0");
+  if (act < ORDERMOE_ACT_NONE || act > ORDERMOE_ACT_SILU)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "linear: unknown activation %d", act);
+  if (ldx < K || ldw < K || ldy < N || (residual && ldr < N))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "linear: a row stride is shorter than the row");
+  if (ldx % 8 != 0 || ldw % 8 != 0 || ldx >= (1ll << 38) || ldw >= (1ll << 38))
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: ldx and ldw must be multiples of 8, below 2^38");
+  if (M == 0) return ORDERMOE_OK;
+  if (!X || !W || !Y) return fail(ORDERMOE_ERR_INVALID_ARG, "linear: null pointer");
+  if (!aligned16(X) || !aligned16(W)) return fail(ORDERMOE_ERR_INVALID_ARG, "linear: X and W must be 16-byte aligned");
+  const uintptr_t y = reinterpret_cast<uintptr_t>(Y), r = reinterpret_cast<uintptr_t>(residual);
+  if (y % (f32 ? 4 : 2) != 0 || r % 2 != 0 || reinterpret_cast<uintptr_t>(bias) % 2 != 0)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "linear: Y, residual or bias is not aligned to its type");
+  ln::Epilogue e{};
+  e.M = M; e.N = N; e.bias = bias; e.residual = residual; e.Y = Y;
+  e.ldr = ldr; e.ldy = ldy; e.act = act; e.f32 = f32 != 0;
+  e.vec_r = ldr % 4 == 0 && r % 8 == 0;
+  e.vec_y = ldy % 4 == 0 && y % (f32 ? 16 : 8) == 0;
+  return linear_launch(X, ldx, W, ldw, M, N, K, e, stream);
+}

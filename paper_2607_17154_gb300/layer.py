@@ -119,15 +119,47 @@ def build_tables(sim, group, placement, theta, qbar, sp, device, out=None):
     return t
 
 
+class DenseFFN:
+    """A dense feed-forward layer (every second layer of Switch-Base-8E is one, with ReLU):
+    y = act(x W1^T + b1) W2^T + b2 through ordermoe_linear, for up to T_max tokens.
+    W1 [dff, d], W2 [d, dff], b1 [dff], b2 [d] bf16 (the biases may be None)."""
+
+    def __init__(self, W1, W2, T_max, b1=None, b2=None, act="relu"):
+        self.W1, self.W2, self.b1, self.b2, self.act = W1, W2, b1, b2, act
+        self.dff, self.d = W1.shape
+        self.T_max = T_max
+        self.H = torch.empty(T_max, self.dff, dtype=torch.bfloat16, device=W1.device)
+
+    def forward(self, x, y, residual=None, stream=None):
+        """y = the layer of x [T, d], added to residual [T, d] when given (y may be it)."""
+        T = x.shape[0]
+        assert T <= self.T_max
+        B.ordermoe_linear(x, self.W1, self.H[:T], bias=self.b1, act=self.act, stream=stream)
+        B.ordermoe_linear(self.H[:T], self.W2, y, bias=self.b2, residual=residual, stream=stream)
+        return y
+
+    def forward_residual(self, x, h, h_out, x_out, eps=B.NORM_EPS, stream=None):
+        """On the residual map: h_out = h + y, x_out = RMSNorm(h_out)."""
+        self.forward(x, h_out, residual=h, stream=stream)
+        B.ordermoe_rmsnorm(h_out, x.shape[0], self.d, eps, x_out, stream)
+        return h_out, x_out
+
+
 class LayerStack:
     """L MoE layers run through ordermoe_layer_forward with the token state
-    (location, accumulated loss; Eqs. 36 and 44) carried from layer to layer."""
+    (location, accumulated loss; Eqs. 36 and 44) carried from layer to layer, and
+    DenseFFN layers between them."""
 
     def __init__(self, layers, tables, k, T_max, device, H=1, stride=0, P=None, few=False):
         """layers: dicts with W_r, W1, W3, W2 (device bf16). tables: a list of
         per-layer device buffers, or (for look-ahead, H > 1) one device buffer
         holding all layers' tables `stride` bytes apart; P [L-1, E, E] the
-        transition matrices. Layer l looks min(H, L - l) - 1 layers ahead."""
+        transition matrices. Layer l looks min(H, L - l) - 1 layers ahead. few: steps of at most
+        B.FEW_TOKENS tokens run each MoE layer in one launch (ordermoe_layer_few). A
+        DenseFFN in `layers` runs in its place; tables, P and L then count the MoE layers
+        alone, in order."""
+        dense = {l: lay for l, lay in enumerate(layers) if isinstance(lay, DenseFFN)}
+        layers = [lay for lay in layers if not isinstance(lay, DenseFFN)]
         E, dff, d = layers[0]["W1"].shape
         L = len(layers)
         self.scratch = torch.empty(B.ordermoe_layer_scratch_bytes(T_max, E, d, dff, k),
@@ -143,6 +175,8 @@ class LayerStack:
             self.descs.append(B.make_layer_desc(T_max, lay["W_r"], lay["W1"], lay["W3"], lay["W2"],
                                                 t, k, self.scratch, lookahead_H=Hl,
                                                 tables_stride=stride, P=Pl))
+        for l, lay in dense.items():
+            self.descs.insert(l, lay)
         self.d, self.T_max = d, T_max
         self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), E, d, dff, k, device) if few else None
 
@@ -155,6 +189,9 @@ class LayerStack:
         T = X_layers[0].shape[0]
         out = B.make_few_out(counters=counters) if self._few(T) and counters is not None else None
         for desc, X, y in zip(self.descs, X_layers, y_layers):
+            if isinstance(desc, DenseFFN):
+                desc.forward(X, y, stream=stream)
+                continue
             if self._few(T):
                 B.ordermoe_layer_few(desc, T, X, home, loc, qhat, y, self.few_ws, out, stream)
                 continue
@@ -166,10 +203,13 @@ class LayerStack:
         then layer l runs on xs[l] and writes hs[l + 1] = hs[l] + y_l and
         xs[l + 1] = RMSNorm(hs[l + 1]). hs, xs: L + 1 device buffers [T, d]
         bf16 (hs[0] is the input); logits: optional [L, T, E] f32 receiving each
-        layer's router logits (layer-major)."""
+        layer's router logits (layer-major; a dense layer leaves its own)."""
         T = hs[0].shape[0]
         B.ordermoe_rmsnorm(hs[0], T, self.d, eps, xs[0], stream)
         for l, desc in enumerate(self.descs):
+            if isinstance(desc, DenseFFN):
+                desc.forward_residual(xs[l], hs[l], hs[l + 1], xs[l + 1], eps, stream)
+                continue
             if self._few(T):
                 out = B.make_few_out(logits=None if logits is None else logits[l], counters=counters)
                 B.ordermoe_layer_few_residual(desc, T, xs[l], hs[l], home, loc, qhat, eps, hs[l + 1],

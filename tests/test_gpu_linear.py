@@ -1,0 +1,254 @@
+"""ordermoe_linear against Y = act(X W^T + bias) + residual in 64 bits, and dense layers in a
+stack.
+
+Tolerance: the fp32 sum of K products and the bias is off by at most (K + 8) 2^-24 of the sum
+of magnitudes S = |x| |w| + |b| (one rounding or truncation of the running sum for each product,
+twice the half-step for truncation: (K + 8) 2^-23 S); an activation's slope is at most
+1.13 (GELU) and its own fp32 evaluation within 2^-20 of its value; the residual adds one
+rounding of 2^-24. Then one rounding to Y: 2^-8 of its value in bf16, 2^-24 in fp32."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_17154_gb300 import binding as B
+from paper_2607_17154_gb300 import synth
+from paper_2607_17154_gb300.layer import DenseFFN, LayerStack, exact_tables
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    B.lib()
+    yield
+    code, detail = B.ordermoe_device_error()
+    assert code == 0, (code, detail)
+
+
+def rows(n, w, std, seed, pad=0, odd=False, dt=torch.bfloat16, offset=0):
+    ld = (w if odd else (w + 7) // 8 * 8) + pad
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    buf = torch.randn(n * ld + offset, generator=g, device=DEV) * std
+    return buf.to(dt)[offset:].view(n, ld)[:, :w]
+
+
+def act64(v, act):
+    if act == "relu":
+        return v.clamp(min=0.0)
+    if act == "gelu":
+        return v * 0.5 * torch.special.erfc(-v / math.sqrt(2.0))
+    if act == "gelu_tanh":
+        # 0.5 (1 + tanh u) = sigmoid(2 u): the sum loses the tail (u = -32: 1e-28) even in 64 bits
+        return v * torch.sigmoid(2.0 * math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3))
+    return v * torch.sigmoid(v) if act == "silu" else v
+
+
+def check(X, W, Y, bias=None, act="none", residual=None):
+    res = None if residual is None else residual.double().clone()
+    keep = None
+    if Y._base is not None:
+        keep = Y._base.clone()
+    B.ordermoe_linear(X, W, Y, bias=bias, act=act, residual=residual)
+    torch.cuda.synchronize()
+    v = X.double() @ W.double().T
+    S = X.double().abs() @ W.double().abs().T
+    if bias is not None:
+        v, S = v + bias.double(), S + bias.double().abs()
+    ref = act64(v, act)
+    err = 1.13 * (X.shape[1] + 8) * 2.0 ** -23 * S + 2.0 ** -20 * ref.abs()
+    if res is not None:
+        ref = ref + res
+        err = err + 2.0 ** -24 * ref.abs()
+    half = 2.0 ** -24 if Y.dtype == torch.float32 else 2.0 ** -8
+    off = (Y.double() - ref).abs()
+    assert (off <= half * ref.abs() + (1 + half) * err + 1e-38).all(), (off / (half * ref.abs() + err + 1e-38)).max()
+    if keep is not None:  # what lies between the rows is as it was
+        Y2 = Y.clone()
+        Y.copy_(torch.as_strided(keep, Y.shape, Y.stride(), Y.storage_offset()))
+        same = Y._base.view(torch.uint8) == keep.view(torch.uint8)
+        assert same.all()
+        Y.copy_(Y2)
+
+
+SIZES = [(1, 1, 1), (1, 4096, 4096), (1, 7, 2048), (3, 129, 65), (16, 256, 256), (17, 1000, 520), (33, 5632, 2048),
+         (64, 128, 72), (100, 2049, 1999), (128, 640, 4096), (129, 300, 100), (255, 257, 8), (300, 4096, 1024)]
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("f32", [False, True])
+def test_split(M, N, K, f32):
+    X, W = rows(M, K, 1.0, 1), rows(N, K, 0.05, 2)
+    Y = torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    check(X, W, Y)
+
+
+# at least 48 tiles of 256 x 256: CTA pairs
+PAIRS = [(1021, 4096, 512), (1500, 2561, 328), (4100, 1024, 200), (257, 6300, 64), (8192, 512, 136)]
+
+
+@pytest.mark.parametrize("M,N,K", PAIRS)
+@pytest.mark.parametrize("f32", [False, True])
+def test_pairs(M, N, K, f32):
+    X, W = rows(M, K, 1.0, 3), rows(N, K, 0.05, 4)
+    Y = torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    check(X, W, Y, bias=rows(1, N, 0.5, 5)[0].contiguous(), residual=rows(M, N, 1.0, 6, odd=True))
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("M,N,K", [(5, 200, 96), (130, 515, 264), (2048, 2048, 128)])
+def test_epilogue(act, M, N, K):
+    X, W, b = rows(M, K, 2.0, 7), rows(N, K, 0.1, 8), rows(1, N, 1.0, 9)[0].contiguous()
+    R = rows(M, N, 1.0, 10, odd=True)
+    for bias in (None, b):
+        for res in (None, R):
+            for dt in (torch.bfloat16, torch.float32):
+                check(X, W, torch.empty(M, N, dtype=dt, device=DEV), bias, act, res)
+
+
+@pytest.mark.parametrize("M,N,K", [(9, 130, 100), (200, 1023, 512), (1100, 4099, 136)])
+def test_strides_and_odd_addresses(M, N, K):
+    """Rows inside wider buffers; Y and residual at addresses and strides that no 8-byte access fits."""
+    for pad, offset in ((8, 0), (13, 0), (24, 4), (5, 1)):
+        X, W = rows(M, K, 1.0, 11, pad=pad // 8 * 8), rows(N, K, 0.1, 12, pad=16)
+        R = rows(M, N, 1.0, 13, pad=pad, odd=True, offset=offset)
+        for dt in (torch.bfloat16, torch.float32):
+            Y = rows(M, N, 1.0, 14, pad=pad, odd=True, dt=dt, offset=offset)
+            check(X, W, Y, act="silu", residual=R)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 512, 512), (77, 300, 1000), (1500, 2048, 256)])
+def test_in_place_and_again(M, N, K):
+    """Y may be the residual; the same call gives the same bits."""
+    X, W = rows(M, K, 1.0, 15), rows(N, K, 0.1, 16)
+    R = rows(M, N, 1.0, 17, pad=8)
+    Y = R.clone()
+    B.ordermoe_linear(X, W, Y, act="gelu", residual=R)
+    for _ in range(3):
+        H = R.clone()
+        B.ordermoe_linear(X, W, H, act="gelu", residual=H)
+        assert torch.equal(H, Y)
+
+
+@pytest.mark.parametrize("M", [4, 1100])
+def test_infinities_and_nan_stay_in_their_rows_and_columns(M):
+    N, K = 2600, 128
+    X, W = rows(M, K, 1.0, 18), rows(N, K, 0.1, 19)
+    Y, Z = (torch.empty(M, N, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    B.ordermoe_linear(X, W, Y, act="relu")
+    X[1, 3], W[5, 7], W[9, 0] = float("nan"), float("nan"), float("inf")
+    B.ordermoe_linear(X, W, Z, act="relu")
+    torch.cuda.synchronize()
+    keep = torch.ones(M, N, dtype=torch.bool, device=DEV)
+    keep[1], keep[:, 5], keep[:, 9] = False, False, False
+    assert torch.equal(Y[keep], Z[keep])
+    assert Z[1].isnan().all() and Z[:, 5].isnan().all()
+    want = torch.relu(X[:, 0].double() * float("inf"))
+    assert torch.equal(Z[[0, 2, 3], 9].double(), want[[0, 2, 3]])
+
+
+def test_extreme_values():
+    """Sums beyond bf16's range, tails of the activations, and zeros."""
+    X = torch.tensor([[1.0] * 8, [3e38] * 8, [-3e38] * 8, [0.0] * 8], device=DEV).to(torch.bfloat16)
+    W = torch.tensor([[1.0] + [0.0] * 7, [-9.0] + [0.0] * 7, [-1e-3] + [0.0] * 7, [1.0] * 8], device=DEV).to(torch.bfloat16)
+    for act in ("none", "relu", "gelu", "gelu_tanh", "silu"):
+        Y = torch.empty(4, 4, dtype=torch.float32, device=DEV)
+        B.ordermoe_linear(X, W, Y, act=act)
+        v = X.float() @ W.float().T
+        ref = act64(v.double(), act).float()
+        # a value past fp32's range in the cube of gelu_tanh, and inf * 0 in the tails, are torch's NaN too
+        ok = torch.isfinite(ref)
+        assert torch.allclose(Y[ok], ref[ok], rtol=1e-5, atol=1e-37), (act, Y, ref)
+        assert not torch.isnan(Y[torch.isposinf(v)]).any() and (Y[torch.isposinf(v)] > 1e38).all()
+        assert torch.equal(Y[3], torch.zeros(4, device=DEV))
+
+
+def test_no_rows_and_no_others():
+    W = rows(64, 64, 0.1, 20)
+    Y = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    B.ordermoe_linear(torch.empty(0, 64, dtype=torch.bfloat16, device=DEV), W, Y)
+    big = torch.full((9, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    X = rows(6, 64, 1.0, 21)
+    B.ordermoe_linear(X, W, big[:6])
+    torch.cuda.synchronize()
+    assert (big[6:] == 3.0).all()
+
+
+def test_another_stream_and_a_graph():
+    X, W, b = rows(40, 512, 1.0, 22), rows(704, 512, 0.1, 23), rows(1, 704, 1.0, 24)[0].contiguous()
+    Y = torch.empty(40, 704, dtype=torch.bfloat16, device=DEV)
+    check(X, W, Y, b, "silu")
+    ref = Y.clone()
+    s = torch.cuda.Stream()
+    Z = torch.zeros_like(Y)
+    torch.cuda.synchronize()
+    B.ordermoe_linear(X, W, Z, bias=b, act="silu", stream=s)
+    s.synchronize()
+    assert torch.equal(Z, ref)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        B.ordermoe_linear(X, W, Z, bias=b, act="silu")
+        B.ordermoe_linear(Z, W[:, :].T.contiguous(), X[:, :], residual=X)
+    X0 = X.clone()
+    Z.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(Z, ref)
+    want = X0.double() + ref.double() @ W.double()
+    assert (X.double() - want).norm() <= 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("T", [2, 16, 70])
+@pytest.mark.parametrize("few", [False, True])
+def test_stack_of_moe_and_dense_layers(T, few):
+    """MoE and dense layers in turn on the residual map, eager and as a graph, against the same
+    layers in 64 bits from each layer's own bf16 inputs. A layer's sum is off by the roundings of
+    its inner activations (2^-8 each of the expert outputs and of H) and h_out by one: 4 * 2^-8
+    of the update and 2^-8 of the stream bound its 2-norm."""
+    d, E, k, dff, M, L = 512, 8, 2, 256, 2, 4
+    layers, tabs = [], []
+    for l in range(L):
+        W1, W3, W2 = synth.ffn_weights(E, d, dff, 100 * l, device=DEV)
+        if l % 2:
+            layers.append(DenseFFN(W1[0], W2[0], T, b1=rows(1, dff, 0.1, l)[0].contiguous(),
+                                   b2=rows(1, d, 0.1, l + 9)[0].contiguous()))
+        else:
+            layers.append({"W_r": synth.router_weights(E, d, 2, l, device=DEV), "W1": W1, "W3": W3, "W2": W2})
+            tabs.append(exact_tables(E, M, DEV))
+    st = LayerStack(layers, tabs, k, T, DEV, few=few)
+    home = torch.zeros(T, dtype=torch.uint8, device=DEV)
+    loc, q = home.clone(), torch.zeros(T, device=DEV)
+    hs = [synth.hidden(T, d, 5, DEV)] + [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(L)]
+    xs = [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(L + 1)]
+    st.step_residual(hs, xs, home, loc, q)
+    torch.cuda.synchronize()
+    for l, lay in enumerate(layers):
+        x, h = xs[l].double(), hs[l].double()
+        if isinstance(lay, DenseFFN):
+            y = torch.relu(x @ lay.W1.double().T + lay.b1.double()) @ lay.W2.double().T + lay.b2.double()
+        else:
+            w, idx = torch.topk(torch.softmax(x @ lay["W_r"].double().T, 1), k, dim=1)
+            w = w / w.sum(1, keepdim=True)
+            y = torch.zeros_like(x)
+            for t in range(T):
+                for j in range(k):
+                    e = idx[t, j]
+                    a = lay["W1"][e].double() @ x[t]
+                    y[t] += w[t, j] * (lay["W2"][e].double() @ (a * torch.sigmoid(a) * (lay["W3"][e].double() @ x[t])))
+        want = h + y
+        off = (hs[l + 1].double() - want).norm()
+        assert off <= 2.0 ** -8 * (want.norm() + 4 * y.norm()), l
+        n = hs[l + 1].double()
+        n = n / (n.square().mean(1, keepdim=True) + B.NORM_EPS).sqrt()
+        assert ((xs[l + 1].double() - n).abs() <= 2.0 ** -7 * n.abs() + 1e-30).all()
+    eager = [v.clone() for v in hs]
+    g = st.capture_residual(hs, xs, home, loc, q, prologue=lambda: (loc.copy_(home), q.zero_()))
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(u, v) for u, v in zip(eager, hs))
