@@ -96,6 +96,7 @@ class FewOut(ctypes.Structure):
     """Mirror of ordermoe_few_out."""
     _fields_ = [(n, _P) for n in ("logits", "topk_idx", "topk_w", "chosen_expert", "chosen_server",
                                   "kind", "counters")]
+    sizes = None  # of the call that its tensors were last checked for
 
 
 class OrderMoEError(RuntimeError):
@@ -461,53 +462,59 @@ def ordermoe_layer_forward_residual(desc, T, x, h, home, loc, qhat, eps, h_out, 
     _check("ordermoe_layer_forward_residual", rc)
 
 
-def _here(*tensors):
-    """The tensors' device must be the current one, where the launch goes."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != dev:
-            raise ValueError("tensor on cuda:%d, but the current device is cuda:%d"
-                             % (t.device.index, dev))
+def _raw_stream(stream=None):
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
-def _matrix(t, name, dtypes, rows=None, cols=None):
+def _matrix(t, name, shape, device, dtypes=(torch.bfloat16,)):
     """Address and row stride of a device matrix whose rows are contiguous."""
-    if t is None:
-        return None, 0
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
-        raise TypeError("%s must be a matrix" % name)
     if t.dtype not in dtypes:
         raise TypeError("%s must be %s, got %s" % (name, " or ".join(map(str, dtypes)), t.dtype))
-    if not t.is_cuda:
-        raise ValueError("%s must be on a CUDA device" % name)
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError("%s must be %s x %s, got %s" % (name, rows, cols, tuple(t.shape)))
-    ld = t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8  # (one row: any)
-    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and ld < t.shape[1]):
-        raise ValueError("the rows of %s must be contiguous and apart" % name)
-    return ctypes.c_void_p(t.data_ptr()), ld
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device, cuda:%d" % (name, device))
+    n, w = shape
+    if w > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    if n <= 1:  # one row: its stride says nothing
+        return t.data_ptr(), (w + 7) // 8 * 8
+    ld = t.stride(0)
+    if ld < w:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return t.data_ptr(), ld
 
 
 def ordermoe_linear(X, W, Y, bias=None, act="none", residual=None, stream=None):
     """Y = act(X W^T + bias) + residual: X [M, K], W [N, K], residual [M, N] bf16, Y [M, N] bf16
     or float32, bias [N] bf16; rows may lie in wider buffers (strides are taken from the
     tensors). act: a name of ACTIVATIONS. Y may be the residual."""
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("unknown activation %r" % (act,))
-    bf16 = (torch.bfloat16,)
-    x, ldx = _matrix(X, "X", bf16)
+    for t in (X, W, Y):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise TypeError("X, W and Y must be matrices")
     M, K = X.shape
-    w, ldw = _matrix(W, "W", bf16, cols=K)
     N = W.shape[0]
-    y, ldy = _matrix(Y, "Y", (torch.bfloat16, torch.float32), M, N)
-    r, ldr = _matrix(residual, "residual", bf16, M, N)
-    _dt(bias, torch.bfloat16, "bias")
-    if bias is not None and bias.numel() != N:
-        raise ValueError("bias must have %d entries" % N)
-    _here(X, W, Y, residual, bias)
-    _check("ordermoe_linear", lib().ordermoe_linear(
-        x, ldx, w, ldw, _ptr(bias), ACTIVATIONS[act], r, ldr, M, N, K, y, ldy,
-        int(Y.dtype == torch.float32), _stream(stream)))
+    dev = torch.cuda.current_device()
+    x, ldx = _matrix(X, "X", X.shape, dev)
+    w, ldw = _matrix(W, "W", (N, K), dev)
+    y, ldy = _matrix(Y, "Y", (M, N), dev, (torch.bfloat16, torch.float32))
+    r, ldr = _matrix(residual, "residual", (M, N), dev) if residual is not None else (None, 0)
+    b = None
+    if bias is not None:
+        if bias.dtype != torch.bfloat16 or bias.shape != (N,) or not bias.is_contiguous():
+            raise ValueError("bias must be %d contiguous bfloat16 entries" % N)
+        if bias.get_device() != dev:
+            raise ValueError("bias must be on the current device, cuda:%d" % dev)
+        b = bias.data_ptr()
+    rc = lib().ordermoe_linear(x, ldx, w, ldw, b, code, r, ldr, M, N, K, y, ldy,
+                               Y.dtype == torch.float32, _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_linear", rc)
 
 
 def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):
@@ -515,7 +522,7 @@ def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):
 
 
 def ordermoe_layer_few_init(workspace, stream=None):
-    _here(workspace)
+    _entries(workspace, "workspace", torch.uint8, 1, torch.cuda.current_device())
     _check("ordermoe_layer_few_init", lib().ordermoe_layer_few_init(
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
@@ -533,45 +540,54 @@ def make_few_out(logits=None, topk_idx=None, topk_w=None, chosen_expert=None, ch
     return out
 
 
-def _few_check(desc, T, rows, home, loc, qhat, out, workspace):
-    """Types, sizes and devices of a few-token call: rows [T, d] and on."""
-    for n, t in rows:
-        _dt(t, torch.bfloat16, n)
-        if t.numel() < T * desc.d:
-            raise ValueError("%s has fewer than T rows of d" % n)
-    _dt(home, torch.uint8, "home"); _dt(loc, torch.uint8, "loc"); _dt(qhat, torch.float32, "qhat")
-    for n, t, w in (("home", home, 1), ("loc", loc, 1), ("qhat", qhat, 1)):
-        if t is not None and t.numel() < T * w:
-            raise ValueError("%s has fewer than T entries" % n)
+def _entries(t, name, dtype, n, device):
+    """Address of a contiguous device tensor of n entries at least (None: null)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device, cuda:%d" % (name, device))
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s must be contiguous, %d entries at least" % (name, n))
+    return t.data_ptr()
+
+
+def _few_args(desc, T, home, loc, qhat, out, workspace, dev):
+    """What both few-token calls take: home, loc, qhat; out, workspace, its bytes."""
     if out is not None:
-        for (n, _), t, w in zip(FewOut._fields_, out._keep, (desc.E,) + (desc.k,) * 5 + (0,)):
-            if t is not None and t.numel() < max(T * w, 0 if w else 4):
-                raise ValueError("%s is too small" % n)
-    _here(*(t for _, t in rows), home, loc, qhat, workspace, *(out._keep if out is not None else ()))
+        if out.sizes is None or out.sizes != (T, desc.E, desc.k, dev):  # checked once for its sizes
+            for (n, _), t, w in zip(FewOut._fields_, out._keep, (T * desc.E,) + (T * desc.k,) * 5 + (4,)):
+                _entries(t, n, t.dtype if t is not None else None, w, dev)
+            out.sizes = (T, desc.E, desc.k, dev)
+        out = ctypes.byref(out)
+    return ((_entries(home, "home", torch.uint8, T, dev), _entries(loc, "loc", torch.uint8, T, dev),
+             _entries(qhat, "qhat", torch.float32, T, dev)),
+            (out, _entries(workspace, "workspace", torch.uint8, 1, dev), workspace.numel()))
 
 
 def ordermoe_layer_few(desc, T, X, home, loc, qhat, y, workspace, out=None, stream=None):
     """A whole MoE layer for T <= FEW_TOKENS tokens in one launch (out: make_few_out)."""
-    _few_check(desc, T, (("X", X), ("y", y)), home, loc, qhat, out, workspace)
-    rc = lib().ordermoe_layer_few(ctypes.byref(desc), T, _ptr(X), _ptr(home), _ptr(loc), _ptr(qhat),
-                                  _ptr(y), None if out is None else ctypes.byref(out),
-                                  _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                  _stream(stream))
-    _check("ordermoe_layer_few", rc)
+    dev, n, bf16 = torch.cuda.current_device(), T * desc.d, torch.bfloat16
+    state, rest = _few_args(desc, T, home, loc, qhat, out, workspace, dev)
+    rc = lib().ordermoe_layer_few(ctypes.byref(desc), T, _entries(X, "X", bf16, n, dev), *state,
+                                  _entries(y, "y", bf16, n, dev), *rest, _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_layer_few", rc)
 
 
 def ordermoe_layer_few_residual(desc, T, x, h, home, loc, qhat, eps, h_out, x_out, workspace,
                                 out=None, stream=None):
     """ordermoe_layer_few on the residual map: h_out = h + y, x_out = RMSNorm(h_out)."""
-    _few_check(desc, T, (("x", x), ("h", h), ("h_out", h_out), ("x_out", x_out)), home, loc, qhat, out,
-               workspace)
-    rc = lib().ordermoe_layer_few_residual(ctypes.byref(desc), T, _ptr(x), _ptr(h), _ptr(home),
-                                           _ptr(loc), _ptr(qhat), float(eps), _ptr(h_out),
-                                           _ptr(x_out), None if out is None else ctypes.byref(out),
-                                           _ptr(workspace),
-                                           workspace.numel() * workspace.element_size(),
-                                           _stream(stream))
-    _check("ordermoe_layer_few_residual", rc)
+    dev, n, bf16 = torch.cuda.current_device(), T * desc.d, torch.bfloat16
+    state, rest = _few_args(desc, T, home, loc, qhat, out, workspace, dev)
+    rc = lib().ordermoe_layer_few_residual(ctypes.byref(desc), T, _entries(x, "x", bf16, n, dev),
+                                           _entries(h, "h", bf16, n, dev), *state, eps,
+                                           _entries(h_out, "h_out", bf16, n, dev),
+                                           _entries(x_out, "x_out", bf16, n, dev), *rest,
+                                           _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_layer_few_residual", rc)
 
 
 def ordermoe_layer_batches_scratch_bytes(T_max, E, d, dff, k):

@@ -5,10 +5,11 @@
 // rows waste little of the tensor pipe, and the accumulator is transposed (TMEM lane =
 // output column), so a chunk of 32 rows x 128 columns goes through shared memory once and each
 // thread then adds bias, activation and residual to 4 columns of a row and writes them.
-//   linear_split_kernel: one tile of 128 columns x up to 128 rows a cluster of S CTAs, which
+//   linear_split_kernel: one tile of up to 128 columns x 128 rows a cluster of S CTAs, which
 //     share its K and add their accumulators through distributed shared memory, every CTA the
 //     rows of its own share in rank order (the same bits at every call). For few rows, whose
-//     weights are one pass over HBM: all SMs stream them, two CTAs on one.
+//     weights are one pass over HBM: the tile's width and S are chosen so that every SM
+//     streams the same share of them.
 //   linear_pair_kernel: persistent CTA pairs, tiles of 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
 //     main loop. For batches with a tile for most pairs, bound by the tensor cores.
@@ -42,18 +43,28 @@ struct Epilogue {
   int vec_r, vec_y;          // 4 columns at a time: strides and addresses allow it
 };
 
-// Each activation in fp32 from the product's sum; NaN stays NaN.
-__device__ __forceinline__ float activate(float v, int act) {
-  switch (act) {
-    case ORDERMOE_ACT_RELU: return v < 0.0f ? 0.0f : v;
+// Each activation in fp32 from the product's sum; NaN stays NaN. Not inlined: the epilogue of a few
+// rows runs once, its instructions come from L2, and five activations a column made it longer
+// (301 x 1009 with SiLU 16.5 us).
+__device__ __noinline__ float4 activate4(float4 v, int act) {
+  float f[4] = {v.x, v.y, v.z, v.w};
+  if (act == ORDERMOE_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = f[j] < 0.0f ? 0.0f : f[j];
+  } else if (act == ORDERMOE_ACT_GELU) {
     // v Phi(v); erfc keeps the digits of a negative v's tail, which 1 + erf loses
-    case ORDERMOE_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
-    // 0.5 v (1 + tanh u) = v / (1 + e^-2u), u = sqrt(2/pi) (v + 0.044715 v^3)
-    case ORDERMOE_ACT_GELU_TANH:
-      return v / (1.0f + expf(-1.5957691216057308f * fmaf(0.044715f * v * v, v, v)));
-    case ORDERMOE_ACT_SILU: return v / (1.0f + expf(-v));
-    default: return v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = 0.5f * f[j] * erfcf(-0.70710678118654752f * f[j]);
+  } else {
+    // v sigmoid(s): s = v, or 2 sqrt(2/pi) (v + 0.044715 v^3), whose sigmoid is (1 + tanh) / 2 of half of it
+    const bool silu = act == ORDERMOE_ACT_SILU;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float g = 1.5957691216057308f * fmaf(0.044715f * f[j] * f[j], f[j], f[j]);
+      f[j] = f[j] / (1.0f + expf(silu ? -f[j] : -g));
+    }
   }
+  return make_float4(f[0], f[1], f[2], f[3]);
 }
 
 __device__ __forceinline__ void load_bias4(float (&b)[4], const Epilogue& e, int n) {
@@ -62,26 +73,38 @@ __device__ __forceinline__ void load_bias4(float (&b)[4], const Epilogue& e, int
     b[j] = e.bias != nullptr && n + j < e.N ? __uint_as_float(static_cast<uint32_t>(e.bias[n + j]) << 16) : 0.0f;
 }
 
-// Columns n .. n + 3 of row m from their sums v.
-__device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 v, const float (&b)[4]) {
-  float f[4] = {v.x + b[0], v.y + b[1], v.z + b[2], v.w + b[3]};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) f[j] = activate(f[j], e.act);
-  const bool whole = n + 4 <= e.N;
+// Columns n .. n + 3 of the residual's row m (0 past N, or without one).
+__device__ __forceinline__ float4 load_residual4(const Epilogue& e, int m, int n) {
+  float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (e.residual != nullptr) {
     const uint16_t* r = e.residual + m * e.ldr + n;
-    if (e.vec_r && whole) {
+    if (e.vec_r && n + 4 <= e.N) {
       const uint2 h = *reinterpret_cast<const uint2*>(r);
-      f[0] += bf16_lo(h.x);
-      f[1] += bf16_hi(h.x);
-      f[2] += bf16_lo(h.y);
-      f[3] += bf16_hi(h.y);
+      f[0] = bf16_lo(h.x);
+      f[1] = bf16_hi(h.x);
+      f[2] = bf16_lo(h.y);
+      f[3] = bf16_hi(h.y);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (n + j < e.N) f[j] += __uint_as_float(static_cast<uint32_t>(r[j]) << 16);
+        if (n + j < e.N) f[j] = __uint_as_float(static_cast<uint32_t>(r[j]) << 16);
     }
   }
+  return make_float4(f[0], f[1], f[2], f[3]);
+}
+
+// Columns n .. n + 3 of row m from their sums v and their residual r.
+__device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 v, const float (&b)[4], float4 r) {
+  v = make_float4(v.x + b[0], v.y + b[1], v.z + b[2], v.w + b[3]);
+  if (e.act != ORDERMOE_ACT_NONE) v = activate4(v, e.act);
+  float f[4] = {v.x, v.y, v.z, v.w};
+  if (e.residual != nullptr) {  // (without one -0 stays -0)
+    f[0] += r.x;
+    f[1] += r.y;
+    f[2] += r.z;
+    f[3] += r.w;
+  }
+  const bool whole = n + 4 <= e.N;
   if (e.f32) {
     float* y = static_cast<float*>(e.Y) + m * e.ldy + n;
     if (e.vec_y && whole) {
@@ -120,7 +143,9 @@ struct SplitSmem {
 struct SplitArgs {
   Epilogue e;
   int rows;      // of a tile: a multiple of 16, at most 128
+  int cols;      // a multiple of 16, at most 128
   int row_tiles;
+  int x_rows;    // rows that are loaded: all, or the M that there are
   int kblocks, split, stages, tmem_cols;
   uint64_t limit_ns;
 };
@@ -171,10 +196,12 @@ __global__ void __launch_bounds__(S_THREADS, 2)
   const uint32_t tmem_base = s.tmem_base;
   volatile int* abort = &s.abort;
   const int rank = static_cast<int>(blockIdx.x % a.split), tile = static_cast<int>(blockIdx.x / a.split);
-  const int n0 = tile / a.row_tiles * 128, m0 = tile % a.row_tiles * a.rows;
+  const int n0 = tile / a.row_tiles * a.cols, m0 = tile % a.row_tiles * a.rows;
   const int kb0 = static_cast<int>(static_cast<long long>(a.kblocks) * rank / a.split);
   const int kb1 = static_cast<int>(static_cast<long long>(a.kblocks) * (rank + 1) / a.split);
-  const int stage_bytes = W_BYTES + a.rows * BK * 2;
+  // The MMA's M side is 128 rows: past `cols` it reads what follows in shared memory, and its N side
+  // past x_rows what an earlier stage left there; those sums are not stored.
+  const int w_bytes = a.cols * BK * 2, stage_bytes = w_bytes + a.rows * BK * 2;
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
 
@@ -190,9 +217,9 @@ __global__ void __launch_bounds__(S_THREADS, 2)
       }
       if (issuer) {
         uint8_t* p = ring + slot * stage_bytes;
-        mbar_arrive_expect_tx(&s.full[slot], stage_bytes);
+        mbar_arrive_expect_tx(&s.full[slot], w_bytes + a.x_rows * BK * 2);
         tma_load_2d(p, &mapW, &s.full[slot], kb * BK, n0);
-        tma_load_2d(p + W_BYTES, &mapX, &s.full[slot], kb * BK, m0);
+        tma_load_2d(p + w_bytes, &mapX, &s.full[slot], kb * BK, m0);
       }
       issued_mask |= 1u << slot;
       last_phase_bits = (last_phase_bits & ~(1u << slot)) | (phase << slot);
@@ -216,7 +243,8 @@ __global__ void __launch_bounds__(S_THREADS, 2)
         break;
       }
       tc_fence_after();
-      const uint64_t dw = desc0 + static_cast<uint64_t>((slot * stage_bytes) >> 4), dx = dw + (W_BYTES >> 4);
+      const uint64_t dw = desc0 + static_cast<uint64_t>((slot * stage_bytes) >> 4);
+      const uint64_t dx = dw + static_cast<uint64_t>(w_bytes >> 4);
       if (leader) {
 #pragma unroll
         for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
@@ -269,8 +297,12 @@ __global__ void __launch_bounds__(S_THREADS, 2)
     const int n = n0 + lane * 4;
     float b[4];
     load_bias4(b, a.e, n);
+    const bool mine = lane * 4 < a.cols && n < a.e.N && !*abort;
+    const int end = min(r1, a.e.M - m0);
 #pragma unroll 1
-    for (int r = r0 + warp; r < r1 && m0 + r < a.e.M; r += S_THREADS / 32) {
+    for (int r = r0 + warp; r < end; r += S_THREADS / 32) {
+      float4 res = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (mine) res = load_residual4(a.e, m0 + r, n);
       float4 u[S_MAX_SPLIT];
 #pragma unroll
       for (int j = 0; j < S_MAX_SPLIT; ++j)
@@ -284,7 +316,7 @@ __global__ void __launch_bounds__(S_THREADS, 2)
           v.z += u[j].z;
           v.w += u[j].w;
         }
-      if (n < a.e.N && !*abort) finish4(a.e, m0 + r, n, v, b);
+      if (mine) finish4(a.e, m0 + r, n, v, b, res);
     }
   }
   cluster_sync();  // no CTA leaves while another reads its sums
@@ -494,7 +526,8 @@ __global__ void __launch_bounds__(P_THREADS, 1)
         if (n < a.e.N)
 #pragma unroll 2
           for (int r = et >> 5; r < 32 && c + r < rows; r += 4)
-            finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias);
+            finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias,
+                    load_residual4(a.e, m0 + c + r, n));
       }
       tc_fence_before();
       __syncwarp();
@@ -521,8 +554,12 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 
 }  // namespace ln
 
-// Tiles of 256 x 256 from which the pair kernel takes a product of more than 128 rows.
-constexpr int kLinearPairTiles = 48;
+// The pair kernel takes products of at least kLinearPairRows rows and kLinearPairTiles tiles of
+// 256 x 256. Measured, pairs against the split kernel with tiles of 128 columns (us, graph
+// replays, K x N): 64 rows, 2048 x 32003 (126 tiles) 28.8 / 30.2, 4096 x 14336 (56) 25.9 / 26.6,
+// 4096 x 4096 (16) 18.3 / 12.6; 128 rows 32.6 / 36.5, 28.4 / 30.5, 21.0 / 15.4; 512 rows,
+// 4096 x 4096 (32) 28.9 / 23.8, 768 (48) 29.3 / 36.7.
+constexpr int kLinearPairRows = 64, kLinearPairTiles = 48;
 
 static cudaError_t linear_attr() {
   const cudaError_t e = cudaFuncSetAttribute(ln::linear_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -575,10 +612,9 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   int rc;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
-  if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
   // pairs: even row tiles of at most 256 rows
   const long long p_tiles = div_up(M, 256) * div_up(N, 256);
-  if (M > 128 && p_tiles >= kLinearPairTiles) {
+  if (M >= kLinearPairRows && p_tiles >= kLinearPairTiles) {
     PairArgs a{};
     a.e = e;
     a.row_tiles = static_cast<int>(div_up(M, 256));
@@ -589,6 +625,7 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     a.limit_ns = wait_limit_ns();
     if ((long long)a.row_tiles * a.col_tiles > INT32_MAX / 2)
       return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+    if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
     if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
     const int most = linear_resident_pairs(), tiles = a.row_tiles * a.col_tiles;
     cluster_config(cfg, attr, 2, stream);
@@ -607,23 +644,40 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   a.row_tiles = static_cast<int>(div_up(M, a.rows));
   a.kblocks = kblocks;
   a.limit_ns = wait_limit_ns();
-  const long long tiles = a.row_tiles * div_up(N, 128);
-  if (tiles > INT32_MAX / S_MAX_SPLIT) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
-  // K over as many CTAs as two an SM leave room for, four K blocks each at least
-  const int sms = num_sms();
+  long long tiles = a.row_tiles * div_up(N, 128);
+  if (a.row_tiles * div_up(N, 80) > INT32_MAX / S_MAX_SPLIT)
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+  // K over as many CTAs as two an SM leave room for, four K blocks each at least: two rings hide each
+  // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
+  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4). Sums of 96 rows and more are exchanged between four at
+  // most (128 rows, 4096 x 4096: four 13.9, eight 15.4).
+  const int sms = num_sms(), most_split = a.rows >= 96 ? 4 : S_MAX_SPLIT;
   a.split = 1;
-  while (a.split * 2 <= S_MAX_SPLIT && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
-  // one CTA an SM takes a ring of most of its shared memory, two half of it each
-  const int stage = W_BYTES + a.rows * BK * 2, most = tiles * a.split <= sms ? 220 * 1024 : 108 * 1024;
+  while (a.split * 2 <= most_split && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
+  a.cols = 128;
+  if (a.split <= 2 && tiles * a.split > sms && tiles * a.split <= 2ll * sms) {
+    // narrower tiles where that gives every SM two CTAs (1 row, 4096 x 14336: 128 columns 23.7 us,
+    // 96 22.9; 512 rows, 2048 x 5632: 128 25.4, 80 24.6). Wider clusters do not fill the GPCs.
+    const int even = static_cast<int>(div_up(div_up((long long)N * a.row_tiles * a.split, 2 * sms), 16) * 16);
+    a.cols = even < 80 ? 80 : even < 128 ? even : 128;
+    if (a.row_tiles * div_up(N, a.cols) * a.split > 2ll * sms) a.cols = 128;
+    tiles = a.row_tiles * div_up(N, a.cols);
+  }
+  // one CTA an SM takes a ring of most of its shared memory, two half of it each; behind it what the
+  // MMA reads past the last stage's weights
+  const int stage = (a.cols + a.rows) * BK * 2, over = W_BYTES > stage ? W_BYTES - stage : 0;
+  const int room = (tiles * a.split <= sms ? 220 * 1024 : 108 * 1024) - over;
   const int share = (kblocks + a.split - 1) / a.split, need = (a.rows * 512 + stage - 1) / stage;
-  a.stages = most / stage < S_MAX_STAGES ? most / stage : S_MAX_STAGES;
+  a.stages = room / stage < S_MAX_STAGES ? room / stage : S_MAX_STAGES;
   if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
+  a.x_rows = M < a.rows ? M : a.rows;
+  if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols))) return rc;
   a.tmem_cols = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
-  if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows))) return rc;
+  if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.x_rows))) return rc;
   cluster_config(cfg, attr, a.split, stream);
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split), 1, 1);
   cfg.blockDim = dim3(S_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = a.stages * stage + 1024;
+  cfg.dynamicSmemBytes = a.stages * stage + over + 1024;
   const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_split_kernel, mW, mX, a);
   if (ce != cudaSuccess) return cuda_fail(ce, "linear_split_kernel");
   OM_LAUNCHED("linear_split_kernel");

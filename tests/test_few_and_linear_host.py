@@ -1,0 +1,185 @@
+"""What needs no GPU of the few-token layer and of the matrix product: the C ABI's refusals, found
+before anything is enqueued (addresses that are passed are not read), sizes of the workspace,
+the binding's checks, and barriers read from the sources."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2607_17154_gb300 import binding as B
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                    "paper_2607_17154_gb300", "csrc")
+OK, ARG, SHAPE = B.OK, B.ERR_INVALID_ARG, B.ERR_UNSUPPORTED_SHAPE
+AT = 1 << 20  # an aligned address that a refused call never reads
+N = None
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2607_17154_gb300 import build
+    build.build()
+
+
+def desc(**over):
+    v = dict(T_max=1, E=8, d=256, dff=512, k=2, renorm=1, W_r=AT, W1=AT, W3=AT, W2=AT, tables=AT,
+             tables_bytes=1 << 16, scratch=N, scratch_bytes=0, lookahead_H=1, tables_stride=0, P=N)
+    v.update(over)
+    return B.LayerDesc(**v)
+
+
+def few(d=None, T=4, X=AT, home=AT, loc=N, qhat=N, y=AT, ws=AT, nbytes=1 << 30):
+    rc = B.lib().ordermoe_layer_few(ctypes.byref(d or desc()), T, X, home, loc, qhat, y, N, ws, nbytes, N)
+    return rc, B.lib().ordermoe_last_error().decode()
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(E=0), SHAPE), (dict(E=65), SHAPE), (dict(k=0), SHAPE), (dict(k=9, E=16), SHAPE), (dict(k=9), SHAPE),
+    (dict(d=128), SHAPE), (dict(d=0), SHAPE), (dict(d=33024), SHAPE), (dict(dff=64), SHAPE), (dict(dff=0), SHAPE),
+    (dict(E=64, dff=1 << 26), SHAPE), (dict(lookahead_H=5), SHAPE),
+    (dict(W_r=N), ARG), (dict(W1=N), ARG), (dict(W3=N), ARG), (dict(W2=N), ARG), (dict(tables=N), ARG),
+    (dict(W_r=AT + 8), ARG), (dict(W1=AT + 2), ARG), (dict(W2=AT + 8), ARG), (dict(tables=AT + 8), ARG),
+    (dict(tables_bytes=100), ARG)])
+def test_layers_that_layer_few_refuses(over, code):
+    for T in (4, 0):  # also where there is nothing to do
+        rc, msg = few(desc(**over), T=T)
+        assert rc == code and msg.startswith("layer_few:"), (over, rc, msg)
+
+
+@pytest.mark.parametrize("call,code", [
+    (dict(T=-1), ARG), (dict(T=17), SHAPE), (dict(X=N), ARG), (dict(home=N), ARG), (dict(y=N), ARG), (dict(X=AT + 8), ARG),
+    (dict(y=AT + 2), ARG), (dict(loc=AT), ARG), (dict(qhat=AT), ARG), (dict(ws=N), ARG), (dict(ws=AT + 16), ARG),
+    (dict(nbytes=1000), ARG)])
+def test_calls_that_layer_few_refuses(call, code):
+    rc, msg = few(**call)
+    assert rc == code and msg.startswith("layer_few:"), (call, rc, msg)
+
+
+def test_no_tokens():
+    assert few(T=0, X=N, home=N, y=N, ws=N, nbytes=0)[0] == OK
+    assert B.lib().ordermoe_layer_few(N, 0, N, N, N, N, N, N, N, 0, N) == ARG
+
+
+def test_layer_few_residual_refuses():
+    d = desc()
+
+    def call(T=4, x=AT, h=AT, eps=1e-6, h_out=AT, x_out=AT):
+        return B.lib().ordermoe_layer_few_residual(ctypes.byref(d), T, x, AT, AT, N, N, eps, h_out, x_out, N, AT, 0, N) \
+            if h else B.lib().ordermoe_layer_few_residual(ctypes.byref(d), T, x, N, AT, N, N, eps, h_out, x_out, N, AT, 0, N)
+    for kw in (dict(h=N), dict(x_out=N), dict(h_out=N), dict(x=N), dict(eps=0.0), dict(eps=-1.0),
+               dict(eps=float("nan")), dict(x_out=AT + 8), dict(h_out=AT + 8), dict()):  # the last: no workspace
+        assert call(**kw) == ARG, kw
+        assert B.lib().ordermoe_last_error().decode().startswith("layer_few_residual:")
+
+
+def test_workspace_sizes():
+    size = B.ordermoe_layer_few_workspace_bytes
+    for shape in ((8, 256, 512, 2), (64, 2048, 1408, 6), (8, 4096, 14336, 2)):
+        sizes = [size(T, *shape) for T in range(1, 17)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0  # enough for every smaller T
+        E, d, dff, k = shape
+        assert sizes[-1] >= min(E, 16 * k) * 16 * dff * 2
+    for bad in ((0, 8, 256, 512, 2), (17, 8, 256, 512, 2), (4, 65, 256, 512, 2), (4, 8, 0, 512, 2), (4, 8, 256, 512, 9),
+                (4, 2, 256, 512, 3)):
+        assert size(*bad) == 0
+    assert B.lib().ordermoe_layer_few_init(N, 1 << 20, N) == ARG
+    assert B.lib().ordermoe_layer_few_init(AT, 128, N) == ARG
+    assert B.lib().ordermoe_layer_few_init(AT + 64, 1 << 20, N) == ARG
+
+
+def linear(X=AT, ldx=64, W=AT, ldw=64, bias=N, act=0, residual=N, ldr=0, M=4, n=32, K=64, Y=AT, ldy=32, f32=0):
+    rc = B.lib().ordermoe_linear(X, ldx, W, ldw, bias, act, residual, ldr, M, n, K, Y, ldy, f32, N)
+    return rc, B.lib().ordermoe_last_error().decode()
+
+
+@pytest.mark.parametrize("call,code", [
+    (dict(M=-1), ARG), (dict(n=0), ARG), (dict(K=0), ARG), (dict(act=-1), ARG), (dict(act=5), ARG),
+    (dict(ldx=56), ARG), (dict(ldw=63), ARG), (dict(ldy=31), ARG), (dict(residual=AT, ldr=31), ARG),
+    (dict(ldx=65), SHAPE), (dict(ldw=68), SHAPE), (dict(ldx=1 << 38), SHAPE), (dict(ldw=1 << 40), SHAPE),
+    (dict(X=N), ARG), (dict(W=N), ARG), (dict(Y=N), ARG), (dict(X=AT + 8), ARG), (dict(W=AT + 2), ARG),
+    (dict(Y=AT + 1), ARG), (dict(Y=AT + 2, f32=1), ARG), (dict(bias=AT + 1), ARG), (dict(residual=AT + 1, ldr=32), ARG)])
+def test_calls_that_linear_refuses(call, code):
+    rc, msg = linear(**call)
+    assert rc == code and msg.startswith("linear:"), (call, rc, msg)
+
+
+def test_linear_of_no_rows():
+    assert linear(M=0, X=N, W=N, Y=N)[0] == OK
+
+
+def test_binding_refuses_host_tensors_types_and_shapes(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    bf = torch.bfloat16
+    X, W, Y = torch.zeros(4, 64, dtype=bf), torch.zeros(32, 64, dtype=bf), torch.zeros(4, 32, dtype=bf)
+    for args, err in (((X, W, Y), ValueError),                                     # not on the GPU
+                      ((X.float(), W, Y), TypeError), ((X[0], W, Y), TypeError),
+                      ((X, W, None), TypeError)):
+        with pytest.raises(err):
+            B.ordermoe_linear(*args)
+    with pytest.raises(ValueError):
+        B.ordermoe_linear(X, W, Y, act="tanh")
+
+    class Fake:  # a device tensor
+        def __init__(self, device, stride=(64, 1), dtype=bf):
+            self.dtype, self.shape, self.device_, self.stride_ = dtype, (4, 64), device, stride
+
+        def get_device(self):
+            return self.device_
+
+        def stride(self, i):
+            return self.stride_[i]
+
+        def data_ptr(self):
+            return AT
+    assert B._matrix(Fake(0), "X", (4, 64), 0) == (AT, 64)
+    assert B._matrix(Fake(0, (80, 1)), "X", (4, 64), 0) == (AT, 80)
+    for t, shape, err, what in ((Fake(1), (4, 64), ValueError, "current device"), (Fake(0), (4, 63), ValueError, "must be"),
+                                (Fake(0, dtype=torch.float16), (4, 64), TypeError, "must be"),
+                                (Fake(0, (1, 4)), (4, 64), ValueError, "contiguous"),
+                                (Fake(0, (0, 1)), (4, 64), ValueError, "overlap")):
+        with pytest.raises(err, match=what):
+            B._matrix(t, "X", shape, 0)
+    with pytest.raises(ValueError):
+        B._entries(X, "X", bf, 4 * 64, 0)
+    with pytest.raises(TypeError):
+        B._entries(X, "X", torch.float32, 1, 0)
+    assert B._entries(None, "loc", torch.uint8, 4, 0) is None
+    with pytest.raises(ValueError):
+        u8 = torch.zeros(1 << 12, dtype=torch.uint8)
+        B.ordermoe_layer_few(desc(), 4, X, u8, None, None, X, u8)
+
+
+def kernel(path, name):
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
+    start = text.index("{", text.index(name + "("))
+    depth = 0
+    for i in range(start, len(text)):
+        depth += {"{": 1, "}": -1}.get(text[i], 0)
+        if depth == 0:
+            return text[start:i]
+
+
+def test_cluster_barriers_around_the_accesses_to_a_peer():
+    """The peers' shared memory is reached through helpers: behind a cluster barrier (every CTA runs),
+    and no CTA leaves before another barrier."""
+    for path, name, helper in (("linear.cu", "linear_split_kernel", "load_rank("),
+                               ("linear.cu", "linear_pair_kernel", "lead_barrier("),
+                               ("few_tokens.cu", "few_tokens_kernel", "store_both(")):
+        body = kernel(path, name)
+        assert "mapa_shared(" not in body
+        first, last = body.index(helper), body.rindex(helper)
+        assert 0 <= body.find("cluster_sync()") < first, name
+        assert body.find("cluster_sync()", last) > last, name
+
+
+def test_waits_of_the_new_kernels_are_bounded():
+    """Every wait goes through a helper that takes a limit; no loop tries a barrier by itself."""
+    for path in ("few_tokens.cu", "linear.cu"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
+        assert "mbar_try_wait" not in text
+        assert all("limit_ns" in m for m in re.findall(r"mbar_wait\((.*?)\)\)?[;,)]", text, flags=re.S))
+        assert text.count("while (true)") == text.count("for (;;)") == 0
+    body = kernel("few_tokens.cu", "bool grid_wait")
+    assert "limit_ns" in body and "return false" in body
