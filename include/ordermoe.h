@@ -366,9 +366,9 @@ int ordermoe_layer_forward_residual(const ordermoe_layer_desc* layer, int T, con
  * One whole MoE layer for a few tokens (a decoding batch of 1 to 16) in one
  * launch: what ordermoe_layer_forward and ordermoe_layer_forward_residual
  * compute, for calls whose time is one pass over the chosen experts' weights
- * and the latency of the launches. Differences: an expert's output is not
- * rounded to bf16 before the weighted sum,
- *   y[t] = bf16( sum_j topk_w[t][j] W2_e H_j ),  H_j = bf16( silu(W1_e x) * (W3_e x) ),
+ * and the latency of the launches. Differences: neither the activations nor an
+ * expert's output are rounded to bf16 on the way,
+ *   y[t] = bf16( sum_j topk_w[t][j] W2_e H_j ),  H_j = silu(W1_e x) * (W3_e x) to 16 bits
  * (fp32 sums in a fixed order, expert after expert, so the same call gives the
  * same bits), and the router logits are summed in another order: decisions are
  * those of ordermoe_route_select from the logits that `out` returns.

@@ -18,7 +18,8 @@
 //            sums of a row tile go to the workspace;
 //   finish   one CTA a token adds the partials of every row tile in CTA order and
 //            writes y, or h + y and its norm.
-// Sums are fp32 in a fixed order: the same call gives the same bits.
+// H, the SwiGLU activations, are handed on as the sum of two bf16 and the experts' outputs stay in
+// fp32, so y is rounded once. Sums are fp32 in a fixed order: the same call gives the same bits.
 // Two producer warps stream the weights and the tokens' K blocks through a ring of TMA
 // boxes with the 128-byte swizzle; eight MMA warps take its slots in turn; an
 // epilogue warp adds their eight partial accumulators. Between gate/up and down
@@ -122,7 +123,7 @@ struct Args {
   uint8_t* kind;
   int32_t* counters;
   unsigned int* sync;  // [0] gate/up done, [1] down done, [2] left: zero between launches
-  uint16_t* H;         // [n_act][T][dff]
+  uint16_t* H;         // [n_act][2][T][dff]: bf16 parts that add up to it
   float* part;         // [row tile + CTA][T][DOWN_ROWS]
   uint64_t limit_ns;
 };
@@ -172,26 +173,33 @@ __device__ __forceinline__ bool grid_wait(const unsigned int* count, unsigned in
 // ldmatrix phase reads are in different banks. Columns past T read the first
 // token's row and are dropped later. (Boxes of 8 or 16 rows, zero-filled past T, took
 // TMA's time for every row: it copies a row of 128 bytes in about 3 cycles.)
-template <int TILES, int NT, int KB>
+// PARTS 2: the tokens' rows are followed by T rows that are added to them (H in two parts).
+template <int TILES, int NT, int KB, int PARTS = 1>
 __device__ __forceinline__ void mma_stage(float (&acc)[TILES][NT][4], uint32_t w, uint32_t kb_pitch,
                                           uint32_t hi, uint32_t tile_pitch, uint32_t x, int T, int lane) {
   const uint32_t r = lane & 7;
   const uint32_t wr = w + ((lane >> 3) & 1) * hi + r * 128;
-  uint32_t xr[NT];  // the lane's token rows
+  uint32_t xr[PARTS][NT];  // the lane's token rows
 #pragma unroll
-  for (int n = 0; n < NT; ++n) xr[n] = static_cast<int>(n * 8 + r) < T ? n * 8 + r : 0;
+  for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xr[p][n] = p * T + (static_cast<int>(n * 8 + r) < T ? n * 8 + r : 0);
   const uint32_t wc = lane >> 4, xc = lane >> 3;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
     if (kb > 0)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) xr[n] += T;
+      for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) xr[p][n] += PARTS * T;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {  // 32 elements: two K steps of the MMA
-      uint32_t b[NT][4];
+      uint32_t b[PARTS][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        ldmatrix4(b[n], x + xr[n] * 128 + (((half * 4 + xc) ^ (xr[n] & 7)) << 4));
+      for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          ldmatrix4(b[p][n], x + xr[p][n] * 128 + (((half * 4 + xc) ^ (xr[p][n] & 7)) << 4));
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
 #pragma unroll
@@ -199,7 +207,9 @@ __device__ __forceinline__ void mma_stage(float (&acc)[TILES][NT][4], uint32_t w
           uint32_t a[4];
           ldmatrix4(a, wr + kb * kb_pitch + i * tile_pitch + (((half * 4 + s * 2 + wc) ^ r) << 4));
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma16816(acc[i][n], a, b[n][2 * s], b[n][2 * s + 1]);
+          for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma16816(acc[i][n], a, b[p][n][2 * s], b[p][n][2 * s + 1]);
         }
       }
     }
@@ -783,7 +793,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     // down: the weights of a stage as soon as its slot is free, H behind the barrier
     // that every CTA's gate/up passes
-    const uint32_t bytes = C::W_BYTES + a.T * KB_DOWN * 128;
+    const uint32_t bytes = C::W_BYTES + 2 * a.T * KB_DOWN * 128;
     Walk w(share), hw(share);
     Ring first = ring_at;
     auto load_w = [&]() {
@@ -793,7 +803,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     auto load_h = [&]() {
       if (issuer)
-        tma_load_3d(slot_ptr(first.slot) + C::W_BYTES, &maps.H, &s.full[first.slot], hw.act * a.T,
+        tma_load_3d(slot_ptr(first.slot) + C::W_BYTES, &maps.H, &s.full[first.slot], hw.act * 2 * a.T,
                     hw.k * KB_DOWN);
     };
     auto next_w = [&]() {
@@ -854,7 +864,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (ring_at.slot % MMA_WARPS == warp) {
         if (!(ok = arrived())) break;
         const uint32_t p = ring0 + ring_at.slot * C::STAGE_BYTES;
-        mma_stage<2 * MT, NT, KB_DOWN>(acc, p, 4096 * MT, 1024, 2048, p + C::W_BYTES, a.T, lane);
+        mma_stage<2 * MT, NT, KB_DOWN, 2>(acc, p, 4096 * MT, 1024, 2048, p + C::W_BYTES, a.T, lane);
         release();
         any = true;
       }
@@ -907,12 +917,25 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int u = cta; u < n_units && ok; u += G) {
       const int e = u / per, f0 = (u - e * per) * 8 * MT + (lane >> 2);
       ok = take_unit([&](int m, int n, float4 v) {
-        // rows 0-7 gate, 8-15 up: silu(g) u, rounded to bf16 as ordermoe_expert_ffn's H
+        // rows 0-7 gate, 8-15 up: silu(g) u as the sum of two bf16 (16 bits: one bf16 would double
+        // the error of y, and flip roundings of h_out that the next norm carries on; at a few
+        // tokens the second part costs no time, HBM bounds it)
         const int t = n * 8 + (lane & 3) * 2;
-        uint16_t* out = a.H + (static_cast<size_t>(e) * a.T + t) * a.dff + f0 + m * 8;
-        const uint32_t pk = pack_bf16x2(v.x / (1.0f + __expf(-v.x)) * v.z, v.y / (1.0f + __expf(-v.y)) * v.w);
-        if (t < a.T) out[0] = static_cast<uint16_t>(pk & 0xFFFFu);
-        if (t + 1 < a.T) out[a.dff] = static_cast<uint16_t>(pk >> 16);
+        uint16_t* out = a.H + (static_cast<size_t>(e) * 2 * a.T + t) * a.dff + f0 + m * 8;
+        const float h0 = v.x / (1.0f + __expf(-v.x)) * v.z, h1 = v.y / (1.0f + __expf(-v.y)) * v.w;
+        const uint32_t hi = pack_bf16x2(h0, h1);
+        const float r0 = h0 - bf16_lo(hi), r1 = h1 - bf16_hi(hi);
+        // (an infinite part has no rest)
+        const uint32_t lo = pack_bf16x2(isfinite(r0) ? r0 : 0.0f, isfinite(r1) ? r1 : 0.0f);
+        const size_t rest = static_cast<size_t>(a.T) * a.dff;
+        if (t < a.T) {
+          out[0] = static_cast<uint16_t>(hi & 0xFFFFu);
+          out[rest] = static_cast<uint16_t>(lo & 0xFFFFu);
+        }
+        if (t + 1 < a.T) {
+          out[a.dff] = static_cast<uint16_t>(hi >> 16);
+          out[rest + a.dff] = static_cast<uint16_t>(lo >> 16);
+        }
       });
     }
     fence_proxy_async();  // H is read by the other CTAs' TMA loads
@@ -1093,7 +1116,7 @@ static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) 
   };
   const size_t R = (size_t)T * k, act = R < (size_t)E ? R : (size_t)E;
   s.sync = reinterpret_cast<unsigned int*>(take(16));
-  s.H = reinterpret_cast<uint16_t*>(take(act * T * dff * 2));
+  s.H = reinterpret_cast<uint16_t*>(take(act * 2 * T * dff * 2));
   // rows of 32 (T <= 4) or 64 columns: a row tile's partials, one for each CTA more
   const size_t rows = T <= 4 ? 32 : 64;
   s.part = reinterpret_cast<float*>(take((d / rows + kFewMaxCtas) * T * rows * 4));
@@ -1130,7 +1153,7 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   if ((rc = make_tmap_bf16_kb(&m.W1, L->W1, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W3, L->W3, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W2, L->W2, (uint64_t)a.E * a.d, a.dff, C::DOWN_ROWS, fw::KB_DOWN))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.H, a.H, (uint64_t)act * a.T, a.dff, a.T, fw::KB_DOWN))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.H, a.H, (uint64_t)act * 2 * a.T, a.dff, 2 * a.T, fw::KB_DOWN))) return rc;
   a.stages = fw::stages<MT, NT>(a.E);
   // a CTA per SM, fewer where there are not as many units of gate/up
   int grid = num_sms() < kFewMaxCtas ? num_sms() : kFewMaxCtas;

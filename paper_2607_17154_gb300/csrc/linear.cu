@@ -13,6 +13,9 @@
 //   linear_pair_kernel: persistent CTA pairs, tiles of 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
 //     main loop. For batches with a tile for most pairs, bound by the tensor cores.
+// The tensor cores truncate a running sum, an error that grows with K (2e-6 of the result at K = 2048,
+// against 4e-7 of fp32 FMAs). Where the sums leave in fp32 (F32), the epilogue warps therefore take
+// the accumulator every 512 of K and add it to sums in registers; bf16 results do not see it.
 // Rows and columns past M, N and K are zero-filled by TMA and not stored. Every wait is bounded; one that
 // runs out reports ORDERMOE_DEV_WAIT_TIMEOUT, and the copies and MMAs under way are drained.
 #include "common.cuh"
@@ -32,6 +35,9 @@ namespace ln {
 
 constexpr int BK = 64;                 // K block: 128 bytes a row
 constexpr int W_BYTES = 128 * BK * 2;  // 128 weight rows of a K block
+constexpr int F32_BLOCKS = 8;          // K blocks that an fp32 result's accumulator sums up
+constexpr int F32_ROWS = 64;           // rows of the split kernel's tiles then: sums in 64 registers
+constexpr int F32_PAIR_ROWS = 128;     // and of the pair kernel's, over two groups of warps
 
 struct Epilogue {
   int M, N;
@@ -135,7 +141,7 @@ constexpr int S_MAX_SPLIT = 8;
 
 struct SplitSmem {
   uint64_t full[S_MAX_STAGES], empty[S_MAX_STAGES];
-  uint64_t tfull, drain;
+  uint64_t tfull[2], tempty[2], drain;
   uint32_t tmem_base;
   int abort, zero;
 };
@@ -160,6 +166,7 @@ __device__ __forceinline__ float4 load_rank(const float* p, uint32_t rank) {
   return v;
 }
 
+template <bool F32>
 __global__ void __launch_bounds__(S_THREADS, 2)
     linear_split_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
                         const __grid_constant__ SplitArgs a) {
@@ -179,7 +186,10 @@ __global__ void __launch_bounds__(S_THREADS, 2)
       mbar_init(&s.full[i], 1);
       mbar_init(&s.empty[i], 1);
     }
-    mbar_init(&s.tfull, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.tfull[i], 1);
+      mbar_init(&s.tempty[i], 4);  // every epilogue warp
+    }
     mbar_init(&s.drain, 1);
     s.abort = 0;
     s.zero = 0;
@@ -204,6 +214,7 @@ __global__ void __launch_bounds__(S_THREADS, 2)
   const int w_bytes = a.cols * BK * 2, stage_bytes = w_bytes + a.rows * BK * 2;
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
+  const int part = F32 ? F32_BLOCKS : kb1 - kb0;  // K blocks of an accumulator, two in turn
 
   if (warp == 0) {
     const bool issuer = elect_one();
@@ -235,48 +246,91 @@ __global__ void __launch_bounds__(S_THREADS, 2)
     int slot = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int kb = kb0; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
-        if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 42);
+    int u = 0;
+    for (int first = kb0; first < kb1 && ok; first += part, ++u) {
+      const int end = min(first + part, kb1), b = u & 1;
+      if (!__all_sync(0xffffffffu, mbar_wait(&s.tempty[b], ((u >> 1) & 1) ^ 1u, a.limit_ns, abort))) {
+        if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 44);
         *abort = 1;
-        ok = false;
         break;
       }
       tc_fence_after();
-      const uint64_t dw = desc0 + static_cast<uint64_t>((slot * stage_bytes) >> 4);
-      const uint64_t dx = dw + static_cast<uint64_t>(w_bytes >> 4);
-      if (leader) {
+      for (int kb = first; kb < end; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
+          if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 42);
+          *abort = 1;
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint64_t dw = desc0 + static_cast<uint64_t>((slot * stage_bytes) >> 4);
+        const uint64_t dx = dw + static_cast<uint64_t>(w_bytes >> 4);
+        if (leader) {
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
-          mma_bf16(tmem_base, dw + 2 * kk, dx + 2 * kk, idesc, kb != kb0 || kk != 0 ? 1u : 0u);
-        mma_commit(&s.empty[slot]);
+          for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
+            mma_bf16(tmem_base + b * (a.tmem_cols / 2), dw + 2 * kk, dx + 2 * kk, idesc,
+                     kb != first || kk != 0 ? 1u : 0u);
+          mma_commit(&s.empty[slot]);
+        }
+        mma_issued = true;
+        if (++slot == a.stages) {
+          slot = 0;
+          phase ^= 1u;
+        }
       }
-      mma_issued = true;
-      if (++slot == a.stages) {
-        slot = 0;
-        phase ^= 1u;
+      if (ok && leader) mma_commit(&s.tfull[b]);
+      __syncwarp();
+    }
+  } else {
+    const int q = warp & 3;
+    const uint32_t tb = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+    float acc[F32 ? F32_ROWS / 32 : 1][32];
+    bool ok = true;
+    int u = 0;
+    for (int first = kb0; first < kb1 && ok; first += part, ++u) {
+      const int b = u & 1;
+      ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull[b], (u >> 1) & 1, a.limit_ns, abort));
+      if (!ok) {
+        if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 43);
+        *abort = 1;
+        break;
+      }
+      tc_fence_after();
+      if (F32) {
+#pragma unroll
+        for (int j = 0; j < F32_ROWS / 32; ++j) {
+          if (j * 32 >= a.rows) continue;
+          uint32_t v[32];
+          tmem_ld32(tb + b * (a.tmem_cols / 2) + j * 32, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            acc[j][i] = first == kb0 ? __uint_as_float(v[i]) : acc[j][i] + __uint_as_float(v[i]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.tempty[b]);
       }
     }
-    if (ok && leader) mma_commit(&s.tfull);
-    __syncwarp();
-  } else {
-    const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull, 0, a.limit_ns, abort));
-    if (!ok) {
-      if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 43);
-      *abort = 1;
-    } else {
-      tc_fence_after();  // the ring's copies and MMAs are done: its memory takes the sums
-      const int q = warp & 3;
-#pragma unroll 1
-      for (int c = 0; c < a.rows; c += 32) {
-        uint32_t v[32];
-        tmem_ld32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, v);
-        tmem_ld_wait();
+    if (ok) {  // the ring's copies and MMAs are done: its memory takes the sums
+      if (F32) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (c + i < a.rows) sums[(c + i) * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+        for (int j = 0; j < F32_ROWS / 32; ++j)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (j * 32 + i < a.rows) sums[(j * 32 + i) * 128 + q * 32 + lane] = acc[j][i];
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < a.rows; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(tb + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c + i < a.rows) sums[(c + i) * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+        }
+        tc_fence_before();
       }
-      tc_fence_before();
     }
   }
   __syncthreads();
@@ -368,6 +422,7 @@ __device__ __forceinline__ void group_sync(int group) {
   asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
 }
 
+template <bool F32>
 __global__ void __launch_bounds__(P_THREADS, 1)
     linear_pair_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
                        const __grid_constant__ PairArgs a) {
@@ -411,6 +466,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int total = a.row_tiles * a.col_tiles;
   const int half = a.rows / 2;  // rows of X in a CTA's shared memory
+  const int part = F32 ? F32_BLOCKS : a.kblocks;  // K blocks of an accumulator, two in turn
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
 
@@ -452,86 +508,124 @@ __global__ void __launch_bounds__(P_THREADS, 1)
       const uint32_t idesc = idesc_bf16_f32(256, a.rows);
       int slot = 0, it = 0;
       uint32_t phase = 0;
-      for (int tile = pair; tile < total; tile += pairs, ++it) {
-        const int b = it & 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(&s.tempty[b], ((it >> 1) & 1) ^ 1u, a.limit_ns, abort))) {
-          if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 52);
-          *abort = 1;
-          break;
-        }
-        tc_fence_after();
-        bool ok = true;
-        for (int kb = 0; kb < a.kblocks; ++kb) {
-          if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
-            if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 53);
+      bool ok = true;
+      for (int tile = pair; tile < total && ok; tile += pairs)
+        for (int first = 0; first < a.kblocks && ok; first += part, ++it) {
+          const int b = it & 1, end = min(first + part, a.kblocks);
+          if (!__all_sync(0xffffffffu, mbar_wait(&s.tempty[b], ((it >> 1) & 1) ^ 1u, a.limit_ns, abort))) {
+            if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 52);
             *abort = 1;
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint64_t dw = desc0 + static_cast<uint64_t>((slot * P_STAGE_BYTES) >> 4), dx = dw + (W_BYTES >> 4);
-          if (leader) {
+          for (int kb = first; kb < end; ++kb) {
+            if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
+              if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 53);
+              *abort = 1;
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint64_t dw = desc0 + static_cast<uint64_t>((slot * P_STAGE_BYTES) >> 4), dx = dw + (W_BYTES >> 4);
+            if (leader) {
 #pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
-              mma_bf16_pair(tmem_base + b * 256, dw + 2 * kk, dx + 2 * kk, idesc, (kb | kk) != 0 ? 1u : 0u);
-            mma_commit_pair(&s.empty[slot], 0x3);
+              for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
+                mma_bf16_pair(tmem_base + b * 256, dw + 2 * kk, dx + 2 * kk, idesc,
+                              kb != first || kk != 0 ? 1u : 0u);
+              mma_commit_pair(&s.empty[slot], 0x3);
+            }
+            mma_issued = true;
+            if (++slot == P_STAGES) {
+              slot = 0;
+              phase ^= 1u;
+            }
           }
-          mma_issued = true;
-          if (++slot == P_STAGES) {
-            slot = 0;
-            phase ^= 1u;
-          }
+          if (ok && leader) mma_commit_pair(&s.tfull[b], 0x3);
+          __syncwarp();
         }
-        if (!ok) break;
-        if (leader) mma_commit_pair(&s.tfull[b], 0x3);
-        __syncwarp();
-      }
     }
   } else {
     const int q = warp & 3, group = (warp - 2) >> 2, et = tid - 64 - 128 * group;
     float* chunk = chunks + group * P_CHUNK_FLOATS;
     int it = 0;
-    for (int tile = pair; tile < total; tile += pairs, ++it) {
-      const int b = it & 1;
-      // a wait that fails leaves the group together: the flag is agreed on behind a barrier
-      const bool waited = mbar_wait(&s.tfull[b], (it >> 1) & 1, a.limit_ns, abort);
+    bool go = true;
+    // this unit's accumulator is there: agreed on behind a barrier, so that a group that gives up
+    // leaves together
+    auto arrived = [&]() {
+      const bool waited = mbar_wait(&s.tfull[it & 1], (it >> 1) & 1, a.limit_ns, abort);
       if (!waited && !*abort) {
         report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 54);
         *abort = 1;
       }
-      uint32_t go;
+      uint32_t all;
       asm volatile(
           "{\n\t.reg .pred p, r;\n\tsetp.ne.u32 p, %1, 0;\n\t"
           "bar.red.and.pred r, %2, 128, p;\n\tselp.u32 %0, 1, 0, r;\n\t}"
-          : "=r"(go)
+          : "=r"(all)
           : "r"(static_cast<uint32_t>(waited)), "r"(1 + group)
           : "memory");
-      if (!go) break;
       tc_fence_after();
+      return all != 0;
+    };
+    auto taken = [&]() {  // its columns may be written again
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(lead_barrier(&s.tempty[it & 1]));
+      ++it;
+    };
+    for (int tile = pair; tile < total && go; tile += pairs) {
       int m0, n0;
       pair_tile(tile, a, m0, n0);
       const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * 128 + (et & 31) * 4;
+      const uint32_t tb = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
       float bias[4];
       load_bias4(bias, a.e, n);
-      const uint32_t tb = tmem_base + b * 256 + (static_cast<uint32_t>(q * 32) << 16);
-#pragma unroll 1
-      for (int c = group * 32; c < rows; c += 32 * P_GROUPS) {
-        uint32_t v[32];
-        tmem_ld32(tb + c, v);  // TMEM column = row c + i of the tile
-        tmem_ld_wait();
-        group_sync(group);     // the chunk before has been read
+      auto store = [&](const auto& v, int c) {  // rows c .. c + 31 of the tile
+        group_sync(group);  // the chunk before has been read
 #pragma unroll
-        for (int i = 0; i < 32; ++i) chunk[i * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+        for (int i = 0; i < 32; ++i) chunk[i * 128 + q * 32 + lane] = v(i);
         group_sync(group);
         if (n < a.e.N)
 #pragma unroll 2
           for (int r = et >> 5; r < 32 && c + r < rows; r += 4)
             finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias,
                     load_residual4(a.e, m0 + c + r, n));
+      };
+      if constexpr (F32) {
+        constexpr int CHUNKS = F32_PAIR_ROWS / 32 / P_GROUPS;
+        float acc[CHUNKS][32];
+        for (int first = 0; first < a.kblocks; first += part) {
+          if (!(go = arrived())) break;
+#pragma unroll
+          for (int j = 0; j < CHUNKS; ++j) {
+            const int c = (group + j * P_GROUPS) * 32;
+            if (c >= rows) continue;
+            uint32_t v[32];
+            tmem_ld32(tb + (it & 1) * 256 + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              acc[j][i] = first == 0 ? __uint_as_float(v[i]) : acc[j][i] + __uint_as_float(v[i]);
+          }
+          taken();
+        }
+        if (!go) break;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+          if ((group + j * P_GROUPS) * 32 < rows)
+            store([&](int i) { return acc[j][i]; }, (group + j * P_GROUPS) * 32);
+      } else {
+        if (!(go = arrived())) break;
+#pragma unroll 1
+        for (int c = group * 32; c < rows; c += 32 * P_GROUPS) {
+          uint32_t v[32];
+          tmem_ld32(tb + (it & 1) * 256 + c, v);  // TMEM column = row c + i of the tile
+          tmem_ld_wait();
+          store([&](int i) { return __uint_as_float(v[i]); }, c);
+        }
+        taken();
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_remote(lead_barrier(&s.tempty[b]));
     }
   }
 
@@ -561,11 +655,12 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 // 4096 x 4096 (32) 28.9 / 23.8, 768 (48) 29.3 / 36.7.
 constexpr int kLinearPairRows = 64, kLinearPairTiles = 48;
 
+template <bool F32>
 static cudaError_t linear_attr() {
-  const cudaError_t e = cudaFuncSetAttribute(ln::linear_split_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  const cudaError_t e = cudaFuncSetAttribute(ln::linear_split_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              227 * 1024 - static_cast<int>(sizeof(ln::SplitSmem)) - 256);
   if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(ln::linear_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ln::P_SMEM);
+  return cudaFuncSetAttribute(ln::linear_pair_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, ln::P_SMEM);
 }
 
 static void cluster_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, int size, cudaStream_t stream) {
@@ -592,7 +687,7 @@ static int linear_resident_pairs() {
     cfg.blockDim = dim3(ln::P_THREADS, 1, 1);
     cfg.dynamicSmemBytes = ln::P_SMEM;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_kernel, &cfg) != cudaSuccess || n <= 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_kernel<false>, &cfg) != cudaSuccess || n <= 0) {
       cudaGetLastError();
       n = num_sms() / 2;
     }
@@ -604,7 +699,10 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
                          const ln::Epilogue& e, cudaStream_t stream) {
   using namespace ln;
   static PerDevice cache;
-  const cudaError_t ae = static_cast<cudaError_t>(per_device(cache, [] { return static_cast<int>(linear_attr()); }));
+  const cudaError_t ae = static_cast<cudaError_t>(per_device(cache, [] {
+    const cudaError_t x = linear_attr<false>();
+    return static_cast<int>(x == cudaSuccess ? linear_attr<true>() : x);
+  }));
   if (ae != cudaSuccess) return cuda_fail(ae, "cudaFuncSetAttribute(linear)");
   const int kblocks = (K + BK - 1) / BK;
   auto div_up = [](long long x, long long y) { return (x + y - 1) / y; };
@@ -617,7 +715,7 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   if (M >= kLinearPairRows && p_tiles >= kLinearPairTiles) {
     PairArgs a{};
     a.e = e;
-    a.row_tiles = static_cast<int>(div_up(M, 256));
+    a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_PAIR_ROWS : 256));
     a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 32) * 32);
     a.row_tiles = static_cast<int>(div_up(M, a.rows));
     a.col_tiles = static_cast<int>(div_up(N, 256));
@@ -632,14 +730,15 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     cfg.gridDim = dim3(2 * (tiles < most ? tiles : most), 1, 1);
     cfg.blockDim = dim3(P_THREADS, 1, 1);
     cfg.dynamicSmemBytes = P_SMEM;
-    const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_kernel, mW, mX, a);
+    const cudaError_t ce = e.f32 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<true>, mW, mX, a)
+                                 : cudaLaunchKernelEx(&cfg, linear_pair_kernel<false>, mW, mX, a);
     if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_kernel");
     OM_LAUNCHED("linear_pair_kernel");
     return ORDERMOE_OK;
   }
   SplitArgs a{};
   a.e = e;
-  a.row_tiles = static_cast<int>(div_up(M, 128));
+  a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_ROWS : 128));
   a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 16) * 16);
   a.row_tiles = static_cast<int>(div_up(M, a.rows));
   a.kblocks = kblocks;
@@ -672,13 +771,14 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
   a.x_rows = M < a.rows ? M : a.rows;
   if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols))) return rc;
-  a.tmem_cols = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+  a.tmem_cols = a.rows <= 32 ? 64 : a.rows <= 64 ? 128 : 256;  // two accumulators
   if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.x_rows))) return rc;
   cluster_config(cfg, attr, a.split, stream);
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split), 1, 1);
   cfg.blockDim = dim3(S_THREADS, 1, 1);
   cfg.dynamicSmemBytes = a.stages * stage + over + 1024;
-  const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_split_kernel, mW, mX, a);
+  const cudaError_t ce = e.f32 ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, mW, mX, a)
+                               : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, mW, mX, a);
   if (ce != cudaSuccess) return cuda_fail(ce, "linear_split_kernel");
   OM_LAUNCHED("linear_split_kernel");
   return ORDERMOE_OK;

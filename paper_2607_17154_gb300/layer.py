@@ -79,7 +79,7 @@ class MoELayer:
 
     def forward_few(self, X, home, loc, qhat, y, T=None, stream=None):
         """forward() of at most B.FEW_TOKENS tokens in one launch: the decisions in the same
-        buffers, the combine's sum without the experts' bf16 rounding."""
+        buffers, y rounded once (neither H nor the experts' outputs are bf16 on the way)."""
         T = X.shape[0] if T is None else T
         assert T <= self.T_max and self.few_ws is not None
         B.ordermoe_layer_few(self.few_desc, T, X, home, loc, qhat, y, self.few_ws, self.few_out,

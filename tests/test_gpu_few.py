@@ -1,14 +1,13 @@
 """The few-token layer (ordermoe_layer_few, ordermoe_layer_few_residual) against the
 oracle's decisions on its own logits and the experts' formulas in 64 bits.
 
-Tolerance of y = bf16(sum_j w_j W2 H_j), H = bf16(silu(g) u): an element of H is off by
-at most half a bf16 step, 2^-8 of its value, so y by at most 2^-8 S, S = sum_j w_j sum_f
-|W2| |H_j|, and by the final rounding 2^-8 |y| (half a step more where the sum that is
-rounded is S 2^-8 away: 2^-8 (1 + 2^-8)). fp32 sums of K terms: at most K 2^-24 of the
-sum of magnitudes in g, u (their error reaches H through |dH/dg| <= 1.1 |u|, |dH/du| <=
-|silu|, here bounded by 2^-10 of S for K <= 4096 and unit-scale g, u) and in y (2^-11 S for
-d_ff k 2^-24 < 2^-11): together 2^-8 |y| + 1.5 2^-8 S.
-As a whole, both roundings are at most 2^-8 in the 2-norm and independent: 2 * 2^-8."""
+Tolerance of y = bf16(sum_j w_j W2 H_j), H = silu(g) u in two bf16: an element of H is off by
+at most 2^-16 of its value (half a step of the second part), so y by at most 2^-16 S, S = sum_j
+w_j sum_f |W2| |H_j|, and by the final rounding 2^-8 |y|. fp32 sums of K terms: at most K 2^-24
+of the sum of magnitudes in g, u (their error reaches H through |dH/dg| <= 1.1 |u|, |dH/du|
+<= |silu|, here bounded by 2^-10 of S for K <= 4096 and unit-scale g, u) and in y (2^-11 S for
+d_ff k 2^-24 < 2^-11): together 2^-8 |y| + 2^-9 S. As a whole, the rounding is at most 2^-8 in the
+2-norm, and the rest, independent from element to element, an eighth of that."""
 import numpy as np
 import pytest
 import torch
@@ -126,8 +125,8 @@ def assert_y(got, ref, mag, base=None):
     """got against base + ref by the bound above."""
     want = ref if base is None else base + ref
     off = np.abs(got - want)
-    assert (off <= STEP * np.abs(want) + 1.5 * STEP * mag + 1e-30).all(), (off / (STEP * (np.abs(want) + 1.5 * mag))).max()
-    assert np.linalg.norm(off) <= 2 * STEP * np.linalg.norm(np.abs(want))
+    assert (off <= STEP * np.abs(want) + 0.5 * STEP * mag + 1e-30).all(), (off / (STEP * (np.abs(want) + 0.5 * mag))).max()
+    assert np.linalg.norm(off) <= 1.125 * STEP * np.linalg.norm(np.abs(want))
 
 
 @pytest.mark.parametrize("T", [1, 2, 4, 5, 8, 9, 16])
@@ -293,7 +292,7 @@ def test_two_calls_at_once():
 def test_stack_of_few_tokens(H, T):
     """A stack with few=True against the same stack by the larger layers' launches: the decisions
     of every layer (near ties apart: none here) and the residual stream within the
-    roundings of both (an expert output's and H's, 2^-8 each, a layer)."""
+    roundings of the other (an expert output's, H's and the stream's, 2^-8 each, a layer)."""
     L, E, k, M, d, dff = 3, 8, 2, 4, 512, 256
     layers, sims = [], []
     for l in range(L):
