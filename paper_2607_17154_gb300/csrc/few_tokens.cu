@@ -216,6 +216,11 @@ __device__ __forceinline__ void mma_stage(float (&acc)[TILES][NT][4], uint32_t w
   }
 }
 
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
 // A value to the same place in both CTAs of the pair.
 __device__ __forceinline__ void store_both(float* p, uint32_t peer, float v) {
   *p = v;
@@ -496,7 +501,7 @@ struct Walk {
 };
 
 template <int MT, int NT>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     few_tokens_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
   using C = Cfg<MT, NT>;
   const int STAGES = a.stages;
@@ -511,6 +516,12 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = gridDim.x, cta = blockIdx.x;
   volatile int* abort = &s.abort;
+  // The pair is the kernel's own, not only the launch's: without it the peer's shared memory is
+  // no address. (A launch that a tool repeats may not carry every attribute.)
+  if (cluster_ctas() != 2) {
+    if (tid == 0) report(&g_err_route, ORDERMOE_DEV_BAD_INDEX, -3);
+    return;
+  }
 
   if (warp == MMA_WARPS + PRODUCERS && lane < static_cast<int>(sizeof(Maps) / sizeof(CUtensorMap)))
     tma_prefetch_map(reinterpret_cast<const CUtensorMap*>(&maps) + lane);
@@ -1166,15 +1177,11 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   cfg.blockDim = dim3(fw::THREADS, 1, 1);
   cfg.dynamicSmemBytes = a.stages * C::STAGE_BYTES + C::other_bytes(a.E);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;  // the CTAs wait for one another: all or none run
   attr[0].val.cooperative = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, fw::few_tokens_kernel<MT, NT>, m, a);
   if (e != cudaSuccess) return cuda_fail(e, "few_tokens_kernel");
   OM_LAUNCHED("few_tokens_kernel");
