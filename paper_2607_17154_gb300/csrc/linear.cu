@@ -51,8 +51,10 @@ struct Epilogue {
 
 // Each activation in fp32 from the product's sum; NaN stays NaN. Not inlined: the epilogue of a few
 // rows runs once, its instructions come from L2, and five activations a column made it longer
-// (301 x 1009 with SiLU 16.5 us).
-__device__ __noinline__ float4 activate4(float4 v, int act) {
+// (301 x 1009 with SiLU 16.5 us). A bf16 result takes the fast exponential and quotient (a few
+// 2^-23 off, 2^-9 of its rounding; 0 where the quotient is below 2^-119): 301 x 1009 with SiLU 12.9
+// -> 10.7 us.
+__device__ __noinline__ float4 activate4(float4 v, int act, int fast) {
   float f[4] = {v.x, v.y, v.z, v.w};
   if (act == ORDERMOE_ACT_RELU) {
 #pragma unroll
@@ -67,7 +69,8 @@ __device__ __noinline__ float4 activate4(float4 v, int act) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float g = 1.5957691216057308f * fmaf(0.044715f * f[j] * f[j], f[j], f[j]);
-      f[j] = f[j] / (1.0f + expf(silu ? -f[j] : -g));
+      const float u = silu ? -f[j] : -g;
+      f[j] = fast ? __fdividef(f[j], 1.0f + __expf(u)) : f[j] / (1.0f + expf(u));
     }
   }
   return make_float4(f[0], f[1], f[2], f[3]);
@@ -102,7 +105,7 @@ __device__ __forceinline__ float4 load_residual4(const Epilogue& e, int m, int n
 // Columns n .. n + 3 of row m from their sums v and their residual r.
 __device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 v, const float (&b)[4], float4 r) {
   v = make_float4(v.x + b[0], v.y + b[1], v.z + b[2], v.w + b[3]);
-  if (e.act != ORDERMOE_ACT_NONE) v = activate4(v, e.act);
+  if (e.act != ORDERMOE_ACT_NONE) v = activate4(v, e.act, !e.f32);
   float f[4] = {v.x, v.y, v.z, v.w};
   if (e.residual != nullptr) {  // (without one -0 stays -0)
     f[0] += r.x;
