@@ -13,6 +13,10 @@
 //   linear_pair_kernel: persistent CTA pairs, tiles of 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
 //     main loop. For batches with a tile for most pairs, bound by the tensor cores.
+//   linear_pair_split_kernel: one tile of 256 columns x up to 256 rows a cluster of 2 or 4 CTA
+//     pairs that share its K, the accumulators added as in the first kernel. For batches in between,
+//     whose tiles are too few for the pairs but whose operands, in tiles of 128 x 128, take
+//     longer from L2 than their products.
 // The tensor cores truncate a running sum, an error that grows with K (2e-6 of the result at K = 2048,
 // against 4e-7 of fp32 FMAs). Where the sums leave in fp32 (F32), the epilogue warps therefore take
 // the accumulator every 512 of K and add it to sums in registers; bf16 results do not see it.
@@ -649,6 +653,198 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   if (warp == 1) tmem_dealloc_pair(tmem_base, 512);
 }
 
+// ------------------------------------------------------ CTA pairs, K over a cluster
+constexpr int Q_STAGES = 6;
+constexpr int Q_SMEM = Q_STAGES * P_STAGE_BYTES + 1024;
+constexpr int Q_MAX_PAIRS = 4;
+
+struct PairSplitSmem {
+  uint64_t full[Q_STAGES], empty[Q_STAGES];
+  uint64_t tfull, drain;
+  uint32_t tmem_base;
+  int abort, zero;
+};
+
+struct PairSplitArgs {
+  Epilogue e;
+  int rows;  // of a tile: a multiple of 32, at most 256
+  int row_tiles, kblocks, pairs;
+  uint64_t limit_ns;
+};
+
+// The barrier of this pair's even CTA.
+__device__ __forceinline__ uint32_t pair_barrier(uint64_t* bar, uint32_t lead) {
+  return mapa_shared(smem_u32(bar), lead);
+}
+
+__global__ void __launch_bounds__(S_THREADS, 1)
+    linear_pair_split_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
+                             const __grid_constant__ PairSplitArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ PairSplitSmem s;
+  uint8_t* ring = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  float* sums = reinterpret_cast<float*>(ring);  // [rows][128], when the main loop is done
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_ctarank(), lead = rank & ~1u;
+  const int h = static_cast<int>(rank & 1u), pair = static_cast<int>(rank >> 1);
+  const bool even = h == 0;
+  pdl_trigger();
+  if (warp == 0 && lane == 0) {
+    tma_prefetch_map(&mapW);
+    tma_prefetch_map(&mapX);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < Q_STAGES; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    mbar_init(&s.tfull, 1);
+    mbar_init(&s.drain, 1);
+    s.abort = 0;
+    s.zero = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&s.tmem_base, 256);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync();  // every CTA's barriers are initialised, TMEM is allocated
+  tc_fence_after();
+  pdl_wait();  // every thread: the previous kernel's outputs are visible
+  const uint32_t tmem_base = s.tmem_base;
+  volatile int* abort = &s.abort;
+  const int tile = static_cast<int>(blockIdx.x) / (2 * a.pairs);
+  const int n0 = tile / a.row_tiles * 256 + h * 128, m0 = tile % a.row_tiles * a.rows;
+  const int half = a.rows / 2;
+  const int kb0 = static_cast<int>(static_cast<long long>(a.kblocks) * pair / a.pairs);
+  const int kb1 = static_cast<int>(static_cast<long long>(a.kblocks) * (pair + 1) / a.pairs);
+  uint32_t issued_mask = 0, last_phase_bits = 0;
+  bool mma_issued = false, leader = false;
+
+  if (warp == 0) {
+    const bool issuer = elect_one();
+    const uint32_t bytes = 2u * static_cast<uint32_t>(W_BYTES + half * BK * 2);
+    int slot = 0;
+    uint32_t phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&s.empty[slot], phase ^ 1u, a.limit_ns, abort))) {
+        if (issuer && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 61);
+        *abort = 1;
+        break;
+      }
+      if (issuer) {
+        uint8_t* p = ring + slot * P_STAGE_BYTES;
+        if (even) mbar_arrive_expect_tx(&s.full[slot], bytes);
+        const uint32_t full = pair_barrier(&s.full[slot], lead);
+        tma_load_2d_pair(p, &mapW, full, kb * BK, n0);
+        tma_load_2d_pair(p + W_BYTES, &mapX, full, kb * BK, m0 + h * half);
+      }
+      issued_mask |= 1u << slot;
+      last_phase_bits = (last_phase_bits & ~(1u << slot)) | (phase << slot);
+      if (++slot == Q_STAGES) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    }
+  } else if (warp == 1) {
+    if (even) {
+      leader = elect_one();
+      const uint64_t desc0 = sdesc_kmajor_sw128(smem_u32(ring));
+      const uint32_t idesc = idesc_bf16_f32(256, a.rows);
+      const uint16_t both = static_cast<uint16_t>(0x3u << lead);
+      int slot = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&s.full[slot], phase, a.limit_ns, abort))) {
+          if (leader && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 62);
+          *abort = 1;
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint64_t dw = desc0 + static_cast<uint64_t>((slot * P_STAGE_BYTES) >> 4), dx = dw + (W_BYTES >> 4);
+        if (leader) {
+#pragma unroll
+          for (int kk = 0; kk < BK / 16; ++kk)  // 16 elements = 32 bytes on
+            mma_bf16_pair(tmem_base, dw + 2 * kk, dx + 2 * kk, idesc, kb != kb0 || kk != 0 ? 1u : 0u);
+          mma_commit_pair(&s.empty[slot], both);
+        }
+        mma_issued = true;
+        if (++slot == Q_STAGES) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
+      if (ok && leader) mma_commit_pair(&s.tfull, both);
+      __syncwarp();
+    }
+  } else {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull, 0, a.limit_ns, abort));
+    if (!ok) {
+      if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 63);
+      *abort = 1;
+    } else {
+      tc_fence_after();  // the pair's copies and MMAs are done: the ring's memory takes the sums
+      const int q = warp & 3;
+#pragma unroll 1
+      for (int c = 0; c < a.rows; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sums[(c + i) * 128 + q * 32 + lane] = __uint_as_float(v[i]);
+      }
+      tc_fence_before();
+    }
+  }
+  __syncthreads();
+  if (s.abort) {
+    volatile int* never = &s.zero;
+    if (warp == 0 && lane == 0 && even)
+      for (int i = 0; i < Q_STAGES; ++i)
+        if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
+    if (leader && mma_issued) {
+      mma_commit_pair(&s.drain, static_cast<uint16_t>(0x1u << lead));
+      mbar_wait(&s.drain, 0, a.limit_ns, never);
+    }
+    __syncthreads();
+  }
+  cluster_sync();  // every CTA's sums are there
+  {
+    const int r0 = a.rows * pair / a.pairs, r1 = a.rows * (pair + 1) / a.pairs;
+    const int n = n0 + lane * 4, end = min(r1, a.e.M - m0);
+    const bool mine = n < a.e.N && !*abort;
+    float b[4];
+    load_bias4(b, a.e, n);
+#pragma unroll 1
+    for (int r = r0 + warp; r < end; r += S_THREADS / 32) {
+      float4 res = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (mine) res = load_residual4(a.e, m0 + r, n);
+      float4 u[Q_MAX_PAIRS];
+#pragma unroll
+      for (int j = 0; j < Q_MAX_PAIRS; ++j)
+        if (j < a.pairs) u[j] = load_rank(sums + r * 128 + lane * 4, 2 * j + h);
+      float4 v = u[0];
+#pragma unroll
+      for (int j = 1; j < Q_MAX_PAIRS; ++j)
+        if (j < a.pairs) {
+          v.x += u[j].x;
+          v.y += u[j].y;
+          v.z += u[j].z;
+          v.w += u[j].w;
+        }
+      if (mine) finish4(a.e, m0 + r, n, v, b, res);
+    }
+  }
+  tc_fence_before();
+  cluster_sync();  // no CTA leaves while another reads its sums
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem_base, 256);
+}
+
 }  // namespace ln
 
 // The pair kernel takes products of at least kLinearPairRows rows and kLinearPairTiles tiles of
@@ -657,12 +853,21 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 // 4096 x 4096 (16) 18.3 / 12.6; 128 rows 32.6 / 36.5, 28.4 / 30.5, 21.0 / 15.4; 512 rows,
 // 4096 x 4096 (32) 28.9 / 23.8, 768 (48) 29.3 / 36.7.
 constexpr int kLinearPairRows = 64, kLinearPairTiles = 48;
+// Pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks. Against the split kernel (us, K x
+// N): 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 35.1 / 34.8, 384 rows 38.6 / 52.7, 512 rows 45.5 /
+// 55.1; 384 rows, 4096 x 4096 19.5 / 22.5, 2048 x 2048 11.1 / 12.6.
+constexpr int kPairSplitRows = 257, kPairSplitBlocks = 32;
 
 template <bool F32>
 static cudaError_t linear_attr() {
   const cudaError_t e = cudaFuncSetAttribute(ln::linear_split_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              227 * 1024 - static_cast<int>(sizeof(ln::SplitSmem)) - 256);
   if (e != cudaSuccess) return e;
+  if (!F32) {
+    const cudaError_t q = cudaFuncSetAttribute(ln::linear_pair_split_kernel,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, ln::Q_SMEM);
+    if (q != cudaSuccess) return q;
+  }
   return cudaFuncSetAttribute(ln::linear_pair_kernel<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, ln::P_SMEM);
 }
 
@@ -698,6 +903,26 @@ static int linear_resident_pairs() {
   });
 }
 
+// Clusters of `pairs` (2 or 4) pairs that can be resident at once: a cluster stays within a GPC.
+static int linear_resident_clusters(int pairs) {
+  static PerDevice cache[2];
+  return per_device(cache[pairs / 4], [pairs] {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cluster_config(cfg, attr, 2 * pairs, nullptr);
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(num_sms() / (2 * pairs) * (2 * pairs), 1, 1);
+    cfg.blockDim = dim3(ln::S_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = ln::Q_SMEM;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_split_kernel, &cfg) != cudaSuccess || n < 0) {
+      cudaGetLastError();
+      n = 0;
+    }
+    return n;
+  });
+}
+
 static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, int M, int N, int K,
                          const ln::Epilogue& e, cudaStream_t stream) {
   using namespace ln;
@@ -713,6 +938,7 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   int rc;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
+  const int sms_now = num_sms();
   // pairs: even row tiles of at most 256 rows
   const long long p_tiles = div_up(M, 256) * div_up(N, 256);
   if (M >= kLinearPairRows && p_tiles >= kLinearPairTiles) {
@@ -739,6 +965,31 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     OM_LAUNCHED("linear_pair_kernel");
     return ORDERMOE_OK;
   }
+  // pairs that share K: as many tiles as all clusters take at once, on most of the pairs
+  if (!e.f32 && M >= kPairSplitRows && kblocks >= kPairSplitBlocks)
+    for (int pairs = 2; pairs <= Q_MAX_PAIRS; pairs *= 2) {
+      const long long ct = div_up(N, 256), cap = linear_resident_clusters(pairs);
+      long long rt = cap / ct;  // row tiles of at most 256 rows and at least 64
+      if (rt > div_up(M, 64)) rt = div_up(M, 64);
+      if (rt < div_up(M, 256) || rt * ct * pairs * 4 < 3ll * (sms_now / 2)) continue;
+      PairSplitArgs a{};
+      a.e = e;
+      a.rows = static_cast<int>(div_up(div_up(M, rt), 32) * 32);
+      a.row_tiles = static_cast<int>(div_up(M, a.rows));
+      a.kblocks = kblocks;
+      a.pairs = pairs;
+      a.limit_ns = wait_limit_ns();
+      if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
+      if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
+      cluster_config(cfg, attr, 2 * pairs, stream);
+      cfg.gridDim = dim3(static_cast<unsigned>(a.row_tiles * ct * 2 * pairs), 1, 1);
+      cfg.blockDim = dim3(S_THREADS, 1, 1);
+      cfg.dynamicSmemBytes = Q_SMEM;
+      const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
+      if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
+      OM_LAUNCHED("linear_pair_split_kernel");
+      return ORDERMOE_OK;
+    }
   SplitArgs a{};
   a.e = e;
   a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_ROWS : 128));
@@ -753,7 +1004,7 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
   // 14336 x 4096: 51.9, 29.7, 24.0, 23.4). Sums of 96 rows and more are exchanged between four at
   // most (128 rows, 4096 x 4096: four 13.9, eight 15.4).
-  const int sms = num_sms(), most_split = a.rows >= 96 ? 4 : S_MAX_SPLIT;
+  const int sms = sms_now, most_split = a.rows >= 96 ? 4 : S_MAX_SPLIT;
   a.split = 1;
   while (a.split * 2 <= most_split && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
   a.cols = 128;

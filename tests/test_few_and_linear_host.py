@@ -166,6 +166,8 @@ def test_cluster_barriers_around_the_accesses_to_a_peer():
     and no CTA leaves before another barrier."""
     for path, name, helper in (("linear.cu", "linear_split_kernel", "load_rank("),
                                ("linear.cu", "linear_pair_kernel", "lead_barrier("),
+                               ("linear.cu", "linear_pair_split_kernel", "pair_barrier("),
+                               ("linear.cu", "linear_pair_split_kernel", "load_rank("),
                                ("few_tokens.cu", "few_tokens_kernel", "store_both(")):
         body = kernel(path, name)
         assert "mapa_shared(" not in body

@@ -101,6 +101,24 @@ def test_pairs(M, N, K, f32):
     check(X, W, Y, bias=rows(1, N, 0.5, 5)[0].contiguous(), residual=rows(M, N, 1.0, 6, odd=True))
 
 
+# fewer tiles, many K blocks: two pairs share K, or four (the last two)
+PAIR_SPLIT = [(300, 4096, 2056), (512, 4000, 2048), (257, 8100, 2200), (333, 2999, 4096), (200, 8100, 2200),
+              (150, 1280, 2048), (300, 700, 2048), (290, 643, 3000)]
+
+
+@pytest.mark.parametrize("M,N,K", PAIR_SPLIT)
+def test_pairs_that_share_k(M, N, K):
+    X, W = rows(M, K, 1.0, 25), rows(N, K, 0.05, 26)
+    Y = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    check(X, W, Y)
+    check(X, W, Y, rows(1, N, 0.5, 27)[0].contiguous(), "gelu", rows(M, N, 1.0, 28, odd=True))
+    ref = Y.clone()
+    B.ordermoe_linear(X, W, Y, bias=rows(1, N, 0.5, 27)[0].contiguous(), act="gelu",
+                      residual=rows(M, N, 1.0, 28, odd=True))
+    assert torch.equal(Y, ref)
+    check(X, W, torch.empty(M, N, device=DEV))
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("M,N,K", [(5, 200, 96), (130, 515, 264), (2048, 2048, 128)])
 def test_epilogue(act, M, N, K):
