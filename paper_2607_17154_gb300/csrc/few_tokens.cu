@@ -72,7 +72,7 @@ struct Smem {
   uint8_t act[64];                 // their indices, ascending
   unsigned int mask[64];           // of an expert: the tokens that use it
   uint8_t slot[64][TOKENS];        // and the slot it is of each
-  float logits[2][TOKENS][68];     // shares of K of either CTA; [0] is -inf past E
+  float logits[2][TOKENS][68];     // shares of K of either CTA
   alignas(16) float ex[TOKENS][68];  // exponentials of the softmax, read 16 bytes at a time
   float delay[TOKENS][ORDERMOE_MAX_SERVERS];  // A[home][location] of the tokens
   int32_t target[TOKENS * ORDERMOE_MAX_TOPK];
@@ -86,6 +86,7 @@ struct Smem {
   int valid[TOKENS];               // decided: its outputs are written
   float sum[THREADS / 32];
 };
+static_assert(MAX_STAGES <= 32, "a lane a barrier");
 static_assert(offsetof(Smem, ex) % 16 == 0 && alignof(Smem) == 16, "16-byte loads");
 // A ring takes what the layer's tables leave of the 227 KB.
 template <int MT, int NT>
@@ -287,7 +288,7 @@ __device__ __forceinline__ void mma_warps_sync() {
 __device__ __forceinline__ void top_k(Smem& s, const Args& a, int t, int lane) {
   const float x0 = s.logits[0][t][lane] + s.logits[1][t][lane];
   const float x1 = s.logits[0][t][lane + 32] + s.logits[1][t][lane + 32];
-  const bool nan = __any_sync(0xffffffffu, x0 != x0 || x1 != x1);
+  const bool nan = __any_sync(0xffffffffu, (lane < a.E && x0 != x0) || (lane + 32 < a.E && x1 != x1));
   auto key = [](float x) {
     const unsigned int u = __float_as_uint(x + 0.0f);
     return u >> 31 ? ~u : u | 0x80000000u;
@@ -525,25 +526,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 
   if (warp == MMA_WARPS + PRODUCERS && lane < static_cast<int>(sizeof(Maps) / sizeof(CUtensorMap)))
     tma_prefetch_map(reinterpret_cast<const CUtensorMap*>(&maps) + lane);
-  if (tid == 0) {
-    for (int i = 0; i < STAGES; ++i) {
-      mbar_init(&s.full[i], 1);
-      mbar_init(&s.empty[i], 1);
+  if (warp == 0) {  // a barrier a lane
+    if (lane < STAGES) {
+      mbar_init(&s.full[lane], 1);
+      mbar_init(&s.empty[lane], 1);
     }
-    for (int i = 0; i < 3; ++i) {
-      mbar_init(&s.red_full[i], MMA_WARPS);
-      mbar_init(&s.red_empty[i], 1);
+    if (lane < 3) {
+      mbar_init(&s.red_full[lane], MMA_WARPS);
+      mbar_init(&s.red_empty[lane], 1);
     }
-    s.abort = 0;
-    s.zero = 0;
+    if (lane < 4) sm.kind[lane] = 0;
+    if (lane == 0) {
+      s.abort = 0;
+      s.zero = 0;
+    }
     fence_mbar_init();
   }
-  if (tid < 4) sm.kind[tid] = 0;
-  for (int i = tid; i < TOKENS * 68; i += THREADS) {
-    (&s.logits[0][0][0])[i] = -INFINITY;
-    (&s.logits[1][0][0])[i] = 0.0f;
-  }
-  for (int i = tid; i < 64; i += THREADS) s.mask[i] = 0;
+  if (warp == 1) s.mask[lane] = s.mask[lane + 32] = 0;
   cluster_sync();  // both CTAs run: the peer's shared memory may be written
 
   Ring ring_at(STAGES);          // producer and MMA warps
@@ -1117,6 +1116,9 @@ struct FewScratch {
 // SMs at most: the partial sums have a place for every CTA of a launch.
 constexpr int kFewMaxCtas = 256;
 
+// Units of two MMA tiles are taken where they fill at least this share of their rounds over the SMs.
+constexpr int kFewEvenPercent = 92;
+
 static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) {
   FewScratch s{};
   size_t off = 0;
@@ -1128,9 +1130,8 @@ static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) 
   const size_t R = (size_t)T * k, act = R < (size_t)E ? R : (size_t)E;
   s.sync = reinterpret_cast<unsigned int*>(take(16));
   s.H = reinterpret_cast<uint16_t*>(take(act * 2 * T * dff * 2));
-  // rows of 32 (T <= 4) or 64 columns: a row tile's partials, one for each CTA more
-  const size_t rows = T <= 4 ? 32 : 64;
-  s.part = reinterpret_cast<float*>(take((d / rows + kFewMaxCtas) * T * rows * 4));
+  // a row tile's partials, one for each CTA more (of 64 columns: of 32 they take less)
+  s.part = reinterpret_cast<float*>(take(((size_t)d / 64 + kFewMaxCtas) * T * 64 * 4));
   s.topk_w = reinterpret_cast<float*>(take(R * 4));
   s.topk_idx = reinterpret_cast<int32_t*>(take(R * 4));
   s.chosen = reinterpret_cast<int32_t*>(take(R * 4));
@@ -1188,12 +1189,15 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   return ORDERMOE_OK;
 }
 
-// Variants by the number of tokens: up to 4 take units of one MMA tile (more units, an even
-// share for every SM), more take two, so that a token's K block is loaded for twice
-// the weights; past 8 tokens a second column tile.
+// Variants: past 8 tokens a second column tile. Units of two MMA tiles, whose token rows are loaded for
+// twice the weights (TMA takes a row of 128 bytes in about 4 cycles, weights or tokens), unless
+// that leaves SMs without a unit at the end and up to 4 tokens: then units of one.
 static int few_dispatch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args& a, cudaStream_t stream) {
-  if (a.T <= 4) return few_launch<1, 1>(L, X, a, stream);
-  return a.T <= 8 ? few_launch<2, 1>(L, X, a, stream) : few_launch<2, 2>(L, X, a, stream);
+  if (a.T > 8) return few_launch<2, 2>(L, X, a, stream);
+  const int R = a.T * a.k, act = R < a.E ? R : a.E, sms = num_sms();
+  const long long units = (long long)act * (a.dff / 16), rounds = (units + sms - 1) / sms;
+  const bool even = units * 100 >= rounds * sms * kFewEvenPercent;
+  return a.T <= 4 && !even ? few_launch<1, 1>(L, X, a, stream) : few_launch<2, 1>(L, X, a, stream);
 }
 
 static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const uint16_t* X, const uint16_t* h,
@@ -1263,10 +1267,7 @@ extern "C" size_t ordermoe_layer_few_workspace_bytes(int T, int E, int d, int df
   if (T <= 0 || T > ORDERMOE_FEW_TOKENS || E <= 0 || E > ORDERMOE_MAX_EXPERTS || d <= 0 || dff <= 0 || k <= 0 ||
       k > ORDERMOE_MAX_TOPK || k > E)
     return 0;
-  // fewer tokens take less, but for rows of partials: the largest of both variants
-  const size_t n = few_carve(nullptr, T, E, d, dff, k).bytes;
-  const size_t four = few_carve(nullptr, T < 4 ? T : 4, E, d, dff, k).bytes;
-  return n > four ? n : four;
+  return few_carve(nullptr, T, E, d, dff, k).bytes;
 }
 
 extern "C" int ordermoe_layer_few_init(void* workspace, size_t workspace_bytes, ordermoe_stream_t stream) {
