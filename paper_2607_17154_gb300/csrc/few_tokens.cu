@@ -10,10 +10,10 @@
 // of HBM between them, so one cooperative kernel of a CTA per SM runs it all:
 //   route    every pair of CTAs computes all logits X W_r^T, half of K each, and both take
 //            the same decisions (the router is small; a grid barrier would take longer);
-//   gate/up  units of 8 MT columns of W1 and W3 of one expert over the whole K = d,
+//   gate/up  units of 16 columns of W1 and W3 of one expert over the whole K = d,
 //            dealt out to the CTAs in turn: gate in rows 0-7 of a 16-row MMA tile
 //            and up in rows 8-15, so that SwiGLU is in one lane's registers;
-//   down     row tiles of 32 MT rows of W2 by all chosen experts' K = d_ff, cut
+//   down     row tiles of 64 rows of W2 by all chosen experts' K = d_ff, cut
 //            into one contiguous share of equal length per CTA. A share's partial
 //            sums of a row tile go to the workspace;
 //   finish   one CTA a token adds the partials of every row tile in CTA order and
@@ -25,6 +25,9 @@
 // epilogue warp adds their eight partial accumulators. Between gate/up and down
 // the producers fill the ring with W2 while the other CTAs finish H: the grid
 // barrier there costs HBM no pause.
+// In a CUDA graph: 16 tokens on 8 experts of d 4096, d_ff 14336 420 us = 6.4 TB/s of weights (0.95 of a
+// copy's rate), 1 token 120 us (0.87); 1 token, top-6 of 64 experts of d 2048, d_ff 1408 38 us, of which the
+// weights take 15: the rest is the latency of what comes one after the other.
 #include <cstddef>
 #include <type_traits>
 
@@ -46,18 +49,24 @@ constexpr int MMA_WARPS = 8;
 constexpr int PRODUCERS = 2;  // the warps behind the MMA warps; the last is the epilogue's
 constexpr int THREADS = 32 * (MMA_WARPS + PRODUCERS + 1);
 constexpr int KB_UP = 4, KB_DOWN = 2;  // 64-element K blocks a stage
-// and in the router, whose stage holds rt tiles of 16 experts (8 MT KB of them, at most 4 blocks)
-__host__ __device__ constexpr int route_kb(int mt, int rt) { return 4 * mt / rt < 4 ? 4 * mt / rt : 4; }
 
-// MT: 16-row MMA tiles of a gate/up unit; NT: 8-token column tiles.
-template <int MT, int NT>
+// 16-row MMA tiles of a gate/up unit: with one, twice as many units share the SMs more evenly, but a
+// token's rows are loaded for half the weights (1 token on 64 narrow experts, 528 units on 152 SMs, 37.8 us
+// with two and 38.2 with one; 4 tokens 68.9 and 72.3; 4 on 8 wide experts 289 and 297).
+constexpr int MT = 2;
+// K blocks of a router stage, which holds rt tiles of 16 experts
+__host__ __device__ constexpr int route_kb(int rt) { return 4 * MT / rt < 4 ? 4 * MT / rt : 4; }
+
+// NT: 8-token column tiles.
+template <int NT>
 struct Cfg {
   static constexpr int W_BYTES = 8192 * MT;            // 16 MT rows x 256, or 32 MT x 128
   static constexpr int STAGE_BYTES = W_BYTES + 4096 * NT;  // and 8 NT tokens x 256
   static constexpr int DOWN_ROWS = 32 * MT;
   // partial accumulators of the MMA warps: two sets of a unit's, or one of a row tile's
   // (the router has up to four tiles, once)
-  static constexpr int RED_FLOATS = MMA_WARPS * (MT == 1 ? 4 : 2 * MT) * NT * 128;
+  static constexpr int RED_FLOATS = MMA_WARPS * 2 * MT * NT * 128;
+  static_assert(2 * MT >= 4, "tiles of 64 experts");
   // shared memory beside the ring: alignment, partials, the selection's Q and Cq
   static constexpr int other_bytes(int E) { return 1024 + RED_FLOATS * 4 + ((8 * E * E + 15) & ~15); }
 };
@@ -89,16 +98,16 @@ struct Smem {
 static_assert(MAX_STAGES <= 32, "a lane a barrier");
 static_assert(offsetof(Smem, ex) % 16 == 0 && alignof(Smem) == 16, "16-byte loads");
 // A ring takes what the layer's tables leave of the 227 KB.
-template <int MT, int NT>
+template <int NT>
 constexpr int stages(int E) {
-  const int left = 227 * 1024 - static_cast<int>(sizeof(Smem) + sizeof(SelSmem)) - 256 - Cfg<MT, NT>::other_bytes(E);
-  const int n = left / Cfg<MT, NT>::STAGE_BYTES;
+  const int left = 227 * 1024 - static_cast<int>(sizeof(Smem) + sizeof(SelSmem)) - 256 - Cfg<NT>::other_bytes(E);
+  const int n = left / Cfg<NT>::STAGE_BYTES;
   return n < MAX_STAGES ? n : MAX_STAGES;
 }
-static_assert(stages<1, 1>(64) >= 12 && stages<2, 1>(64) >= 6 && stages<2, 2>(64) >= 5, "ring");
-static_assert(MAX_D / 32 * 4 + MAX_D * 2 <= 5 * Cfg<2, 2>::STAGE_BYTES && Cfg<1, 1>::STAGE_BYTES * 12 >= 5 * Cfg<2, 2>::STAGE_BYTES &&
-                  Cfg<2, 1>::STAGE_BYTES * 6 >= 5 * Cfg<2, 2>::STAGE_BYTES, "finish");
-static_assert(TOKENS * ORDERMOE_MAX_TOPK * 64 * 12 <= 5 * Cfg<2, 2>::STAGE_BYTES, "candidates");
+static_assert(stages<1>(64) >= 6 && stages<2>(64) >= 5, "ring");
+static_assert(MAX_D / Cfg<1>::DOWN_ROWS * 4 + MAX_D * 2 <= 5 * Cfg<2>::STAGE_BYTES &&
+                  Cfg<1>::STAGE_BYTES * 6 >= 5 * Cfg<2>::STAGE_BYTES, "finish");
+static_assert(TOKENS * ORDERMOE_MAX_TOPK * 64 * 12 <= 5 * Cfg<2>::STAGE_BYTES, "candidates");
 
 struct Maps {
   CUtensorMap Wr, Xr, X, W1, W3, W2, H;
@@ -501,10 +510,10 @@ struct Walk {
   }
 };
 
-template <int MT, int NT>
+template <int NT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     few_tokens_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Args a) {
-  using C = Cfg<MT, NT>;
+  using C = Cfg<NT>;
   const int STAGES = a.stages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Smem s;
@@ -671,7 +680,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   auto route = [&](auto row_tiles) {
     // stages of all experts' rows (RT tiles of 16) by KB blocks of K, the first half of them in
     // rank 0
-    constexpr int RT = decltype(row_tiles)::value, KB = route_kb(MT, RT);
+    constexpr int RT = decltype(row_tiles)::value, KB = route_kb(RT);
     constexpr uint32_t W = RT * 2048 * KB;
     const int all = a.d / (64 * KB), half = (all + 1) / 2;
     const int s0 = rank == 0 ? 0 : half, s1 = rank == 0 ? half : all;
@@ -989,7 +998,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     const int first_tile = tiles * part / parts, last_tile = tiles * (part + 1) / parts;
     // the first and last owner of every row tile, while the others finish (the ring is free)
     int16_t* own = reinterpret_cast<int16_t*>(ring);
-    uint2* s_row = reinterpret_cast<uint2*>(ring + MAX_D / 32 * 4);  // the token's row of h_out
+    uint2* s_row = reinterpret_cast<uint2*>(ring + MAX_D / C::DOWN_ROWS * 4);  // the token's row of h_out
     if (share.total > 0)
       for (int i = first_tile + tid; i < last_tile; i += THREADS) {
         own[2 * i] = static_cast<int16_t>(share.owner(static_cast<long long>(i) * share.per_tile));
@@ -1116,9 +1125,6 @@ struct FewScratch {
 // SMs at most: the partial sums have a place for every CTA of a launch.
 constexpr int kFewMaxCtas = 256;
 
-// Units of two MMA tiles are taken where they fill at least this share of their rounds over the SMs.
-constexpr int kFewEvenPercent = 92;
-
 static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) {
   FewScratch s{};
   size_t off = 0;
@@ -1130,8 +1136,9 @@ static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) 
   const size_t R = (size_t)T * k, act = R < (size_t)E ? R : (size_t)E;
   s.sync = reinterpret_cast<unsigned int*>(take(16));
   s.H = reinterpret_cast<uint16_t*>(take(act * 2 * T * dff * 2));
-  // a row tile's partials, one for each CTA more (of 64 columns: of 32 they take less)
-  s.part = reinterpret_cast<float*>(take(((size_t)d / 64 + kFewMaxCtas) * T * 64 * 4));
+  // a row tile's partials, one for each CTA more
+  constexpr int rows = fw::Cfg<1>::DOWN_ROWS;
+  s.part = reinterpret_cast<float*>(take(((size_t)d / rows + kFewMaxCtas) * T * rows * 4));
   s.topk_w = reinterpret_cast<float*>(take(R * 4));
   s.topk_idx = reinterpret_cast<int32_t*>(take(R * 4));
   s.chosen = reinterpret_cast<int32_t*>(take(R * 4));
@@ -1141,35 +1148,35 @@ static FewScratch few_carve(uint8_t* base, int T, int E, int d, int dff, int k) 
   return s;
 }
 
-template <int MT, int NT>
+template <int NT>
 static cudaError_t few_attr() {
-  return cudaFuncSetAttribute(fw::few_tokens_kernel<MT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(fw::few_tokens_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               227 * 1024 - static_cast<int>(sizeof(fw::Smem) + sizeof(SelSmem)) - 256);
 }
 
-template <int MT, int NT>
+template <int NT>
 static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args& a, cudaStream_t stream) {
-  using C = fw::Cfg<MT, NT>;
+  using C = fw::Cfg<NT>;
   static PerDevice cache;
   const cudaError_t ae = static_cast<cudaError_t>(per_device(cache, [] {
-    return static_cast<int>(few_attr<MT, NT>());
+    return static_cast<int>(few_attr<NT>());
   }));
   if (ae != cudaSuccess) return cuda_fail(ae, "cudaFuncSetAttribute(few_tokens_kernel)");
   const int R = a.T * a.k, act = R < a.E ? R : a.E;
   fw::Maps m;
   int rc;
-  const int rt = a.E <= 16 ? 1 : a.E <= 32 ? 2 : 4, kb = fw::route_kb(MT, rt);  // as the kernel's route
+  const int rt = a.E <= 16 ? 1 : a.E <= 32 ? 2 : 4, kb = fw::route_kb(rt);  // as the kernel's route
   if ((rc = make_tmap_bf16_kb(&m.Wr, L->W_r, a.E, a.d, 16 * rt, kb))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.Xr, X, a.T, a.d, a.T, kb))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.X, X, a.T, a.d, a.T, fw::KB_UP))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.W1, L->W1, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
-  if ((rc = make_tmap_bf16_kb(&m.W3, L->W3, (uint64_t)a.E * a.dff, a.d, 8 * MT, fw::KB_UP))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.W1, L->W1, (uint64_t)a.E * a.dff, a.d, 8 * fw::MT, fw::KB_UP))) return rc;
+  if ((rc = make_tmap_bf16_kb(&m.W3, L->W3, (uint64_t)a.E * a.dff, a.d, 8 * fw::MT, fw::KB_UP))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.W2, L->W2, (uint64_t)a.E * a.d, a.dff, C::DOWN_ROWS, fw::KB_DOWN))) return rc;
   if ((rc = make_tmap_bf16_kb(&m.H, a.H, (uint64_t)act * 2 * a.T, a.dff, 2 * a.T, fw::KB_DOWN))) return rc;
-  a.stages = fw::stages<MT, NT>(a.E);
+  a.stages = fw::stages<NT>(a.E);
   // a CTA per SM, fewer where there are not as many units of gate/up
   int grid = num_sms() < kFewMaxCtas ? num_sms() : kFewMaxCtas;
-  const long long units = (long long)act * (a.dff / (8 * MT));
+  const long long units = (long long)act * (a.dff / (8 * fw::MT));
   if (units < grid) grid = static_cast<int>(units);
   grid = (grid < a.T ? a.T : grid) / 2 * 2;  // pairs
   if (grid < 2) grid = 2;
@@ -1183,21 +1190,10 @@ static int few_launch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args&
   attr[0].val.cooperative = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, fw::few_tokens_kernel<MT, NT>, m, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, fw::few_tokens_kernel<NT>, m, a);
   if (e != cudaSuccess) return cuda_fail(e, "few_tokens_kernel");
   OM_LAUNCHED("few_tokens_kernel");
   return ORDERMOE_OK;
-}
-
-// Variants: past 8 tokens a second column tile. Units of two MMA tiles, whose token rows are loaded for
-// twice the weights (TMA takes a row of 128 bytes in about 4 cycles, weights or tokens), unless
-// that leaves SMs without a unit at the end and up to 4 tokens: then units of one.
-static int few_dispatch(const ordermoe_layer_desc* L, const uint16_t* X, fw::Args& a, cudaStream_t stream) {
-  if (a.T > 8) return few_launch<2, 2>(L, X, a, stream);
-  const int R = a.T * a.k, act = R < a.E ? R : a.E, sms = num_sms();
-  const long long units = (long long)act * (a.dff / 16), rounds = (units + sms - 1) / sms;
-  const bool even = units * 100 >= rounds * sms * kFewEvenPercent;
-  return a.T <= 4 && !even ? few_launch<1, 1>(L, X, a, stream) : few_launch<2, 1>(L, X, a, stream);
 }
 
 static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const uint16_t* X, const uint16_t* h,
@@ -1256,7 +1252,7 @@ static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const
     if (rc) return rc;
     a.given = 1;
   }
-  return few_dispatch(L, X, a, stream);
+  return T <= 8 ? few_launch<1>(L, X, a, stream) : few_launch<2>(L, X, a, stream);
 }
 
 }  // namespace om
