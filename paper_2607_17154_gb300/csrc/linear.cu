@@ -10,7 +10,7 @@
 //     rows of its own share in rank order (the same bits at every call). For few rows, whose
 //     weights are one pass over HBM: the tile's width and S are chosen so that every SM
 //     streams the same share of them.
-//   linear_pair_kernel: persistent CTA pairs, tiles of 256 columns x up to 256 rows with
+//   linear_pair_kernel: persistent CTA pairs, tiles of up to 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
 //     main loop. For batches with a tile for most pairs, bound by the tensor cores.
 //   linear_pair_split_kernel: one tile of 256 columns x up to 256 rows a cluster of 2 or 4 CTA
@@ -408,6 +408,8 @@ static_assert(P_SMEM <= 227 * 1024, "shared memory of the pair kernel");
 struct PairArgs {
   Epilogue e;
   int rows;  // of a tile: a multiple of 32, at most 256
+  int cols;  // of a tile: a multiple of 16, at most 256. The MMA's rows past cols / 2 multiply what lies
+             // in shared memory and are not stored (a row of A reaches its own lane alone)
   int row_tiles, col_tiles, kblocks;
   uint64_t limit_ns;
 };
@@ -419,7 +421,7 @@ __device__ __forceinline__ void pair_tile(int tile, const PairArgs& a, int& m0, 
   const int in = min(P_GROUP_ROWS, a.row_tiles - g * P_GROUP_ROWS);
   const int ct = i / in;
   m0 = (g * P_GROUP_ROWS + i - ct * in) * a.rows;
-  n0 = ct * 256;
+  n0 = ct * a.cols;
 }
 
 // The even CTA's barrier, on which both CTAs' copies and arrivals count.
@@ -472,14 +474,14 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   volatile int* abort = &s.abort;
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
   const int total = a.row_tiles * a.col_tiles;
-  const int half = a.rows / 2;  // rows of X in a CTA's shared memory
+  const int half = a.rows / 2, cols = a.cols / 2;  // rows of X and of W in a CTA's shared memory
   const int part = F32 ? F32_BLOCKS : a.kblocks;  // K blocks of an accumulator, two in turn
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
 
   if (warp == 0) {
     const bool issuer = elect_one();
-    const uint32_t bytes = 2u * static_cast<uint32_t>(W_BYTES + half * BK * 2);
+    const uint32_t bytes = 2u * static_cast<uint32_t>((cols + half) * BK * 2);
     int slot = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -497,7 +499,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
           uint8_t* p = ring + slot * P_STAGE_BYTES;
           if (even) mbar_arrive_expect_tx(&s.full[slot], bytes);
           const uint32_t full = lead_barrier(&s.full[slot]);
-          tma_load_2d_pair(p, &mapW, full, kb * BK, n0 + rank * 128);
+          tma_load_2d_pair(p, &mapW, full, kb * BK, n0 + rank * cols);
           tma_load_2d_pair(p + W_BYTES, &mapX, full, kb * BK, m0 + rank * half);
         }
         issued_mask |= 1u << slot;
@@ -584,7 +586,8 @@ __global__ void __launch_bounds__(P_THREADS, 1)
     for (int tile = pair; tile < total && go; tile += pairs) {
       int m0, n0;
       pair_tile(tile, a, m0, n0);
-      const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * 128 + (et & 31) * 4;
+      const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * cols + (et & 31) * 4;
+      const bool mine = (et & 31) * 4 < cols && n < a.e.N;
       const uint32_t tb = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
       float bias[4];
       load_bias4(bias, a.e, n);
@@ -593,7 +596,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 #pragma unroll
         for (int i = 0; i < 32; ++i) chunk[i * 128 + q * 32 + lane] = v(i);
         group_sync(group);
-        if (n < a.e.N)
+        if (mine)
 #pragma unroll 2
           for (int r = et >> 5; r < 32 && c + r < rows; r += 4)
             finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias,
@@ -947,14 +950,25 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_PAIR_ROWS : 256));
     a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 32) * 32);
     a.row_tiles = static_cast<int>(div_up(M, a.rows));
-    a.col_tiles = static_cast<int>(div_up(N, 256));
+    const int most = linear_resident_pairs();
+    a.cols = 256;
+    // One or two row tiles are bound by the weights' bytes: tiles as narrow as the same number of rounds
+    // allows, so that every pair loads the same share (32003 x 2048: 64 rows 29.2 -> 28.7 us, 128 32.9 -> 31.2,
+    // 256 39.9 -> 38.2, 512 57.9 -> 55.2; 14336 x 4096, 64 rows 26.5 -> 25.8). From three on, X's rows loaded
+    // once more a column tile cost more (4096 x 14336: 768 rows 70.3 -> 72.9, 1021 72.9 -> 75.8).
+    if (a.row_tiles <= 2) {
+      const long long rounds = div_up(a.row_tiles * div_up(N, 256), most);
+      const long long even = div_up(div_up((long long)N * a.row_tiles, rounds * most), 16) * 16;
+      if (even < 256 && a.row_tiles * div_up(N, even) <= rounds * most) a.cols = static_cast<int>(even);
+    }
+    a.col_tiles = static_cast<int>(div_up(N, a.cols));
     a.kblocks = kblocks;
     a.limit_ns = wait_limit_ns();
     if ((long long)a.row_tiles * a.col_tiles > INT32_MAX / 2)
       return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
-    if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
+    if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols / 2))) return rc;
     if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
-    const int most = linear_resident_pairs(), tiles = a.row_tiles * a.col_tiles;
+    const int tiles = a.row_tiles * a.col_tiles;
     cluster_config(cfg, attr, 2, stream);
     cfg.gridDim = dim3(2 * (tiles < most ? tiles : most), 1, 1);
     cfg.blockDim = dim3(P_THREADS, 1, 1);

@@ -101,6 +101,22 @@ def test_pairs(M, N, K, f32):
     check(X, W, Y, bias=rows(1, N, 0.5, 5)[0].contiguous(), residual=rows(M, N, 1.0, 6, odd=True))
 
 
+@pytest.mark.parametrize("M,N,K", [(64, 12289, 264), (101, 14000, 136), (128, 32003, 72), (256, 12050, 328),
+                                   (300, 12161, 200), (511, 24700, 64), (66, 19456, 64)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_pairs_of_narrow_column_tiles(M, N, K, f32):
+    """One or two row tiles: the column tiles as wide as the rounds ask for (the last size: 256)."""
+    X, W = rows(M, K, 1.0, 31), rows(N, K, 0.05, 32)
+    dt = torch.float32 if f32 else torch.bfloat16
+    check(X, W, rows(M, N, 1.0, 33, pad=5, odd=True, dt=dt), bias=rows(1, N, 0.5, 34)[0].contiguous(), act="silu")
+    W[:, :] = float("nan")  # no column reads another's weights
+    W[N // 2] = 0.5
+    Y = torch.empty(M, N, dtype=dt, device=DEV)
+    B.ordermoe_linear(X, W, Y)
+    assert torch.equal(torch.isnan(Y).all(0), torch.arange(N, device=DEV) != N // 2)
+    assert torch.isfinite(Y[:, N // 2]).all()
+
+
 # fewer tiles, many K blocks: two pairs share K, or four (the last two)
 PAIR_SPLIT = [(300, 4096, 2056), (512, 4000, 2048), (257, 8100, 2200), (333, 2999, 4096), (200, 8100, 2200),
               (150, 1280, 2048), (300, 700, 2048), (290, 643, 3000)]
