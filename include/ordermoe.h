@@ -388,7 +388,8 @@ int ordermoe_layer_forward_residual(const ordermoe_layer_desc* layer, int T, con
  * Weights that a token does not use do not reach its output, whatever they hold. A token
  * whose decisions fail (a NaN logit, a bad home or location) is reported as by
  * ordermoe_route_select; its rows of y, h_out and x_out, loc and qhat are left
- * unwritten, the other tokens are computed.
+ * unwritten (its chosen_expert is -1 with lookahead_H > 1), the other tokens are
+ * computed.
  * The launch is cooperative, one CTA per SM: it starts when that many fit beside what
  * runs, and can be captured into a graph.
  * Shapes: d % 256 == 0, d <= 32768, dff % 128 == 0, 1 <= k <= min(E, 8), E <= 64. */

@@ -1245,6 +1245,8 @@ static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const
   a.sync = s.sync; a.H = s.H; a.part = s.part;
   a.limit_ns = wait_limit_ns();
   if (L->lookahead_H > 1) {  // decided by the look-ahead's launches, the experts here
+    // (it leaves an undecided token's experts unwritten: none is what is read here then)
+    OM_CUDA(cudaMemsetAsync(a.chosen, 0xff, (size_t)T * a.k * 4, stream));
     const int rc = ordermoe_route_select_lookahead(X, L->W_r, nullptr, T, a.E, a.d, a.k, a.renorm, L->tables,
                                                    L->tables_stride, L->lookahead_H, L->P, home, loc, qhat,
                                                    o.logits, a.topk_idx, a.topk_w, a.chosen, a.server, a.kind,
