@@ -1068,12 +1068,17 @@ extern "C" int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W
     return fail(ORDERMOE_ERR_INVALID_ARG, "linear: a row stride is shorter than the row");
   if (ldx % 8 != 0 || ldw % 8 != 0 || ldx >= (1ll << 38) || ldw >= (1ll << 38))
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: ldx and ldw must be multiples of 8, below 2^38");
+  constexpr int most = INT32_MAX - 512;  // indices of a tile's end stay in 32 bits
+  if (M > most || N > most || K > most)
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: need M, N and K of at most %d", most);
   if (M == 0) return ORDERMOE_OK;
   if (!X || !W || !Y) return fail(ORDERMOE_ERR_INVALID_ARG, "linear: null pointer");
   if (!aligned16(X) || !aligned16(W)) return fail(ORDERMOE_ERR_INVALID_ARG, "linear: X and W must be 16-byte aligned");
   const uintptr_t y = reinterpret_cast<uintptr_t>(Y), r = reinterpret_cast<uintptr_t>(residual);
   if (y % (f32 ? 4 : 2) != 0 || r % 2 != 0 || reinterpret_cast<uintptr_t>(bias) % 2 != 0)
     return fail(ORDERMOE_ERR_INVALID_ARG, "linear: Y, residual or bias is not aligned to its type");
+  if (r == y && (f32 || (M > 1 && ldr != ldy)))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "linear: a Y that is the residual must have its type and stride");
   ln::Epilogue e{};
   e.M = M; e.N = N; e.bias = bias; e.residual = residual; e.Y = Y;
   e.ldr = ldr; e.ldy = ldy; e.act = act; e.f32 = f32 != 0;

@@ -105,6 +105,16 @@ def test_calls_that_linear_refuses(call, code):
     assert rc == code and msg.startswith("linear:"), (call, rc, msg)
 
 
+@pytest.mark.parametrize("call,code", [
+    (dict(residual=AT, ldr=32, f32=1), ARG),            # each row of floats covers two of the residual's
+    (dict(residual=AT, ldr=40), ARG),
+    (dict(M=2 ** 31 - 100), SHAPE), (dict(n=2 ** 31 - 300, ldy=2 ** 32), SHAPE),
+    (dict(K=2 ** 31 - 60, ldx=2 ** 32, ldw=2 ** 32), SHAPE)])
+def test_results_in_place_and_sizes_that_linear_refuses(call, code):
+    rc, msg = linear(**call)
+    assert rc == code and msg.startswith("linear:"), (call, rc, msg)
+
+
 def test_linear_of_no_rows():
     assert linear(M=0, X=N, W=N, Y=N)[0] == OK
 
