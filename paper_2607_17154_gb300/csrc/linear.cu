@@ -1006,8 +1006,17 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     }
   SplitArgs a{};
   a.e = e;
-  a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_ROWS : 128));
-  a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 16) * 16);
+  // Row tiles of 32 rows and more, as many as leave each tile four CTAs (or what K has for them) of two an
+  // SM: the sums that a CTA exchanges and finishes are fewer (tiles of up to 128 rows / these, us:
+  // 128 x 1024 x 2048 9.3 / 7.2, 128 x 2048 x 2048 9.3 / 7.7, 301 x 1009 x 1999 11.8 / 10.3, 64 x
+  // 4096 x 4096 12.4 / 11.8, 1000 x 512 x 512 9.3 / 6.7). Without the four it loses (33 x 5632 x 2048 in
+  // two row tiles 11.8 for 9.8).
+  int want = 1;
+  while (want < 4 && kblocks / (want * 2) >= 4) want *= 2;
+  long long rt = 2ll * sms_now / (div_up(N, 128) * want);
+  if (rt > div_up(M, 32)) rt = div_up(M, 32);
+  if (rt < div_up(M, e.f32 ? F32_ROWS : 128)) rt = div_up(M, e.f32 ? F32_ROWS : 128);
+  a.rows = static_cast<int>(div_up(div_up(M, rt), 16) * 16);
   a.row_tiles = static_cast<int>(div_up(M, a.rows));
   a.kblocks = kblocks;
   a.limit_ns = wait_limit_ns();
@@ -1016,11 +1025,10 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
   // K over as many CTAs as two an SM leave room for, four K blocks each at least: two rings hide each
   // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
-  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4). Sums of 96 rows and more are exchanged between four at
-  // most (128 rows, 4096 x 4096: four 13.9, eight 15.4).
-  const int sms = sms_now, most_split = a.rows >= 96 ? 4 : S_MAX_SPLIT;
+  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4)
+  const int sms = sms_now;
   a.split = 1;
-  while (a.split * 2 <= most_split && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
+  while (a.split * 2 <= S_MAX_SPLIT && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
   a.cols = 128;
   if (a.split <= 2 && tiles * a.split > sms && tiles * a.split <= 2ll * sms) {
     // narrower tiles where that gives every SM two CTAs (1 row, 4096 x 14336: 128 columns 23.7 us,
@@ -1030,10 +1038,11 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     if (a.row_tiles * div_up(N, a.cols) * a.split > 2ll * sms) a.cols = 128;
     tiles = a.row_tiles * div_up(N, a.cols);
   }
-  // one CTA an SM takes a ring of most of its shared memory, two half of it each; behind it what the
-  // MMA reads past the last stage's weights
+  // One CTA an SM takes a ring of most of its shared memory, two half of it each. So do clusters of eight,
+  // which do not fill the GPCs with one an SM (128 CTAs, 1 x 2048 x 8192: 17.1 us and 10.9; 64 rows 20.3 and
+  // 12.5; clusters of four 13.4 and 14.0). Behind the ring what the MMA reads past the last stage's weights.
   const int stage = (a.cols + a.rows) * BK * 2, over = W_BYTES > stage ? W_BYTES - stage : 0;
-  const int room = (tiles * a.split <= sms ? 220 * 1024 : 108 * 1024) - over;
+  const int room = (tiles * a.split <= sms && a.split < S_MAX_SPLIT ? 220 * 1024 : 108 * 1024) - over;
   const int share = (kblocks + a.split - 1) / a.split, need = (a.rows * 512 + stage - 1) / stage;
   a.stages = room / stage < S_MAX_STAGES ? room / stage : S_MAX_STAGES;
   if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
