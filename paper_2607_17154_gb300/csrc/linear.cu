@@ -145,6 +145,12 @@ __device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 
 constexpr int S_THREADS = 192;  // TMA warp, MMA warp, four epilogue warps; all of them reduce
 constexpr int S_MAX_STAGES = 12;
 constexpr int S_MAX_SPLIT = 8;
+// An allocation of TMEM that has to wait holds up a cluster, or a kernel whose dependents already wait for it,
+// and nothing bounds that wait. So none has to: a CTA takes 128 of the 512 columns at most, and shared memory
+// for at most four on an SM (228 KB, 1 KB of it reserved for each), which does not fit beside a CTA that
+// takes all columns (those, here and in the expert GEMMs, the logits and the similarity, hold 180 KB and more).
+constexpr int S_MIN_SMEM = 48 * 1024, S_MAX_COLS = 128;
+static_assert(5 * (S_MIN_SMEM + 1024) > 228 * 1024 && 4 * S_MAX_COLS <= 512, "TMEM of the CTAs of an SM");
 
 struct SplitSmem {
   uint64_t full[S_MAX_STAGES], empty[S_MAX_STAGES];
@@ -404,6 +410,7 @@ struct PairSmem {
 constexpr int P_SMEM =
     P_STAGES * P_STAGE_BYTES + P_GROUPS * P_CHUNK_FLOATS * 4 + 1024 + static_cast<int>(sizeof(PairSmem));
 static_assert(P_SMEM <= 227 * 1024, "shared memory of the pair kernel");
+static_assert(P_SMEM + S_MIN_SMEM > 226 * 1024, "no CTA of the split kernel beside its TMEM");
 
 struct PairArgs {
   Epilogue e;
@@ -659,6 +666,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
 // ------------------------------------------------------ CTA pairs, K over a cluster
 constexpr int Q_STAGES = 6;
 constexpr int Q_SMEM = Q_STAGES * P_STAGE_BYTES + 1024;
+static_assert(Q_SMEM + S_MIN_SMEM > 226 * 1024, "no CTA of the split kernel beside its TMEM");
 constexpr int Q_MAX_PAIRS = 4;
 
 struct PairSplitSmem {
@@ -1048,12 +1056,15 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
   a.x_rows = M < a.rows ? M : a.rows;
   if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols))) return rc;
-  a.tmem_cols = a.rows <= 32 ? 64 : a.rows <= 64 ? 128 : 256;  // two accumulators
+  const int acc = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
+  a.tmem_cols = e.f32 ? 2 * acc : acc;  // in turn, or the one of all K
+  static_assert(2 * F32_ROWS <= S_MAX_COLS, "two accumulators");
   if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.x_rows))) return rc;
   cluster_config(cfg, attr, a.split, stream);
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split), 1, 1);
   cfg.blockDim = dim3(S_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = a.stages * stage + over + 1024;
+  const int smem = a.stages * stage + over + 1024;
+  cfg.dynamicSmemBytes = smem < S_MIN_SMEM ? S_MIN_SMEM : smem;
   const cudaError_t ce = e.f32 ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, mW, mX, a)
                                : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, mW, mX, a);
   if (ce != cudaSuccess) return cuda_fail(ce, "linear_split_kernel");

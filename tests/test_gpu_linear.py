@@ -286,3 +286,24 @@ def test_stack_of_moe_and_dense_layers(T, few):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(u, v) for u, v in zip(eager, hs))
+
+
+def test_short_products_behind_long_ones_on_two_streams():
+    """Every kernel behind every other, launched eagerly, two streams side by side: TMEM of a CTA is free when it asks."""
+    sizes = [(1021, 4096, 512), (1, 256, 64), (300, 2048, 2048), (16, 256, 256), (4096, 128, 64), (128, 2048, 4096),
+             (1, 2048, 8192), (100, 12289, 128)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    sets = [[(rows(M, K, 1.0, 40 + i), rows(N, K, 0.05, 60 + i), torch.empty(M, N, dtype=dt, device=DEV))
+             for i, (M, N, K) in enumerate(sizes)] for dt in (torch.bfloat16, torch.float32)]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for i in range(len(sizes)):
+            for st, work in zip(streams, sets):
+                with torch.cuda.stream(st):
+                    B.ordermoe_linear(*work[(i * (turn % 7 + 1) + turn) % len(sizes)])
+    torch.cuda.synchronize()
+    for work in sets:
+        for X, W, Y in work:
+            first = Y.clone()
+            check(X, W, Y)
+            assert torch.equal(first, Y)
