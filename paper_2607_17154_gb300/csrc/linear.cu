@@ -24,6 +24,8 @@
 // runs out reports ORDERMOE_DEV_WAIT_TIMEOUT, and the copies and MMAs under way are drained.
 #include "common.cuh"
 
+#include <type_traits>
+
 namespace om {
 
 static __device__ unsigned long long g_err_linear = 0;
@@ -53,30 +55,37 @@ struct Epilogue {
   int vec_r, vec_y;          // 4 columns at a time: strides and addresses allow it
 };
 
-// Each activation in fp32 from the product's sum; NaN stays NaN. Not inlined: the epilogue of a few
-// rows runs once, its instructions come from L2, and five activations a column made it longer
-// (301 x 1009 with SiLU 16.5 us). A bf16 result takes the fast exponential and quotient (a few
-// 2^-23 off, 2^-9 of its rounding; 0 where the quotient is below 2^-119): 301 x 1009 with SiLU 12.9
-// -> 10.7 us.
-__device__ __noinline__ float4 activate4(float4 v, int act, int fast) {
+// An activation in fp32 of the product's sum; NaN stays NaN. A bf16 result takes the fast exponential and
+// quotient (a few 2^-23 off, 2^-9 of its rounding; 0 where the quotient is below 2^-119): 301 x 1009
+// with SiLU 12.9 -> 10.7 us.
+template <int ACT, bool FAST>
+__device__ __forceinline__ float activate(float v) {
+  if (ACT == ORDERMOE_ACT_RELU) return v < 0.0f ? 0.0f : v;
+  // v Phi(v); erfc keeps the digits of a negative v's tail, which 1 + erf loses
+  if (ACT == ORDERMOE_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);
+  // v sigmoid(s): s = v, or 2 sqrt(2/pi) (v + 0.044715 v^3), whose sigmoid is (1 + tanh) / 2 of half of it
+  const float u = ACT == ORDERMOE_ACT_SILU ? -v : -1.5957691216057308f * fmaf(0.044715f * v * v, v, v);
+  return FAST ? __fdividef(v, 1.0f + __expf(u)) : v / (1.0f + expf(u));
+}
+
+template <int N, bool FAST>
+__device__ __forceinline__ void activate_all(float (&f)[N], int act) {
+  auto all = [&](auto kind) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = activate<decltype(kind)::value, FAST>(f[j]);
+  };
+  if (act == ORDERMOE_ACT_RELU) all(std::integral_constant<int, ORDERMOE_ACT_RELU>{});
+  else if (act == ORDERMOE_ACT_GELU) all(std::integral_constant<int, ORDERMOE_ACT_GELU>{});
+  else if (act == ORDERMOE_ACT_GELU_TANH) all(std::integral_constant<int, ORDERMOE_ACT_GELU_TANH>{});
+  else if (act == ORDERMOE_ACT_SILU) all(std::integral_constant<int, ORDERMOE_ACT_SILU>{});
+}
+
+// Not inlined: the epilogue of a few rows runs once, its instructions come from L2, and five activations a
+// column made it longer (301 x 1009 with SiLU 16.5 us).
+template <bool FAST>
+__device__ __noinline__ float4 activate4(float4 v, int act) {
   float f[4] = {v.x, v.y, v.z, v.w};
-  if (act == ORDERMOE_ACT_RELU) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = f[j] < 0.0f ? 0.0f : f[j];
-  } else if (act == ORDERMOE_ACT_GELU) {
-    // v Phi(v); erfc keeps the digits of a negative v's tail, which 1 + erf loses
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = 0.5f * f[j] * erfcf(-0.70710678118654752f * f[j]);
-  } else {
-    // v sigmoid(s): s = v, or 2 sqrt(2/pi) (v + 0.044715 v^3), whose sigmoid is (1 + tanh) / 2 of half of it
-    const bool silu = act == ORDERMOE_ACT_SILU;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float g = 1.5957691216057308f * fmaf(0.044715f * f[j] * f[j], f[j], f[j]);
-      const float u = silu ? -f[j] : -g;
-      f[j] = fast ? __fdividef(f[j], 1.0f + __expf(u)) : f[j] / (1.0f + expf(u));
-    }
-  }
+  activate_all<4, FAST>(f, act);
   return make_float4(f[0], f[1], f[2], f[3]);
 }
 
@@ -106,10 +115,15 @@ __device__ __forceinline__ float4 load_residual4(const Epilogue& e, int m, int n
   return make_float4(f[0], f[1], f[2], f[3]);
 }
 
+// The line of the residual's row m that holds column n, into L2 while the sums are made.
+__device__ __forceinline__ void prefetch_residual(const Epilogue& e, int m, int n) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(e.residual + m * e.ldr + n));
+}
+
 // Columns n .. n + 3 of row m from their sums v and their residual r.
 __device__ __forceinline__ void finish4(const Epilogue& e, int m, int n, float4 v, const float (&b)[4], float4 r) {
   v = make_float4(v.x + b[0], v.y + b[1], v.z + b[2], v.w + b[3]);
-  if (e.act != ORDERMOE_ACT_NONE) v = activate4(v, e.act, !e.f32);
+  if (e.act != ORDERMOE_ACT_NONE) v = e.f32 ? activate4<false>(v, e.act) : activate4<true>(v, e.act);
   float f[4] = {v.x, v.y, v.z, v.w};
   if (e.residual != nullptr) {  // (without one -0 stays -0)
     f[0] += r.x;
@@ -228,6 +242,7 @@ __global__ void __launch_bounds__(S_THREADS, 2)
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
   const int part = F32 ? F32_BLOCKS : kb1 - kb0;  // K blocks of an accumulator, two in turn
+  const int r0 = a.rows * rank / a.split, r1 = a.rows * (rank + 1) / a.split;  // rows that this CTA finishes
 
   if (warp == 0) {
     const bool issuer = elect_one();
@@ -296,6 +311,8 @@ __global__ void __launch_bounds__(S_THREADS, 2)
     }
   } else {
     const int q = warp & 3;
+    if (a.e.residual != nullptr && lane * 4 < a.cols && n0 + lane * 4 < a.e.N)  // what this CTA finishes
+      for (int r = r0 + q; r < min(r1, a.e.M - m0); r += 4) prefetch_residual(a.e, m0 + r, n0 + lane * 4);
     const uint32_t tb = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
     float acc[F32 ? F32_ROWS / 32 : 1][32];
     bool ok = true;
@@ -360,7 +377,6 @@ __global__ void __launch_bounds__(S_THREADS, 2)
   }
   cluster_sync();  // every CTA's sums are there
   {
-    const int r0 = a.rows * rank / a.split, r1 = a.rows * (rank + 1) / a.split;
     const int n = n0 + lane * 4;
     float b[4];
     load_bias4(b, a.e, n);
@@ -396,9 +412,8 @@ __global__ void __launch_bounds__(S_THREADS, 2)
 // ---------------------------------------------------------------- CTA pairs
 constexpr int P_STAGES = 6;
 constexpr int P_STAGE_BYTES = 2 * W_BYTES;  // 128 weight rows and up to 128 rows of X a CTA
-constexpr int P_GROUPS = 2;                 // of four epilogue warps, alternate chunks of 32 rows
+constexpr int P_GROUPS = 4;                 // of four epilogue warps, eight rows of a tile in turn
 constexpr int P_THREADS = 64 + 128 * P_GROUPS;
-constexpr int P_CHUNK_FLOATS = 32 * 128;
 constexpr int P_GROUP_ROWS = 16;            // row tiles that share a pass over the weights
 
 struct PairSmem {
@@ -407,8 +422,7 @@ struct PairSmem {
   uint32_t tmem_base;
   int abort, zero;
 };
-constexpr int P_SMEM =
-    P_STAGES * P_STAGE_BYTES + P_GROUPS * P_CHUNK_FLOATS * 4 + 1024 + static_cast<int>(sizeof(PairSmem));
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + 1024 + static_cast<int>(sizeof(PairSmem));
 static_assert(P_SMEM <= 227 * 1024, "shared memory of the pair kernel");
 static_assert(P_SMEM + S_MIN_SMEM > 226 * 1024, "no CTA of the split kernel beside its TMEM");
 
@@ -434,8 +448,12 @@ __device__ __forceinline__ void pair_tile(int tile, const PairArgs& a, int& m0, 
 // The even CTA's barrier, on which both CTAs' copies and arrivals count.
 __device__ __forceinline__ uint32_t lead_barrier(uint64_t* bar) { return mapa_shared(smem_u32(bar), 0); }
 
-__device__ __forceinline__ void group_sync(int group) {
-  asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+// Eight columns of this warp's lanes.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
 }
 
 template <bool F32>
@@ -445,8 +463,7 @@ __global__ void __launch_bounds__(P_THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  float* chunks = reinterpret_cast<float*>(ring + P_STAGES * P_STAGE_BYTES);
-  PairSmem& s = *reinterpret_cast<PairSmem*>(chunks + P_GROUPS * P_CHUNK_FLOATS);
+  PairSmem& s = *reinterpret_cast<PairSmem*>(ring + P_STAGES * P_STAGE_BYTES);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = static_cast<int>(cluster_ctarank() & 1u);
   const bool even = rank == 0;
@@ -562,27 +579,19 @@ __global__ void __launch_bounds__(P_THREADS, 1)
         }
     }
   } else {
-    const int q = warp & 3, group = (warp - 2) >> 2, et = tid - 64 - 128 * group;
-    float* chunk = chunks + group * P_CHUNK_FLOATS;
+    // A thread's column of eight rows at a time, straight from TMEM: a warp writes 64 bytes of a row (128 in
+    // fp32), whatever the strides.
+    const int q = warp & 3, group = (warp - 2) >> 2, column = q * 32 + lane;
     int it = 0;
     bool go = true;
-    // this unit's accumulator is there: agreed on behind a barrier, so that a group that gives up
-    // leaves together
-    auto arrived = [&]() {
-      const bool waited = mbar_wait(&s.tfull[it & 1], (it >> 1) & 1, a.limit_ns, abort);
-      if (!waited && !*abort) {
-        report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 54);
+    auto arrived = [&]() {  // this unit's accumulator is there
+      const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull[it & 1], (it >> 1) & 1, a.limit_ns, abort));
+      if (!ok) {
+        if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 54);
         *abort = 1;
       }
-      uint32_t all;
-      asm volatile(
-          "{\n\t.reg .pred p, r;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-          "bar.red.and.pred r, %2, 128, p;\n\tselp.u32 %0, 1, 0, r;\n\t}"
-          : "=r"(all)
-          : "r"(static_cast<uint32_t>(waited)), "r"(1 + group)
-          : "memory");
       tc_fence_after();
-      return all != 0;
+      return ok;
     };
     auto taken = [&]() {  // its columns may be written again
       tc_fence_before();
@@ -593,53 +602,95 @@ __global__ void __launch_bounds__(P_THREADS, 1)
     for (int tile = pair; tile < total && go; tile += pairs) {
       int m0, n0;
       pair_tile(tile, a, m0, n0);
-      const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * cols + (et & 31) * 4;
-      const bool mine = (et & 31) * 4 < cols && n < a.e.N;
+      const int rows = min(a.rows, a.e.M - m0), n = n0 + rank * cols + column;
+      const bool mine = column < cols && n < a.e.N;
       const uint32_t tb = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
-      float bias[4];
-      load_bias4(bias, a.e, n);
-      auto store = [&](const auto& v, int c) {  // rows c .. c + 31 of the tile
-        group_sync(group);  // the chunk before has been read
+      const float bias = mine && a.e.bias != nullptr ? bf16_lo(a.e.bias[n]) : 0.0f;
+      const bool add = mine && a.e.residual != nullptr;
+      uint32_t res[8], next[8];
+      auto load_next = [&](int r) {  // the residual of rows r .. r + 7
+        if (!add) return;
+        const uint16_t* p = a.e.residual + (m0 + r) * a.e.ldr + n;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) chunk[i * 128 + q * 32 + lane] = v(i);
-        group_sync(group);
-        if (mine)
-#pragma unroll 2
-          for (int r = et >> 5; r < 32 && c + r < rows; r += 4)
-            finish4(a.e, m0 + c + r, n, *reinterpret_cast<const float4*>(chunk + r * 128 + (et & 31) * 4), bias,
-                    load_residual4(a.e, m0 + c + r, n));
+        for (int i = 0; i < 8; ++i, p += a.e.ldr)
+          if (r + i < rows) next[i] = *p;
       };
+      auto finish = [&](float (&v)[8], int r) {
+        if (!mine) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += bias;
+        activate_all<8, !F32>(v, a.e.act);
+        if (add) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += bf16_lo(res[i]);
+        }
+        if constexpr (F32) {
+          float* y = static_cast<float*>(a.e.Y) + (m0 + r) * a.e.ldy + n;
+#pragma unroll
+          for (int i = 0; i < 8; ++i, y += a.e.ldy)
+            if (r + i < rows) *y = v[i];
+        } else {
+          uint16_t* y = static_cast<uint16_t*>(a.e.Y) + (m0 + r) * a.e.ldy + n;
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const uint32_t o = pack_bf16x2(v[i], v[i + 1]);
+            if (r + i < rows) *y = static_cast<uint16_t>(o);
+            y += a.e.ldy;
+            if (r + i + 1 < rows) *y = static_cast<uint16_t>(o >> 16);
+            y += a.e.ldy;
+          }
+        }
+      };
+      // (the first rows' residual while the sums are made, the others' one step ahead)
+      load_next(group * 8);
       if constexpr (F32) {
-        constexpr int CHUNKS = F32_PAIR_ROWS / 32 / P_GROUPS;
-        float acc[CHUNKS][32];
+        constexpr int BLOCKS = F32_PAIR_ROWS / 8 / P_GROUPS;
+        float acc[BLOCKS][8];
         for (int first = 0; first < a.kblocks; first += part) {
           if (!(go = arrived())) break;
 #pragma unroll
-          for (int j = 0; j < CHUNKS; ++j) {
-            const int c = (group + j * P_GROUPS) * 32;
-            if (c >= rows) continue;
-            uint32_t v[32];
-            tmem_ld32(tb + (it & 1) * 256 + c, v);
+          for (int j = 0; j < BLOCKS; ++j) {
+            const int r = (group + j * P_GROUPS) * 8;
+            if (r >= rows) continue;
+            uint32_t v[8];
+            tmem_ld8(tb + (it & 1) * 256 + r, v);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < 8; ++i)
               acc[j][i] = first == 0 ? __uint_as_float(v[i]) : acc[j][i] + __uint_as_float(v[i]);
           }
           taken();
         }
         if (!go) break;
+#pragma unroll 1
+        for (int j = 0; j < BLOCKS; ++j) {
+          const int r = (group + j * P_GROUPS) * 8;
+          if (r >= rows) break;
+          float v[8];
 #pragma unroll
-        for (int j = 0; j < CHUNKS; ++j)
-          if ((group + j * P_GROUPS) * 32 < rows)
-            store([&](int i) { return acc[j][i]; }, (group + j * P_GROUPS) * 32);
+          for (int i = 0; i < 8; ++i) {
+            v[i] = acc[0][i];
+            res[i] = next[i];
+#pragma unroll
+            for (int b = 1; b < BLOCKS; ++b) v[i] = j == b ? acc[b][i] : v[i];
+          }
+          load_next(r + 8 * P_GROUPS);
+          finish(v, r);
+        }
       } else {
         if (!(go = arrived())) break;
 #pragma unroll 1
-        for (int c = group * 32; c < rows; c += 32 * P_GROUPS) {
-          uint32_t v[32];
-          tmem_ld32(tb + (it & 1) * 256 + c, v);  // TMEM column = row c + i of the tile
+        for (int r = group * 8; r < rows; r += 8 * P_GROUPS) {
+          uint32_t u[8];
+          tmem_ld8(tb + (it & 1) * 256 + r, u);  // TMEM column = row r + i of the tile
+#pragma unroll
+          for (int i = 0; i < 8; ++i) res[i] = next[i];
+          load_next(r + 8 * P_GROUPS);
           tmem_ld_wait();
-          store([&](int i) { return __uint_as_float(v[i]); }, c);
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+          finish(v, r);
         }
         taken();
       }
@@ -731,6 +782,7 @@ __global__ void __launch_bounds__(S_THREADS, 1)
   const int half = a.rows / 2;
   const int kb0 = static_cast<int>(static_cast<long long>(a.kblocks) * pair / a.pairs);
   const int kb1 = static_cast<int>(static_cast<long long>(a.kblocks) * (pair + 1) / a.pairs);
+  const int r0 = a.rows * pair / a.pairs, r1 = a.rows * (pair + 1) / a.pairs;  // rows that this CTA finishes
   uint32_t issued_mask = 0, last_phase_bits = 0;
   bool mma_issued = false, leader = false;
 
@@ -793,6 +845,8 @@ __global__ void __launch_bounds__(S_THREADS, 1)
       __syncwarp();
     }
   } else {
+    if (a.e.residual != nullptr && n0 + lane * 4 < a.e.N)
+      for (int r = r0 + (warp & 3); r < min(r1, a.e.M - m0); r += 4) prefetch_residual(a.e, m0 + r, n0 + lane * 4);
     const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull, 0, a.limit_ns, abort));
     if (!ok) {
       if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 63);
@@ -825,7 +879,6 @@ __global__ void __launch_bounds__(S_THREADS, 1)
   }
   cluster_sync();  // every CTA's sums are there
   {
-    const int r0 = a.rows * pair / a.pairs, r1 = a.rows * (pair + 1) / a.pairs;
     const int n = n0 + lane * 4, end = min(r1, a.e.M - m0);
     const bool mine = n < a.e.N && !*abort;
     float b[4];
