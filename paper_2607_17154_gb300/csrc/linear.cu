@@ -719,6 +719,8 @@ constexpr int Q_STAGES = 6;
 constexpr int Q_SMEM = Q_STAGES * P_STAGE_BYTES + 1024;
 static_assert(Q_SMEM + S_MIN_SMEM > 226 * 1024, "no CTA of the split kernel beside its TMEM");
 constexpr int Q_MAX_PAIRS = 4;
+constexpr int Q_GROUPS = 4;  // of four epilogue warps
+constexpr int Q_THREADS = 64 + 128 * Q_GROUPS;
 
 struct PairSplitSmem {
   uint64_t full[Q_STAGES], empty[Q_STAGES];
@@ -739,7 +741,7 @@ __device__ __forceinline__ uint32_t pair_barrier(uint64_t* bar, uint32_t lead) {
   return mapa_shared(smem_u32(bar), lead);
 }
 
-__global__ void __launch_bounds__(S_THREADS, 1)
+__global__ void __launch_bounds__(Q_THREADS, 1)
     linear_pair_split_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
                              const __grid_constant__ PairSplitArgs a) {
   extern __shared__ uint8_t smem_raw[];
@@ -846,7 +848,8 @@ __global__ void __launch_bounds__(S_THREADS, 1)
     }
   } else {
     if (a.e.residual != nullptr && n0 + lane * 4 < a.e.N)
-      for (int r = r0 + (warp & 3); r < min(r1, a.e.M - m0); r += 4) prefetch_residual(a.e, m0 + r, n0 + lane * 4);
+      for (int r = r0 + warp - 2; r < min(r1, a.e.M - m0); r += 4 * Q_GROUPS)
+        prefetch_residual(a.e, m0 + r, n0 + lane * 4);
     const bool ok = __all_sync(0xffffffffu, mbar_wait(&s.tfull, 0, a.limit_ns, abort));
     if (!ok) {
       if (lane == 0 && !*abort) report(&g_err_linear, ORDERMOE_DEV_WAIT_TIMEOUT, 63);
@@ -855,7 +858,7 @@ __global__ void __launch_bounds__(S_THREADS, 1)
       tc_fence_after();  // the pair's copies and MMAs are done: the ring's memory takes the sums
       const int q = warp & 3;
 #pragma unroll 1
-      for (int c = 0; c < a.rows; c += 32) {
+      for (int c = (warp - 2) / 4 * 32; c < a.rows; c += 32 * Q_GROUPS) {
         uint32_t v[32];
         tmem_ld32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + c, v);
         tmem_ld_wait();
@@ -884,7 +887,7 @@ __global__ void __launch_bounds__(S_THREADS, 1)
     float b[4];
     load_bias4(b, a.e, n);
 #pragma unroll 1
-    for (int r = r0 + warp; r < end; r += S_THREADS / 32) {
+    for (int r = r0 + warp; r < end; r += Q_THREADS / 32) {
       float4 res = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       if (mine) res = load_residual4(a.e, m0 + r, n);
       float4 u[Q_MAX_PAIRS];
@@ -976,7 +979,7 @@ static int linear_resident_clusters(int pairs) {
     cluster_config(cfg, attr, 2 * pairs, nullptr);
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(num_sms() / (2 * pairs) * (2 * pairs), 1, 1);
-    cfg.blockDim = dim3(ln::S_THREADS, 1, 1);
+    cfg.blockDim = dim3(ln::Q_THREADS, 1, 1);
     cfg.dynamicSmemBytes = ln::Q_SMEM;
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_split_kernel, &cfg) != cudaSuccess || n < 0) {
@@ -1058,7 +1061,7 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
       if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
       cluster_config(cfg, attr, 2 * pairs, stream);
       cfg.gridDim = dim3(static_cast<unsigned>(a.row_tiles * ct * 2 * pairs), 1, 1);
-      cfg.blockDim = dim3(S_THREADS, 1, 1);
+      cfg.blockDim = dim3(Q_THREADS, 1, 1);
       cfg.dynamicSmemBytes = Q_SMEM;
       const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
       if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
