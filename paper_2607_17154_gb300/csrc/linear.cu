@@ -3,20 +3,23 @@
 //
 // The weights are the MMA's M side and the rows of X its N side, as in the expert GEMMs: few
 // rows waste little of the tensor pipe, and the accumulator is transposed (TMEM lane =
-// output column), so a chunk of 32 rows x 128 columns goes through shared memory once and each
-// thread then adds bias, activation and residual to 4 columns of a row and writes them.
+// output column).
 //   linear_split_kernel: one tile of up to 128 columns x 128 rows a cluster of S CTAs, which
 //     share its K and add their accumulators through distributed shared memory, every CTA the
-//     rows of its own share in rank order (the same bits at every call). For few rows, whose
-//     weights are one pass over HBM: the tile's width and S are chosen so that every SM
-//     streams the same share of them.
+//     rows of its own share in rank order (the same bits at every call), four columns a thread.
+//     For few rows, whose weights are one pass over HBM: the tile's width and S are chosen so
+//     that every SM streams the same share of them.
 //   linear_pair_kernel: persistent CTA pairs, tiles of up to 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
-//     main loop. For batches with a tile for most pairs, bound by the tensor cores.
+//     main loop. For batches with a tile for most pairs, bound by the tensor cores (4096 x 14336 x
+//     4096 239 us, 2010 TFLOP/s). Its epilogue is bound by instructions and latency: sixteen
+//     warps, eight rows of a column at a time from TMEM (eight warps, 32 rows through shared memory:
+//     2048 x 4096 x 4096 with SiLU and residual 87 us for 47).
 //   linear_pair_split_kernel: one tile of 256 columns x up to 256 rows a cluster of 2 or 4 CTA
 //     pairs that share its K, the accumulators added as in the first kernel. For batches in between,
 //     whose tiles are too few for the pairs but whose operands, in tiles of 128 x 128, take
-//     longer from L2 than their products.
+//     longer from L2 than their products. (Sixteen warps in the epilogue for four: 300 x 4096 x
+//     4096 with residual 22.9 -> 19.0 us.)
 // The tensor cores truncate a running sum, an error that grows with K (2e-6 of the result at K = 2048,
 // against 4e-7 of fp32 FMAs). Where the sums leave in fp32 (F32), the epilogue warps therefore take
 // the accumulator every 512 of K and add it to sums in registers; bf16 results do not see it.
@@ -115,7 +118,8 @@ __device__ __forceinline__ float4 load_residual4(const Epilogue& e, int m, int n
   return make_float4(f[0], f[1], f[2], f[3]);
 }
 
-// The line of the residual's row m that holds column n, into L2 while the sums are made.
+// The line of the residual's row m that holds column n, into L2 while the sums are made (300 x 4096 x 4096
+// 25.2 -> 23.0 us, 64 rows 12.8 -> 12.4).
 __device__ __forceinline__ void prefetch_residual(const Epilogue& e, int m, int n) {
   asm volatile("prefetch.global.L2 [%0];" ::"l"(e.residual + m * e.ldr + n));
 }
@@ -410,7 +414,7 @@ __global__ void __launch_bounds__(S_THREADS, 2)
 }
 
 // ---------------------------------------------------------------- CTA pairs
-constexpr int P_STAGES = 6;
+constexpr int P_STAGES = 7;  // (six: 300 x 14336 x 4096 39.5 us for 36.8, 64 rows 25.7 for 25.3)
 constexpr int P_STAGE_BYTES = 2 * W_BYTES;  // 128 weight rows and up to 128 rows of X a CTA
 constexpr int P_GROUPS = 4;                 // of four epilogue warps, eight rows of a tile in turn
 constexpr int P_THREADS = 64 + 128 * P_GROUPS;
@@ -915,14 +919,18 @@ __global__ void __launch_bounds__(Q_THREADS, 1)
 }  // namespace ln
 
 // The pair kernel takes products of at least kLinearPairRows rows and kLinearPairTiles tiles of
-// 256 x 256. Measured, pairs against the split kernel with tiles of 128 columns (us, graph
-// replays, K x N): 64 rows, 2048 x 32003 (126 tiles) 28.8 / 30.2, 4096 x 14336 (56) 25.9 / 26.6,
-// 4096 x 4096 (16) 18.3 / 12.6; 128 rows 32.6 / 36.5, 28.4 / 30.5, 21.0 / 15.4; 512 rows,
-// 4096 x 4096 (32) 28.9 / 23.8, 768 (48) 29.3 / 36.7.
-constexpr int kLinearPairRows = 64, kLinearPairTiles = 48;
-// Pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks. Against the split kernel (us, K x
-// N): 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 35.1 / 34.8, 384 rows 38.6 / 52.7, 512 rows 45.5 /
-// 55.1; 384 rows, 4096 x 4096 19.5 / 22.5, 2048 x 2048 11.1 / 12.6.
+// 256 x 256 (us, graph replays, bias and residual, K x N, pairs / split kernel: 64 rows, 4096 x 14336 (56
+// tiles) 25.7 / 28.9, 128 rows 28.1 / 35.8, 256 rows 33.6 / 50.0, 768 rows, 4096 x 4096 (48) 27.8 / 41.4);
+// and from kLinearPairLeast of them where the rows are kPairSplitRows or more (512 rows, 5120 x 5120
+// (40) 33.2 / 45.1, 300 rows 24.3 / 28.5) or K is at most kLinearPairShort blocks (64 rows, 1024 x 5120 8.1 / 8.9,
+// 128 rows 10.0 / 13.0, 2048 x 5632 13.6 / 15.4). Else the split kernel, whose CTAs stream the weights faster
+// (128 rows, 13824 x 5120 37.8, pairs 44.8; 64 rows, 4096 x 4096 (16) 12.1, pairs 16.0; 8192 x 2048
+// 12.2, pairs 25.2).
+constexpr int kLinearPairRows = 64, kLinearPairTiles = 48, kLinearPairLeast = 20, kLinearPairShort = 32;
+// Below kLinearPairTiles, pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks. Against the split
+// kernel (us, K x N): 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 37.1 / 37.6, 300 rows 37.0 / 46.9, 512 rows
+// 45.3 / 54.5; 384 rows, 4096 x 4096 19.3 / 22.6; against pairs on their own: 300 rows, 4096 x 4096 19.0 / 21.4,
+// 14336 x 4096 39.2 / 53.7.
 constexpr int kPairSplitRows = 257, kPairSplitBlocks = 32;
 
 template <bool F32>
@@ -1006,9 +1014,36 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   const int sms_now = num_sms();
-  // pairs: even row tiles of at most 256 rows
   const long long p_tiles = div_up(M, 256) * div_up(N, 256);
-  if (M >= kLinearPairRows && p_tiles >= kLinearPairTiles) {
+  // pairs that share K: as many tiles as all clusters take at once, on most of the pairs
+  if (!e.f32 && p_tiles < kLinearPairTiles && M >= kPairSplitRows && kblocks >= kPairSplitBlocks)
+    for (int pairs = 2; pairs <= Q_MAX_PAIRS; pairs *= 2) {
+      const long long ct = div_up(N, 256), cap = linear_resident_clusters(pairs);
+      long long rt = cap / ct;  // row tiles of at most 256 rows and at least 64
+      if (rt > div_up(M, 64)) rt = div_up(M, 64);
+      if (rt < div_up(M, 256) || rt * ct * pairs * 4 < 3ll * (sms_now / 2)) continue;
+      PairSplitArgs a{};
+      a.e = e;
+      a.rows = static_cast<int>(div_up(div_up(M, rt), 32) * 32);
+      a.row_tiles = static_cast<int>(div_up(M, a.rows));
+      a.kblocks = kblocks;
+      a.pairs = pairs;
+      a.limit_ns = wait_limit_ns();
+      if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
+      if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
+      cluster_config(cfg, attr, 2 * pairs, stream);
+      cfg.gridDim = dim3(static_cast<unsigned>(a.row_tiles * ct * 2 * pairs), 1, 1);
+      cfg.blockDim = dim3(Q_THREADS, 1, 1);
+      cfg.dynamicSmemBytes = Q_SMEM;
+      const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
+      if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
+      OM_LAUNCHED("linear_pair_split_kernel");
+      return ORDERMOE_OK;
+    }
+  // pairs: even row tiles of at most 256 rows
+  if (M >= kLinearPairRows &&
+      (p_tiles >= kLinearPairTiles ||
+       (p_tiles >= kLinearPairLeast && (M >= kPairSplitRows || kblocks <= kLinearPairShort)))) {
     PairArgs a{};
     a.e = e;
     a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_PAIR_ROWS : 256));
@@ -1043,31 +1078,6 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
     OM_LAUNCHED("linear_pair_kernel");
     return ORDERMOE_OK;
   }
-  // pairs that share K: as many tiles as all clusters take at once, on most of the pairs
-  if (!e.f32 && M >= kPairSplitRows && kblocks >= kPairSplitBlocks)
-    for (int pairs = 2; pairs <= Q_MAX_PAIRS; pairs *= 2) {
-      const long long ct = div_up(N, 256), cap = linear_resident_clusters(pairs);
-      long long rt = cap / ct;  // row tiles of at most 256 rows and at least 64
-      if (rt > div_up(M, 64)) rt = div_up(M, 64);
-      if (rt < div_up(M, 256) || rt * ct * pairs * 4 < 3ll * (sms_now / 2)) continue;
-      PairSplitArgs a{};
-      a.e = e;
-      a.rows = static_cast<int>(div_up(div_up(M, rt), 32) * 32);
-      a.row_tiles = static_cast<int>(div_up(M, a.rows));
-      a.kblocks = kblocks;
-      a.pairs = pairs;
-      a.limit_ns = wait_limit_ns();
-      if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
-      if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
-      cluster_config(cfg, attr, 2 * pairs, stream);
-      cfg.gridDim = dim3(static_cast<unsigned>(a.row_tiles * ct * 2 * pairs), 1, 1);
-      cfg.blockDim = dim3(Q_THREADS, 1, 1);
-      cfg.dynamicSmemBytes = Q_SMEM;
-      const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
-      if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
-      OM_LAUNCHED("linear_pair_split_kernel");
-      return ORDERMOE_OK;
-    }
   SplitArgs a{};
   a.e = e;
   // Row tiles of 32 rows and more, as many as leave each tile four CTAs (or what K has for them) of two an
