@@ -1046,10 +1046,22 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
        (p_tiles >= kLinearPairLeast && (M >= kPairSplitRows || kblocks <= kLinearPairShort)))) {
     PairArgs a{};
     a.e = e;
-    a.row_tiles = static_cast<int>(div_up(M, e.f32 ? F32_PAIR_ROWS : 256));
-    a.rows = static_cast<int>(div_up(div_up(M, a.row_tiles), 32) * 32);
-    a.row_tiles = static_cast<int>(div_up(M, a.rows));
+    // Row tiles of 128 to 256 rows, by the rounds over the pairs that they take. A K block of a tile takes
+    // the longer of its products, as rows, and its loads, 0.8 of (128 + rows / 2) (256 rows 66 us a round of
+    // K = 14336, 192 51, 160 42, 128 40, 96 37). 4096 x 14336, in tiles of up to 256 rows / by this rule: 768
+    // rows 68.1 / 55.9, 1500 rows 132 / 106, 2500 rows 204 / 166, 4096 rows 284 / 265; 512 rows of 5632 x
+    // 2048 16.8 / 14.2. A gain of less than 3 % is left to the larger tiles, which load less.
     const int most = linear_resident_pairs();
+    long long best = INT64_MAX;
+    for (int rows = e.f32 ? F32_PAIR_ROWS : 256; rows >= 128; rows -= 32) {
+      const long long rt = div_up(M, rows), even = div_up(div_up(M, rt), 32) * 32, loads = 102 + even * 2 / 5;
+      const long long cost = div_up(rt * div_up(N, 256), most) * (even > loads ? even : loads);
+      if (best == INT64_MAX || cost * 100 < best * 97) {
+        best = cost;
+        a.rows = static_cast<int>(even);
+      }
+    }
+    a.row_tiles = static_cast<int>(div_up(M, a.rows));
     a.cols = 256;
     // One or two row tiles are bound by the weights' bytes: tiles as narrow as the same number of rounds
     // allows, so that every pair loads the same share (32003 x 2048: 64 rows 29.2 -> 28.7 us, 128 32.9 -> 31.2,
