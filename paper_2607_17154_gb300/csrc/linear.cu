@@ -927,11 +927,12 @@ __global__ void __launch_bounds__(Q_THREADS, 1)
 // (128 rows, 13824 x 5120 37.8, pairs 44.8; 64 rows, 4096 x 4096 (16) 12.1, pairs 16.0; 8192 x 2048
 // 12.2, pairs 25.2).
 constexpr int kLinearPairRows = 64, kLinearPairTiles = 48, kLinearPairLeast = 20, kLinearPairShort = 32;
-// Below kLinearPairTiles, pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks. Against the split
-// kernel (us, K x N): 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 37.1 / 37.6, 300 rows 37.0 / 46.9, 512 rows
-// 45.3 / 54.5; 384 rows, 4096 x 4096 19.3 / 22.6; against pairs on their own: 300 rows, 4096 x 4096 19.0 / 21.4,
-// 14336 x 4096 39.2 / 53.7.
-constexpr int kPairSplitRows = 257, kPairSplitBlocks = 32;
+// Below kLinearPairTiles, pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks (us, K x N, shared /
+// split kernel: 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 37.1 / 37.6, 300 rows 37.0 / 46.9, 512 rows 45.3 / 54.5;
+// 512 rows, 2048 x 2048 11.6 / 13.1), and from kPairSplitLong where there are kLinearPairLeast tiles (shared / pairs on
+// their own: 300 rows, 14336 x 4096 36.4 / 45.9, 512 rows 44.0 / 46.6; 384 rows, 4096 x 4096 18.2 / 17.8, 512 rows
+// 20.7 / 18.1; 768 rows, 2048 x 2048 13.3 / 11.6).
+constexpr int kPairSplitRows = 257, kPairSplitBlocks = 32, kPairSplitLong = 96;
 
 template <bool F32>
 static cudaError_t linear_attr() {
@@ -1016,7 +1017,8 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   const int sms_now = num_sms();
   const long long p_tiles = div_up(M, 256) * div_up(N, 256);
   // pairs that share K: as many tiles as all clusters take at once, on most of the pairs
-  if (!e.f32 && p_tiles < kLinearPairTiles && M >= kPairSplitRows && kblocks >= kPairSplitBlocks)
+  if (!e.f32 && p_tiles < kLinearPairTiles && M >= kPairSplitRows &&
+      kblocks >= (p_tiles < kLinearPairLeast ? kPairSplitBlocks : kPairSplitLong))
     for (int pairs = 2; pairs <= Q_MAX_PAIRS; pairs *= 2) {
       const long long ct = div_up(N, 256), cap = linear_resident_clusters(pairs);
       long long rt = cap / ct;  // row tiles of at most 256 rows and at least 64

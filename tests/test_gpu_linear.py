@@ -119,7 +119,8 @@ def test_pairs_of_narrow_column_tiles(M, N, K, f32):
 
 # fewer tiles, many K blocks: two pairs share K, or four (the last two)
 PAIR_SPLIT = [(300, 4096, 2056), (512, 4000, 2048), (257, 8100, 2200), (333, 2999, 4096), (200, 8100, 2200),
-              (150, 1280, 2048), (300, 700, 2048), (290, 643, 3000)]
+              (150, 1280, 2048), (300, 700, 2048), (290, 643, 3000), (300, 4096, 6200), (512, 4000, 6144),
+              (400, 2000, 2048), (257, 5000, 6400)]
 
 
 @pytest.mark.parametrize("M,N,K", PAIR_SPLIT)
