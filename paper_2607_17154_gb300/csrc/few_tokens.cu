@@ -993,6 +993,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   // On the residual map a CTA a token (its norm is a sum over the row), otherwise every token's
   // columns over G / T CTAs.
   const int parts = a.h != nullptr ? 1 : max(1, G / a.T);
+  // Thread 0 leaves the counters behind its CTA's last wait, not behind its last store; the answer is not
+  // needed before the end (8 experts, d 256: 8 tokens 18.5 -> 17.8 us, 16 tokens 23.9 -> 22.8).
+  unsigned int before = 0;
+  if (tid == 0 && cta >= a.T * parts) before = atomicAdd(&a.sync[2], 1u);
   if (cta < a.T * parts) {
     const int tiles = a.d / C::DOWN_ROWS, part = cta / a.T;
     const int first_tile = tiles * part / parts, last_tile = tiles * (part + 1) / parts;
@@ -1004,7 +1008,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         own[2 * i] = static_cast<int16_t>(share.owner(static_cast<long long>(i) * share.per_tile));
         own[2 * i + 1] = static_cast<int16_t>(share.owner(static_cast<long long>(i + 1) * share.per_tile - 1));
       }
-    if (tid == 0 && !grid_wait(&a.sync[1], G, a.limit_ns, abort)) timeout(36);
+    if (tid == 0) {
+      if (!grid_wait(&a.sync[1], G, a.limit_ns, abort)) timeout(36);
+      before = atomicAdd(&a.sync[2], 1u);
+    }
     __syncthreads();
     for (int t = cta % a.T; t < a.T && !*abort; t += G) {
       if (!s.valid[t]) continue;
@@ -1097,15 +1104,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     for (int i = 0; i < STAGES; ++i)
       if ((issued_mask >> i) & 1u) mbar_wait(&s.full[i], (last_phase_bits >> i) & 1u, a.limit_ns, never);
   }
-  cluster_sync();  // (no access to the peer is under way)
-  // the last CTA to leave sets the counters back
-  if (tid == 0) {
-    __threadfence();
-    if (atomicAdd(&a.sync[2], 1u) == static_cast<unsigned int>(G) - 1) {
-      a.sync[0] = a.sync[1] = a.sync[2] = 0;
-      __threadfence();
-    }
-  }
+  // the last CTA that left the counters sets them back (none accesses its peer's memory here)
+  if (tid == 0 && before == static_cast<unsigned int>(G) - 1) a.sync[0] = a.sync[1] = a.sync[2] = 0;
 }
 
 }  // namespace fw
