@@ -494,11 +494,10 @@ def ordermoe_linear(X, W, Y, bias=None, act="none", residual=None, stream=None):
     code = ACTIVATIONS.get(act)
     if code is None:
         raise ValueError("unknown activation %r" % (act,))
-    for t in (X, W, Y):
-        if not isinstance(t, torch.Tensor) or t.dim() != 2:
-            raise TypeError("X, W and Y must be matrices")
-    M, K = X.shape
-    N = W.shape[0]
+    try:
+        (M, K), (N, _), (_, _) = X.shape, W.shape, Y.shape
+    except (AttributeError, ValueError):
+        raise TypeError("X, W and Y must be matrices") from None
     dev = torch.cuda.current_device()
     x, ldx = _matrix(X, "X", X.shape, dev)
     w, ldw = _matrix(W, "W", (N, K), dev)
