@@ -1212,6 +1212,9 @@ static int few_layer(const char* who, const ordermoe_layer_desc* L, int T, const
   if ((long long)L->E * L->dff > INT32_MAX || (long long)L->E * L->d > INT32_MAX)
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: sizes too large", who);
   if (L->lookahead_H > 4) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "%s: look-ahead of at most 4 layers", who);
+  if (L->lookahead_H > 1 &&
+      (!L->P || L->tables_stride < om::tables_bytes(L->E, 1) || L->tables_stride % 16 != 0))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "%s: look-ahead needs P and a table stride of a multiple of 16", who);
   if (!L->W_r || !L->W1 || !L->W3 || !L->W2 || !L->tables)
     return fail(ORDERMOE_ERR_INVALID_ARG, "%s: null pointer in the layer", who);
   if (!aligned16(L->W_r) || !aligned16(L->W1) || !aligned16(L->W3) || !aligned16(L->W2) || !aligned16(L->tables))

@@ -57,6 +57,16 @@ def test_calls_that_layer_few_refuses(call, code):
     assert rc == code and msg.startswith("layer_few:"), (call, rc, msg)
 
 
+@pytest.mark.parametrize("over", [dict(P=N), dict(tables_stride=0), dict(tables_stride=100),
+                                  dict(tables_stride=4104)])
+@pytest.mark.parametrize("T", [4, 0])
+def test_look_ahead_is_refused_before_anything_is_enqueued(over, T):
+    """The decisions of a look-ahead are prepared by a copy of their own on the stream: without a GPU that
+    copy fails, so a refusal that came behind it would be another error."""
+    rc, msg = few(desc(**dict(dict(lookahead_H=2, tables_stride=4096, P=AT), **over)), T=T)
+    assert rc == ARG and msg.startswith("layer_few:"), (rc, msg)
+
+
 def test_no_tokens():
     assert few(T=0, X=N, home=N, y=N, ws=N, nbytes=0)[0] == OK
     assert B.lib().ordermoe_layer_few(N, 0, N, N, N, N, N, N, N, 0, N) == ARG
