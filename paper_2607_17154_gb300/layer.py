@@ -6,7 +6,8 @@ from . import binding as B
 
 
 class MoELayer:
-    """Holds a layer's weights, tables and scratch for up to T_max tokens."""
+    """Holds a layer's weights, tables and scratch for up to T_max tokens. Its calls share the scratch:
+    they may not overlap on the GPU (one stream, or one ordered behind the other)."""
 
     def __init__(self, W_r, W1, W3, W2, tables, k, T_max, renorm=1, device=None, few=False):
         """few: also keep the workspace of forward_few (calls of up to B.FEW_TOKENS tokens)."""
@@ -102,7 +103,18 @@ def few_workspace(T, E, d, dff, k, device):
                      device=device)
     with torch.cuda.device(device):
         B.ordermoe_layer_few_init(ws)
+    _settle(device)
     return ws
+
+
+def _settle(device):
+    """Waits for the current stream: buffers that were made and cleared there may then be used on any
+    other. (While it is being captured nothing runs, and only the graph may use them.)"""
+    if torch.device(device).type != "cuda":
+        return
+    with torch.cuda.device(device):
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
 
 
 def build_tables(sim, group, placement, theta, qbar, sp, device, out=None):
@@ -122,13 +134,15 @@ def build_tables(sim, group, placement, theta, qbar, sp, device, out=None):
 class DenseFFN:
     """A dense feed-forward layer (every second layer of Switch-Base-8E is one, with ReLU):
     y = act(x W1^T + b1) W2^T + b2 through ordermoe_linear, for up to T_max tokens.
-    W1 [dff, d], W2 [d, dff], b1 [dff], b2 [d] bf16 (the biases may be None)."""
+    W1 [dff, d], W2 [d, dff], b1 [dff], b2 [d] bf16 (the biases may be None). Calls share H: they may
+    not overlap on the GPU."""
 
     def __init__(self, W1, W2, T_max, b1=None, b2=None, act="relu"):
         self.W1, self.W2, self.b1, self.b2, self.act = W1, W2, b1, b2, act
         self.dff, self.d = W1.shape
         self.T_max = T_max
         self.H = torch.empty(T_max, self.dff, dtype=torch.bfloat16, device=W1.device)
+        _settle(W1.device)
 
     def forward(self, x, y, residual=None, stream=None):
         """y = the layer of x [T, d], added to residual [T, d] when given (y may be it)."""
@@ -148,7 +162,8 @@ class DenseFFN:
 class LayerStack:
     """L MoE layers run through ordermoe_layer_forward with the token state
     (location, accumulated loss; Eqs. 36 and 44) carried from layer to layer, and
-    DenseFFN layers between them."""
+    DenseFFN layers between them. Steps, and the graphs captured from them, share
+    the scratch: they may not overlap on the GPU."""
 
     def __init__(self, layers, tables, k, T_max, device, H=1, stride=0, P=None, few=False):
         """layers: dicts with W_r, W1, W3, W2 (device bf16). tables: a list of

@@ -99,6 +99,30 @@ def test_workspace_sizes():
     assert B.lib().ordermoe_layer_few_init(AT + 64, 1 << 20, N) == ARG
 
 
+def test_a_workspace_is_ready_for_any_stream_when_it_is_returned(monkeypatch):
+    """The counters are cleared on the stream that is current where it is made; a first call on another
+    stream is ordered behind nothing. So the clearing has ended before anyone has the workspace."""
+    from contextlib import nullcontext
+
+    from paper_2607_17154_gb300 import layer
+    done, capturing = [], [False]
+
+    class Stream:
+        def synchronize(self):
+            done.append("wait")
+    monkeypatch.setattr(B, "ordermoe_layer_few_init", lambda ws, stream=None: done.append("clear"))
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
+    monkeypatch.setattr(torch.cuda, "device", lambda d: nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: Stream())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    layer.few_workspace(4, 8, 256, 512, 2, "cuda:0")
+    assert done == ["clear", "wait"]
+    capturing[0] = True  # nothing to wait for
+    layer.few_workspace(4, 8, 256, 512, 2, "cuda:0")
+    assert done == ["clear", "wait", "clear"]
+
+
 def linear(X=AT, ldx=64, W=AT, ldw=64, bias=N, act=0, residual=N, ldr=0, M=4, n=32, K=64, Y=AT, ldy=32, f32=0):
     rc = B.lib().ordermoe_linear(X, ldx, W, ldw, bias, act, residual, ldr, M, n, K, Y, ldy, f32, N)
     return rc, B.lib().ordermoe_last_error().decode()

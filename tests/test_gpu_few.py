@@ -334,6 +334,31 @@ def test_two_calls_at_once():
     assert np.array_equal(args[1][4].float().cpu().numpy(), yb)
 
 
+def test_first_call_on_another_stream():
+    """Layers made behind work that is still under way, on memory that it leaves full of ones, whose
+    first call is on a stream that nobody ordered behind it."""
+    a = Case(TINY, 6, seed=45)
+    ya = a.run(state=False)[0]
+    X, home = a.X.to(DEV), torch.as_tensor(a.home).to(DEV)
+    y = torch.zeros(6, a.d, dtype=torch.bfloat16, device=DEV)
+    m, s = a.layer, torch.cuda.Stream()
+    big = torch.ones(1 << 28, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        dirty = torch.empty(m.few_ws.numel(), dtype=torch.uint8, device=DEV)
+        for _ in range(20):
+            big.mul_(1.0)
+        dirty.fill_(1)
+        del dirty
+        b = MoELayer(m.W_r, m.W1, m.W3, m.W2, m.tables, m.k, 6, few=True)
+        b.forward_few(X, home, None, None, y, stream=s)
+        s.synchronize()
+        assert np.array_equal(y.float().cpu().numpy(), ya)
+        assert not b.few_ws[:12].any()
+        y.zero_()
+        torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("H", [1, 3])
 @pytest.mark.parametrize("T", [1, 13, 17])
 def test_stack_of_few_tokens(H, T):
