@@ -36,9 +36,33 @@ class MoELayer:
         self.few_ws = None
         if few:
             self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), self.E, self.d, self.dff, k, dev)
-            self.few_desc = B.make_layer_desc(T_max, W_r, W1, W3, W2, tables, k, self.ws, renorm)
-            self.few_out = B.make_few_out(self.logits, self.topk_idx, self.topk_w, self.chosen,
-                                          self.server, self.kind, self.counters)
+
+    # What forward_few's descriptors point to: forward() reads these at every call, so a new plan's
+    # tables, new weights or another buffer put in their place have to reach forward_few too.
+    _DESCRIBED = frozenset(("W_r", "W1", "W3", "W2", "tables", "k", "renorm", "logits", "topk_idx",
+                            "topk_w", "chosen", "server", "kind", "counters"))
+    _few = None
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name in self._DESCRIBED:
+            object.__setattr__(self, "_few", None)
+
+    def _described(self):
+        if self._few is None:
+            self._few = (B.make_layer_desc(self.T_max, self.W_r, self.W1, self.W3, self.W2,
+                                           self.tables, self.k, self.ws, self.renorm),
+                         B.make_few_out(self.logits, self.topk_idx, self.topk_w, self.chosen,
+                                        self.server, self.kind, self.counters))
+        return self._few
+
+    @property
+    def few_desc(self):
+        return self._described()[0]
+
+    @property
+    def few_out(self):
+        return self._described()[1]
 
     def forward(self, X, home, loc, qhat, y, T=None, logits_in=None, stream=None):
         """y[:T] = MoE(X[:T]); loc/qhat are updated in place (Eq. 44)."""

@@ -123,6 +123,34 @@ def test_a_workspace_is_ready_for_any_stream_when_it_is_returned(monkeypatch):
     assert done == ["clear", "wait", "clear"]
 
 
+def test_what_replaces_a_layers_tensors_reaches_its_few_token_calls(monkeypatch):
+    """forward() reads a layer's weights, tables and buffers at every call; so must forward_few(), whose
+    descriptors are made before (a plan made again puts new tables in place of the old)."""
+    from paper_2607_17154_gb300 import layer
+    seen = []
+    monkeypatch.setattr(layer, "few_workspace", lambda *a: torch.zeros(1 << 12, dtype=torch.uint8))
+    monkeypatch.setattr(B, "ordermoe_layer_few", lambda desc, T, X, home, loc, qhat, y, ws, out, stream: seen.append((desc, out)))
+    monkeypatch.setattr(B, "_ptr", lambda t: t.data_ptr() if t is not None else None)
+    bf = torch.bfloat16
+    Wr, W1, W2 = torch.zeros(4, 256, dtype=bf), torch.zeros(4, 128, 256, dtype=bf), torch.zeros(4, 256, 128, dtype=bf)
+    tables = torch.zeros(B.ordermoe_tables_bytes(4, 1), dtype=torch.uint8)
+    m = layer.MoELayer(Wr, W1, W1.clone(), W2, tables, 2, 4, few=True)
+    x = torch.zeros(4, 256, dtype=bf)
+    for name in ("tables", "W_r", "W1", "W3", "W2"):
+        old = getattr(m, name)
+        setattr(m, name, old.clone())
+        m.forward_few(x, None, None, None, x)
+        assert getattr(seen[-1][0], name) == getattr(m, name).data_ptr() != old.data_ptr(), name
+    for name, field in (("logits", "logits"), ("topk_idx", "topk_idx"), ("topk_w", "topk_w"), ("chosen", "chosen_expert"),
+                        ("server", "chosen_server"), ("kind", "kind"), ("counters", "counters")):
+        setattr(m, name, getattr(m, name).clone())
+        m.forward_few(x, None, None, None, x)
+        assert getattr(seen[-1][1], field) == getattr(m, name).data_ptr(), name
+    m.renorm, m.k = 0, 1
+    m.forward_few(x, None, None, None, x)
+    assert (seen[-1][0].renorm, seen[-1][0].k) == (0, 1)
+
+
 def linear(X=AT, ldx=64, W=AT, ldw=64, bias=N, act=0, residual=N, ldr=0, M=4, n=32, K=64, Y=AT, ldy=32, f32=0):
     rc = B.lib().ordermoe_linear(X, ldx, W, ldw, bias, act, residual, ldr, M, n, K, Y, ldy, f32, N)
     return rc, B.lib().ordermoe_last_error().decode()
