@@ -155,17 +155,27 @@ def build_tables(sim, group, placement, theta, qbar, sp, device, out=None):
     return t
 
 
+def _rows16(W):
+    """The matrix W as ordermoe_linear takes it, rows at multiples of 16 bytes: itself, or a copy."""
+    n, w = W.shape
+    if W.data_ptr() % 16 == 0 and (w <= 1 or W.stride(1) == 1) and (n <= 1 or W.stride(0) % 8 == 0):
+        return W
+    return torch.empty(n, (w + 7) // 8 * 8, dtype=W.dtype, device=W.device)[:, :w].copy_(W)
+
+
 class DenseFFN:
     """A dense feed-forward layer (every second layer of Switch-Base-8E is one, with ReLU):
     y = act(x W1^T + b1) W2^T + b2 through ordermoe_linear, for up to T_max tokens.
-    W1 [dff, d], W2 [d, dff], b1 [dff], b2 [d] bf16 (the biases may be None). Calls share H: they may
-    not overlap on the GPU."""
+    W1 [dff, d], W2 [d, dff], b1 [dff], b2 [d] bf16 (the biases may be None). Weights whose rows do not
+    start at multiples of 16 bytes (a d_ff that is no multiple of 8) are copied once to rows that do; x
+    of more than one row needs such rows itself. Calls share H: they may not overlap on the GPU."""
 
     def __init__(self, W1, W2, T_max, b1=None, b2=None, act="relu"):
-        self.W1, self.W2, self.b1, self.b2, self.act = W1, W2, b1, b2, act
+        self.W1, self.W2, self.b1, self.b2, self.act = _rows16(W1), _rows16(W2), b1, b2, act
         self.dff, self.d = W1.shape
         self.T_max = T_max
-        self.H = torch.empty(T_max, self.dff, dtype=torch.bfloat16, device=W1.device)
+        self.H = torch.empty(T_max, (self.dff + 7) // 8 * 8, dtype=torch.bfloat16,
+                             device=W1.device)[:, :self.dff]
         _settle(W1.device)
 
     def forward(self, x, y, residual=None, stream=None):

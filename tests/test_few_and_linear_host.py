@@ -223,6 +223,27 @@ def test_binding_refuses_host_tensors_types_and_shapes(monkeypatch):
         B.ordermoe_layer_few(desc(), 4, X, u8, None, None, X, u8)
 
 
+@pytest.mark.parametrize("d,dff", [(64, 100), (64, 1), (72, 9), (20, 36), (64, 128)])
+def test_dense_layers_hand_on_rows_that_the_product_takes(monkeypatch, d, dff):
+    """Whatever d_ff is, both products of a DenseFFN get weights and activations whose rows start at
+    multiples of 16 bytes, with the caller's values."""
+    from paper_2607_17154_gb300 import layer
+    bf, calls = torch.bfloat16, []
+    W1, W2 = torch.randn(dff, d).to(bf), torch.randn(d, dff).to(bf)
+    monkeypatch.setattr(B, "ordermoe_linear", lambda X, W, Y, **kw: calls.append((X, W, Y, kw)))
+    m = layer.DenseFFN(W1, W2, 5)
+    x, y = torch.zeros(5, (d + 7) // 8 * 8, dtype=bf)[:, :d], torch.zeros(5, d, dtype=bf)
+    m.forward(x, y, residual=y)
+    (X, V1, H, k1), (H2, V2, Y, k2) = calls
+    for t in (V1, V2, H, H2):
+        assert t.stride(0) % 8 == 0 and t.data_ptr() % 16 == 0 and (t.shape[1] == 1 or t.stride(1) == 1)
+    assert torch.equal(V1, W1) and torch.equal(V2, W2)
+    assert H.shape == H2.shape == (5, dff) and H.data_ptr() == H2.data_ptr() and H.stride() == H2.stride()
+    assert X is x and Y is y and k1["act"] == "relu" and k2["residual"] is y
+    if d % 8 == 0 and dff % 8 == 0:  # nothing is copied
+        assert V1 is W1 and V2 is W2
+
+
 def kernel(path, name):
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
     start = text.index("{", text.index(name + "("))

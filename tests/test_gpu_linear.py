@@ -289,6 +289,27 @@ def test_stack_of_moe_and_dense_layers(T, few):
     assert all(torch.equal(u, v) for u, v in zip(eager, hs))
 
 
+@pytest.mark.parametrize("T,d,dff", [(1, 64, 100), (6, 64, 9), (70, 256, 501), (300, 512, 1001), (5, 64, 1)])
+def test_dense_layers_of_any_width(T, d, dff):
+    """A d_ff that is no multiple of 8. H is rounded once (2^-8) and carries the first product's bound; y is
+    off by W2 times that and by its own sum's and rounding's."""
+    W1, W2 = rows(dff, d, 0.1, 70, odd=True).clone(), rows(d, dff, 0.1, 71, odd=True).clone()
+    b1, b2 = rows(1, dff, 0.5, 72)[0].contiguous(), rows(1, d, 0.5, 73)[0].contiguous()
+    x, h = rows(T, d, 1.0, 74), rows(T, d, 1.0, 75)
+    y = torch.empty(T, d, dtype=torch.bfloat16, device=DEV)
+    DenseFFN(W1, W2, T, b1=b1, b2=b2).forward(x, y, residual=h)
+    X, A1, A2 = x.double(), W1.double(), W2.double()
+    g = X @ A1.T + b1.double()
+    S = X.abs() @ A1.abs().T + b1.double().abs()
+    H = g.clamp(min=0.0)
+    dH = 2.0 ** -8 * H + (1 + 2.0 ** -8) * (d + 8) * 2.0 ** -23 * S
+    ref = H @ A2.T + b2.double() + h.double()
+    mag = (H + dH) @ A2.abs().T + b2.double().abs()
+    err = dH @ A2.abs().T + (dff + 8) * 2.0 ** -23 * mag + 2.0 ** -24 * ref.abs()
+    off = (y.double() - ref).abs()
+    assert (off <= 2.0 ** -8 * ref.abs() + (1 + 2.0 ** -8) * err).all(), (off / (2.0 ** -8 * ref.abs() + err)).max()
+
+
 def test_short_products_behind_long_ones_on_two_streams():
     """Every kernel behind every other, launched eagerly, two streams side by side: TMEM of a CTA is free when it asks."""
     sizes = [(1021, 4096, 512), (1, 256, 64), (300, 2048, 2048), (16, 256, 256), (4096, 128, 64), (128, 2048, 4096),
