@@ -206,12 +206,14 @@ class LayerStack:
         transition matrices. Layer l looks min(H, L - l) - 1 layers ahead. few: steps of at most
         B.FEW_TOKENS tokens run each MoE layer in one launch (ordermoe_layer_few). A
         DenseFFN in `layers` runs in its place; tables, P and L then count the MoE layers
-        alone, in order."""
+        alone, in order (a stack may have none: tables, k, P and few say nothing then)."""
         dense = {l: lay for l, lay in enumerate(layers) if isinstance(lay, DenseFFN)}
         layers = [lay for lay in layers if not isinstance(lay, DenseFFN)]
-        E, dff, d = layers[0]["W1"].shape
+        if not layers and not dense:
+            raise ValueError("a stack needs a layer")
+        E, dff, d = layers[0]["W1"].shape if layers else (0, 0, next(iter(dense.values())).d)
         L = len(layers)
-        self.scratch = torch.empty(B.ordermoe_layer_scratch_bytes(T_max, E, d, dff, k),
+        self.scratch = torch.empty(B.ordermoe_layer_scratch_bytes(T_max, E, d, dff, k) if layers else 0,
                                    dtype=torch.uint8, device=device)
         self.descs = []
         for l, lay in enumerate(layers):
@@ -227,7 +229,9 @@ class LayerStack:
         for l, lay in dense.items():
             self.descs.insert(l, lay)
         self.d, self.T_max = d, T_max
-        self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), E, d, dff, k, device) if few else None
+        self.few_ws = None
+        if few and layers:
+            self.few_ws = few_workspace(min(T_max, B.FEW_TOKENS), E, d, dff, k, device)
 
     def _few(self, T):
         return self.few_ws is not None and T <= B.FEW_TOKENS

@@ -244,6 +244,25 @@ def test_dense_layers_hand_on_rows_that_the_product_takes(monkeypatch, d, dff):
         assert V1 is W1 and V2 is W2
 
 
+@pytest.mark.parametrize("few", [False, True])
+def test_a_stack_of_dense_layers_alone(monkeypatch, few):
+    from paper_2607_17154_gb300 import layer
+    bf, calls = torch.bfloat16, []
+    monkeypatch.setattr(B, "ordermoe_linear", lambda X, W, Y, **kw: calls.append((X, W, Y, kw["residual"] if "residual" in kw else None)))
+    monkeypatch.setattr(B, "ordermoe_rmsnorm", lambda h, T, d, eps, x, stream: calls.append((h, x)))
+    dense = [layer.DenseFFN(torch.zeros(128, 64, dtype=bf), torch.zeros(64, 128, dtype=bf), 4) for _ in range(2)]
+    st = layer.LayerStack(dense, [], 0, 4, "cpu", few=few)
+    xs, hs = [torch.zeros(4, 64, dtype=bf) for _ in range(3)], [torch.zeros(4, 64, dtype=bf) for _ in range(3)]
+    st.step(xs[:2], None, None, None, hs[:2])
+    assert [c[2] is y for c, y in zip(calls[1::2], hs)] == [True, True] and len(calls) == 4
+    calls.clear()
+    st.step_residual(hs, xs, None, None, None)
+    assert len(calls) == 7 and calls[0] == (hs[0], xs[0]) and calls[3] == (hs[1], xs[1]) and calls[6] == (hs[2], xs[2])
+    assert calls[1][0] is xs[0] and calls[2][3] is hs[0] and calls[2][2] is hs[1]
+    with pytest.raises(ValueError):
+        layer.LayerStack([], [], 2, 4, "cpu")
+
+
 def kernel(path, name):
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
     start = text.index("{", text.index(name + "("))

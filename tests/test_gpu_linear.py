@@ -310,6 +310,32 @@ def test_dense_layers_of_any_width(T, d, dff):
     assert (off <= 2.0 ** -8 * ref.abs() + (1 + 2.0 ** -8) * err).all(), (off / (2.0 ** -8 * ref.abs() + err)).max()
 
 
+@pytest.mark.parametrize("few", [False, True])
+def test_stack_of_dense_layers_alone(few):
+    """No MoE layer: a step and its graph give what the layers give one by one."""
+    T, d, dff, L = 5, 256, 384, 3
+    dense = [DenseFFN(rows(dff, d, 0.1, 80 + l), rows(d, dff, 0.1, 90 + l), T, act="gelu") for l in range(L)]
+    st = LayerStack(dense, [], 1, T, DEV, few=few)
+    hs = [synth.hidden(T, d, 6, DEV)] + [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(L)]
+    xs = [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(L + 1)]
+    home = torch.zeros(T, dtype=torch.uint8, device=DEV)
+    st.step_residual(hs, xs, home, None, None)
+    want = [hs[0].clone()]
+    x = torch.zeros_like(hs[0])
+    B.ordermoe_rmsnorm(want[0], T, d, B.NORM_EPS, x)
+    for lay in dense:
+        want.append(torch.zeros_like(hs[0]))
+        lay.forward_residual(x.clone(), want[-2], want[-1], x)
+    torch.cuda.synchronize()
+    assert all(torch.equal(u, v) for u, v in zip(hs, want)) and torch.equal(xs[-1], x)
+    g = st.capture_residual(hs, xs, home, None, None)
+    for h in hs[1:]:
+        h.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(u, v) for u, v in zip(hs, want))
+
+
 def test_short_products_behind_long_ones_on_two_streams():
     """Every kernel behind every other, launched eagerly, two streams side by side: TMEM of a CTA is free when it asks."""
     sizes = [(1021, 4096, 512), (1, 256, 64), (300, 2048, 2048), (16, 256, 256), (4096, 128, 64), (128, 2048, 4096),
