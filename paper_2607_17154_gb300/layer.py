@@ -256,7 +256,8 @@ class LayerStack:
         then layer l runs on xs[l] and writes hs[l + 1] = hs[l] + y_l and
         xs[l + 1] = RMSNorm(hs[l + 1]). hs, xs: L + 1 device buffers [T, d]
         bf16 (hs[0] is the input); logits: optional [L, T, E] f32 receiving each
-        layer's router logits (layer-major; a dense layer leaves its own)."""
+        layer's router logits (layer-major; a dense layer leaves its own), or a
+        list of [T, E] buffers (None: not wanted)."""
         T = hs[0].shape[0]
         B.ordermoe_rmsnorm(hs[0], T, self.d, eps, xs[0], stream)
         for l, desc in enumerate(self.descs):
@@ -324,26 +325,38 @@ def calibrate_stack(layers, h_cal, k_freq, M, eps=B.NORM_EPS):
     [N, d] pass through the unmodified stack (every routed expert kept), and
     layer l's similarity and counts (Eqs. 3-5) are taken over its own inputs
     x_l = RMSNorm(h_l), its transitions (Eq. 41) between the router logits of
-    consecutive layers along the same pass. Returns a dict: sim [L, E, E],
-    counts [L, E], P [L-1, E, E], tcount [L-1, E, E], logits [L, N, E] (f32
-    device), hs and xs (the L + 1 residual states and normalised inputs)."""
+    consecutive layers along the same pass. DenseFFN layers run in their place,
+    and what is returned counts the MoE layers alone, in order, as LayerStack's
+    tables and P do. Returns a dict: sim [L, E, E], counts [L, E],
+    P [L-1, E, E], tcount [L-1, E, E], logits [L, N, E] (f32 device) of the L
+    MoE layers, hs and xs (the residual states and normalised inputs of all
+    layers, one more than there are)."""
     dev = h_cal.device
     N, d = h_cal.shape
-    L = len(layers)
-    E = layers[0]["W1"].shape[0]
+    moe = [l for l, lay in enumerate(layers) if not isinstance(lay, DenseFFN)]
+    L = len(moe)
+    if L == 0:
+        raise ValueError("calibrate_stack: no MoE layer")
+    E = layers[moe[0]]["W1"].shape[0]
+    # (more tokens than a dense layer serves: its weights, with room for these)
+    run = [lay if not isinstance(lay, DenseFFN) or lay.T_max >= N
+           else DenseFFN(lay.W1, lay.W2, N, lay.b1, lay.b2, lay.act) for lay in layers]
     tab = exact_tables(E, M, dev)
-    stack = LayerStack(layers, [tab] * L, k_freq, N, dev)
-    hs = [h_cal] + [torch.empty_like(h_cal) for _ in range(L)]
-    xs = [torch.empty_like(h_cal) for _ in range(L + 1)]
+    stack = LayerStack(run, [tab] * L, k_freq, N, dev)
+    hs = [h_cal] + [torch.empty_like(h_cal) for _ in layers]
+    xs = [torch.empty_like(h_cal) for _ in range(len(layers) + 1)]
     home = torch.zeros(N, dtype=torch.uint8, device=dev)
     logits = torch.empty(L, N, E, dtype=torch.float32, device=dev)
-    stack.step_residual(hs, xs, home, None, None, logits=logits, eps=eps)
+    of = [None] * len(layers)  # a layer's logits
+    for i, l in enumerate(moe):
+        of[l] = logits[i]
+    stack.step_residual(hs, xs, home, None, None, logits=of, eps=eps)
     sim = torch.empty(L, E, E, dtype=torch.float32, device=dev)
     counts = torch.empty(L, E, dtype=torch.int32, device=dev)
     ws = torch.empty(B.ordermoe_similarity_workspace_bytes(1, E, N), dtype=torch.uint8, device=dev)
-    for l in range(L):
-        B.ordermoe_similarity_no_logits(layers[l]["W_r"], xs[l], 1, E, d, N, k_freq, sim[l],
-                                        counts[l], ws)
+    for i, l in enumerate(moe):
+        B.ordermoe_similarity_no_logits(layers[l]["W_r"], xs[l], 1, E, d, N, k_freq, sim[i],
+                                        counts[i], ws)
     P = torch.empty(max(L - 1, 1), E, E, dtype=torch.float32, device=dev)
     tcount = torch.empty(max(L - 1, 1), E, E, dtype=torch.int32, device=dev)
     if L >= 2:

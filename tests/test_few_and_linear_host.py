@@ -263,6 +263,38 @@ def test_a_stack_of_dense_layers_alone(monkeypatch, few):
         layer.LayerStack([], [], 2, 4, "cpu")
 
 
+def test_calibration_counts_the_moe_layers_of_a_stack(monkeypatch):
+    """Of MoE, dense, MoE: each MoE layer's own inputs and logits, in order; the dense one with room for all
+    calibration tokens."""
+    from paper_2607_17154_gb300 import layer
+    bf, N, d, E, seen = torch.bfloat16, 9, 64, 4, {}
+
+    class Stack:
+        def __init__(self, layers, tables, k, T_max, device):
+            seen.update(layers=layers, tables=tables)
+
+        def step_residual(self, hs, xs, home, loc, qhat, logits, eps):
+            seen.update(hs=hs, xs=xs, logits=logits)
+    monkeypatch.setattr(layer, "LayerStack", Stack)
+    monkeypatch.setattr(layer, "exact_tables", lambda *a: "tables")
+    monkeypatch.setattr(B, "ordermoe_similarity_no_logits", lambda W, x, *a: seen.setdefault("sim", []).append((W, x)))
+    monkeypatch.setattr(B, "ordermoe_transitions_strided", lambda lg, *a: seen.update(trans=(lg, a)))
+    dense = layer.DenseFFN(torch.ones(128, d, dtype=bf), torch.ones(d, 128, dtype=bf), 2)
+    lays = [{"W1": torch.zeros(E, 128, d), "W_r": torch.zeros(E, d)} for _ in range(2)]
+    cal = layer.calibrate_stack([lays[0], dense, lays[1]], torch.zeros(N, d, dtype=bf), 2, 1)
+    assert seen["tables"] == ["tables"] * 2 and seen["layers"][0] is lays[0] and seen["layers"][2] is lays[1]
+    assert seen["layers"][1].T_max == N and torch.equal(seen["layers"][1].W1, dense.W1)
+    assert len(seen["hs"]) == len(seen["xs"]) == 4 and seen["logits"][1] is None
+    lg = cal["logits"]
+    assert lg.shape == (2, N, E) and [t.data_ptr() for t in (seen["logits"][0], seen["logits"][2])] == [t.data_ptr() for t in lg]
+    assert [(w is l["W_r"]) for (w, _), l in zip(seen["sim"], lays)] == [True, True]
+    assert seen["sim"][0][1] is seen["xs"][0] and seen["sim"][1][1] is seen["xs"][2]
+    assert seen["trans"][0] is lg and seen["trans"][1][:3] == (N, 2, E)
+    assert cal["sim"].shape == (2, E, E) and cal["P"].shape == (1, E, E)
+    with pytest.raises(ValueError):
+        layer.calibrate_stack([dense], torch.zeros(N, d, dtype=bf), 2, 1)
+
+
 def kernel(path, name):
     text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
     start = text.index("{", text.index(name + "("))

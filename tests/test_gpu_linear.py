@@ -12,9 +12,11 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 from paper_2607_17154_gb300 import binding as B
 from paper_2607_17154_gb300 import synth
 from paper_2607_17154_gb300.layer import DenseFFN, LayerStack, exact_tables
+from paper_2607_17154_gb300.layer import build_tables, calibrate_stack
 
 pytestmark = pytest.mark.gpu
 
@@ -334,6 +336,63 @@ def test_stack_of_dense_layers_alone(few):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(u, v) for u, v in zip(hs, want))
+
+
+@pytest.mark.parametrize("kinds", ["MDMDM", "DMM", "MD", "DMDDMD"])
+def test_a_stack_with_dense_layers_is_calibrated(kinds):
+    """Similarities, counts and transitions are those of the MoE layers, from each one's own inputs, in the
+    order of LayerStack's tables and P; then the stack runs with them and looks ahead."""
+    d, E, k, dff, M, N = 512, 8, 2, 256, 2, 700
+    layers = []
+    for l, kind in enumerate(kinds):
+        W1, W3, W2 = synth.ffn_weights(E, d, dff, 200 * l, device=DEV)
+        layers.append(DenseFFN(W1[0], W2[0], 4) if kind == "D" else
+                      {"W_r": synth.router_weights(E, d, 2, l, device=DEV), "W1": W1, "W3": W3, "W2": W2})
+    moe = [l for l, kind in enumerate(kinds) if kind == "M"]
+    L = len(moe)
+    cal = calibrate_stack(layers, synth.calibration(N, d, 7, device=DEV), k, M)
+    torch.cuda.synchronize()
+    assert len(cal["hs"]) == len(cal["xs"]) == len(kinds) + 1
+    assert cal["sim"].shape == (L, E, E) and cal["counts"].shape == (L, E) and cal["logits"].shape == (L, N, E)
+    assert cal["P"].shape == cal["tcount"].shape == (L - 1, E, E)
+    logits = cal["logits"].cpu().numpy()
+    for i, l in enumerate(moe):
+        x, Wr = cal["xs"][l], layers[l]["W_r"]
+        ref, mag = x.double() @ Wr.double().T, x.double().abs() @ Wr.double().abs().T
+        assert ((cal["logits"][i].double() - ref).abs() <= (d + 8) * 2.0 ** -23 * mag).all()
+        o_sim = oracle.similarity(synth.bits(Wr), synth.bits(x))
+        np.testing.assert_allclose(cal["sim"][i].cpu().numpy(), o_sim, atol=2e-5)
+        assert cal["counts"][i].sum() == N * k
+    for l, kind in enumerate(kinds):
+        if kind == "D":  # it ran, in its place
+            x, W1, W2 = cal["xs"][l].double(), layers[l].W1.double(), layers[l].W2.double()
+            y = torch.relu(x @ W1.T) @ W2.T
+            want = cal["hs"][l].double() + y
+            assert (cal["hs"][l + 1].double() - want).norm() <= 2.0 ** -8 * (want.norm() + 4 * y.norm())
+    if L > 1:
+        ref_c, ref_P = oracle.transitions(np.ascontiguousarray(logits.transpose(1, 0, 2)), k)
+        np.testing.assert_array_equal(cal["tcount"].cpu().numpy(), ref_c)
+        np.testing.assert_array_equal(cal["P"].cpu().numpy().view(np.uint32), ref_P.view(np.uint32))
+    # the plan's tables from these similarities, and two steps with the horizon that P allows
+    stride = B.ordermoe_tables_bytes(E, M)
+    tabs = torch.zeros(L * stride, dtype=torch.uint8, device=DEV)
+    place = np.zeros((M, E), np.uint8)
+    place[np.arange(E) % M, np.arange(E)] = 1
+    for i in range(L):
+        build_tables(cal["sim"][i], (np.arange(E) // 4).astype(np.int32), place, 0.1, 0.3,
+                     synth.server_params(M, d, dff, 0), DEV, out=tabs[i * stride:(i + 1) * stride])
+    T = 4
+    home = torch.as_tensor(synth.homes(T, M, 1)).to(DEV)
+    out = []
+    for few in (False, True):
+        st = LayerStack(layers, tabs, k, T, DEV, H=3, stride=stride, P=cal["P"], few=few)
+        hs = [cal["hs"][0][:T].clone()] + [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in kinds]
+        xs = [torch.zeros(T, d, dtype=torch.bfloat16, device=DEV) for _ in range(len(kinds) + 1)]
+        st.step_residual(hs, xs, home, home.clone(), torch.zeros(T, device=DEV))
+        torch.cuda.synchronize()
+        out.append(hs)
+    for l, (u, v) in enumerate(zip(*out)):  # as test_stack_of_few_tokens: 2^-8 of H, Y, h a layer
+        assert (u.double() - v.double()).norm() <= 4 * 2.0 ** -8 * max(l, 1) * u.double().norm()
 
 
 def test_short_products_behind_long_ones_on_two_streams():
