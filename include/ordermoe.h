@@ -270,6 +270,15 @@ int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t l
                     const uint16_t* bias, int act, const uint16_t* residual, int64_t ldr, int M,
                     int N, int K, void* Y, int64_t ldy, int f32, ordermoe_stream_t stream);
 
+/* For tests: the kernel and the tiles that ordermoe_linear takes for a product's sizes. Host only; M, N, K
+ * as there, M > 0.
+ *   device [4] host: SMs, CTA pairs resident at once, clusters of two pairs, of four. NULL: the current
+ *          device's
+ *   plan   [8] host out: kernel (0 K split over CTAs, 1 CTA pairs, 2 pairs that share K), rows and columns
+ *          of a tile, row tiles, column tiles, CTAs (0) or pairs (2) that share a tile's K, stages of the
+ *          ring (0; else 0), CTAs */
+int ordermoe_selftest_linear_plan(int M, int N, int K, int f32, const int32_t* device, int32_t* plan);
+
 /* ------------------------------------------------------------------------
  * Weighted combine: y[t] = bf16( sum_{j=0..k-1} topk_w[t][j] * Y_perm[row_of[t][j]] )
  * with fp32 accumulation in slot order.

@@ -69,6 +69,7 @@ _SIGNATURES = {
     "ordermoe_combine_residual_norm": ([_P, _P, _P, _P, _I, _I, _I, _F, _P, _P, _P], _I),
     "ordermoe_layer_forward_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P], _I),
     "ordermoe_linear": ([_P, _I64, _P, _I64, _P, _I, _P, _I64, _I, _I, _I, _P, _I64, _I, _P], _I),
+    "ordermoe_selftest_linear_plan": ([_I, _I, _I, _I, _P, _P], _I),
     "ordermoe_layer_few_workspace_bytes": ([_I, _I, _I, _I, _I], _SZ),
     "ordermoe_layer_few_init": ([_P, _SZ, _P], _I),
     "ordermoe_layer_few": ([_P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
@@ -514,6 +515,19 @@ def ordermoe_linear(X, W, Y, bias=None, act="none", residual=None, stream=None):
                                Y.dtype == torch.float32, _raw_stream(stream))
     if rc != OK:
         _check("ordermoe_linear", rc)
+
+
+LINEAR_KERNELS = ("split", "pair", "pair_split")
+
+
+def ordermoe_selftest_linear_plan(M, N, K, f32=False, device=None):
+    """The kernel and tiles of a product: a dict. device: (SMs, resident CTA pairs, clusters of two pairs,
+    of four); None: the current one."""
+    plan = (_I * 8)()
+    _check("ordermoe_selftest_linear_plan", lib().ordermoe_selftest_linear_plan(
+        M, N, K, bool(f32), None if device is None else (_I * 4)(*device), plan))
+    names = ("kernel", "rows", "cols", "row_tiles", "col_tiles", "split", "stages", "grid")
+    return dict(zip(names, plan), kernel=LINEAR_KERNELS[plan[0]])
 
 
 def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):

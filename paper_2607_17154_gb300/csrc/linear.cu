@@ -961,129 +961,224 @@ static void cluster_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute* attr, i
 
 // CTA pairs that can be resident at once: the persistent grid never exceeds them.
 static int linear_resident_pairs() {
-  static PerDevice cache;
-  return per_device(cache, [] {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[2];
-    cluster_config(cfg, attr, 2, nullptr);
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3(2 * (num_sms() / 2), 1, 1);
-    cfg.blockDim = dim3(ln::P_THREADS, 1, 1);
-    cfg.dynamicSmemBytes = ln::P_SMEM;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_kernel<false>, &cfg) != cudaSuccess || n <= 0) {
-      cudaGetLastError();
-      n = num_sms() / 2;
-    }
-    return n < num_sms() / 2 ? n : num_sms() / 2;
-  });
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cluster_config(cfg, attr, 2, nullptr);
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(2 * (num_sms() / 2), 1, 1);
+  cfg.blockDim = dim3(ln::P_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = ln::P_SMEM;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_kernel<false>, &cfg) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    n = num_sms() / 2;
+  }
+  return n < num_sms() / 2 ? n : num_sms() / 2;
 }
 
 // Clusters of `pairs` (2 or 4) pairs that can be resident at once: a cluster stays within a GPC.
 static int linear_resident_clusters(int pairs) {
-  static PerDevice cache[2];
-  return per_device(cache[pairs / 4], [pairs] {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[2];
-    cluster_config(cfg, attr, 2 * pairs, nullptr);
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3(num_sms() / (2 * pairs) * (2 * pairs), 1, 1);
-    cfg.blockDim = dim3(ln::Q_THREADS, 1, 1);
-    cfg.dynamicSmemBytes = ln::Q_SMEM;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_split_kernel, &cfg) != cudaSuccess || n < 0) {
-      cudaGetLastError();
-      n = 0;
-    }
-    return n;
-  });
-}
-
-static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, int M, int N, int K,
-                         const ln::Epilogue& e, cudaStream_t stream) {
-  using namespace ln;
-  static PerDevice cache;
-  const cudaError_t ae = static_cast<cudaError_t>(per_device(cache, [] {
-    const cudaError_t x = linear_attr<false>();
-    return static_cast<int>(x == cudaSuccess ? linear_attr<true>() : x);
-  }));
-  if (ae != cudaSuccess) return cuda_fail(ae, "cudaFuncSetAttribute(linear)");
-  const int kblocks = (K + BK - 1) / BK;
-  auto div_up = [](long long x, long long y) { return (x + y - 1) / y; };
-  CUtensorMap mW, mX;
-  int rc;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
-  const int sms_now = num_sms();
+  cluster_config(cfg, attr, 2 * pairs, nullptr);
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(num_sms() / (2 * pairs) * (2 * pairs), 1, 1);
+  cfg.blockDim = dim3(ln::Q_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = ln::Q_SMEM;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, ln::linear_pair_split_kernel, &cfg) != cudaSuccess || n < 0) {
+    cudaGetLastError();
+    n = 0;
+  }
+  return n;
+}
+
+// What the choice of a kernel asks of a device: its SMs, and how many CTA pairs, clusters of two pairs and
+// clusters of four are resident at once.
+struct LinearDevice {
+  int sms, pairs, clusters[2];
+};
+
+// The current device's, and the kernels' limits of shared memory: once per device (beyond the 64 that
+// PerDevice keeps, at every call).
+static cudaError_t linear_device(LinearDevice& dev) {
+  static PerDevice cache;
+  static LinearDevice devices[64];
+  auto count = [](LinearDevice& to) {
+    cudaError_t e = linear_attr<false>();
+    if (e == cudaSuccess) e = linear_attr<true>();
+    if (e == cudaSuccess)
+      to = {num_sms(), linear_resident_pairs(), {linear_resident_clusters(2), linear_resident_clusters(4)}};
+    return e;
+  };
+  int id = 0;
+  const cudaError_t e = cudaGetDevice(&id);
+  if (e != cudaSuccess) return e;
+  if (id < 0 || id >= 64) return count(dev);
+  const cudaError_t a =
+      static_cast<cudaError_t>(per_device(cache, [&] { return static_cast<int>(count(devices[id])); }));
+  if (a == cudaSuccess) dev = devices[id];  // (written before per_device returned)
+  return a;
+}
+
+enum { LINEAR_SPLIT = 0, LINEAR_PAIR = 1, LINEAR_PAIR_SPLIT = 2 };
+struct LinearPlan {
+  int kernel;
+  int rows, cols;  // of a tile
+  int row_tiles, col_tiles;
+  int split;       // CTAs (LINEAR_SPLIT) or pairs (LINEAR_PAIR_SPLIT) that share a tile's K
+  int stages, x_rows, tmem_cols, smem;  // LINEAR_SPLIT
+  int grid;
+};
+
+static long long div_up(long long x, long long y) { return (x + y - 1) / y; }
+
+// The kernel of a product and its tiles; on the host alone. false: more tiles than 32 bits count.
+static bool linear_plan(int M, int N, int K, bool f32, const LinearDevice& dev, LinearPlan& p) {
+  using namespace ln;
+  const int kblocks = static_cast<int>(div_up(K, BK));
   const long long p_tiles = div_up(M, 256) * div_up(N, 256);
   // pairs that share K: as many tiles as all clusters take at once, on most of the pairs
-  if (!e.f32 && p_tiles < kLinearPairTiles && M >= kPairSplitRows &&
+  if (!f32 && p_tiles < kLinearPairTiles && M >= kPairSplitRows &&
       kblocks >= (p_tiles < kLinearPairLeast ? kPairSplitBlocks : kPairSplitLong))
     for (int pairs = 2; pairs <= Q_MAX_PAIRS; pairs *= 2) {
-      const long long ct = div_up(N, 256), cap = linear_resident_clusters(pairs);
+      const long long ct = div_up(N, 256), cap = dev.clusters[pairs / 4];
       long long rt = cap / ct;  // row tiles of at most 256 rows and at least 64
       if (rt > div_up(M, 64)) rt = div_up(M, 64);
-      if (rt < div_up(M, 256) || rt * ct * pairs * 4 < 3ll * (sms_now / 2)) continue;
-      PairSplitArgs a{};
-      a.e = e;
-      a.rows = static_cast<int>(div_up(div_up(M, rt), 32) * 32);
-      a.row_tiles = static_cast<int>(div_up(M, a.rows));
-      a.kblocks = kblocks;
-      a.pairs = pairs;
-      a.limit_ns = wait_limit_ns();
-      if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
-      if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
-      cluster_config(cfg, attr, 2 * pairs, stream);
-      cfg.gridDim = dim3(static_cast<unsigned>(a.row_tiles * ct * 2 * pairs), 1, 1);
-      cfg.blockDim = dim3(Q_THREADS, 1, 1);
-      cfg.dynamicSmemBytes = Q_SMEM;
-      const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
-      if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
-      OM_LAUNCHED("linear_pair_split_kernel");
-      return ORDERMOE_OK;
+      if (rt < div_up(M, 256) || rt * ct * pairs * 4 < 3ll * (dev.sms / 2)) continue;
+      p.kernel = LINEAR_PAIR_SPLIT;
+      p.rows = static_cast<int>(div_up(div_up(M, rt), 32) * 32);
+      p.cols = 256;
+      p.row_tiles = static_cast<int>(div_up(M, p.rows));
+      p.col_tiles = static_cast<int>(ct);
+      p.split = pairs;
+      p.grid = p.row_tiles * p.col_tiles * 2 * pairs;
+      return true;
     }
   // pairs: even row tiles of at most 256 rows
   if (M >= kLinearPairRows &&
       (p_tiles >= kLinearPairTiles ||
        (p_tiles >= kLinearPairLeast && (M >= kPairSplitRows || kblocks <= kLinearPairShort)))) {
-    PairArgs a{};
-    a.e = e;
+    p.kernel = LINEAR_PAIR;
     // Row tiles of 128 to 256 rows, by the rounds over the pairs that they take. A K block of a tile takes
     // the longer of its products, as rows, and its loads, 0.8 of (128 + rows / 2) (256 rows 66 us a round of
     // K = 14336, 192 51, 160 42, 128 40, 96 37). 4096 x 14336, in tiles of up to 256 rows / by this rule: 768
     // rows 68.1 / 55.9, 1500 rows 132 / 106, 2500 rows 204 / 166, 4096 rows 284 / 265; 512 rows of 5632 x
     // 2048 16.8 / 14.2. A gain of less than 3 % is left to the larger tiles, which load less.
-    const int most = linear_resident_pairs();
+    const int most = dev.pairs;
     long long best = INT64_MAX;
-    for (int rows = e.f32 ? F32_PAIR_ROWS : 256; rows >= 128; rows -= 32) {
+    for (int rows = f32 ? F32_PAIR_ROWS : 256; rows >= 128; rows -= 32) {
       const long long rt = div_up(M, rows), even = div_up(div_up(M, rt), 32) * 32, loads = 102 + even * 2 / 5;
       const long long cost = div_up(rt * div_up(N, 256), most) * (even > loads ? even : loads);
       if (best == INT64_MAX || cost * 100 < best * 97) {
         best = cost;
-        a.rows = static_cast<int>(even);
+        p.rows = static_cast<int>(even);
       }
     }
-    a.row_tiles = static_cast<int>(div_up(M, a.rows));
-    a.cols = 256;
+    p.row_tiles = static_cast<int>(div_up(M, p.rows));
+    p.cols = 256;
     // One or two row tiles are bound by the weights' bytes: tiles as narrow as the same number of rounds
     // allows, so that every pair loads the same share (32003 x 2048: 64 rows 29.2 -> 28.7 us, 128 32.9 -> 31.2,
     // 256 39.9 -> 38.2, 512 57.9 -> 55.2; 14336 x 4096, 64 rows 26.5 -> 25.8). From three on, X's rows loaded
     // once more a column tile cost more (4096 x 14336: 768 rows 70.3 -> 72.9, 1021 72.9 -> 75.8).
-    if (a.row_tiles <= 2) {
-      const long long rounds = div_up(a.row_tiles * div_up(N, 256), most);
-      const long long even = div_up(div_up((long long)N * a.row_tiles, rounds * most), 16) * 16;
-      if (even < 256 && a.row_tiles * div_up(N, even) <= rounds * most) a.cols = static_cast<int>(even);
+    if (p.row_tiles <= 2) {
+      const long long rounds = div_up(p.row_tiles * div_up(N, 256), most);
+      const long long even = div_up(div_up((long long)N * p.row_tiles, rounds * most), 16) * 16;
+      if (even < 256 && p.row_tiles * div_up(N, even) <= rounds * most) p.cols = static_cast<int>(even);
     }
-    a.col_tiles = static_cast<int>(div_up(N, a.cols));
-    a.kblocks = kblocks;
+    p.col_tiles = static_cast<int>(div_up(N, p.cols));
+    p.split = 1;
+    if ((long long)p.row_tiles * p.col_tiles > INT32_MAX / 2) return false;
+    const int tiles = p.row_tiles * p.col_tiles;
+    p.grid = 2 * (tiles < most ? tiles : most);
+    return true;
+  }
+  p.kernel = LINEAR_SPLIT;
+  // Row tiles of 32 rows and more, as many as leave each tile four CTAs (or what K has for them) of two an
+  // SM: the sums that a CTA exchanges and finishes are fewer (tiles of up to 128 rows / these, us:
+  // 128 x 1024 x 2048 9.3 / 7.2, 128 x 2048 x 2048 9.3 / 7.7, 301 x 1009 x 1999 11.8 / 10.3, 64 x
+  // 4096 x 4096 12.4 / 11.8, 1000 x 512 x 512 9.3 / 6.7). Without the four it loses (33 x 5632 x 2048 in
+  // two row tiles 11.8 for 9.8).
+  int want = 1;
+  while (want < 4 && kblocks / (want * 2) >= 4) want *= 2;
+  long long rt = 2ll * dev.sms / (div_up(N, 128) * want);
+  if (rt > div_up(M, 32)) rt = div_up(M, 32);
+  if (rt < div_up(M, f32 ? F32_ROWS : 128)) rt = div_up(M, f32 ? F32_ROWS : 128);
+  p.rows = static_cast<int>(div_up(div_up(M, rt), 16) * 16);
+  p.row_tiles = static_cast<int>(div_up(M, p.rows));
+  long long tiles = p.row_tiles * div_up(N, 128);
+  if (p.row_tiles * div_up(N, 80) > INT32_MAX / S_MAX_SPLIT) return false;
+  // K over as many CTAs as two an SM leave room for, four K blocks each at least: two rings hide each
+  // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
+  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4)
+  p.split = 1;
+  while (p.split * 2 <= S_MAX_SPLIT && tiles * p.split * 2 <= 2ll * dev.sms && kblocks / (p.split * 2) >= 4) p.split *= 2;
+  p.cols = 128;
+  if (p.split <= 2 && tiles * p.split > dev.sms && tiles * p.split <= 2ll * dev.sms) {
+    // narrower tiles where that gives every SM two CTAs (1 row, 4096 x 14336: 128 columns 23.7 us,
+    // 96 22.9; 512 rows, 2048 x 5632: 128 25.4, 80 24.6). Wider clusters do not fill the GPCs.
+    const int even = static_cast<int>(div_up(div_up((long long)N * p.row_tiles * p.split, 2 * dev.sms), 16) * 16);
+    p.cols = even < 80 ? 80 : even < 128 ? even : 128;
+    if (p.row_tiles * div_up(N, p.cols) * p.split > 2ll * dev.sms) p.cols = 128;
+    tiles = p.row_tiles * div_up(N, p.cols);
+  }
+  // One CTA an SM takes a ring of most of its shared memory, two half of it each. So do clusters of eight,
+  // which do not fill the GPCs with one an SM (128 CTAs, 1 x 2048 x 8192: 17.1 us and 10.9; 64 rows 20.3 and
+  // 12.5; clusters of four 13.4 and 14.0). Behind the ring what the MMA reads past the last stage's weights.
+  const int stage = (p.cols + p.rows) * BK * 2, over = W_BYTES > stage ? W_BYTES - stage : 0;
+  const int room = (tiles * p.split <= dev.sms && p.split < S_MAX_SPLIT ? 220 * 1024 : 108 * 1024) - over;
+  const int share = (kblocks + p.split - 1) / p.split, need = (p.rows * 512 + stage - 1) / stage;
+  p.stages = room / stage < S_MAX_STAGES ? room / stage : S_MAX_STAGES;
+  if (p.stages > share) p.stages = share > need ? share : need;  // and the sums fit in it
+  p.x_rows = M < p.rows ? M : p.rows;
+  const int acc = p.rows <= 32 ? 32 : p.rows <= 64 ? 64 : 128;
+  p.tmem_cols = f32 ? 2 * acc : acc;  // in turn, or the one of all K
+  static_assert(2 * F32_ROWS <= S_MAX_COLS, "two accumulators");
+  const int smem = p.stages * stage + over + 1024;
+  p.smem = smem < S_MIN_SMEM ? S_MIN_SMEM : smem;
+  p.col_tiles = static_cast<int>(tiles / p.row_tiles);
+  p.grid = static_cast<int>(tiles * p.split);
+  return true;
+}
+
+static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, int M, int N, int K,
+                         const ln::Epilogue& e, cudaStream_t stream) {
+  using namespace ln;
+  LinearDevice dev;
+  const cudaError_t de = linear_device(dev);
+  if (de != cudaSuccess) return cuda_fail(de, "cudaFuncSetAttribute(linear)");
+  LinearPlan p{};
+  if (!linear_plan(M, N, K, e.f32 != 0, dev, p))
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+  const int kblocks = static_cast<int>(div_up(K, BK));
+  CUtensorMap mW, mX;
+  int rc;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.gridDim = dim3(static_cast<unsigned>(p.grid), 1, 1);
+  if (p.kernel == LINEAR_PAIR_SPLIT) {
+    PairSplitArgs a{};
+    a.e = e;
+    a.rows = p.rows; a.row_tiles = p.row_tiles; a.kblocks = kblocks; a.pairs = p.split;
     a.limit_ns = wait_limit_ns();
-    if ((long long)a.row_tiles * a.col_tiles > INT32_MAX / 2)
-      return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
+    if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, 128))) return rc;
+    if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
+    cluster_config(cfg, attr, 2 * a.pairs, stream);
+    cfg.blockDim = dim3(Q_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = Q_SMEM;
+    const cudaError_t ce = cudaLaunchKernelEx(&cfg, linear_pair_split_kernel, mW, mX, a);
+    if (ce != cudaSuccess) return cuda_fail(ce, "linear_pair_split_kernel");
+    OM_LAUNCHED("linear_pair_split_kernel");
+    return ORDERMOE_OK;
+  }
+  if (p.kernel == LINEAR_PAIR) {
+    PairArgs a{};
+    a.e = e;
+    a.rows = p.rows; a.cols = p.cols; a.row_tiles = p.row_tiles; a.col_tiles = p.col_tiles; a.kblocks = kblocks;
+    a.limit_ns = wait_limit_ns();
     if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols / 2))) return rc;
     if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.rows / 2))) return rc;
-    const int tiles = a.row_tiles * a.col_tiles;
     cluster_config(cfg, attr, 2, stream);
-    cfg.gridDim = dim3(2 * (tiles < most ? tiles : most), 1, 1);
     cfg.blockDim = dim3(P_THREADS, 1, 1);
     cfg.dynamicSmemBytes = P_SMEM;
     const cudaError_t ce = e.f32 ? cudaLaunchKernelEx(&cfg, linear_pair_kernel<true>, mW, mX, a)
@@ -1094,57 +1189,14 @@ static int linear_launch(const uint16_t* X, int64_t ldx, const uint16_t* W, int6
   }
   SplitArgs a{};
   a.e = e;
-  // Row tiles of 32 rows and more, as many as leave each tile four CTAs (or what K has for them) of two an
-  // SM: the sums that a CTA exchanges and finishes are fewer (tiles of up to 128 rows / these, us:
-  // 128 x 1024 x 2048 9.3 / 7.2, 128 x 2048 x 2048 9.3 / 7.7, 301 x 1009 x 1999 11.8 / 10.3, 64 x
-  // 4096 x 4096 12.4 / 11.8, 1000 x 512 x 512 9.3 / 6.7). Without the four it loses (33 x 5632 x 2048 in
-  // two row tiles 11.8 for 9.8).
-  int want = 1;
-  while (want < 4 && kblocks / (want * 2) >= 4) want *= 2;
-  long long rt = 2ll * sms_now / (div_up(N, 128) * want);
-  if (rt > div_up(M, 32)) rt = div_up(M, 32);
-  if (rt < div_up(M, e.f32 ? F32_ROWS : 128)) rt = div_up(M, e.f32 ? F32_ROWS : 128);
-  a.rows = static_cast<int>(div_up(div_up(M, rt), 16) * 16);
-  a.row_tiles = static_cast<int>(div_up(M, a.rows));
-  a.kblocks = kblocks;
+  a.rows = p.rows; a.cols = p.cols; a.row_tiles = p.row_tiles; a.x_rows = p.x_rows; a.kblocks = kblocks;
+  a.split = p.split; a.stages = p.stages; a.tmem_cols = p.tmem_cols;
   a.limit_ns = wait_limit_ns();
-  long long tiles = a.row_tiles * div_up(N, 128);
-  if (a.row_tiles * div_up(N, 80) > INT32_MAX / S_MAX_SPLIT)
-    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "linear: sizes too large");
-  // K over as many CTAs as two an SM leave room for, four K blocks each at least: two rings hide each
-  // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
-  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4)
-  const int sms = sms_now;
-  a.split = 1;
-  while (a.split * 2 <= S_MAX_SPLIT && tiles * a.split * 2 <= 2ll * sms && kblocks / (a.split * 2) >= 4) a.split *= 2;
-  a.cols = 128;
-  if (a.split <= 2 && tiles * a.split > sms && tiles * a.split <= 2ll * sms) {
-    // narrower tiles where that gives every SM two CTAs (1 row, 4096 x 14336: 128 columns 23.7 us,
-    // 96 22.9; 512 rows, 2048 x 5632: 128 25.4, 80 24.6). Wider clusters do not fill the GPCs.
-    const int even = static_cast<int>(div_up(div_up((long long)N * a.row_tiles * a.split, 2 * sms), 16) * 16);
-    a.cols = even < 80 ? 80 : even < 128 ? even : 128;
-    if (a.row_tiles * div_up(N, a.cols) * a.split > 2ll * sms) a.cols = 128;
-    tiles = a.row_tiles * div_up(N, a.cols);
-  }
-  // One CTA an SM takes a ring of most of its shared memory, two half of it each. So do clusters of eight,
-  // which do not fill the GPCs with one an SM (128 CTAs, 1 x 2048 x 8192: 17.1 us and 10.9; 64 rows 20.3 and
-  // 12.5; clusters of four 13.4 and 14.0). Behind the ring what the MMA reads past the last stage's weights.
-  const int stage = (a.cols + a.rows) * BK * 2, over = W_BYTES > stage ? W_BYTES - stage : 0;
-  const int room = (tiles * a.split <= sms && a.split < S_MAX_SPLIT ? 220 * 1024 : 108 * 1024) - over;
-  const int share = (kblocks + a.split - 1) / a.split, need = (a.rows * 512 + stage - 1) / stage;
-  a.stages = room / stage < S_MAX_STAGES ? room / stage : S_MAX_STAGES;
-  if (a.stages > share) a.stages = share > need ? share : need;  // and the sums fit in it
-  a.x_rows = M < a.rows ? M : a.rows;
   if ((rc = make_tmap_bf16_ld(&mW, W, N, K, ldw, a.cols))) return rc;
-  const int acc = a.rows <= 32 ? 32 : a.rows <= 64 ? 64 : 128;
-  a.tmem_cols = e.f32 ? 2 * acc : acc;  // in turn, or the one of all K
-  static_assert(2 * F32_ROWS <= S_MAX_COLS, "two accumulators");
   if ((rc = make_tmap_bf16_ld(&mX, X, M, K, ldx, a.x_rows))) return rc;
   cluster_config(cfg, attr, a.split, stream);
-  cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split), 1, 1);
   cfg.blockDim = dim3(S_THREADS, 1, 1);
-  const int smem = a.stages * stage + over + 1024;
-  cfg.dynamicSmemBytes = smem < S_MIN_SMEM ? S_MIN_SMEM : smem;
+  cfg.dynamicSmemBytes = p.smem;
   const cudaError_t ce = e.f32 ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, mW, mX, a)
                                : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, mW, mX, a);
   if (ce != cudaSuccess) return cuda_fail(ce, "linear_split_kernel");
@@ -1185,4 +1237,25 @@ extern "C" int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W
   e.vec_r = ldr % 4 == 0 && r % 8 == 0;
   e.vec_y = ldy % 4 == 0 && y % (f32 ? 16 : 8) == 0;
   return linear_launch(X, ldx, W, ldw, M, N, K, e, stream);
+}
+
+extern "C" int ordermoe_selftest_linear_plan(int M, int N, int K, int f32, const int32_t* device, int32_t* plan) {
+  OM_TRACE();
+  if (M <= 0 || N <= 0 || K <= 0 || !plan)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "selftest_linear_plan: need M, N, K > 0 and a plan");
+  LinearDevice dev;
+  if (device) {
+    dev = {device[0], device[1], {device[2], device[3]}};
+    if (dev.sms < 2 || dev.pairs < 1 || dev.clusters[0] < 0 || dev.clusters[1] < 0)
+      return fail(ORDERMOE_ERR_INVALID_ARG, "selftest_linear_plan: no such device");
+  } else {
+    const cudaError_t e = linear_device(dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(linear)");
+  }
+  LinearPlan p{};
+  if (!linear_plan(M, N, K, f32 != 0, dev, p))
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "selftest_linear_plan: sizes too large");
+  const int32_t v[8] = {p.kernel, p.rows, p.cols, p.row_tiles, p.col_tiles, p.split, p.stages, p.grid};
+  for (int i = 0; i < 8; ++i) plan[i] = v[i];
+  return ORDERMOE_OK;
 }

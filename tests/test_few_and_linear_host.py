@@ -177,6 +177,64 @@ def test_results_in_place_and_sizes_that_linear_refuses(call, code):
     assert rc == code and msg.startswith("linear:"), (call, rc, msg)
 
 
+GB300 = (152, 76, 36, 16)  # SMs, CTA pairs, clusters of two pairs and of four that are resident at once
+
+
+@pytest.mark.parametrize("sizes,kernel,split", [
+    ((1, 4096, 4096), "split", 8), ((33, 5632, 2048), "split", None), ((64, 128, 72), "split", 1),
+    ((200, 8100, 2200), "split", 2), ((64, 12289, 264), "pair", 1), ((300, 4096, 2056), "pair", 1),
+    ((1021, 4096, 14336), "pair", 1), ((690, 768, 2048), "pair_split", 2), ((401, 2003, 2111), "pair_split", 2),
+    ((300, 700, 2048), "pair_split", 4), ((930, 250, 2500), "pair_split", 4), ((513, 2500, 6150), "pair_split", 2)])
+def test_kernels_that_the_product_takes(sizes, kernel, split):
+    p = B.ordermoe_selftest_linear_plan(*sizes, device=GB300)
+    assert p["kernel"] == kernel and (split is None or p["split"] == split), p
+
+
+@pytest.mark.parametrize("device", [GB300, (152, 76, 38, 19), (152, 76, 30, 0), (148, 74, 33, 14), (2, 1, 0, 0)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_tiles_of_the_product(device, f32):
+    """For sizes over the whole range: the tiles cover Y once and no row or column of tiles is empty, a
+    tile's accumulator and sums fit, and the grid is what the kernel's index arithmetic takes."""
+    rng = __import__("random").Random(17)
+    sms, pairs, c2, c4 = device
+    kinds = set()
+    for _ in range(4000):
+        M, n, K = (int(round(a * (b / a) ** rng.random())) for a, b in ((1, 20000), (1, 70000), (1, 40000)))
+        p = B.ordermoe_selftest_linear_plan(M, n, K, f32, device)
+        kinds.add((p["kernel"], p["split"]))
+        blocks = (K + 63) // 64
+        assert (p["row_tiles"] - 1) * p["rows"] < M <= p["row_tiles"] * p["rows"], (M, n, K, p)
+        assert (p["col_tiles"] - 1) * p["cols"] < n <= p["col_tiles"] * p["cols"], (M, n, K, p)
+        tiles = p["row_tiles"] * p["col_tiles"]
+        if p["kernel"] == "split":
+            assert p["rows"] % 16 == 0 and p["rows"] <= (64 if f32 else 128) and p["cols"] % 16 == 0 and 80 <= p["cols"] <= 128
+            assert p["split"] in (1, 2, 4, 8) and p["split"] <= blocks and p["grid"] == tiles * p["split"]
+            stage = (p["rows"] + p["cols"]) * 128  # bytes; the last one's weights are read as 128 rows
+            assert 1 <= p["stages"] <= 12 and p["stages"] * stage >= p["rows"] * 512
+            assert p["stages"] * stage + max(0, 128 * 128 - stage) + 1024 <= 221 * 1024
+        elif p["kernel"] == "pair":
+            assert p["rows"] % 32 == 0 and p["rows"] <= (128 if f32 else 256) and p["cols"] % 16 == 0 and p["cols"] <= 256
+            assert p["grid"] == 2 * min(tiles, pairs) and M >= 64
+        else:
+            assert not f32 and p["rows"] % 32 == 0 and p["rows"] <= 256 and p["cols"] == 256 and M > 256
+            assert p["split"] in (2, 4) and tiles <= (c2 if p["split"] == 2 else c4)
+            assert p["grid"] == 2 * p["split"] * tiles and p["split"] <= blocks
+    if sms > 100:
+        assert {("split", 1), ("split", 2), ("split", 4), ("split", 8), ("pair", 1)} <= kinds
+        assert f32 or ("pair_split", 2) in kinds and (c4 == 0 or ("pair_split", 4) in kinds)
+
+
+def test_linear_plan_refuses():
+    plan = (ctypes.c_int * 8)()
+    call = B.lib().ordermoe_selftest_linear_plan
+    for args in ((0, 1, 1, 0, N, plan), (1, 0, 1, 0, N, plan), (1, 1, 0, 0, N, plan), (1, 1, 1, 0, N, N),
+                 (1, 1, 1, 0, (ctypes.c_int * 4)(1, 1, 0, 0), plan), (1, 1, 1, 0, (ctypes.c_int * 4)(152, 0, 0, 0), plan)):
+        assert call(*args) == ARG
+        assert B.lib().ordermoe_last_error().decode().startswith("selftest_linear_plan:")
+    big = (2 ** 31 - 600, 2 ** 31 - 600, 64, 0, (ctypes.c_int * 4)(*GB300), plan)
+    assert call(*big) == SHAPE
+
+
 def test_linear_of_no_rows():
     assert linear(M=0, X=N, W=N, Y=N)[0] == OK
 

@@ -125,6 +125,7 @@ PAIR_SPLIT = [(300, 4096, 2056), (512, 4000, 2048), (257, 8100, 2200), (333, 299
               (400, 2000, 2048), (257, 5000, 6400)]
 
 
+# (The kernels of the sizes above are what the rules give; the sizes below say theirs and check it.)
 @pytest.mark.parametrize("M,N,K", PAIR_SPLIT)
 def test_pairs_that_share_k(M, N, K):
     X, W = rows(M, K, 1.0, 25), rows(N, K, 0.05, 26)
@@ -136,6 +137,44 @@ def test_pairs_that_share_k(M, N, K):
                       residual=rows(M, N, 1.0, 28, odd=True))
     assert torch.equal(Y, ref)
     check(X, W, torch.empty(M, N, device=DEV))
+
+
+@pytest.mark.parametrize("split,M,N,K", [
+    (2, 690, 768, 2048), (2, 401, 2003, 2111), (2, 999, 1001, 2300), (2, 1021, 517, 4100), (2, 330, 1030, 2304),
+    (2, 513, 2500, 6150), (2, 260, 3900, 6200), (4, 300, 700, 2048), (4, 290, 643, 3000), (4, 930, 250, 2500),
+    (2, 257, 1281, 2057), (4, 320, 600, 2300)])
+def test_pairs_that_share_k_in_clusters(split, M, N, K):
+    """Ragged products of the kernel whose pairs share K, two and four to a cluster: K blocks that the pairs
+    do not share evenly, tiles that end past M and N."""
+    plan = B.ordermoe_selftest_linear_plan(M, N, K)
+    if split == 4 and plan["kernel"] == "split":
+        pytest.skip("fewer than 15 clusters of eight CTAs fit this device: it never takes them")
+    assert (plan["kernel"], plan["split"]) == ("pair_split", split), plan
+    X, W = rows(M, K, 1.0, 25), rows(N, K, 0.05, 26)
+    Y = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    check(X, W, Y)
+    bias, R = rows(1, N, 0.5, 27)[0].contiguous(), rows(M, N, 1.0, 28, odd=True)
+    for act in ("gelu", "silu"):
+        check(X, W, Y, bias, act, R)
+    ref, Z = Y.clone(), R.clone()
+    B.ordermoe_linear(X, W, Z, bias=bias, act="silu", residual=Z)  # in place, and again
+    assert torch.equal(Z, ref)
+    wide = rows(M, N, 1.0, 29, pad=13, odd=True, offset=1)
+    check(X, W, wide, bias, "relu", R)
+    W[:, :] = float("nan")  # no column reads another's weights
+    W[N // 2] = 0.5
+    B.ordermoe_linear(X, W, Y)
+    assert torch.equal(torch.isnan(Y).all(0), torch.arange(N, device=DEV) != N // 2)
+
+
+@pytest.mark.parametrize("kernel,M,N,K", [
+    ("split", 1, 1, 1), ("split", 17, 1000, 520), ("split", 255, 257, 8), ("split", 200, 8100, 2200),
+    ("split", 150, 1280, 2048), ("pair", 300, 4096, 1024), ("pair", 300, 4096, 2056), ("pair", 333, 2999, 4096),
+    ("pair", 1021, 4096, 512), ("pair", 257, 5000, 6400)])
+def test_kernels_of_the_other_sizes(kernel, M, N, K):
+    assert B.ordermoe_selftest_linear_plan(M, N, K)["kernel"] == kernel
+    X, W = rows(M, K, 1.0, 35), rows(N, K, 0.05, 36)
+    check(X, W, torch.empty(M, N, dtype=torch.bfloat16, device=DEV), act="silu", residual=rows(M, N, 1.0, 37))
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
