@@ -5,6 +5,7 @@ import ctypes
 import os
 import re
 
+import numpy as np
 import pytest
 import torch
 
@@ -233,6 +234,30 @@ def test_linear_plan_refuses():
         assert B.lib().ordermoe_last_error().decode().startswith("selftest_linear_plan:")
     big = (2 ** 31 - 600, 2 ** 31 - 600, 64, 0, (ctypes.c_int * 4)(*GB300), plan)
     assert call(*big) == SHAPE
+
+
+def test_bound_of_fp32_results_sees_the_length_of_an_accumulator():
+    """The bound on sums that are truncated as above, on the host: 512 of K a sum within it, all of K not."""
+    from tests.test_gpu_linear import F32_OFF
+    rng = np.random.default_rng(3)
+    for K in (2048, 6400):
+        x, w = (rng.standard_normal((300, K)).astype(np.float32) for _ in range(2))
+        steps = (x.astype(np.float64) * w).reshape(300, K // 16, 16).sum(2)
+        ref = steps.sum(1)
+
+        def trunc(v):
+            f = v.astype(np.float32)
+            return np.where(np.abs(f.astype(np.float64)) > np.abs(v), np.nextafter(f, np.float32(0)), f)
+
+        def off(per):
+            total = np.zeros(300, np.float32)
+            for c in range(0, K // 16, per):
+                acc = np.zeros(300, np.float32)
+                for j in range(c, min(c + per, K // 16)):
+                    acc = trunc(acc.astype(np.float64) + steps[:, j])
+                total = total + acc
+            return np.linalg.norm(total - ref) / np.linalg.norm(ref)
+        assert off(32) <= F32_OFF < off(K // 16)
 
 
 def test_linear_of_no_rows():

@@ -177,6 +177,34 @@ def test_kernels_of_the_other_sizes(kernel, M, N, K):
     check(X, W, torch.empty(M, N, dtype=torch.bfloat16, device=DEV), act="silu", residual=rows(M, N, 1.0, 37))
 
 
+# How far an fp32 result is off in the 2-norm, of random operands. An MMA adds 16 products to a sum and truncates
+# it: half a unit of the last place is lost on average, toward zero; a unit is 0.72 2^-23 of the value (the mean
+# over a binade). After j of the n = 32 MMAs of 512 of K the sum's norm is sqrt(j / n) of what it ends with, and the
+# losses along them add up to 0.36 2^-23 n / sqrt(3) = 6.6 2^-23 of it; from one 512 of K to the next they are
+# independent, as the sums are. Their random part (0.21 2^-23 sqrt(n / 2)) and the additions of the 512s' sums
+# (0.21 2^-23 sqrt(28 / 2) for 28 of them) are 0.8 2^-23 each: 6.8 2^-23 = 8.1e-7 in all, for K up to 14336. One
+# accumulator over K = 2048 loses 0.36 2^-23 128 / sqrt(3) = 3.2e-6.
+F32_OFF = 1e-6
+
+
+@pytest.mark.parametrize("kernel,M,N", [("split", 1, 4096), ("split", 48, 1000), ("split", 130, 700), ("pair", 300, 4100),
+                                        ("pair", 70, 12300)])
+@pytest.mark.parametrize("K", [1000, 2048, 6400, 14336])
+def test_fp32_results_are_fp32_sums(kernel, M, N, K):
+    assert B.ordermoe_selftest_linear_plan(M, N, K, f32=True)["kernel"] == kernel
+    X, W = rows(M, K, 1.0, 45), rows(N, K, 0.05, 46)
+    Y = torch.empty(M, N, device=DEV)
+    B.ordermoe_linear(X, W, Y)
+    v = X.double() @ W.double().T
+    off = (Y.double() - v).norm()
+    assert off <= F32_OFF * v.norm(), float(off / v.norm())
+    bias, R = rows(1, N, 0.5, 47)[0].contiguous(), rows(M, N, 1.0, 48)
+    B.ordermoe_linear(X, W, Y, bias=bias, residual=R)
+    u = v + bias.double()
+    off = (Y.double() - (u + R.double())).norm()
+    assert off <= F32_OFF * v.norm() + 2.0 ** -24 * (u.norm() + (u + R.double()).norm())
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("M,N,K", [(5, 200, 96), (130, 515, 264), (2048, 2048, 128)])
 def test_epilogue(act, M, N, K):
