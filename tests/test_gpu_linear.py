@@ -257,6 +257,34 @@ def test_infinities_and_nan_stay_in_their_rows_and_columns(M):
     assert torch.equal(Z[[0, 2, 3], 9].double(), want[[0, 2, 3]])
 
 
+@pytest.mark.parametrize("kernel,N,K", [("split", 8, 8), ("pair", 4100, 8), ("pair_split", 768, 2048)])
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_tails_of_the_activations(kernel, N, K, f32, act):
+    """Sums of one product (exact) from -105 to 105: an activation's negative tail down to the smallest normal
+    number of either type (2^-126) is as near as any other value. The exponent s is off by 2^-21 |s| (roundings of the
+    cubic or of the square and of the constants: s up to 88) and a bf16 result's fast exponential by (2 + 1.2 |s|) 2^-23 of
+    its value: 2^-14 covers them beside the rounding; SiLU's s in fp32 is exact, 2^-20."""
+    if kernel == "pair_split" and f32:
+        kernel = "pair" if B.ordermoe_selftest_linear_plan(690, N, K, True)["kernel"] == "pair" else "split"
+    v = torch.cat([torch.arange(-105.0, -16.0, 0.5), torch.arange(-16.0, 16.0, 0.0625)])
+    v = torch.cat([v, torch.arange(16.0, 105.5, 0.5)]).to(DEV)
+    v = v[torch.randperm(len(v), generator=torch.Generator().manual_seed(1)).to(DEV)][:690]
+    M = len(v)
+    assert M == 690 and B.ordermoe_selftest_linear_plan(M, N, K, f32)["kernel"] == kernel
+    X, W = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV), torch.zeros(N, K, dtype=torch.bfloat16, device=DEV)
+    X[:, 0], W[:, 0] = v.to(torch.bfloat16), 1.0
+    assert torch.equal(X[:, 0].float(), v)
+    Y = torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    B.ordermoe_linear(X, W, Y, act=act)
+    ref = act64(v.double(), act)[:, None]
+    tol = (2.0 ** -24 if f32 else 2.0 ** -8) + (2.0 ** -20 if f32 and act == "silu" else 2.0 ** -14)
+    normal = (ref.abs() >= 2.0 ** -126).expand(M, N)
+    off = (Y.double() - ref).abs()
+    assert (off <= tol * ref.abs())[normal].all(), (off / ref.abs())[normal].max()
+    assert (Y.double().abs() <= 2.0 ** -125)[~normal].all()
+
+
 def test_extreme_values():
     """Sums beyond bf16's range, tails of the activations, and zeros."""
     X = torch.tensor([[1.0] * 8, [3e38] * 8, [-3e38] * 8, [0.0] * 8], device=DEV).to(torch.bfloat16)
