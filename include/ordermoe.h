@@ -256,9 +256,10 @@ int ordermoe_expert_down(const uint16_t* H, const int32_t* offsets, int R, const
  *   Y [M][N] out, rows ldy apart: bf16, or float when f32 != 0. Y may be the
  *   residual itself (bf16, the same address and stride); it may not overlap
  *   anything else that is read. What lies between its rows is left as it was.
- * Any M >= 0 and N, K > 0, up to 2^31 - 513. Rows of Y and residual that start at a multiple of 8
- * bytes (16 for float) with strides that are multiples of 4 are moved 4
- * elements at a time, others one by one. The sums of a call are in a fixed order. */
+ * Any M >= 0 and N, K > 0, up to 2^31 - 513. With few rows, rows of Y and residual that start at a
+ * multiple of 8 bytes (16 for float) with strides that are multiples of 4 are moved 4
+ * elements at a time, others one by one; with many rows every thread moves one column, whatever
+ * the strides. The sums of a call are in a fixed order. */
 enum {
   ORDERMOE_ACT_NONE = 0,
   ORDERMOE_ACT_RELU = 1,

@@ -12,17 +12,19 @@
 //   linear_pair_kernel: persistent CTA pairs, tiles of up to 256 columns x up to 256 rows with
 //     cta_group::2 MMAs, two accumulators, so that a tile's epilogue overlaps the next tile's
 //     main loop. For batches with a tile for most pairs, bound by the tensor cores (4096 x 14336 x
-//     4096 239 us, 2010 TFLOP/s). Its epilogue is bound by instructions and latency: sixteen
+//     4096 274 us launched from the host or in a long loop of graphs, 1755 TFLOP/s, as a library product
+//     there; 240 in the first few replays, before the chip's power cap). Its epilogue is bound by instructions and latency: sixteen
 //     warps, eight rows of a column at a time from TMEM (eight warps, 32 rows through shared memory:
 //     2048 x 4096 x 4096 with SiLU and residual 87 us for 47).
 //   linear_pair_split_kernel: one tile of 256 columns x up to 256 rows a cluster of 2 or 4 CTA
 //     pairs that share its K, the accumulators added as in the first kernel. For batches in between,
 //     whose tiles are too few for the pairs but whose operands, in tiles of 128 x 128, take
 //     longer from L2 than their products. (Sixteen warps in the epilogue for four: 300 x 4096 x
-//     4096 with residual 22.9 -> 19.0 us.)
-// The tensor cores truncate a running sum, an error that grows with K (2e-6 of the result at K = 2048,
-// against 4e-7 of fp32 FMAs). Where the sums leave in fp32 (F32), the epilogue warps therefore take
-// the accumulator every 512 of K and add it to sums in registers; bf16 results do not see it.
+//     14336 with residual 44.3 -> 38.5 us, 512 x 2048 x 2048 16.2 -> 13.2.)
+// The tensor cores truncate a running sum, an error that grows with K (2e-6 of the result at K = 2048).
+// Where the sums leave in fp32 (F32), the epilogue warps therefore take the accumulator every 512 of K
+// and add it to sums in registers: 4.7e-7 off in the 2-norm at K = 512, 4.8e-7 at 14336 (sums of fp32
+// FMAs 1.6e-7 and 1.4e-6). bf16 results, rounded by 1.7e-3, do not see it.
 // Rows and columns past M, N and K are zero-filled by TMA and not stored. Every wait is bounded; one that
 // runs out reports ORDERMOE_DEV_WAIT_TIMEOUT, and the copies and MMAs under way are drained.
 #include "common.cuh"
@@ -46,7 +48,7 @@ constexpr int BK = 64;                 // K block: 128 bytes a row
 constexpr int W_BYTES = 128 * BK * 2;  // 128 weight rows of a K block
 constexpr int F32_BLOCKS = 8;          // K blocks that an fp32 result's accumulator sums up
 constexpr int F32_ROWS = 64;           // rows of the split kernel's tiles then: sums in 64 registers
-constexpr int F32_PAIR_ROWS = 128;     // and of the pair kernel's, over two groups of warps
+constexpr int F32_PAIR_ROWS = 128;     // and of the pair kernel's, over its groups of epilogue warps
 
 struct Epilogue {
   int M, N;
@@ -87,8 +89,8 @@ __device__ __forceinline__ void activate_all(float (&f)[N], int act) {
   else if (act == ORDERMOE_ACT_SILU) all(std::integral_constant<int, ORDERMOE_ACT_SILU>{});
 }
 
-// Not inlined: the epilogue of a few rows runs once, its instructions come from L2, and five activations a
-// column made it longer (301 x 1009 with SiLU 16.5 us).
+// Not inlined: the epilogue of a few rows runs once and its instructions come from L2, so one copy of the five
+// activations serves all four columns (inlined the same: 301 x 1009 x 1999 with SiLU 9.5 and 9.4 us).
 template <bool FAST>
 __device__ __noinline__ float4 activate4(float4 v, int act) {
   float f[4] = {v.x, v.y, v.z, v.w};
@@ -122,8 +124,8 @@ __device__ __forceinline__ float4 load_residual4(const Epilogue& e, int m, int n
   return make_float4(f[0], f[1], f[2], f[3]);
 }
 
-// The line of the residual's row m that holds column n, into L2 while the sums are made (300 x 4096 x 4096
-// 25.2 -> 23.0 us, 64 rows 12.8 -> 12.4).
+// The line of the residual's row m that holds column n, into L2 while the sums are made (64 x 4096 x 4096
+// 12.9 -> 12.3 us, 300 x 2048 x 2048 12.5 -> 12.0; 300 x 4096 x 14336, whose sums take long, the same).
 __device__ __forceinline__ void prefetch_residual(const Epilogue& e, int m, int n) {
   asm volatile("prefetch.global.L2 [%0];" ::"l"(e.residual + m * e.ldr + n));
 }
@@ -418,7 +420,7 @@ __global__ void __launch_bounds__(S_THREADS, 2)
 }
 
 // ---------------------------------------------------------------- CTA pairs
-constexpr int P_STAGES = 7;  // (six: 300 x 14336 x 4096 39.5 us for 36.8, 64 rows 25.7 for 25.3)
+constexpr int P_STAGES = 7;  // (six: 300 x 14336 x 4096 38.9 us for 36.4, 64 rows 26.3 for 25.6)
 constexpr int P_STAGE_BYTES = 2 * W_BYTES;  // 128 weight rows and up to 128 rows of X a CTA
 constexpr int P_GROUPS = 4;                 // of four epilogue warps, eight rows of a tile in turn
 constexpr int P_THREADS = 64 + 128 * P_GROUPS;
@@ -923,19 +925,20 @@ __global__ void __launch_bounds__(Q_THREADS, 1)
 }  // namespace ln
 
 // The pair kernel takes products of at least kLinearPairRows rows and kLinearPairTiles tiles of
-// 256 x 256 (us, graph replays, bias and residual, K x N, pairs / split kernel: 64 rows, 4096 x 14336 (56
-// tiles) 25.7 / 28.9, 128 rows 28.1 / 35.8, 256 rows 33.6 / 50.0, 768 rows, 4096 x 4096 (48) 27.8 / 41.4);
-// and from kLinearPairLeast of them where the rows are kPairSplitRows or more (512 rows, 5120 x 5120
-// (40) 33.2 / 45.1, 300 rows 24.3 / 28.5) or K is at most kLinearPairShort blocks (64 rows, 1024 x 5120 8.1 / 8.9,
-// 128 rows 10.0 / 13.0, 2048 x 5632 13.6 / 15.4). Else the split kernel, whose CTAs stream the weights faster
-// (128 rows, 13824 x 5120 37.8, pairs 44.8; 64 rows, 4096 x 4096 (16) 12.1, pairs 16.0; 8192 x 2048
-// 12.2, pairs 25.2).
+// 256 x 256 (M x N x K in us, graph replays, bias and residual, pairs / split kernel: 64 x 14336 x 4096 (56
+// tiles) 25.3 / 28.7, 128 rows 27.0 / 35.8, 256 rows 32.4 / 49.7; 768 x 4096 x 4096 (48) 23.4 / 42.2);
+// and from kLinearPairLeast of them where the rows are kPairSplitRows or more (512 x 5120 x 5120
+// (40) 27.0 / 46.2, 300 rows 22.6 / 28.6) or K is at most kLinearPairShort blocks (64 x 5120 x 1024 8.5 / 9.0,
+// 128 rows 10.0 / 12.8; 128 x 5632 x 2048 13.3 / 15.6). Else the split kernel, whose CTAs stream the weights
+// faster (128 x 5120 x 13824 44.5 / 37.4, 128 x 5120 x 5120 21.8 / 21.0; 64 x 4096 x 4096 (16) 16.5 / 12.2, 64 x
+// 2048 x 8192 25.9 / 12.3; at 256 x 5120 x 5120 the pairs would be faster, 22.2 / 27.3).
 constexpr int kLinearPairRows = 64, kLinearPairTiles = 48, kLinearPairLeast = 20, kLinearPairShort = 32;
-// Below kLinearPairTiles, pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks (us, K x N, shared /
-// split kernel: 160 rows, 14336 x 4096 33.6 / 29.6, 256 rows 37.1 / 37.6, 300 rows 37.0 / 46.9, 512 rows 45.3 / 54.5;
-// 512 rows, 2048 x 2048 11.6 / 13.1), and from kPairSplitLong where there are kLinearPairLeast tiles (shared / pairs on
-// their own: 300 rows, 14336 x 4096 36.4 / 45.9, 512 rows 44.0 / 46.6; 384 rows, 4096 x 4096 18.2 / 17.8, 512 rows
-// 20.7 / 18.1; 768 rows, 2048 x 2048 13.3 / 11.6).
+// Below kLinearPairTiles, pairs share K from kPairSplitRows rows and kPairSplitBlocks K blocks (shared / split
+// kernel: 160 x 4096 x 14336 35.1 / 31.4, 256 rows 37.2 / 37.7, 300 rows 38.7 / 51.3, 512 rows 46.7 / 59.8;
+// 256 x 2048 x 2048 11.3 / 11.0, 300 rows 12.3 / 11.9, 512 rows 13.5 / 14.5), and from kPairSplitLong where there are
+// kLinearPairLeast tiles (shared / pairs on their own: 300 x 4096 x 14336 38.9 / 47.2, 512 rows 46.9 / 47.3; 384 x
+// 4096 x 8192 28.8 / 30.7, but 512 rows 33.2 / 30.6, 512 x 4096 x 6144 27.7 / 25.2; 384 x 4096 x 4096 20.1 / 19.3, 512
+// rows 22.7 / 19.4; 768 x 2048 x 2048 15.4 / 13.3).
 constexpr int kPairSplitRows = 257, kPairSplitBlocks = 32, kPairSplitLong = 96;
 
 template <bool F32>
@@ -1064,11 +1067,12 @@ static bool linear_plan(int M, int N, int K, bool f32, const LinearDevice& dev, 
       (p_tiles >= kLinearPairTiles ||
        (p_tiles >= kLinearPairLeast && (M >= kPairSplitRows || kblocks <= kLinearPairShort)))) {
     p.kernel = LINEAR_PAIR;
-    // Row tiles of 128 to 256 rows, by the rounds over the pairs that they take. A K block of a tile takes
-    // the longer of its products, as rows, and its loads, 0.8 of (128 + rows / 2) (256 rows 66 us a round of
-    // K = 14336, 192 51, 160 42, 128 40, 96 37). 4096 x 14336, in tiles of up to 256 rows / by this rule: 768
-    // rows 68.1 / 55.9, 1500 rows 132 / 106, 2500 rows 204 / 166, 4096 rows 284 / 265; 512 rows of 5632 x
-    // 2048 16.8 / 14.2. A gain of less than 3 % is left to the larger tiles, which load less.
+    // Row tiles of 128 to 256 rows, by the rounds over the pairs that they take. A K block of a tile is taken
+    // to cost the longer of its products, as rows, and its loads, 0.8 of (128 + rows / 2). (One round of N = 4096,
+    // K = 14336 with start and epilogue: 256 rows 73 us, 224 67, 192 61, 160 55, 128 51, 96 46.) In tiles of up to
+    // 256 rows / by this rule, N = 4096, K = 14336: 768 rows 70.7 / 57.3, 1500 rows 141 / 110, 2500 rows 220 / 172,
+    // 4096 rows 322 / 285; 512 x 5632 x 2048 20.5 / 17.3. A gain of less than 3 % is left to the larger tiles, which
+    // load less.
     const int most = dev.pairs;
     long long best = INT64_MAX;
     for (int rows = f32 ? F32_PAIR_ROWS : 256; rows >= 128; rows -= 32) {
@@ -1082,9 +1086,9 @@ static bool linear_plan(int M, int N, int K, bool f32, const LinearDevice& dev, 
     p.row_tiles = static_cast<int>(div_up(M, p.rows));
     p.cols = 256;
     // One or two row tiles are bound by the weights' bytes: tiles as narrow as the same number of rounds
-    // allows, so that every pair loads the same share (32003 x 2048: 64 rows 29.2 -> 28.7 us, 128 32.9 -> 31.2,
-    // 256 39.9 -> 38.2, 512 57.9 -> 55.2; 14336 x 4096, 64 rows 26.5 -> 25.8). From three on, X's rows loaded
-    // once more a column tile cost more (4096 x 14336: 768 rows 70.3 -> 72.9, 1021 72.9 -> 75.8).
+    // allows, so that every pair loads the same share (tiles of 256 columns / these: 64 x 32003 x 2048 28.1 / 27.5
+    // us, 128 rows 30.1 / 29.9, 256 rows 35.7 / 35.9, 64 x 14336 x 4096 26.2 / 26.2). From three on, X's rows
+    // loaded once more a column tile cost more (768 x 4096 x 14336 57.6 / 60.5, 1021 rows 81.5 / 83.3).
     if (p.row_tiles <= 2) {
       const long long rounds = div_up(p.row_tiles * div_up(N, 256), most);
       const long long even = div_up(div_up((long long)N * p.row_tiles, rounds * most), 16) * 16;
@@ -1100,9 +1104,9 @@ static bool linear_plan(int M, int N, int K, bool f32, const LinearDevice& dev, 
   p.kernel = LINEAR_SPLIT;
   // Row tiles of 32 rows and more, as many as leave each tile four CTAs (or what K has for them) of two an
   // SM: the sums that a CTA exchanges and finishes are fewer (tiles of up to 128 rows / these, us:
-  // 128 x 1024 x 2048 9.3 / 7.2, 128 x 2048 x 2048 9.3 / 7.7, 301 x 1009 x 1999 11.8 / 10.3, 64 x
-  // 4096 x 4096 12.4 / 11.8, 1000 x 512 x 512 9.3 / 6.7). Without the four it loses (33 x 5632 x 2048 in
-  // two row tiles 11.8 for 9.8).
+  // 128 x 1024 x 2048 10.3 / 8.1, 128 x 2048 x 2048 10.9 / 9.0, 301 x 1009 x 1999 10.8 / 9.0, 64 x
+  // 4096 x 4096 13.1 / 12.3, 1000 x 512 x 512 11.0 / 7.5). Without the four it loses (33 x 5632 x 2048 in
+  // two row tiles 11.7 for 11.0).
   int want = 1;
   while (want < 4 && kblocks / (want * 2) >= 4) want *= 2;
   long long rt = 2ll * dev.sms / (div_up(N, 128) * want);
@@ -1113,22 +1117,23 @@ static bool linear_plan(int M, int N, int K, bool f32, const LinearDevice& dev, 
   long long tiles = p.row_tiles * div_up(N, 128);
   if (p.row_tiles * div_up(N, 80) > INT32_MAX / S_MAX_SPLIT) return false;
   // K over as many CTAs as two an SM leave room for, four K blocks each at least: two rings hide each
-  // other's latency (1 row, 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.5, 12.4, 10.6, 10.3 us;
-  // 14336 x 4096: 51.9, 29.7, 24.0, 23.4)
+  // other's latency (1 x 4096 x 4096: 1, 2, 4, 8 CTAs a tile 18.0, 12.4, 11.3, 11.0 us;
+  // 1 x 4096 x 14336: 48.6, 28.7, 24.7, 23.9)
   p.split = 1;
   while (p.split * 2 <= S_MAX_SPLIT && tiles * p.split * 2 <= 2ll * dev.sms && kblocks / (p.split * 2) >= 4) p.split *= 2;
   p.cols = 128;
   if (p.split <= 2 && tiles * p.split > dev.sms && tiles * p.split <= 2ll * dev.sms) {
-    // narrower tiles where that gives every SM two CTAs (1 row, 4096 x 14336: 128 columns 23.7 us,
-    // 96 22.9; 512 rows, 2048 x 5632: 128 25.4, 80 24.6). Wider clusters do not fill the GPCs.
+    // narrower tiles where that gives every SM two CTAs (1 x 14336 x 4096: 128 columns 24.1 us, 96 23.7;
+    // 128 x 10000 x 4096: 128 29.8, 80 28.6; 200 x 8100 x 2200: 128 26.9, 112 26.0). Wider clusters do not fill
+    // the GPCs.
     const int even = static_cast<int>(div_up(div_up((long long)N * p.row_tiles * p.split, 2 * dev.sms), 16) * 16);
     p.cols = even < 80 ? 80 : even < 128 ? even : 128;
     if (p.row_tiles * div_up(N, p.cols) * p.split > 2ll * dev.sms) p.cols = 128;
     tiles = p.row_tiles * div_up(N, p.cols);
   }
   // One CTA an SM takes a ring of most of its shared memory, two half of it each. So do clusters of eight,
-  // which do not fill the GPCs with one an SM (128 CTAs, 1 x 2048 x 8192: 17.1 us and 10.9; 64 rows 20.3 and
-  // 12.5; clusters of four 13.4 and 14.0). Behind the ring what the MMA reads past the last stage's weights.
+  // which do not fill the GPCs with one an SM (128 CTAs, 1 x 2048 x 8192: 18.0 us, two an SM 11.0, clusters of
+  // four 12.6). Behind the ring what the MMA reads past the last stage's weights.
   const int stage = (p.cols + p.rows) * BK * 2, over = W_BYTES > stage ? W_BYTES - stage : 0;
   const int room = (tiles * p.split <= dev.sms && p.split < S_MAX_SPLIT ? 220 * 1024 : 108 * 1024) - over;
   const int share = (kblocks + p.split - 1) / p.split, need = (p.rows * 512 + stage - 1) / stage;

@@ -204,7 +204,10 @@ class LayerStack:
         per-layer device buffers, or (for look-ahead, H > 1) one device buffer
         holding all layers' tables `stride` bytes apart; P [L-1, E, E] the
         transition matrices. Layer l looks min(H, L - l) - 1 layers ahead. few: steps of at most
-        B.FEW_TOKENS tokens run each MoE layer in one launch (ordermoe_layer_few). A
+        B.FEW_TOKENS tokens run each MoE layer in one launch (ordermoe_layer_few). Myopic steps
+        of 1 to 8 tokens gain by it (64 narrow experts, us a layer: 1 token 50 -> 39, 8 tokens 125 ->
+        113), 16 tokens do not (168 -> 173); with H = 3, whose decisions keep launches of their own, only
+        wide experts do (1 token 148 -> 144; 64 narrow experts 104 -> 107, 16 tokens 227 -> 243). A
         DenseFFN in `layers` runs in its place; tables, P and L then count the MoE layers
         alone, in order (a stack may have none: tables, k, P and few say nothing then)."""
         dense = {l: lay for l, lay in enumerate(layers) if isinstance(lay, DenseFFN)}
