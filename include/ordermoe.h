@@ -281,6 +281,124 @@ int ordermoe_linear(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t l
 int ordermoe_selftest_linear_plan(int M, int N, int K, int f32, const int32_t* device, int32_t* plan);
 
 /* ------------------------------------------------------------------------
+ * The attention half of a decoder block that serves a batch of requests: a paged
+ * cache of keys and values, attention of one new token a request over it, and
+ * its cut to a budget of slots. The paper's servers hold decoder models
+ * (Section VI-A) and give no attention of their own; these calls are the
+ * usual softmax attention, softmax(scale q K^T) V, with query heads in groups that share
+ * a head of the cache.
+ *
+ * A cache (the descriptor is host memory, its pointers are device memory of the caller):
+ *   k, v    [pages][heads][page][dim] bf16, 16-byte aligned. dim 64, 128 or 256; page (slots of a page) a
+ *           power of two, at most 1024; at most 1024 heads
+ *   table   [seqs][seq_pages] i32, rows ld_table apart: slot i of sequence s is row i % page of page
+ *           table[s][i / page]. Entries behind a sequence's length are not read. At most 65535 sequences,
+ *           2^30 slots each
+ *   length  [seqs] i32 slots held, each 0 to seq_pages * page
+ *   mass    [seqs][heads][seq_pages * page] f32, nullable: the weight that a slot has received
+ *   pos     the same shape, i32, nullable: the position of a slot's token (slots need not be in the order of
+ *           positions once a cache was cut). Without it slot numbers count as positions
+ * Sequences may share pages that no call writes to (a common prompt). A slot that is written (append, evict)
+ * belongs to one sequence.
+ * A length outside its range, or a page outside [0, pages) that a call needs, sets ORDERMOE_DEV_BAD_INDEX (detail:
+ * the sequence, for append the token): the length is taken as the nearest one inside, what such a page holds as
+ * zeros, and what would go there is not written. */
+typedef struct {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t pages;
+  int page, heads, dim;
+  int seqs, seq_pages;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* length;
+  float* mass;
+  int32_t* pos;
+} ordermoe_cache;
+
+/* New tokens' keys and values into the cache, with rotary positions: the pairs (a, b) of a head of k and q turn
+ * by the angle position * inv_freq[i] to (a cos - b sin, a sin + b cos); v is copied.
+ *   k, v     [T][heads * dim] bf16, rows ldk, ldv apart; q [T][q_heads * dim] and q_out, rows ldq, ldqo apart,
+ *            both nullable, q_out may be q (same stride). Row strides are multiples of 8 and every base is 16-byte
+ *            aligned (parts of one product's rows, say)
+ *   starts   [seqs + 1] i32, ascending from 0: tokens starts[s] to starts[s + 1] - 1 are sequence s's newest ones, in
+ *            slots length[s] - (starts[s + 1] - starts[s]) and on: length counts them already. Tokens from
+ *            starts[seqs] on are padding: nothing of them is read or written. NULL: one token a sequence, T = seqs
+ *   position [T] i32, nullable (the slot)
+ *   inv_freq [rot_dim / 2] f64 radians a position; pair i is (i, i + rot_dim / 2), or (2 i, 2 i + 1) when adjacent
+ *            != 0. rot_dim: a multiple of 16, at most dim; what is behind it is copied. 0: nothing turns
+ * The angle is reduced in 64 bits, the turn is done in fp32 and rounded once. A cache's pos takes the position
+ * and its mass 0 for every head. A token whose slot or page does not exist is reported and left out (its q_out too). */
+int ordermoe_cache_append(const ordermoe_cache* cache, const uint16_t* k, int64_t ldk,
+                          const uint16_t* v, int64_t ldv, const uint16_t* q, int64_t ldq,
+                          uint16_t* q_out, int64_t ldqo, int T, int q_heads, const int32_t* starts,
+                          const int32_t* position, const double* inv_freq, int rot_dim, int adjacent,
+                          ordermoe_stream_t stream);
+
+/* Attention of one query a sequence over its slots: for query head j, which reads head j / (q_heads / heads),
+ *   x_i = scale <q_j, k_i>, i < length;  out_j = sum_i p_i v_i, p = softmax(x);  lse_j = log sum_i exp(x_i).
+ *   q, out   [seqs][q_heads * dim] bf16, rows ldq, ldo apart (multiples of 8, 16-byte aligned bases); q_heads is a
+ *            multiple of heads. out may be q itself (same stride)
+ *   lse      [seqs][q_heads] f32, nullable
+ *   weights  != 0: mass[s][h][i] += the sum of p_i over the query heads of head h
+ *   workspace  device scratch of ordermoe_attention_paged_workspace_bytes(...) bytes, 256-byte aligned, not to be
+ *            prepared; calls that may overlap on the GPU need one each
+ * Statistics and sums in fp32, p in two bf16 parts (16 bits), one rounding to out. A sequence with no slot, or whose
+ * every x is -inf, gets out = 0 and lse = -inf. Slots at and behind the length are not read into a result, whatever they
+ * hold. The work is cut evenly over the GPU by the lengths on the device: the same lengths and table
+ * sizes give the same bits, and a captured call follows lengths that change between replays. */
+size_t ordermoe_attention_paged_workspace_bytes(int seqs, int q_heads, int heads, int dim,
+                                                int64_t seq_slots, int weights);
+int ordermoe_attention_paged(const ordermoe_cache* cache, const uint16_t* q, int64_t ldq, int q_heads,
+                             float scale, uint16_t* out, int64_t ldo, float* lse, int weights,
+                             void* workspace, size_t workspace_bytes, ordermoe_stream_t stream);
+
+/* Cuts every head of sequences with more than `budget` slots to that many. Protected tokens stay first (those of
+ * positions below `sinks` and above newest[s] - recent), then the largest mass; ties go to the lower slot (NaN counts as
+ * 0). Kept slots behind the budget move, in ascending order, into the freed slots below it, with their rows of k and v,
+ * mass and pos; kept slots below it do not move. What is behind the budget afterwards is left as it was.
+ *   sinks, recent  >= 0, together at most budget (> 0)
+ *   newest   [seqs] i32: position of each sequence's newest token; nullable when recent = 0 or the cache has
+ *            no pos (the newest is then its last slot)
+ *   length_out [seqs] i32 = min(length, budget); not the cache's own length, which other layers' calls may still
+ *            need as it is
+ *   workspace  device scratch of ordermoe_cache_evict_workspace_bytes(seqs, heads, budget) bytes, 256-byte
+ *            aligned; calls that may overlap on the GPU need one each
+ * Needs mass. Rows whose page does not exist are reported and not moved. */
+size_t ordermoe_cache_evict_workspace_bytes(int seqs, int heads, int budget);
+int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int sinks, int recent,
+                         const int32_t* newest, int32_t* length_out, void* workspace,
+                         size_t workspace_bytes, ordermoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection: for token t with adapter a = ids[t],
+ *   Y[t] = residual[t] + scale[a] B_a (A_a X[t]),
+ * and Y[t] = residual[t] for a token without one (id -1). The shared product is ordermoe_linear's, its result
+ * the residual here.
+ *   X        [T][K] bf16, rows ldx apart
+ *   A        [n][R][K] bf16: the rows of adapter a at A + a * stride_a, lda apart
+ *   B        [n][N][R] bf16: at B + a * stride_b, rows ldb apart
+ *            (every stride a multiple of 8, 16-byte aligned bases; R a multiple of 8, 8 to 128)
+ *   ids      [T] i32, -1 to n - 1, in any order; tokens with the same adapter read its weights once a tile
+ *   rank     [n] i32, nullable: rows of A and columns of B in use, 0 to R; what is behind them is not used, whatever it
+ *            holds
+ *   scale    [n] f32, nullable (1)
+ *   residual [T][N] bf16, rows ldr apart, nullable (zeros)
+ *   Y        [T][N] out, rows ldy apart, bf16 or float (f32 != 0); may be the residual itself (bf16, same
+ *            stride)
+ *   workspace  device scratch of ordermoe_adapters_workspace_bytes(T, K, N, R) bytes, 256-byte aligned; calls that
+ *            may overlap on the GPU need one each
+ * A X in fp32, handed on in two bf16 parts (16 bits), fp32 sums in a fixed order, one rounding to Y. T and N up to
+ * 2^31 - 513, K up to 2^30, n up to 2^31 - 1. An id outside [-1, n) or a rank outside [0, R] sets ORDERMOE_DEV_BAD_INDEX
+ * (detail: the token; the adapter): the token is taken to have none, the rank to be the nearest. */
+size_t ordermoe_adapters_workspace_bytes(int T, int K, int N, int R);
+int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t* A, int64_t stride_a, int64_t lda,
+                      const uint16_t* B, int64_t stride_b, int64_t ldb, const int32_t* ids,
+                      const int32_t* rank, const float* scale, int n, int R,
+                      const uint16_t* residual, int64_t ldr, int T, int N, int K, void* Y, int64_t ldy,
+                      int f32, void* workspace, size_t workspace_bytes, ordermoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * Weighted combine: y[t] = bf16( sum_{j=0..k-1} topk_w[t][j] * Y_perm[row_of[t][j]] )
  * with fp32 accumulation in slot order.
  *   Y_perm [T*k][d] bf16, row_of [T][k] i32, topk_w [T][k] f32, y [T][d] bf16 out.

@@ -74,6 +74,14 @@ _SIGNATURES = {
     "ordermoe_layer_few_init": ([_P, _SZ, _P], _I),
     "ordermoe_layer_few": ([_P, _I, _P, _P, _P, _P, _P, _P, _P, _SZ, _P], _I),
     "ordermoe_layer_few_residual": ([_P, _I, _P, _P, _P, _P, _P, _F, _P, _P, _P, _P, _SZ, _P], _I),
+    "ordermoe_cache_append": ([_P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _I, _I, _P, _P, _P, _I, _I, _P], _I),
+    "ordermoe_attention_paged_workspace_bytes": ([_I, _I, _I, _I, _I64, _I], _SZ),
+    "ordermoe_attention_paged": ([_P, _P, _I64, _I, _F, _P, _I64, _P, _I, _P, _SZ, _P], _I),
+    "ordermoe_cache_evict_workspace_bytes": ([_I, _I, _I], _SZ),
+    "ordermoe_cache_evict": ([_P, _I, _I, _I, _P, _P, _P, _SZ, _P], _I),
+    "ordermoe_adapters_workspace_bytes": ([_I, _I, _I, _I], _SZ),
+    "ordermoe_adapters": ([_P, _I64, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _I, _I, _P, _I64, _I, _I, _I, _P,
+                           _I64, _I, _P, _SZ, _P], _I),
     "ordermoe_transitions_strided": ([_P, _I64, _I, _I, _I, _I64, _I64, _P, _P, _P], _I),
 }
 
@@ -98,6 +106,17 @@ class FewOut(ctypes.Structure):
     _fields_ = [(n, _P) for n in ("logits", "topk_idx", "topk_w", "chosen_expert", "chosen_server",
                                   "kind", "counters")]
     sizes = None  # of the call that its tensors were last checked for
+
+
+class Cache(ctypes.Structure):
+    """Mirror of ordermoe_cache."""
+    _fields_ = [("k", _P), ("v", _P), ("pages", _I64), ("page", _I), ("heads", _I), ("dim", _I), ("seqs", _I),
+                ("seq_pages", _I), ("table", _P), ("ld_table", _I64), ("length", _P), ("mass", _P), ("pos", _P)]
+
+    @property
+    def slots(self):
+        """Slots that a sequence's row of the table reaches."""
+        return self.seq_pages * self.page
 
 
 class OrderMoEError(RuntimeError):
@@ -528,6 +547,162 @@ def ordermoe_selftest_linear_plan(M, N, K, f32=False, device=None):
         M, N, K, bool(f32), None if device is None else (_I * 4)(*device), plan))
     names = ("kernel", "rows", "cols", "row_tiles", "col_tiles", "split", "stages", "grid")
     return dict(zip(names, plan), kernel=LINEAR_KERNELS[plan[0]])
+
+
+def make_cache(k, v, table, length, mass=None, pos=None):
+    """A paged cache for ordermoe_cache_append, ordermoe_attention_paged and ordermoe_cache_evict over the
+    caller's tensors, all on one device: k, v [pages, heads, page, dim] bf16, table [seqs, n] int32 (rows may lie in a
+    wider buffer), length [seqs] int32; mass float32 and pos int32 [seqs, heads, n * page], nullable."""
+    if k.dim() != 4 or k.shape != v.shape:
+        raise ValueError("k and v must be [pages, heads, page, dim], got %s and %s" % (tuple(k.shape), tuple(v.shape)))
+    pages, heads, page, dim = k.shape
+    dev = k.get_device()
+    for n, t in (("k", k), ("v", v)):
+        _entries(t, n, torch.bfloat16, 0, dev)
+    if dev < 0:
+        raise ValueError("the cache must be on a CUDA device")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise TypeError("table must be an int32 matrix")
+    seqs, n = table.shape
+    at, ld = _matrix(table, "table", table.shape, dev, (torch.int32,))
+    ld = max(ld, n)
+    if length.shape != (seqs,):
+        raise ValueError("length must be [%d], got %s" % (seqs, tuple(length.shape)))
+    side = (seqs, heads, n * page)
+    for what, t in (("mass", mass), ("pos", pos)):
+        if t is not None and t.shape != side:
+            raise ValueError("%s must be %s, got %s" % (what, side, tuple(t.shape)))
+    c = Cache(k.data_ptr(), v.data_ptr(), pages, page, heads, dim, seqs, n, at, ld,
+              _entries(length, "length", torch.int32, seqs, dev), _entries(mass, "mass", torch.float32, 0, dev),
+              _entries(pos, "pos", torch.int32, 0, dev))
+    c._keep = (k, v, table, length, mass, pos)
+    c._device = dev
+    return c
+
+
+def _cache(cache):
+    dev = torch.cuda.current_device()
+    if cache._device != dev:
+        raise ValueError("the cache must be on the current device, cuda:%d" % dev)
+    return dev
+
+
+def _heads(t, name, width):
+    if t.dim() != 2 or t.shape[1] % width or t.shape[1] == 0:
+        raise ValueError("%s must be [tokens, heads * %d], got %s" % (name, width, tuple(t.shape)))
+    return t.shape[1] // width
+
+
+def ordermoe_cache_append(cache, k, v, q=None, q_out=None, starts=None, position=None, inv_freq=None,
+                          adjacent=False, stream=None):
+    """New tokens into a cache (make_cache): k, v [T, heads * dim] bf16, their rows may lie in wider buffers; q
+    [T, q_heads * dim] is turned into q_out (which may be q). starts [seqs + 1] int32 (None: one token a
+    sequence), position [T] int32 (None: the slot), inv_freq [rot / 2] float64 (None: nothing turns). length
+    counts the new tokens already."""
+    dev, T = _cache(cache), k.shape[0]
+    shape = (T, cache.heads * cache.dim)
+    ka, ldk = _matrix(k, "k", shape, dev)
+    va, ldv = _matrix(v, "v", shape, dev)
+    qa = qo = None
+    ldq = ldqo = hq = 0
+    if q is not None:
+        hq = _heads(q, "q", cache.dim)
+        shape = (T, hq * cache.dim)
+        qa, ldq = _matrix(q, "q", shape, dev)
+        qo, ldqo = (None, 0) if q_out is None else _matrix(q_out, "q_out", shape, dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    rc = lib().ordermoe_cache_append(
+        ctypes.byref(cache), ka, ldk, va, ldv, qa, ldq, qo, ldqo, T, hq,
+        _entries(starts, "starts", torch.int32, cache.seqs + 1, dev),
+        _entries(position, "position", torch.int32, T, dev),
+        _entries(inv_freq, "inv_freq", torch.float64, 0, dev), rot, bool(adjacent), _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_cache_append", rc)
+
+
+def ordermoe_attention_paged_workspace_bytes(cache, q_heads, weights=False):
+    """Workspace of ordermoe_attention_paged over a cache of these sizes (of q_heads query heads)."""
+    return int(lib().ordermoe_attention_paged_workspace_bytes(cache.seqs, q_heads, cache.heads, cache.dim, cache.slots,
+                                                              bool(weights)))
+
+
+def ordermoe_attention_paged(cache, q, out, workspace, scale=None, lse=None, weights=False, stream=None):
+    """Attention of one query a sequence over its slots of the cache: q, out [seqs, q_heads * dim] bf16 (rows may
+    lie in wider buffers; out may be q), scale 1 / sqrt(dim) unless given, lse [seqs, q_heads] float32 out (or None).
+    weights: the cache's mass grows by the weight that each slot receives."""
+    dev = _cache(cache)
+    hq = _heads(q, "q", cache.dim)
+    shape = (cache.seqs, hq * cache.dim)
+    qa, ldq = _matrix(q, "q", shape, dev)
+    oa, ldo = _matrix(out, "out", shape, dev)
+    rc = lib().ordermoe_attention_paged(
+        ctypes.byref(cache), qa, ldq, hq, cache.dim ** -0.5 if scale is None else scale, oa, ldo,
+        _entries(lse, "lse", torch.float32, cache.seqs * hq, dev), bool(weights),
+        _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_attention_paged", rc)
+
+
+def ordermoe_cache_evict_workspace_bytes(cache, budget):
+    return int(lib().ordermoe_cache_evict_workspace_bytes(cache.seqs, cache.heads, budget))
+
+
+def ordermoe_cache_evict(cache, budget, length_out, workspace, newest=None, recent=0, sinks=0, stream=None):
+    """Cuts the sequences of more than `budget` slots to that many a head: the first `sinks` and last `recent`
+    positions (newest [seqs] int32: each sequence's last one) and the largest mass stay. length_out [seqs] int32."""
+    dev = _cache(cache)
+    rc = lib().ordermoe_cache_evict(
+        ctypes.byref(cache), budget, sinks, recent, _entries(newest, "newest", torch.int32, cache.seqs, dev),
+        _entries(length_out, "length_out", torch.int32, cache.seqs, dev),
+        _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_cache_evict", rc)
+
+
+def ordermoe_adapters_workspace_bytes(T, K, N, R):
+    return int(lib().ordermoe_adapters_workspace_bytes(T, K, N, R))
+
+
+def _stack(t, name, shape, device):
+    """Address, stride of a matrix and of a row of a stack of device matrices whose rows are contiguous."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.get_device() != device:
+        raise ValueError("%s must be on the current device, cuda:%d" % (name, device))
+    n, rows, w = shape
+    if w > 1 and t.stride(2) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    ld = t.stride(1) if rows > 1 else (w + 7) // 8 * 8
+    if ld < w:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return t.data_ptr(), t.stride(0) if n > 1 else 0, ld
+
+
+def ordermoe_adapters(X, A, Bw, ids, Y, workspace, scale=None, rank=None, residual=None, stream=None):
+    """Y[t] = residual[t] + scale[a] Bw[a] (A[a] X[t]) with a = ids[t], or the residual alone where that is -1: X
+    [T, K], A [n, R, K], Bw [n, N, R], residual [T, N] bf16 (None: zeros), Y [T, N] bf16 or float32, ids [T] int32,
+    scale [n] float32 (None: 1), rank [n] int32 (None: R). Rows may lie in wider buffers; Y may be the residual."""
+    try:
+        (T, K), (n, R, _), (_, N) = X.shape, A.shape, Y.shape
+    except (AttributeError, ValueError):
+        raise TypeError("X and Y must be matrices, A and Bw stacks of matrices") from None
+    dev = torch.cuda.current_device()
+    x, ldx = _matrix(X, "X", X.shape, dev)
+    a, sa, lda = _stack(A, "A", (n, R, K), dev)
+    b, sb, ldb = _stack(Bw, "Bw", (n, N, R), dev)
+    y, ldy = _matrix(Y, "Y", (T, N), dev, (torch.bfloat16, torch.float32))
+    r, ldr = _matrix(residual, "residual", (T, N), dev) if residual is not None else (None, 0)
+    rc = lib().ordermoe_adapters(
+        x, ldx, a, sa, lda, b, sb, ldb, _entries(ids, "ids", torch.int32, T, dev),
+        _entries(rank, "rank", torch.int32, n, dev), _entries(scale, "scale", torch.float32, n, dev), n, R, r, ldr, T, N,
+        K, y, ldy, Y.dtype == torch.float32, _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(),
+        _raw_stream(stream))
+    if rc != OK:
+        _check("ordermoe_adapters", rc)
 
 
 def ordermoe_layer_few_workspace_bytes(T, E, d, dff, k):

@@ -15,6 +15,9 @@ int read_clear_err_cost(unsigned long long* out);
 int read_clear_err_simtc(unsigned long long* out);
 int read_clear_err_few(unsigned long long* out);
 int read_clear_err_linear(unsigned long long* out);
+int read_clear_err_cache(unsigned long long* out);
+int read_clear_err_attention(unsigned long long* out);
+int read_clear_err_adapters(unsigned long long* out);
 int selftest_wait_timeout(uint64_t limit_ns, cudaStream_t stream);
 
 static thread_local char t_msg[512] = "";
@@ -60,7 +63,7 @@ extern "C" int ordermoe_device_error(int* code, int* detail) {
   OM_TRACE();
   if (!code) return fail(ORDERMOE_ERR_INVALID_ARG, "device_error: null code");
   OM_CUDA(cudaDeviceSynchronize());
-  unsigned long long words[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  unsigned long long words[11] = {};
   int rc;
   if ((rc = read_clear_err_route(&words[0]))) return rc;
   if ((rc = read_clear_err_dispatch(&words[1]))) return rc;
@@ -70,6 +73,9 @@ extern "C" int ordermoe_device_error(int* code, int* detail) {
   if ((rc = read_clear_err_simtc(&words[5]))) return rc;
   if ((rc = read_clear_err_few(&words[6]))) return rc;
   if ((rc = read_clear_err_linear(&words[7]))) return rc;
+  if ((rc = read_clear_err_cache(&words[8]))) return rc;
+  if ((rc = read_clear_err_attention(&words[9]))) return rc;
+  if ((rc = read_clear_err_adapters(&words[10]))) return rc;
   *code = 0;
   if (detail) *detail = 0;
   for (unsigned long long w : words) {

@@ -1,0 +1,548 @@
+// Attention of one new token a sequence over a paged cache.
+//
+// For a cached head with G query heads: x_i = scale <q, k_i>, out = sum_i exp(x_i - m) v_i / sum_i exp(x_i - m). Every byte
+// of the cache is used G times, so HBM bounds it. The slots of all sequences and heads, cut into units of 16, form
+// one list that is shared out evenly over the warps of a grid of one CTA an SM, by the lengths on the device;
+// a warp runs through its part with a running maximum and sum and a ring of its own in shared memory, and what is left of
+// rows that several warps share is joined by a second kernel in a fixed order.
+#include "kvcache.cuh"
+
+namespace om {
+
+static __device__ unsigned long long g_err_attention = 0;
+
+int read_clear_err_attention(unsigned long long* out) {
+  unsigned long long zero = 0;
+  OM_CUDA(cudaMemcpyFromSymbol(out, g_err_attention, sizeof(*out)));
+  OM_CUDA(cudaMemcpyToSymbol(g_err_attention, &zero, sizeof(zero)));
+  return ORDERMOE_OK;
+}
+
+namespace at {
+
+constexpr int UNIT = 16;        // slots of a unit: the K of one m16n8k16 product with V
+constexpr int MAX_CTAS = 192;   // workspaces hold partial results of so many
+constexpr int MAX_WARPS = 8;
+
+template <int D>
+struct Shape {
+  static constexpr int WARPS = D == 256 ? 4 : 8;
+  static constexpr int STAGES = D == 64 ? 6 : 3;
+  static constexpr int HALF = UNIT * D * 2;  // bytes of a unit's keys
+  static constexpr int SMEM = WARPS * STAGES * 2 * HALF;
+};
+
+struct Args {
+  CacheView c;
+  int Hq, G, GC, chunks;  // query heads, per cached head, per row, rows per cached head
+  const uint16_t* q; int64_t ldq;
+  uint16_t* out; int64_t ldo;
+  float* lse;
+  float scale2;   // scale * log2(e)
+  int warps;      // of the grid
+  float* part;    // [warps][2]: maxima, sums, outputs of a row's heads
+  float* stat;    // weights: [rows][GP][2] maximum and 1 / sum
+  float* score;   // weights: [units][GP][16]
+};
+
+// Units before each of the block's groups of sequences. Thread i has the sequences [i * per, (i + 1) * per).
+template <int NT>
+struct Units {
+  long long before[NT + 1];
+  long long warp_sum[NT / 32];
+};
+__device__ __forceinline__ int units_of(const Args& a, int s) { return (a.c.slots(s) + UNIT - 1) / UNIT; }
+
+template <int NT>
+__device__ __forceinline__ int count_units(const Args& a, Units<NT>& u) {
+  const int per = (a.c.seqs + NT - 1) / NT, tid = threadIdx.x, lane = tid % 32;
+  long long mine = 0;
+  for (int s = tid * per; s < a.c.seqs && s < (tid + 1) * per; ++s) mine += units_of(a, s);
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(~0u, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) u.warp_sum[tid / 32] = upto;
+  __syncthreads();
+  long long base = 0;
+  for (int i = 0; i < tid / 32; ++i) base += u.warp_sum[i];
+  u.before[tid] = base + upto - mine;
+  if (tid == NT - 1) u.before[NT] = base + upto;
+  __syncthreads();
+  return per;
+}
+// Units of the sequences before s.
+template <int NT>
+__device__ __forceinline__ long long units_before(const Args& a, const Units<NT>& u, int per, int s) {
+  long long b = u.before[s / per];
+  for (int i = s / per * per; i < s; ++i) b += units_of(a, i);
+  return b;
+}
+
+// Where a warp's part begins: warp w has the units [w U / W, (w + 1) U / W).
+__device__ __forceinline__ long long first_unit(long long U, int w, int W) { return U * w / W; }
+__device__ __forceinline__ int owner(long long U, long long unit, int W) {
+  return static_cast<int>(((unit + 1) * W - 1) / U);
+}
+// Warps that take part: four units each where there are enough.
+__device__ __forceinline__ int active_warps(long long U, int warps) {
+  const long long w = (U + 3) / 4;
+  return w < 1 ? 1 : w > warps ? warps : static_cast<int>(w);
+}
+
+// A unit's place: sequence, row (cached head and chunk of its query heads) and unit of the row.
+struct Place {
+  int s, r, j, nu, n;
+};
+__device__ __forceinline__ void next_place(const Args& a, Place& p, int rows) {
+  if (++p.j < p.nu) return;
+  p.j = 0;
+  if (++p.r < rows) return;
+  p.r = 0;
+  for (++p.s; p.s < a.c.seqs; ++p.s) {
+    p.n = a.c.slots(p.s);
+    if (p.n > 0) break;
+  }
+  p.nu = (p.n + UNIT - 1) / UNIT;
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+               "{%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Loads a unit's keys and values, rows of D with their 16-byte vectors exchanged by the row's lowest three
+// bits (no bank is met twice by a matrix load). Rows behind the length, and pages that do not exist, are zeros.
+template <int D>
+__device__ __forceinline__ void load_unit(const Args& a, const Place& p, int32_t page, uint32_t stage) {
+  constexpr int VECS = D / 8, HALF = Shape<D>::HALF;
+  const int lane = threadIdx.x % 32, head = p.r / a.chunks, base = p.j * UNIT;
+#pragma unroll
+  for (int i = 0; i < UNIT * VECS / 32; ++i) {
+    const int x = i * 32 + lane, row = x / VECS, vec = x % VECS, slot = base + row;
+    const int32_t pg = a.c.page_log >= 4 || slot >= p.n ? page : a.c.page_of(p.s, slot);
+    const bool ok = slot < p.n && a.c.good(pg);
+    if (slot < p.n && !ok && vec == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
+    const int64_t at = ok ? a.c.row(pg, head, slot) * D + vec * 8 : 0;
+    const uint32_t dst = stage + (row * VECS + (vec ^ (row & 7))) * 16;
+    cp16(dst, a.c.k + at, ok ? 16 : 0);
+    cp16(dst + HALF, a.c.v + at, ok ? 16 : 0);
+  }
+}
+
+// GP = 8 NG rows of the 16-row product hold query heads. With eight, the other eight rows carry the second bf16 part of
+// p in the product with V; with sixteen a second product does.
+template <int D, int NG, bool WEIGHTS>
+__global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const Args a) {
+  constexpr int WARPS = Shape<D>::WARPS, NT = WARPS * 32, STAGES = Shape<D>::STAGES, HALF = Shape<D>::HALF;
+  constexpr int GP = 8 * NG, PS = GP * (D + 2), KS = D / 16, VECS = D / 8;
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ Units<NT> units;
+  pdl_wait();
+  pdl_trigger();
+  const int per = count_units(a, units), lane = threadIdx.x % 32, g = lane / 4, q4 = lane % 4;
+  const int rows = a.c.heads * a.chunks;
+  const long long U = units.before[NT] * rows;
+  if (blockIdx.x == 0)
+    for (int s = threadIdx.x; s < a.c.seqs; s += NT)
+      if (a.c.length[s] != a.c.slots(s)) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, s);
+  const int W = active_warps(U, a.warps);
+  // consecutive parts on different SMs: fewer than all of them still use every SM
+  const int w = static_cast<int>(threadIdx.x / 32) * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+  if (U == 0 || w >= W) return;
+  const long long u0 = first_unit(U, w, W), u1 = first_unit(U, w + 1, W);
+  if (u0 >= u1) return;
+  Place p;
+  {
+    const long long t = u0 / rows;
+    int lo = 0, hi = NT;  // before[lo] <= t < before[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (units.before[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    long long b = units.before[lo];
+    p.s = lo * per;
+    while (b + units_of(a, p.s) <= t) b += units_of(a, p.s++);
+    p.n = a.c.slots(p.s);
+    p.nu = units_of(a, p.s);
+    const long long rest = u0 - b * rows;
+    p.r = static_cast<int>(rest / p.nu);
+    p.j = static_cast<int>(rest % p.nu);
+  }
+  const uint32_t mine = smem_u32(ring) + (threadIdx.x / 32) * STAGES * 2 * HALF;
+  Place f = p;  // what is loaded next, and its page
+  long long fu = u0;
+  int32_t page = a.c.page_of(f.s, f.j * UNIT);
+  auto fetch = [&]() {
+    if (fu < u1) {
+      load_unit<D>(a, f, page, mine + static_cast<uint32_t>((fu - u0) % STAGES) * 2 * HALF);
+      if (++fu < u1) {
+        next_place(a, f, rows);
+        page = a.c.page_of(f.s, f.j * UNIT);
+      }
+    }
+    cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) fetch();
+
+  uint32_t qa[KS][NG == 1 ? 2 : 4];
+  float o[VECS][4], m[2], l[2];
+  int heads = 0, j0 = 0;
+  bool fresh = true;
+  for (long long u = u0; u < u1; ++u) {
+    const int head = p.r / a.chunks, first = (p.r % a.chunks) * a.GC;
+    if (fresh) {  // a row begins in this part
+      fresh = false;
+      j0 = p.j;
+      heads = min(a.GC, a.G - first);
+      const uint16_t* q = a.q + p.s * a.ldq + (static_cast<int64_t>(head) * a.G + first) * D + q4 * 2;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const bool on = g + 8 * i < heads;
+          const uint16_t* x = q + static_cast<int64_t>(on ? g + 8 * i : 0) * D + k * 16;
+          const uint32_t lo = *reinterpret_cast<const uint32_t*>(x), hi = *reinterpret_cast<const uint32_t*>(x + 8);
+          qa[k][i] = on ? lo : 0u;
+          qa[k][NG + i] = on ? hi : 0u;
+        }
+#pragma unroll
+      for (int n = 0; n < VECS; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
+      m[0] = m[1] = -INFINITY;
+      l[0] = l[1] = 0.0f;
+    }
+    cp_wait<STAGES - 2>();
+    __syncwarp();
+    fetch();  // into the stage that was read a unit ago
+    const uint32_t kb = mine + static_cast<uint32_t>((u - u0) % STAGES) * 2 * HALF, vb = kb + HALF;
+    float x[2][4] = {};
+    {
+      const int row = (lane & 7) + (lane >= 16 ? 8 : 0), half = lane / 8 % 2;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t b[4];
+        ldm4(b, kb + (row * VECS + ((2 * k + half) ^ (row & 7))) * 16);
+        if constexpr (NG == 1) {
+          mma(x[0], qa[k][0], 0u, qa[k][1], 0u, b[0], b[1]);
+          mma(x[1], qa[k][0], 0u, qa[k][1], 0u, b[2], b[3]);
+        } else {
+          mma(x[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], b[0], b[1]);
+          mma(x[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], b[2], b[3]);
+        }
+      }
+    }
+    const int left = p.n - p.j * UNIT;  // slots from here to the length
+    uint32_t hi[2][2], lo[2][2];  // p's parts: [slots 0-7, 8-15][heads g, g + 8]
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      float* y[2] = {&x[0][2 * i], &x[1][2 * i]};
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          y[t][e] = t * 8 + q4 * 2 + e < left ? __fmul_rn(y[t][e], a.scale2) : -INFINITY;
+          top = fmaxf(top, y[t][e]);
+        }
+      if constexpr (WEIGHTS) {
+        float* sc = a.score + (u * GP + g + 8 * i) * UNIT + q4 * 2;
+        *reinterpret_cast<float2*>(sc) = make_float2(y[0][0], y[0][1]);
+        *reinterpret_cast<float2*>(sc + 8) = make_float2(y[1][0], y[1][1]);
+      }
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+      top = fmaxf(top, m[i]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      const float shrink = exp2f(m[i] - ref);
+      m[i] = top;
+      l[i] *= shrink;
+      if (__any_sync(~0u, shrink != 1.0f)) {
+#pragma unroll
+        for (int n = 0; n < VECS; ++n) {
+          o[n][2 * i] *= shrink;
+          o[n][2 * i + 1] *= shrink;
+          if constexpr (NG == 1) {
+            o[n][2] *= shrink;
+            o[n][3] *= shrink;
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float e0 = exp2f(y[t][0] - ref), e1 = exp2f(y[t][1] - ref);
+        l[i] += e0 + e1;
+        hi[t][i] = pack_bf16x2(e0, e1);
+        lo[t][i] = pack_bf16x2(e0 - bf16_lo(hi[t][i]), e1 - bf16_hi(hi[t][i]));
+      }
+    }
+    {
+      const int row = (lane & 7) + (lane / 8 % 2) * 8, next = lane / 16;
+#pragma unroll
+      for (int n = 0; n < VECS; n += 2) {
+        uint32_t b[4];
+        ldm4t(b, vb + (row * VECS + ((n + next) ^ (row & 7))) * 16);
+        if constexpr (NG == 1) {
+          mma(o[n], hi[0][0], lo[0][0], hi[1][0], lo[1][0], b[0], b[1]);
+          mma(o[n + 1], hi[0][0], lo[0][0], hi[1][0], lo[1][0], b[2], b[3]);
+        } else {
+          mma(o[n], hi[0][0], hi[0][1], hi[1][0], hi[1][1], b[0], b[1]);
+          mma(o[n + 1], hi[0][0], hi[0][1], hi[1][0], hi[1][1], b[2], b[3]);
+          mma(o[n], lo[0][0], lo[0][1], lo[1][0], lo[1][1], b[0], b[1]);
+          mma(o[n + 1], lo[0][0], lo[0][1], lo[1][0], lo[1][1], b[2], b[3]);
+        }
+      }
+    }
+    if (p.j + 1 == p.nu || u + 1 == u1) {  // the row ends, or the part
+      fresh = true;
+      const bool whole = j0 == 0 && p.j + 1 == p.nu;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        float sum = l[i] + __shfl_xor_sync(~0u, l[i], 1);
+        sum += __shfl_xor_sync(~0u, sum, 2);
+        const int y = g + 8 * i;
+        const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
+        float* part = a.part + (static_cast<int64_t>(w) * 2 + (j0 == 0)) * PS;
+        uint16_t* out = a.out + p.s * a.ldo + (static_cast<int64_t>(head) * a.G + first + y) * D + q4 * 2;
+        if (y >= heads) continue;
+        if (q4 == 0) {
+          if (whole) {
+            if (a.lse)
+              a.lse[static_cast<int64_t>(p.s) * a.Hq + head * a.G + first + y] =
+                  sum == 0.0f ? -INFINITY : (m[i] + log2f(sum)) * 0.69314718055994531f;
+            if constexpr (WEIGHTS)
+              *reinterpret_cast<float2*>(a.stat + ((static_cast<int64_t>(p.s) * rows + p.r) * GP + y) * 2) =
+                  make_float2(m[i], inv);
+          } else {
+            part[y] = m[i];
+            part[GP + y] = sum;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < VECS; ++n) {
+          float e0 = o[n][2 * i], e1 = o[n][2 * i + 1];
+          if constexpr (NG == 1) {
+            e0 += o[n][2];
+            e1 += o[n][3];
+          }
+          if (whole) *reinterpret_cast<uint32_t*>(out + n * 8) = pack_bf16x2(e0 * inv, e1 * inv);
+          else *reinterpret_cast<float2*>(part + 2 * GP + y * D + n * 8 + q4 * 2) = make_float2(e0, e1);
+        }
+      }
+    }
+    if (u + 1 < u1) next_place(a, p, rows);
+  }
+}
+
+// Joins the rows that several warps share, in the order of their slots, and writes the rows without slots.
+constexpr int JOIN_THREADS = 128;
+template <int D, int GP, bool WEIGHTS>
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const Args a) {
+  constexpr int PS = GP * (D + 2);
+  __shared__ Units<JOIN_THREADS> units;
+  __shared__ float top[GP], inv[GP];
+  pdl_wait();
+  pdl_trigger();
+  const int per = count_units(a, units), rows = a.c.heads * a.chunks, tid = threadIdx.x;
+  const int s = blockIdx.x / rows, r = blockIdx.x % rows, head = r / a.chunks, first = (r % a.chunks) * a.GC;
+  const int heads = min(a.GC, a.G - first), nu = units_of(a, s);
+  uint16_t* out = a.out + s * a.ldo + (static_cast<int64_t>(head) * a.G + first) * D;
+  float* lse = a.lse ? a.lse + static_cast<int64_t>(s) * a.Hq + head * a.G + first : nullptr;
+  if (nu == 0) {
+    for (int i = tid; i < heads * D / 8; i += JOIN_THREADS) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
+    if (lse && tid < heads) lse[tid] = -INFINITY;
+    return;
+  }
+  const long long U = units.before[JOIN_THREADS] * rows;
+  const int W = active_warps(U, a.warps);
+  const long long b = units_before(a, units, per, s) * rows + static_cast<long long>(r) * nu;
+  const int w0 = owner(U, b, W), w1 = owner(U, b + nu - 1, W);
+  if (w0 == w1) return;
+  auto part = [&](int w) { return a.part + (static_cast<int64_t>(w) * 2 + (w == w0)) * PS; };
+  for (int y = tid / 32; y < heads; y += JOIN_THREADS / 32) {
+    float t = -INFINITY, sum = 0.0f;
+    for (int w = w0 + tid % 32; w <= w1; w += 32) t = fmaxf(t, part(w)[y]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, o));
+    const float ref = t == -INFINITY ? 0.0f : t;
+    for (int w = w0 + tid % 32; w <= w1; w += 32) sum += part(w)[GP + y] * exp2f(part(w)[y] - ref);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (tid % 32 == 0) {
+      top[y] = ref;
+      inv[y] = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (lse) lse[y] = sum == 0.0f ? -INFINITY : (t + log2f(sum)) * 0.69314718055994531f;
+      if constexpr (WEIGHTS)
+        *reinterpret_cast<float2*>(a.stat + (static_cast<int64_t>(blockIdx.x) * GP + y) * 2) = make_float2(t, inv[y]);
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < heads * D / 4; i += JOIN_THREADS) {
+    const int y = i / (D / 4), d = i % (D / 4) * 4;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+      const float f = exp2f(part(w)[y] - top[y]);
+      const float4 x = *reinterpret_cast<const float4*>(part(w) + 2 * GP + y * D + d);
+      v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+    }
+    const float z = inv[y];
+    *reinterpret_cast<uint2*>(out + y * D + d) = make_uint2(pack_bf16x2(v.x * z, v.y * z), pack_bf16x2(v.z * z, v.w * z));
+  }
+}
+
+// mass[s][h][i] += the sum of p_i over the query heads of head h, from the scores that were kept.
+constexpr int MASS_THREADS = 128;
+template <int GP>
+__global__ void __launch_bounds__(MASS_THREADS) attend_mass_kernel(const Args a) {
+  __shared__ Units<MASS_THREADS> units;
+  pdl_wait();
+  pdl_trigger();
+  const int per = count_units(a, units), rows = a.c.heads * a.chunks;
+  const int s = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, n = a.c.slots(s), nu = units_of(a, s);
+  if (n == 0) return;
+  const long long b = units_before(a, units, per, s) * rows + static_cast<long long>(h) * a.chunks * nu;
+  float* mass = a.c.mass + a.c.side(s, h, 0);
+  for (int i = blockIdx.y * MASS_THREADS + threadIdx.x; i < n; i += gridDim.y * MASS_THREADS) {
+    float sum = 0.0f;
+    for (int c = 0; c < a.chunks; ++c) {
+      const int heads = min(a.GC, a.G - c * a.GC);
+      const float* sc = a.score + (b + static_cast<long long>(c) * nu + i / UNIT) * GP * UNIT + i % UNIT;
+      const float* st = a.stat + (static_cast<int64_t>(s) * rows + h * a.chunks + c) * GP * 2;
+      for (int y = 0; y < heads; ++y) {
+        const float inv = st[2 * y + 1];
+        sum += inv == 0.0f ? 0.0f : exp2f(sc[y * UNIT] - st[2 * y]) * inv;
+      }
+    }
+    mass[i] += sum;
+  }
+}
+
+// What a call's sizes decide: query heads of a row (8 or 16), rows a cached head, and the workspace.
+struct Layout {
+  int GP, GC, chunks;
+  size_t part, stat, score;  // bytes
+};
+static Layout layout(int seqs, int G, int heads, int dim, int64_t seq_slots, bool weights) {
+  Layout l{};
+  // Sixteen heads a row halve the passes over the cache of wide groups; heads of 256 have no registers for them.
+  l.GP = G > 8 && dim <= 128 ? 16 : 8;
+  l.GC = l.GP;
+  l.chunks = (G + l.GC - 1) / l.GC;
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  l.part = up(static_cast<size_t>(MAX_CTAS) * MAX_WARPS * 2 * l.GP * (dim + 2) * 4);
+  if (weights) {
+    const size_t rows = static_cast<size_t>(seqs) * heads * l.chunks;
+    l.stat = up(rows * l.GP * 8);
+    l.score = up(rows * ((static_cast<size_t>(seq_slots) + UNIT - 1) / UNIT) * UNIT * l.GP * 4);
+  }
+  return l;
+}
+
+template <int D, int NG, bool WEIGHTS>
+static int attend_attr() {
+  return static_cast<int>(cudaFuncSetAttribute(attend_kernel<D, NG, WEIGHTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               Shape<D>::SMEM));
+}
+
+template <int D, int NG, bool WEIGHTS>
+static int launch(Args& a, cudaStream_t stream) {
+  static PerDevice attr_;
+  const int e = per_device(attr_, attend_attr<D, NG, WEIGHTS>);
+  if (e != 0) return cuda_fail(static_cast<cudaError_t>(e), "cudaFuncSetAttribute(attend)");
+  const int sms = num_sms(), grid = sms < MAX_CTAS ? sms : MAX_CTAS;
+  a.warps = grid * Shape<D>::WARPS;
+  OM_LAUNCH_PDL("attend_kernel", attend_kernel<D, NG, WEIGHTS>, dim3(grid), dim3(Shape<D>::WARPS * 32),
+                static_cast<size_t>(Shape<D>::SMEM), stream, a);
+  const int64_t rows = static_cast<int64_t>(a.c.seqs) * a.c.heads;
+  OM_LAUNCH_PDL("attend_join_kernel", attend_join_kernel<D, 8 * NG, WEIGHTS>, dim3(static_cast<unsigned>(rows * a.chunks)),
+                dim3(JOIN_THREADS), 0, stream, a);
+  if (WEIGHTS) {
+    const int64_t fill = 16ll * sms / rows + 1, need = (a.c.cap + MASS_THREADS - 1) / MASS_THREADS;
+    OM_LAUNCH_PDL("attend_mass_kernel", attend_mass_kernel<8 * NG>,
+                  dim3(static_cast<unsigned>(rows), static_cast<unsigned>(fill < need ? fill : need)), dim3(MASS_THREADS), 0,
+                  stream, a);
+  }
+  return ORDERMOE_OK;
+}
+template <int D, int NG>
+static int launch(Args& a, bool weights, cudaStream_t stream) {
+  return weights ? launch<D, NG, true>(a, stream) : launch<D, NG, false>(a, stream);
+}
+
+}  // namespace at
+}  // namespace om
+
+using namespace om;
+
+extern "C" size_t ordermoe_attention_paged_workspace_bytes(int seqs, int q_heads, int heads, int dim, int64_t seq_slots,
+                                                           int weights) {
+  if (seqs < 0 || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || seq_slots <= 0 || seq_slots > (1 << 30) ||
+      (dim != 64 && dim != 128 && dim != 256))
+    return 0;
+  const at::Layout l = at::layout(seqs, q_heads / heads, heads, dim, seq_slots, weights != 0);
+  return l.part + l.stat + l.score;
+}
+
+extern "C" int ordermoe_attention_paged(const ordermoe_cache* cache, const uint16_t* q, int64_t ldq, int q_heads,
+                                        float scale, uint16_t* out, int64_t ldo, float* lse, int weights,
+                                        void* workspace, size_t workspace_bytes, ordermoe_stream_t stream) {
+  OM_TRACE();
+  const int rc = check_cache(cache, "attention_paged");
+  if (rc) return rc;
+  if (q_heads <= 0 || q_heads % cache->heads != 0 || q_heads > 4096)
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "attention_paged: need query heads that are a multiple of the cache's, at most 4096");
+  if (!(scale > 0.0f) || scale > 1e30f) return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: need a scale > 0");
+  if (cache->seqs == 0) return ORDERMOE_OK;
+  if (!q || !out || (weights && !cache->mass))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: null pointer (q, out, or a mass for the weights)");
+  const int64_t width = static_cast<int64_t>(q_heads) * cache->dim;
+  const bool many = cache->seqs > 1;
+  if (!aligned16(q) || !aligned16(out) || reinterpret_cast<uintptr_t>(lse) % 4 != 0)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: q and out must be 16-byte aligned, lse to its type");
+  if (many && (ldq < width || ldo < width || ldq % 8 != 0 || ldo % 8 != 0 || ldq >= (1ll << 38) || ldo >= (1ll << 38)))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: ldq and ldo must be multiples of 8, not shorter than a row");
+  if (q == out && many && ldq != ldo)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: an out that is q must have its stride");
+  const int64_t cap = static_cast<int64_t>(cache->seq_pages) * cache->page;
+  const at::Layout l = at::layout(cache->seqs, q_heads / cache->heads, cache->heads, cache->dim, cap, weights != 0);
+  if (static_cast<int64_t>(cache->seqs) * cache->heads * l.chunks > INT32_MAX / 32)
+    return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "attention_paged: need fewer sequences times heads");
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < l.part + l.stat + l.score)
+    return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: workspace is null, too small or not 256-byte aligned");
+  at::Args a{};
+  a.c = cache_view(cache);
+  a.Hq = q_heads; a.G = q_heads / cache->heads; a.GC = l.GC; a.chunks = l.chunks;
+  a.q = q; a.ldq = ldq; a.out = out; a.ldo = ldo; a.lse = lse;
+  a.scale2 = scale * 1.4426950408889634f;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  a.part = reinterpret_cast<float*>(ws);
+  a.stat = reinterpret_cast<float*>(ws + l.part);
+  a.score = reinterpret_cast<float*>(ws + l.part + l.stat);
+  const bool wt = weights != 0;
+  if (cache->dim == 64) return l.GP == 8 ? at::launch<64, 1>(a, wt, stream) : at::launch<64, 2>(a, wt, stream);
+  if (cache->dim == 128) return l.GP == 8 ? at::launch<128, 1>(a, wt, stream) : at::launch<128, 2>(a, wt, stream);
+  return at::launch<256, 1>(a, wt, stream);
+}

@@ -193,10 +193,115 @@ class DenseFFN:
         return h_out, x_out
 
 
+class PagedCache:
+    """The paged cache of one layer for `seqs` sequences of up to max_slots slots each, with pages of its own
+    (PagedCache.cache is the descriptor of the calls). share: another layer's PagedCache whose table, lengths and
+    positions this one uses: the layers of a stack take one step together. weights: also keep what each slot was
+    attended and its position, which cut() needs. Tables, lengths and pages may be written by the caller too."""
+
+    def __init__(self, seqs, max_slots, heads, dim, device, page=64, share=None, weights=False):
+        n = -(-max_slots // page)
+        if share is not None and share.table.shape != (seqs, n):
+            raise ValueError("a shared table must be of the same sequences and pages")
+        new = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype, device=device)
+        self.k, self.v = (new(seqs * n, heads, page, dim, dtype=torch.bfloat16) for _ in range(2))
+        if share is None:
+            self.table = torch.arange(seqs * n, dtype=torch.int32, device=device).view(seqs, n)
+            self.length, self.position = new(seqs), torch.full((seqs,), -1, dtype=torch.int32, device=device)
+        else:
+            self.table, self.length, self.position = share.table, share.length, share.position
+        self.mass = new(seqs, heads, n * page, dtype=torch.float32) if weights else None
+        self.pos = new(seqs, heads, n * page) if weights else None
+        self.cache = B.make_cache(self.k, self.v, self.table, self.length, self.mass, self.pos)
+        self._cut = None
+        _settle(device)
+
+    def advance(self, n=1):
+        """Room for n new tokens in every sequence: before the step that appends them, once for all layers that
+        share the lengths. The caller keeps lengths within max_slots."""
+        self.length += n
+        self.position += n
+
+    def cut(self, budget, recent=0, sinks=0, stream=None):
+        """ordermoe_cache_evict of this layer. Returns the new lengths (a buffer that the next cut overwrites):
+        after the last layer that shares them, copy them into length."""
+        if self._cut is None or self._cut[0] != budget:
+            self._cut = (budget, torch.empty_like(self.length),
+                         torch.empty(B.ordermoe_cache_evict_workspace_bytes(self.cache, budget), dtype=torch.uint8,
+                                     device=self.length.device))
+        _, out, ws = self._cut
+        B.ordermoe_cache_evict(self.cache, budget, out, ws, newest=self.position, recent=recent, sinks=sinks,
+                               stream=stream)
+        return out
+
+
+class DecodeAttention:
+    """The attention half of a decoder block for one new token a sequence:
+    y = softmax(scale R(q) [K, R(k)]^T) [V, v] Wo^T with q, k, v = x Wqkv^T + bqkv, R the rotary turn, through
+    ordermoe_linear, ordermoe_cache_append and ordermoe_attention_paged. Wqkv [(q_heads + 2 heads) * dim, d], Wo
+    [d, q_heads * dim], bqkv bf16; cache: a PagedCache, advanced before each step; inv_freq [dim / 2 or fewer] float64
+    (None: no positions). adapters: a dict of A_qkv [n, R, d], B_qkv [n, (q_heads + 2 heads) * dim, R], A_o [n, R, q_heads
+    * dim], B_o [n, d, R] bf16 and, if wanted, scale [n] float32 and rank [n] int32; `ids` ([seqs] int32, an attribute,
+    -1 at first) says which one each sequence has (ordermoe_adapters; the projections' results are rounded to bf16
+    before an adapter's part is added). Steps share the scratch: they may not overlap on the GPU."""
+
+    def __init__(self, Wqkv, Wo, cache, q_heads, inv_freq=None, adjacent=False, bqkv=None, scale=None, weights=False,
+                 adapters=None):
+        c = cache.cache
+        self.Wqkv, self.Wo, self.bqkv, self.cache = _rows16(Wqkv), _rows16(Wo), bqkv, cache
+        self.q_heads, self.inv_freq, self.adjacent, self.scale, self.weights = q_heads, inv_freq, adjacent, scale, weights
+        self.d, self.T_max = Wo.shape[0], c.seqs
+        nq, nk, dev = q_heads * c.dim, c.heads * c.dim, Wqkv.device
+        if Wqkv.shape != (nq + 2 * nk, self.d) or Wo.shape != (self.d, nq):
+            raise ValueError("Wqkv must be %s and Wo %s" % ((nq + 2 * nk, self.d), (self.d, nq)))
+        self.qkv = torch.empty(c.seqs, nq + 2 * nk, dtype=torch.bfloat16, device=dev)
+        self.q, self.k, self.v = self.qkv.split([nq, nk, nk], dim=1)
+        self.o = torch.empty(c.seqs, nq, dtype=torch.bfloat16, device=dev)
+        self.ws = torch.empty(B.ordermoe_attention_paged_workspace_bytes(c, q_heads, weights), dtype=torch.uint8, device=dev)
+        self.adapters, self.ids = adapters, torch.full((c.seqs,), -1, dtype=torch.int32, device=dev)
+        if adapters is not None:
+            R = adapters["A_qkv"].shape[1]
+            self.low_ws = torch.empty(max(B.ordermoe_adapters_workspace_bytes(c.seqs, self.d, nq + 2 * nk, R),
+                                          B.ordermoe_adapters_workspace_bytes(c.seqs, nq, self.d, R)),
+                                      dtype=torch.uint8, device=dev)
+        _settle(dev)
+
+    def _adapt(self, x, name, y, stream):
+        a = self.adapters
+        if a is not None:
+            B.ordermoe_adapters(x, a["A_" + name], a["B_" + name], self.ids, y, self.low_ws, scale=a.get("scale"),
+                                rank=a.get("rank"), residual=y, stream=stream)
+
+    def forward(self, x, y, residual=None, stream=None):
+        """y = the layer of x [seqs, d], one row a sequence, added to residual when given (y may be it)."""
+        if x.shape[0] != self.T_max:
+            raise ValueError("x must have a row for each of the cache's %d sequences" % self.T_max)
+        c = self.cache
+        B.ordermoe_linear(x, self.Wqkv, self.qkv, bias=self.bqkv, stream=stream)
+        self._adapt(x, "qkv", self.qkv, stream)
+        B.ordermoe_cache_append(c.cache, self.k, self.v, q=self.q, q_out=self.q, position=c.position,
+                                inv_freq=self.inv_freq, adjacent=self.adjacent, stream=stream)
+        B.ordermoe_attention_paged(c.cache, self.q, self.o, self.ws, scale=self.scale, weights=self.weights,
+                                   stream=stream)
+        B.ordermoe_linear(self.o, self.Wo, y, residual=residual, stream=stream)
+        self._adapt(self.o, "o", y, stream)
+        return y
+
+    def forward_residual(self, x, h, h_out, x_out, eps=B.NORM_EPS, stream=None):
+        """On the residual map: h_out = h + y, x_out = RMSNorm(h_out)."""
+        self.forward(x, h_out, residual=h, stream=stream)
+        B.ordermoe_rmsnorm(h_out, x.shape[0], self.d, eps, x_out, stream)
+        return h_out, x_out
+
+
+# layers that run by their own forward and count among no stack's tables
+_OWN = (DenseFFN, DecodeAttention)
+
+
 class LayerStack:
     """L MoE layers run through ordermoe_layer_forward with the token state
     (location, accumulated loss; Eqs. 36 and 44) carried from layer to layer, and
-    DenseFFN layers between them. Steps, and the graphs captured from them, share
+    DenseFFN and DecodeAttention layers between them. Steps, and the graphs captured from them, share
     the scratch: they may not overlap on the GPU."""
 
     def __init__(self, layers, tables, k, T_max, device, H=1, stride=0, P=None, few=False):
@@ -208,10 +313,10 @@ class LayerStack:
         of 1 to 8 tokens gain by it (64 narrow experts, us a layer: 1 token 50 -> 39, 8 tokens 125 ->
         113), 16 tokens do not (168 -> 173); with H = 3, whose decisions keep launches of their own, only
         wide experts do (1 token 148 -> 144; 64 narrow experts 104 -> 107, 16 tokens 227 -> 243). A
-        DenseFFN in `layers` runs in its place; tables, P and L then count the MoE layers
+        DenseFFN or DecodeAttention in `layers` runs in its place; tables, P and L then count the MoE layers
         alone, in order (a stack may have none: tables, k, P and few say nothing then)."""
-        dense = {l: lay for l, lay in enumerate(layers) if isinstance(lay, DenseFFN)}
-        layers = [lay for lay in layers if not isinstance(lay, DenseFFN)]
+        dense = {l: lay for l, lay in enumerate(layers) if isinstance(lay, _OWN)}
+        layers = [lay for lay in layers if not isinstance(lay, _OWN)]
         if not layers and not dense:
             raise ValueError("a stack needs a layer")
         E, dff, d = layers[0]["W1"].shape if layers else (0, 0, next(iter(dense.values())).d)
@@ -245,7 +350,7 @@ class LayerStack:
         T = X_layers[0].shape[0]
         out = B.make_few_out(counters=counters) if self._few(T) and counters is not None else None
         for desc, X, y in zip(self.descs, X_layers, y_layers):
-            if isinstance(desc, DenseFFN):
+            if isinstance(desc, _OWN):
                 desc.forward(X, y, stream=stream)
                 continue
             if self._few(T):
@@ -264,7 +369,7 @@ class LayerStack:
         T = hs[0].shape[0]
         B.ordermoe_rmsnorm(hs[0], T, self.d, eps, xs[0], stream)
         for l, desc in enumerate(self.descs):
-            if isinstance(desc, DenseFFN):
+            if isinstance(desc, _OWN):
                 desc.forward_residual(xs[l], hs[l], hs[l + 1], xs[l + 1], eps, stream)
                 continue
             if self._few(T):
@@ -336,6 +441,8 @@ def calibrate_stack(layers, h_cal, k_freq, M, eps=B.NORM_EPS):
     layers, one more than there are)."""
     dev = h_cal.device
     N, d = h_cal.shape
+    if any(isinstance(lay, DecodeAttention) for lay in layers):
+        raise ValueError("calibrate_stack: calibration tokens are no sequences: a stack with attention has no such pass")
     moe = [l for l, lay in enumerate(layers) if not isinstance(lay, DenseFFN)]
     L = len(moe)
     if L == 0:
