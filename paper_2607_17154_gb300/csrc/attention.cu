@@ -3,8 +3,8 @@
 // For a cached head with G query heads: x_i = scale <q, k_i>, out = sum_i exp(x_i - m) v_i / sum_i exp(x_i - m). Every byte
 // of the cache is used G times, so HBM bounds it. The slots of all sequences and heads, cut into units of 16, form
 // one list that is shared out evenly over the warps of a grid of one CTA an SM, by the lengths on the device;
-// a warp runs through its part with a running maximum and sum and a ring of its own in shared memory, and what is left of
-// rows that several warps share is joined by a second kernel in a fixed order.
+// a warp runs through its part with a running maximum and sum and a ring of its own in shared memory. Rows that warps of one
+// CTA share are joined there, rows that CTAs share by a second kernel, in the order of their slots.
 #include "kvcache.cuh"
 
 namespace om {
@@ -39,11 +39,18 @@ struct Args {
   uint16_t* out; int64_t ldo;
   float* lse;
   float scale2;   // scale * log2(e)
-  int warps;      // of the grid
-  float* part;    // [warps][2]: maxima, sums, outputs of a row's heads
+  int ctas;
+  int by_row;     // a CTA a row
+  int row_units;  // units of a row of as many slots as the table reaches
+  float* part;    // [CTAs][2]: maxima, sums and outputs of the rows that other CTAs share
+  float* early;   // [CTAs][warps]: the same of a row that ended early in a warp's part
   float* stat;    // weights: [rows][GP][2] maximum and 1 / sum
-  float* score;   // weights: [units][GP][16]
+  float* score;   // weights: [rows][row_units][GC][16]
 };
+
+// Rows of tables that reach few slots, where there are no more of them than CTAs, have one CTA each: no sums over the
+// lengths and no second kernel (one sequence of 100 slots, 4 heads of 64: see the figures at the launch).
+constexpr int ROW_SLOTS = 512;
 
 // Units before each of the block's groups of sequences. Thread i has the sequences [i * per, (i + 1) * per).
 template <int NT>
@@ -81,21 +88,42 @@ __device__ __forceinline__ long long units_before(const Args& a, const Units<NT>
   return b;
 }
 
-// Where a warp's part begins: warp w has the units [w U / W, (w + 1) U / W).
+// The list is cut into W parts, one a warp: part w has the units [w U / W, (w + 1) U / W). A CTA has the next
+// WARPS parts, so that it can join what its own warps share.
 __device__ __forceinline__ long long first_unit(long long U, int w, int W) { return U * w / W; }
 __device__ __forceinline__ int owner(long long U, long long unit, int W) {
   return static_cast<int>(((unit + 1) * W - 1) / U);
 }
-// Warps that take part: four units each where there are enough.
-__device__ __forceinline__ int active_warps(long long U, int warps) {
-  const long long w = (U + 3) / 4;
-  return w < 1 ? 1 : w > warps ? warps : static_cast<int>(w);
+// All warps of as many CTAs as have a unit for each, and no part is empty.
+__device__ __forceinline__ int parts(long long U, int ctas, int warps) {
+  const long long most = static_cast<long long>(ctas) * warps;
+  return static_cast<int>(U < most ? U : most);
 }
 
 // A unit's place: sequence, row (cached head and chunk of its query heads) and unit of the row.
 struct Place {
   int s, r, j, nu, n;
 };
+template <int NT>
+__device__ __forceinline__ Place find_place(const Args& a, const Units<NT>& u, int per, long long unit, int rows) {
+  const long long t = unit / rows;
+  int lo = 0, hi = NT;  // before[lo] <= t < before[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (u.before[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  Place p;
+  long long b = u.before[lo];
+  p.s = lo * per;
+  while (b + units_of(a, p.s) <= t) b += units_of(a, p.s++);
+  p.n = a.c.slots(p.s);
+  p.nu = (p.n + UNIT - 1) / UNIT;
+  const long long rest = unit - b * rows;
+  p.r = static_cast<int>(rest / p.nu);
+  p.j = static_cast<int>(rest % p.nu);
+  return p;
+}
 __device__ __forceinline__ void next_place(const Args& a, Place& p, int rows) {
   if (++p.j < p.nu) return;
   p.j = 0;
@@ -136,19 +164,59 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 // bits (no bank is met twice by a matrix load). Rows behind the length, and pages that do not exist, are zeros.
 template <int D>
 __device__ __forceinline__ void load_unit(const Args& a, const Place& p, int32_t page, uint32_t stage) {
-  constexpr int VECS = D / 8, HALF = Shape<D>::HALF;
-  const int lane = threadIdx.x % 32, head = p.r / a.chunks, base = p.j * UNIT;
+  constexpr int VECS = D / 8, HALF = Shape<D>::HALF, N = UNIT * VECS / 32;
+  const int lane = threadIdx.x % 32, head = p.r / a.chunks, base = p.j * UNIT, left = p.n - base;
+  if (a.c.page_log >= 4) {  // a unit lies in one page, row after row
+    const bool good = a.c.good(page);
+    if (!good && lane == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
+    const int64_t at = good ? a.c.row(page, head, base) * D + lane * 8 : 0;
+    const int end = good ? left : 0;
+    const uint16_t *k = a.c.k + at, *v = a.c.v + at;
 #pragma unroll
-  for (int i = 0; i < UNIT * VECS / 32; ++i) {
+    for (int i = 0; i < N; ++i) {
+      const int x = i * 32 + lane, row = x / VECS, vec = x % VECS;
+      const uint32_t dst = stage + (row * VECS + (vec ^ (row & 7))) * 16;
+      const bool ok = row < end;
+      cp16(dst, ok ? k + i * 256 : a.c.k, ok ? 16 : 0);
+      cp16(dst + HALF, ok ? v + i * 256 : a.c.v, ok ? 16 : 0);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
     const int x = i * 32 + lane, row = x / VECS, vec = x % VECS, slot = base + row;
-    const int32_t pg = a.c.page_log >= 4 || slot >= p.n ? page : a.c.page_of(p.s, slot);
-    const bool ok = slot < p.n && a.c.good(pg);
-    if (slot < p.n && !ok && vec == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
+    const bool in = row < left;
+    const int32_t pg = in ? a.c.page_of(p.s, slot) : 0;
+    const bool ok = in && a.c.good(pg);
+    if (in && !ok && vec == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
     const int64_t at = ok ? a.c.row(pg, head, slot) * D + vec * 8 : 0;
     const uint32_t dst = stage + (row * VECS + (vec ^ (row & 7))) * 16;
     cp16(dst, a.c.k + at, ok ? 16 : 0);
     cp16(dst + HALF, a.c.v + at, ok ? 16 : 0);
   }
+}
+
+// A row: one cached head of a sequence and up to GP of its query heads, `first` and on.
+struct Row {
+  int s, r, head, first, heads;
+};
+__device__ __forceinline__ Row row_of(const Args& a, int s, int r) {
+  Row x{s, r, r / a.chunks, (r % a.chunks) * a.GC, 0};
+  x.heads = min(a.GC, a.G - x.first);
+  return x;
+}
+__device__ __forceinline__ uint16_t* out_of(const Args& a, const Row& x, int y, int D) {
+  return a.out + x.s * a.ldo + (static_cast<int64_t>(x.head) * a.G + x.first + y) * D;
+}
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
+// lse, and what the weights are computed from, of head y.
+template <int GP, bool WEIGHTS>
+__device__ __forceinline__ void put_sums(const Args& a, const Row& x, int y, float m, float sum, float inv, int rows) {
+  if (a.lse)
+    a.lse[static_cast<int64_t>(x.s) * a.Hq + x.head * a.G + x.first + y] =
+        sum == 0.0f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
+  if constexpr (WEIGHTS)
+    *reinterpret_cast<float2*>(a.stat + ((static_cast<int64_t>(x.s) * rows + x.r) * GP + y) * 2) = make_float2(m, inv);
 }
 
 // GP = 8 NG rows of the 16-row product hold query heads. With eight, the other eight rows carry the second bf16 part of
@@ -157,48 +225,56 @@ template <int D, int NG, bool WEIGHTS>
 __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const Args a) {
   constexpr int WARPS = Shape<D>::WARPS, NT = WARPS * 32, STAGES = Shape<D>::STAGES, HALF = Shape<D>::HALF;
   constexpr int GP = 8 * NG, PS = GP * (D + 2), KS = D / 16, VECS = D / 8;
+  static_assert(WARPS * PS * 4 <= Shape<D>::SMEM, "a row's partial results a warp fit in the ring");
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ Units<NT> units;
+  // The row that a warp's part begins inside of ([0]; where its results are, and whether it ends in the part), and the
+  // one that begins in the part and goes on behind it ([1]). Sequence, -1: none.
+  __shared__ int cut_s[WARPS][2], cut_r[WARPS][2], cut_ends[WARPS];
+  __shared__ const float* cut_at[WARPS][2];
   pdl_wait();
   pdl_trigger();
-  const int per = count_units(a, units), lane = threadIdx.x % 32, g = lane / 4, q4 = lane % 4;
+  const int per = a.by_row ? 0 : count_units(a, units);
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, q4 = lane % 4;
   const int rows = a.c.heads * a.chunks;
-  const long long U = units.before[NT] * rows;
-  if (blockIdx.x == 0)
-    for (int s = threadIdx.x; s < a.c.seqs; s += NT)
-      if (a.c.length[s] != a.c.slots(s)) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, s);
-  const int W = active_warps(U, a.warps);
-  // consecutive parts on different SMs: fewer than all of them still use every SM
-  const int w = static_cast<int>(threadIdx.x / 32) * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
-  if (U == 0 || w >= W) return;
-  const long long u0 = first_unit(U, w, W), u1 = first_unit(U, w + 1, W);
-  if (u0 >= u1) return;
-  Place p;
-  {
-    const long long t = u0 / rows;
-    int lo = 0, hi = NT;  // before[lo] <= t < before[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (units.before[mid] <= t) lo = mid;
-      else hi = mid;
-    }
-    long long b = units.before[lo];
-    p.s = lo * per;
-    while (b + units_of(a, p.s) <= t) b += units_of(a, p.s++);
-    p.n = a.c.slots(p.s);
-    p.nu = units_of(a, p.s);
-    const long long rest = u0 - b * rows;
-    p.r = static_cast<int>(rest / p.nu);
-    p.j = static_cast<int>(rest % p.nu);
+  for (int s = blockIdx.x; s < a.c.seqs; s += gridDim.x) {  // sequences without slots, and bad lengths
+    const int n = a.c.slots(s);
+    if (threadIdx.x == 0 && n != a.c.length[s]) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, s);
+    if (n > 0) continue;
+    for (int i = threadIdx.x; i < a.Hq * VECS; i += NT)
+      reinterpret_cast<uint4*>(a.out + s * a.ldo)[i] = make_uint4(0, 0, 0, 0);
+    if (a.lse)
+      for (int i = threadIdx.x; i < a.Hq; i += NT) a.lse[static_cast<int64_t>(s) * a.Hq + i] = -INFINITY;
   }
-  const uint32_t mine = smem_u32(ring) + (threadIdx.x / 32) * STAGES * 2 * HALF;
-  Place f = p;  // what is loaded next, and its page
-  long long fu = u0;
-  int32_t page = a.c.page_of(f.s, f.j * UNIT);
+  // all units, or those of this CTA's row
+  const long long U = a.by_row ? units_of(a, blockIdx.x / rows) : units.before[NT] * rows;
+  const int W = parts(U, a.by_row ? 1 : a.ctas, WARPS), w0 = a.by_row ? 0 : blockIdx.x * WARPS, w = w0 + warp;
+  if (w0 >= W) return;
+  const long long u0 = w < W ? first_unit(U, w, W) : 0;
+  const int count = w < W ? static_cast<int>(first_unit(U, w + 1, W) - u0) : 0;
+  if (lane < 2) cut_s[warp][lane] = -1;
+  Place p{};
+  int32_t page = 0;
+  if (count > 0) {
+    if (a.by_row) {
+      p.s = blockIdx.x / rows;
+      p.r = blockIdx.x % rows;
+      p.j = static_cast<int>(u0);
+      p.nu = static_cast<int>(U);
+      p.n = a.c.slots(p.s);
+    } else {
+      p = find_place(a, units, per, u0, rows);
+    }
+    page = a.c.page_of(p.s, p.j * UNIT);
+  }
+  const uint32_t mine = smem_u32(ring) + warp * STAGES * 2 * HALF;
+  Place f = p;  // what is loaded next, its page and stage
+  int fetched = 0, fstage = 0;
   auto fetch = [&]() {
-    if (fu < u1) {
-      load_unit<D>(a, f, page, mine + static_cast<uint32_t>((fu - u0) % STAGES) * 2 * HALF);
-      if (++fu < u1) {
+    if (fetched < count) {
+      load_unit<D>(a, f, page, mine + fstage * 2 * HALF);
+      fstage = fstage + 1 == STAGES ? 0 : fstage + 1;
+      if (++fetched < count) {
         next_place(a, f, rows);
         page = a.c.page_of(f.s, f.j * UNIT);
       }
@@ -210,25 +286,48 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
 
   uint32_t qa[KS][NG == 1 ? 2 : 4];
   float o[VECS][4], m[2], l[2];
-  int heads = 0, j0 = 0;
+  int j0 = 0, stage = 0;
   bool fresh = true;
-  for (long long u = u0; u < u1; ++u) {
-    const int head = p.r / a.chunks, first = (p.r % a.chunks) * a.GC;
+  auto load_q = [&](const Row& x) {
+    const uint16_t* q = a.q + x.s * a.ldq + (static_cast<int64_t>(x.head) * a.G + x.first) * D + q4 * 2;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const bool on = g + 8 * i < x.heads;
+        const uint16_t* v = q + static_cast<int64_t>(on ? g + 8 * i : 0) * D + k * 16;
+        const uint32_t lo = *reinterpret_cast<const uint32_t*>(v), hi = *reinterpret_cast<const uint32_t*>(v + 8);
+        qa[k][i] = on ? lo : 0u;
+        qa[k][NG + i] = on ? hi : 0u;
+      }
+  };
+  // a head's sum over the lanes, and two of its outputs
+  auto total = [&](int i) {
+    const float s = l[i] + __shfl_xor_sync(~0u, l[i], 1);
+    return s + __shfl_xor_sync(~0u, s, 2);
+  };
+  auto pair = [&](int n, int i) {
+    return NG == 1 ? make_float2(o[n][0] + o[n][2], o[n][1] + o[n][3]) : make_float2(o[n][2 * i], o[n][2 * i + 1]);
+  };
+  auto park = [&](float* part) {  // maxima, sums and outputs of the row in hand
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const float sum = total(i);
+      const int y = g + 8 * i;
+      if (q4 == 0) {
+        part[y] = m[i];
+        part[GP + y] = sum;
+      }
+#pragma unroll
+      for (int n = 0; n < VECS; ++n) *reinterpret_cast<float2*>(part + 2 * GP + y * D + n * 8 + q4 * 2) = pair(n, i);
+    }
+  };
+  int open = -1;  // which of the cut rows is in the registers at the part's end
+  for (int u = 0; u < count; ++u) {
     if (fresh) {  // a row begins in this part
       fresh = false;
       j0 = p.j;
-      heads = min(a.GC, a.G - first);
-      const uint16_t* q = a.q + p.s * a.ldq + (static_cast<int64_t>(head) * a.G + first) * D + q4 * 2;
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const bool on = g + 8 * i < heads;
-          const uint16_t* x = q + static_cast<int64_t>(on ? g + 8 * i : 0) * D + k * 16;
-          const uint32_t lo = *reinterpret_cast<const uint32_t*>(x), hi = *reinterpret_cast<const uint32_t*>(x + 8);
-          qa[k][i] = on ? lo : 0u;
-          qa[k][NG + i] = on ? hi : 0u;
-        }
+      load_q(row_of(a, p.s, p.r));
 #pragma unroll
       for (int n = 0; n < VECS; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
       m[0] = m[1] = -INFINITY;
@@ -237,7 +336,8 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
     cp_wait<STAGES - 2>();
     __syncwarp();
     fetch();  // into the stage that was read a unit ago
-    const uint32_t kb = mine + static_cast<uint32_t>((u - u0) % STAGES) * 2 * HALF, vb = kb + HALF;
+    const uint32_t kb = mine + stage * 2 * HALF, vb = kb + HALF;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
     float x[2][4] = {};
     {
       const int row = (lane & 7) + (lane >= 16 ? 8 : 0), half = lane / 8 % 2;
@@ -268,9 +368,11 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
           top = fmaxf(top, y[t][e]);
         }
       if constexpr (WEIGHTS) {
-        float* sc = a.score + (u * GP + g + 8 * i) * UNIT + q4 * 2;
-        *reinterpret_cast<float2*>(sc) = make_float2(y[0][0], y[0][1]);
-        *reinterpret_cast<float2*>(sc + 8) = make_float2(y[1][0], y[1][1]);
+        if (g + 8 * i < a.GC) {
+          float* sc = a.score + (((static_cast<int64_t>(p.s) * rows + p.r) * a.row_units + p.j) * a.GC + g + 8 * i) * UNIT + q4 * 2;
+          *reinterpret_cast<float2*>(sc) = make_float2(y[0][0], y[0][1]);
+          *reinterpret_cast<float2*>(sc + 8) = make_float2(y[1][0], y[1][1]);
+        }
       }
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
@@ -315,122 +417,151 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
         }
       }
     }
-    if (p.j + 1 == p.nu || u + 1 == u1) {  // the row ends, or the part
+    const bool ends = p.j + 1 == p.nu, last = u + 1 == count;
+    if (ends || last) {  // the row ends, or the part
       fresh = true;
-      const bool whole = j0 == 0 && p.j + 1 == p.nu;
+      if (ends && j0 == 0) {  // all of the row was here
+        const Row x = row_of(a, p.s, p.r);
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        float sum = l[i] + __shfl_xor_sync(~0u, l[i], 1);
-        sum += __shfl_xor_sync(~0u, sum, 2);
-        const int y = g + 8 * i;
-        const float inv = whole ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
-        float* part = a.part + (static_cast<int64_t>(w) * 2 + (j0 == 0)) * PS;
-        uint16_t* out = a.out + p.s * a.ldo + (static_cast<int64_t>(head) * a.G + first + y) * D + q4 * 2;
-        if (y >= heads) continue;
-        if (q4 == 0) {
-          if (whole) {
-            if (a.lse)
-              a.lse[static_cast<int64_t>(p.s) * a.Hq + head * a.G + first + y] =
-                  sum == 0.0f ? -INFINITY : (m[i] + log2f(sum)) * 0.69314718055994531f;
-            if constexpr (WEIGHTS)
-              *reinterpret_cast<float2*>(a.stat + ((static_cast<int64_t>(p.s) * rows + p.r) * GP + y) * 2) =
-                  make_float2(m[i], inv);
-          } else {
-            part[y] = m[i];
-            part[GP + y] = sum;
+        for (int i = 0; i < NG; ++i) {
+          const float sum = total(i), inv = inverse(sum);
+          const int y = g + 8 * i;
+          if (y >= x.heads) continue;
+          if (q4 == 0) put_sums<GP, WEIGHTS>(a, x, y, m[i], sum, inv, rows);
+          uint16_t* out = out_of(a, x, y, D) + q4 * 2;
+#pragma unroll
+          for (int n = 0; n < VECS; ++n) {
+            const float2 v = pair(n, i);
+            *reinterpret_cast<uint32_t*>(out + n * 8) = pack_bf16x2(v.x * inv, v.y * inv);
           }
         }
-#pragma unroll
-        for (int n = 0; n < VECS; ++n) {
-          float e0 = o[n][2 * i], e1 = o[n][2 * i + 1];
-          if constexpr (NG == 1) {
-            e0 += o[n][2];
-            e1 += o[n][3];
-          }
-          if (whole) *reinterpret_cast<uint32_t*>(out + n * 8) = pack_bf16x2(e0 * inv, e1 * inv);
-          else *reinterpret_cast<float2*>(part + 2 * GP + y * D + n * 8 + q4 * 2) = make_float2(e0, e1);
+      } else {
+        const int which = j0 == 0;
+        float* at = last ? reinterpret_cast<float*>(ring) + warp * PS : a.early + static_cast<int64_t>(w) * PS;
+        if (last) open = which;
+        else park(at);  // the ring is in use
+        if (lane == 0) {
+          cut_s[warp][which] = p.s;
+          cut_r[warp][which] = p.r;
+          cut_at[warp][which] = at;
+          if (which == 0) cut_ends[warp] = ends;
         }
       }
     }
-    if (u + 1 < u1) next_place(a, p, rows);
+    if (!last) next_place(a, p, rows);
+  }
+  cp_wait<0>();
+  __syncthreads();  // the ring is free
+  if (open >= 0) park(reinterpret_cast<float*>(ring) + warp * PS);
+  __syncthreads();
+  // Chains of parts that share a row: the one that reaches into this CTA from the one before, and those that begin in
+  // it. Each is joined by all threads, four outputs of a head each, part after part.
+  for (int c = -1; c < WARPS; ++c) {
+    const int b = c < 0 ? 0 : c, side = c < 0 ? 0 : 1;
+    if (cut_s[b][side] < 0) continue;
+    const Row x = row_of(a, cut_s[b][side], cut_r[b][side]);
+    int end = b + 1;  // parts [b, end) of this CTA, and whether the row ends with the last
+    bool done = side == 0 && cut_ends[0];
+    while (!done && end < WARPS && w0 + end < W) done = cut_ends[end++];
+    const bool whole = side == 1 && done;
+    float* part = a.part + (static_cast<int64_t>(blockIdx.x) * 2 + side) * PS;
+    for (int i = threadIdx.x; i < x.heads * (D / 4); i += NT) {
+      const int y = i / (D / 4), d = i % (D / 4) * 4;
+      float top = -INFINITY, sum = 0.0f;
+      for (int k = b; k < end; ++k) top = fmaxf(top, cut_at[k][k == b ? side : 0][y]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int k = b; k < end; ++k) {
+        const float* from = cut_at[k][k == b ? side : 0];
+        const float z = exp2f(from[y] - ref);
+        const float4 e = *reinterpret_cast<const float4*>(from + 2 * GP + y * D + d);
+        sum += z * from[GP + y];
+        v.x += z * e.x; v.y += z * e.y; v.z += z * e.z; v.w += z * e.w;
+      }
+      if (whole) {
+        const float inv = inverse(sum);
+        if (d == 0) put_sums<GP, WEIGHTS>(a, x, y, top, sum, inv, rows);
+        *reinterpret_cast<uint2*>(out_of(a, x, y, D) + d) =
+            make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+      } else {
+        if (d == 0) {
+          part[y] = top;
+          part[GP + y] = sum;
+        }
+        *reinterpret_cast<float4*>(part + 2 * GP + y * D + d) = v;
+      }
+    }
   }
 }
 
-// Joins the rows that several warps share, in the order of their slots, and writes the rows without slots.
-constexpr int JOIN_THREADS = 128;
+// Joins the rows that CTAs share. CTA (b, y) has head y of the row in which CTA b's units end, if the row began there:
+// its threads are D / 4 columns of four outputs, and groups that share the partial results, in order.
+constexpr int JOIN_THREADS = 256;
 template <int D, int GP, bool WEIGHTS>
 __global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const Args a) {
-  constexpr int PS = GP * (D + 2);
+  constexpr int PS = GP * (D + 2), WARPS = Shape<D>::WARPS, COLS = D / 4, GROUPS = JOIN_THREADS / COLS;
   __shared__ Units<JOIN_THREADS> units;
-  __shared__ float top[GP], inv[GP];
+  __shared__ float tops[MAX_CTAS], lens[MAX_CTAS];
+  __shared__ float4 sums[GROUPS][COLS];
   pdl_wait();
   pdl_trigger();
-  const int per = count_units(a, units), rows = a.c.heads * a.chunks, tid = threadIdx.x;
-  const int s = blockIdx.x / rows, r = blockIdx.x % rows, head = r / a.chunks, first = (r % a.chunks) * a.GC;
-  const int heads = min(a.GC, a.G - first), nu = units_of(a, s);
-  uint16_t* out = a.out + s * a.ldo + (static_cast<int64_t>(head) * a.G + first) * D;
-  float* lse = a.lse ? a.lse + static_cast<int64_t>(s) * a.Hq + head * a.G + first : nullptr;
-  if (nu == 0) {
-    for (int i = tid; i < heads * D / 8; i += JOIN_THREADS) reinterpret_cast<uint4*>(out)[i] = make_uint4(0, 0, 0, 0);
-    if (lse && tid < heads) lse[tid] = -INFINITY;
-    return;
-  }
+  const int per = count_units(a, units), rows = a.c.heads * a.chunks, tid = threadIdx.x, y = blockIdx.y;
   const long long U = units.before[JOIN_THREADS] * rows;
-  const int W = active_warps(U, a.warps);
-  const long long b = units_before(a, units, per, s) * rows + static_cast<long long>(r) * nu;
-  const int w0 = owner(U, b, W), w1 = owner(U, b + nu - 1, W);
-  if (w0 == w1) return;
-  auto part = [&](int w) { return a.part + (static_cast<int64_t>(w) * 2 + (w == w0)) * PS; };
-  for (int y = tid / 32; y < heads; y += JOIN_THREADS / 32) {
-    float t = -INFINITY, sum = 0.0f;
-    for (int w = w0 + tid % 32; w <= w1; w += 32) t = fmaxf(t, part(w)[y]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(~0u, t, o));
-    const float ref = t == -INFINITY ? 0.0f : t;
-    for (int w = w0 + tid % 32; w <= w1; w += 32) sum += part(w)[GP + y] * exp2f(part(w)[y] - ref);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    if (tid % 32 == 0) {
-      top[y] = ref;
-      inv[y] = sum == 0.0f ? 0.0f : 1.0f / sum;
-      if (lse) lse[y] = sum == 0.0f ? -INFINITY : (t + log2f(sum)) * 0.69314718055994531f;
-      if constexpr (WEIGHTS)
-        *reinterpret_cast<float2*>(a.stat + (static_cast<int64_t>(blockIdx.x) * GP + y) * 2) = make_float2(t, inv[y]);
-    }
+  const int W = parts(U, a.ctas, WARPS), next = (static_cast<int>(blockIdx.x) + 1) * WARPS;
+  if (next >= W) return;
+  const long long at = first_unit(U, next, W);
+  const Place p = find_place(a, units, per, at, rows);
+  const Row x = row_of(a, p.s, p.r);
+  const int c0 = owner(U, at - p.j, W) / WARPS, c1 = owner(U, at - p.j + p.nu - 1, W) / WARPS;
+  if (p.j == 0 || c0 != static_cast<int>(blockIdx.x) || y >= x.heads) return;
+  auto part = [&](int c) { return a.part + (static_cast<int64_t>(c) * 2 + (c == c0)) * PS; };
+  const int n = c1 - c0 + 1;
+  for (int i = tid; i < n; i += JOIN_THREADS) {
+    tops[i] = part(c0 + i)[y];
+    lens[i] = part(c0 + i)[GP + y];
   }
   __syncthreads();
-  for (int i = tid; i < heads * D / 4; i += JOIN_THREADS) {
-    const int y = i / (D / 4), d = i % (D / 4) * 4;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float top = -INFINITY, sum = 0.0f;
+  for (int i = 0; i < n; ++i) top = fmaxf(top, tops[i]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const int col = tid % COLS, group = tid / COLS;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const float f = exp2f(part(w)[y] - top[y]);
-      const float4 x = *reinterpret_cast<const float4*>(part(w) + 2 * GP + y * D + d);
-      v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
-    }
-    const float z = inv[y];
-    *reinterpret_cast<uint2*>(out + y * D + d) = make_uint2(pack_bf16x2(v.x * z, v.y * z), pack_bf16x2(v.z * z, v.w * z));
+  for (int i = group; i < n; i += GROUPS) {
+    const float z = exp2f(tops[i] - ref);
+    const float4 e = *reinterpret_cast<const float4*>(part(c0 + i) + 2 * GP + y * D + col * 4);
+    v.x += z * e.x; v.y += z * e.y; v.z += z * e.z; v.w += z * e.w;
   }
+  sums[group][col] = v;
+  __syncthreads();
+  if (tid >= COLS) return;
+  for (int i = 0; i < n; ++i) sum += lens[i] * exp2f(tops[i] - ref);
+  for (int i = 1; i < GROUPS; ++i) {
+    const float4 e = sums[i][col];
+    v.x += e.x; v.y += e.y; v.z += e.z; v.w += e.w;
+  }
+  const float inv = inverse(sum);
+  if (tid == 0) put_sums<GP, WEIGHTS>(a, x, y, top, sum, inv, rows);
+  *reinterpret_cast<uint2*>(out_of(a, x, y, D) + col * 4) =
+      make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
 }
 
 // mass[s][h][i] += the sum of p_i over the query heads of head h, from the scores that were kept.
 constexpr int MASS_THREADS = 128;
 template <int GP>
 __global__ void __launch_bounds__(MASS_THREADS) attend_mass_kernel(const Args a) {
-  __shared__ Units<MASS_THREADS> units;
   pdl_wait();
   pdl_trigger();
-  const int per = count_units(a, units), rows = a.c.heads * a.chunks;
-  const int s = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, n = a.c.slots(s), nu = units_of(a, s);
-  if (n == 0) return;
-  const long long b = units_before(a, units, per, s) * rows + static_cast<long long>(h) * a.chunks * nu;
+  const int rows = a.c.heads * a.chunks, s = blockIdx.x / a.c.heads, h = blockIdx.x % a.c.heads, n = a.c.slots(s);
   float* mass = a.c.mass + a.c.side(s, h, 0);
   for (int i = blockIdx.y * MASS_THREADS + threadIdx.x; i < n; i += gridDim.y * MASS_THREADS) {
     float sum = 0.0f;
     for (int c = 0; c < a.chunks; ++c) {
       const int heads = min(a.GC, a.G - c * a.GC);
-      const float* sc = a.score + (b + static_cast<long long>(c) * nu + i / UNIT) * GP * UNIT + i % UNIT;
-      const float* st = a.stat + (static_cast<int64_t>(s) * rows + h * a.chunks + c) * GP * 2;
+      const int64_t row = static_cast<int64_t>(s) * rows + h * a.chunks + c;
+      const float* sc = a.score + (row * a.row_units + i / UNIT) * a.GC * UNIT + i % UNIT;
+      const float* st = a.stat + row * GP * 2;
+#pragma unroll 4
       for (int y = 0; y < heads; ++y) {
         const float inv = st[2 * y + 1];
         sum += inv == 0.0f ? 0.0f : exp2f(sc[y * UNIT] - st[2 * y]) * inv;
@@ -443,20 +574,22 @@ __global__ void __launch_bounds__(MASS_THREADS) attend_mass_kernel(const Args a)
 // What a call's sizes decide: query heads of a row (8 or 16), rows a cached head, and the workspace.
 struct Layout {
   int GP, GC, chunks;
-  size_t part, stat, score;  // bytes
+  size_t part, early, stat, score;  // bytes
 };
 static Layout layout(int seqs, int G, int heads, int dim, int64_t seq_slots, bool weights) {
   Layout l{};
   // Sixteen heads a row halve the passes over the cache of wide groups; heads of 256 have no registers for them.
   l.GP = G > 8 && dim <= 128 ? 16 : 8;
-  l.GC = l.GP;
+  l.GC = G < l.GP ? G : l.GP;
   l.chunks = (G + l.GC - 1) / l.GC;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  l.part = up(static_cast<size_t>(MAX_CTAS) * MAX_WARPS * 2 * l.GP * (dim + 2) * 4);
+  const size_t partial = static_cast<size_t>(l.GP) * (dim + 2) * 4;
+  l.part = up(MAX_CTAS * 2 * partial);
+  l.early = up(MAX_CTAS * MAX_WARPS * partial);
   if (weights) {
     const size_t rows = static_cast<size_t>(seqs) * heads * l.chunks;
     l.stat = up(rows * l.GP * 8);
-    l.score = up(rows * ((static_cast<size_t>(seq_slots) + UNIT - 1) / UNIT) * UNIT * l.GP * 4);
+    l.score = up(rows * ((static_cast<size_t>(seq_slots) + UNIT - 1) / UNIT) * UNIT * l.GC * 4);
   }
   return l;
 }
@@ -472,13 +605,20 @@ static int launch(Args& a, cudaStream_t stream) {
   static PerDevice attr_;
   const int e = per_device(attr_, attend_attr<D, NG, WEIGHTS>);
   if (e != 0) return cuda_fail(static_cast<cudaError_t>(e), "cudaFuncSetAttribute(attend)");
-  const int sms = num_sms(), grid = sms < MAX_CTAS ? sms : MAX_CTAS;
-  a.warps = grid * Shape<D>::WARPS;
+  const int sms = num_sms();
+  a.ctas = sms < MAX_CTAS ? sms : MAX_CTAS;
+  const int64_t rows = static_cast<int64_t>(a.c.seqs) * a.c.heads;
+  const int64_t units = rows * a.chunks * ((static_cast<int64_t>(a.c.cap) + UNIT - 1) / UNIT);
+  const int64_t most = (units + Shape<D>::WARPS - 1) / Shape<D>::WARPS;  // CTAs that can have work
+  if (units / a.ctas > INT32_MAX) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "attention_paged: the table reaches too many slots");
+  a.row_units = (a.c.cap + UNIT - 1) / UNIT;
+  a.by_row = a.c.cap <= ROW_SLOTS && rows * a.chunks <= a.ctas;
+  const int grid = a.by_row ? static_cast<int>(rows * a.chunks) : most < a.ctas ? static_cast<int>(most) : a.ctas;
   OM_LAUNCH_PDL("attend_kernel", attend_kernel<D, NG, WEIGHTS>, dim3(grid), dim3(Shape<D>::WARPS * 32),
                 static_cast<size_t>(Shape<D>::SMEM), stream, a);
-  const int64_t rows = static_cast<int64_t>(a.c.seqs) * a.c.heads;
-  OM_LAUNCH_PDL("attend_join_kernel", attend_join_kernel<D, 8 * NG, WEIGHTS>, dim3(static_cast<unsigned>(rows * a.chunks)),
-                dim3(JOIN_THREADS), 0, stream, a);
+  if (grid > 1 && !a.by_row)
+    OM_LAUNCH_PDL("attend_join_kernel", attend_join_kernel<D, 8 * NG, WEIGHTS>, dim3(grid - 1, a.GC), dim3(JOIN_THREADS), 0,
+                  stream, a);
   if (WEIGHTS) {
     const int64_t fill = 16ll * sms / rows + 1, need = (a.c.cap + MASS_THREADS - 1) / MASS_THREADS;
     OM_LAUNCH_PDL("attend_mass_kernel", attend_mass_kernel<8 * NG>,
@@ -503,7 +643,7 @@ extern "C" size_t ordermoe_attention_paged_workspace_bytes(int seqs, int q_heads
       (dim != 64 && dim != 128 && dim != 256))
     return 0;
   const at::Layout l = at::layout(seqs, q_heads / heads, heads, dim, seq_slots, weights != 0);
-  return l.part + l.stat + l.score;
+  return l.part + l.early + l.stat + l.score;
 }
 
 extern "C" int ordermoe_attention_paged(const ordermoe_cache* cache, const uint16_t* q, int64_t ldq, int q_heads,
@@ -530,7 +670,7 @@ extern "C" int ordermoe_attention_paged(const ordermoe_cache* cache, const uint1
   const at::Layout l = at::layout(cache->seqs, q_heads / cache->heads, cache->heads, cache->dim, cap, weights != 0);
   if (static_cast<int64_t>(cache->seqs) * cache->heads * l.chunks > INT32_MAX / 32)
     return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "attention_paged: need fewer sequences times heads");
-  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < l.part + l.stat + l.score)
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < l.part + l.early + l.stat + l.score)
     return fail(ORDERMOE_ERR_INVALID_ARG, "attention_paged: workspace is null, too small or not 256-byte aligned");
   at::Args a{};
   a.c = cache_view(cache);
@@ -539,8 +679,9 @@ extern "C" int ordermoe_attention_paged(const ordermoe_cache* cache, const uint1
   a.scale2 = scale * 1.4426950408889634f;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.part = reinterpret_cast<float*>(ws);
-  a.stat = reinterpret_cast<float*>(ws + l.part);
-  a.score = reinterpret_cast<float*>(ws + l.part + l.stat);
+  a.early = reinterpret_cast<float*>(ws + l.part);
+  a.stat = reinterpret_cast<float*>(ws + l.part + l.early);
+  a.score = reinterpret_cast<float*>(ws + l.part + l.early + l.stat);
   const bool wt = weights != 0;
   if (cache->dim == 64) return l.GP == 8 ? at::launch<64, 1>(a, wt, stream) : at::launch<64, 2>(a, wt, stream);
   if (cache->dim == 128) return l.GP == 8 ? at::launch<128, 1>(a, wt, stream) : at::launch<128, 2>(a, wt, stream);

@@ -128,6 +128,7 @@ def test_attention_at_edges(hq, H, D, page):
 @pytest.mark.parametrize("lens,hq,H,D,page", [
     ([70001], 32, 8, 128, 16), ([40000], 8, 1, 64, 64), ([1], 32, 8, 128, 16), ([5], 8, 4, 256, 16), ([20000, 3, 0], 8, 4, 256, 32),
     ([3, 9000, 0, 1, 4097, 12], 16, 1, 128, 16), ([i % 4 for i in range(1100)], 4, 2, 64, 8), ([0] * 700 + [50], 8, 8, 128, 16),
+    ([100], 4, 4, 64, 16), ([17, 0, 300], 32, 8, 128, 16), ([480, 495], 33, 1, 128, 8), ([1, 129], 20, 2, 256, 16),
     ([0, 0, 0], 4, 4, 64, 16), ([1200 - i for i in range(40)], 32, 8, 128, 16)])
 def test_attention_of_long_and_many_sequences(lens, hq, H, D, page):
     cache = make(lens, H, D, page, seed=3)
@@ -147,10 +148,11 @@ def test_attention_of_sharp_and_flat_scores(scale, size):
     check(cache, q, out, lse, 8, scale)
 
 
+@pytest.mark.parametrize("lens", [[0, 1, 50, 700, 3001], [33, 0, 200]])
 @pytest.mark.parametrize("hq,H,D,page", [(4, 4, 64, 8), (32, 8, 128, 16), (40, 2, 128, 64), (16, 1, 128, 16), (9, 1, 256, 32)])
-def test_weights_add_up_in_mass(hq, H, D, page):
-    cache = make([0, 1, 50, 700, 3001], H, D, page, seed=6, weights=True)
-    q = torch.randn(5, hq * D, device=DEV, generator=gen(4)).to(BF16)
+def test_weights_add_up_in_mass(hq, H, D, page, lens):
+    cache = make(lens, H, D, page, seed=6, weights=True)
+    q = torch.randn(len(lens), hq * D, device=DEV, generator=gen(4)).to(BF16)
     mass = cache._keep[4]
     before = mass.double()
     ws = workspace(cache, hq, True)
@@ -415,7 +417,9 @@ def cut(cache, budget, recent=0, sinks=0, newest=None):
 
 @pytest.mark.parametrize("H,D,page,lens,budget,recent,sinks", [
     (2, 64, 8, [0, 1, 15, 16, 17, 18, 40], 16, 4, 2), (3, 128, 16, [700, 33, 5], 32, 32, 0), (1, 256, 4, [1000, 999], 1, 1, 0),
-    (8, 128, 64, [1025] * 3, 1024, 256, 4), (2, 64, 16, [2500, 3000], 2049, 100, 1), (1, 64, 16, [60000], 777, 10, 3)])
+    (8, 128, 64, [1025] * 3, 1024, 256, 4), (2, 64, 16, [2500, 3000], 2049, 100, 1), (1, 64, 16, [60000], 777, 10, 3),
+    (4, 128, 8, [1025, 1030, 1024], 1024, 100, 2), (2, 256, 1, [40, 64], 30, 3, 1), (2, 64, 16, [4095, 4000], 4060, 64, 0),
+    (2, 128, 16, [5000, 700, 701], 700, 10, 3), (1, 64, 32, [16384], 9000, 0, 0), (1, 64, 16, [20000, 16385], 3000, 100, 4)])
 def test_evict(H, D, page, lens, budget, recent, sinks):
     cache = make(lens, H, D, page, seed=30, weights=True)
     length, mass, pos = cache._keep[3:]
