@@ -78,22 +78,69 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
 //   (a, b) -> (a cos - b sin, a sin + b cos),
 // it writes R q, R k and v as they are. The angle is taken in turns in 64 bits and reduced to half a turn
 // before it becomes 32 bits: far positions lose nothing. A thread holds 16 values of a head, the eight pairs
-// of two vectors of 16 bytes (adjacent pairs: the two next to each other; else half a rotation apart).
-__global__ void __launch_bounds__(APPEND_THREADS) append_kernel(AppendArgs a) {
+// of two vectors of 16 bytes (adjacent pairs: the two next to each other; else half a rotation apart). It is
+// bound by bytes, or with few tokens by the chain sequence - length - page - store: a token's rows are read
+// before that chain, which does not say where they are.
+constexpr int APPEND_AHEAD = 2;      // items of a thread that are read first
+constexpr int APPEND_SCAN = 1024;    // sequences whose starts the threads compare all at once
+__global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs a) {
   __shared__ float cs[MAX_DIM / 2], sn[MAX_DIM / 2];
   pdl_wait();
   pdl_trigger();
-  const int t = blockIdx.x, D = a.D, H = a.c.heads;
+  const int t = blockIdx.x, D = a.D, H = a.c.heads, tid = threadIdx.x;
+  const int log_pairs = D == 64 ? 2 : D == 128 ? 3 : 4, half = a.rot / 2;
+  const int nq = a.q ? a.Hq : 0, items = (nq + 2 * H) << log_pairs;
+  auto vectors = [&](int i, int& x, int& y) {  // of item i, in its head; true: to be turned
+    const int head = i >> log_pairs, p = i & ((1 << log_pairs) - 1);
+    const bool in = p < a.rot / 16;
+    x = a.adjacent || !in ? p * 16 : p * 8;
+    y = a.adjacent || !in ? x + 8 : x + half;
+    return in && head < nq + H;
+  };
+  auto source = [&](int i) {
+    const int head = i >> log_pairs;
+    return head < nq ? a.q + t * a.ldq + static_cast<int64_t>(head) * D
+           : head < nq + H ? a.k + t * a.ldk + static_cast<int64_t>(head - nq) * D
+                           : a.v + t * a.ldv + static_cast<int64_t>(head - nq - H) * D;
+  };
+  uint4 ahead[APPEND_AHEAD][2];
+#pragma unroll
+  for (int n = 0; n < APPEND_AHEAD; ++n) {
+    const int i = tid + n * APPEND_THREADS;
+    if (i < items) {
+      int x, y;
+      vectors(i, x, y);
+      const uint16_t* src = source(i);
+      ahead[n][0] = *reinterpret_cast<const uint4*>(src + x);
+      ahead[n][1] = *reinterpret_cast<const uint4*>(src + y);
+    }
+  }
+  auto turns = [&](int pos) {
+    for (int i = tid; i < half; i += APPEND_THREADS) {
+      double v = static_cast<double>(pos) * a.inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
+      v -= rint(v);
+      sincospif(static_cast<float>(2.0 * v), &sn[i], &cs[i]);
+    }
+  };
+  const int given = a.position ? a.position[t] : 0;
+  if (a.position) turns(given);
   int s = t, first = t, count = 1;
   if (a.starts) {  // the last sequence that starts at t or before it
     if (t >= a.starts[a.c.seqs]) return;  // rows behind the last sequence
-    int lo = 0, hi = a.c.seqs;  // starts[lo] <= t < starts[hi] where the starts ascend
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.starts[mid] <= t) lo = mid;
-      else hi = mid;
+    if (a.c.seqs <= APPEND_SCAN) {
+      int n = 0;
+      for (int i = 0; i < a.c.seqs; i += APPEND_THREADS)
+        n += __syncthreads_count(i + tid < a.c.seqs && a.starts[i + tid] <= t);
+      s = n > 0 ? n - 1 : 0;
+    } else {
+      int lo = 0, hi = a.c.seqs;  // starts[lo] <= t < starts[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.starts[mid] <= t) lo = mid;
+        else hi = mid;
+      }
+      s = lo;
     }
-    s = lo;
     first = a.starts[s];
     count = a.starts[s + 1] - first;
   }
@@ -102,72 +149,61 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(AppendArgs a) {
   const int slot = inside ? static_cast<int>(at) : 0;
   const int32_t page = inside ? a.c.page_of(s, slot) : -1;
   if (!a.c.good(page)) {  // no such slot or page: the token is left out
-    if (threadIdx.x == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, t);
+    if (tid == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, t);
     return;
   }
-  const int pos = a.position ? a.position[t] : slot;
-  const int half = a.rot / 2;
-  for (int i = threadIdx.x; i < half; i += APPEND_THREADS) {
-    double turns = static_cast<double>(pos) * a.inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
-    turns -= rint(turns);
-    sincospif(static_cast<float>(2.0 * turns), &sn[i], &cs[i]);
-  }
+  const int pos = a.position ? given : slot;
+  if (!a.position) turns(pos);
   if (a.c.pos)
-    for (int h = threadIdx.x; h < H; h += APPEND_THREADS) a.c.pos[a.c.side(s, h, slot)] = pos;
+    for (int h = tid; h < H; h += APPEND_THREADS) a.c.pos[a.c.side(s, h, slot)] = pos;
   if (a.c.mass)
-    for (int h = threadIdx.x; h < H; h += APPEND_THREADS) a.c.mass[a.c.side(s, h, slot)] = 0.0f;
+    for (int h = tid; h < H; h += APPEND_THREADS) a.c.mass[a.c.side(s, h, slot)] = 0.0f;
   __syncthreads();
-  const int pairs = D / 16, nq = a.q ? a.Hq : 0;
-  const int items = (nq + 2 * H) * pairs;
-  for (int i = threadIdx.x; i < items; i += APPEND_THREADS) {
-    const int head = i / pairs, p = i % pairs;
-    const uint16_t* src;
-    uint16_t* dst;
-    bool turn = true;
-    if (head < nq) {
-      src = a.q + t * a.ldq + static_cast<int64_t>(head) * D;
-      dst = a.q_out + t * a.ldqo + static_cast<int64_t>(head) * D;
-    } else if (head < nq + H) {
-      const int h = head - nq;
-      src = a.k + t * a.ldk + static_cast<int64_t>(h) * D;
-      dst = a.c.k + a.c.row(page, h, slot) * D;
-    } else {
-      const int h = head - nq - H;
-      src = a.v + t * a.ldv + static_cast<int64_t>(h) * D;
-      dst = a.c.v + a.c.row(page, h, slot) * D;
-      turn = false;
-    }
-    // the two vectors of this thread, in the rotated part or behind it
-    int x, y, f;
-    if (a.adjacent || p >= a.rot / 16) {
-      x = p * 16; y = x + 8; f = p * 8;
-    } else {
-      x = p * 8; y = x + half; f = p * 8;
-    }
-    const uint4 u = *reinterpret_cast<const uint4*>(src + x), w = *reinterpret_cast<const uint4*>(src + y);
-    if (!turn || p >= a.rot / 16) {
+  auto finish = [&](int i, const uint4& u, const uint4& w) {
+    const int head = i >> log_pairs, f = (i & ((1 << log_pairs) - 1)) * 8;
+    int x, y;
+    const bool turn = vectors(i, x, y);
+    uint16_t* dst = head < nq ? a.q_out + t * a.ldqo + static_cast<int64_t>(head) * D
+                    : head < nq + H ? a.c.k + a.c.row(page, head - nq, slot) * D
+                                    : a.c.v + a.c.row(page, head - nq - H, slot) * D;
+    if (!turn) {
       *reinterpret_cast<uint4*>(dst + x) = u;
       *reinterpret_cast<uint4*>(dst + y) = w;
-      continue;
+      return;
     }
     float m[16];
     unpack8(u, m);
     unpack8(w, m + 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float &e = a.adjacent ? m[2 * j] : m[j], &o = a.adjacent ? m[2 * j + 1] : m[8 + j];
-      const float c = cs[f + j], z = sn[f + j], e2 = e * c - o * z;
-      o = e * z + o * c;
-      e = e2;
+      const float c = cs[f + j], z = sn[f + j];
+      const float e = a.adjacent ? m[2 * j] : m[j], o = a.adjacent ? m[2 * j + 1] : m[8 + j];
+      const float e2 = e * c - o * z, o2 = e * z + o * c;
+      if (a.adjacent) {
+        m[2 * j] = e2;
+        m[2 * j + 1] = o2;
+      } else {
+        m[j] = e2;
+        m[8 + j] = o2;
+      }
     }
     *reinterpret_cast<uint4*>(dst + x) = pack8(m);
     *reinterpret_cast<uint4*>(dst + y) = pack8(m + 8);
+  };
+#pragma unroll
+  for (int n = 0; n < APPEND_AHEAD; ++n)
+    if (tid + n * APPEND_THREADS < items) finish(tid + n * APPEND_THREADS, ahead[n][0], ahead[n][1]);
+  for (int i = tid + APPEND_AHEAD * APPEND_THREADS; i < items; i += APPEND_THREADS) {
+    int x, y;
+    vectors(i, x, y);
+    const uint16_t* src = source(i);
+    finish(i, *reinterpret_cast<const uint4*>(src + x), *reinterpret_cast<const uint4*>(src + y));
   }
 }
 
 // -------------------------------------------------------------------------- evict
 constexpr int EVICT_THREADS = 1024, EVICT_WARPS = 32;
-constexpr int EVICT_KEYS = 49152;  // keys of a row that shared memory holds; longer rows are read again a pass
+constexpr int EVICT_KEYS = 49152;  // keys of a row that shared memory holds; longer rows are read again a round
 
 struct EvictArgs {
   CacheView c;
@@ -187,89 +223,283 @@ __device__ __forceinline__ uint32_t evict_key(const EvictArgs& a, float mass, in
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ int block_before(int v, int* warp_sums, int* total) {  // exclusive sum of a value a warp
+// Exclusive sums of one value a warp, and their total.
+template <int WARPS>
+__device__ __forceinline__ int block_before(int v, int* warp_sums, int* total) {
   const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (lane == 0) warp_sums[w] = v;
   __syncthreads();
-  const int x = warp_sums[lane];  // every warp sums for itself
-  int before = lane < w ? x : 0, all = x;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    before += __shfl_xor_sync(~0u, before, o);
-    all += __shfl_xor_sync(~0u, all, o);
-  }
+  const int x = lane < WARPS ? warp_sums[lane] : 0;  // every warp sums for itself
+  const int before = __reduce_add_sync(~0u, lane < w ? x : 0);
+  *total = __reduce_add_sync(~0u, x);
   __syncthreads();
-  *total = all;
   return before;
 }
 
-// One CTA a (sequence, head). The budget-th largest key by four passes over 8 bits of it, ties to the lower
-// slot; then the freed slots below the budget and the kept ones behind it, each ascending: the i-th kept one
-// moves into the i-th freed one. Order within the cache says nothing to attention, so only these rows move.
-__global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(EvictArgs a) {
-  extern __shared__ uint32_t keys[];
-  __shared__ int hist[256];
-  __shared__ int sums[EVICT_WARPS];
-  __shared__ int pick[2];
+// One CTA a (sequence, head). The budget-th largest key, ties to the lower slot; then the freed slots below the
+// budget and the kept ones behind it, each ascending: the i-th kept one moves into the i-th freed one. Order
+// within the cache says nothing to attention, so only these rows move.
+//
+// The key is found two bits a round, by how many keys reach each of three candidates (histograms of eight bits met in
+// few bins, weights being of a kind: 16383 slots 51 us), and as soon as a candidate is reached by exactly the budget
+// no further. Rows of up to KEYS * NT slots have their keys in registers, key i in thread i % NT; longer ones in
+// shared memory, or beyond that they are read again a round.
+constexpr int KEYS = 16;
+template <int NT>
+struct Select {
+  static constexpr int WARPS = NT / 32;
+  int hits[16][3];
+  int sums[WARPS];
+  int block[KEYS * WARPS];  // of 32 slots each, in order
+};
+
+// Exclusive sums over the blocks of 32 slots; every entry may hold two counts of 16 bits.
+template <int NT>
+__device__ __forceinline__ int blocks_before(Select<NT>& s, int blocks) {
+  constexpr int WARPS = NT / 32;
+  static_assert(KEYS * WARPS <= NT, "a block a thread at most");
+  const int tid = threadIdx.x, lane = tid % 32;
+  __syncthreads();
+  const int v = tid < blocks ? s.block[tid] : 0;
+  int upto = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(~0u, upto, o);
+    if (lane >= o) upto += x;
+  }
+  int total;
+  const int base = block_before<WARPS>(__shfl_sync(~0u, upto, 31), s.sums, &total);
+  if (tid < blocks) s.block[tid] = base + upto - v;
+  __syncthreads();
+  return total;
+}
+
+template <int NT>
+__device__ __forceinline__ int select_held(const EvictArgs& a, Select<NT>& s, const float* mass, const int32_t* pos, int n,
+                                           int64_t old, int32_t* to, int32_t* from) {
+  constexpr int WARPS = NT / 32;
+  const int tid = threadIdx.x, lane = tid % 32, w = tid / 32;
+  const unsigned below = (1u << lane) - 1;
+  uint32_t key[KEYS];
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    const int i = k * NT + tid;
+    key[k] = i < n ? evict_key(a, mass[i], pos ? pos[i] : i, old) : 0u;
+  }
+  if (tid < 48) s.hits[tid / 3][tid % 3] = 0;
+  __syncthreads();
+  uint32_t known = 0;
+  bool exact = false;
+  for (int round = 0; round < 16 && !exact; ++round) {
+    const int shift = 30 - 2 * round;
+    const uint32_t c1 = known | 1u << shift, c2 = known | 2u << shift, c3 = known | 3u << shift;
+    uint32_t c = 0;  // three counts of ten bits: 512 a warp at most
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (k * NT >= n) break;
+      c += (key[k] >= c1 ? 1u : 0u) + (key[k] >= c2 ? 1u << 10 : 0u) + (key[k] >= c3 ? 1u << 20 : 0u);
+    }
+    c = __reduce_add_sync(~0u, c);
+    if (lane < 3) atomicAdd(&s.hits[round][lane], static_cast<int>(c >> (10 * lane) & 1023u));
+    __syncthreads();
+    int up = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      const int h = s.hits[round][j];
+      up += h >= a.budget;
+      exact = exact || h == a.budget;
+    }
+    known |= static_cast<uint32_t>(up) << shift;
+  }
+  // Kept: keys above `known`, and of those equal to it the first `left`. Exactly as many keys as the budget reach an exact one.
+  int left = n, total = 0;
+  if (!exact) {
+    int above = 0;
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (k * NT >= n) break;
+      above += key[k] > known;
+      const unsigned eq = __ballot_sync(~0u, k * NT + tid < n && key[k] == known);
+      if (lane == 0) s.block[k * WARPS + w] = __popc(eq);
+    }
+    block_before<WARPS>(__reduce_add_sync(~0u, above), s.sums, &total);
+    left = a.budget - total;
+    blocks_before<NT>(s, (n + NT - 1) / NT * WARPS);
+  }
+  unsigned kept = 0;  // bit k: key k stays
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    if (k * NT >= n) break;
+    const bool in = k * NT + tid < n;
+    const unsigned eq = __ballot_sync(~0u, in && key[k] == known);
+    const int tie = (exact ? 0 : s.block[k * WARPS + w]) + __popc(eq & below);
+    if (in && (key[k] > known || (key[k] == known && (exact || tie < left)))) kept |= 1u << k;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    if (k * NT >= n) break;
+    const int i = k * NT + tid;
+    const unsigned fr = __ballot_sync(~0u, i < n && i < a.budget && !(kept >> k & 1));
+    const unsigned lt = __ballot_sync(~0u, i >= a.budget && (kept >> k & 1));
+    if (lane == 0) s.block[k * WARPS + w] = __popc(fr) | __popc(lt) << 16;
+  }
+  total = blocks_before<NT>(s, (n + NT - 1) / NT * WARPS);
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    if (k * NT >= n) break;
+    const int i = k * NT + tid, at = s.block[k * WARPS + w];
+    const bool freed = i < n && i < a.budget && !(kept >> k & 1), late = i >= a.budget && (kept >> k & 1);
+    const unsigned fr = __ballot_sync(~0u, freed), lt = __ballot_sync(~0u, late);
+    if (freed) to[(at & 0xFFFF) + __popc(fr & below)] = i;
+    if (late) from[(at >> 16) + __popc(lt & below)] = i;
+  }
+  return total & 0xFFFF;  // as many late kept slots as freed ones
+}
+
+// Moves some of the listed rows of both halves of the cache with their weights and positions: threads that share a
+// 16-byte vector of `AHEAD` rows at a time, rows first and on by `step`. Sources lie behind the budget and targets below it: no
+// move reads what another one writes.
+template <int D>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, int s, int h, const int32_t* to, const int32_t* from, int n,
+                                          int first, int step) {
+  constexpr int VECS = D / 8, PER = 2 * VECS, AHEAD = 4;  // vectors of a row, of both halves
+  const int v = threadIdx.x % PER;
+  uint16_t* half = (v < VECS ? a.c.k : a.c.v) + v % VECS * 8;
+  for (int m = first + static_cast<int>(threadIdx.x) / PER; m < n; m += AHEAD * step) {
+    int x[AHEAD], y[AHEAD];
+    int32_t px[AHEAD], py[AHEAD];
+    uint4 u[AHEAD];
+    bool ok[AHEAD];
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      const bool in = m + e * step < n;
+      x[e] = in ? from[m + e * step] : -1;
+      y[e] = in ? to[m + e * step] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      px[e] = x[e] >= 0 ? a.c.page_of(s, x[e]) : 0;
+      py[e] = x[e] >= 0 ? a.c.page_of(s, y[e]) : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      ok[e] = x[e] >= 0 && a.c.good(px[e]) && a.c.good(py[e]);
+      if (ok[e]) u[e] = *reinterpret_cast<const uint4*>(half + a.c.row(px[e], h, x[e]) * D);
+      else if (x[e] >= 0 && v == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, s);
+    }
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e) {
+      if (!ok[e]) continue;
+      *reinterpret_cast<uint4*>(half + a.c.row(py[e], h, y[e]) * D) = u[e];
+      if (v == 0) a.c.mass[a.c.side(s, h, y[e])] = a.c.mass[a.c.side(s, h, x[e])];
+      if (v == 1 && a.c.pos) a.c.pos[a.c.side(s, h, y[e])] = a.c.pos[a.c.side(s, h, x[e])];
+    }
+  }
+}
+
+// What every CTA of a selection does first: the length out, bad lengths, and whether there is anything to cut.
+struct Cut {
+  int s, h, n;
+  int64_t old;  // the newest position that no longer counts as recent; without a newest one and recent = 0 every one
+  const float* mass;
+  const int32_t* pos;
+};
+__device__ __forceinline__ bool begin_cut(const EvictArgs& a, Cut& c) {
+  const int row = blockIdx.x;
+  c.s = row / a.c.heads;
+  c.h = row % a.c.heads;
+  c.n = a.c.slots(c.s);
+  if (threadIdx.x == 0) {
+    if (c.n != a.c.length[c.s]) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, c.s);
+    if (c.h == 0) a.length_out[c.s] = c.n < a.budget ? c.n : a.budget;
+    if (c.n <= a.budget) a.count[row] = 0;
+  }
+  if (c.n <= a.budget) return false;
+  c.old = a.newest ? static_cast<int64_t>(a.newest[c.s]) - a.recent
+                   : a.c.pos ? static_cast<int64_t>(INT32_MAX) : static_cast<int64_t>(c.n) - 1 - a.recent;
+  c.mass = a.c.mass + a.c.side(c.s, c.h, 0);
+  c.pos = a.c.pos ? a.c.pos + a.c.side(c.s, c.h, 0) : nullptr;
+  return true;
+}
+
+// Rows of up to KEYS * NT slots. Where a row can have few moves only (MOVES: a cache that is cut at every step), its own
+// CTA does them and there is no second launch.
+template <int NT, int D, bool MOVES>
+__global__ void __launch_bounds__(NT) evict_short_kernel(const EvictArgs a) {
+  __shared__ Select<NT> s;
   pdl_wait();
   pdl_trigger();
-  const int row = blockIdx.x, s = row / a.c.heads, h = row % a.c.heads;
-  const int tid = threadIdx.x, lane = tid % 32, w = tid / 32;
-  const int n = a.c.slots(s);
-  if (tid == 0) {
-    if (n != a.c.length[s]) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, s);
-    if (h == 0) a.length_out[s] = n < a.budget ? n : a.budget;
-    if (n <= a.budget) a.count[row] = 0;
+  Cut c;
+  if (!begin_cut(a, c)) return;
+  int32_t* to = a.moves + static_cast<int64_t>(blockIdx.x) * 2 * a.budget;
+  int32_t* from = to + a.budget;
+  const int moves = select_held<NT>(a, s, c.mass, c.pos, c.n, c.old, to, from);
+  if constexpr (MOVES) {
+    __syncthreads();  // the lists are written
+    move_rows<D>(a, c.s, c.h, to, from, moves, 0, NT / (D / 4));
+  } else if (threadIdx.x == 0) {
+    a.count[blockIdx.x] = moves;
   }
-  if (n <= a.budget) return;
-  // the newest position that no longer counts as recent; without a newest one and recent = 0 every one
-  const int64_t old = a.newest ? static_cast<int64_t>(a.newest[s]) - a.recent
-                               : a.c.pos ? static_cast<int64_t>(INT32_MAX) : static_cast<int64_t>(n) - 1 - a.recent;
-  const float* mass = a.c.mass + a.c.side(s, h, 0);
-  const int32_t* pos = a.c.pos ? a.c.pos + a.c.side(s, h, 0) : nullptr;
-  auto read = [&](int i) { return evict_key(a, mass[i], pos ? pos[i] : i, old); };
+}
+
+__global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(const EvictArgs a) {
+  extern __shared__ uint32_t keys[];
+  __shared__ Select<EVICT_THREADS> held_s;
+  __shared__ int counts[2][3][EVICT_WARPS];
+  pdl_wait();
+  pdl_trigger();
+  Cut cut;
+  if (!begin_cut(a, cut)) return;
+  const int row = blockIdx.x, n = cut.n, tid = threadIdx.x, lane = tid % 32, w = tid / 32;
+  int32_t* to = a.moves + static_cast<int64_t>(row) * 2 * a.budget;
+  int32_t* from = to + a.budget;
+  if (n <= KEYS * EVICT_THREADS) {
+    const int moves = select_held<EVICT_THREADS>(a, held_s, cut.mass, cut.pos, n, cut.old, to, from);
+    if (tid == 0) a.count[row] = moves;
+    return;
+  }
+  int* sums = held_s.sums;
+  const float* mass = cut.mass;
+  const int32_t* pos = cut.pos;
+  auto read = [&](int i) { return evict_key(a, mass[i], pos ? pos[i] : i, cut.old); };
   const bool held = n <= a.smem_keys;
   auto key = [&](int i) { return held ? keys[i] : read(i); };
   if (held)
     for (int i = tid; i < n; i += EVICT_THREADS) keys[i] = read(i);
   uint32_t known = 0;
-  int left = a.budget;  // of the keys whose higher bits are `known`, the left-th largest is looked for
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    const uint32_t mask = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
+  __syncthreads();
+  for (int round = 0; round < 16; ++round) {
+    const int shift = 30 - 2 * round;
+    int c[3] = {0, 0, 0};
     for (int i = tid; i < n; i += EVICT_THREADS) {
       const uint32_t x = key(i);
-      if ((x & mask) == known) atomicAdd(&hist[(x >> shift) & 255], 1);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) c[j] += x >= (known | static_cast<uint32_t>(j + 1) << shift);
+    }
+    int(*hits)[EVICT_WARPS] = counts[round & 1];
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      c[j] = __reduce_add_sync(~0u, c[j]);
+      if (lane == 0) hits[j][w] = c[j];
     }
     __syncthreads();
-    if (w == 0) {  // bins from the largest: lane l has bins 255 - 8 l and the seven below it
-      int mine = 0;
-      for (int j = 0; j < 8; ++j) mine += hist[255 - 8 * lane - j];
-      int upto = mine;
-      for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(~0u, upto, o);
-        if (lane >= o) upto += x;
-      }
-      const int above = upto - mine;
-      if (above < left && left <= upto) {
-        int b = 255 - 8 * lane, sum = above;
-        while (sum + hist[b] < left) sum += hist[b--];
-        pick[0] = b;
-        pick[1] = left - sum;
-      }
-    }
-    __syncthreads();
-    known |= static_cast<uint32_t>(pick[0]) << shift;
-    left = pick[1];
-    __syncthreads();
+    int up = 0;  // candidates that the budget-th largest reaches
+#pragma unroll
+    for (int j = 0; j < 3; ++j) up += __reduce_add_sync(~0u, hits[j][lane]) >= a.budget;
+    known |= static_cast<uint32_t>(up) << shift;
   }
+  // the keys above it all stay, and so many of its equals
+  int above = 0, total;
+  for (int i = tid; i < n; i += EVICT_THREADS) above += key(i) > known;
+  block_before<EVICT_WARPS>(__reduce_add_sync(~0u, above), sums, &total);
+  const int left = a.budget - total;
   // every warp has a range of slots, 32 at a time
   const int per = ((n + EVICT_WARPS - 1) / EVICT_WARPS + 31) / 32 * 32;
   const int b0 = min(w * per, n), b1 = min(b0 + per, n);
-  int ties = 0, total;
+  int ties = 0;
   for (int i = b0; i < b1; i += 32) ties += __popc(__ballot_sync(~0u, i + lane < b1 && key(i + lane) == known));
-  const int ties_before = block_before(ties, sums, &total);
+  const int ties_before = block_before<EVICT_WARPS>(ties, sums, &total);
   const unsigned below_me = (1u << lane) - 1;
   // freed and late kept slots of 32 slots from i on, as votes
   auto votes = [&](int i, int& tie, unsigned& freed, unsigned& late) {
@@ -288,10 +518,8 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(EvictArgs a
     n_freed += __popc(freed);
     n_late += __popc(late);
   }
-  int at_to = block_before(n_freed, sums, &total), at_from = block_before(n_late, sums, &total);
+  int at_to = block_before<EVICT_WARPS>(n_freed, sums, &total), at_from = block_before<EVICT_WARPS>(n_late, sums, &total);
   if (tid == 0) a.count[row] = total;  // as many late kept slots as freed ones
-  int32_t* to = a.moves + static_cast<int64_t>(row) * 2 * a.budget;
-  int32_t* from = to + a.budget;
   tie = ties_before;
   for (int i = b0; i < b1; i += 32) {
     votes(i, tie, freed, late);
@@ -302,32 +530,42 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(EvictArgs a
   }
 }
 
-// Moves the listed rows of both halves of the cache with their weights and positions. Sources lie behind
-// the budget and targets below it: no move reads what another one writes.
-constexpr int MOVE_THREADS = 256;
-__global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(EvictArgs a, int D) {
+constexpr int MOVE_THREADS = 256, MOVE_SELF = 64;  // moves of a row that its selection does itself
+template <int D>
+__global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const EvictArgs a) {
   pdl_wait();
   pdl_trigger();
-  const int row = blockIdx.x, s = row / a.c.heads, h = row % a.c.heads;
-  const int n = a.count[row], vecs = D / 8, per = 2 * vecs;  // 16-byte vectors of a row, of both halves
+  const int row = blockIdx.x, n = a.count[row];
+  constexpr int PER = MOVE_THREADS / (D / 4);  // rows of a CTA at a time
   const int32_t* to = a.moves + static_cast<int64_t>(row) * 2 * a.budget;
-  const int32_t* from = to + a.budget;
-  const int64_t items = static_cast<int64_t>(n) * per, step = static_cast<int64_t>(gridDim.y) * MOVE_THREADS;
-  for (int64_t i = static_cast<int64_t>(blockIdx.y) * MOVE_THREADS + threadIdx.x; i < items; i += step) {
-    const int m = static_cast<int>(i / per), v = static_cast<int>(i % per);
-    const int x = from[m], y = to[m];
-    const int32_t px = a.c.page_of(s, x), py = a.c.page_of(s, y);
-    if (!a.c.good(px) || !a.c.good(py)) {
-      if (v == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, s);
-      continue;
-    }
-    uint16_t* half = v < vecs ? a.c.k : a.c.v;
-    const int at = (v < vecs ? v : v - vecs) * 8;
-    *reinterpret_cast<uint4*>(half + a.c.row(py, h, y) * D + at) =
-        *reinterpret_cast<const uint4*>(half + a.c.row(px, h, x) * D + at);
-    if (v == 0) a.c.mass[a.c.side(s, h, y)] = a.c.mass[a.c.side(s, h, x)];
-    if (v == 1 && a.c.pos) a.c.pos[a.c.side(s, h, y)] = a.c.pos[a.c.side(s, h, x)];
+  move_rows<D>(a, row / a.c.heads, row % a.c.heads, to, to + a.budget, n, blockIdx.y * PER, gridDim.y * PER);
+}
+
+template <int D>
+static int evict(const EvictArgs& a, cudaStream_t stream) {
+  const int rows = a.c.seqs * a.c.heads;
+  const int most = a.c.cap - a.budget < a.budget ? a.c.cap - a.budget : a.budget;  // moves of a row
+  if (most <= 0) {  // no row can have more than the budget: lengths alone
+    OM_LAUNCH_PDL("evict_short_kernel", evict_short_kernel<256, D, true>, dim3(rows), dim3(256), 0, stream, a);
+    return ORDERMOE_OK;
   }
+  if (a.c.cap <= KEYS * 256 && most <= MOVE_SELF) {
+    OM_LAUNCH_PDL("evict_short_kernel", evict_short_kernel<256, D, true>, dim3(rows), dim3(256), 0, stream, a);
+    return ORDERMOE_OK;
+  }
+  if (a.c.cap <= KEYS * 256)
+    OM_LAUNCH_PDL("evict_short_kernel", evict_short_kernel<256, D, false>, dim3(rows), dim3(256), 0, stream, a);
+  else if (a.c.cap <= KEYS * EVICT_THREADS)
+    OM_LAUNCH_PDL("evict_short_kernel", evict_short_kernel<EVICT_THREADS, D, false>, dim3(rows), dim3(EVICT_THREADS), 0,
+                  stream, a);
+  else
+    OM_LAUNCH_PDL("evict_select_kernel", evict_select_kernel, dim3(rows), dim3(EVICT_THREADS),
+                  static_cast<size_t>(a.smem_keys) * 4, stream, a);
+  int64_t y = (static_cast<int64_t>(most) * (D / 4) + 4 * MOVE_THREADS - 1) / (4 * MOVE_THREADS);
+  const int64_t fill = 16ll * num_sms() / rows + 1;
+  y = y > fill ? fill : y;
+  OM_LAUNCH_PDL("evict_move_kernel", evict_move_kernel<D>, dim3(rows, static_cast<unsigned>(y)), dim3(MOVE_THREADS), 0, stream, a);
+  return ORDERMOE_OK;
 }
 
 }  // namespace kv
@@ -415,14 +653,7 @@ extern "C" int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int
   a.count = static_cast<int32_t*>(workspace);
   a.moves = a.count + (static_cast<size_t>(rows) + 63) / 64 * 64;
   a.smem_keys = a.c.cap < kv::EVICT_KEYS ? a.c.cap : kv::EVICT_KEYS;
-  OM_LAUNCH_PDL("evict_select_kernel", kv::evict_select_kernel, dim3(rows), dim3(kv::EVICT_THREADS),
-                static_cast<size_t>(a.smem_keys) * 4, stream, a);
-  // rows of more than the budget's slots move at most so many
-  const int64_t most = a.c.cap - static_cast<int64_t>(budget) < budget ? a.c.cap - static_cast<int64_t>(budget) : budget;
-  int64_t y = (most * (cache->dim / 4) + 4 * kv::MOVE_THREADS - 1) / (4 * kv::MOVE_THREADS);
-  const int64_t fill = 16ll * num_sms() / rows + 1;
-  y = y < 1 ? 1 : y > fill ? fill : y;
-  OM_LAUNCH_PDL("evict_move_kernel", kv::evict_move_kernel, dim3(rows, static_cast<unsigned>(y)), dim3(kv::MOVE_THREADS),
-                0, stream, a, static_cast<int>(cache->dim));
-  return ORDERMOE_OK;
+  if (cache->dim == 64) return kv::evict<64>(a, stream);
+  if (cache->dim == 128) return kv::evict<128>(a, stream);
+  return kv::evict<256>(a, stream);
 }
