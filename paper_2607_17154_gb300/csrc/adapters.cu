@@ -24,7 +24,7 @@ constexpr int THREADS = 256;
 constexpr int MAX_R = 128;
 constexpr int MAX_SPLIT = 32;  // CTAs that share K
 constexpr int KB = 64;         // of K a step
-constexpr int NB = 256;        // columns of a CTA of the second product
+constexpr int NB = 128;        // columns of a slice of the second product
 
 struct Args {
   const uint16_t* X; int64_t ldx;
@@ -37,6 +37,7 @@ struct Args {
   void* Y; int64_t ldy;
   int n, R, T, N, K, f32, split, share;  // share: steps of K of a CTA
   int vec_r, vec_y;                      // residual and Y may be moved 16 bytes at a time
+  int rows, ranks;                       // of a tile, in steps of 16 (what shared memory is laid out for)
   float* H;                              // [split][T][R]
 };
 
@@ -61,7 +62,7 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 
 // The tokens of a tile by adapter.
 struct Groups {
-  int id[TILE];       // adapter of each token, -1: none
+  alignas(16) int id[TILE];  // adapter of each token, -1: none
   int leader[TILE];   // the first token of each distinct adapter, in order
   int row[TILE];      // tokens of the adapter in hand, in order
   int warp[4];
@@ -85,8 +86,14 @@ __device__ __forceinline__ void find_groups(const Args& a, Groups& s, int t0, bo
   bool first = false;
   if (tid < TILE) {
     const int id = s.id[tid];
-    first = id >= 0;
-    for (int i = 0; i < tid && first; ++i) first = s.id[i] != id;
+    const unsigned same = __match_any_sync(~0u, id);  // by every lane, with a token or without
+    first = id >= 0 && (same & ((1u << lane) - 1)) == 0;
+    bool seen = false;
+    for (int i = 0; i < tid / 32 * 32; i += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(s.id + i);
+      seen = seen || x.x == id || x.y == id || x.z == id || x.w == id;
+    }
+    first = first && !seen;
     const unsigned v = __ballot_sync(~0u, first);
     if (lane == 0) s.warp[tid / 32] = __popc(v);
   }
@@ -133,8 +140,12 @@ __device__ __forceinline__ uint32_t at64(int row, int vec) { return (row * 8 + (
 // H[split][t][r] over a CTA's steps of K. A step has 64 of K of up to 128 tokens and all ranks in shared memory.
 // Up to 16 tokens: the warps share the step's four products of 16 of K and halves of the ranks, and add up at the end;
 // more: 16 tokens a warp.
-constexpr int X_BYTES = TILE * KB * 2, A_BYTES = MAX_R * KB * 2, DOWN_STAGES = 3;
-constexpr int DOWN_SMEM = DOWN_STAGES * (X_BYTES + A_BYTES);
+constexpr int DOWN_STAGES = 3;
+constexpr int SUMS = 4 * 16 * (MAX_R + 2) * 4;  // bytes of four warps' sums of 16 tokens
+constexpr int down_smem(int rows, int ranks) {
+  const int ring = DOWN_STAGES * (rows + ranks) * KB * 2;
+  return ring > SUMS ? ring : SUMS;
+}
 __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ Groups s;
@@ -146,6 +157,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
   const int k0 = blockIdx.z * a.share, steps_all = (a.K + KB - 1) / KB;
   const int k1 = min(k0 + a.share, steps_all);
   const uint32_t base = smem_u32(ring);
+  const int x_bytes = a.rows * KB * 2, stage_bytes = x_bytes + a.ranks * KB * 2;
   for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
     const int id = s.id[s.leader[d]];
     list_rows(s, id);
@@ -153,7 +165,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
     const int m16 = (rows + 15) / 16 * 16;
     const uint16_t* A = a.A + id * a.stride_a;
     auto fetch = [&](int kb, int stage) {
-      const uint32_t xs = base + stage * (X_BYTES + A_BYTES), as = xs + X_BYTES;
+      const uint32_t xs = base + stage * stage_bytes, as = xs + x_bytes;
       for (int i = tid; i < m16 * 8; i += THREADS) {
         const int row = i / 8, v = i % 8, k = kb * KB + v * 8;
         const int left = row < rows ? min(8, a.K - k) : 0;
@@ -179,7 +191,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
       const int next = kb + DOWN_STAGES - 1;
       if (next < k1) fetch(next, (next - k0) % DOWN_STAGES);
       cp_commit();
-      const uint32_t xs = base + (kb - k0) % DOWN_STAGES * (X_BYTES + A_BYTES), as = xs + X_BYTES;
+      const uint32_t xs = base + (kb - k0) % DOWN_STAGES * stage_bytes, as = xs + x_bytes;
       const int m0 = few ? 0 : w * 16;
       if (m0 >= rows) continue;
 #pragma unroll
@@ -200,20 +212,21 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
     __syncthreads();
     float* H = a.H + (static_cast<int64_t>(blockIdx.z) * a.T + t0) * a.R;
     if (few) {  // four warps have sums of the same ranks
-      float* part = reinterpret_cast<float*>(ring);  // [4][16][MAX_R]
+      float* part = reinterpret_cast<float*>(ring);  // [4][16][LD]
+      constexpr int LD = MAX_R + 2;
 #pragma unroll
       for (int n = 0; n < MAX_R / 8; ++n) {
         if (n * 8 >= r || (n / 2 & 1) != w / 4) continue;
-        float* p = part + (w & 3) * 16 * MAX_R + n * 8 + q4 * 2;
-        *reinterpret_cast<float2*>(p + g * MAX_R) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(p + (g + 8) * MAX_R) = make_float2(acc[n][2], acc[n][3]);
+        float* p = part + (w & 3) * 16 * LD + n * 8 + q4 * 2;
+        *reinterpret_cast<float2*>(p + g * LD) = make_float2(acc[n][0], acc[n][1]);
+        *reinterpret_cast<float2*>(p + (g + 8) * LD) = make_float2(acc[n][2], acc[n][3]);
       }
       __syncthreads();
       for (int i = tid; i < rows * r; i += THREADS) {
         const int row = i / r, c = i % r;
-        const float* p = part + row * MAX_R + c;
+        const float* p = part + row * LD + c;
         H[static_cast<int64_t>(s.row[row]) * a.R + c] =
-            (p[0] + p[16 * MAX_R]) + (p[2 * 16 * MAX_R] + p[3 * 16 * MAX_R]);
+            (p[0] + p[16 * LD]) + (p[2 * 16 * LD] + p[3 * 16 * LD]);
       }
     } else {
 #pragma unroll
@@ -228,25 +241,39 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
   }
 }
 
-// One token's part of Y: eight columns from c on, v their sums.
-__device__ __forceinline__ void put8(const Args& a, int64_t t, int c, float* v) {
-  const int left = min(8, a.N - c);
-  if (left <= 0) return;
-  if (a.res) {
-    const uint16_t* r = a.res + t * a.ldr + c;
-    if (a.vec_r && left == 8) {
-      const uint4 u = *reinterpret_cast<const uint4*>(r);
-      v[0] += bf16_lo(u.x); v[1] += bf16_hi(u.x); v[2] += bf16_lo(u.y); v[3] += bf16_hi(u.y);
-      v[4] += bf16_lo(u.z); v[5] += bf16_hi(u.z); v[6] += bf16_lo(u.w); v[7] += bf16_hi(u.w);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < left) v[i] += bf16_lo(r[i]);
-    }
+// Four of a token's ranks, c and on, from the first kernel's partial sums; zeros behind the rank.
+__device__ __forceinline__ float4 sum_h(const Args& a, int64_t t, int c, int r) {
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (c >= r) return v;
+  const float* h = a.H + t * a.R + c;
+#pragma unroll 8
+  for (int p = 0; p < a.split; ++p, h += static_cast<int64_t>(a.T) * a.R) {
+    const float4 x = *reinterpret_cast<const float4*>(h);
+    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
   }
+  return make_float4(v.x, c + 1 < r ? v.y : 0.0f, c + 2 < r ? v.z : 0.0f, c + 3 < r ? v.w : 0.0f);
+}
+// Eight columns of a token's residual from c on, as they are.
+__device__ __forceinline__ uint4 get8(const Args& a, int64_t t, int c) {
+  const int left = a.N - c;
+  uint4 u = make_uint4(0, 0, 0, 0);
+  if (!a.res || left <= 0) return u;
+  const uint16_t* r = a.res + t * a.ldr + c;
+  if (a.vec_r && left >= 8) return *reinterpret_cast<const uint4*>(r);
+  uint32_t x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = i < left ? r[i] : 0u;
+  return make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+}
+// Y = u + v there.
+__device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint4& u, float* v) {
+  const int left = a.N - c;
+  if (left <= 0) return;
+  v[0] += bf16_lo(u.x); v[1] += bf16_hi(u.x); v[2] += bf16_lo(u.y); v[3] += bf16_hi(u.y);
+  v[4] += bf16_lo(u.z); v[5] += bf16_hi(u.z); v[6] += bf16_lo(u.w); v[7] += bf16_hi(u.w);
   if (a.f32) {
     float* y = static_cast<float*>(a.Y) + t * a.ldy + c;
-    if (a.vec_y && left == 8) {
+    if (a.vec_y && left >= 8) {
       *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
       *reinterpret_cast<float4*>(y + 4) = make_float4(v[4], v[5], v[6], v[7]);
     } else {
@@ -257,7 +284,7 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, float* v) 
     return;
   }
   uint16_t* y = static_cast<uint16_t*>(a.Y) + t * a.ldy + c;
-  if (a.vec_y && left == 8) {
+  if (a.vec_y && left >= 8) {
     *reinterpret_cast<uint4*>(y) =
         make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
   } else {
@@ -267,105 +294,228 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, float* v) 
   }
 }
 
-// Y = residual + scale B H, 256 columns of a tile's j-th distinct adapter. H's fp32 sums become two bf16 parts. The columns
-// of four products of 8 are dealt out so that each thread holds eight in a row: column c of product j is
-// 8 (c / 2) + 2 j + c % 2 of 32. Tokens without an adapter go with the first.
-constexpr int ROW16 = MAX_R * 2;  // bytes of a row of H's parts and of B
-constexpr int UP_SMEM = 2 * TILE * ROW16 + NB * ROW16;
-__device__ __forceinline__ uint32_t at128(int row, int vec) { return row * ROW16 + (vec ^ (row & 7)) * 16; }
-__global__ void __launch_bounds__(THREADS) adapters_up_kernel(const Args a) {
+// Y = residual + scale B H for a tile's j-th distinct adapter, in slices of 128 columns: those of a CTA are
+// blockIdx.z, + gridDim.z and so on, the next one's weights on their way while one is computed. H's fp32 sums become
+// PARTS bf16 parts: two (16 bits) for results of 16 bits, three for those of 32. Warps share the blocks of 16 tokens and, where
+// there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
+// holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
+// residual) is asked for before the first kernel has ended. Tokens without an adapter go with the first.
+constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice
+constexpr int up_smem(int rows, int ranks, int parts) {
+  const int many = (parts * rows + 2 * NB) * up_row(ranks), few = 16 * (MAX_R + 4) * 4;
+  return rows > 16 && many > few ? many : few;  // 16 tokens at most: all adapters have few
+}
+template <int PARTS, int RANKS>
+__global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) adapters_up_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Groups s;
-  pdl_wait();
-  pdl_trigger();
   const int t0 = blockIdx.x * TILE, tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
+  const int ld = up_row(a.ranks), slices = (a.N + NB - 1) / NB, z0 = blockIdx.z, dz = gridDim.z;
+  const uint32_t hs = smem_u32(smem), bs = hs + PARTS * a.rows * ld;
+  bool waited = false;
   find_groups(a, s, t0, false);
-  const int c0 = blockIdx.z * NB;
-  if (blockIdx.y == 0)
-    for (int i = tid; i < TILE * (NB / 8); i += THREADS) {
-      const int row = i / (NB / 8), c = c0 + i % (NB / 8) * 8;
-      if (t0 + row < a.T && s.id[row] < 0) {
-        float v[8] = {};
-        put8(a, t0 + row, c, v);
-      }
-    }
-  const uint32_t hi = smem_u32(smem), lo = hi + TILE * ROW16, bs = lo + TILE * ROW16;
+  if (blockIdx.y == 0) {
+    if (a.res != a.Y)
+      for (int z = z0; z < slices; z += dz)
+        for (int i = tid; i < TILE * (NB / 8); i += THREADS) {
+          const int row = i / (NB / 8), c = z * NB + i % (NB / 8) * 8;
+          if (t0 + row < a.T && s.id[row] < 0) {
+            float v[8] = {};
+            put8(a, t0 + row, c, get8(a, t0 + row, c), v);
+          }
+        }
+  }
   for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
     const int id = s.id[s.leader[d]];
     list_rows(s, id);
     const int rows = s.rows, r = rank_of(a, id, false), rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
     const uint16_t* B = a.B + id * a.stride_b;
-    for (int i = tid; i < NB * rv; i += THREADS) {
-      const int row = i / rv, v = i % rv, left = c0 + row < a.N ? min(8, r - v * 8) : 0;
-      cp16(bs + at128(row, v), left > 0 ? B + (c0 + row) * a.ldb + v * 8 : a.B, left > 0 ? left * 2 : 0);
-    }
-    cp_commit();
-    const int m16 = (rows + 15) / 16 * 16;
-    for (int i = tid; i < m16 * rv * 4; i += THREADS) {  // two ranks of a token
-      const int row = i / (rv * 4), c = i % (rv * 4) * 2;
-      float v[2] = {0.0f, 0.0f};
-      if (row < rows)
-        for (int p = 0; p < a.split; ++p) {
-          const float* h = a.H + (static_cast<int64_t>(p) * a.T + t0 + s.row[row]) * a.R + c;
-          if (c < r) v[0] += h[0];
-          if (c + 1 < r) v[1] += h[1];
+    if (rows <= 16) {  // weights and H in registers, 32 columns a warp and turn
+      float* sum = reinterpret_cast<float*>(smem);  // [16][LD] of H
+      constexpr int LD = RANKS + 4;
+      const int steps = (r + 31) / 32, groups = (a.N + 31) / 32;
+      const float scale = a.scale ? a.scale[id] : 1.0f;
+      int64_t tok[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) tok[h] = g + h * 8 < rows ? t0 + s.row[g + h * 8] : -1;
+      // Within 32 ranks a thread has eight in a row, q4 * 8 and on: two products' shares, of weights and of H alike.
+      uint4 b[4][RANKS / 32], u[2];
+      auto ask = [&](int n) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int col = n * 32 + g / 2 * 8 + j * 2 + g % 2;
+          const uint16_t* from = B + col * a.ldb + q4 * 8;
+#pragma unroll
+          for (int k = 0; k < RANKS / 32; ++k) {
+            b[j][k] = make_uint4(0, 0, 0, 0);
+            const int left = r - k * 32 - q4 * 8;
+            if (col >= a.N || left <= 0) continue;
+            b[j][k] = *reinterpret_cast<const uint4*>(from + k * 32);
+            if (left < 8) {  // columns behind the rank say nothing, whatever they hold
+              uint32_t* x = reinterpret_cast<uint32_t*>(&b[j][k]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                x[e] = 2 * e + 1 < left ? x[e] : 2 * e < left ? x[e] & 0xFFFFu : 0u;
+            }
+          }
         }
-      const uint32_t x = pack_bf16x2(v[0], v[1]);
-      const uint32_t y = pack_bf16x2(v[0] - bf16_lo(x), v[1] - bf16_hi(x));
-      const uint32_t at = at128(row, c / 8) + c % 8 * 2;
-      *reinterpret_cast<uint32_t*>(smem + at) = x;
-      *reinterpret_cast<uint32_t*>(smem + TILE * ROW16 + at) = y;
-    }
-    cp_wait<0>();
-    __syncthreads();
-    const float scale = a.scale ? a.scale[id] : 1.0f;
-    const bool few = rows <= 16;  // 32 columns a warp, else 16 tokens a warp
-    const int m0 = few ? 0 : w * 16;
-    if (m0 < rows)
-      for (int n0 = few ? w * 32 : 0; n0 < (few ? w * 32 + 32 : NB); n0 += 32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (tok[h] >= 0) u[h] = get8(a, tok[h], n * 32 + q4 * 8);
+      };
+      const int n0 = z0 * 8 + w, dn = dz * 8;
+      if (n0 < groups) ask(n0);
+      if (!waited) pdl_wait();
+      waited = true;
+      for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
+        const int row = i / (steps * 8), c = (i - row * steps * 8) * 4;
+        const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        *reinterpret_cast<float4*>(sum + row * LD + c) = v;
+      }
+      __syncthreads();
+      for (int n = n0; n < groups; n += dn) {
+        if (n != n0) ask(n);
         float acc[4][4] = {};
-        for (int k = 0; k < rv / 2; ++k) {
-          uint32_t x[4], y[4], b[2][4];
-          const int row = m0 + (lane & 7) + (lane / 8 % 2) * 8;
-          ldm4(x, hi + at128(row, 2 * k + lane / 16));
-          ldm4(y, lo + at128(row, 2 * k + lane / 16));
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {  // products 2 j and 2 j + 1
-            const int c = lane & 7, col = n0 + c / 2 * 8 + (2 * j + lane / 16) * 2 + c % 2;
-            ldm4(b[j], bs + at128(col, 2 * k + lane / 8 % 2));
-          }
+        for (int k = 0; k < RANKS / 32; ++k) {
+          if (k >= steps) continue;
+          float h[2][8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            mma(acc[j], x, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
-            mma(acc[j], y, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
-          }
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+              *reinterpret_cast<float4*>(&h[e][4 * f]) =
+                  *reinterpret_cast<const float4*>(sum + (g + 8 * e) * LD + k * 32 + q4 * 8 + f * 4);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t x[4];  // rows g, g + 8 of ranks 4 half, + 1, then of + 2, + 3
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float* v = &h[e & 1][4 * half + (e / 2) * 2];
+                x[e] = pack_bf16x2(v[0], v[1]);
+                v[0] -= bf16_lo(x[e]);
+                v[1] -= bf16_hi(x[e]);
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (half == 0) mma(acc[j], x, b[j][k].x, b[j][k].y);
+                else mma(acc[j], x, b[j][k].z, b[j][k].w);
+            }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int row = m0 + g + h * 8;
-          if (row >= rows) continue;
+          if (tok[h] < 0) continue;
           float v[8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             v[2 * j] = acc[j][2 * h] * scale;
             v[2 * j + 1] = acc[j][2 * h + 1] * scale;
           }
-          put8(a, t0 + s.row[row], c0 + n0 + q4 * 8, v);
+          put8(a, tok[h], n * 32 + q4 * 8, u[h], v);
         }
       }
+      __syncthreads();
+      continue;
+    }
+    auto fetch = [&](int z, int buffer) {
+      const int c0 = z * NB;
+      for (int i = tid; i < NB * rv; i += THREADS) {
+        const int row = i / rv, v = i - row * rv, left = c0 + row < a.N ? min(8, r - v * 8) : 0;
+        const int place = (row & ~31) + (row % 8 / 2) * 8 + row % 32 / 8 * 2 + row % 2;  // column c of product j: 8 j + c
+        cp16(bs + (buffer * NB + place) * ld + v * 16, left > 0 ? B + (c0 + row) * a.ldb + v * 8 : a.B, left > 0 ? left * 2 : 0);
+      }
+    };
+    if (z0 < slices) fetch(z0, 0);
+    cp_commit();
+    if (!waited) pdl_wait();
+    waited = true;
+    const int blocks = (rows + 15) / 16, m16 = blocks * 16;
+    for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
+      const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
+      alignas(16) float v[4] = {};
+      if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[row], c, r);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        const uint32_t x = pack_bf16x2(v[0], v[1]), y = pack_bf16x2(v[2], v[3]);
+        *reinterpret_cast<uint2*>(smem + (p * a.rows + row) * ld + c * 2) = make_uint2(x, y);
+        v[0] -= bf16_lo(x); v[1] -= bf16_hi(x); v[2] -= bf16_lo(y); v[3] -= bf16_hi(y);
+      }
+    }
+    const float scale = a.scale ? a.scale[id] : 1.0f;
+    const int share = blocks > 4 ? 1 : blocks > 2 ? 2 : 4;  // warps that share a block of tokens, each up to 128 / share columns
+    const int m0 = w / share * 16, first = w % share;
+    const bool busy = m0 < rows;
+    int64_t tok[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[m0 + g + h * 8] : -1;
+    int buffer = 0;
+    for (int z = z0; z < slices; z += dz, buffer ^= 1) {
+      if (z + dz < slices) fetch(z + dz, buffer ^ 1);
+      cp_commit();
+      uint4 u[4][2];
+      if (busy)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (first + n * share < 4 && tok[h] >= 0) u[n][h] = get8(a, tok[h], z * NB + (first + n * share) * 32 + q4 * 8);
+      cp_wait<1>();
+      __syncthreads();
+      if (busy)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if (first + n * share >= 4) continue;
+          float acc[4][4] = {};
+          for (int k = 0; k < rv / 2; ++k) {
+            uint32_t x[PARTS][4], b[2][4];
+            const int row = m0 + (lane & 7) + (lane / 8 % 2) * 8;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)  // products 2 j and 2 j + 1
+              ldm4(b[j], bs + (buffer * NB + (first + n * share) * 32 + (2 * j + lane / 16) * 8 + (lane & 7)) * ld +
+                             (2 * k + lane / 8 % 2) * 16);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+              ldm4(x[p], hs + (p * a.rows + row) * ld + (2 * k + lane / 16) * 16);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma(acc[j], x[p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (tok[h] < 0) continue;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              v[2 * j] = acc[j][2 * h] * scale;
+              v[2 * j + 1] = acc[j][2 * h + 1] * scale;
+            }
+            put8(a, tok[h], z * NB + (first + n * share) * 32 + q4 * 8, u[n][h], v);
+          }
+        }
+      __syncthreads();  // the buffer is free
+    }
+    cp_wait<0>();
     __syncthreads();
   }
+  if (!waited) pdl_wait();  // never done before the first kernel
 }
 
-// How K is shared out: as many CTAs as fill the SMs twice with the tiles, four steps each at least.
+// How K is shared out: a CTA an SM with the tiles, or up to two where a tile may have many adapters; four steps each at
+// least.
+constexpr int SMS = 152;
 struct Plan {
   int tiles, split, share;
 };
-static Plan plan(int T, int K) {
+static Plan plan(int T, int K, int n) {
   Plan p{};
-  p.tiles = (T + TILE - 1) / TILE;
+  p.tiles = T / TILE + (T % TILE != 0);
   const int steps = (K + KB - 1) / KB;
-  int want = 2 * 152 / p.tiles;
+  const int tokens = T < TILE ? T : TILE, distinct = tokens < n ? tokens : n;
+  int want = 2 * SMS / (p.tiles * distinct);
+  if (want < 4) want = 4;
+  if (want > SMS / p.tiles) want = SMS / p.tiles;
   if (want > MAX_SPLIT) want = MAX_SPLIT;
   if (want > steps / 4) want = steps / 4;
   if (want < 1) want = 1;
@@ -375,8 +525,12 @@ static Plan plan(int T, int K) {
 }
 
 static int adapters_attr() {
-  cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, DOWN_SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, UP_SMEM);
+  const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel, most, down_smem(TILE, MAX_R));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<2, 64>, most, up_smem(TILE, 64, 2));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<2, MAX_R>, most, up_smem(TILE, MAX_R, 2));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<3, 64>, most, up_smem(TILE, 64, 3));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<3, MAX_R>, most, up_smem(TILE, MAX_R, 3));
   return static_cast<int>(e);
 }
 
@@ -392,7 +546,7 @@ static bool sizes_ok(int T, int K, int N, int R) {
 
 extern "C" size_t ordermoe_adapters_workspace_bytes(int T, int K, int N, int R) {
   if (!sizes_ok(T, K, N, R) || T == 0) return 0;
-  const ad::Plan p = ad::plan(T, K);
+  const ad::Plan p = ad::plan(T, K, 1);
   return static_cast<size_t>(p.split) * T * R * 4;
 }
 
@@ -428,11 +582,10 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
       workspace_bytes < ordermoe_adapters_workspace_bytes(T, K, N, R))
     return fail(ORDERMOE_ERR_INVALID_ARG, "adapters: workspace is null, too small or not 256-byte aligned");
   const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB;
-  if (slices > 65535) return fail(ORDERMOE_ERR_UNSUPPORTED_SHAPE, "adapters: need N of at most %d", 65535 * ad::NB);
   static PerDevice attr_;
   const int e = per_device(attr_, ad::adapters_attr);
   if (e != 0) return cuda_fail(static_cast<cudaError_t>(e), "cudaFuncSetAttribute(adapters)");
-  const ad::Plan p = ad::plan(T, K);
+  const ad::Plan p = ad::plan(T, K, n);
   ad::Args a{};
   a.X = X; a.ldx = ldx; a.A = A; a.stride_a = stride_a; a.lda = lda; a.B = B; a.stride_b = stride_b; a.ldb = ldb;
   a.ids = ids; a.rank = rank; a.scale = scale; a.res = residual; a.ldr = ldr; a.Y = Y; a.ldy = ldy;
@@ -440,17 +593,26 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   a.vec_r = ldr % 8 == 0 && r % 16 == 0;
   a.vec_y = ldy % (f32 ? 4 : 8) == 0 && y % 16 == 0;
   a.H = static_cast<float*>(workspace);
+  a.rows = T < ad::TILE ? (T + 15) / 16 * 16 : ad::TILE;
+  a.ranks = (R + 15) / 16 * 16;
   // CTAs for a tile's distinct adapters: as many as it can have, while the grid is not many times the SMs
-  const int distinct = T < n ? (T < ad::TILE ? T : ad::TILE) : (n < ad::TILE ? n : ad::TILE);
+  const int64_t tokens = T < ad::TILE ? T : ad::TILE, distinct = tokens < n ? tokens : n;
   auto side = [&](int64_t others) {
-    const int64_t fill = 8ll * 152 / others + 1;
+    const int64_t fill = 4ll * ad::SMS / others + 1;
     return static_cast<unsigned>(fill < distinct ? fill : distinct);
   };
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel,
                 dim3(p.tiles, side(static_cast<int64_t>(p.tiles) * p.split), p.split), dim3(ad::THREADS),
-                static_cast<size_t>(ad::DOWN_SMEM), stream, a);
-  OM_LAUNCH_PDL("adapters_up_kernel", ad::adapters_up_kernel,
-                dim3(p.tiles, side(p.tiles * slices), static_cast<unsigned>(slices)), dim3(ad::THREADS),
-                static_cast<size_t>(ad::UP_SMEM), stream, a);
+                static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
+  // slices: those of all distinct adapters share the SMs' rooms for CTAs
+  const int parts = f32 ? 3 : 2;
+  const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
+  const unsigned z = static_cast<unsigned>(slices < room ? slices : room);
+  const dim3 grid(p.tiles, side(static_cast<int64_t>(p.tiles) * z), z);
+  const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, a.ranks, parts));
+  const bool low = a.ranks <= 64;  // registers for the weights of few tokens
+  const auto up = f32 ? (low ? ad::adapters_up_kernel<3, 64> : ad::adapters_up_kernel<3, ad::MAX_R>)
+                      : (low ? ad::adapters_up_kernel<2, 64> : ad::adapters_up_kernel<2, ad::MAX_R>);
+  OM_LAUNCH_PDL("adapters_up_kernel", up, grid, dim3(ad::THREADS), smem, stream, a);
   return ORDERMOE_OK;
 }
