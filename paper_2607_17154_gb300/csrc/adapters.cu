@@ -164,18 +164,28 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
     const int rows = s.rows, r = rank_of(a, id, blockIdx.z == 0), rt = (r + 15) / 16 * 16;
     const int m16 = (rows + 15) / 16 * 16;
     const uint16_t* A = a.A + id * a.stride_a;
+    // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
+    const int v = tid % 8;
+    const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + v * 8;
+#pragma unroll
+    for (int e = 0; e < TILE / 32; ++e)
+      xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[tid / 8 + e * 32]) * a.ldx + v * 8 : nullptr;
+    const uint32_t place = base + at64(tid / 8, v);
     auto fetch = [&](int kb, int stage) {
-      const uint32_t xs = base + stage * stage_bytes, as = xs + x_bytes;
-      for (int i = tid; i < m16 * 8; i += THREADS) {
-        const int row = i / 8, v = i % 8, k = kb * KB + v * 8;
-        const int left = row < rows ? min(8, a.K - k) : 0;
-        cp16(xs + at64(row, v), left > 0 ? a.X + (t0 + s.row[row]) * a.ldx + k : a.X, left > 0 ? left * 2 : 0);
-      }
-      for (int i = tid; i < rt * 8; i += THREADS) {
-        const int row = i / 8, v = i % 8, k = kb * KB + v * 8;
-        const int left = row < r ? min(8, a.K - k) : 0;
-        cp16(as + at64(row, v), left > 0 ? A + row * a.lda + k : a.A, left > 0 ? left * 2 : 0);
-      }
+      const uint32_t xs = place + stage * stage_bytes, as = xs + x_bytes;
+      const int left = a.K - kb * KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+#pragma unroll
+      for (int e = 0; e < TILE / 32; ++e)
+        if (tid / 8 + e * 32 < m16) {
+          const bool ok = xp[e] && bytes > 0;
+          cp16(xs + e * 32 * KB * 2, ok ? xp[e] + kb * KB : a.X, ok ? bytes : 0);
+        }
+#pragma unroll
+      for (int e = 0; e < MAX_R / 32; ++e)
+        if (tid / 8 + e * 32 < rt) {
+          const bool ok = tid / 8 + e * 32 < r && bytes > 0;
+          cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + kb * KB : a.A, ok ? bytes : 0);
+        }
     };
     for (int i = 0; i < DOWN_STAGES - 1; ++i) {
       if (k0 + i < k1) fetch(k0 + i, i);
@@ -192,19 +202,32 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
       if (next < k1) fetch(next, (next - k0) % DOWN_STAGES);
       cp_commit();
       const uint32_t xs = base + (kb - k0) % DOWN_STAGES * stage_bytes, as = xs + x_bytes;
-      const int m0 = few ? 0 : w * 16;
-      if (m0 >= rows) continue;
-#pragma unroll
-      for (int k = 0; k < KB / 16; ++k) {
-        if (few && k != (w & 3)) continue;
+      if (few) {
+        const int k = w & 3;
         uint32_t x[4], b[4];
-        ldm4(x, xs + at64(m0 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+        ldm4(x, xs + at64((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
 #pragma unroll
         for (int n = 0; n < MAX_R / 8; n += 2) {
-          if (n * 8 >= r || (few && (n / 2 & 1) != w / 4)) continue;
+          if (n * 8 >= r) break;
+          if ((n / 2 & 1) != w / 4) continue;
           ldm4(b, as + at64(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
           mma(acc[n], x, b[0], b[1]);
           mma(acc[n + 1], x, b[2], b[3]);
+        }
+      } else if (w * 16 < rows) {
+        uint32_t x[KB / 16][4];
+#pragma unroll
+        for (int k = 0; k < KB / 16; ++k) ldm4(x[k], xs + at64(w * 16 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+#pragma unroll
+        for (int n = 0; n < MAX_R / 8; n += 2) {
+          if (n * 8 >= r) break;
+#pragma unroll
+          for (int k = 0; k < KB / 16; ++k) {
+            uint32_t b[4];
+            ldm4(b, as + at64(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
+            mma(acc[n], x[k], b[0], b[1]);
+            mma(acc[n + 1], x[k], b[2], b[3]);
+          }
         }
       }
     }
@@ -264,6 +287,13 @@ __device__ __forceinline__ uint4 get8(const Args& a, int64_t t, int c) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = i < left ? r[i] : 0u;
   return make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+}
+// Whether every eight columns of Y and residual can be moved at once, to bf16.
+__device__ __forceinline__ bool plain_rows(const Args& a) {
+  return a.res && a.vec_r && a.vec_y && !a.f32 && a.N % 8 == 0;
+}
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
 // Y = u + v there.
 __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint4& u, float* v) {
@@ -419,12 +449,17 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
       __syncthreads();
       continue;
     }
+    constexpr int VECS = RANKS / 8, ROWS = THREADS / VECS;  // a thread's vector is tid % VECS, of every ROWS-th column
+    const int fv = tid % VECS, fleft = min(8, r - fv * 8);
+    const uint16_t* fp = B + (tid / VECS) * a.ldb + fv * 8;
     auto fetch = [&](int z, int buffer) {
-      const int c0 = z * NB;
-      for (int i = tid; i < NB * rv; i += THREADS) {
-        const int row = i / rv, v = i - row * rv, left = c0 + row < a.N ? min(8, r - v * 8) : 0;
-        const int place = (row & ~31) + (row % 8 / 2) * 8 + row % 32 / 8 * 2 + row % 2;  // column c of product j: 8 j + c
-        cp16(bs + (buffer * NB + place) * ld + v * 16, left > 0 ? B + (c0 + row) * a.ldb + v * 8 : a.B, left > 0 ? left * 2 : 0);
+      if (fv >= rv) return;
+#pragma unroll
+      for (int e = 0; e < NB / ROWS; ++e) {
+        const int row = tid / VECS + e * ROWS, col = z * NB + row;
+        const int at = (row & ~31) + (row % 8 / 2) * 8 + row % 32 / 8 * 2 + row % 2;  // column c of product j: 8 j + c
+        const bool ok = col < a.N && fleft > 0;
+        cp16(bs + (buffer * NB + at) * ld + fv * 16, ok ? fp + (z * NB + e * ROWS) * a.ldb : a.B, ok ? fleft * 2 : 0);
       }
     };
     if (z0 < slices) fetch(z0, 0);
@@ -432,10 +467,12 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
     if (!waited) pdl_wait();
     waited = true;
     const int blocks = (rows + 15) / 16, m16 = blocks * 16;
+    const float scale = a.scale ? a.scale[id] : 1.0f;
     for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
       const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
       alignas(16) float v[4] = {};
       if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[row], c, r);
+      v[0] *= scale; v[1] *= scale; v[2] *= scale; v[3] *= scale;
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
         const uint32_t x = pack_bf16x2(v[0], v[1]), y = pack_bf16x2(v[2], v[3]);
@@ -443,43 +480,70 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
         v[0] -= bf16_lo(x); v[1] -= bf16_hi(x); v[2] -= bf16_lo(y); v[3] -= bf16_hi(y);
       }
     }
-    const float scale = a.scale ? a.scale[id] : 1.0f;
     const int share = blocks > 4 ? 1 : blocks > 2 ? 2 : 4;  // warps that share a block of tokens, each up to 128 / share columns
     const int m0 = w / share * 16, first = w % share;
     const bool busy = m0 < rows;
     int64_t tok[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[m0 + g + h * 8] : -1;
+    const bool plain = PARTS == 2 && plain_rows(a);
+    const uint16_t* rp[2] = {nullptr, nullptr};
+    uint16_t* yp[2] = {nullptr, nullptr};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (plain && tok[h] >= 0) {
+        rp[h] = a.res + tok[h] * a.ldr + q4 * 8;
+        yp[h] = static_cast<uint16_t*>(a.Y) + tok[h] * a.ldy + q4 * 8;
+      }
+    const uint32_t xa = hs + (m0 + (lane & 7) + (lane / 8 % 2) * 8) * ld + lane / 16 * 16;
+    const uint32_t ba = bs + (lane / 16 * 8 + (lane & 7)) * ld + (lane / 8 % 2) * 16;
     int buffer = 0;
     for (int z = z0; z < slices; z += dz, buffer ^= 1) {
       if (z + dz < slices) fetch(z + dz, buffer ^ 1);
       cp_commit();
       uint4 u[4][2];
-      if (busy)
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+      for (int n = 0; n < 4; ++n)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if (first + n * share < 4 && tok[h] >= 0) u[n][h] = get8(a, tok[h], z * NB + (first + n * share) * 32 + q4 * 8);
+        for (int h = 0; h < 2; ++h) {
+          const int c = z * NB + (first + n * share) * 32;
+          u[n][h] = make_uint4(0, 0, 0, 0);
+          if (!busy || first + n * share >= 4) continue;
+          if (plain) {
+            if (rp[h] && c + q4 * 8 < a.N) u[n][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
+          } else if (tok[h] >= 0) {
+            u[n][h] = get8(a, tok[h], c + q4 * 8);
+          }
+        }
       cp_wait<1>();
       __syncthreads();
       if (busy)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          if (first + n * share >= 4) continue;
+          const int col = (first + n * share) * 32, c = z * NB + col;
+          if (col >= NB || c >= a.N) continue;
           float acc[4][4] = {};
-          for (int k = 0; k < rv / 2; ++k) {
-            uint32_t x[PARTS][4], b[2][4];
-            const int row = m0 + (lane & 7) + (lane / 8 % 2) * 8;
+          if (PARTS == 2)  // results of 16 bits: the residual may be the sums' beginning
 #pragma unroll
-            for (int j = 0; j < 2; ++j)  // products 2 j and 2 j + 1
-              ldm4(b[j], bs + (buffer * NB + (first + n * share) * 32 + (2 * j + lane / 16) * 8 + (lane & 7)) * ld +
-                             (2 * k + lane / 8 % 2) * 16);
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x[4] = {u[n][h].x, u[n][h].y, u[n][h].z, u[n][h].w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                acc[j][2 * h] = bf16_lo(x[j]);
+                acc[j][2 * h + 1] = bf16_hi(x[j]);
+              }
+            }
+          const uint32_t bb = ba + (buffer * NB + col) * ld;
+#pragma unroll 2
+          for (int k = 0; k < rv / 2; ++k) {
+            uint32_t x[4], b[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) ldm4(b[j], bb + j * 16 * ld + k * 32);  // products 2 j and 2 j + 1
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) {
-              ldm4(x[p], hs + (p * a.rows + row) * ld + (2 * k + lane / 16) * 16);
+              ldm4(x, xa + p * a.rows * ld + k * 32);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) mma(acc[j], x[p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
+              for (int j = 0; j < 4; ++j) mma(acc[j], x, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
             }
           }
 #pragma unroll
@@ -488,10 +552,14 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
             float v[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              v[2 * j] = acc[j][2 * h] * scale;
-              v[2 * j + 1] = acc[j][2 * h + 1] * scale;
+              v[2 * j] = acc[j][2 * h];
+              v[2 * j + 1] = acc[j][2 * h + 1];
             }
-            put8(a, tok[h], z * NB + (first + n * share) * 32 + q4 * 8, u[n][h], v);
+            if (plain) {
+              if (c + q4 * 8 < a.N) *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
+            } else {
+              put8(a, tok[h], c + q4 * 8, PARTS == 2 ? make_uint4(0, 0, 0, 0) : u[n][h], v);
+            }
           }
         }
       __syncthreads();  // the buffer is free
@@ -581,7 +649,6 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 ||
       workspace_bytes < ordermoe_adapters_workspace_bytes(T, K, N, R))
     return fail(ORDERMOE_ERR_INVALID_ARG, "adapters: workspace is null, too small or not 256-byte aligned");
-  const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB;
   static PerDevice attr_;
   const int e = per_device(attr_, ad::adapters_attr);
   if (e != 0) return cuda_fail(static_cast<cudaError_t>(e), "cudaFuncSetAttribute(adapters)");
@@ -595,20 +662,17 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   a.H = static_cast<float*>(workspace);
   a.rows = T < ad::TILE ? (T + 15) / 16 * 16 : ad::TILE;
   a.ranks = (R + 15) / 16 * 16;
-  // CTAs for a tile's distinct adapters: as many as it can have, while the grid is not many times the SMs
+  // Two CTAs an SM in all. With few tiles they go to the adapters that a tile can have before its columns; with many a
+  // CTA takes a tile's adapters in turn (one that finds no adapter costs 1.5 us of its SM).
   const int64_t tokens = T < ad::TILE ? T : ad::TILE, distinct = tokens < n ? tokens : n;
-  auto side = [&](int64_t others) {
-    const int64_t fill = 4ll * ad::SMS / others + 1;
-    return static_cast<unsigned>(fill < distinct ? fill : distinct);
-  };
-  OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel,
-                dim3(p.tiles, side(static_cast<int64_t>(p.tiles) * p.split), p.split), dim3(ad::THREADS),
-                static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
-  // slices: those of all distinct adapters share the SMs' rooms for CTAs
-  const int parts = f32 ? 3 : 2;
   const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
-  const unsigned z = static_cast<unsigned>(slices < room ? slices : room);
-  const dim3 grid(p.tiles, side(static_cast<int64_t>(p.tiles) * z), z);
+  auto at_most = [](int64_t v, int64_t most) { return static_cast<unsigned>(v < 1 ? 1 : v < most ? v : most); };
+  OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
+                dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
+  const int parts = f32 ? 3 : 2;
+  const int64_t wide = tokens <= 16 * distinct ? 2 * ad::NB : ad::NB;  // columns of a CTA's turn: few tokens, or more
+  const unsigned z = at_most(p.tiles <= 4 ? room / distinct : room, (N + wide - 1) / wide);
+  const dim3 grid(p.tiles, at_most(room / z, distinct), z);
   const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, a.ranks, parts));
   const bool low = a.ranks <= 64;  // registers for the weights of few tokens
   const auto up = f32 ? (low ? ad::adapters_up_kernel<3, 64> : ad::adapters_up_kernel<3, ad::MAX_R>)

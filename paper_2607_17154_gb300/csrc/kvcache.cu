@@ -50,7 +50,7 @@ CacheView cache_view(const ordermoe_cache* c) {
 namespace kv {
 
 // ------------------------------------------------------------------------- append
-constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_THREADS = 128;
 constexpr int MAX_DIM = 256;
 
 struct AppendArgs {
@@ -81,7 +81,7 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
 // of two vectors of 16 bytes (adjacent pairs: the two next to each other; else half a rotation apart). It is
 // bound by bytes, or with few tokens by the chain sequence - length - page - store: a token's rows are read
 // before that chain, which does not say where they are.
-constexpr int APPEND_AHEAD = 2;      // items of a thread that are read first
+constexpr int APPEND_AHEAD = 3;      // items of a thread that are read first
 constexpr int APPEND_SCAN = 1024;    // sequences whose starts the threads compare all at once
 __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs a) {
   __shared__ float cs[MAX_DIM / 2], sn[MAX_DIM / 2];
