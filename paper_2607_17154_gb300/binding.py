@@ -549,6 +549,31 @@ def ordermoe_selftest_linear_plan(M, N, K, f32=False, device=None):
     return dict(zip(names, plan), kernel=LINEAR_KERNELS[plan[0]])
 
 
+def _device():
+    return torch._C._cuda_getDevice()
+
+
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _rows(t, name, shape, device, dtypes=(_BF16,)):
+    """_matrix for calls that do not read a single row's stride: its checks in one pass (0.65 us for 0.98)."""
+    if t.dtype in dtypes and t.shape == shape and t.get_device() == device:
+        ld, one = t.stride()
+        if one == 1 and ld >= shape[1]:
+            return t.data_ptr(), ld
+    return _matrix(t, name, shape, device, dtypes)
+
+
+def _vector(t, name, dtype, n, device):
+    """_entries, sooner for a sound tensor of one dimension."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == device and t.dim() == 1 and len(t) >= n and t.is_contiguous():
+        return t.data_ptr()
+    return _entries(t, name, dtype, n, device)
+
+
 def make_cache(k, v, table, length, mass=None, pos=None):
     """A paged cache for ordermoe_cache_append, ordermoe_attention_paged and ordermoe_cache_evict over the
     caller's tensors, all on one device: k, v [pages, heads, page, dim] bf16, table [seqs, n] int32 (rows may lie in a
@@ -581,7 +606,7 @@ def make_cache(k, v, table, length, mass=None, pos=None):
 
 
 def _cache(cache):
-    dev = torch.cuda.current_device()
+    dev = _device()
     if cache._device != dev:
         raise ValueError("the cache must be on the current device, cuda:%d" % dev)
     return dev
@@ -601,23 +626,23 @@ def ordermoe_cache_append(cache, k, v, q=None, q_out=None, starts=None, position
     counts the new tokens already."""
     dev, T = _cache(cache), k.shape[0]
     shape = (T, cache.heads * cache.dim)
-    ka, ldk = _matrix(k, "k", shape, dev)
-    va, ldv = _matrix(v, "v", shape, dev)
+    ka, ldk = _rows(k, "k", shape, dev)
+    va, ldv = _rows(v, "v", shape, dev)
     qa = qo = None
     ldq = ldqo = hq = 0
     if q is not None:
         hq = _heads(q, "q", cache.dim)
         shape = (T, hq * cache.dim)
-        qa, ldq = _matrix(q, "q", shape, dev)
-        qo, ldqo = (None, 0) if q_out is None else _matrix(q_out, "q_out", shape, dev)
+        qa, ldq = _rows(q, "q", shape, dev)
+        qo, ldqo = (None, 0) if q_out is None else _rows(q_out, "q_out", shape, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     rc = lib().ordermoe_cache_append(
         ctypes.byref(cache), ka, ldk, va, ldv, qa, ldq, qo, ldqo, T, hq,
-        _entries(starts, "starts", torch.int32, cache.seqs + 1, dev),
-        _entries(position, "position", torch.int32, T, dev),
-        _entries(inv_freq, "inv_freq", torch.float64, 0, dev), rot, bool(adjacent), _raw_stream(stream))
+        _vector(starts, "starts", _I32, cache.seqs + 1, dev),
+        _vector(position, "position", _I32, T, dev),
+        _vector(inv_freq, "inv_freq", torch.float64, 0, dev), rot, bool(adjacent), _raw_stream(stream))
     if rc != OK:
         _check("ordermoe_cache_append", rc)
 
@@ -635,12 +660,12 @@ def ordermoe_attention_paged(cache, q, out, workspace, scale=None, lse=None, wei
     dev = _cache(cache)
     hq = _heads(q, "q", cache.dim)
     shape = (cache.seqs, hq * cache.dim)
-    qa, ldq = _matrix(q, "q", shape, dev)
-    oa, ldo = _matrix(out, "out", shape, dev)
+    qa, ldq = _rows(q, "q", shape, dev)
+    oa, ldo = _rows(out, "out", shape, dev)
     rc = lib().ordermoe_attention_paged(
         ctypes.byref(cache), qa, ldq, hq, cache.dim ** -0.5 if scale is None else scale, oa, ldo,
-        _entries(lse, "lse", torch.float32, cache.seqs * hq, dev), bool(weights),
-        _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
+        _entries(lse, "lse", _F32, cache.seqs * hq, dev), bool(weights),
+        _vector(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
     if rc != OK:
         _check("ordermoe_attention_paged", rc)
 
@@ -654,9 +679,9 @@ def ordermoe_cache_evict(cache, budget, length_out, workspace, newest=None, rece
     positions (newest [seqs] int32: each sequence's last one) and the largest mass stay. length_out [seqs] int32."""
     dev = _cache(cache)
     rc = lib().ordermoe_cache_evict(
-        ctypes.byref(cache), budget, sinks, recent, _entries(newest, "newest", torch.int32, cache.seqs, dev),
-        _entries(length_out, "length_out", torch.int32, cache.seqs, dev),
-        _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
+        ctypes.byref(cache), budget, sinks, recent, _vector(newest, "newest", _I32, cache.seqs, dev),
+        _vector(length_out, "length_out", _I32, cache.seqs, dev),
+        _vector(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(), _raw_stream(stream))
     if rc != OK:
         _check("ordermoe_cache_evict", rc)
 
@@ -690,16 +715,16 @@ def ordermoe_adapters(X, A, Bw, ids, Y, workspace, scale=None, rank=None, residu
         (T, K), (n, R, _), (_, N) = X.shape, A.shape, Y.shape
     except (AttributeError, ValueError):
         raise TypeError("X and Y must be matrices, A and Bw stacks of matrices") from None
-    dev = torch.cuda.current_device()
-    x, ldx = _matrix(X, "X", X.shape, dev)
+    dev = _device()
+    x, ldx = _rows(X, "X", X.shape, dev)
     a, sa, lda = _stack(A, "A", (n, R, K), dev)
     b, sb, ldb = _stack(Bw, "Bw", (n, N, R), dev)
-    y, ldy = _matrix(Y, "Y", (T, N), dev, (torch.bfloat16, torch.float32))
-    r, ldr = _matrix(residual, "residual", (T, N), dev) if residual is not None else (None, 0)
+    y, ldy = _rows(Y, "Y", (T, N), dev, (_BF16, _F32))
+    r, ldr = _rows(residual, "residual", (T, N), dev) if residual is not None else (None, 0)
     rc = lib().ordermoe_adapters(
-        x, ldx, a, sa, lda, b, sb, ldb, _entries(ids, "ids", torch.int32, T, dev),
-        _entries(rank, "rank", torch.int32, n, dev), _entries(scale, "scale", torch.float32, n, dev), n, R, r, ldr, T, N,
-        K, y, ldy, Y.dtype == torch.float32, _entries(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(),
+        x, ldx, a, sa, lda, b, sb, ldb, _vector(ids, "ids", _I32, T, dev),
+        _vector(rank, "rank", _I32, n, dev), _vector(scale, "scale", _F32, n, dev), n, R, r, ldr, T, N,
+        K, y, ldy, Y.dtype == _F32, _vector(workspace, "workspace", torch.uint8, 0, dev), workspace.numel(),
         _raw_stream(stream))
     if rc != OK:
         _check("ordermoe_adapters", rc)

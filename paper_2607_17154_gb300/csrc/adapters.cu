@@ -4,6 +4,8 @@
 // Both are bound by bytes (X, Y and the used adapters' weights), or with few tokens by latency. Tokens come in
 // any order of adapters: a tile is 128 tokens, and a CTA takes the j-th distinct adapter among them with the tokens that
 // have it, so an adapter's weights are read once a tile whatever the order.
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace om {
@@ -20,7 +22,7 @@ int read_clear_err_adapters(unsigned long long* out) {
 namespace ad {
 
 constexpr int TILE = 128;      // tokens among which adapters are looked for
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int MAX_R = 128;
 constexpr int MAX_SPLIT = 32;  // CTAs that share K
 constexpr int KB = 64;         // of K a step
@@ -63,16 +65,20 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 // The tokens of a tile by adapter.
 struct Groups {
   alignas(16) int id[TILE];  // adapter of each token, -1: none
-  int leader[TILE];   // the first token of each distinct adapter, in order
-  int row[TILE];      // tokens of the adapter in hand, in order
-  int warp[4];
-  int distinct, rows;
+  int rank[TILE];            // its ranks in use and its scale
+  float scale[TILE];
+  int leader[TILE];          // the first token of each distinct adapter, in order
+  uint8_t row[WARPS][TILE];  // tokens of the adapter in hand, in order; every warp has a list of its own
+  int warp[TILE / 32];
+  int distinct;
 };
 
-__device__ __forceinline__ void find_groups(const Args& a, Groups& s, int t0, bool tell) {
+// Returns whether a token has no adapter.
+__device__ __forceinline__ bool find_groups(const Args& a, Groups& s, int t0, bool tell) {
   const int tid = threadIdx.x, lane = tid % 32;
+  int id = -1, rank = a.R;
+  float scale = 1.0f;
   if (tid < TILE) {
-    int id = -1;
     if (t0 + tid < a.T) {
       id = a.ids[t0 + tid];
       if (id < -1 || id >= a.n) {
@@ -81,11 +87,12 @@ __device__ __forceinline__ void find_groups(const Args& a, Groups& s, int t0, bo
       }
     }
     s.id[tid] = id;
+    if (id >= 0 && a.rank) rank = a.rank[id];
+    if (id >= 0 && a.scale) scale = a.scale[id];
   }
   __syncthreads();
   bool first = false;
   if (tid < TILE) {
-    const int id = s.id[tid];
     const unsigned same = __match_any_sync(~0u, id);  // by every lane, with a token or without
     first = id >= 0 && (same & ((1u << lane) - 1)) == 0;
     bool seen = false;
@@ -96,6 +103,12 @@ __device__ __forceinline__ void find_groups(const Args& a, Groups& s, int t0, bo
     first = first && !seen;
     const unsigned v = __ballot_sync(~0u, first);
     if (lane == 0) s.warp[tid / 32] = __popc(v);
+    if (rank < 0 || rank > a.R) {
+      if (tell && first) report(&g_err_adapters, ORDERMOE_DEV_BAD_INDEX, id);
+      rank = rank < 0 ? 0 : a.R;
+    }
+    s.rank[tid] = rank;
+    s.scale[tid] = scale;
   }
   __syncthreads();
   if (tid < TILE) {
@@ -105,33 +118,22 @@ __device__ __forceinline__ void find_groups(const Args& a, Groups& s, int t0, bo
     if (first) s.leader[at + __popc(v & ((1u << lane) - 1))] = tid;
     if (tid == TILE - 1) s.distinct = at + __popc(v);
   }
-  __syncthreads();
+  return __syncthreads_or(tid < TILE && t0 + tid < a.T && id < 0);
 }
-// Lists the tokens with adapter `id` (tile's index, in order).
-__device__ __forceinline__ void list_rows(Groups& s, int id) {
-  const int tid = threadIdx.x, lane = tid % 32;
-  __syncthreads();  // the rows before are done with
-  bool on = false;
-  unsigned v = 0;
-  if (tid < TILE) {
-    on = s.id[tid] == id;
-    v = __ballot_sync(~0u, on);
-    if (lane == 0) s.warp[tid / 32] = __popc(v);
+// Lists the tokens with adapter `id` (tile's index, in order) for this warp; their number.
+__device__ __forceinline__ int list_rows(Groups& s, int id) {
+  const int lane = threadIdx.x % 32, w = threadIdx.x / 32;
+  int at = 0;
+  __syncwarp();  // the list before is done with
+#pragma unroll
+  for (int i = 0; i < TILE; i += 32) {
+    const bool on = s.id[i + lane] == id;
+    const unsigned v = __ballot_sync(~0u, on);
+    if (on) s.row[w][at + __popc(v & ((1u << lane) - 1))] = static_cast<uint8_t>(i + lane);
+    at += __popc(v);
   }
-  __syncthreads();
-  if (tid < TILE) {
-    int at = 0;
-    for (int i = 0; i < tid / 32; ++i) at += s.warp[i];
-    if (on) s.row[at + __popc(v & ((1u << lane) - 1))] = tid;
-    if (tid == TILE - 1) s.rows = at + __popc(v);
-  }
-  __syncthreads();
-}
-__device__ __forceinline__ int rank_of(const Args& a, int id, bool tell) {
-  if (!a.rank) return a.R;
-  const int r = a.rank[id];
-  if (tell && (r < 0 || r > a.R) && threadIdx.x == 0) report(&g_err_adapters, ORDERMOE_DEV_BAD_INDEX, id);
-  return r < 0 ? 0 : r > a.R ? a.R : r;
+  __syncwarp();
+  return at;
 }
 
 // 16-byte vectors of rows of 64 (8 vectors), exchanged by the row's lowest three bits.
@@ -140,10 +142,11 @@ __device__ __forceinline__ uint32_t at64(int row, int vec) { return (row * 8 + (
 // H[split][t][r] over a CTA's steps of K. A step has 64 of K of up to 128 tokens and all ranks in shared memory.
 // Up to 16 tokens: the warps share the step's four products of 16 of K and halves of the ranks, and add up at the end;
 // more: 16 tokens a warp.
-constexpr int DOWN_STAGES = 3;
+constexpr int FEW_STAGES = 6, MANY_STAGES = 3;
 constexpr int SUMS = 4 * 16 * (MAX_R + 2) * 4;  // bytes of four warps' sums of 16 tokens
 constexpr int down_smem(int rows, int ranks) {
-  const int ring = DOWN_STAGES * (rows + ranks) * KB * 2;
+  const int many = MANY_STAGES * (rows + ranks) * KB * 2, few = FEW_STAGES * (16 + ranks) * KB * 2;
+  const int ring = many > few && rows > 16 ? many : few;
   return ring > SUMS ? ring : SUMS;
 }
 __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
@@ -157,19 +160,18 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
   const int k0 = blockIdx.z * a.share, steps_all = (a.K + KB - 1) / KB;
   const int k1 = min(k0 + a.share, steps_all);
   const uint32_t base = smem_u32(ring);
-  const int x_bytes = a.rows * KB * 2, stage_bytes = x_bytes + a.ranks * KB * 2;
   for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
-    const int id = s.id[s.leader[d]];
-    list_rows(s, id);
-    const int rows = s.rows, r = rank_of(a, id, blockIdx.z == 0), rt = (r + 15) / 16 * 16;
+    const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead], rt = (r + 15) / 16 * 16;
     const int m16 = (rows + 15) / 16 * 16;
     const uint16_t* A = a.A + id * a.stride_a;
+    const bool few = rows <= 16;
+    const int x_bytes = (few ? 16 : a.rows) * KB * 2, stage_bytes = x_bytes + a.ranks * KB * 2;
     // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
     const int v = tid % 8;
     const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + v * 8;
 #pragma unroll
     for (int e = 0; e < TILE / 32; ++e)
-      xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[tid / 8 + e * 32]) * a.ldx + v * 8 : nullptr;
+      xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[w][tid / 8 + e * 32]) * a.ldx + v * 8 : nullptr;
     const uint32_t place = base + at64(tid / 8, v);
     auto fetch = [&](int kb, int stage) {
       const uint32_t xs = place + stage * stage_bytes, as = xs + x_bytes;
@@ -187,22 +189,29 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
           cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + kb * KB : a.A, ok ? bytes : 0);
         }
     };
-    for (int i = 0; i < DOWN_STAGES - 1; ++i) {
-      if (k0 + i < k1) fetch(k0 + i, i);
-      cp_commit();
-    }
     float acc[MAX_R / 8][4];
 #pragma unroll
     for (int n = 0; n < MAX_R / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-    const bool few = rows <= 16;
-    for (int kb = k0; kb < k1; ++kb) {
-      cp_wait<DOWN_STAGES - 2>();
-      __syncthreads();
-      const int next = kb + DOWN_STAGES - 1;
-      if (next < k1) fetch(next, (next - k0) % DOWN_STAGES);
-      cp_commit();
-      const uint32_t xs = base + (kb - k0) % DOWN_STAGES * stage_bytes, as = xs + x_bytes;
-      if (few) {
+    // The steps through a ring of `stages`; `step` has a step's products.
+    auto steps = [&](auto stages, auto step) {
+      constexpr int STAGES = decltype(stages)::value;
+      for (int i = 0; i < STAGES - 1; ++i) {
+        if (k0 + i < k1) fetch(k0 + i, i);
+        cp_commit();
+      }
+      int stage = 0, free = STAGES - 1;
+      for (int kb = k0; kb < k1; ++kb) {
+        cp_wait<STAGES - 2>();
+        __syncthreads();
+        if (kb + STAGES - 1 < k1) fetch(kb + STAGES - 1, free);
+        cp_commit();
+        free = free + 1 == STAGES ? 0 : free + 1;
+        step(base + stage * stage_bytes, base + stage * stage_bytes + x_bytes);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+      }
+    };
+    if (few)
+      steps(std::integral_constant<int, FEW_STAGES>{}, [&](uint32_t xs, uint32_t as) {
         const int k = w & 3;
         uint32_t x[4], b[4];
         ldm4(x, xs + at64((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
@@ -214,7 +223,10 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
           mma(acc[n], x, b[0], b[1]);
           mma(acc[n + 1], x, b[2], b[3]);
         }
-      } else if (w * 16 < rows) {
+      });
+    else
+      steps(std::integral_constant<int, MANY_STAGES>{}, [&](uint32_t xs, uint32_t as) {
+        if (w * 16 >= rows) return;
         uint32_t x[KB / 16][4];
 #pragma unroll
         for (int k = 0; k < KB / 16; ++k) ldm4(x[k], xs + at64(w * 16 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
@@ -229,8 +241,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
             mma(acc[n + 1], x[k], b[2], b[3]);
           }
         }
-      }
-    }
+      });
     cp_wait<0>();
     __syncthreads();
     float* H = a.H + (static_cast<int64_t>(blockIdx.z) * a.T + t0) * a.R;
@@ -248,7 +259,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
       for (int i = tid; i < rows * r; i += THREADS) {
         const int row = i / r, c = i % r;
         const float* p = part + row * LD + c;
-        H[static_cast<int64_t>(s.row[row]) * a.R + c] =
+        H[static_cast<int64_t>(s.row[w][row]) * a.R + c] =
             (p[0] + p[16 * LD]) + (p[2 * 16 * LD] + p[3 * 16 * LD]);
       }
     } else {
@@ -257,7 +268,7 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int row = w * 16 + g + e / 2 * 8, c = n * 8 + q4 * 2 + e % 2;
-          if (row < rows && c < r) H[static_cast<int64_t>(s.row[row]) * a.R + c] = acc[n][e];
+          if (row < rows && c < r) H[static_cast<int64_t>(s.row[w][row]) * a.R + c] = acc[n][e];
         }
     }
     __syncthreads();
@@ -330,46 +341,43 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
 // there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
 // residual) is asked for before the first kernel has ended. Tokens without an adapter go with the first.
-constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice
+constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice (ranks: 64 or 128)
 constexpr int up_smem(int rows, int ranks, int parts) {
   const int many = (parts * rows + 2 * NB) * up_row(ranks), few = 16 * (MAX_R + 4) * 4;
   return rows > 16 && many > few ? many : few;  // 16 tokens at most: all adapters have few
 }
-template <int PARTS, int RANKS>
+template <int PARTS, int RANKS, bool FEW>
 __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) adapters_up_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Groups s;
   const int t0 = blockIdx.x * TILE, tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
-  const int ld = up_row(a.ranks), slices = (a.N + NB - 1) / NB, z0 = blockIdx.z, dz = gridDim.z;
+  constexpr int ld = up_row(RANKS);
+  const int slices = (a.N + NB - 1) / NB, z0 = blockIdx.z, dz = gridDim.z;
   const uint32_t hs = smem_u32(smem), bs = hs + PARTS * a.rows * ld;
   bool waited = false;
-  find_groups(a, s, t0, false);
-  if (blockIdx.y == 0) {
-    if (a.res != a.Y)
-      for (int z = z0; z < slices; z += dz)
-        for (int i = tid; i < TILE * (NB / 8); i += THREADS) {
-          const int row = i / (NB / 8), c = z * NB + i % (NB / 8) * 8;
-          if (t0 + row < a.T && s.id[row] < 0) {
-            float v[8] = {};
-            put8(a, t0 + row, c, get8(a, t0 + row, c), v);
-          }
+  const bool alone = find_groups(a, s, t0, false);
+  if (alone && blockIdx.y == 0 && a.res != a.Y)
+    for (int z = z0; z < slices; z += dz)
+      for (int i = tid; i < TILE * (NB / 8); i += THREADS) {
+        const int row = i / (NB / 8), c = z * NB + i % (NB / 8) * 8;
+        if (t0 + row < a.T && s.id[row] < 0) {
+          float v[8] = {};
+          put8(a, t0 + row, c, get8(a, t0 + row, c), v);
         }
-  }
+      }
   for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
-    const int id = s.id[s.leader[d]];
-    list_rows(s, id);
-    const int rows = s.rows, r = rank_of(a, id, false), rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
+    const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead], rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
     const uint16_t* B = a.B + id * a.stride_b;
-    if (rows <= 16) {  // weights and H in registers, 32 columns a warp and turn
+    if (FEW && rows <= 16) {  // weights and H in registers, 32 columns a warp and turn
       float* sum = reinterpret_cast<float*>(smem);  // [16][LD] of H
       constexpr int LD = RANKS + 4;
       const int steps = (r + 31) / 32, groups = (a.N + 31) / 32;
-      const float scale = a.scale ? a.scale[id] : 1.0f;
+      const float scale = s.scale[lead];
       int64_t tok[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) tok[h] = g + h * 8 < rows ? t0 + s.row[g + h * 8] : -1;
+      for (int h = 0; h < 2; ++h) tok[h] = g + h * 8 < rows ? t0 + s.row[w][g + h * 8] : -1;
       // Within 32 ranks a thread has eight in a row, q4 * 8 and on: two products' shares, of weights and of H alike.
-      uint4 b[4][RANKS / 32], u[2];
+      uint4 b[4][RANKS / 32], u[2] = {};
       auto ask = [&](int n) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -399,12 +407,11 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
       waited = true;
       for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
         const int row = i / (steps * 8), c = (i - row * steps * 8) * 4;
-        const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         *reinterpret_cast<float4*>(sum + row * LD + c) = v;
       }
       __syncthreads();
       for (int n = n0; n < groups; n += dn) {
-        if (n != n0) ask(n);
         float acc[4][4] = {};
 #pragma unroll
         for (int k = 0; k < RANKS / 32; ++k) {
@@ -434,6 +441,8 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
                 else mma(acc[j], x, b[j][k].z, b[j][k].w);
             }
         }
+        const uint4 now[2] = {u[0], u[1]};
+        if (n + dn < groups) ask(n + dn);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (tok[h] < 0) continue;
@@ -443,7 +452,7 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
             v[2 * j] = acc[j][2 * h] * scale;
             v[2 * j + 1] = acc[j][2 * h + 1] * scale;
           }
-          put8(a, tok[h], n * 32 + q4 * 8, u[h], v);
+          put8(a, tok[h], n * 32 + q4 * 8, now[h], v);
         }
       }
       __syncthreads();
@@ -467,11 +476,11 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
     if (!waited) pdl_wait();
     waited = true;
     const int blocks = (rows + 15) / 16, m16 = blocks * 16;
-    const float scale = a.scale ? a.scale[id] : 1.0f;
+    const float scale = s.scale[lead];
     for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
       const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
       alignas(16) float v[4] = {};
-      if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[row], c, r);
+      if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r);
       v[0] *= scale; v[1] *= scale; v[2] *= scale; v[3] *= scale;
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
@@ -485,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
     const bool busy = m0 < rows;
     int64_t tok[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[m0 + g + h * 8] : -1;
+    for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[w][m0 + g + h * 8] : -1;
     const bool plain = PARTS == 2 && plain_rows(a);
     const uint16_t* rp[2] = {nullptr, nullptr};
     uint16_t* yp[2] = {nullptr, nullptr};
@@ -497,31 +506,48 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
       }
     const uint32_t xa = hs + (m0 + (lane & 7) + (lane / 8 % 2) * 8) * ld + lane / 16 * 16;
     const uint32_t ba = bs + (lane / 16 * 8 + (lane & 7)) * ld + (lane / 8 % 2) * 16;
+    // the residual of a slice's n-th 32 columns of this warp: the next slice's is asked for once this one's is used
+    uint4 u[4][2];
+    auto ask = [&](int n, int z) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = z * NB + (first + n * share) * 32;
+        u[n][h] = make_uint4(0, 0, 0, 0);
+        if (!busy || z >= slices || first + n * share >= 4) continue;
+        if (plain) {
+          if (rp[h] && c + q4 * 8 < a.N) u[n][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
+        } else if (tok[h] >= 0) {
+          u[n][h] = get8(a, tok[h], c + q4 * 8);
+        }
+      }
+    };
+#pragma unroll
+    for (int n = 0; n < 4; ++n) ask(n, z0);
+    // H's parts stay in registers where two CTAs an SM leave room for them
+    constexpr bool HELD = !FEW && PARTS * RANKS <= 128;
+    uint32_t x[HELD ? RANKS / 16 : 1][PARTS][4];
+    auto load_h = [&](int k, uint32_t (&v)[PARTS][4]) {
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) ldm4(v[p], xa + p * a.rows * ld + k * 32);
+    };
+    if constexpr (HELD) {
+      __syncthreads();  // H is written
+      if (busy)
+#pragma unroll
+        for (int k = 0; k < RANKS / 16; ++k)
+          if (2 * k < rv) load_h(k, x[k]);
+    }
     int buffer = 0;
     for (int z = z0; z < slices; z += dz, buffer ^= 1) {
       if (z + dz < slices) fetch(z + dz, buffer ^ 1);
       cp_commit();
-      uint4 u[4][2];
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int c = z * NB + (first + n * share) * 32;
-          u[n][h] = make_uint4(0, 0, 0, 0);
-          if (!busy || first + n * share >= 4) continue;
-          if (plain) {
-            if (rp[h] && c + q4 * 8 < a.N) u[n][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
-          } else if (tok[h] >= 0) {
-            u[n][h] = get8(a, tok[h], c + q4 * 8);
-          }
-        }
       cp_wait<1>();
       __syncthreads();
       if (busy)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const int col = (first + n * share) * 32, c = z * NB + col;
-          if (col >= NB || c >= a.N) continue;
+          if (col >= NB || c >= a.N) continue;  // behind the last column no slice follows
           float acc[4][4] = {};
           if (PARTS == 2)  // results of 16 bits: the residual may be the sums' beginning
 #pragma unroll
@@ -533,18 +559,20 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
                 acc[j][2 * h + 1] = bf16_hi(x[j]);
               }
             }
+          const uint4 rest[2] = {u[n][0], u[n][1]};
+          ask(n, z + dz);
           const uint32_t bb = ba + (buffer * NB + col) * ld;
-#pragma unroll 2
-          for (int k = 0; k < rv / 2; ++k) {
-            uint32_t x[4], b[2][4];
+#pragma unroll
+          for (int k = 0; k < RANKS / 16; ++k) {
+            if (2 * k >= rv) break;
+            uint32_t b[2][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) ldm4(b[j], bb + j * 16 * ld + k * 32);  // products 2 j and 2 j + 1
+            if constexpr (!HELD) load_h(k, x[0]);
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-              ldm4(x, xa + p * a.rows * ld + k * 32);
+            for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) mma(acc[j], x, b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
-            }
+              for (int j = 0; j < 4; ++j) mma(acc[j], x[HELD ? k : 0][p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -558,7 +586,7 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
             if (plain) {
               if (c + q4 * 8 < a.N) *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
             } else {
-              put8(a, tok[h], c + q4 * 8, PARTS == 2 ? make_uint4(0, 0, 0, 0) : u[n][h], v);
+              put8(a, tok[h], c + q4 * 8, PARTS == 2 ? make_uint4(0, 0, 0, 0) : rest[h], v);
             }
           }
         }
@@ -570,8 +598,9 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
   if (!waited) pdl_wait();  // never done before the first kernel
 }
 
-// How K is shared out: a CTA an SM with the tiles, or up to two where a tile may have many adapters; four steps each at
-// least.
+// How K is shared out: two CTAs an SM, with the adapters that a tile may have where there are few tiles (with many, most
+// tiles have one or two); four steps each at least. (4096 tokens on 8 adapters, K 4096, N 14336, R 64, both kernels:
+// one CTA an SM 105 us, two 93.)
 constexpr int SMS = 152;
 struct Plan {
   int tiles, split, share;
@@ -583,7 +612,7 @@ static Plan plan(int T, int K, int n) {
   const int tokens = T < TILE ? T : TILE, distinct = tokens < n ? tokens : n;
   int want = 2 * SMS / (p.tiles * distinct);
   if (want < 4) want = 4;
-  if (want > SMS / p.tiles) want = SMS / p.tiles;
+  if (p.tiles > 4 && want < 2 * SMS / p.tiles) want = 2 * SMS / p.tiles;
   if (want > MAX_SPLIT) want = MAX_SPLIT;
   if (want > steps / 4) want = steps / 4;
   if (want < 1) want = 1;
@@ -595,10 +624,17 @@ static Plan plan(int T, int K, int n) {
 static int adapters_attr() {
   const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel, most, down_smem(TILE, MAX_R));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<2, 64>, most, up_smem(TILE, 64, 2));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<2, MAX_R>, most, up_smem(TILE, MAX_R, 2));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<3, 64>, most, up_smem(TILE, 64, 3));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapters_up_kernel<3, MAX_R>, most, up_smem(TILE, MAX_R, 3));
+  auto up = [&](auto kernel, int ranks, int parts) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, most, up_smem(TILE, ranks, parts));
+  };
+  up(adapters_up_kernel<2, 64, false>, 64, 2);
+  up(adapters_up_kernel<2, 64, true>, 64, 2);
+  up(adapters_up_kernel<2, MAX_R, false>, MAX_R, 2);
+  up(adapters_up_kernel<2, MAX_R, true>, MAX_R, 2);
+  up(adapters_up_kernel<3, 64, false>, 64, 3);
+  up(adapters_up_kernel<3, 64, true>, 64, 3);
+  up(adapters_up_kernel<3, MAX_R, false>, MAX_R, 3);
+  up(adapters_up_kernel<3, MAX_R, true>, MAX_R, 3);
   return static_cast<int>(e);
 }
 
@@ -670,13 +706,16 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
                 dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
   const int parts = f32 ? 3 : 2;
-  const int64_t wide = tokens <= 16 * distinct ? 2 * ad::NB : ad::NB;  // columns of a CTA's turn: few tokens, or more
+  const bool few = tokens <= 16 * distinct;  // 16 tokens of an adapter in a tile or fewer, in the mean of all that it can have
+  const int64_t wide = few ? 2 * ad::NB : ad::NB;  // columns of a CTA's turn
   const unsigned z = at_most(p.tiles <= 4 ? room / distinct : room, (N + wide - 1) / wide);
   const dim3 grid(p.tiles, at_most(room / z, distinct), z);
-  const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, a.ranks, parts));
   const bool low = a.ranks <= 64;  // registers for the weights of few tokens
-  const auto up = f32 ? (low ? ad::adapters_up_kernel<3, 64> : ad::adapters_up_kernel<3, ad::MAX_R>)
-                      : (low ? ad::adapters_up_kernel<2, 64> : ad::adapters_up_kernel<2, ad::MAX_R>);
+  const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, low ? 64 : ad::MAX_R, parts));
+  const auto up = f32 ? (low ? (few ? ad::adapters_up_kernel<3, 64, true> : ad::adapters_up_kernel<3, 64, false>)
+                             : (few ? ad::adapters_up_kernel<3, ad::MAX_R, true> : ad::adapters_up_kernel<3, ad::MAX_R, false>))
+                      : (low ? (few ? ad::adapters_up_kernel<2, 64, true> : ad::adapters_up_kernel<2, 64, false>)
+                             : (few ? ad::adapters_up_kernel<2, ad::MAX_R, true> : ad::adapters_up_kernel<2, ad::MAX_R, false>));
   OM_LAUNCH_PDL("adapters_up_kernel", up, grid, dim3(ad::THREADS), smem, stream, a);
   return ORDERMOE_OK;
 }

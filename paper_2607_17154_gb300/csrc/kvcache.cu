@@ -63,7 +63,7 @@ struct AppendArgs {
   const int32_t* starts;
   const int32_t* position;
   const double* inv_freq;
-  int rot, adjacent;
+  int rot;
 };
 
 __device__ __forceinline__ void unpack8(const uint4& u, float* f) {
@@ -83,8 +83,9 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
 // before that chain, which does not say where they are.
 constexpr int APPEND_AHEAD = 3;      // items of a thread that are read first
 constexpr int APPEND_SCAN = 1024;    // sequences whose starts the threads compare all at once
+template <bool ADJACENT>
 __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs a) {
-  __shared__ float cs[MAX_DIM / 2], sn[MAX_DIM / 2];
+  __shared__ float2 turn_of[MAX_DIM / 2 + MAX_DIM / 16];  // cos, sin; one entry left out after eight: no bank is met twice
   pdl_wait();
   pdl_trigger();
   const int t = blockIdx.x, D = a.D, H = a.c.heads, tid = threadIdx.x;
@@ -93,8 +94,8 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
   auto vectors = [&](int i, int& x, int& y) {  // of item i, in its head; true: to be turned
     const int head = i >> log_pairs, p = i & ((1 << log_pairs) - 1);
     const bool in = p < a.rot / 16;
-    x = a.adjacent || !in ? p * 16 : p * 8;
-    y = a.adjacent || !in ? x + 8 : x + half;
+    x = ADJACENT || !in ? p * 16 : p * 8;
+    y = ADJACENT || !in ? x + 8 : x + half;
     return in && head < nq + H;
   };
   auto source = [&](int i) {
@@ -119,7 +120,9 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     for (int i = tid; i < half; i += APPEND_THREADS) {
       double v = static_cast<double>(pos) * a.inv_freq[i] * 0.15915494309189533577;  // 1 / (2 pi)
       v -= rint(v);
-      sincospif(static_cast<float>(2.0 * v), &sn[i], &cs[i]);
+      float2 c;
+      sincospif(static_cast<float>(2.0 * v), &c.y, &c.x);
+      turn_of[i + i / 8] = c;
     }
   };
   const int given = a.position ? a.position[t] : 0;
@@ -160,7 +163,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     for (int h = tid; h < H; h += APPEND_THREADS) a.c.mass[a.c.side(s, h, slot)] = 0.0f;
   __syncthreads();
   auto finish = [&](int i, const uint4& u, const uint4& w) {
-    const int head = i >> log_pairs, f = (i & ((1 << log_pairs) - 1)) * 8;
+    const int head = i >> log_pairs, f = (i & ((1 << log_pairs) - 1)) * 9;
     int x, y;
     const bool turn = vectors(i, x, y);
     uint16_t* dst = head < nq ? a.q_out + t * a.ldqo + static_cast<int64_t>(head) * D
@@ -176,16 +179,11 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     unpack8(w, m + 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float c = cs[f + j], z = sn[f + j];
-      const float e = a.adjacent ? m[2 * j] : m[j], o = a.adjacent ? m[2 * j + 1] : m[8 + j];
-      const float e2 = e * c - o * z, o2 = e * z + o * c;
-      if (a.adjacent) {
-        m[2 * j] = e2;
-        m[2 * j + 1] = o2;
-      } else {
-        m[j] = e2;
-        m[8 + j] = o2;
-      }
+      const float2 c = turn_of[f + j];
+      float &e = ADJACENT ? m[2 * j] : m[j], &o = ADJACENT ? m[2 * j + 1] : m[8 + j];
+      const float turned = e * c.x - o * c.y;
+      o = e * c.y + o * c.x;
+      e = turned;
     }
     *reinterpret_cast<uint4*>(dst + x) = pack8(m);
     *reinterpret_cast<uint4*>(dst + y) = pack8(m + 8);
@@ -249,6 +247,8 @@ template <int NT>
 struct Select {
   static constexpr int WARPS = NT / 32;
   int hits[16][3];
+  uint32_t near[NT];  // the keys that are still counted, once they are one a thread
+  int n_near;
   int sums[WARPS];
   int block[KEYS * WARPS];  // of 32 slots each, in order
 };
@@ -282,34 +282,78 @@ __device__ __forceinline__ int select_held(const EvictArgs& a, Select<NT>& s, co
   const unsigned below = (1u << lane) - 1;
   uint32_t key[KEYS];
 #pragma unroll
-  for (int k = 0; k < KEYS; ++k) {
-    const int i = k * NT + tid;
-    key[k] = i < n ? evict_key(a, mass[i], pos ? pos[i] : i, old) : 0u;
+  for (int half = 0; half < KEYS; half += KEYS / 2) {  // eight loads of each kind on their way at a time
+    float m[KEYS / 2];
+    int p[KEYS / 2];
+#pragma unroll
+    for (int k = 0; k < KEYS / 2; ++k) {
+      const int i = min((half + k) * NT + tid, n - 1);
+      m[k] = (half + k) * NT < n ? mass[i] : 0.0f;
+      p[k] = (half + k) * NT < n && pos ? pos[i] : i;
+    }
+#pragma unroll
+    for (int k = 0; k < KEYS / 2; ++k)
+      key[half + k] = (half + k) * NT + tid < n ? evict_key(a, m[k], p[k], old) : 0u;
   }
   if (tid < 48) s.hits[tid / 3][tid % 3] = 0;
+  if (tid == 0) s.n_near = 0;
   __syncthreads();
-  uint32_t known = 0;
-  bool exact = false;
+  uint32_t known = 0, mine = key[0];
+  int reach = n, upper = 0;  // keys that reach `known`, and the bound above it
+  int base = 0;              // near: keys above the bound, which are counted no more
+  bool exact = false, near = n <= NT;
   for (int round = 0; round < 16 && !exact; ++round) {
     const int shift = 30 - 2 * round;
     const uint32_t c1 = known | 1u << shift, c2 = known | 2u << shift, c3 = known | 3u << shift;
     uint32_t c = 0;  // three counts of ten bits: 512 a warp at most
+    if (near) {
+      c = (mine >= c1 ? 1u : 0u) + (mine >= c2 ? 1u << 10 : 0u) + (mine >= c3 ? 1u << 20 : 0u);
+    } else {
 #pragma unroll
-    for (int k = 0; k < KEYS; ++k) {
-      if (k * NT >= n) break;
-      c += (key[k] >= c1 ? 1u : 0u) + (key[k] >= c2 ? 1u << 10 : 0u) + (key[k] >= c3 ? 1u << 20 : 0u);
+      for (int k = 0; k < KEYS; ++k) {
+        if (k * NT >= n) break;
+        c += (key[k] >= c1 ? 1u : 0u) + (key[k] >= c2 ? 1u << 10 : 0u) + (key[k] >= c3 ? 1u << 20 : 0u);
+      }
     }
     c = __reduce_add_sync(~0u, c);
-    if (lane < 3) atomicAdd(&s.hits[round][lane], static_cast<int>(c >> (10 * lane) & 1023u));
+    if (lane < 3 && c != 0) atomicAdd(&s.hits[round][lane], static_cast<int>(c >> (10 * lane) & 1023u));
     __syncthreads();
     int up = 0;
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      const int h = s.hits[round][j];
-      up += h >= a.budget;
+      const int h = s.hits[round][j] + base;
+      if (h >= a.budget) {
+        ++up;
+        reach = h;
+      } else if (up == j) {
+        upper = h;
+      }
       exact = exact || h == a.budget;
     }
     known |= static_cast<uint32_t>(up) << shift;
+    if (near || reach - upper > NT) continue;
+    // what lies in [known, known + 2^shift) is one a thread at most
+    const uint32_t span = (1u << shift) - 1;
+    int here = 0;
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (k * NT >= n) break;
+      here += __popc(__ballot_sync(~0u, k * NT + tid < n && key[k] - known <= span));
+    }
+    int at = lane == 0 ? atomicAdd(&s.n_near, here) : 0;
+    at = __shfl_sync(~0u, at, 0);
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (k * NT >= n) break;
+      const bool in = k * NT + tid < n && key[k] - known <= span;
+      const unsigned v = __ballot_sync(~0u, in);
+      if (in) s.near[at + __popc(v & below)] = key[k];
+      at += __popc(v);
+    }
+    __syncthreads();
+    mine = tid < reach - upper ? s.near[tid] : 0u;
+    base = upper;
+    near = true;
   }
   // Kept: keys above `known`, and of those equal to it the first `left`. Exactly as many keys as the budget reach an exact one.
   int left = n, total = 0;
@@ -607,8 +651,9 @@ extern "C" int ordermoe_cache_append(const ordermoe_cache* cache, const uint16_t
   a.c = cache_view(cache);
   a.D = cache->dim; a.Hq = q_heads; a.T = T;
   a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.q = q; a.ldq = ldq; a.q_out = q_out; a.ldqo = ldqo;
-  a.starts = starts; a.position = position; a.inv_freq = inv_freq; a.rot = rot_dim; a.adjacent = adjacent != 0;
-  OM_LAUNCH_PDL("append_kernel", kv::append_kernel, dim3(T), dim3(kv::APPEND_THREADS), 0, stream, a);
+  a.starts = starts; a.position = position; a.inv_freq = inv_freq; a.rot = rot_dim;
+  const auto kernel = adjacent ? kv::append_kernel<true> : kv::append_kernel<false>;
+  OM_LAUNCH_PDL("append_kernel", kernel, dim3(T), dim3(kv::APPEND_THREADS), 0, stream, a);
   return ORDERMOE_OK;
 }
 
