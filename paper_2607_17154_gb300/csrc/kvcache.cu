@@ -404,16 +404,20 @@ __device__ __forceinline__ int select_held(const EvictArgs& a, Select<NT>& s, co
 // Moves some of the listed rows of both halves of the cache with their weights and positions: threads that share a
 // 16-byte vector of `AHEAD` rows at a time, rows first and on by `step`. Sources lie behind the budget and targets below it: no
 // move reads what another one writes.
+constexpr int MOVE_AHEAD = 2;  // (64 heads of 1500 to 16383 slots to 2048, both launches: 1 row 55 us, 2 48, 4 49, 8 56)
 template <int D>
 __device__ __forceinline__ void move_rows(const EvictArgs& a, int s, int h, const int32_t* to, const int32_t* from, int n,
                                           int first, int step) {
-  constexpr int VECS = D / 8, PER = 2 * VECS, AHEAD = 4;  // vectors of a row, of both halves
+  constexpr int VECS = D / 8, PER = 2 * VECS, AHEAD = MOVE_AHEAD;  // vectors of a row, of both halves
   const int v = threadIdx.x % PER;
   uint16_t* half = (v < VECS ? a.c.k : a.c.v) + v % VECS * 8;
+  uint32_t* beside = v == 0 ? reinterpret_cast<uint32_t*>(a.c.mass) : v == 1 ? reinterpret_cast<uint32_t*>(a.c.pos) : nullptr;
+  if (beside) beside += a.c.side(s, h, 0);
   for (int m = first + static_cast<int>(threadIdx.x) / PER; m < n; m += AHEAD * step) {
     int x[AHEAD], y[AHEAD];
     int32_t px[AHEAD], py[AHEAD];
     uint4 u[AHEAD];
+    uint32_t w[AHEAD];  // weight or position, by the threads of a row's first vectors
     bool ok[AHEAD];
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e) {
@@ -429,15 +433,16 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int s, int h, cons
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e) {
       ok[e] = x[e] >= 0 && a.c.good(px[e]) && a.c.good(py[e]);
-      if (ok[e]) u[e] = *reinterpret_cast<const uint4*>(half + a.c.row(px[e], h, x[e]) * D);
-      else if (x[e] >= 0 && v == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, s);
+      if (ok[e]) {
+        u[e] = *reinterpret_cast<const uint4*>(half + a.c.row(px[e], h, x[e]) * D);
+        if (beside) w[e] = beside[x[e]];
+      } else if (x[e] >= 0 && v == 0) report(&g_err_cache, ORDERMOE_DEV_BAD_INDEX, s);
     }
 #pragma unroll
     for (int e = 0; e < AHEAD; ++e) {
       if (!ok[e]) continue;
       *reinterpret_cast<uint4*>(half + a.c.row(py[e], h, y[e]) * D) = u[e];
-      if (v == 0) a.c.mass[a.c.side(s, h, y[e])] = a.c.mass[a.c.side(s, h, x[e])];
-      if (v == 1 && a.c.pos) a.c.pos[a.c.side(s, h, y[e])] = a.c.pos[a.c.side(s, h, x[e])];
+      if (beside) beside[y[e]] = w[e];
     }
   }
 }
@@ -605,8 +610,8 @@ static int evict(const EvictArgs& a, cudaStream_t stream) {
   else
     OM_LAUNCH_PDL("evict_select_kernel", evict_select_kernel, dim3(rows), dim3(EVICT_THREADS),
                   static_cast<size_t>(a.smem_keys) * 4, stream, a);
-  int64_t y = (static_cast<int64_t>(most) * (D / 4) + 4 * MOVE_THREADS - 1) / (4 * MOVE_THREADS);
-  const int64_t fill = 16ll * num_sms() / rows + 1;
+  int64_t y = (static_cast<int64_t>(most) * (D / 4) + MOVE_AHEAD * MOVE_THREADS - 1) / (MOVE_AHEAD * MOVE_THREADS);
+  const int64_t fill = 48ll * num_sms() / rows + 1;
   y = y > fill ? fill : y;
   OM_LAUNCH_PDL("evict_move_kernel", evict_move_kernel<D>, dim3(rows, static_cast<unsigned>(y)), dim3(MOVE_THREADS), 0, stream, a);
   return ORDERMOE_OK;
