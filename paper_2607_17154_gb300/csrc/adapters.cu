@@ -299,9 +299,11 @@ __device__ __forceinline__ uint4 get8(const Args& a, int64_t t, int c) {
   for (int i = 0; i < 8; ++i) x[i] = i < left ? r[i] : 0u;
   return make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
 }
-// Whether every eight columns of Y and residual can be moved at once, to bf16.
-__device__ __forceinline__ bool plain_rows(const Args& a) {
-  return a.res && a.vec_r && a.vec_y && !a.f32 && a.N % 8 == 0;
+// One column of Y, u its residual's bits.
+__device__ __forceinline__ void put1(const Args& a, int64_t t, int c, uint32_t u, float v) {
+  v += bf16_lo(u);
+  if (a.f32) static_cast<float*>(a.Y)[t * a.ldy + c] = v;
+  else static_cast<uint16_t*>(a.Y)[t * a.ldy + c] = static_cast<uint16_t>(pack_bf16x2(v, 0.0f));
 }
 __device__ __forceinline__ uint4 pack8(const float* v) {
   return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
@@ -342,29 +344,36 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
 // residual) is asked for before the first kernel has ended. Tokens without an adapter go with the first.
 constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice (ranks: 64 or 128)
+constexpr int TURN = WARPS * 16 * 33 * 4;
 constexpr int up_smem(int rows, int ranks, int parts) {
-  const int many = (parts * rows + 2 * NB) * up_row(ranks), few = 16 * (MAX_R + 4) * 4;
+  const int many = TURN + (parts * rows + 2 * NB) * up_row(ranks), few = 16 * (MAX_R + 4) * 4;
   return rows > 16 && many > few ? many : few;  // 16 tokens at most: all adapters have few
 }
-template <int PARTS, int RANKS, bool FEW>
+template <int PARTS, int RANKS, bool FEW, bool PLAIN>
 __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) adapters_up_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Groups s;
   const int t0 = blockIdx.x * TILE, tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
   constexpr int ld = up_row(RANKS);
   const int slices = (a.N + NB - 1) / NB, z0 = blockIdx.z, dz = gridDim.z;
-  const uint32_t hs = smem_u32(smem), bs = hs + PARTS * a.rows * ld;
+  float* const turn = reinterpret_cast<float*>(smem) + w * 16 * 33;  // 16 tokens x 32 columns a warp
+  const uint32_t hs = smem_u32(smem) + TURN, bs = hs + PARTS * a.rows * ld;
   bool waited = false;
   const bool alone = find_groups(a, s, t0, false);
-  if (alone && blockIdx.y == 0 && a.res != a.Y)
+  if (alone && blockIdx.y == 0 && a.res != a.Y) {
+    const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
     for (int z = z0; z < slices; z += dz)
-      for (int i = tid; i < TILE * (NB / 8); i += THREADS) {
-        const int row = i / (NB / 8), c = z * NB + i % (NB / 8) * 8;
-        if (t0 + row < a.T && s.id[row] < 0) {
+      for (int i = tid; i < TILE * (by8 ? NB / 8 : NB); i += THREADS) {
+        const int row = by8 ? i / (NB / 8) : i / NB, c = z * NB + (by8 ? i % (NB / 8) * 8 : i % NB);
+        if (t0 + row >= a.T || s.id[row] >= 0 || c >= a.N) continue;
+        if (by8) {
           float v[8] = {};
           put8(a, t0 + row, c, get8(a, t0 + row, c), v);
+        } else {
+          put1(a, t0 + row, c, a.res ? a.res[static_cast<int64_t>(t0 + row) * a.ldr + c] : 0u, 0.0f);
         }
       }
+  }
   for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
     const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead], rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
     const uint16_t* B = a.B + id * a.stride_b;
@@ -485,7 +494,7 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
         const uint32_t x = pack_bf16x2(v[0], v[1]), y = pack_bf16x2(v[2], v[3]);
-        *reinterpret_cast<uint2*>(smem + (p * a.rows + row) * ld + c * 2) = make_uint2(x, y);
+        *reinterpret_cast<uint2*>(smem + TURN + (p * a.rows + row) * ld + c * 2) = make_uint2(x, y);
         v[0] -= bf16_lo(x); v[1] -= bf16_hi(x); v[2] -= bf16_lo(y); v[3] -= bf16_hi(y);
       }
     }
@@ -495,34 +504,40 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
     int64_t tok[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[w][m0 + g + h * 8] : -1;
-    const bool plain = PARTS == 2 && plain_rows(a);
     const uint16_t* rp[2] = {nullptr, nullptr};
     uint16_t* yp[2] = {nullptr, nullptr};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      if (plain && tok[h] >= 0) {
+      if (PLAIN && tok[h] >= 0) {
         rp[h] = a.res + tok[h] * a.ldr + q4 * 8;
         yp[h] = static_cast<uint16_t*>(a.Y) + tok[h] * a.ldy + q4 * 8;
       }
     const uint32_t xa = hs + (m0 + (lane & 7) + (lane / 8 % 2) * 8) * ld + lane / 16 * 16;
     const uint32_t ba = bs + (lane / 16 * 8 + (lane & 7)) * ld + (lane / 8 % 2) * 16;
-    // the residual of a slice's n-th 32 columns of this warp: the next slice's is asked for once this one's is used
-    uint4 u[4][2];
-    auto ask = [&](int n, int z) {
+    // The residual is asked for ahead. In vectors: that of a slice's n-th 32 columns of this warp, once the slice before
+    // has used its own. Else a column a lane, of 16 tokens, two times 32 columns ahead.
+    const int count = 4 / share;  // times 32 columns of a slice that this warp has
+    uint4 u[PLAIN ? 4 : 1][2];
+    uint16_t one[PLAIN ? 1 : 2][16];
+    auto ask = [&](int set, int n, int z) {  // `set` is known when this is compiled: an index of registers
+      const int c = z * NB + (first + n * share) * 32;
+      if constexpr (PLAIN) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = z * NB + (first + n * share) * 32;
-        u[n][h] = make_uint4(0, 0, 0, 0);
-        if (!busy || z >= slices || first + n * share >= 4) continue;
-        if (plain) {
-          if (rp[h] && c + q4 * 8 < a.N) u[n][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
-        } else if (tok[h] >= 0) {
-          u[n][h] = get8(a, tok[h], c + q4 * 8);
+        for (int h = 0; h < 2; ++h) {
+          u[set][h] = make_uint4(0, 0, 0, 0);
+          if (busy && z < slices && n < count && rp[h] && c + q4 * 8 < a.N) u[set][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          one[set][e] = 0;
+          if (busy && a.res && z < slices && n < count && c + lane < a.N && m0 + e < rows)
+            one[set][e] = a.res[static_cast<int64_t>(t0 + s.row[w][m0 + e]) * a.ldr + c + lane];
         }
       }
     };
 #pragma unroll
-    for (int n = 0; n < 4; ++n) ask(n, z0);
+    for (int n = 0; n < (PLAIN ? 4 : 2); ++n) ask(n, n, z0);
     // H's parts stay in registers where two CTAs an SM leave room for them
     constexpr bool HELD = !FEW && PARTS * RANKS <= 128;
     uint32_t x[HELD ? RANKS / 16 : 1][PARTS][4];
@@ -547,9 +562,9 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const int col = (first + n * share) * 32, c = z * NB + col;
-          if (col >= NB || c >= a.N) continue;  // behind the last column no slice follows
+          if (n >= count || c >= a.N) continue;  // behind the last column no slice follows
           float acc[4][4] = {};
-          if (PARTS == 2)  // results of 16 bits: the residual may be the sums' beginning
+          if constexpr (PLAIN)  // results of 16 bits: the residual may be the sums' beginning
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t x[4] = {u[n][h].x, u[n][h].y, u[n][h].z, u[n][h].w};
@@ -559,8 +574,7 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
                 acc[j][2 * h + 1] = bf16_hi(x[j]);
               }
             }
-          const uint4 rest[2] = {u[n][0], u[n][1]};
-          ask(n, z + dz);
+          if constexpr (PLAIN) ask(n, n, z + dz);
           const uint32_t bb = ba + (buffer * NB + col) * ld;
 #pragma unroll
           for (int k = 0; k < RANKS / 16; ++k) {
@@ -574,20 +588,31 @@ __global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) ad
 #pragma unroll
               for (int j = 0; j < 4; ++j) mma(acc[j], x[HELD ? k : 0][p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
           }
+          if (PLAIN) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (tok[h] < 0) continue;
-            float v[8];
+            for (int h = 0; h < 2; ++h) {
+              if (tok[h] < 0 || c + q4 * 8 >= a.N) continue;
+              float v[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              v[2 * j] = acc[j][2 * h];
-              v[2 * j + 1] = acc[j][2 * h + 1];
+              for (int j = 0; j < 4; ++j) {
+                v[2 * j] = acc[j][2 * h];
+                v[2 * j + 1] = acc[j][2 * h + 1];
+              }
+              *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
             }
-            if (plain) {
-              if (c + q4 * 8 < a.N) *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
-            } else {
-              put8(a, tok[h], c + q4 * 8, PARTS == 2 ? make_uint4(0, 0, 0, 0) : rest[h], v);
-            }
+          } else {  // through shared memory: a column a lane, token after token
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) turn[(g + e / 2 * 8) * 33 + q4 * 8 + j * 2 + e % 2] = acc[j][e];
+            __syncwarp();
+            if (c + lane < a.N)
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (m0 + e < rows) put1(a, t0 + s.row[w][m0 + e], c + lane, one[n & 1][e], turn[e * 33 + lane]);
+            const bool here = n + 2 < count;
+            ask(n & 1, here ? n + 2 : count >= 2 ? n + 2 - count : 0, here ? z : z + dz);
           }
         }
       __syncthreads();  // the buffer is free
@@ -605,14 +630,21 @@ constexpr int SMS = 152;
 struct Plan {
   int tiles, split, share;
 };
-static Plan plan(int T, int K, int n) {
+// n = 0: the most that any number of adapters asks for (what a workspace holds).
+static Plan plan(int T, int K, int R, int n) {
   Plan p{};
   p.tiles = T / TILE + (T % TILE != 0);
   const int steps = (K + KB - 1) / KB;
-  const int tokens = T < TILE ? T : TILE, distinct = tokens < n ? tokens : n;
-  int want = 2 * SMS / (p.tiles * distinct);
+  int want = 2 * SMS / p.tiles;
+  if (n > 0) {
+    const int tokens = T < TILE ? T : TILE, distinct = p.tiles > 4 ? 1 : tokens < n ? tokens : n;
+    want = 2 * SMS / (p.tiles * distinct);
+    // A step costs a CTA about what one more partial sum of 128 tokens and 64 ranks costs each CTA of the second
+    // kernel (0.35 us): no more parts than make the two equal.
+    const long long even = static_cast<long long>(steps) * (TILE * 64) * distinct / (static_cast<long long>(tokens) * R);
+    while (want > 4 && static_cast<long long>(want) * want > even) --want;
+  }
   if (want < 4) want = 4;
-  if (p.tiles > 4 && want < 2 * SMS / p.tiles) want = 2 * SMS / p.tiles;
   if (want > MAX_SPLIT) want = MAX_SPLIT;
   if (want > steps / 4) want = steps / 4;
   if (want < 1) want = 1;
@@ -621,20 +653,31 @@ static Plan plan(int T, int K, int n) {
   return p;
 }
 
+using Up = void (*)(const Args);
+// The second kernel's forms: parts of H, ranks, few tokens an adapter, rows of residual and Y in 16-byte vectors.
+template <class F>
+static void each_up(F f) {
+  f(adapters_up_kernel<2, 64, false, true>, 2, 64, false, true);
+  f(adapters_up_kernel<2, 64, true, true>, 2, 64, true, true);
+  f(adapters_up_kernel<2, MAX_R, false, true>, 2, MAX_R, false, true);
+  f(adapters_up_kernel<2, MAX_R, true, true>, 2, MAX_R, true, true);
+  f(adapters_up_kernel<2, 64, false, false>, 2, 64, false, false);
+  f(adapters_up_kernel<2, 64, true, false>, 2, 64, true, false);
+  f(adapters_up_kernel<2, MAX_R, false, false>, 2, MAX_R, false, false);
+  f(adapters_up_kernel<2, MAX_R, true, false>, 2, MAX_R, true, false);
+  f(adapters_up_kernel<3, 64, false, false>, 3, 64, false, false);
+  f(adapters_up_kernel<3, 64, true, false>, 3, 64, true, false);
+  f(adapters_up_kernel<3, MAX_R, false, false>, 3, MAX_R, false, false);
+  f(adapters_up_kernel<3, MAX_R, true, false>, 3, MAX_R, true, false);
+}
+
 static int adapters_attr() {
   const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel, most, down_smem(TILE, MAX_R));
   auto up = [&](auto kernel, int ranks, int parts) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, most, up_smem(TILE, ranks, parts));
   };
-  up(adapters_up_kernel<2, 64, false>, 64, 2);
-  up(adapters_up_kernel<2, 64, true>, 64, 2);
-  up(adapters_up_kernel<2, MAX_R, false>, MAX_R, 2);
-  up(adapters_up_kernel<2, MAX_R, true>, MAX_R, 2);
-  up(adapters_up_kernel<3, 64, false>, 64, 3);
-  up(adapters_up_kernel<3, 64, true>, 64, 3);
-  up(adapters_up_kernel<3, MAX_R, false>, MAX_R, 3);
-  up(adapters_up_kernel<3, MAX_R, true>, MAX_R, 3);
+  each_up([&](auto kernel, int parts, int ranks, bool, bool) { up(kernel, ranks, parts); });
   return static_cast<int>(e);
 }
 
@@ -650,7 +693,7 @@ static bool sizes_ok(int T, int K, int N, int R) {
 
 extern "C" size_t ordermoe_adapters_workspace_bytes(int T, int K, int N, int R) {
   if (!sizes_ok(T, K, N, R) || T == 0) return 0;
-  const ad::Plan p = ad::plan(T, K, 1);
+  const ad::Plan p = ad::plan(T, K, R, 0);
   return static_cast<size_t>(p.split) * T * R * 4;
 }
 
@@ -688,7 +731,7 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   static PerDevice attr_;
   const int e = per_device(attr_, ad::adapters_attr);
   if (e != 0) return cuda_fail(static_cast<cudaError_t>(e), "cudaFuncSetAttribute(adapters)");
-  const ad::Plan p = ad::plan(T, K, n);
+  const ad::Plan p = ad::plan(T, K, R, n);
   ad::Args a{};
   a.X = X; a.ldx = ldx; a.A = A; a.stride_a = stride_a; a.lda = lda; a.B = B; a.stride_b = stride_b; a.ldb = ldb;
   a.ids = ids; a.rank = rank; a.scale = scale; a.res = residual; a.ldr = ldr; a.Y = Y; a.ldy = ldy;
@@ -701,21 +744,24 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   // Two CTAs an SM in all. With few tiles they go to the adapters that a tile can have before its columns; with many a
   // CTA takes a tile's adapters in turn (one that finds no adapter costs 1.5 us of its SM).
   const int64_t tokens = T < ad::TILE ? T : ad::TILE, distinct = tokens < n ? tokens : n;
+  const bool low = a.ranks <= 64;
   const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
+  // the second kernel's other forms have an SM each
+  const int64_t up_room = low && !f32 ? room : p.tiles < ad::SMS ? ad::SMS / p.tiles : 1;
   auto at_most = [](int64_t v, int64_t most) { return static_cast<unsigned>(v < 1 ? 1 : v < most ? v : most); };
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
                 dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
   const int parts = f32 ? 3 : 2;
   const bool few = tokens <= 16 * distinct;  // 16 tokens of an adapter in a tile or fewer, in the mean of all that it can have
   const int64_t wide = few ? 2 * ad::NB : ad::NB;  // columns of a CTA's turn
-  const unsigned z = at_most(p.tiles <= 4 ? room / distinct : room, (N + wide - 1) / wide);
-  const dim3 grid(p.tiles, at_most(room / z, distinct), z);
-  const bool low = a.ranks <= 64;  // registers for the weights of few tokens
+  const unsigned z = at_most(p.tiles <= 4 ? up_room / distinct : up_room, (N + wide - 1) / wide);
+  const dim3 grid(p.tiles, at_most(up_room / z, distinct), z);
   const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, low ? 64 : ad::MAX_R, parts));
-  const auto up = f32 ? (low ? (few ? ad::adapters_up_kernel<3, 64, true> : ad::adapters_up_kernel<3, 64, false>)
-                             : (few ? ad::adapters_up_kernel<3, ad::MAX_R, true> : ad::adapters_up_kernel<3, ad::MAX_R, false>))
-                      : (low ? (few ? ad::adapters_up_kernel<2, 64, true> : ad::adapters_up_kernel<2, 64, false>)
-                             : (few ? ad::adapters_up_kernel<2, ad::MAX_R, true> : ad::adapters_up_kernel<2, ad::MAX_R, false>));
+  const bool plain = !f32 && residual && a.vec_r && a.vec_y && N % 8 == 0;
+  ad::Up up = nullptr;
+  ad::each_up([&](ad::Up kernel, int p_, int ranks_, bool few_, bool plain_) {
+    if (p_ == parts && (ranks_ == 64) == low && few_ == few && plain_ == plain) up = kernel;
+  });
   OM_LAUNCH_PDL("adapters_up_kernel", up, grid, dim3(ad::THREADS), smem, stream, a);
   return ORDERMOE_OK;
 }

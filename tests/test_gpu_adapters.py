@@ -201,3 +201,18 @@ def test_captured_with_ids_that_change_and_on_a_stream():
         graph.replay()
         check(X, A, Bw, ids, want, residual=res)
         assert torch.equal(Y, want)
+
+
+@pytest.mark.parametrize("rows", [16, 17, 33, 65, 128])
+@pytest.mark.parametrize("N", [1, 31, 129, 383, 640])
+def test_tokens_of_one_adapter_over_slices_of_columns(rows, N):
+    """Every share of the warps between tokens and columns, over several slices, with rows in any place and in vectors."""
+    T, K, R, n = 300, 72, 40, 2
+    g = gen(rows + N)
+    X, A, Bw = rnd(g, T, K), rnd(g, n, R, K, std=0.05), rnd(g, n, N, R, std=0.1)
+    ids = torch.full((T,), -1, dtype=torch.int32, device=DEV)
+    ids[5:5 + rows] = 1
+    ids[200:299:3] = 0
+    for dt in (BF16, torch.float32):
+        check(X, A, Bw, ids, torch.empty(T, N, dtype=dt, device=DEV), residual=rnd(g, T, N))
+        check(X, A, Bw, ids, torch.empty(T, N + 3, dtype=dt, device=DEV)[:, :N])
