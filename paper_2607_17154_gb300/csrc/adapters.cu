@@ -22,7 +22,7 @@ int read_clear_err_adapters(unsigned long long* out) {
 namespace ad {
 
 constexpr int TILE = 128;      // tokens among which adapters are looked for
-constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int THREADS = 256, MAX_WARPS = 16;
 constexpr int MAX_R = 128;
 constexpr int MAX_SPLIT = 32;  // CTAs that share K
 constexpr int KB = 64;         // of K a step
@@ -39,6 +39,7 @@ struct Args {
   void* Y; int64_t ldy;
   int n, R, T, N, K, f32, split, share;  // share: steps of K of a CTA
   int vec_r, vec_y;                      // residual and Y may be moved 16 bytes at a time
+  int flat;                              // second kernel: all tiles' slices shared out evenly over the CTAs
   int rows, ranks;                       // of a tile, in steps of 16 (what shared memory is laid out for)
   float* H;                              // [split][T][R]
 };
@@ -68,7 +69,7 @@ struct Groups {
   int rank[TILE];            // its ranks in use and its scale
   float scale[TILE];
   int leader[TILE];          // the first token of each distinct adapter, in order
-  uint8_t row[WARPS][TILE];  // tokens of the adapter in hand, in order; every warp has a list of its own
+  uint8_t row[MAX_WARPS][TILE];  // tokens of the adapter in hand, in order; every warp has a list of its own
   int warp[TILE / 32];
   int distinct;
 };
@@ -344,281 +345,319 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
 // residual) is asked for before the first kernel has ended. Tokens without an adapter go with the first.
 constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice (ranks: 64 or 128)
-constexpr int TURN = WARPS * 16 * 33 * 4;
-constexpr int up_smem(int rows, int ranks, int parts) {
-  const int many = TURN + (parts * rows + 2 * NB) * up_row(ranks), few = 16 * (MAX_R + 4) * 4;
+// Threads of a CTA: two CTAs an SM, or one of as many warps where shared memory has no room for two; with few tokens
+// registers (for weights) are worth more than warps.
+constexpr bool up_pairs(int parts, int ranks) { return parts == 2 && ranks == 64; }
+constexpr int up_threads(int parts, int ranks, bool few) { return few || up_pairs(parts, ranks) ? 256 : 512; }
+constexpr int TURN = 16 * 33 * 4;  // bytes of 16 tokens x 32 columns, a warp
+constexpr int up_smem(int rows, int ranks, int parts, bool few_tokens) {
+  const int many = up_threads(parts, ranks, few_tokens) / 32 * TURN + (parts * rows + 2 * NB) * up_row(ranks);
+  const int few = 16 * (MAX_R + 4) * 4;
   return rows > 16 && many > few ? many : few;  // 16 tokens at most: all adapters have few
 }
 template <int PARTS, int RANKS, bool FEW, bool PLAIN>
-__global__ void __launch_bounds__(THREADS, PARTS == 2 && RANKS == 64 ? 2 : 1) adapters_up_kernel(const Args a) {
+__global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS, RANKS) ? 2 : 1)
+    adapters_up_kernel(const Args a) {
+  constexpr int THREADS = up_threads(PARTS, RANKS, FEW), WARPS = THREADS / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Groups s;
-  const int t0 = blockIdx.x * TILE, tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
+  __shared__ const uint16_t* res_of[PLAIN ? 1 : WARPS][16];  // a warp's rows
+  __shared__ char* y_of[PLAIN ? 1 : WARPS][16];
+  const int tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
   constexpr int ld = up_row(RANKS);
-  const int slices = (a.N + NB - 1) / NB, z0 = blockIdx.z, dz = gridDim.z;
-  float* const turn = reinterpret_cast<float*>(smem) + w * 16 * 33;  // 16 tokens x 32 columns a warp
-  const uint32_t hs = smem_u32(smem) + TURN, bs = hs + PARTS * a.rows * ld;
+  float* const turn = reinterpret_cast<float*>(smem + w * TURN);
+  uint8_t* const parts = smem + WARPS * TURN;
+  const uint32_t hs = smem_u32(parts), bs = hs + PARTS * a.rows * ld;
+  const int slices = (a.N + NB - 1) / NB;
+  const long long all = static_cast<long long>(slices) * ((a.T - 1) / TILE + 1);
+  const long long lo = all * blockIdx.x / gridDim.x, hi = all * (blockIdx.x + 1) / gridDim.x;
+  const int tile0 = a.flat ? static_cast<int>(lo / slices) : static_cast<int>(blockIdx.x);
+  const int tile1 = a.flat ? static_cast<int>((hi - 1) / slices) : tile0;
   bool waited = false;
-  const bool alone = find_groups(a, s, t0, false);
-  if (alone && blockIdx.y == 0 && a.res != a.Y) {
-    const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
-    for (int z = z0; z < slices; z += dz)
-      for (int i = tid; i < TILE * (by8 ? NB / 8 : NB); i += THREADS) {
-        const int row = by8 ? i / (NB / 8) : i / NB, c = z * NB + (by8 ? i % (NB / 8) * 8 : i % NB);
-        if (t0 + row >= a.T || s.id[row] >= 0 || c >= a.N) continue;
-        if (by8) {
-          float v[8] = {};
-          put8(a, t0 + row, c, get8(a, t0 + row, c), v);
-        } else {
-          put1(a, t0 + row, c, a.res ? a.res[static_cast<int64_t>(t0 + row) * a.ldr + c] : 0u, 0.0f);
-        }
-      }
-  }
-  for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
-    const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead], rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
-    const uint16_t* B = a.B + id * a.stride_b;
-    if (FEW && rows <= 16) {  // weights and H in registers, 32 columns a warp and turn
-      float* sum = reinterpret_cast<float*>(smem);  // [16][LD] of H
-      constexpr int LD = RANKS + 4;
-      const int steps = (r + 31) / 32, groups = (a.N + 31) / 32;
-      const float scale = s.scale[lead];
-      int64_t tok[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) tok[h] = g + h * 8 < rows ? t0 + s.row[w][g + h * 8] : -1;
-      // Within 32 ranks a thread has eight in a row, q4 * 8 and on: two products' shares, of weights and of H alike.
-      uint4 b[4][RANKS / 32], u[2] = {};
-      auto ask = [&](int n) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int col = n * 32 + g / 2 * 8 + j * 2 + g % 2;
-          const uint16_t* from = B + col * a.ldb + q4 * 8;
-#pragma unroll
-          for (int k = 0; k < RANKS / 32; ++k) {
-            b[j][k] = make_uint4(0, 0, 0, 0);
-            const int left = r - k * 32 - q4 * 8;
-            if (col >= a.N || left <= 0) continue;
-            b[j][k] = *reinterpret_cast<const uint4*>(from + k * 32);
-            if (left < 8) {  // columns behind the rank say nothing, whatever they hold
-              uint32_t* x = reinterpret_cast<uint32_t*>(&b[j][k]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[e] = 2 * e + 1 < left ? x[e] : 2 * e < left ? x[e] & 0xFFFFu : 0u;
-            }
+  for (int tile = tile0; tile <= tile1; ++tile) {
+    const int t0 = tile * TILE;
+    const long long before = static_cast<long long>(tile) * slices;
+    // this CTA's slices of the tile: z0, z0 + dz and so on below z1
+    const int z0 = !a.flat ? static_cast<int>(blockIdx.z) : lo > before ? static_cast<int>(lo - before) : 0;
+    const int z1 = a.flat && hi - before < slices ? static_cast<int>(hi - before) : slices, dz = a.flat ? 1 : gridDim.z;
+    if (tile > tile0) __syncthreads();  // the groups before are done with
+    const bool alone = find_groups(a, s, t0, false);
+    if (alone && blockIdx.y == 0 && a.res != a.Y) {
+      const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
+      for (int z = z0; z < z1; z += dz)
+        for (int i = tid; i < TILE * (by8 ? NB / 8 : NB); i += THREADS) {
+          const int row = by8 ? i / (NB / 8) : i / NB, c = z * NB + (by8 ? i % (NB / 8) * 8 : i % NB);
+          if (t0 + row >= a.T || s.id[row] >= 0 || c >= a.N) continue;
+          if (by8) {
+            float v[8] = {};
+            put8(a, t0 + row, c, get8(a, t0 + row, c), v);
+          } else {
+            put1(a, t0 + row, c, a.res ? a.res[static_cast<int64_t>(t0 + row) * a.ldr + c] : 0u, 0.0f);
           }
         }
+    }
+    for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
+      const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead];
+      const int rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
+      const uint16_t* B = a.B + id * a.stride_b;
+      if (FEW && rows <= 16) {  // weights and H in registers, 32 columns a warp and turn
+        float* sum = reinterpret_cast<float*>(smem);  // [16][LD] of H
+        constexpr int LD = RANKS + 4;
+        const int steps = (r + 31) / 32, groups = (a.N + 31) / 32;
+        const float scale = s.scale[lead];
+        int64_t tok[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (tok[h] >= 0) u[h] = get8(a, tok[h], n * 32 + q4 * 8);
-      };
-      const int n0 = z0 * 8 + w, dn = dz * 8;
-      if (n0 < groups) ask(n0);
-      if (!waited) pdl_wait();
-      waited = true;
-      for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
-        const int row = i / (steps * 8), c = (i - row * steps * 8) * 4;
-        const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        *reinterpret_cast<float4*>(sum + row * LD + c) = v;
-      }
-      __syncthreads();
-      for (int n = n0; n < groups; n += dn) {
-        float acc[4][4] = {};
-#pragma unroll
-        for (int k = 0; k < RANKS / 32; ++k) {
-          if (k >= steps) continue;
-          float h[2][8];
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-              *reinterpret_cast<float4*>(&h[e][4 * f]) =
-                  *reinterpret_cast<const float4*>(sum + (g + 8 * e) * LD + k * 32 + q4 * 8 + f * 4);
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t x[4];  // rows g, g + 8 of ranks 4 half, + 1, then of + 2, + 3
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float* v = &h[e & 1][4 * half + (e / 2) * 2];
-                x[e] = pack_bf16x2(v[0], v[1]);
-                v[0] -= bf16_lo(x[e]);
-                v[1] -= bf16_hi(x[e]);
-              }
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (half == 0) mma(acc[j], x, b[j][k].x, b[j][k].y);
-                else mma(acc[j], x, b[j][k].z, b[j][k].w);
-            }
-        }
-        const uint4 now[2] = {u[0], u[1]};
-        if (n + dn < groups) ask(n + dn);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (tok[h] < 0) continue;
-          float v[8];
+        for (int h = 0; h < 2; ++h) tok[h] = g + h * 8 < rows ? t0 + s.row[w][g + h * 8] : -1;
+        // Within 32 ranks a thread has eight in a row, q4 * 8 and on: two products' shares, of weights and of H alike.
+        uint4 b[4][RANKS / 32], u[2] = {};
+        auto ask = [&](int n) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            v[2 * j] = acc[j][2 * h] * scale;
-            v[2 * j + 1] = acc[j][2 * h + 1] * scale;
-          }
-          put8(a, tok[h], n * 32 + q4 * 8, now[h], v);
-        }
-      }
-      __syncthreads();
-      continue;
-    }
-    constexpr int VECS = RANKS / 8, ROWS = THREADS / VECS;  // a thread's vector is tid % VECS, of every ROWS-th column
-    const int fv = tid % VECS, fleft = min(8, r - fv * 8);
-    const uint16_t* fp = B + (tid / VECS) * a.ldb + fv * 8;
-    auto fetch = [&](int z, int buffer) {
-      if (fv >= rv) return;
+            const int col = n * 32 + g / 2 * 8 + j * 2 + g % 2;
+            const uint16_t* from = B + col * a.ldb + q4 * 8;
 #pragma unroll
-      for (int e = 0; e < NB / ROWS; ++e) {
-        const int row = tid / VECS + e * ROWS, col = z * NB + row;
-        const int at = (row & ~31) + (row % 8 / 2) * 8 + row % 32 / 8 * 2 + row % 2;  // column c of product j: 8 j + c
-        const bool ok = col < a.N && fleft > 0;
-        cp16(bs + (buffer * NB + at) * ld + fv * 16, ok ? fp + (z * NB + e * ROWS) * a.ldb : a.B, ok ? fleft * 2 : 0);
-      }
-    };
-    if (z0 < slices) fetch(z0, 0);
-    cp_commit();
-    if (!waited) pdl_wait();
-    waited = true;
-    const int blocks = (rows + 15) / 16, m16 = blocks * 16;
-    const float scale = s.scale[lead];
-    for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
-      const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
-      alignas(16) float v[4] = {};
-      if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r);
-      v[0] *= scale; v[1] *= scale; v[2] *= scale; v[3] *= scale;
+            for (int k = 0; k < RANKS / 32; ++k) {
+              b[j][k] = make_uint4(0, 0, 0, 0);
+              const int left = r - k * 32 - q4 * 8;
+              if (col >= a.N || left <= 0) continue;
+              b[j][k] = *reinterpret_cast<const uint4*>(from + k * 32);
+              if (left < 8) {  // columns behind the rank say nothing, whatever they hold
+                uint32_t* x = reinterpret_cast<uint32_t*>(&b[j][k]);
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) {
-        const uint32_t x = pack_bf16x2(v[0], v[1]), y = pack_bf16x2(v[2], v[3]);
-        *reinterpret_cast<uint2*>(smem + TURN + (p * a.rows + row) * ld + c * 2) = make_uint2(x, y);
-        v[0] -= bf16_lo(x); v[1] -= bf16_hi(x); v[2] -= bf16_lo(y); v[3] -= bf16_hi(y);
-      }
-    }
-    const int share = blocks > 4 ? 1 : blocks > 2 ? 2 : 4;  // warps that share a block of tokens, each up to 128 / share columns
-    const int m0 = w / share * 16, first = w % share;
-    const bool busy = m0 < rows;
-    int64_t tok[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[w][m0 + g + h * 8] : -1;
-    const uint16_t* rp[2] = {nullptr, nullptr};
-    uint16_t* yp[2] = {nullptr, nullptr};
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (PLAIN && tok[h] >= 0) {
-        rp[h] = a.res + tok[h] * a.ldr + q4 * 8;
-        yp[h] = static_cast<uint16_t*>(a.Y) + tok[h] * a.ldy + q4 * 8;
-      }
-    const uint32_t xa = hs + (m0 + (lane & 7) + (lane / 8 % 2) * 8) * ld + lane / 16 * 16;
-    const uint32_t ba = bs + (lane / 16 * 8 + (lane & 7)) * ld + (lane / 8 % 2) * 16;
-    // The residual is asked for ahead. In vectors: that of a slice's n-th 32 columns of this warp, once the slice before
-    // has used its own. Else a column a lane, of 16 tokens, two times 32 columns ahead.
-    const int count = 4 / share;  // times 32 columns of a slice that this warp has
-    uint4 u[PLAIN ? 4 : 1][2];
-    uint16_t one[PLAIN ? 1 : 2][16];
-    auto ask = [&](int set, int n, int z) {  // `set` is known when this is compiled: an index of registers
-      const int c = z * NB + (first + n * share) * 32;
-      if constexpr (PLAIN) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          u[set][h] = make_uint4(0, 0, 0, 0);
-          if (busy && z < slices && n < count && rp[h] && c + q4 * 8 < a.N) u[set][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          one[set][e] = 0;
-          if (busy && a.res && z < slices && n < count && c + lane < a.N && m0 + e < rows)
-            one[set][e] = a.res[static_cast<int64_t>(t0 + s.row[w][m0 + e]) * a.ldr + c + lane];
-        }
-      }
-    };
-#pragma unroll
-    for (int n = 0; n < (PLAIN ? 4 : 2); ++n) ask(n, n, z0);
-    // H's parts stay in registers where two CTAs an SM leave room for them
-    constexpr bool HELD = !FEW && PARTS * RANKS <= 128;
-    uint32_t x[HELD ? RANKS / 16 : 1][PARTS][4];
-    auto load_h = [&](int k, uint32_t (&v)[PARTS][4]) {
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) ldm4(v[p], xa + p * a.rows * ld + k * 32);
-    };
-    if constexpr (HELD) {
-      __syncthreads();  // H is written
-      if (busy)
-#pragma unroll
-        for (int k = 0; k < RANKS / 16; ++k)
-          if (2 * k < rv) load_h(k, x[k]);
-    }
-    int buffer = 0;
-    for (int z = z0; z < slices; z += dz, buffer ^= 1) {
-      if (z + dz < slices) fetch(z + dz, buffer ^ 1);
-      cp_commit();
-      cp_wait<1>();
-      __syncthreads();
-      if (busy)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const int col = (first + n * share) * 32, c = z * NB + col;
-          if (n >= count || c >= a.N) continue;  // behind the last column no slice follows
-          float acc[4][4] = {};
-          if constexpr (PLAIN)  // results of 16 bits: the residual may be the sums' beginning
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t x[4] = {u[n][h].x, u[n][h].y, u[n][h].z, u[n][h].w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                acc[j][2 * h] = bf16_lo(x[j]);
-                acc[j][2 * h + 1] = bf16_hi(x[j]);
+                for (int e = 0; e < 4; ++e)
+                  x[e] = 2 * e + 1 < left ? x[e] : 2 * e < left ? x[e] & 0xFFFFu : 0u;
               }
             }
-          if constexpr (PLAIN) ask(n, n, z + dz);
-          const uint32_t bb = ba + (buffer * NB + col) * ld;
+          }
 #pragma unroll
-          for (int k = 0; k < RANKS / 16; ++k) {
-            if (2 * k >= rv) break;
-            uint32_t b[2][4];
+          for (int h = 0; h < 2; ++h)
+            if (tok[h] >= 0) u[h] = get8(a, tok[h], n * 32 + q4 * 8);
+        };
+        const int n0 = a.flat ? z0 * (NB / 32) + w : z0 * WARPS + w, dn = a.flat ? WARPS : dz * WARPS;
+        const int n1 = a.flat && z1 * (NB / 32) < groups ? z1 * (NB / 32) : groups;
+        if (n0 < n1) ask(n0);
+        if (!waited) pdl_wait();
+        waited = true;
+        for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
+          const int row = i / (steps * 8), c = (i - row * steps * 8) * 4;
+          const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          *reinterpret_cast<float4*>(sum + row * LD + c) = v;
+        }
+        __syncthreads();
+        for (int n = n0; n < n1; n += dn) {
+          float acc[4][4] = {};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) ldm4(b[j], bb + j * 16 * ld + k * 32);  // products 2 j and 2 j + 1
-            if constexpr (!HELD) load_h(k, x[0]);
+          for (int k = 0; k < RANKS / 32; ++k) {
+            if (k >= steps) continue;
+            float h[2][8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int f = 0; f < 2; ++f)
+                *reinterpret_cast<float4*>(&h[e][4 * f]) =
+                    *reinterpret_cast<const float4*>(sum + (g + 8 * e) * LD + k * 32 + q4 * 8 + f * 4);
 #pragma unroll
             for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) mma(acc[j], x[HELD ? k : 0][p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
-          }
-          if (PLAIN) {
+              for (int half = 0; half < 2; ++half) {
+                uint32_t x[4];  // rows g, g + 8 of ranks 4 half, + 1, then of + 2, + 3
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (tok[h] < 0 || c + q4 * 8 >= a.N) continue;
-              float v[8];
+                for (int e = 0; e < 4; ++e) {
+                  float* v = &h[e & 1][4 * half + (e / 2) * 2];
+                  x[e] = pack_bf16x2(v[0], v[1]);
+                  v[0] -= bf16_lo(x[e]);
+                  v[1] -= bf16_hi(x[e]);
+                }
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                v[2 * j] = acc[j][2 * h];
-                v[2 * j + 1] = acc[j][2 * h + 1];
+                for (int j = 0; j < 4; ++j)
+                  if (half == 0) mma(acc[j], x, b[j][k].x, b[j][k].y);
+                  else mma(acc[j], x, b[j][k].z, b[j][k].w);
               }
-              *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
+          }
+          const uint4 now[2] = {u[0], u[1]};
+          if (n + dn < n1) ask(n + dn);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (tok[h] < 0) continue;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              v[2 * j] = acc[j][2 * h] * scale;
+              v[2 * j + 1] = acc[j][2 * h + 1] * scale;
             }
-          } else {  // through shared memory: a column a lane, token after token
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) turn[(g + e / 2 * 8) * 33 + q4 * 8 + j * 2 + e % 2] = acc[j][e];
-            __syncwarp();
-            if (c + lane < a.N)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (m0 + e < rows) put1(a, t0 + s.row[w][m0 + e], c + lane, one[n & 1][e], turn[e * 33 + lane]);
-            const bool here = n + 2 < count;
-            ask(n & 1, here ? n + 2 : count >= 2 ? n + 2 - count : 0, here ? z : z + dz);
+            put8(a, tok[h], n * 32 + q4 * 8, now[h], v);
           }
         }
-      __syncthreads();  // the buffer is free
+        __syncthreads();
+        continue;
+      }
+      constexpr int VECS = RANKS / 8, ROWS = THREADS / VECS;  // a thread's vector is tid % VECS, of every ROWS-th column
+      const int fv = tid % VECS, fleft = min(8, r - fv * 8);
+      const uint16_t* fp = B + (tid / VECS) * a.ldb + fv * 8;
+      auto fetch = [&](int z, int buffer) {
+        if (fv >= rv) return;
+#pragma unroll
+        for (int e = 0; e < NB / ROWS; ++e) {
+          const int row = tid / VECS + e * ROWS, col = z * NB + row;
+          const int at = (row & ~31) + (row % 8 / 2) * 8 + row % 32 / 8 * 2 + row % 2;  // column c of product j: 8 j + c
+          const bool ok = col < a.N && fleft > 0;
+          cp16(bs + (buffer * NB + at) * ld + fv * 16, ok ? fp + (z * NB + e * ROWS) * a.ldb : a.B, ok ? fleft * 2 : 0);
+        }
+      };
+      if (z0 < z1) fetch(z0, 0);
+      cp_commit();
+      if (!waited) pdl_wait();
+      waited = true;
+      const int blocks = (rows + 15) / 16, m16 = blocks * 16;
+      const float scale = s.scale[lead];
+      for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
+        const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
+        alignas(16) float v[4] = {};
+        if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r);
+        v[0] *= scale; v[1] *= scale; v[2] *= scale; v[3] *= scale;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          const uint32_t x = pack_bf16x2(v[0], v[1]), y = pack_bf16x2(v[2], v[3]);
+          *reinterpret_cast<uint2*>(parts + (p * a.rows + row) * ld + c * 2) = make_uint2(x, y);
+          v[0] -= bf16_lo(x); v[1] -= bf16_hi(x); v[2] -= bf16_lo(y); v[3] -= bf16_hi(y);
+        }
+      }
+      constexpr int LEAST = WARPS / 8;
+      const int share = blocks > 4 ? LEAST : blocks > 2 ? 2 * LEAST : 4;  // warps that share a block's columns
+      const int m0 = w / share * 16, first = w % share;
+      const bool busy = m0 < rows;
+      int64_t tok[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) tok[h] = m0 + g + h * 8 < rows ? t0 + s.row[w][m0 + g + h * 8] : -1;
+      const uint16_t* rp[2] = {nullptr, nullptr};
+      uint16_t* yp[2] = {nullptr, nullptr};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (PLAIN && tok[h] >= 0) {
+          rp[h] = a.res + tok[h] * a.ldr + q4 * 8;
+          yp[h] = static_cast<uint16_t*>(a.Y) + tok[h] * a.ldy + q4 * 8;
+        }
+      if constexpr (!PLAIN) {
+        if (lane < 16) {
+          const bool on = m0 + lane < rows;
+          const int64_t t = on ? t0 + s.row[w][m0 + lane] : 0;
+          res_of[w][lane] = on && a.res ? a.res + t * a.ldr : nullptr;
+          y_of[w][lane] = on ? static_cast<char*>(a.Y) + t * a.ldy * (a.f32 ? 4 : 2) : nullptr;
+        }
+        __syncwarp();
+      }
+      const uint32_t xa = hs + (m0 + (lane & 7) + (lane / 8 % 2) * 8) * ld + lane / 16 * 16;
+      const uint32_t ba = bs + (lane / 16 * 8 + (lane & 7)) * ld + (lane / 8 % 2) * 16;
+      // The residual is asked for ahead. In vectors: that of a slice's n-th 32 columns of this warp, once the slice before
+      // has used its own. Else a column a lane, of 16 tokens, two times 32 columns ahead.
+      const int count = 4 / share;  // times 32 columns of a slice that this warp has
+      uint4 u[PLAIN ? 4 : 1][2];
+      uint16_t one[PLAIN ? 1 : 2][16];
+      auto ask = [&](int set, int n, int z) {  // `set` is known when this is compiled: an index of registers
+        const int c = z * NB + (first + n * share) * 32;
+        if constexpr (PLAIN) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            u[set][h] = make_uint4(0, 0, 0, 0);
+            if (busy && z < z1 && n < count && rp[h] && c + q4 * 8 < a.N) u[set][h] = *reinterpret_cast<const uint4*>(rp[h] + c);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            one[set][e] = 0;
+            const uint16_t* from = res_of[w][e];
+            if (from && z < z1 && n < count && c + lane < a.N) one[set][e] = from[c + lane];
+          }
+        }
+      };
+#pragma unroll
+      for (int n = 0; n < (PLAIN ? 4 : 2); ++n) ask(n, n, z0);
+      // H's parts stay in registers where two CTAs an SM leave room for them
+      constexpr bool HELD = !FEW && PARTS * RANKS <= 128;
+      uint32_t x[HELD ? RANKS / 16 : 1][PARTS][4];
+      auto load_h = [&](int k, uint32_t (&v)[PARTS][4]) {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) ldm4(v[p], xa + p * a.rows * ld + k * 32);
+      };
+      if constexpr (HELD) {
+        __syncthreads();  // H is written
+        if (busy)
+#pragma unroll
+          for (int k = 0; k < RANKS / 16; ++k)
+            if (2 * k < rv) load_h(k, x[k]);
+      }
+      int buffer = 0;
+      for (int z = z0; z < z1; z += dz, buffer ^= 1) {
+        if (z + dz < z1) fetch(z + dz, buffer ^ 1);
+        cp_commit();
+        cp_wait<1>();
+        __syncthreads();
+        if (busy)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const int col = (first + n * share) * 32, c = z * NB + col;
+            if (n >= count || c >= a.N) continue;  // behind the last column no slice follows
+            float acc[4][4] = {};
+            if constexpr (PLAIN)  // results of 16 bits: the residual may be the sums' beginning
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t x[4] = {u[n][h].x, u[n][h].y, u[n][h].z, u[n][h].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  acc[j][2 * h] = bf16_lo(x[j]);
+                  acc[j][2 * h + 1] = bf16_hi(x[j]);
+                }
+              }
+            if constexpr (PLAIN) ask(n, n, z + dz);
+            const uint32_t bb = ba + (buffer * NB + col) * ld;
+#pragma unroll
+            for (int k = 0; k < RANKS / 16; ++k) {
+              if (2 * k >= rv) break;
+              uint32_t b[2][4];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) ldm4(b[j], bb + j * 16 * ld + k * 32);  // products 2 j and 2 j + 1
+              if constexpr (!HELD) load_h(k, x[0]);
+#pragma unroll
+              for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma(acc[j], x[HELD ? k : 0][p], b[j / 2][j % 2 * 2], b[j / 2][j % 2 * 2 + 1]);
+            }
+            if (PLAIN) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                if (tok[h] < 0 || c + q4 * 8 >= a.N) continue;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  v[2 * j] = acc[j][2 * h];
+                  v[2 * j + 1] = acc[j][2 * h + 1];
+                }
+                *reinterpret_cast<uint4*>(yp[h] + c) = pack8(v);
+              }
+            } else {  // through shared memory: a column a lane, token after token
+              __syncwarp();
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turn[(g + e / 2 * 8) * 33 + q4 * 8 + j * 2 + e % 2] = acc[j][e];
+              __syncwarp();
+              if (c + lane < a.N)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  if (char* y = y_of[w][e]) {
+                    const float v = turn[e * 33 + lane] + bf16_lo(one[n & 1][e]);
+                    if (PARTS == 3) reinterpret_cast<float*>(y)[c + lane] = v;
+                    else reinterpret_cast<uint16_t*>(y)[c + lane] = static_cast<uint16_t>(pack_bf16x2(v, 0.0f));
+                  }
+              const bool here = n + 2 < count;
+              ask(n & 1, here ? n + 2 : count >= 2 ? n + 2 - count : 0, here ? z : z + dz);
+            }
+          }
+        __syncthreads();  // the buffer is free
+      }
+      cp_wait<0>();
+      __syncthreads();
     }
-    cp_wait<0>();
-    __syncthreads();
   }
   if (!waited) pdl_wait();  // never done before the first kernel
 }
@@ -674,10 +713,9 @@ static void each_up(F f) {
 static int adapters_attr() {
   const auto most = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e = cudaFuncSetAttribute(adapters_down_kernel, most, down_smem(TILE, MAX_R));
-  auto up = [&](auto kernel, int ranks, int parts) {
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, most, up_smem(TILE, ranks, parts));
-  };
-  each_up([&](auto kernel, int parts, int ranks, bool, bool) { up(kernel, ranks, parts); });
+  each_up([&](auto kernel, int parts, int ranks, bool few, bool) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, most, up_smem(TILE, ranks, parts, few));
+  });
   return static_cast<int>(e);
 }
 
@@ -741,27 +779,35 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   a.H = static_cast<float*>(workspace);
   a.rows = T < ad::TILE ? (T + 15) / 16 * 16 : ad::TILE;
   a.ranks = (R + 15) / 16 * 16;
-  // Two CTAs an SM in all. With few tiles they go to the adapters that a tile can have before its columns; with many a
-  // CTA takes a tile's adapters in turn (one that finds no adapter costs 1.5 us of its SM).
+  // As many CTAs as run at once. With few tiles they go to the adapters that a tile can have before its columns; with
+  // many a CTA takes a tile's adapters in turn (one that finds no adapter costs 1.5 us of its SM).
   const int64_t tokens = T < ad::TILE ? T : ad::TILE, distinct = tokens < n ? tokens : n;
   const bool low = a.ranks <= 64;
   const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
-  // the second kernel's other forms have an SM each
-  const int64_t up_room = low && !f32 ? room : p.tiles < ad::SMS ? ad::SMS / p.tiles : 1;
   auto at_most = [](int64_t v, int64_t most) { return static_cast<unsigned>(v < 1 ? 1 : v < most ? v : most); };
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
                 dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
   const int parts = f32 ? 3 : 2;
   const bool few = tokens <= 16 * distinct;  // 16 tokens of an adapter in a tile or fewer, in the mean of all that it can have
-  const int64_t wide = few ? 2 * ad::NB : ad::NB;  // columns of a CTA's turn
-  const unsigned z = at_most(p.tiles <= 4 ? up_room / distinct : up_room, (N + wide - 1) / wide);
-  const dim3 grid(p.tiles, at_most(up_room / z, distinct), z);
-  const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, low ? 64 : ad::MAX_R, parts));
+  const int64_t ctas = (ad::up_pairs(parts, low ? 64 : ad::MAX_R) ? 2 : 1) * ad::SMS;
+  const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB, mine = ctas / p.tiles;
+  dim3 grid;
+  if (p.tiles <= 4) {
+    const unsigned z = at_most(mine / distinct, few ? (slices + 1) / 2 : slices);  // few: a turn has two slices
+    grid = dim3(p.tiles, at_most(mine / z, distinct), z);
+  } else {
+    // Slices of a CTA where the tiles share the CTAs evenly, and where all tiles' slices do: then most CTAs meet two tiles
+    // and sum up H twice, which costs as much as 1.5 slices (32 tiles, N 14336, R 64, 304 CTAs: 13 slices 82 us, 11.8 90).
+    const int64_t z = at_most(mine, slices), rounds = (p.tiles * z + ctas - 1) / ctas * ((slices + z - 1) / z);
+    a.flat = 2 * rounds * ctas > 2 * p.tiles * slices + 3 * ctas;
+    grid = a.flat ? dim3(at_most(ctas, p.tiles * slices), 1, 1) : dim3(p.tiles, at_most(mine / z, distinct), static_cast<unsigned>(z));
+  }
+  const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, low ? 64 : ad::MAX_R, parts, few));
   const bool plain = !f32 && residual && a.vec_r && a.vec_y && N % 8 == 0;
   ad::Up up = nullptr;
   ad::each_up([&](ad::Up kernel, int p_, int ranks_, bool few_, bool plain_) {
     if (p_ == parts && (ranks_ == 64) == low && few_ == few && plain_ == plain) up = kernel;
   });
-  OM_LAUNCH_PDL("adapters_up_kernel", up, grid, dim3(ad::THREADS), smem, stream, a);
+  OM_LAUNCH_PDL("adapters_up_kernel", up, grid, dim3(ad::up_threads(parts, low ? 64 : ad::MAX_R, few)), smem, stream, a);
   return ORDERMOE_OK;
 }

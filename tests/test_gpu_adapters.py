@@ -78,7 +78,7 @@ def check(X, A, Bw, ids, Y, scale=None, rank=None, residual=None):
 SIZES = [  # T, K, N, R, adapters
     (1, 64, 64, 8, 1), (1, 4096, 4096, 16, 3), (2, 1, 1, 8, 2), (5, 63, 9, 24, 4), (16, 100, 300, 32, 2), (17, 512, 257, 64, 1),
     (33, 1999, 1009, 40, 7), (64, 128, 256, 128, 64), (127, 320, 100, 16, 3), (128, 1024, 512, 64, 32), (129, 72, 520, 8, 200),
-    (300, 2048, 130, 120, 5), (1000, 96, 64, 48, 2), (4096, 256, 264, 16, 8), (3, 14336, 64, 8, 2), (200, 300, 700, 128, 12), (128, 64, 1500, 72, 3), (40, 33, 65, 16, 40)]
+    (300, 2048, 130, 120, 5), (1000, 96, 64, 48, 2), (4096, 256, 264, 16, 8), (3, 14336, 64, 8, 2), (200, 300, 700, 128, 12), (128, 64, 1500, 72, 3), (40, 33, 65, 16, 40), (4100, 64, 9000, 72, 3), (45000, 32, 200, 8, 5)]
 
 
 @pytest.mark.parametrize("T,K,N,R,n", SIZES)
