@@ -323,7 +323,8 @@ typedef struct {
  *            aligned (parts of one product's rows, say)
  *   starts   [seqs + 1] i32, ascending from 0: tokens starts[s] to starts[s + 1] - 1 are sequence s's newest ones, in
  *            slots length[s] - (starts[s + 1] - starts[s]) and on: length counts them already. Tokens from
- *            starts[seqs] on are padding: nothing of them is used or written. NULL: one token a sequence, T = seqs
+ *            starts[seqs] on are padding: nothing of them is used or written. NULL: one token a sequence, T = seqs,
+ *            and the token of a sequence of length 0 (an idle row of a batch) is left out
  *   position [T] i32, nullable (the slot)
  *   inv_freq [rot_dim / 2] f64 radians a position; pair i is (i, i + rot_dim / 2), or (2 i, 2 i + 1) when adjacent
  *            != 0. rot_dim: a multiple of 16, at most dim; what is behind it is copied. 0: nothing turns

@@ -503,17 +503,23 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const Args a)
   __shared__ Units<JOIN_THREADS> units;
   __shared__ float tops[MAX_CTAS], lens[MAX_CTAS];
   __shared__ float4 sums[GROUPS][COLS];
-  pdl_wait();
-  pdl_trigger();
+  // lengths are the call's inputs: the row is looked for while the first kernel ends
   const int per = count_units(a, units), rows = a.c.heads * a.chunks, tid = threadIdx.x, y = blockIdx.y;
   const long long U = units.before[JOIN_THREADS] * rows;
   const int W = parts(U, a.ctas, WARPS), next = (static_cast<int>(blockIdx.x) + 1) * WARPS;
-  if (next >= W) return;
-  const long long at = first_unit(U, next, W);
-  const Place p = find_place(a, units, per, at, rows);
-  const Row x = row_of(a, p.s, p.r);
-  const int c0 = owner(U, at - p.j, W) / WARPS, c1 = owner(U, at - p.j + p.nu - 1, W) / WARPS;
-  if (p.j == 0 || c0 != static_cast<int>(blockIdx.x) || y >= x.heads) return;
+  Place p{};
+  Row x{};
+  int c0 = -1, c1 = -1;
+  if (next < W) {
+    const long long at = first_unit(U, next, W);
+    p = find_place(a, units, per, at, rows);
+    x = row_of(a, p.s, p.r);
+    c0 = owner(U, at - p.j, W) / WARPS;
+    c1 = owner(U, at - p.j + p.nu - 1, W) / WARPS;
+  }
+  pdl_wait();
+  pdl_trigger();
+  if (next >= W || p.j == 0 || c0 != static_cast<int>(blockIdx.x) || y >= x.heads) return;
   auto part = [&](int c) { return a.part + (static_cast<int64_t>(c) * 2 + (c == c0)) * PS; };
   const int n = c1 - c0 + 1;
   for (int i = tid; i < n; i += JOIN_THREADS) {

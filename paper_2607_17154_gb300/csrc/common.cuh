@@ -91,6 +91,9 @@ int per_device(PerDevice& c, F init) {
 // stream finishes. Every kernel launched this way calls pdl_wait() before its
 // first access to global memory: it returns once the previous kernel has
 // completed and its writes are visible (at once when there is no such kernel).
+// The second kernel of a call may read the call's inputs before it: the first one
+// waited, before it let the second one start, for whatever wrote them (it may not
+// touch what the first one writes, and waits before it ends).
 // pdl_trigger() lets the next kernel's blocks be scheduled as soon as every
 // block of this one has started.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -147,7 +147,9 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     first = a.starts[s];
     count = a.starts[s + 1] - first;
   }
-  const int64_t at = static_cast<int64_t>(a.c.length[s]) - count + (t - first);
+  const int held = a.c.length[s];
+  if (!a.starts && held == 0) return;  // an idle sequence of the batch
+  const int64_t at = static_cast<int64_t>(held) - count + (t - first);
   const bool inside = at >= 0 && at < a.c.cap && t >= first && t - first < count;
   const int slot = inside ? static_cast<int>(at) : 0;
   const int32_t page = inside ? a.c.page_of(s, slot) : -1;

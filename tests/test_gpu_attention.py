@@ -364,7 +364,12 @@ def test_append_in_place_by_slot_and_bad_places():
     B.ordermoe_cache_append(cache, nk, nv, q=same, q_out=same, inv_freq=freq)  # positions are slots
     assert torch.equal(same, out)
     before = k.clone(), v.clone()
-    length[0], length[1], length[2] = 0, cache.slots + 1, 3
+    length[0] = 0  # idle: left out without a word
+    left = torch.full_like(q, 3.0)
+    B.ordermoe_cache_append(cache, nk, nv, q=q, q_out=left, inv_freq=freq)
+    assert B.ordermoe_device_error()[0] == 0
+    assert bool((left[0] == 3.0).all()) and torch.equal(left[1:], out[1:]) and torch.equal(k, before[0])
+    length[0], length[1], length[2] = -1, cache.slots + 1, 3
     table[2, 0] = k.shape[0] + 7
     left = torch.full_like(q, 3.0)
     B.ordermoe_cache_append(cache, nk, nv, q=q, q_out=left, inv_freq=freq)
