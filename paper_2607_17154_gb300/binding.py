@@ -566,10 +566,10 @@ def _rows(t, name, shape, device, dtypes=(_BF16,)):
 
 
 def _vector(t, name, dtype, n, device):
-    """_entries, sooner for a sound tensor of one dimension."""
+    """_entries, with its checks in one pass."""
     if t is None:
         return None
-    if t.dtype is dtype and t.get_device() == device and t.dim() == 1 and len(t) >= n and t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == device and t.numel() >= n and t.is_contiguous():
         return t.data_ptr()
     return _entries(t, name, dtype, n, device)
 
@@ -699,12 +699,14 @@ def _stack(t, name, shape, device):
     if t.get_device() != device:
         raise ValueError("%s must be on the current device, cuda:%d" % (name, device))
     n, rows, w = shape
-    if w > 1 and t.stride(2) != 1:
+    stride, ld, one = t.stride()
+    if w > 1 and one != 1:
         raise ValueError("the rows of %s must be contiguous" % name)
-    ld = t.stride(1) if rows > 1 else (w + 7) // 8 * 8
+    if rows <= 1:
+        ld = (w + 7) // 8 * 8
     if ld < w:
         raise ValueError("the rows of %s must not overlap" % name)
-    return t.data_ptr(), t.stride(0) if n > 1 else 0, ld
+    return t.data_ptr(), stride if n > 1 else 0, ld
 
 
 def ordermoe_adapters(X, A, Bw, ids, Y, workspace, scale=None, rank=None, residual=None, stream=None):
