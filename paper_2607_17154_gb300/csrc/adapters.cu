@@ -65,7 +65,7 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 
 // The tokens of a tile by adapter.
 struct Groups {
-  alignas(16) int id[TILE];  // adapter of each token, -1: none
+  alignas(16) int id[TILE];  // adapter of each token, -1: none, -2: no token
   int rank[TILE];            // its ranks in use and its scale
   float scale[TILE];
   int leader[TILE];          // the first token of each distinct adapter, in order
@@ -77,7 +77,7 @@ struct Groups {
 // Returns whether a token has no adapter.
 __device__ __forceinline__ bool find_groups(const Args& a, Groups& s, int t0, bool tell) {
   const int tid = threadIdx.x, lane = tid % 32;
-  int id = -1, rank = a.R;
+  int id = t0 + tid < a.T ? -1 : -2, rank = a.R;
   float scale = 1.0f;
   if (tid < TILE) {
     if (t0 + tid < a.T) {
@@ -119,7 +119,7 @@ __device__ __forceinline__ bool find_groups(const Args& a, Groups& s, int t0, bo
     if (first) s.leader[at + __popc(v & ((1u << lane) - 1))] = tid;
     if (tid == TILE - 1) s.distinct = at + __popc(v);
   }
-  return __syncthreads_or(tid < TILE && t0 + tid < a.T && id < 0);
+  return __syncthreads_or(tid < TILE && id == -1);
 }
 // Lists the tokens with adapter `id` (tile's index, in order) for this warp; their number.
 __device__ __forceinline__ int list_rows(Groups& s, int id) {
@@ -343,7 +343,7 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
 // PARTS bf16 parts: two (16 bits) for results of 16 bits, three for those of 32. Warps share the blocks of 16 tokens and, where
 // there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
-// residual) is asked for before the first kernel has ended. Tokens without an adapter go with the first.
+// residual) is asked for before the first kernel has ended. Tokens without an adapter are a group of their own.
 constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice (ranks: 64 or 128)
 // Threads of a CTA: two CTAs an SM, or one of as many warps where shared memory has no room for two; with few tokens
 // registers (for weights) are worth more than warps.
@@ -382,21 +382,25 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
     const int z1 = a.flat && hi - before < slices ? static_cast<int>(hi - before) : slices, dz = a.flat ? 1 : gridDim.z;
     if (tile > tile0) __syncthreads();  // the groups before are done with
     const bool alone = find_groups(a, s, t0, false);
-    if (alone && blockIdx.y == 0 && a.res != a.Y) {
-      const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
-      for (int z = z0; z < z1; z += dz)
-        for (int i = tid; i < TILE * (by8 ? NB / 8 : NB); i += THREADS) {
-          const int row = by8 ? i / (NB / 8) : i / NB, c = z * NB + (by8 ? i % (NB / 8) * 8 : i % NB);
-          if (t0 + row >= a.T || s.id[row] >= 0 || c >= a.N) continue;
+    const int groups_of = s.distinct + (alone && a.res != a.Y ? 1 : 0);
+    for (int d = blockIdx.y; d < groups_of; d += gridDim.y) {
+      if (d == s.distinct) {  // tokens without an adapter: the residual as it is
+        const int rows = list_rows(s, -1), mine = z1 > z0 ? (z1 - z0 + dz - 1) / dz : 0;
+        const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
+        const int width = by8 ? NB / 8 : NB;
+        for (int64_t i = tid; i < static_cast<int64_t>(mine) * rows * width; i += THREADS) {
+          const int64_t t = t0 + s.row[w][i / width % rows];
+          const int c = (z0 + static_cast<int>(i / (width * rows)) * dz) * NB + static_cast<int>(i % width) * (by8 ? 8 : 1);
+          if (c >= a.N) continue;
           if (by8) {
             float v[8] = {};
-            put8(a, t0 + row, c, get8(a, t0 + row, c), v);
+            put8(a, t, c, get8(a, t, c), v);
           } else {
-            put1(a, t0 + row, c, a.res ? a.res[static_cast<int64_t>(t0 + row) * a.ldr + c] : 0u, 0.0f);
+            put1(a, t, c, a.res ? a.res[t * a.ldr + c] : 0u, 0.0f);
           }
         }
-    }
-    for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
+        continue;
+      }
       const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead];
       const int rv = (r + 15) / 16 * 2;  // vectors of 8 ranks, even
       const uint16_t* B = a.B + id * a.stride_b;
@@ -418,15 +422,7 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
 #pragma unroll
             for (int k = 0; k < RANKS / 32; ++k) {
               b[j][k] = make_uint4(0, 0, 0, 0);
-              const int left = r - k * 32 - q4 * 8;
-              if (col >= a.N || left <= 0) continue;
-              b[j][k] = *reinterpret_cast<const uint4*>(from + k * 32);
-              if (left < 8) {  // columns behind the rank say nothing, whatever they hold
-                uint32_t* x = reinterpret_cast<uint32_t*>(&b[j][k]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  x[e] = 2 * e + 1 < left ? x[e] : 2 * e < left ? x[e] & 0xFFFFu : 0u;
-              }
+              if (col < a.N && k * 32 + q4 * 8 < r) b[j][k] = *reinterpret_cast<const uint4*>(from + k * 32);
             }
           }
 #pragma unroll
@@ -436,6 +432,10 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
         const int n0 = a.flat ? z0 * (NB / 32) + w : z0 * WARPS + w, dn = a.flat ? WARPS : dz * WARPS;
         const int n1 = a.flat && z1 * (NB / 32) < groups ? z1 * (NB / 32) : groups;
         if (n0 < n1) ask(n0);
+        for (int n = n0 + dn; n < n1; n += dn)  // the turns behind it, as far as L2
+          if (n * 32 + lane < a.N)
+            for (int c = 0; c < r; c += 64)
+              asm volatile("prefetch.global.L2 [%0];" ::"l"(B + (n * 32 + lane) * a.ldb + c));
         if (!waited) pdl_wait();
         waited = true;
         for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
@@ -449,6 +449,15 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
 #pragma unroll
           for (int k = 0; k < RANKS / 32; ++k) {
             if (k >= steps) continue;
+            if (k * 32 + 32 > r) {  // columns behind the rank say nothing, whatever they hold
+              const int left = r - k * 32 - q4 * 8;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t* x = reinterpret_cast<uint32_t*>(&b[j][k]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = 2 * e + 1 < left ? x[e] : 2 * e < left ? x[e] & 0xFFFFu : 0u;
+              }
+            }
             float h[2][8];
 #pragma unroll
             for (int e = 0; e < 2; ++e)
