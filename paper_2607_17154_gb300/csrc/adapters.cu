@@ -338,8 +338,8 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
   }
 }
 
-// Y = residual + scale B H for a tile's j-th distinct adapter, in slices of 128 columns: those of a CTA are
-// blockIdx.z, + gridDim.z and so on, the next one's weights on their way while one is computed. H's fp32 sums become
+// Y = residual + scale B H for a tile's adapters, in slices of 128 columns, the next one's weights on their way while
+// one is computed. H's fp32 sums become
 // PARTS bf16 parts: two (16 bits) for results of 16 bits, three for those of 32. Warps share the blocks of 16 tokens and, where
 // there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
@@ -370,20 +370,46 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
   const uint32_t hs = smem_u32(parts), bs = hs + PARTS * a.rows * ld;
   const int slices = (a.N + NB - 1) / NB;
   const long long all = static_cast<long long>(slices) * ((a.T - 1) / TILE + 1);
-  const long long lo = all * blockIdx.x / gridDim.x, hi = all * (blockIdx.x + 1) / gridDim.x;
-  const int tile0 = a.flat ? static_cast<int>(lo / slices) : static_cast<int>(blockIdx.x);
-  const int tile1 = a.flat ? static_cast<int>((hi - 1) / slices) : tile0;
+  const long long lo = all * blockIdx.x / gridDim.x, hi = all * (blockIdx.x + 1) / gridDim.x;  // flat: this CTA's slices
+  const int tile0 = !FEW && a.flat ? static_cast<int>(lo / slices) : static_cast<int>(blockIdx.x);
+  const int tile1 = !FEW && a.flat ? static_cast<int>((hi - 1) / slices) : tile0;
   bool waited = false;
   for (int tile = tile0; tile <= tile1; ++tile) {
     const int t0 = tile * TILE;
     const long long before = static_cast<long long>(tile) * slices;
-    // this CTA's slices of the tile: z0, z0 + dz and so on below z1
-    const int z0 = !a.flat ? static_cast<int>(blockIdx.z) : lo > before ? static_cast<int>(lo - before) : 0;
-    const int z1 = a.flat && hi - before < slices ? static_cast<int>(hi - before) : slices, dz = a.flat ? 1 : gridDim.z;
     if (tile > tile0) __syncthreads();  // the groups before are done with
     const bool alone = find_groups(a, s, t0, false);
-    const int groups_of = s.distinct + (alone && a.res != a.Y ? 1 : 0);
-    for (int d = blockIdx.y; d < groups_of; d += gridDim.y) {
+    // The tile's groups are its adapters, and the tokens without one. Few tokens an adapter: where the groups leave few of
+    // the tile's CTAs idle each has as many for itself, which take every dz-th slice; else groups times slices are shared
+    // out evenly, group after group. More tokens: a CTA has the same slices of every group, or of every dg-th where
+    // there are more CTAs than slices, because groups of more tokens cost more (2001 tokens of runs of 466, R 128: 131 us,
+    // groups apart 171).
+    const int groups_of = s.distinct + (alone && a.res != a.Y ? 1 : 0), q = blockIdx.y, Q = gridDim.y;
+    const bool apart = FEW && groups_of > 0 && groups_of <= Q && Q % groups_of <= Q / 16;
+    const int dz = FEW ? (apart ? Q / groups_of : 1) : a.flat ? 1 : min(Q, slices), dg = FEW || a.flat ? 1 : Q / dz;
+    int d0 = FEW || a.flat ? 0 : q / dz, d1 = !FEW && d0 >= dg ? 0 : groups_of;
+    int z_first = a.flat ? static_cast<int>(max(lo - before, 0ll)) : q % dz, z_end = slices;
+    long long u0 = 0, u1 = 0;
+    if (!FEW && a.flat && hi - before < slices) z_end = static_cast<int>(hi - before);
+    if (FEW && apart) {
+      d0 = q / dz;
+      d1 = min(d0 + 1, groups_of);
+    } else if (FEW) {
+      const long long units = static_cast<long long>(groups_of) * slices;
+      u0 = units * q / Q;
+      u1 = units * (q + 1) / Q;
+      d0 = static_cast<int>(u0 / slices);
+      d1 = static_cast<int>((u1 + slices - 1) / slices);
+    }
+    for (int d = d0; d < d1; d += dg) {
+      if (FEW && apart) {
+        z_first = q % dz;
+      } else if (FEW) {
+        const long long start = static_cast<long long>(d) * slices;
+        z_first = static_cast<int>(max(u0 - start, 0ll));
+        z_end = static_cast<int>(min(u1 - start, static_cast<long long>(slices)));
+      }
+      const int z0 = z_first, z1 = z_end;
       if (d == s.distinct) {  // tokens without an adapter: the residual as it is
         const int rows = list_rows(s, -1), mine = z1 > z0 ? (z1 - z0 + dz - 1) / dz : 0;
         const bool by8 = a.vec_y && (a.vec_r || !a.res) && a.N % 8 == 0;
@@ -429,8 +455,9 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
           for (int h = 0; h < 2; ++h)
             if (tok[h] >= 0) u[h] = get8(a, tok[h], n * 32 + q4 * 8);
         };
-        const int n0 = a.flat ? z0 * (NB / 32) + w : z0 * WARPS + w, dn = a.flat ? WARPS : dz * WARPS;
-        const int n1 = a.flat && z1 * (NB / 32) < groups ? z1 * (NB / 32) : groups;
+        // eight times 32 columns a turn
+        const int n0 = apart ? z0 * WARPS + w : z0 * (NB / 32) + w, dn = dz * WARPS;
+        const int n1 = apart ? groups : min(z1 * (NB / 32), groups);
         if (n0 < n1) ask(n0);
         for (int n = n0 + dn; n < n1; n += dn)  // the turns behind it, as far as L2
           if (n * 32 + lane < a.N)
@@ -800,17 +827,12 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   const bool few = tokens <= 16 * distinct;  // 16 tokens of an adapter in a tile or fewer, in the mean of all that it can have
   const int64_t ctas = (ad::up_pairs(parts, low ? 64 : ad::MAX_R) ? 2 : 1) * ad::SMS;
   const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB, mine = ctas / p.tiles;
-  dim3 grid;
-  if (p.tiles <= 4) {
-    const unsigned z = at_most(mine / distinct, few ? (slices + 1) / 2 : slices);  // few: a turn has two slices
-    grid = dim3(p.tiles, at_most(mine / z, distinct), z);
-  } else {
-    // Slices of a CTA where the tiles share the CTAs evenly, and where all tiles' slices do: then most CTAs meet two tiles
-    // and sum up H twice, which costs as much as 1.5 slices (32 tiles, N 14336, R 64, 304 CTAs: 13 slices 82 us, 11.8 90).
-    const int64_t z = at_most(mine, slices), rounds = (p.tiles * z + ctas - 1) / ctas * ((slices + z - 1) / z);
-    a.flat = 2 * rounds * ctas > 2 * p.tiles * slices + 3 * ctas;
-    grid = a.flat ? dim3(at_most(ctas, p.tiles * slices), 1, 1) : dim3(p.tiles, at_most(mine / z, distinct), static_cast<unsigned>(z));
-  }
+  // Slices of a CTA where the tiles share the CTAs evenly, and where all tiles' slices do: then most CTAs meet two tiles
+  // and sum up H twice, which costs as much as 1.5 slices (32 tiles, N 14336, R 64, 304 CTAs: 13 slices 82 us, 11.8 90).
+  const int64_t z = at_most(mine, slices), rounds = (p.tiles * z + ctas - 1) / ctas * ((slices + z - 1) / z);
+  a.flat = !few && p.tiles > 4 && 2 * rounds * ctas > 2 * p.tiles * slices + 3 * ctas;
+  const int64_t turns = (distinct + 1) * (few ? (slices + 1) / 2 : slices);  // few: a turn has two slices
+  const dim3 grid = a.flat ? dim3(at_most(ctas, p.tiles * slices)) : dim3(p.tiles, at_most(mine, turns));
   const size_t smem = static_cast<size_t>(ad::up_smem(a.rows, low ? 64 : ad::MAX_R, parts, few));
   const bool plain = !f32 && residual && a.vec_r && a.vec_y && N % 8 == 0;
   ad::Up up = nullptr;
