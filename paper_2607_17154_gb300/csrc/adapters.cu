@@ -1,9 +1,14 @@
 // Low-rank adapters of many requests beside a shared projection: Y[t] = residual[t] + scale_a B_a (A_a X[t]).
 //
 // Two products of R <= 128: H = A X^T by a first kernel (K shared out over CTAs, partial sums in fp32), B H by a second one.
-// Both are bound by bytes (X, Y and the used adapters' weights), or with few tokens by latency. Tokens come in
-// any order of adapters: a tile is 128 tokens, and a CTA takes the j-th distinct adapter among them with the tokens that
-// have it, so an adapter's weights are read once a tile whatever the order.
+// What the operator cannot do without are bytes (X, Y, residual, the used adapters' weights); with few tokens latency is
+// longer. Tokens come in any order of adapters: a tile is 128 tokens, and a CTA takes adapters of a tile with the tokens
+// that have them, so an adapter's weights are read once a tile whatever the order (and from L2 by the later tiles). Both products run on
+// mma.sync: the tokens of an adapter are its M side, 1 to 128 of them, in blocks of 16.
+// Measured (both kernels, launched from the host): 1 token, K = N = 4096, R 16: 6.7 us; 128 tokens on 32 adapters, K 4096, N
+// 6144, R 64: 18.8 us, floor 3.7; 4096 tokens on 8 adapters, K 4096, N 14336, R 64: 79 us = 3.6 TB/s, floor 42.6
+// (the first kernel 16, the second 62: four products of 16 tokens x 32 columns a residual vector, 1.5 instructions a cycle
+// and SM; its tensor pipe is busy for 25 us).
 #include <type_traits>
 
 #include "common.cuh"
@@ -339,12 +344,12 @@ __device__ __forceinline__ void put8(const Args& a, int64_t t, int c, const uint
 }
 
 // Y = residual + scale B H for a tile's adapters, in slices of 128 columns, the next one's weights on their way while
-// one is computed. H's fp32 sums become
-// PARTS bf16 parts: two (16 bits) for results of 16 bits, three for those of 32. Warps share the blocks of 16 tokens and, where
-// there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
+// one is computed. H's fp32 sums, times the scale, become PARTS bf16 parts: two (16 bits) for results of 16 bits (with one
+// Y would be off by as much again as its own rounding), three for those of 32. Warps share the blocks of 16 tokens and,
+// where there are fewer of those, the slice's columns. The columns of four products of 8 are dealt out so that each thread
 // holds eight in a row: column c of product j is 8 (c / 2) + 2 j + c % 2 of 32. What does not depend on H (weights,
 // residual) is asked for before the first kernel has ended. Tokens without an adapter are a group of their own.
-constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice (ranks: 64 or 128)
+constexpr int up_row(int ranks) { return ranks * 2 + 16; }  // bytes of a row of H's parts and of B: no bank is met twice
 // Threads of a CTA: two CTAs an SM, or one of as many warps where shared memory has no room for two; with few tokens
 // registers (for weights) are worth more than warps.
 constexpr bool up_pairs(int parts, int ranks) { return parts == 2 && ranks == 64; }
@@ -824,7 +829,10 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
                 dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
   const int parts = f32 ? 3 : 2;
-  const bool few = tokens <= 16 * distinct;  // 16 tokens of an adapter in a tile or fewer, in the mean of all that it can have
+  // Few tokens an adapter: up to 16 in the mean of all adapters that a tile can have; in batches of many tiles, where an
+  // adapter's tokens mostly follow one another, up to 8 (4096 tokens, N 14336, 8 adapters in runs of 512: 85 us by the
+  // form for few, 79 by the other; 2072 tokens, N 9512, 25 adapters in runs of 7: 71 and 119)
+  const bool few = tokens <= (p.tiles > 4 ? 8 : 16) * distinct;
   const int64_t ctas = (ad::up_pairs(parts, low ? 64 : ad::MAX_R) ? 2 : 1) * ad::SMS;
   const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB, mine = ctas / p.tiles;
   // Slices of a CTA where the tiles share the CTAs evenly, and where all tiles' slices do: then most CTAs meet two tiles
