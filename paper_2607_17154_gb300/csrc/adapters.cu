@@ -5,8 +5,8 @@
 // longer. Tokens come in any order of adapters: a tile is 128 tokens, and a CTA takes adapters of a tile with the tokens
 // that have them, so an adapter's weights are read once a tile whatever the order (and from L2 by the later tiles). Both products run on
 // mma.sync: the tokens of an adapter are its M side, 1 to 128 of them, in blocks of 16.
-// Measured (both kernels, launched from the host): 1 token, K = N = 4096, R 16: 6.7 us; 128 tokens on 32 adapters, K 4096, N
-// 6144, R 64: 18.8 us, floor 3.7; 4096 tokens on 8 adapters, K 4096, N 14336, R 64: 79 us = 3.6 TB/s, floor 42.6
+// Measured (both kernels, launched from the host): 1 token, K = N = 4096, R 16: 6.1 us; 128 tokens on 32 adapters, K 4096, N
+// 6144, R 64: 16.0 us, floor 3.7; 4096 tokens on 8 adapters, K 4096, N 14336, R 64: 79 us = 3.6 TB/s, floor 42.6
 // (the first kernel 16, the second 62: four products of 16 tokens x 32 columns a residual vector, 1.5 instructions a cycle
 // and SM; its tensor pipe is busy for 25 us).
 #include <type_traits>
@@ -42,7 +42,7 @@ struct Args {
   const float* scale;
   const uint16_t* res; int64_t ldr;
   void* Y; int64_t ldy;
-  int n, R, T, N, K, f32, split, share;  // share: steps of K of a CTA
+  int n, R, T, N, K, f32, split, ctas;   // the most parts of K, and the first kernel's CTAs of a tile
   int vec_r, vec_y;                      // residual and Y may be moved 16 bytes at a time
   int flat;                              // second kernel: all tiles' slices shared out evenly over the CTAs
   int rows, ranks;                       // of a tile, in steps of 16 (what shared memory is laid out for)
@@ -142,97 +142,132 @@ __device__ __forceinline__ int list_rows(Groups& s, int id) {
   return at;
 }
 
+// Into how many parts K goes for every adapter of a tile, so that its adapters use the tile's CTAs; `share`: steps of a part.
+__device__ __forceinline__ int tile_split(const Args& a, int distinct, int& share) {
+  const int steps = (a.K + KB - 1) / KB, want = distinct > 0 ? a.ctas / distinct : 1;
+  share = (steps + a.split - 1) / a.split;
+  if (want < a.split) share = want > 1 ? (steps + want - 1) / want : steps;
+  return (steps + share - 1) / share;
+}
+
 // 16-byte vectors of rows of 64 (8 vectors), exchanged by the row's lowest three bits.
 __device__ __forceinline__ uint32_t at64(int row, int vec) { return (row * 8 + (vec ^ (row & 7))) * 16; }
 
-// H[split][t][r] over a CTA's steps of K. A step has 64 of K of up to 128 tokens and all ranks in shared memory.
-// Up to 16 tokens: the warps share the step's four products of 16 of K and halves of the ranks, and add up at the end;
-// more: 16 tokens a warp.
-constexpr int FEW_STAGES = 6, MANY_STAGES = 3;
+// H[split][t][r] over a CTA's part of K, in steps of 64 of K of up to 128 tokens and all ranks in shared memory, 16 tokens
+// a warp. Up to 16 tokens: steps of 128, whose instructions are fewer (64: 51 us where 128 take 18, 9 tiles x 32 adapters of 4
+// tokens, K 4431, R 16); the warps share a step's products of 16 of K and the ranks, and add up at the end.
+constexpr int FEW_KB = 128, MANY_STAGES = 3;
+constexpr int few_stages(int ranks) { return ranks <= 64 ? 4 : 3; }  // so that an SM has room for two CTAs
 constexpr int SUMS = 4 * 16 * (MAX_R + 2) * 4;  // bytes of four warps' sums of 16 tokens
 constexpr int down_smem(int rows, int ranks) {
-  const int many = MANY_STAGES * (rows + ranks) * KB * 2, few = FEW_STAGES * (16 + ranks) * KB * 2;
+  const int many = MANY_STAGES * (rows + ranks) * KB * 2, few = few_stages(ranks) * (16 + ranks) * FEW_KB * 2;
   const int ring = many > few && rows > 16 ? many : few;
   return ring > SUMS ? ring : SUMS;
 }
-__global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
+__global__ void __launch_bounds__(THREADS, 2) adapters_down_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ Groups s;
   pdl_wait();
   pdl_trigger();
   const int t0 = blockIdx.x * TILE, tid = threadIdx.x, lane = tid % 32, w = tid / 32, g = lane / 4, q4 = lane % 4;
-  const bool tell = blockIdx.y == 0 && blockIdx.z == 0;
-  find_groups(a, s, t0, tell);
-  const int k0 = blockIdx.z * a.share, steps_all = (a.K + KB - 1) / KB;
-  const int k1 = min(k0 + a.share, steps_all);
+  find_groups(a, s, t0, blockIdx.y == 0);
+  int share;
+  const int split = tile_split(a, s.distinct, share), part_of = blockIdx.y % split, dg = gridDim.y / split;
+  const int k0 = part_of * share, k1 = min(k0 + share, (a.K + KB - 1) / KB);
+  if (static_cast<int>(blockIdx.y) / split >= dg) return;
   const uint32_t base = smem_u32(ring);
-  for (int d = blockIdx.y; d < s.distinct; d += gridDim.y) {
+  for (int d = blockIdx.y / split; d < s.distinct; d += dg) {
     const int lead = s.leader[d], id = s.id[lead], rows = list_rows(s, id), r = s.rank[lead], rt = (r + 15) / 16 * 16;
     const int m16 = (rows + 15) / 16 * 16;
     const uint16_t* A = a.A + id * a.stride_a;
     const bool few = rows <= 16;
-    const int x_bytes = (few ? 16 : a.rows) * KB * 2, stage_bytes = x_bytes + a.ranks * KB * 2;
-    // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
-    const int v = tid % 8;
-    const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + v * 8;
-#pragma unroll
-    for (int e = 0; e < TILE / 32; ++e)
-      xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[w][tid / 8 + e * 32]) * a.ldx + v * 8 : nullptr;
-    const uint32_t place = base + at64(tid / 8, v);
-    auto fetch = [&](int kb, int stage) {
-      const uint32_t xs = place + stage * stage_bytes, as = xs + x_bytes;
-      const int left = a.K - kb * KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-#pragma unroll
-      for (int e = 0; e < TILE / 32; ++e)
-        if (tid / 8 + e * 32 < m16) {
-          const bool ok = xp[e] && bytes > 0;
-          cp16(xs + e * 32 * KB * 2, ok ? xp[e] + kb * KB : a.X, ok ? bytes : 0);
-        }
-#pragma unroll
-      for (int e = 0; e < MAX_R / 32; ++e)
-        if (tid / 8 + e * 32 < rt) {
-          const bool ok = tid / 8 + e * 32 < r && bytes > 0;
-          cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + kb * KB : a.A, ok ? bytes : 0);
-        }
-    };
     float acc[MAX_R / 8][4];
 #pragma unroll
     for (int n = 0; n < MAX_R / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-    // The steps through a ring of `stages`; `step` has a step's products.
-    auto steps = [&](auto stages, auto step) {
+    // `count` steps through a ring of `stages`: `fetch` fills a stage, `step` has its products.
+    auto steps = [&](auto stages, int count, int stage_bytes, auto fetch, auto step) {
       constexpr int STAGES = decltype(stages)::value;
       for (int i = 0; i < STAGES - 1; ++i) {
-        if (k0 + i < k1) fetch(k0 + i, i);
+        if (i < count) fetch(i, base + i * stage_bytes);
         cp_commit();
       }
       int stage = 0, free = STAGES - 1;
-      for (int kb = k0; kb < k1; ++kb) {
+      for (int i = 0; i < count; ++i) {
         cp_wait<STAGES - 2>();
         __syncthreads();
-        if (kb + STAGES - 1 < k1) fetch(kb + STAGES - 1, free);
+        if (i + STAGES - 1 < count) fetch(i + STAGES - 1, base + free * stage_bytes);
         cp_commit();
         free = free + 1 == STAGES ? 0 : free + 1;
-        step(base + stage * stage_bytes, base + stage * stage_bytes + x_bytes);
+        step(base + stage * stage_bytes);
         stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
     };
-    if (few)
-      steps(std::integral_constant<int, FEW_STAGES>{}, [&](uint32_t xs, uint32_t as) {
-        const int k = w & 3;
-        uint32_t x[4], b[4];
-        ldm4(x, xs + at64((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+    const int k_first = k0 * KB, k_end = min(k1 * KB, a.K);
+    if (few) {  // steps of 128 of K: a row is 16 vectors, a thread's rows are tid / 16 and of A every 16th from there
+      constexpr int X_BYTES = 16 * FEW_KB * 2;
+      const int v = tid % 16, row = tid / 16;
+      const uint16_t* xp = row < rows ? a.X + (t0 + s.row[w][row]) * a.ldx + k_first + v * 8 : nullptr;
+      const uint16_t* ap = A + row * a.lda + k_first + v * 8;
+      auto at = [](int r_, int v_) { return (r_ * 16 + (v_ ^ (r_ & 7))) * 16; };
+      const uint32_t place = at(row, v);
+      auto fetch = [&](int i, uint32_t stage) {
+        const int left = k_end - k_first - i * FEW_KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+        const bool on = xp && bytes > 0;
+        cp16(stage + place, on ? xp + i * FEW_KB : a.X, on ? bytes : 0);
 #pragma unroll
-        for (int n = 0; n < MAX_R / 8; n += 2) {
-          if (n * 8 >= r) break;
-          if ((n / 2 & 1) != w / 4) continue;
-          ldm4(b, as + at64(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
-          mma(acc[n], x, b[0], b[1]);
-          mma(acc[n + 1], x, b[2], b[3]);
+        for (int e = 0; e < MAX_R / 16; ++e) {
+          if (e * 16 >= rt) break;
+          const bool ok = row + e * 16 < r && bytes > 0;
+          cp16(stage + X_BYTES + place + e * X_BYTES, ok ? ap + e * 16 * a.lda + i * FEW_KB : a.A, ok ? bytes : 0);
         }
-      });
-    else
-      steps(std::integral_constant<int, MANY_STAGES>{}, [&](uint32_t xs, uint32_t as) {
+      };
+      // warps w and w + 4 have products w % 4 and w % 4 + 4 of 16 of K, of every other 16 ranks
+      auto step = [&](uint32_t xs) {
+#pragma unroll
+        for (int h = 0; h < FEW_KB / 64; ++h) {
+          const int k = (w & 3) + 4 * h;
+          uint32_t x[4], b[4];
+          ldm4(x, xs + at((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+#pragma unroll
+          for (int n = 0; n < MAX_R / 8; n += 2) {
+            if (n * 8 >= r) break;
+            if ((n / 2 & 1) != w / 4) continue;
+            ldm4(b, xs + X_BYTES + at(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
+            mma(acc[n], x, b[0], b[1]);
+            mma(acc[n + 1], x, b[2], b[3]);
+          }
+        }
+      };
+      const int count = (k_end - k_first + FEW_KB - 1) / FEW_KB, bytes = (16 + a.ranks) * FEW_KB * 2;
+      if (a.ranks <= 64) steps(std::integral_constant<int, few_stages(64)>{}, count, bytes, fetch, step);
+      else steps(std::integral_constant<int, few_stages(MAX_R)>{}, count, bytes, fetch, step);
+    } else {
+      // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
+      const int v = tid % 8, x_bytes = a.rows * KB * 2;
+      const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + k_first + v * 8;
+#pragma unroll
+      for (int e = 0; e < TILE / 32; ++e)
+        xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[w][tid / 8 + e * 32]) * a.ldx + k_first + v * 8 : nullptr;
+      const uint32_t place = at64(tid / 8, v);
+      auto fetch = [&](int i, uint32_t stage) {
+        const uint32_t xs = stage + place, as = xs + x_bytes;
+        const int left = k_end - k_first - i * KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+#pragma unroll
+        for (int e = 0; e < TILE / 32; ++e)
+          if (tid / 8 + e * 32 < m16) {
+            const bool ok = xp[e] && bytes > 0;
+            cp16(xs + e * 32 * KB * 2, ok ? xp[e] + i * KB : a.X, ok ? bytes : 0);
+          }
+#pragma unroll
+        for (int e = 0; e < MAX_R / 32; ++e)
+          if (tid / 8 + e * 32 < rt) {
+            const bool ok = tid / 8 + e * 32 < r && bytes > 0;
+            cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + i * KB : a.A, ok ? bytes : 0);
+          }
+      };
+      auto step = [&](uint32_t xs) {
         if (w * 16 >= rows) return;
+        const uint32_t as = xs + x_bytes;
         uint32_t x[KB / 16][4];
 #pragma unroll
         for (int k = 0; k < KB / 16; ++k) ldm4(x[k], xs + at64(w * 16 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
@@ -247,10 +282,12 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
             mma(acc[n + 1], x[k], b[2], b[3]);
           }
         }
-      });
+      };
+      steps(std::integral_constant<int, MANY_STAGES>{}, k1 - k0, x_bytes + a.ranks * KB * 2, fetch, step);
+    }
     cp_wait<0>();
     __syncthreads();
-    float* H = a.H + (static_cast<int64_t>(blockIdx.z) * a.T + t0) * a.R;
+    float* H = a.H + (static_cast<int64_t>(part_of) * a.T + t0) * a.R;
     if (few) {  // four warps have sums of the same ranks
       float* part = reinterpret_cast<float*>(ring);  // [4][16][LD]
       constexpr int LD = MAX_R + 2;
@@ -282,12 +319,12 @@ __global__ void __launch_bounds__(THREADS) adapters_down_kernel(const Args a) {
 }
 
 // Four of a token's ranks, c and on, from the first kernel's partial sums; zeros behind the rank.
-__device__ __forceinline__ float4 sum_h(const Args& a, int64_t t, int c, int r) {
+__device__ __forceinline__ float4 sum_h(const Args& a, int split, int64_t t, int c, int r) {
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   if (c >= r) return v;
   const float* h = a.H + t * a.R + c;
 #pragma unroll 8
-  for (int p = 0; p < a.split; ++p, h += static_cast<int64_t>(a.T) * a.R) {
+  for (int p = 0; p < split; ++p, h += static_cast<int64_t>(a.T) * a.R) {
     const float4 x = *reinterpret_cast<const float4*>(h);
     v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
   }
@@ -389,6 +426,8 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
     // out evenly, group after group. More tokens: a CTA has the same slices of every group, or of every dg-th where
     // there are more CTAs than slices, because groups of more tokens cost more (2001 tokens of runs of 466, R 128: 131 us,
     // groups apart 171).
+    int share_k;
+    const int split = tile_split(a, s.distinct, share_k);
     const int groups_of = s.distinct + (alone && a.res != a.Y ? 1 : 0), q = blockIdx.y, Q = gridDim.y;
     const bool apart = FEW && groups_of > 0 && groups_of <= Q && Q % groups_of <= Q / 16;
     const int dz = FEW ? (apart ? Q / groups_of : 1) : a.flat ? 1 : min(Q, slices), dg = FEW || a.flat ? 1 : Q / dz;
@@ -472,7 +511,7 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
         waited = true;
         for (int i = tid; i < 16 * steps * 8; i += THREADS) {  // four ranks of a token
           const int row = i / (steps * 8), c = (i - row * steps * 8) * 4;
-          const float4 v = row < rows ? sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          const float4 v = row < rows ? sum_h(a, split, static_cast<int64_t>(t0) + s.row[w][row], c, r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           *reinterpret_cast<float4*>(sum + row * LD + c) = v;
         }
         __syncthreads();
@@ -554,7 +593,7 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
       for (int i = tid; i < m16 * rv * 2; i += THREADS) {  // four ranks of a token
         const int row = i / (rv * 2), c = (i - row * rv * 2) * 4;
         alignas(16) float v[4] = {};
-        if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, static_cast<int64_t>(t0) + s.row[w][row], c, r);
+        if (row < rows) *reinterpret_cast<float4*>(v) = sum_h(a, split, static_cast<int64_t>(t0) + s.row[w][row], c, r);
         v[0] *= scale; v[1] *= scale; v[2] *= scale; v[3] *= scale;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
@@ -703,12 +742,12 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
   if (!waited) pdl_wait();  // never done before the first kernel
 }
 
-// How K is shared out: two CTAs an SM, with the adapters that a tile may have where there are few tiles (with many, most
-// tiles have one or two); four steps each at least. (4096 tokens on 8 adapters, K 4096, N 14336, R 64, both kernels:
+// Into how many parts K may go: two CTAs an SM with the tiles (less where a tile turns out to have many adapters, see
+// tile_split); four steps each at least. (4096 tokens on 8 adapters, K 4096, N 14336, R 64, both kernels:
 // one CTA an SM 105 us, two 93.)
 constexpr int SMS = 152;
 struct Plan {
-  int tiles, split, share;
+  int tiles, split;
 };
 // n = 0: the most that any number of adapters asks for (what a workspace holds).
 static Plan plan(int T, int K, int R, int n) {
@@ -718,7 +757,6 @@ static Plan plan(int T, int K, int R, int n) {
   int want = 2 * SMS / p.tiles;
   if (n > 0) {
     const int tokens = T < TILE ? T : TILE, distinct = p.tiles > 4 ? 1 : tokens < n ? tokens : n;
-    want = 2 * SMS / (p.tiles * distinct);
     // A step costs a CTA about what one more partial sum of 128 tokens and 64 ranks costs each CTA of the second
     // kernel (0.35 us): no more parts than make the two equal.
     const long long even = static_cast<long long>(steps) * (TILE * 64) * distinct / (static_cast<long long>(tokens) * R);
@@ -728,8 +766,8 @@ static Plan plan(int T, int K, int R, int n) {
   if (want > MAX_SPLIT) want = MAX_SPLIT;
   if (want > steps / 4) want = steps / 4;
   if (want < 1) want = 1;
-  p.share = (steps + want - 1) / want;
-  p.split = (steps + p.share - 1) / p.share;
+  const int share = (steps + want - 1) / want;
+  p.split = (steps + share - 1) / share;
   return p;
 }
 
@@ -814,7 +852,7 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   ad::Args a{};
   a.X = X; a.ldx = ldx; a.A = A; a.stride_a = stride_a; a.lda = lda; a.B = B; a.stride_b = stride_b; a.ldb = ldb;
   a.ids = ids; a.rank = rank; a.scale = scale; a.res = residual; a.ldr = ldr; a.Y = Y; a.ldy = ldy;
-  a.n = n; a.R = R; a.T = T; a.N = N; a.K = K; a.f32 = f32 != 0; a.split = p.split; a.share = p.share;
+  a.n = n; a.R = R; a.T = T; a.N = N; a.K = K; a.f32 = f32 != 0; a.split = p.split;
   a.vec_r = ldr % 8 == 0 && r % 16 == 0;
   a.vec_y = ldy % (f32 ? 4 : 8) == 0 && y % 16 == 0;
   a.H = static_cast<float*>(workspace);
@@ -826,8 +864,9 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   const bool low = a.ranks <= 64;
   const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
   auto at_most = [](int64_t v, int64_t most) { return static_cast<unsigned>(v < 1 ? 1 : v < most ? v : most); };
-  OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, at_most(room / p.split, distinct), p.split),
-                dim3(ad::THREADS), static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
+  a.ctas = static_cast<int>(at_most(room, distinct * p.split));
+  OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, a.ctas), dim3(ad::THREADS),
+                static_cast<size_t>(ad::down_smem(a.rows, a.ranks)), stream, a);
   const int parts = f32 ? 3 : 2;
   // Few tokens an adapter: up to 16 in the mean of all adapters that a tile can have; in batches of many tiles, where an
   // adapter's tokens mostly follow one another, up to 8 (4096 tokens, N 14336, 8 adapters in runs of 512: 85 us by the
