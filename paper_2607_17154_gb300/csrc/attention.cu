@@ -129,14 +129,21 @@ __device__ __forceinline__ Place find_place(const Args& a, const Units<NT>& u, i
   p.j = static_cast<int>(rest % p.nu);
   return p;
 }
+// By a whole warp: sequences without slots are skipped 32 at a time.
 __device__ __forceinline__ void next_place(const Args& a, Place& p, int rows) {
   if (++p.j < p.nu) return;
   p.j = 0;
   if (++p.r < rows) return;
   p.r = 0;
-  for (++p.s; p.s < a.c.seqs; ++p.s) {
-    p.n = a.c.slots(p.s);
-    if (p.n > 0) break;
+  for (++p.s; p.s < a.c.seqs; p.s += 32) {
+    const int s = p.s + static_cast<int>(threadIdx.x % 32);
+    const int n = s < a.c.seqs ? a.c.slots(s) : 0;
+    const unsigned held = __ballot_sync(~0u, n > 0);
+    if (held == 0) continue;
+    const int first = __ffs(held) - 1;
+    p.n = __shfl_sync(~0u, n, first);
+    p.s += first;
+    break;
   }
   p.nu = (p.n + UNIT - 1) / UNIT;
 }
@@ -244,14 +251,15 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
   const int per = a.by_row ? 0 : count_units(a, units);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, q4 = lane % 4;
   const int rows = a.c.heads * a.chunks;
-  for (int s = blockIdx.x; s < a.c.seqs; s += gridDim.x) {  // sequences without slots, and bad lengths
-    const int n = a.c.slots(s);
-    if (threadIdx.x == 0 && n != a.c.length[s]) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, s);
-    if (n > 0) continue;
-    for (int i = threadIdx.x; i < a.Hq * VECS; i += NT)
-      reinterpret_cast<uint4*>(a.out + s * a.ldo)[i] = make_uint4(0, 0, 0, 0);
-    if (a.lse)
-      for (int i = threadIdx.x; i < a.Hq; i += NT) a.lse[static_cast<int64_t>(s) * a.Hq + i] = -INFINITY;
+  for (int s0 = (blockIdx.x * WARPS + warp) * 32; s0 < a.c.seqs; s0 += gridDim.x * NT) {  // bad lengths, and none
+    const int mine = s0 + lane, n = mine < a.c.seqs ? a.c.slots(mine) : 1;
+    if (mine < a.c.seqs && n != a.c.length[mine]) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, mine);
+    for (unsigned none = __ballot_sync(~0u, n == 0); none != 0; none &= none - 1) {
+      const int s = s0 + __ffs(none) - 1;
+      for (int i = lane; i < a.Hq * VECS; i += 32) reinterpret_cast<uint4*>(a.out + s * a.ldo)[i] = make_uint4(0, 0, 0, 0);
+      if (a.lse)
+        for (int i = lane; i < a.Hq; i += 32) a.lse[static_cast<int64_t>(s) * a.Hq + i] = -INFINITY;
+    }
   }
   // all units, or those of this CTA's row
   const long long U = a.by_row ? units_of(a, blockIdx.x / rows) : units.before[NT] * rows;

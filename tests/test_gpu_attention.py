@@ -129,6 +129,7 @@ def test_attention_at_edges(hq, H, D, page):
     ([70001], 32, 8, 128, 16), ([40000], 8, 1, 64, 64), ([1], 32, 8, 128, 16), ([5], 8, 4, 256, 16), ([20000, 3, 0], 8, 4, 256, 32),
     ([3, 9000, 0, 1, 4097, 12], 16, 1, 128, 16), ([i % 4 for i in range(1100)], 4, 2, 64, 8), ([0] * 700 + [50], 8, 8, 128, 16),
     ([100], 4, 4, 64, 16), ([17, 0, 300], 32, 8, 128, 16), ([480, 495], 33, 1, 128, 8), ([1, 129], 20, 2, 256, 16),
+    ([0] * 1000 + [70] + [0] * 40 + [1, 90] + [0] * 500, 4, 2, 64, 16), ([33 if i % 37 == 0 else 0 for i in range(3000)], 8, 4, 64, 64),
     ([0, 0, 0], 4, 4, 64, 16), ([1200 - i for i in range(40)], 32, 8, 128, 16)])
 def test_attention_of_long_and_many_sequences(lens, hq, H, D, page):
     cache = make(lens, H, D, page, seed=3)
