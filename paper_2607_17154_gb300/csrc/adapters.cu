@@ -181,140 +181,164 @@ __global__ void __launch_bounds__(THREADS, 2) adapters_down_kernel(const Args a)
     const int m16 = (rows + 15) / 16 * 16;
     const uint16_t* A = a.A + id * a.stride_a;
     const bool few = rows <= 16;
-    float acc[MAX_R / 8][4];
+    // Results of 32 bits: a sum of at most 512 of K at a time, added up in H by the thread that has it. The tensor
+    // cores cut a running sum (K 14336 in parts of 1600: 4.0e-6 off in the 2-norm, the plain form in fp32 1.3e-6).
+    const int chunk = a.f32 && few ? 512 / KB : k1 - k0;  // (many tokens: see flush)
+    float* const H = a.H + (static_cast<int64_t>(part_of) * a.T + t0) * a.R;
+    for (int kc0 = k0; kc0 < k1; kc0 += chunk) {
+      float acc[MAX_R / 8][4];
 #pragma unroll
-    for (int n = 0; n < MAX_R / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-    // `count` steps through a ring of `stages`: `fetch` fills a stage, `step` has its products.
-    auto steps = [&](auto stages, int count, int stage_bytes, auto fetch, auto step) {
-      constexpr int STAGES = decltype(stages)::value;
-      for (int i = 0; i < STAGES - 1; ++i) {
-        if (i < count) fetch(i, base + i * stage_bytes);
-        cp_commit();
-      }
-      int stage = 0, free = STAGES - 1;
-      for (int i = 0; i < count; ++i) {
-        cp_wait<STAGES - 2>();
-        __syncthreads();
-        if (i + STAGES - 1 < count) fetch(i + STAGES - 1, base + free * stage_bytes);
-        cp_commit();
-        free = free + 1 == STAGES ? 0 : free + 1;
-        step(base + stage * stage_bytes);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-      }
-    };
-    const int k_first = k0 * KB, k_end = min(k1 * KB, a.K);
-    if (few) {  // steps of 128 of K: a row is 16 vectors, a thread's rows are tid / 16 and of A every 16th from there
-      constexpr int X_BYTES = 16 * FEW_KB * 2;
-      const int v = tid % 16, row = tid / 16;
-      const uint16_t* xp = row < rows ? a.X + (t0 + s.row[w][row]) * a.ldx + k_first + v * 8 : nullptr;
-      const uint16_t* ap = A + row * a.lda + k_first + v * 8;
-      auto at = [](int r_, int v_) { return (r_ * 16 + (v_ ^ (r_ & 7))) * 16; };
-      const uint32_t place = at(row, v);
-      auto fetch = [&](int i, uint32_t stage) {
-        const int left = k_end - k_first - i * FEW_KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-        const bool on = xp && bytes > 0;
-        cp16(stage + place, on ? xp + i * FEW_KB : a.X, on ? bytes : 0);
-#pragma unroll
-        for (int e = 0; e < MAX_R / 16; ++e) {
-          if (e * 16 >= rt) break;
-          const bool ok = row + e * 16 < r && bytes > 0;
-          cp16(stage + X_BYTES + place + e * X_BYTES, ok ? ap + e * 16 * a.lda + i * FEW_KB : a.A, ok ? bytes : 0);
+      for (int n = 0; n < MAX_R / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+      // `count` steps through a ring of `stages`: `fetch` fills a stage, `step` has its products.
+      auto steps = [&](auto stages, int count, int stage_bytes, auto fetch, auto step) {
+        constexpr int STAGES = decltype(stages)::value;
+        for (int i = 0; i < STAGES - 1; ++i) {
+          if (i < count) fetch(i, base + i * stage_bytes);
+          cp_commit();
+        }
+        int stage = 0, free = STAGES - 1;
+        for (int i = 0; i < count; ++i) {
+          cp_wait<STAGES - 2>();
+          __syncthreads();
+          if (i + STAGES - 1 < count) fetch(i + STAGES - 1, base + free * stage_bytes);
+          cp_commit();
+          free = free + 1 == STAGES ? 0 : free + 1;
+          step(base + stage * stage_bytes);
+          stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
       };
-      // warps w and w + 4 have products w % 4 and w % 4 + 4 of 16 of K, of every other 16 ranks
-      auto step = [&](uint32_t xs) {
+      bool held = false;  // H has a sum of this thread's
+      auto flush = [&]() {  // more than 16 tokens: a warp's 16 of them
 #pragma unroll
-        for (int h = 0; h < FEW_KB / 64; ++h) {
-          const int k = (w & 3) + 4 * h;
-          uint32_t x[4], b[4];
-          ldm4(x, xs + at((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+        for (int h = 0; h < 2; ++h) {
+          const int row = w * 16 + g + h * 8;
+          if (row >= rows) continue;
+          float* to = H + static_cast<int64_t>(s.row[w][row]) * a.R + q4 * 2;  // (a column behind the rank is not read)
+#pragma unroll
+          for (int n = 0; n < MAX_R / 8; ++n) {
+            if (n * 8 + q4 * 2 >= r) continue;
+            float2 v = make_float2(acc[n][2 * h], acc[n][2 * h + 1]);
+            if (held) {
+              const float2 was = *reinterpret_cast<const float2*>(to + n * 8);
+              v = make_float2(was.x + v.x, was.y + v.y);
+            }
+            *reinterpret_cast<float2*>(to + n * 8) = v;
+            acc[n][2 * h] = acc[n][2 * h + 1] = 0.0f;
+          }
+        }
+        held = true;
+      };
+      const int kc1 = min(kc0 + chunk, k1), k_first = kc0 * KB, k_end = min(kc1 * KB, a.K);
+      if (few) {  // steps of 128 of K: a row is 16 vectors, a thread's rows are tid / 16 and of A every 16th from there
+        constexpr int X_BYTES = 16 * FEW_KB * 2;
+        const int v = tid % 16, row = tid / 16;
+        const uint16_t* xp = row < rows ? a.X + (t0 + s.row[w][row]) * a.ldx + k_first + v * 8 : nullptr;
+        const uint16_t* ap = A + row * a.lda + k_first + v * 8;
+        auto at = [](int r_, int v_) { return (r_ * 16 + (v_ ^ (r_ & 7))) * 16; };
+        const uint32_t place = at(row, v);
+        auto fetch = [&](int i, uint32_t stage) {
+          const int left = k_end - k_first - i * FEW_KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+          const bool on = xp && bytes > 0;
+          cp16(stage + place, on ? xp + i * FEW_KB : a.X, on ? bytes : 0);
+#pragma unroll
+          for (int e = 0; e < MAX_R / 16; ++e) {
+            if (e * 16 >= rt) break;
+            const bool ok = row + e * 16 < r && bytes > 0;
+            cp16(stage + X_BYTES + place + e * X_BYTES, ok ? ap + e * 16 * a.lda + i * FEW_KB : a.A, ok ? bytes : 0);
+          }
+        };
+        // warps w and w + 4 have products w % 4 and w % 4 + 4 of 16 of K, of every other 16 ranks
+        auto step = [&](uint32_t xs) {
+#pragma unroll
+          for (int h = 0; h < FEW_KB / 64; ++h) {
+            const int k = (w & 3) + 4 * h;
+            uint32_t x[4], b[4];
+            ldm4(x, xs + at((lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
+#pragma unroll
+            for (int n = 0; n < MAX_R / 8; n += 2) {
+              if (n * 8 >= r) break;
+              if ((n / 2 & 1) != w / 4) continue;
+              ldm4(b, xs + X_BYTES + at(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
+              mma(acc[n], x, b[0], b[1]);
+              mma(acc[n + 1], x, b[2], b[3]);
+            }
+          }
+        };
+        const int count = (k_end - k_first + FEW_KB - 1) / FEW_KB, bytes = (16 + a.ranks) * FEW_KB * 2;
+        if (a.ranks <= 64) steps(std::integral_constant<int, few_stages(64)>{}, count, bytes, fetch, step);
+        else steps(std::integral_constant<int, few_stages(MAX_R)>{}, count, bytes, fetch, step);
+      } else {
+        // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
+        const int v = tid % 8, x_bytes = a.rows * KB * 2;
+        const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + k_first + v * 8;
+#pragma unroll
+        for (int e = 0; e < TILE / 32; ++e)
+          xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[w][tid / 8 + e * 32]) * a.ldx + k_first + v * 8 : nullptr;
+        const uint32_t place = at64(tid / 8, v);
+        auto fetch = [&](int i, uint32_t stage) {
+          const uint32_t xs = stage + place, as = xs + x_bytes;
+          const int left = k_end - k_first - i * KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+#pragma unroll
+          for (int e = 0; e < TILE / 32; ++e)
+            if (tid / 8 + e * 32 < m16) {
+              const bool ok = xp[e] && bytes > 0;
+              cp16(xs + e * 32 * KB * 2, ok ? xp[e] + i * KB : a.X, ok ? bytes : 0);
+            }
+#pragma unroll
+          for (int e = 0; e < MAX_R / 32; ++e)
+            if (tid / 8 + e * 32 < rt) {
+              const bool ok = tid / 8 + e * 32 < r && bytes > 0;
+              cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + i * KB : a.A, ok ? bytes : 0);
+            }
+        };
+        int done = 0;
+        auto step = [&](uint32_t xs) {
+          if (w * 16 >= rows) return;
+          if (a.f32 && done > 0 && done % (512 / KB) == 0) flush();
+          ++done;
+          const uint32_t as = xs + x_bytes;
+          uint32_t x[KB / 16][4];
+#pragma unroll
+          for (int k = 0; k < KB / 16; ++k) ldm4(x[k], xs + at64(w * 16 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
 #pragma unroll
           for (int n = 0; n < MAX_R / 8; n += 2) {
             if (n * 8 >= r) break;
-            if ((n / 2 & 1) != w / 4) continue;
-            ldm4(b, xs + X_BYTES + at(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
-            mma(acc[n], x, b[0], b[1]);
-            mma(acc[n + 1], x, b[2], b[3]);
+#pragma unroll
+            for (int k = 0; k < KB / 16; ++k) {
+              uint32_t b[4];
+              ldm4(b, as + at64(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
+              mma(acc[n], x[k], b[0], b[1]);
+              mma(acc[n + 1], x[k], b[2], b[3]);
+            }
           }
+        };
+        steps(std::integral_constant<int, MANY_STAGES>{}, kc1 - kc0, x_bytes + a.ranks * KB * 2, fetch, step);
+      }
+      cp_wait<0>();
+      __syncthreads();
+      if (few) {  // four warps have sums of the same ranks
+        float* part = reinterpret_cast<float*>(ring);  // [4][16][LD]
+        constexpr int LD = MAX_R + 2;
+#pragma unroll
+        for (int n = 0; n < MAX_R / 8; ++n) {
+          if (n * 8 >= r || (n / 2 & 1) != w / 4) continue;
+          float* p = part + (w & 3) * 16 * LD + n * 8 + q4 * 2;
+          *reinterpret_cast<float2*>(p + g * LD) = make_float2(acc[n][0], acc[n][1]);
+          *reinterpret_cast<float2*>(p + (g + 8) * LD) = make_float2(acc[n][2], acc[n][3]);
         }
-      };
-      const int count = (k_end - k_first + FEW_KB - 1) / FEW_KB, bytes = (16 + a.ranks) * FEW_KB * 2;
-      if (a.ranks <= 64) steps(std::integral_constant<int, few_stages(64)>{}, count, bytes, fetch, step);
-      else steps(std::integral_constant<int, few_stages(MAX_R)>{}, count, bytes, fetch, step);
-    } else {
-      // a thread's rows are tid / 8 and every 32nd from there, of X and of A; its vector of a step is tid % 8
-      const int v = tid % 8, x_bytes = a.rows * KB * 2;
-      const uint16_t *xp[TILE / 32], *ap = A + (tid / 8) * a.lda + k_first + v * 8;
-#pragma unroll
-      for (int e = 0; e < TILE / 32; ++e)
-        xp[e] = tid / 8 + e * 32 < rows ? a.X + (t0 + s.row[w][tid / 8 + e * 32]) * a.ldx + k_first + v * 8 : nullptr;
-      const uint32_t place = at64(tid / 8, v);
-      auto fetch = [&](int i, uint32_t stage) {
-        const uint32_t xs = stage + place, as = xs + x_bytes;
-        const int left = k_end - k_first - i * KB - v * 8, bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-#pragma unroll
-        for (int e = 0; e < TILE / 32; ++e)
-          if (tid / 8 + e * 32 < m16) {
-            const bool ok = xp[e] && bytes > 0;
-            cp16(xs + e * 32 * KB * 2, ok ? xp[e] + i * KB : a.X, ok ? bytes : 0);
-          }
-#pragma unroll
-        for (int e = 0; e < MAX_R / 32; ++e)
-          if (tid / 8 + e * 32 < rt) {
-            const bool ok = tid / 8 + e * 32 < r && bytes > 0;
-            cp16(as + e * 32 * KB * 2, ok ? ap + e * 32 * a.lda + i * KB : a.A, ok ? bytes : 0);
-          }
-      };
-      auto step = [&](uint32_t xs) {
-        if (w * 16 >= rows) return;
-        const uint32_t as = xs + x_bytes;
-        uint32_t x[KB / 16][4];
-#pragma unroll
-        for (int k = 0; k < KB / 16; ++k) ldm4(x[k], xs + at64(w * 16 + (lane & 7) + (lane / 8 % 2) * 8, 2 * k + lane / 16));
-#pragma unroll
-        for (int n = 0; n < MAX_R / 8; n += 2) {
-          if (n * 8 >= r) break;
-#pragma unroll
-          for (int k = 0; k < KB / 16; ++k) {
-            uint32_t b[4];
-            ldm4(b, as + at64(n * 8 + (lane & 7) + lane / 16 * 8, 2 * k + lane / 8 % 2));
-            mma(acc[n], x[k], b[0], b[1]);
-            mma(acc[n + 1], x[k], b[2], b[3]);
-          }
+        __syncthreads();
+        for (int i = tid; i < rows * r; i += THREADS) {
+          const int row = i / r, c = i % r;
+          const float* p = part + row * LD + c;
+          float* h = H + static_cast<int64_t>(s.row[w][row]) * a.R + c;
+          const float sum = (p[0] + p[16 * LD]) + (p[2 * 16 * LD] + p[3 * 16 * LD]);
+          *h = kc0 == k0 ? sum : *h + sum;
         }
-      };
-      steps(std::integral_constant<int, MANY_STAGES>{}, k1 - k0, x_bytes + a.ranks * KB * 2, fetch, step);
-    }
-    cp_wait<0>();
-    __syncthreads();
-    float* H = a.H + (static_cast<int64_t>(part_of) * a.T + t0) * a.R;
-    if (few) {  // four warps have sums of the same ranks
-      float* part = reinterpret_cast<float*>(ring);  // [4][16][LD]
-      constexpr int LD = MAX_R + 2;
-#pragma unroll
-      for (int n = 0; n < MAX_R / 8; ++n) {
-        if (n * 8 >= r || (n / 2 & 1) != w / 4) continue;
-        float* p = part + (w & 3) * 16 * LD + n * 8 + q4 * 2;
-        *reinterpret_cast<float2*>(p + g * LD) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(p + (g + 8) * LD) = make_float2(acc[n][2], acc[n][3]);
+      } else {
+        flush();
       }
       __syncthreads();
-      for (int i = tid; i < rows * r; i += THREADS) {
-        const int row = i / r, c = i % r;
-        const float* p = part + row * LD + c;
-        H[static_cast<int64_t>(s.row[w][row]) * a.R + c] =
-            (p[0] + p[16 * LD]) + (p[2 * 16 * LD] + p[3 * 16 * LD]);
-      }
-    } else {
-#pragma unroll
-      for (int n = 0; n < MAX_R / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = w * 16 + g + e / 2 * 8, c = n * 8 + q4 * 2 + e % 2;
-          if (row < rows && c < r) H[static_cast<int64_t>(s.row[w][row]) * a.R + c] = acc[n][e];
-        }
     }
-    __syncthreads();
   }
 }
 

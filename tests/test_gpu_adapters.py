@@ -216,3 +216,18 @@ def test_tokens_of_one_adapter_over_slices_of_columns(rows, N):
     for dt in (BF16, torch.float32):
         check(X, A, Bw, ids, torch.empty(T, N, dtype=dt, device=DEV), residual=rnd(g, T, N))
         check(X, A, Bw, ids, torch.empty(T, N + 3, dtype=dt, device=DEV)[:, :N])
+
+
+@pytest.mark.parametrize("T", [3, 128, 1000, 4096])
+def test_results_in_32_bits_over_a_long_k(T):
+    """In the 2-norm: a sum of 512 of K is 32 products of 16. Where each is cut instead of rounded, by 2^-24 of the running
+    sum in the mean, and that grows as the root of their number, the sum is off by 2^-24 * 32 * 2 / 3 < 2^-19 of itself;
+    what follows is rounded. (One running sum over K = 14336 would be off by 28 times that.)"""
+    K, N, R, n = 14336, 128, 128, 2
+    g = gen(T)
+    X, A, Bw = rnd(g, T, K), rnd(g, n, R, K, std=0.02), rnd(g, n, N, R, std=0.1)
+    ids = (torch.arange(T, dtype=torch.int32, device=DEV) // 64 % n).int()
+    Y = torch.empty(T, N, dtype=torch.float32, device=DEV)
+    call(X, A, Bw, ids, Y)
+    y, _ = reference(X, A, Bw, ids, None, None, None, Y)
+    assert float((Y.double() - y).norm() / y.norm()) <= 2.0 ** -19

@@ -592,3 +592,31 @@ def test_layers_refuse_other_batches_and_calibration():
         DecodeAttention(z(192, 64), z(64, 128), c, 1)
     with pytest.raises(ValueError):
         PagedCache(3, 16, 1, 64, DEV, page=16, share=c)
+
+
+def test_a_captured_cut_follows_lengths_and_weights():
+    for slots, budget in ((1040, 1024), (3000, 300), (20000, 500)):  # by itself, with a second launch, long rows
+        H, D, page = 2, 64, 16
+        cache = make([min(slots, 40)] * 2, H, D, page, seed=60, width=slots // page, extra=0, weights=True, fill=0.5)
+        k, v, table, length, mass, pos = cache._keep
+        out, newest = torch.zeros_like(length), torch.zeros_like(length)
+        ws = torch.empty(B.ordermoe_cache_evict_workspace_bytes(cache, budget), dtype=torch.uint8, device=DEV)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            B.ordermoe_cache_evict(cache, budget, out, ws, newest=newest, recent=9, sinks=1)
+            s.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                B.ordermoe_cache_evict(cache, budget, out, ws, newest=newest, recent=9, sinks=1)
+        torch.cuda.synchronize()
+        for i, lens in enumerate(([slots, 7], [budget + 1, budget], [slots - 5, slots])):
+            length.copy_(torch.tensor(lens))
+            newest.copy_(length - 1)
+            mass.copy_(torch.rand(mass.shape, device=DEV, generator=gen(61 + i)))
+            k.copy_(torch.randn(k.shape, device=DEV, generator=gen(71 + i)).to(BF16))
+            want = evicted(cache, budget, 9, 1, newest.cpu())
+            g.replay()
+            for got, w in zip((k, v, mass, pos, out), want):
+                assert torch.equal(got.cpu(), w)
+            pos.copy_(torch.arange(cache.slots, dtype=torch.int32, device=DEV).expand_as(pos))
