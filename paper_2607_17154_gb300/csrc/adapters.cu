@@ -6,8 +6,8 @@
 // that have them, so an adapter's weights are read once a tile whatever the order (and from L2 by the later tiles). Both products run on
 // mma.sync: the tokens of an adapter are its M side, 1 to 128 of them, in blocks of 16.
 // Measured (both kernels, launched from the host): 1 token, K = N = 4096, R 16: 6.1 us; 128 tokens on 32 adapters, K 4096, N
-// 6144, R 64: 16.0 us, floor 3.7; 4096 tokens on 8 adapters, K 4096, N 14336, R 64: 79 us = 3.6 TB/s, floor 42.6
-// (the first kernel 16, the second 62: four products of 16 tokens x 32 columns a residual vector, 1.5 instructions a cycle
+// 6144, R 64: 16.0 us, floor 3.7; 4096 tokens on 8 adapters, K 4096, N 14336, R 64: 77 us = 3.7 TB/s, floor 42.6
+// (the first kernel 15, the second 62: four products of 16 tokens x 32 columns a residual vector, 1.5 instructions a cycle
 // and SM; its tensor pipe is busy for 25 us).
 #include <type_traits>
 

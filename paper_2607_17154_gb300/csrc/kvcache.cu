@@ -78,10 +78,10 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
 //   (a, b) -> (a cos - b sin, a sin + b cos),
 // it writes R q, R k and v as they are. The angle is taken in turns in 64 bits and reduced to half a turn
 // before it becomes 32 bits: far positions lose nothing. A thread holds 16 values of a head, the eight pairs
-// of two vectors of 16 bytes (adjacent pairs: the two next to each other; else half a rotation apart). It is
-// bound by bytes, or with few tokens by the chain sequence - length - page - store: a token's rows are read
-// before that chain, which does not say where they are. (4094 tokens of 5 sequences, 32 / 8 heads of 128: 23.5 us = 4.3
-// TB/s, 0.64 of the measured rate, floor 15: chains of 3 us, ten CTAs an SM, 2.7 waves of them; read behind the chain 40.
+// of two vectors of 16 bytes half a rotation apart (next to each other a load would touch half of each sector: 24 us
+// for 21). It is bound by bytes, or with few tokens by the chain sequence - length - page - store: a token's rows are read
+// before that chain, which does not say where they are. (4094 tokens of 5 sequences, 32 / 8 heads of 128: 20.8 us = 4.9
+// TB/s, 0.72 of the measured rate, floor 15: chains of 3 us, ten CTAs an SM, 2.7 waves of them; read behind the chain 40.
 // One token 3.1 us.)
 constexpr int APPEND_AHEAD = 3;      // items of a thread that are read first
 constexpr int APPEND_SCAN = 1024;    // sequences whose starts the threads compare all at once
@@ -95,10 +95,10 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
   const int nq = a.q ? a.Hq : 0, items = (nq + 2 * H) << log_pairs;
   auto vectors = [&](int i, int& x, int& y) {  // of item i, in its head; true: to be turned
     const int head = i >> log_pairs, p = i & ((1 << log_pairs) - 1);
-    const bool in = p < a.rot / 16;
-    x = ADJACENT || !in ? p * 16 : p * 8;
-    y = ADJACENT || !in ? x + 8 : x + half;
-    return in && head < nq + H;
+    const bool in = a.rot == 0 || p < a.rot / 16;
+    x = in ? p * 8 : p * 16;
+    y = in ? x + (a.rot == 0 ? D / 2 : half) : x + 8;
+    return in && a.rot > 0 && head < nq + H;
   };
   auto source = [&](int i) {
     const int head = i >> log_pairs;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     for (int h = tid; h < H; h += APPEND_THREADS) a.c.mass[a.c.side(s, h, slot)] = 0.0f;
   __syncthreads();
   auto finish = [&](int i, const uint4& u, const uint4& w) {
-    const int head = i >> log_pairs, f = (i & ((1 << log_pairs) - 1)) * 9;
+    const int head = i >> log_pairs, p = i & ((1 << log_pairs) - 1);
     int x, y;
     const bool turn = vectors(i, x, y);
     uint16_t* dst = head < nq ? a.q_out + t * a.ldqo + static_cast<int64_t>(head) * D
@@ -183,7 +183,9 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
     unpack8(w, m + 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float2 c = turn_of[f + j];
+      // pair j: (j, j + 8) of the two vectors, or neighbours in one of them
+      const int f = ADJACENT ? p * 4 + j % 4 + j / 4 * (half / 2) : p * 8 + j;
+      const float2 c = turn_of[f + f / 8];
       float &e = ADJACENT ? m[2 * j] : m[j], &o = ADJACENT ? m[2 * j + 1] : m[8 + j];
       const float turned = e * c.x - o * c.y;
       o = e * c.y + o * c.x;
