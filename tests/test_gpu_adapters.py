@@ -231,3 +231,35 @@ def test_results_in_32_bits_over_a_long_k(T):
     call(X, A, Bw, ids, Y)
     y, _ = reference(X, A, Bw, ids, None, None, None, Y)
     assert float((Y.double() - y).norm() / y.norm()) <= 2.0 ** -19
+
+
+def test_inputs_written_by_the_kernels_before():
+    """Ids, weights, ranks, the residual (a product's result) and X change right before each call, nothing waits in between:
+    the same bits as with a wait after every step."""
+    T, K, N, R, n = 150, 512, 1024, 32, 6
+    g = gen(14)
+    W = rnd(g, N, K, std=0.02)
+    X, A, Bw = rnd(g, T, K), rnd(g, n, R, K, std=0.05), rnd(g, n, N, R, std=0.1)
+    ids, rank = torch.zeros(T, dtype=torch.int32, device=DEV), torch.full((n,), R, dtype=torch.int32, device=DEV)
+    Y = torch.empty(T, N, dtype=BF16, device=DEV)
+    ws = torch.empty(B.ordermoe_adapters_workspace_bytes(T, K, N, R), dtype=torch.uint8, device=DEV)
+    sets = [(rnd(g, T, K), rnd(g, n, N, R, std=0.1), torch.randint(-1, n, (T,), dtype=torch.int32, device=DEV, generator=g),
+             torch.randint(0, R + 1, (n,), dtype=torch.int32, device=DEV, generator=g)) for _ in range(24)]
+
+    def steps(wait):
+        out = []
+        for x, b, i, r in sets:
+            for to, what in ((X, x), (Bw, b), (ids, i), (rank, r)):
+                to.copy_(what)
+                wait()
+            B.ordermoe_linear(X, W, Y)
+            wait()
+            B.ordermoe_adapters(X, A, Bw, ids, Y, ws, rank=rank, residual=Y)
+            wait()
+            out.append(Y.clone())
+        return out
+
+    want = steps(torch.cuda.synchronize)
+    for _ in range(4):
+        for a, b in zip(steps(lambda: None), want):
+            assert torch.equal(a, b)

@@ -620,3 +620,39 @@ def test_a_captured_cut_follows_lengths_and_weights():
             for got, w in zip((k, v, mass, pos, out), want):
                 assert torch.equal(got.cpu(), w)
             pos.copy_(torch.arange(cache.slots, dtype=torch.int32, device=DEV).expand_as(pos))
+
+
+def test_lengths_and_queries_written_by_the_kernels_before():
+    """Lengths, queries and the cache change right before each call, nothing waits in between: the same bits as with a wait
+    after every step."""
+    hq, H, D = 16, 4, 128
+    cache = make([2000, 2000, 2000], H, D, 16, seed=80, weights=True, fill=0.5)
+    k, v, table, length, mass, pos = cache._keep
+    ws = workspace(cache, hq, True)
+    q = torch.zeros(3, hq * D, dtype=BF16, device=DEV)
+    out = torch.zeros_like(q)
+    g = gen(81)
+    sets = [(torch.randint(0, 2001, (3,), dtype=torch.int32, device=DEV, generator=g), torch.randn(q.shape, device=DEV, generator=g).to(BF16),
+             torch.randn(3, 2 * H * D, device=DEV, generator=g).to(BF16)) for _ in range(24)]
+
+    def steps(wait):
+        k0, v0, res = k.clone(), v.clone(), []
+        mass.zero_()
+        for n, x, kv in sets:
+            length.copy_(n)
+            wait()
+            q.copy_(x)
+            wait()
+            B.ordermoe_cache_append(cache, kv[:, :H * D], kv[:, H * D:])
+            wait()
+            B.ordermoe_attention_paged(cache, q, out, ws, weights=True)
+            wait()
+            res += [out.clone(), mass.clone()]
+        k.copy_(k0)
+        v.copy_(v0)
+        return res
+
+    want = steps(torch.cuda.synchronize)
+    for _ in range(4):
+        for a, b in zip(steps(lambda: None), want):
+            assert torch.equal(a, b)
