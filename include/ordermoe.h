@@ -346,7 +346,7 @@ int ordermoe_cache_append(const ordermoe_cache* cache, const uint16_t* k, int64_
  *            prepared; calls that may overlap on the GPU need one each
  * Statistics and sums in fp32, p in two bf16 parts (16 bits), one rounding to out. A sequence with no slot, or whose
  * every x is -inf, gets out = 0 and lse = -inf. Slots at and behind the length are not read into a result, whatever they
- * hold. The work is cut evenly over the GPU by the lengths on the device: the same lengths and table
+ * hold; an infinite value of v in use makes infinities or NaN of out. The work is cut evenly over the GPU by the lengths on the device: the same lengths and table
  * sizes give the same bits, and a captured call follows lengths that change between replays. */
 size_t ordermoe_attention_paged_workspace_bytes(int seqs, int q_heads, int heads, int dim,
                                                 int64_t seq_slots, int weights);
@@ -389,7 +389,8 @@ int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int sinks, int
  *            stride)
  *   workspace  device scratch of ordermoe_adapters_workspace_bytes(T, K, N, R) bytes, 256-byte aligned; calls that
  *            may overlap on the GPU need one each
- * A X in fp32, handed on in two bf16 parts (16 bits), fp32 sums in a fixed order, one rounding to Y. T and N up to
+ * A X in fp32, handed on in two bf16 parts (16 bits; three for a float Y), fp32 sums in a fixed order, one rounding to
+ * Y. Infinities in what a token uses make infinities or NaN of its row, and of no other. T and N up to
  * 2^31 - 513, K up to 2^30, n up to 2^31 - 1. An id outside [-1, n) or a rank outside [0, R] sets ORDERMOE_DEV_BAD_INDEX
  * (detail: the token; the adapter): the token is taken to have none, the rank to be the nearest. */
 size_t ordermoe_adapters_workspace_bytes(int T, int K, int N, int R);

@@ -9,7 +9,7 @@
 // Measured (launched from the host, 32 / 8 heads of 128): one sequence of 131071 slots 88 us = 6.1 TB/s, 0.91 of the measured
 // rate; 128 sequences of 1 to 8191 slots 334 us = 6.4 TB/s, 0.95; with a partial result a warp and one join for all of them
 // 143 and 386. 17 sequences of up to 4097 slots, 16 heads of 128, weights kept: 65 us, floor 43 (attention 50, the two
-// kernels behind it and their starts 15). Pages of 8 slots look a page up for every row: 54 us where pages of 128 take 45.
+// kernels behind it and their starts 15). Pages of fewer than 8 slots look a page up for every row.
 #include "kvcache.cuh"
 
 namespace om {
@@ -175,13 +175,13 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 // Loads a unit's keys and values, rows of D with their 16-byte vectors exchanged by the row's lowest three
 // bits (no bank is met twice by a matrix load). Rows behind the length, and pages that do not exist, are zeros.
 template <int D>
-__device__ __forceinline__ void load_unit(const Args& a, const Place& p, int32_t page, uint32_t stage) {
+__device__ __forceinline__ void load_unit(const Args& a, const Place& p, const int32_t (&page)[2], uint32_t stage) {
   constexpr int VECS = D / 8, HALF = Shape<D>::HALF, N = UNIT * VECS / 32;
   const int lane = threadIdx.x % 32, head = p.r / a.chunks, base = p.j * UNIT, left = p.n - base;
   if (a.c.page_log >= 4) {  // a unit lies in one page, row after row
-    const bool good = a.c.good(page);
+    const bool good = a.c.good(page[0]);
     if (!good && lane == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
-    const int64_t at = good ? a.c.row(page, head, base) * D + lane * 8 : 0;
+    const int64_t at = good ? a.c.row(page[0], head, base) * D + lane * 8 : 0;
     const int end = good ? left : 0;
     const uint16_t *k = a.c.k + at, *v = a.c.v + at;
 #pragma unroll
@@ -191,6 +191,26 @@ __device__ __forceinline__ void load_unit(const Args& a, const Place& p, int32_t
       const bool ok = row < end;
       cp16(dst, ok ? k + i * 256 : a.c.k, ok ? 16 : 0);
       cp16(dst + HALF, ok ? v + i * 256 : a.c.v, ok ? 16 : 0);
+    }
+    return;
+  }
+  if (a.c.page_log == 3) {  // in two
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int slot = base + 8 * h;
+      const bool in = slot < p.n, good = in && a.c.good(page[h]);
+      if (in && !good && lane == 0) report(&g_err_attention, ORDERMOE_DEV_BAD_INDEX, p.s);
+      const int64_t at = good ? a.c.row(page[h], head, slot) * D + lane * 8 : 0;
+      const int end = good ? left - 8 * h : 0;
+      const uint16_t *k = a.c.k + at, *v = a.c.v + at;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const int x = i * 32 + lane, row = x / VECS, vec = x % VECS;
+        const uint32_t dst = stage + ((row + 8 * h) * VECS + (vec ^ (row & 7))) * 16;
+        const bool ok = row < end;
+        cp16(dst, ok ? k + i * 256 : a.c.k, ok ? 16 : 0);
+        cp16(dst + HALF, ok ? v + i * 256 : a.c.v, ok ? 16 : 0);
+      }
     }
     return;
   }
@@ -269,7 +289,12 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
   const int count = w < W ? static_cast<int>(first_unit(U, w + 1, W) - u0) : 0;
   if (lane < 2) cut_s[warp][lane] = -1;
   Place p{};
-  int32_t page = 0;
+  int32_t page[2] = {0, 0};  // of the two halves of the unit that is loaded next
+  auto find_pages = [&](const Place& at) {
+    const int slot = at.j * UNIT;
+    page[0] = a.c.page_of(at.s, slot);
+    if (a.c.page_log == 3 && slot + 8 < at.n) page[1] = a.c.page_of(at.s, slot + 8);
+  };
   if (count > 0) {
     if (a.by_row) {
       p.s = blockIdx.x / rows;
@@ -280,10 +305,10 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
     } else {
       p = find_place(a, units, per, u0, rows);
     }
-    page = a.c.page_of(p.s, p.j * UNIT);
+    find_pages(p);
   }
   const uint32_t mine = smem_u32(ring) + warp * STAGES * 2 * HALF;
-  Place f = p;  // what is loaded next, its page and stage
+  Place f = p;  // what is loaded next, and its stage
   int fetched = 0, fstage = 0;
   auto fetch = [&]() {
     if (fetched < count) {
@@ -291,7 +316,7 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
       fstage = fstage + 1 == STAGES ? 0 : fstage + 1;
       if (++fetched < count) {
         next_place(a, f, rows);
-        page = a.c.page_of(f.s, f.j * UNIT);
+        find_pages(f);
       }
     }
     cp_commit();
