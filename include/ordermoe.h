@@ -364,7 +364,8 @@ int ordermoe_attention_paged(const ordermoe_cache* cache, const uint16_t* q, int
  *   length_out [seqs] i32 = min(length, budget); not the cache's own length, which other layers' calls may still
  *            need as it is
  *   workspace  device scratch of ordermoe_cache_evict_workspace_bytes(seqs, heads, budget) bytes, 256-byte
- *            aligned; calls that may overlap on the GPU need one each
+ *            aligned (for budgets above seq_pages * page that of seq_pages * page is enough: one of that size serves every
+ *            budget); calls that may overlap on the GPU need one each
  * Needs mass. Rows whose page does not exist are reported and not moved. */
 size_t ordermoe_cache_evict_workspace_bytes(int seqs, int heads, int budget);
 int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int sinks, int recent,

@@ -698,8 +698,10 @@ extern "C" int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int
     return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: length_out may not be the cache's length");
   if (reinterpret_cast<uintptr_t>(newest) % 4 || reinterpret_cast<uintptr_t>(length_out) % 4)
     return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: newest or length_out is not aligned to its type");
+  const int64_t cap = static_cast<int64_t>(cache->seq_pages) * cache->page;  // with a budget of as many nothing moves
+  const int listed = static_cast<int>(budget < cap ? budget : cap);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 ||
-      workspace_bytes < ordermoe_cache_evict_workspace_bytes(cache->seqs, cache->heads, budget))
+      workspace_bytes < ordermoe_cache_evict_workspace_bytes(cache->seqs, cache->heads, listed))
     return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: workspace is null, too small or not 256-byte aligned");
   static PerDevice attr_;
   const int e = per_device(attr_, evict_attr);

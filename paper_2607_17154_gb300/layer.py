@@ -197,7 +197,8 @@ class PagedCache:
     """The paged cache of one layer for `seqs` sequences of up to max_slots slots each, with pages of its own
     (PagedCache.cache is the descriptor of the calls). share: another layer's PagedCache whose table, lengths and
     positions this one uses: the layers of a stack take one step together. weights: also keep what each slot was
-    attended and its position, which cut() needs. Tables, lengths and pages may be written by the caller too."""
+    attended and its position, which cut() needs (16 bytes a slot and head with cut()'s scratch, which is made here for
+    every budget). Tables, lengths and pages may be written by the caller too."""
 
     def __init__(self, seqs, max_slots, heads, dim, device, page=64, share=None, weights=False):
         n = -(-max_slots // page)
@@ -213,7 +214,10 @@ class PagedCache:
         self.mass = new(seqs, heads, n * page, dtype=torch.float32) if weights else None
         self.pos = new(seqs, heads, n * page) if weights else None
         self.cache = B.make_cache(self.k, self.v, self.table, self.length, self.mass, self.pos)
-        self._cut = None
+        # cut()'s, at the same place for as long as the cache is there: captured cuts go on writing to them
+        self._cut_length = new(seqs)
+        self._cut_ws = torch.empty(B.ordermoe_cache_evict_workspace_bytes(self.cache, self.cache.slots) if weights else 0,
+                                   dtype=torch.uint8, device=device)
         _settle(device)
 
     def advance(self, n=1):
@@ -224,15 +228,11 @@ class PagedCache:
 
     def cut(self, budget, recent=0, sinks=0, stream=None):
         """ordermoe_cache_evict of this layer. Returns the new lengths (a buffer that the next cut overwrites):
-        after the last layer that shares them, copy them into length."""
-        if self._cut is None or self._cut[0] != budget:
-            self._cut = (budget, torch.empty_like(self.length),
-                         torch.empty(B.ordermoe_cache_evict_workspace_bytes(self.cache, budget), dtype=torch.uint8,
-                                     device=self.length.device))
-        _, out, ws = self._cut
-        B.ordermoe_cache_evict(self.cache, budget, out, ws, newest=self.position, recent=recent, sinks=sinks,
-                               stream=stream)
-        return out
+        after the last layer that shares them, copy them into length. Cuts of a cache, captured ones among them,
+        share that buffer and their scratch: they may not overlap on the GPU."""
+        B.ordermoe_cache_evict(self.cache, budget, self._cut_length, self._cut_ws, newest=self.position, recent=recent,
+                               sinks=sinks, stream=stream)
+        return self._cut_length
 
 
 class DecodeAttention:

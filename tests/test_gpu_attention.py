@@ -656,3 +656,74 @@ def test_lengths_and_queries_written_by_the_kernels_before():
     for _ in range(4):
         for a, b in zip(steps(lambda: None), want):
             assert torch.equal(a, b)
+
+
+def filled(seqs, slots, H=2, D=64, seed=120):
+    """A PagedCache whose sequences are full, weights and values random."""
+    from paper_2607_17154_gb300.layer import PagedCache
+    c = PagedCache(seqs, slots, H, D, DEV, page=16, weights=True)
+    fill(c, seed)
+    return c
+
+
+def fill(c, seed):
+    g = gen(seed)
+    for t in (c.k, c.v, c.mass):
+        t.copy_(torch.rand(t.shape, device=DEV, generator=g))
+    c.pos.copy_(torch.arange(c.cache.slots, dtype=torch.int32, device=DEV).expand_as(c.pos))
+    c.length.fill_(c.cache.slots)
+    c.position.fill_(c.cache.slots - 1)
+
+
+def same_cache(c, out, want):
+    return all(torch.equal(a.cpu(), b) for a, b in zip((c.k, c.v, c.mass, c.pos, out), want))
+
+
+def test_cuts_of_other_budgets_leave_a_captured_one_its_memory():
+    """A captured cut is replayed after cuts with other budgets, when what those could have given back to the allocator is
+    in use by others."""
+    c = filled(3, 208)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        first = c.cut(64, recent=4, sinks=2)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            assert c.cut(64, recent=4, sinks=2).data_ptr() == first.data_ptr()
+    torch.cuda.synchronize()
+    for budget in (32, 150, 208, 10 ** 6):  # the last two cut nothing
+        fill(c, budget)
+        want = evicted(c.cache, budget, 4, 2, c.position.cpu())
+        assert same_cache(c, c.cut(budget, recent=4, sinks=2), want)
+    del first
+    others = [torch.full((n,), 7, dtype=torch.uint8, device=DEV) for n in [512] * 64 + [4096] * 64 + [65536] * 16]
+    fill(c, 121)
+    want = evicted(c.cache, 64, 4, 2, c.position.cpu())
+    graph.replay()
+    assert same_cache(c, c.cut(208), want[:4] + (c.length.cpu(),))  # (nothing more to cut)
+    assert all(bool((o == 7).all()) for o in others)
+
+
+def test_cut_on_another_stream():
+    """The buffers of a cut that runs behind pending work on a stream of its own are nobody else's."""
+    c, s = filled(3, 208), torch.cuda.Stream()
+    want = evicted(c.cache, 50, 0, 0, c.position.cpu())
+    busy = torch.zeros(1 << 26, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy += 1  # pending on the current stream, with temporary memory that it gives back
+        (busy[:4096] * 2).sum()
+    with torch.cuda.stream(s):
+        for _ in range(20):
+            busy.square()
+    out = c.cut(50, stream=s)
+    s.synchronize()
+    assert same_cache(c, out, want)
+    torch.cuda.synchronize()
+
+
+def test_a_cache_without_weights_is_not_cut():
+    from paper_2607_17154_gb300.layer import PagedCache
+    with pytest.raises(B.OrderMoEError, match="mass"):
+        PagedCache(2, 32, 1, 64, DEV, page=16).cut(8)

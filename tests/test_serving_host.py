@@ -145,3 +145,12 @@ def test_the_binding_refuses_other_tensors():
         B.make_cache(k, k[:2], table, length)
     with pytest.raises(TypeError):
         B.make_cache(k.float(), k.float(), table, length)
+
+
+def test_a_budget_above_the_slots_asks_for_the_slots_workspace():
+    c = cache()
+    slots = c.seq_pages * c.page
+    need = B.lib().ordermoe_cache_evict_workspace_bytes(c.seqs, c.heads, slots)
+    for budget in (slots, slots + 1, 1 << 30):
+        rc, msg = evict(c, budget=budget, nbytes=need - 1)
+        assert rc == ARG and "workspace" in msg
