@@ -1,5 +1,7 @@
 """One OrderMoE MoE layer on the GPU: device buffers from torch, every step
 through the C ABI (route_select -> dispatch -> expert_ffn -> combine)."""
+import contextlib
+
 import torch
 
 from . import binding as B
@@ -386,7 +388,9 @@ class LayerStack:
         """Records one step (every layer's kernels, after the optional prologue,
         e.g. resetting loc and qhat) as a CUDA graph over these buffers, so a
         step is one graph launch. Returns the torch.cuda.CUDAGraph; replay()
-        runs the step on the buffers' current contents."""
+        runs the step on the buffers' current contents. The prologue and the step run once
+        before that, with the caches of the stack's DecodeAttention layers taken as empty: what these
+        hold, their lengths and positions are afterwards as they were."""
         return self._capture(lambda s: self.step(X_layers, home, loc, qhat, y_layers, counters,
                                                  stream=s), prologue)
 
@@ -396,13 +400,35 @@ class LayerStack:
         return self._capture(lambda s: self.step_residual(hs, xs, home, loc, qhat, counters,
                                                           eps=eps, stream=s), prologue)
 
+    @contextlib.contextmanager
+    def _empty_caches(self):
+        """The attention layers' caches without slots, on the current stream: nothing is cut, a step's tokens are left
+        out, no slot is written or weighed. Yields a call that empties them again, behind one that
+        advanced them; lengths and positions come back at the end."""
+        caches = [desc.cache for desc in self.descs if isinstance(desc, DecodeAttention)]
+        lengths = list({id(c.length): c.length for c in caches}.values())  # layers share them
+        kept = [(t, t.clone()) for t in lengths + list({id(c.position): c.position for c in caches}.values())]
+
+        def empty():
+            for t in lengths:
+                t.zero_()
+
+        empty()
+        try:
+            yield empty
+        finally:
+            for t, value in kept:
+                t.copy_(value)
+
     def _capture(self, body, prologue):
         s = torch.cuda.Stream(device=self.scratch.device)
         s.wait_stream(torch.cuda.current_stream(self.scratch.device))
         with torch.cuda.stream(s):  # one eager step first: per-device set-up outside the capture
-            if prologue is not None:
-                prologue()
-            body(s)
+            with self._empty_caches() as empty:
+                if prologue is not None:
+                    prologue()
+                empty()
+                body(s)
         torch.cuda.current_stream(self.scratch.device).wait_stream(s)
         torch.cuda.synchronize(self.scratch.device)
         g = torch.cuda.CUDAGraph()

@@ -727,3 +727,90 @@ def test_a_cache_without_weights_is_not_cut():
     from paper_2607_17154_gb300.layer import PagedCache
     with pytest.raises(B.OrderMoEError, match="mass"):
         PagedCache(2, 32, 1, 64, DEV, page=16).cut(8)
+
+
+def attention_stack(S, slots, seed):
+    """Two layers of attention that share lengths (the second keeps weights) and a dense one."""
+    from paper_2607_17154_gb300.layer import DecodeAttention, DenseFFN, LayerStack, PagedCache
+    d, hq, H, D, g = 256, 4, 2, 64, gen(seed)
+    rnd = lambda *s: (torch.randn(*s, device=DEV, generator=g) * 0.05).to(BF16)
+    freq = 10000.0 ** (-torch.arange(D // 2, dtype=torch.float64, device=DEV) * 2 / D)
+    first = PagedCache(S, slots, H, D, DEV, page=16)
+    second = PagedCache(S, slots, H, D, DEV, page=16, share=first, weights=True)
+    layers = [DecodeAttention(rnd((hq + 2 * H) * D, d), rnd(d, hq * D), c, hq, inv_freq=freq, weights=c is second)
+              for c in (first, second)]
+    layers.append(DenseFFN(rnd(512, d), rnd(d, 512), S))
+    hs, xs = ([torch.zeros(S, d, dtype=BF16, device=DEV) for _ in range(4)] for _ in range(2))
+    return (first, second), LayerStack(layers, [], 1, S, DEV), hs, xs
+
+
+def state(caches):
+    return [t.clone() for c in caches for t in (c.k, c.v, c.mass, c.pos, c.length, c.position) if t is not None]
+
+
+@pytest.mark.parametrize("inside", [True, False])
+def test_a_capture_leaves_the_caches_as_they_are(inside):
+    """Requests are held while the step is captured, one of them with a full cache and one idle: what the caches hold
+    stays, and the graph then goes on where the eager steps ended. The step's advance is captured, or called before each
+    replay."""
+    S, slots, steps = 4, 16, 5
+    tokens = [torch.randn(S, 256, device=DEV, generator=gen(110 + i)).to(BF16) for i in range(2 * steps)]
+    home = torch.zeros(S, dtype=torch.uint8, device=DEV)
+    results = []
+    for captured in (False, True):
+        caches, stack, hs, xs = attention_stack(S, slots, 100)
+        c, got = caches[0], []
+
+        def run(step, x):
+            hs[0].copy_(x)
+            step()
+            got.append(hs[3].clone())
+
+        def eager():
+            c.advance()
+            stack.step_residual(hs, xs, home, None, None)
+
+        for x in tokens[:steps]:
+            run(eager, x)
+        step = eager
+        if captured:
+            length, position = c.length.clone(), c.position.clone()
+            c.length[1], c.length[2] = slots, 0  # a full one and an idle one, for the capture alone
+            before = state(caches)
+            graph = stack.capture_residual(hs, xs, home, None, None, prologue=c.advance if inside else None)
+            for a, b in zip(state(caches), before):
+                assert torch.equal(a, b)
+            c.length.copy_(length)
+            c.position.copy_(position)
+            step = graph.replay if inside else lambda: (c.advance(), graph.replay())
+        for x in tokens[steps:]:
+            run(step, x)
+        results.append(got + state(caches))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert c.length.tolist() == [2 * steps] * S and c.position.tolist() == [2 * steps - 1] * S
+
+
+def test_a_capture_whose_prologue_cuts():
+    """A prologue that cuts the cache before it advances: nothing is cut while the step is captured."""
+    S, slots, budget = 3, 16, 8
+    caches, stack, hs, xs = attention_stack(S, slots, 101)
+    first, second = caches
+    home = torch.zeros(S, dtype=torch.uint8, device=DEV)
+
+    def prologue():
+        first.length.copy_(second.cut(budget, recent=2, sinks=1))
+        first.advance()
+
+    for i in range(12):
+        hs[0].copy_(torch.randn(S, 256, device=DEV, generator=gen(130 + i)).to(BF16))
+        first.advance()
+        stack.step_residual(hs, xs, home, None, None)
+    before = state(caches)
+    graph = stack.capture_residual(hs, xs, home, None, None, prologue=prologue)
+    for a, b in zip(state(caches), before):
+        assert torch.equal(a, b)
+    want = evicted(second.cache, budget, 2, 1, second.position.cpu())
+    graph.replay()
+    assert first.length.tolist() == [budget + 1] * S
+    assert torch.equal(second.pos[:, :, :budget].cpu(), want[3][:, :, :budget])
