@@ -345,8 +345,9 @@ int ordermoe_cache_append(const ordermoe_cache* cache, const uint16_t* k, int64_
  *   workspace  device scratch of ordermoe_attention_paged_workspace_bytes(...) bytes, 256-byte aligned, not to be
  *            prepared; calls that may overlap on the GPU need one each
  * Statistics and sums in fp32, p in two bf16 parts (16 bits), one rounding to out. A sequence with no slot, or whose
- * every x is -inf, gets out = 0 and lse = -inf. Slots at and behind the length are not read into a result, whatever they
- * hold; an infinite value of v in use makes infinities or NaN of out. The work is cut evenly over the GPU by the lengths on the device: the same lengths and table
+ * every x is -inf, gets out = 0 and lse = -inf, whatever its v hold. Slots at and behind the length are not read into a
+ * result, whatever they hold; beside a finite x, infinities and NaN of v at any slot (its x -inf or not) make infinities
+ * or NaN of out. The work is cut evenly over the GPU by the lengths on the device: the same lengths and table
  * sizes give the same bits, and a captured call follows lengths that change between replays. */
 size_t ordermoe_attention_paged_workspace_bytes(int seqs, int q_heads, int heads, int dim,
                                                 int64_t seq_slots, int weights);

@@ -241,6 +241,10 @@ __device__ __forceinline__ uint16_t* out_of(const Args& a, const Row& x, int y, 
   return a.out + x.s * a.ldo + (static_cast<int64_t>(x.head) * a.G + x.first + y) * D;
 }
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.0f ? 0.0f : 1.0f / sum; }
+// Two outputs. Where nothing is attended they are 0, whatever the sums of p v became (0 times an infinity).
+__device__ __forceinline__ uint32_t output2(float x, float y, float inv) {
+  return inv == 0.0f ? 0u : pack_bf16x2(x * inv, y * inv);
+}
 // lse, and what the weights are computed from, of head y.
 template <int GP, bool WEIGHTS>
 __device__ __forceinline__ void put_sums(const Args& a, const Row& x, int y, float m, float sum, float inv, int rows) {
@@ -472,7 +476,7 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
 #pragma unroll
           for (int n = 0; n < VECS; ++n) {
             const float2 v = pair(n, i);
-            *reinterpret_cast<uint32_t*>(out + n * 8) = pack_bf16x2(v.x * inv, v.y * inv);
+            *reinterpret_cast<uint32_t*>(out + n * 8) = output2(v.x, v.y, inv);
           }
         }
       } else {
@@ -522,7 +526,7 @@ __global__ void __launch_bounds__(Shape<D>::WARPS * 32, 1) attend_kernel(const A
         const float inv = inverse(sum);
         if (d == 0) put_sums<GP, WEIGHTS>(a, x, y, top, sum, inv, rows);
         *reinterpret_cast<uint2*>(out_of(a, x, y, D) + d) =
-            make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+            make_uint2(output2(v.x, v.y, inv), output2(v.z, v.w, inv));
       } else {
         if (d == 0) {
           part[y] = top;
@@ -589,7 +593,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const Args a)
   const float inv = inverse(sum);
   if (tid == 0) put_sums<GP, WEIGHTS>(a, x, y, top, sum, inv, rows);
   *reinterpret_cast<uint2*>(out_of(a, x, y, D) + col * 4) =
-      make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+      make_uint2(output2(v.x, v.y, inv), output2(v.z, v.w, inv));
 }
 
 // mass[s][h][i] += the sum of p_i over the query heads of head h, from the scores that were kept.

@@ -814,3 +814,25 @@ def test_a_capture_whose_prologue_cuts():
     graph.replay()
     assert first.length.tolist() == [budget + 1] * S
     assert torch.equal(second.pos[:, :, :budget].cpu(), want[3][:, :, :budget])
+
+
+def held(cache, x):
+    """Places of sequence s's first x[s] slots: pages and rows in them."""
+    table = cache._keep[2].long()
+    return [(table[s][(i := torch.arange(n, device=DEV)) // cache.page], i % cache.page) for s, n in enumerate(x)]
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("lens,H", [([40, 0, 500], 2), ([5000], 1), ([16] * 2000 + [9000], 1)])
+def test_values_behind_scores_of_minus_infinity_alone_say_nothing(lens, H, bad):
+    """Every score of a sequence is -inf: 0 and -inf, whatever its values hold. Rows that a warp, a CTA's warps and CTAs share."""
+    cache = make(lens, H, 64, 16, seed=92, weights=True)
+    k, v = cache._keep[:2]
+    for at, row in held(cache, lens):
+        k[at, :, row] = -math.inf
+        v[at, :, row] = bad
+    q = torch.ones(len(lens), 2 * H * 64, dtype=BF16, device=DEV)
+    before = cache._keep[4].clone()
+    out, lse = attend(cache, q, 2 * H, weights=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    assert torch.equal(cache._keep[4], before)
