@@ -363,7 +363,7 @@ int ordermoe_attention_paged(const ordermoe_cache* cache, const uint16_t* q, int
  *   newest   [seqs] i32: position of each sequence's newest token; nullable when recent = 0 or the cache has
  *            no pos (the newest is then its last slot)
  *   length_out [seqs] i32 = min(length, budget); not the cache's own length, which other layers' calls may still
- *            need as it is
+ *            need as it is, nor newest, and no part of them
  *   workspace  device scratch of ordermoe_cache_evict_workspace_bytes(seqs, heads, budget) bytes, 256-byte
  *            aligned (for budgets above seq_pages * page that of seq_pages * page is enough: one of that size serves every
  *            budget); calls that may overlap on the GPU need one each

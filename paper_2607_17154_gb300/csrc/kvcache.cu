@@ -694,8 +694,13 @@ extern "C" int ordermoe_cache_evict(const ordermoe_cache* cache, int budget, int
   if (!cache->mass || !length_out) return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: null pointer (mass or length_out)");
   if (recent > 0 && cache->pos && !newest)
     return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: recent positions need a pointer to the newest ones");
-  if (length_out == cache->length)
-    return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: length_out may not be the cache's length");
+  // every head's CTA reads them, and one of them writes the new length
+  auto meets = [&](const int32_t* p) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(length_out), b = reinterpret_cast<uintptr_t>(p);
+    return p && (a < b ? b - a : a - b) < static_cast<uintptr_t>(cache->seqs) * 4;
+  };
+  if (meets(cache->length) || meets(newest))
+    return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: length_out may overlap neither the cache's length nor newest");
   if (reinterpret_cast<uintptr_t>(newest) % 4 || reinterpret_cast<uintptr_t>(length_out) % 4)
     return fail(ORDERMOE_ERR_INVALID_ARG, "cache_evict: newest or length_out is not aligned to its type");
   const int64_t cap = static_cast<int64_t>(cache->seq_pages) * cache->page;  // with a budget of as many nothing moves

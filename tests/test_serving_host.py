@@ -154,3 +154,12 @@ def test_a_budget_above_the_slots_asks_for_the_slots_workspace():
     for budget in (slots, slots + 1, 1 << 30):
         rc, msg = evict(c, budget=budget, nbytes=need - 1)
         assert rc == ARG and "workspace" in msg
+
+
+@pytest.mark.parametrize("at", [AT, AT + 4, AT + 8, AT - 8])
+def test_evict_refuses_new_lengths_over_what_it_reads(at):
+    """Three sequences: any of the twelve bytes of length, or of newest."""
+    far = AT * 4
+    for over in (dict(newest=far), dict(c=cache(length=far))):
+        rc, msg = evict(out=at, **over)
+        assert rc == ARG and "overlap" in msg, (over, rc, msg)
