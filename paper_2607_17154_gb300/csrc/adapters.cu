@@ -768,8 +768,9 @@ __global__ void __launch_bounds__(up_threads(PARTS, RANKS, FEW), up_pairs(PARTS,
 
 // Into how many parts K may go: two CTAs an SM with the tiles (less where a tile turns out to have many adapters, see
 // tile_split); four steps each at least. (4096 tokens on 8 adapters, K 4096, N 14336, R 64, both kernels:
-// one CTA an SM 105 us, two 93.)
-constexpr int SMS = 152;
+// one CTA an SM 105 us, two 93.) By a GB300's SMs whatever the device has: workspaces and the most parts of a sum are
+// the same on all. Grids go by the device's own.
+constexpr int SPLIT_SMS = 152;
 struct Plan {
   int tiles, split;
 };
@@ -778,7 +779,7 @@ static Plan plan(int T, int K, int R, int n) {
   Plan p{};
   p.tiles = T / TILE + (T % TILE != 0);
   const int steps = (K + KB - 1) / KB;
-  int want = 2 * SMS / p.tiles;
+  int want = 2 * SPLIT_SMS / p.tiles;
   if (n > 0) {
     const int tokens = T < TILE ? T : TILE, distinct = p.tiles > 4 ? 1 : tokens < n ? tokens : n;
     // A step costs a CTA about what one more partial sum of 128 tokens and 64 ranks costs each CTA of the second
@@ -886,7 +887,7 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   // many a CTA takes a tile's adapters in turn (one that finds no adapter costs 1.5 us of its SM).
   const int64_t tokens = T < ad::TILE ? T : ad::TILE, distinct = tokens < n ? tokens : n;
   const bool low = a.ranks <= 64;
-  const int64_t room = p.tiles < 2 * ad::SMS ? 2 * ad::SMS / p.tiles : 1;
+  const int64_t sms = num_sms(), room = p.tiles < 2 * sms ? 2 * sms / p.tiles : 1;
   auto at_most = [](int64_t v, int64_t most) { return static_cast<unsigned>(v < 1 ? 1 : v < most ? v : most); };
   a.ctas = static_cast<int>(at_most(room, distinct * p.split));
   OM_LAUNCH_PDL("adapters_down_kernel", ad::adapters_down_kernel, dim3(p.tiles, a.ctas), dim3(ad::THREADS),
@@ -896,7 +897,7 @@ extern "C" int ordermoe_adapters(const uint16_t* X, int64_t ldx, const uint16_t*
   // adapter's tokens mostly follow one another, up to 8 (4096 tokens, N 14336, 8 adapters in runs of 512: 85 us by the
   // form for few, 79 by the other; 2072 tokens, N 9512, 25 adapters in runs of 7: 71 and 119)
   const bool few = tokens <= (p.tiles > 4 ? 8 : 16) * distinct;
-  const int64_t ctas = (ad::up_pairs(parts, low ? 64 : ad::MAX_R) ? 2 : 1) * ad::SMS;
+  const int64_t ctas = (ad::up_pairs(parts, low ? 64 : ad::MAX_R) ? 2 : 1) * sms;
   const int64_t slices = (static_cast<int64_t>(N) + ad::NB - 1) / ad::NB, mine = ctas / p.tiles;
   // Slices of a CTA where the tiles share the CTAs evenly, and where all tiles' slices do: then most CTAs meet two tiles
   // and sum up H twice, which costs as much as 1.5 slices (32 tiles, N 14336, R 64, 304 CTAs: 13 slices 82 us, 11.8 90).

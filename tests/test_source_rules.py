@@ -75,3 +75,15 @@ def test_limits_of_shared_memory_are_set_once_per_device():
             calls += [text[text.rindex("\n}", 0, m.start()):m.start()]
                       for m in re.finditer(helper + r"(<[^>]*>)?\(\)(?! \{)", text)]
         assert calls and all("per_device(" in c for c in calls), helper
+
+
+@pytest.mark.parametrize("name", ["adapters", "attention", "kvcache"])
+def test_grids_go_by_the_devices_own_sms(name):
+    """A number of SMs that is written down may bound a workspace; what launches asks the device."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name + ".cu")).read())
+    fixed = re.findall(r"constexpr int (\w*SMS)\b", text)
+    launches = [m.start() for m in re.finditer(r"OM_LAUNCH_PDL\(", text)]
+    for at in launches:
+        function = text[text.rindex("\n}", 0, at):text.index("\n}", at)]
+        assert not any(re.search(r"\b%s\b" % f, function) for f in fixed), (name, function[:80])
+    assert launches and "num_sms()" in text
