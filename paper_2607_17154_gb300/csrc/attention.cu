@@ -4,8 +4,9 @@
 // of the cache is used G times, so HBM bounds it (2 G operations a byte; from about 100 the tensor cores would). The
 // slots of all sequences and heads, cut into units of 16, form one list that is shared out evenly over the warps of a grid
 // of one CTA an SM, by the lengths on the device; a warp runs through its part with a running maximum and sum and a ring of
-// its own in shared memory, filled two units ahead by 16-byte asynchronous copies (128 KB on their way an SM). Rows that
-// warps of one CTA share are joined there, rows that CTAs share by a second kernel, in the order of their slots.
+// its own in shared memory, filled STAGES - 1 units ahead by 16-byte asynchronous copies (two for heads of
+// 128 and 256, five for 64: 128 KB on their way an SM, 160 for 64). Rows that warps of one CTA share are joined there, rows
+// that CTAs share by a second kernel, in the order of their slots.
 // Measured (launched from the host, 32 / 8 heads of 128): one sequence of 131071 slots 88 us = 6.1 TB/s, 0.91 of the measured
 // rate; 128 sequences of 1 to 8191 slots 334 us = 6.4 TB/s, 0.95; with a partial result a warp and one join for all of them
 // 143 and 386. 17 sequences of up to 4097 slots, 16 heads of 128, weights kept: 65 us, floor 43 (attention 50, the two
@@ -84,13 +85,6 @@ __device__ __forceinline__ int count_units(const Args& a, Units<NT>& u) {
   if (tid == NT - 1) u.before[NT] = base + upto;
   __syncthreads();
   return per;
-}
-// Units of the sequences before s.
-template <int NT>
-__device__ __forceinline__ long long units_before(const Args& a, const Units<NT>& u, int per, int s) {
-  long long b = u.before[s / per];
-  for (int i = s / per * per; i < s; ++i) b += units_of(a, i);
-  return b;
 }
 
 // The list is cut into W parts, one a warp: part w has the units [w U / W, (w + 1) U / W). A CTA has the next
