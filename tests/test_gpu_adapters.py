@@ -263,3 +263,17 @@ def test_inputs_written_by_the_kernels_before():
     for _ in range(4):
         for a, b in zip(steps(lambda: None), want):
             assert torch.equal(a, b)
+
+
+def test_on_another_stream():
+    T, K, N, R, n = 130, 256, 320, 16, 4
+    g = gen(15)
+    X, A, Bw, res = rnd(g, T, K), rnd(g, n, R, K, std=0.05), rnd(g, n, N, R, std=0.1), rnd(g, T, N)
+    ids = torch.randint(-1, n, (T,), dtype=torch.int32, device=DEV, generator=g)
+    ws = torch.empty(B.ordermoe_adapters_workspace_bytes(T, K, N, R), dtype=torch.uint8, device=DEV)
+    Y, want, s = torch.zeros(T, N, dtype=BF16, device=DEV), torch.zeros(T, N, dtype=BF16, device=DEV), torch.cuda.Stream()
+    check(X, A, Bw, ids, want, residual=res)
+    s.wait_stream(torch.cuda.current_stream())
+    B.ordermoe_adapters(X, A, Bw, ids, Y, ws, residual=res, stream=s)
+    s.synchronize()
+    assert torch.equal(Y, want)

@@ -836,3 +836,113 @@ def test_values_behind_scores_of_minus_infinity_alone_say_nothing(lens, H, bad):
     out, lse = attend(cache, q, 2 * H, weights=True)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
     assert torch.equal(cache._keep[4], before)
+
+
+BORDERS = [([70001], 32, 8, 128, 16), ([40000], 8, 1, 64, 64), ([20000, 3, 0], 8, 4, 256, 32), ([3, 9000, 0, 1, 4097, 12], 16, 1, 128, 16),
+           ([480, 495], 33, 1, 128, 8), ([1200 - i for i in range(40)], 32, 8, 128, 16), ([2000, 17], 9, 1, 256, 4), ([5000], 40, 2, 128, 16)]
+
+
+@pytest.mark.parametrize("steps", [False, True])
+@pytest.mark.parametrize("lens,hq,H,D,page", BORDERS)
+def test_every_unit_of_slots_counts_once(lens, hq, H, D, page, steps):
+    """One slot of each unit of 16 holds the value 1 in a column of its own, all others are 0: a unit that is lost or
+    counted twice between warps and CTAs changes an output from p to 0 or 2 p. Keys are equal, or (steps) their scores are
+    integers in powers of two that rise and fall from unit to unit, so that partial results are joined with other maxima.
+
+    Equal keys: x = 0 and all sums are whole numbers, so p = 1 / n is off by a division (2^-24) and out by its rounding (2^-8);
+    lse = log2f(n) ln 2 by 2^-22 of itself (log2f 1 ulp, the constant and the product half each), less than a slot more or
+    less would change it. Steps: x up to 6, off by 2^-20 (the scale's roundings, 6 * 2^-23), exp2f 2^-22, and sums of at most 2^9 terms
+    after one another (units of a warp, warps, CTAs), 2^-15: less than 2^-14 together."""
+    cache = make(lens, H, D, page, seed=90)
+    k, v = cache._keep[:2]
+    places = held(cache, lens)
+    q = torch.zeros(len(lens), hq * D, dtype=BF16, device=DEV)
+    level = []
+    for (at, row), n in zip(places, lens):
+        unit = torch.arange(n, device=DEV) // 16
+        e = torch.where(unit // 5 % 2 == 0, unit // 3 % 7, 6 - unit % 7) if steps else 0 * unit
+        level.append(e.double())
+        k[at, :, row] = 0
+        k[at, :, row, 0] = e.to(BF16)[:, None]
+        v[at, :, row] = 0
+    q.view(-1, hq, D)[:, :, 0] = 1
+    total = [float((2.0 ** e).sum()) for e in level]
+    lse_far = 2.0 ** -14 if steps else 0.0
+    far = 2.0 ** -8 + (2.0 ** -14 if steps else 2.0 ** -23)
+    ws, empty = workspace(cache, hq), v.clone()
+    for turn in range((max(lens) + 16 * D - 1) // (16 * D)):  # D units of every sequence at a time
+        want = torch.zeros(len(lens), D, dtype=torch.double, device=DEV)
+        v.copy_(empty)
+        for s, ((at, row), n) in enumerate(zip(places, lens)):
+            unit = torch.arange((n + 15) // 16, device=DEV)[turn * D:(turn + 1) * D]
+            slot = (unit * 16 + (unit * 7 + turn) % 16).clamp(max=n - 1)
+            v[at[slot], :, row[slot], unit - turn * D] = 1
+            want[s, unit - turn * D] = 2.0 ** level[s][slot] / max(total[s], 1.0)
+        out, lse = attend(cache, q, hq, scale=math.log(2.0), ws=ws)
+        off = (out.double().view(-1, hq, D) - want[:, None]).abs()
+        assert bool((off <= want[:, None] * far).all()), float((off / want[:, None]).nan_to_num().max())
+        for s, t in enumerate(total):
+            if lens[s] == 0:
+                assert bool((lse[s] == -math.inf).all())
+            else:
+                assert bool(((lse[s].double() - math.log(t)).abs() <= math.log(t) * 2.0 ** -22 + lse_far).all())
+
+
+@pytest.mark.parametrize("lens,hq,H,D,page", [b for b in BORDERS if max(b[0]) < 10000])
+def test_every_slot_has_its_weight(lens, hq, H, D, page):
+    """Equal keys: each slot of a sequence gets 1 / n (off by 2^-24) from every query head of the group, whose sum is off by
+    2^-24 a head."""
+    cache = make(lens, H, D, page, seed=91, weights=True)
+    mass = cache._keep[4].zero_()
+    q = torch.zeros(len(lens), hq * D, dtype=BF16, device=DEV)
+    attend(cache, q, hq, weights=True)
+    for s, n in enumerate(lens):
+        want = hq // H / max(n, 1)
+        assert bool(((mass[s, :, :n].double() - want).abs() <= want * (hq // H + 2) * 2.0 ** -24).all())
+        assert bool((mass[s, :, n:] == 0).all())
+
+
+@pytest.mark.parametrize("S", [129, 300, 1024, 1500])
+def test_append_to_many_sequences(S):
+    """Sequences without new tokens at the beginning, in runs and at the end; rows of padding behind the last token."""
+    H, D, page, pad = 1, 64, 8, 7
+    new = [0 if i < 9 or i >= S - 11 or i // 6 % 3 == 1 else 1 + i % 3 for i in range(S)]
+    past = [i * 5 % 14 for i in range(S)]
+    T = sum(new)
+    cache = make([a + b for a, b in zip(past, new)], H, D, page, seed=93, extra=0, weights=True, fill=0.25)
+    k, v, table, length, mass, pos = cache._keep
+    nk, nv, q = (torch.randn(T + pad, n * D, device=DEV, generator=gen(94 + n)).to(BF16) for n in (H, H, 2 * H))
+    starts = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).int().to(DEV)
+    position = torch.arange(T + pad, dtype=torch.int32, device=DEV) + 100
+    want = [x.clone() for x in (k, v, mass, pos)]
+    seq = torch.repeat_interleave(torch.arange(S), torch.tensor(new)).to(DEV)
+    t = torch.arange(T, device=DEV)
+    slot = torch.tensor(past, device=DEV)[seq] + t - starts.long()[seq]
+    at = table.long()[seq, slot // page]
+    want[0][at, :, slot % page] = nk[:T].view(T, H, D)
+    want[1][at, :, slot % page] = nv[:T].view(T, H, D)
+    want[2][seq, :, slot] = 0
+    want[3][seq, :, slot] = position[:T, None]
+    q_out = torch.full_like(q, 9.0)
+    B.ordermoe_cache_append(cache, nk, nv, q=q, q_out=q_out, starts=starts, position=position)
+    for got, w in zip((k, v, mass, pos), want):
+        assert torch.equal(got, w)
+    assert torch.equal(q_out[:T], q[:T]) and bool((q_out[T:] == 9.0).all())
+
+
+def test_append_and_cut_on_another_stream():
+    H, D, budget = 2, 64, 40
+    nk, nv = (torch.randn(3, H * D, device=DEV, generator=gen(95 + i)).to(BF16) for i in range(2))
+    results = []
+    for s in (None, torch.cuda.Stream()):
+        cache = make([90, 17, 41], H, D, 16, seed=97, weights=True, fill=0.5)
+        out = torch.zeros_like(cache._keep[3])
+        ws = torch.empty(B.ordermoe_cache_evict_workspace_bytes(cache, budget), dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        B.ordermoe_cache_append(cache, nk, nv, stream=s)
+        B.ordermoe_cache_evict(cache, budget, out, ws, stream=s)
+        torch.cuda.synchronize()
+        results.append([x.clone() for x in cache._keep] + [out])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert results[0][-1].tolist() == [40, 17, 40]
