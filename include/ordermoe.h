@@ -293,7 +293,8 @@ int ordermoe_selftest_linear_plan(int M, int N, int K, int f32, const int32_t* d
  *           power of two, at most 1024; at most 1024 heads
  *   table   [seqs][seq_pages] i32, rows ld_table apart: slot i of sequence s is row i % page of page
  *           table[s][i / page]. Entries behind a sequence's length are not read. At most 65535 sequences,
- *           2^30 slots each
+ *           2^30 slots each. seq_pages decides which kernels run (lengths are on the device): short sequences are faster in
+ *           a table that reaches no further than they can
  *   length  [seqs] i32 slots held, each 0 to seq_pages * page
  *   mass    [seqs][heads][seq_pages * page] f32, nullable: the weight that a slot has received
  *   pos     the same shape, i32, nullable: the position of a slot's token (slots need not be in the order of
@@ -340,6 +341,7 @@ int ordermoe_cache_append(const ordermoe_cache* cache, const uint16_t* k, int64_
  *   x_i = scale <q_j, k_i>, i < length;  out_j = sum_i p_i v_i, p = softmax(x);  lse_j = log sum_i exp(x_i).
  *   q, out   [seqs][q_heads * dim] bf16, rows ldq, ldo apart (multiples of 8, 16-byte aligned bases); q_heads is a
  *            multiple of heads. out may be q itself (same stride)
+ *   scale    > 0, at most 1e30
  *   lse      [seqs][q_heads] f32, nullable
  *   weights  != 0: mass[s][h][i] += the sum of p_i over the query heads of head h
  *   workspace  device scratch of ordermoe_attention_paged_workspace_bytes(...) bytes, 256-byte aligned, not to be

@@ -249,7 +249,8 @@ __device__ __forceinline__ int block_before(int v, int* warp_sums, int* total) {
 // no further. Rows of up to KEYS * NT slots have their keys in registers, key i in thread i % NT; longer ones in
 // shared memory, or beyond that they are read again a round. Once the keys that a candidate can still part are one a
 // thread at most, they alone are counted. (64 rows of 1500 to 16383 slots: 21 us, most of it instructions of 64 SMs, and 21 for
-// the moves behind it, 100000 rows of 2 x 256 bytes; 256 rows of 1025 slots with their one move each: 10.3 us.)
+// the moves behind it, 100000 rows of 2 x 256 bytes; 256 rows of 1025 slots with their one move each: 10.3 us. 8 rows cut to
+// 4096, both launches: of 16384 slots 27 us, of 32768 in shared memory 68, of 65536 and 131072 read again 345 and 658.)
 constexpr int KEYS = 16;
 template <int NT>
 struct Select {
