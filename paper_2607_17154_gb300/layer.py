@@ -423,13 +423,15 @@ class LayerStack:
     def _capture(self, body, prologue):
         s = torch.cuda.Stream(device=self.scratch.device)
         s.wait_stream(torch.cuda.current_stream(self.scratch.device))
-        with torch.cuda.stream(s):  # one eager step first: per-device set-up outside the capture
-            with self._empty_caches() as empty:
+        try:
+            # one eager step first: per-device set-up outside the capture
+            with torch.cuda.stream(s), self._empty_caches() as empty:
                 if prologue is not None:
                     prologue()
                 empty()
                 body(s)
-        torch.cuda.current_stream(self.scratch.device).wait_stream(s)
+        finally:
+            torch.cuda.current_stream(self.scratch.device).wait_stream(s)
         torch.cuda.synchronize(self.scratch.device)
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g, stream=s):

@@ -946,3 +946,28 @@ def test_append_and_cut_on_another_stream():
     for a, b in zip(*results):
         assert torch.equal(a, b)
     assert results[0][-1].tolist() == [40, 17, 40]
+
+
+def test_a_capture_that_raises_leaves_the_caches_as_they_are():
+    S, slots = 3, 16
+    caches, stack, hs, xs = attention_stack(S, slots, 102)
+    home = torch.zeros(S, dtype=torch.uint8, device=DEV)
+    for i in range(4):
+        hs[0].copy_(torch.randn(S, 256, device=DEV, generator=gen(150 + i)).to(BF16))
+        caches[0].advance()
+        stack.step_residual(hs, xs, home, None, None)
+    before = state(caches)
+
+    def prologue():
+        caches[0].advance()
+        raise KeyError("no such request")
+
+    with pytest.raises(KeyError):
+        stack.capture_residual(hs, xs, home, None, None, prologue=prologue)
+    for a, b in zip(state(caches), before):
+        assert torch.equal(a, b)
+    wrong = [torch.zeros(S + 1, 256, dtype=BF16, device=DEV) for _ in range(4)]  # refused within the step
+    with pytest.raises(ValueError):
+        stack.capture_residual(wrong, [w.clone() for w in wrong], home, None, None, prologue=caches[0].advance)
+    for a, b in zip(state(caches), before):
+        assert torch.equal(a, b)
